@@ -479,6 +479,89 @@ pp_status pp_round_bf16(const float* src, uint16_t* dst, size_t count);
 const char* pp_status_str(pp_status s);
 const char* pp_last_error(void);
 
+/* ------------------------------------------------------------------------
+ * Training operators.  Structured pruning alternates training steps with the
+ * projections above (Sec. 2: min f(W) subject to W_i in S_i); these are the
+ * loss with its gradient of a network's linear head, and the weight step.
+ * Conventions as above: caller-owned device buffers, caller's stream, no
+ * synchronisation, no allocation, fixed summation orders (repeated calls are
+ * bitwise identical).  All can be recorded into a HIP graph.
+ * ---------------------------------------------------------------------- */
+
+enum { PP_MEAN = 0, PP_SUM = 1, PP_NONE = 2 };           /* pp_xent_desc.reduction */
+enum { PP_XENT_FWD = 1, PP_XENT_BWD = 2 };               /* parts of pp_xent_workspace */
+
+/*
+ * Softmax cross entropy of a linear head (a 1x1 convolution with v output
+ * channels, or a fully connected layer: hw = 1).  Token t = (i, p), i < n,
+ * p < hw, has features x[t][c] at x + i x_sn + c x_sc + p x_sp (strides in
+ * elements; channels first, channels last and token rows are all such
+ * layouts), and
+ *   l[t][j] = sum_c x[t][c] w[j][c] + bias[j]
+ *   lse[t]  = log sum_j exp l[t][j]
+ *   loss[t] = class_weight[y] (lse[t] - l[t][y]),  y = target[t]
+ * PP_SUM sums loss over the tokens, PP_MEAN divides that by the sum of
+ * class_weight[y] (a mean over no token is 0), PP_NONE stores each.  A token
+ * whose target is ignore_index contributes nothing to the loss or to any
+ * gradient, whatever its features hold; its dx is 0 (NaN where the incoming
+ * gradient or the mean's divisor is not finite).  A token whose target is
+ * neither ignore_index nor in 0..v-1 makes the loss (PP_NONE: its own) and the
+ * gradients it reaches NaN.  A class whose logits are -inf (a bias of -inf)
+ * has probability 0; a token all of whose logits are -inf has loss NaN.
+ * The logits are accumulated in fp32 and are neither rounded nor stored; fp32
+ * features are multiplied as sums of three bf16 values each (24 bits).
+ */
+typedef struct {
+  int32_t dtype;                       /* pp_dtype of x, w, dx and dw                 */
+  int32_t reduction;                   /* PP_MEAN, PP_SUM or PP_NONE                  */
+  int64_t n, d, hw, v;                 /* images, features, pixels of each, classes   */
+  int64_t x_sn, x_sc, x_sp;            /* strides of x                                */
+  int64_t dx_sn, dx_sc, dx_sp;         /* strides of dx (elements must not overlap)   */
+  int64_t w_ld;                        /* elements from one class of w to the next    */
+  int64_t ignore_index;
+} pp_xent_desc;
+
+/*
+ * pp_xent_workspace -- device bytes a call needs (parts: PP_XENT_FWD for
+ * pp_xent_fwd, PP_XENT_BWD for pp_xent_bwd, both for pp_xent_step), which do
+ * not grow with v times the tokens beyond about 0.3 GB.  Host-only.
+ *
+ * pp_xent_fwd -- the loss, and the statistics pp_xent_bwd needs.
+ *   x, w          device [n][d][hw] (by strides) and [v][d] (rows w_ld apart)
+ *   bias          device fp32 [v], or NULL
+ *   class_weight  device fp32 [v], or NULL for ones
+ *   target        device int64 [n][hw]
+ *   loss          device fp32: one value, or [n][hw] with PP_NONE
+ *   stats         device fp32 [n hw + 1]: lse of each token (0 where ignored),
+ *                 then what PP_MEAN divides by (1 for PP_SUM and PP_NONE, and
+ *                 for a mean over no token)
+ *   workspace     256-byte aligned
+ * pp_xent_bwd -- the gradients of sum_t grad[t] loss[t] (PP_NONE), or of
+ * grad[0] loss; stats as pp_xent_fwd left it for the same inputs.
+ *   grad          device fp32: [n][hw] with PP_NONE, else one value; NULL: ones
+ *   dx, dw, db    device: dx as x, by its own strides; dw [v][d] contiguous; db
+ *                 fp32 [v].  Any of them may be NULL: not computed
+ * pp_xent_step -- both in one call, sharing what they prepare of x and w.
+ *
+ * The backward pass rounds the logits' gradient to bf16 (bf16 features) or to
+ * 24 bits (fp32) for the products with w and x, and sums in fp32.
+ * n hw = 0 is a loss of 0 and zero gradients.
+ * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, reduction, dtype,
+ * negative strides), PP_EUNSUPPORTED (d, v or the tokens 2^22 - 64 or more),
+ * PP_ESIZE (workspace too small), PP_EHIP.
+ */
+pp_status pp_xent_workspace(const pp_xent_desc* desc, int32_t parts, size_t* bytes);
+pp_status pp_xent_fwd(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,
+                      const float* class_weight, const int64_t* target, float* loss, float* stats,
+                      void* workspace, size_t ws_bytes, void* hip_stream);
+pp_status pp_xent_bwd(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,
+                      const float* class_weight, const int64_t* target, const float* stats, const float* grad,
+                      void* dx, void* dw, float* db, void* workspace, size_t ws_bytes, void* hip_stream);
+pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,
+                       const float* class_weight, const int64_t* target, const float* grad, float* loss,
+                       float* stats, void* dx, void* dw, float* db, void* workspace, size_t ws_bytes,
+                       void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

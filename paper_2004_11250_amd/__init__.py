@@ -35,7 +35,8 @@ SYMBOLS = ("pp_pack", "pp_blob_info", "pp_conv2d_fwd", "pp_conv2d_workspace", "p
            "pp_conv2d_out_size", "pp_net_workspace", "pp_net_fwd", "pp_status_str", "pp_last_error",
            "pp_project_patterns", "pp_project_connectivity", "pp_project_columns", "pp_column_library",
            "pp_fold_bn", "pp_jit_library", "pp_conv2d_fwd_noalloc", "pp_net_plan", "pp_round_bf16",
-           "pp_conv2d_prepare", "pp_conv2d_fwd_prepared", "pp_conv2d_scratch")
+           "pp_conv2d_prepare", "pp_conv2d_fwd_prepared", "pp_conv2d_scratch",
+           "pp_xent_workspace", "pp_xent_fwd", "pp_xent_bwd", "pp_xent_step")
 
 
 class PPError(RuntimeError):
@@ -103,6 +104,7 @@ def load_library(path: str = LIB_PATH):
             fn = getattr(lib, name)
             fn.argtypes = at
             fn.restype = ctypes.c_char_p if name in ("pp_status_str", "pp_last_error") else i32
+    train.bind(lib)
     _lib = lib
     return lib
 
@@ -619,3 +621,7 @@ class Net:
         with torch.cuda.graph(graph):
             self.forward(x, out, workspace)
         return graph
+
+
+from . import train   # noqa: E402  (uses the helpers above)
+from .train import linear_xent_bwd, linear_xent_fwd, linear_xent_step   # noqa: E402,F401

@@ -1,0 +1,208 @@
+// gemm_nt.hpp -- the matrix-core product the training operators are built on:
+//
+//   acc[r][c] = sum over plane pairs (p, q), sum over k of A_p[r][k] B_q[c][k]
+//
+// with both operands stored with k contiguous.  16-bit operands multiply at
+// the full matrix-core rate; an operand that needs more bits than one 16-bit
+// value holds is stored as a sum of two or three such values ("planes", the
+// first the rounded value, the next the rounded rest), and the product is the
+// sum of the plane products that matter, taken one after the other along a
+// longer k into the same fp32 accumulators.
+//
+// A workgroup of WM x WN waves owns a BM x BN tile and walks k in steps of 64.
+// A step's operands go from global memory straight into LDS (16 bytes a lane;
+// no registers), one step ahead of the products; two LDS buffers, one barrier
+// a step.  A row of 64 values is 128 bytes, the whole of the LDS banks, so the
+// 16-byte pieces of row r are stored at piece position p ^ (r & 7): the eight
+// rows that a quarter of a wave reads at once then lie in different banks.
+// The permutation is applied to the global address, since the LDS side of the
+// DMA is fixed (lane after lane).  Rows past the operand's end are read
+// through an offset outside the descriptor's range, which gives zeros.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace pp {
+
+using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+using u32x4_t = __attribute__((ext_vector_type(4))) uint32_t;
+
+constexpr int kBK = 64;              // k per step; operands are padded with zeros to a multiple of it
+constexpr int kMaxPlanes = 3;
+constexpr int64_t kMaxLd = 1 << 22;  // row pitch limit: a tile's rows stay within 31-bit byte offsets
+
+// one operand: up to three planes of [rows][ld], k contiguous, 16-byte aligned
+// rows
+struct GemmOperand {
+  const void* plane[kMaxPlanes];
+  int64_t ld;
+  int32_t rows;
+};
+
+// Which planes are multiplied, in order (the smallest products first, so that
+// they are added while the sum is small): two bits of A's plane, two of B's.
+struct PlanePairs {
+  uint32_t code;
+  int32_t n;
+};
+constexpr uint32_t plane_pair(int p, int q, int i) { return static_cast<uint32_t>(p | q << 2) << (4 * i); }
+// one plane each: 16-bit operands
+constexpr PlanePairs kPairs1 = {plane_pair(0, 0, 0), 1};
+// two planes of A, one of B
+constexpr PlanePairs kPairs2 = {plane_pair(1, 0, 0) | plane_pair(0, 0, 1), 2};
+// two planes each; what is left out is the product of the two rests
+constexpr PlanePairs kPairs3 = {plane_pair(1, 0, 0) | plane_pair(0, 1, 1) | plane_pair(0, 0, 2), 3};
+// three bf16 planes each hold all 24 bits of an fp32 value; what is left out
+// is 2^-24 of the product and less
+constexpr PlanePairs kPairs6 = {plane_pair(2, 0, 0) | plane_pair(0, 2, 1) | plane_pair(1, 1, 2) | plane_pair(1, 0, 3) |
+                                    plane_pair(0, 1, 4) | plane_pair(0, 0, 5), 6};
+
+template <class T>
+struct Mfma;
+template <>
+struct Mfma<__bf16> {
+  using Frag = bf16x8;
+  static __device__ __forceinline__ f32x4 mul(Frag a, Frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mfma<_Float16> {
+  using Frag = f16x8;
+  static __device__ __forceinline__ f32x4 mul(Frag a, Frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+  }
+};
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+// 16 bytes a lane from base + voff + soff to LDS byte lds + 16 lane.  As
+// assembly: the compiler would otherwise wait for every DMA in flight before
+// any LDS read that follows.
+__device__ __forceinline__ void gemm_dma(u32x4_t rsrc, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff), "s"(rsrc), "s"(lds)
+               : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// the wave's DMAs have landed and its LDS reads are done; then all waves meet
+__device__ __forceinline__ void gemm_sync() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <class T, int BM_, int BN_, int WM_, int WN_>
+struct GemmTile {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int NW = WM * WN, THREADS = NW * 64;
+  static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
+  static constexpr int FM = TM / 16, FN = TN / 16;      // in 16 x 16 blocks
+  static constexpr int QA = BM / (8 * NW), QB = BN / (8 * NW);   // DMAs a wave issues for a step
+  static constexpr uint32_t LDS_A = BM * kBK * 2, LDS_STEP = (BM + BN) * kBK * 2;
+  static constexpr uint32_t LDS_BYTES = 2 * LDS_STEP;
+  static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 16 == 0 && TN % 16 == 0, "tile");
+
+  // Row and column of acc[i][j][e] in the tile.  A lane holds four rows that
+  // follow each other of one column.
+  static __device__ __forceinline__ int row_of(int i) { return (wave() / WN) * TM + 16 * i + (lane() >> 4) * 4; }
+  static __device__ __forceinline__ int col_of(int j) { return (wave() % WN) * TN + 16 * j + (lane() & 15); }
+  static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
+  static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+  // steps [s0, s1) of the flattened (plane pair, k step) range; ksteps k steps
+  // a pair.  k0: first k (a multiple of 8).  lds: LDS_BYTES of shared memory.
+  static __device__ __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0,
+                                             int col0, int ksteps, int64_t k0, int s0, int s1, uint8_t* lds,
+                                             f32x4 (&acc)[FM][FN]) {
+    using Frag = typename Mfma<T>::Frag;
+    const int ln = lane(), wv = wave();
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // per-lane offsets of the DMAs: row 8 (NW i + wave) + lane / 8 of the tile
+    uint32_t va[QA], vb[QB];
+    const uint32_t piece = static_cast<uint32_t>((ln & 7) ^ (ln >> 3)) * 16u;
+#pragma unroll
+    for (int i = 0; i < QA; ++i) {
+      const int r = 8 * (NW * i + wv) + (ln >> 3);
+      va[i] = row0 + r < A.rows ? static_cast<uint32_t>(r * static_cast<int>(A.ld) * 2) + piece : 0x80000000u;
+    }
+#pragma unroll
+    for (int i = 0; i < QB; ++i) {
+      const int r = 8 * (NW * i + wv) + (ln >> 3);
+      vb[i] = col0 + r < B.rows ? static_cast<uint32_t>(r * static_cast<int>(B.ld) * 2) + piece : 0x80000000u;
+    }
+    const int64_t offa = (static_cast<int64_t>(row0) * A.ld + k0) * 2, offb = (static_cast<int64_t>(col0) * B.ld + k0) * 2;
+    int pair = s0 / ksteps, kk = s0 - pair * ksteps;
+
+    auto rsrc = [](const void* p, int64_t off) {
+      const uint64_t b = reinterpret_cast<uint64_t>(p) + off;
+      u32x4_t r;
+      r.x = static_cast<uint32_t>(b);
+      r.y = static_cast<uint32_t>(b >> 32) & 0xFFFFu;
+      r.z = 0x7FFFFFFFu;
+      r.w = 0x00020000u;
+      return r;
+    };
+    auto fetch = [&](uint32_t buf) {
+      const uint32_t c = pairs.code >> (4 * pair);
+      const int64_t ko = static_cast<int64_t>(kk) * (kBK * 2);
+      const u32x4_t ra = rsrc(A.plane[c & 3], offa + ko), rb = rsrc(B.plane[c >> 2 & 3], offb + ko);
+#pragma unroll
+      for (int i = 0; i < QA; ++i) gemm_dma(ra, va[i], buf + 1024u * (NW * i + wv));
+#pragma unroll
+      for (int i = 0; i < QB; ++i) gemm_dma(rb, vb[i], buf + LDS_A + 1024u * (NW * i + wv));
+      if (++kk == ksteps) kk = 0, ++pair;
+    };
+
+    // a lane's operand of block i, k half h: row 16 i + lane % 16, piece 4 h + lane / 16
+    const uint32_t ar = static_cast<uint32_t>((wv / WN) * TM + (ln & 15)) * 128u;
+    const uint32_t br = LDS_A + static_cast<uint32_t>((wv % WN) * TN + (ln & 15)) * 128u;
+    const uint32_t p0 = static_cast<uint32_t>((ln >> 4) ^ (ln & 7)) * 16u;
+
+    if (s0 >= s1) return;
+    fetch(lds0);
+    uint32_t cur = 0;
+    for (int s = s0; s < s1; ++s) {
+      gemm_sync();
+      if (s + 1 < s1) fetch(lds0 + (LDS_STEP - cur));
+      const uint8_t* base = lds + cur;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t p = p0 ^ (h * 64u);
+        Frag a[FM], b[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) b[j] = *reinterpret_cast<const Frag*>(base + br + j * 2048u + p);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) a[i] = *reinterpret_cast<const Frag*>(base + ar + i * 2048u + p);
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
+      }
+      cur = LDS_STEP - cur;
+    }
+  }
+};
+
+// Workgroups are dealt to the eight XCDs in turn, each with an L2 of its own:
+// consecutive logical tiles are put on one XCD.
+__device__ __forceinline__ int xcd_order(int id, int n) {
+  const int q = n >> 3, r = n & 7, x = id & 7;
+  return x * q + (x < r ? x : r) + (id >> 3);
+}
+
+// Tile t of a tm x tn grid, in bands of eight rows walked column by column, so
+// that tiles that run together share operand rows of both sides.
+__device__ __forceinline__ void band_order(int t, int tm, int tn, int* ti, int* tj) {
+  constexpr int kBand = 8;
+  const int per = kBand * tn, band = t / per, first = band * kBand;
+  const int h = tm - first < kBand ? tm - first : kBand, in = t - band * per;
+  *ti = first + in % h;
+  *tj = in / h;
+}
+
+}  // namespace pp

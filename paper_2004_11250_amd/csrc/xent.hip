@@ -1,0 +1,799 @@
+// xent.hip -- pp_xent_fwd / pp_xent_bwd / pp_xent_step: softmax cross entropy
+// of a linear (1x1) head over a large number of classes, with its gradient,
+// without keeping the logits.
+//
+//   l[t][v] = x[t] . w[v] + b[v],  lse[t] = log sum_v exp l[t][v]
+//   loss[t] = c[y] (lse[t] - l[t][y]),            y = target[t]
+//   G[t][v] = c[y] g[t] (exp(l[t][v] - lse[t]) - [v = y])
+//   dx = a G w,  dw = a G^T x,  db = a sum_t G,  a = (incoming gradient) / divisor
+//
+// Forward: the logits are a product on the matrix cores whose tiles never
+// leave the registers: each wave reduces its tile to a maximum and a sum of
+// exponentials per token (a few bytes per token and 64 to 128 classes), and a
+// second kernel joins those.  Backward: the logits are computed again, a
+// piece of the classes at a time, turned into G in the epilogue (the logits
+// themselves are not rounded), rounded to the operands' type and stored in
+// both orders, since one product sums over classes and the other over tokens;
+// then the two products.  The piece bounds what the workspace holds.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include "api_internal.hpp"
+#include "gemm_nt.hpp"
+#include "train.hpp"
+
+namespace pp {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+struct Tokens {   // what the kernels know of the tokens
+  const int64_t* target;
+  const float* class_weight;   // or null
+  const float* grad;           // or null: 1
+  const float* stats;          // lse of each token, then the divisor
+  int64_t ignore;
+  int32_t t, v;                // tokens, classes
+  int32_t grad_each;           // grad has one value a token
+};
+
+// What all tokens' gradients have in common: the incoming gradient of a single
+// loss over the divisor.  It is left out of G and multiplied into the fp32
+// sums: most of G's weight lies in the values near -1 at the targets, which
+// 16 bits hold well and which a common factor would round all alike.
+__device__ __forceinline__ float common_scale(const Tokens& k) {
+  return (k.grad && !k.grad_each ? k.grad[0] : 1.f) / k.stats[k.t];
+}
+
+// Token t's own factor of G; false: ignored.  A target outside the classes
+// makes it NaN.
+__device__ __forceinline__ bool token_scale(const Tokens& k, int t, int64_t y, float* s) {
+  if (y == k.ignore) return false;
+  if (y < 0 || y >= k.v) {
+    *s = __builtin_nanf("");
+    return true;
+  }
+  float g = k.grad && k.grad_each ? k.grad[t] : 1.f;
+  if (k.class_weight) g *= k.class_weight[y];
+  *s = g;
+  return true;
+}
+
+// ---------------------------------------------------------------------------
+// operands: [rows][cols] of any strides -> 16-bit planes, k contiguous, padded
+// with zeros to multiples of 64, in one or both orders
+// ---------------------------------------------------------------------------
+
+struct StageArgs {
+  const void* src;
+  int64_t s_hi, s_lo, s_col;   // element (r, c) at (r / inner) s_hi + (r % inner) s_lo + c s_col
+  int32_t inner, rows, cols;
+  const int64_t* target;       // rows whose target is `ignore` become zeros (null: none)
+  int64_t ignore;
+  __bf16* direct;              // [rows][cols padded] planes, or null
+  __bf16* turned;              // [cols][rows padded] planes, or null
+  int64_t direct_plane, turned_plane;   // elements between planes
+  int32_t cols_pad, rows_pad;
+};
+
+// An fp32 value as a sum of three bf16 values: 8 bits of it each.
+template <int P>
+__device__ __forceinline__ void bf16_planes(float x, __bf16 (&p)[P]) {
+  p[0] = static_cast<__bf16>(x);
+  if constexpr (P > 1) {
+    const float h = static_cast<float>(p[0]);
+    const float rest = __builtin_isfinite(h) ? x - h : 0.f;   // (an infinity has no rest)
+    p[1] = static_cast<__bf16>(rest);
+    if constexpr (P > 2) p[2] = static_cast<__bf16>(rest - static_cast<float>(p[1]));
+  }
+}
+
+template <class S, int P>
+__global__ __launch_bounds__(256) void stage_kernel(StageArgs a) {
+  __shared__ float tile[64][65];
+  const int tc = a.cols_pad / 64;
+  const int r0 = blockIdx.x / tc * 64, c0 = blockIdx.x % tc * 64, tid = threadIdx.x;
+  const S* src = static_cast<const S*>(a.src);
+  const bool along_cols = a.s_col == 1;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int u = tid & 63, w = (tid >> 6) + 4 * i;
+    const int r = along_cols ? w : u, c = along_cols ? u : w;
+    const int row = r0 + r, col = c0 + c;
+    float x = 0.f;
+    if (row < a.rows && col < a.cols && !(a.target && a.target[row] == a.ignore)) {
+      const int hi = row / a.inner, lo = row - hi * a.inner;
+      x = static_cast<float>(src[hi * a.s_hi + lo * a.s_lo + col * a.s_col]);
+    }
+    tile[r][c] = x;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
+    if (a.direct && r0 + u < a.rows) {
+      bf16x8 o[P];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        __bf16 p[P];
+        bf16_planes<P>(tile[u][w + e], p);
+#pragma unroll
+        for (int q = 0; q < P; ++q) o[q][e] = p[q];
+      }
+#pragma unroll
+      for (int q = 0; q < P; ++q)
+        *reinterpret_cast<bf16x8*>(a.direct + q * a.direct_plane + static_cast<int64_t>(r0 + u) * a.cols_pad + c0 + w) = o[q];
+    }
+    if (a.turned && c0 + u < a.cols) {
+      bf16x8 o[P];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        __bf16 p[P];
+        bf16_planes<P>(tile[w + e][u], p);
+#pragma unroll
+        for (int q = 0; q < P; ++q) o[q][e] = p[q];
+      }
+#pragma unroll
+      for (int q = 0; q < P; ++q)
+        *reinterpret_cast<bf16x8*>(a.turned + q * a.turned_plane + static_cast<int64_t>(c0 + u) * a.rows_pad + r0 + w) = o[q];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// the logits' product, rows = classes [v0, v0 + A.rows), columns = tokens
+// ---------------------------------------------------------------------------
+
+struct LogitArgs {
+  GemmOperand w, x;
+  PlanePairs pairs;
+  int32_t ksteps, tm, tn;
+  int32_t v0;
+  const float* bias;
+  Tokens k;
+  // statistics
+  float2* part;            // [class part][token]: maximum, sum of exp(l - maximum)
+  float* target_logit;     // [token]
+  // gradient
+  __bf16* g;               // [token][v_pad] planes
+  __bf16* gt;              // [class][t_pad] planes
+  int64_t g_plane, gt_plane;
+  int32_t v_pad, t_pad;
+  float* db_part;          // [token part][w.rows], or null
+};
+
+template <class Tile, bool GRAD, int P>
+__global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
+  __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
+  int ti, tj;
+  band_order(xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, &ti, &tj);
+  const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
+  f32x4 acc[Tile::FM][Tile::FN];
+  Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, 0, a.ksteps * a.pairs.n, lds, acc);
+
+  const int lane = Tile::lane(), wave = Tile::wave();
+  const int rows = a.w.rows, nt = a.k.t;
+  // the logits: bias added; classes past the end take no part
+#pragma unroll
+  for (int i = 0; i < Tile::FM; ++i) {
+    const int r = row0 + Tile::row_of(i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float b = r + e < rows ? (a.bias ? a.bias[a.v0 + r + e] : 0.f) : -INFINITY;
+#pragma unroll
+      for (int j = 0; j < Tile::FN; ++j) acc[i][j][e] = r + e < rows ? acc[i][j][e] + b : -INFINITY;
+    }
+  }
+  if constexpr (!GRAD) {
+#pragma unroll
+    for (int j = 0; j < Tile::FN; ++j) {
+      const int t = col0 + Tile::col_of(j);
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[i][j][e]);
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      // (a column with nothing above -inf: every term is exp(-inf); NaNs reach the sum)
+      const float ref = m == -INFINITY ? 0.f : m;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += fast_exp(acc[i][j][e] - ref);
+      s += __shfl_xor(s, 16);
+      s += __shfl_xor(s, 32);
+      if (t < nt) {
+        if (lane < 16) a.part[static_cast<int64_t>(ti * Tile::WM + wave / Tile::WN) * nt + t] = make_float2(m, s);
+        const int64_t y = a.k.target[t] - a.v0;
+        const int64_t first = row0 + Tile::row_of(0);
+        if (y >= first && y < first + Tile::TM && y < rows) {
+          const int d = static_cast<int>(y - first);
+#pragma unroll
+          for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (d == 16 * i + e) a.target_logit[t] = acc[i][j][e];
+        }
+      }
+    }
+  } else {
+    float s[Tile::FN], lse[Tile::FN];
+    int hit[Tile::FN];   // target's row in this lane's rows, or out of them
+    bool kept[Tile::FN];
+#pragma unroll
+    for (int j = 0; j < Tile::FN; ++j) {
+      const int t = col0 + Tile::col_of(j);
+      kept[j] = false;
+      s[j] = lse[j] = 0.f;
+      hit[j] = -1;
+      if (t < nt) {
+        const int64_t y = a.k.target[t];
+        kept[j] = token_scale(a.k, t, y, &s[j]);
+        lse[j] = a.k.stats[t];
+        const int64_t d = y - a.v0 - (row0 + Tile::row_of(0));
+        if (d >= 0 && d < Tile::TM) hit[j] = static_cast<int>(d);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < Tile::FM; ++i) {
+      const int r = row0 + Tile::row_of(i);
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < Tile::FN; ++j) {
+        const int t = col0 + Tile::col_of(j);
+        __bf16 o[4][P];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float g = 0.f;
+          if (kept[j] && r + e < rows) g = (fast_exp(acc[i][j][e] - lse[j]) - (hit[j] == 16 * i + e ? 1.f : 0.f)) * s[j];
+          sum[e] += g;
+          bf16_planes<P>(g, o[e]);
+          if (r + e < rows && t < a.t_pad) {
+#pragma unroll
+            for (int q = 0; q < P; ++q) a.gt[q * a.gt_plane + static_cast<int64_t>(r + e) * a.t_pad + t] = o[e][q];
+          }
+        }
+        if (t < nt && r < a.v_pad) {
+#pragma unroll
+          for (int q = 0; q < P; ++q) {
+            using bf16x4 = __attribute__((ext_vector_type(4))) __bf16;
+            *reinterpret_cast<bf16x4*>(a.g + q * a.g_plane + static_cast<int64_t>(t) * a.v_pad + r) =
+                bf16x4{o[0][q], o[1][q], o[2][q], o[3][q]};
+          }
+        }
+      }
+      if (a.db_part) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int d = 1; d < 16; d <<= 1) sum[e] += __shfl_xor(sum[e], d);
+          if ((lane & 15) == 0 && r + e < rows)
+            a.db_part[static_cast<int64_t>(tj * Tile::WN + wave % Tile::WN) * rows + r + e] = sum[e];
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// joining the parts: each token's log-sum-exp and loss
+// ---------------------------------------------------------------------------
+
+struct JoinArgs {
+  Tokens k;
+  const float2* part;
+  const float* target_logit;
+  int32_t parts;
+  float* lse;       // [token]
+  float* loss;      // [token]
+  float* weight;    // [token], or null
+};
+
+// 16 tokens a workgroup, 16 threads each taking every 16th part.
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+  __shared__ float2 got[16][17];
+  const int u = threadIdx.x & 15, w = threadIdx.x >> 4, t = blockIdx.x * 16 + u;
+  float m = -INFINITY, s = 0.f;
+  if (t < a.k.t)
+    for (int p = w; p < a.parts; p += 16) {
+      const float2 q = a.part[static_cast<int64_t>(p) * a.k.t + t];
+      const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
+      s = s * fast_exp(m - ref) + q.y * fast_exp(q.x - ref);
+      m = top;
+    }
+  got[w][u] = make_float2(m, s);
+  __syncthreads();
+  if (w || t >= a.k.t) return;
+  for (int p = 1; p < 16; ++p) {
+    const float2 q = got[p][u];
+    const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
+    s = s * fast_exp(m - ref) + q.y * fast_exp(q.x - ref);
+    m = top;
+  }
+  const int64_t y = a.k.target[t];
+  float lse = 0.f, loss = 0.f, weight = 0.f;
+  if (y != a.k.ignore) {
+    lse = m + logf(s);
+    if (y < 0 || y >= a.k.v) {
+      loss = weight = __builtin_nanf("");
+    } else {
+      weight = a.k.class_weight ? a.k.class_weight[y] : 1.f;
+      loss = weight * (lse - a.target_logit[t]);
+    }
+  }
+  a.lse[t] = lse;
+  a.loss[t] = loss;
+  if (a.weight) a.weight[t] = weight;
+}
+
+// the loss and its divisor (sums in 64 bits, in a fixed order)
+__global__ __launch_bounds__(1024) void loss_kernel(const float* loss, const float* weight, int32_t n, int32_t mean,
+                                                    float* out, float* divisor) {
+  __shared__ double a[16], b[16];
+  double x = 0., w = 0.;
+  if (loss)
+    for (int i = threadIdx.x; i < n; i += 1024) {
+      x += loss[i];
+      w += weight[i];
+    }
+  for (int d = 32; d; d >>= 1) {
+    x += __shfl_xor(x, d);
+    w += __shfl_xor(w, d);
+  }
+  if ((threadIdx.x & 63) == 0) a[threadIdx.x >> 6] = x, b[threadIdx.x >> 6] = w;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < 16; ++i) x += a[i], w += b[i];
+  // (a mean over no token: a loss of 0)
+  const double div = mean && !(w == 0.) ? w : 1.;
+  if (out) *out = static_cast<float>(x / div);
+  *divisor = static_cast<float>(div);
+}
+
+__global__ __launch_bounds__(256) void column_sum_kernel(const float* part, int32_t parts, int32_t n, Tokens k, float* out) {
+  const int v = blockIdx.x * 256 + threadIdx.x;
+  if (v >= n) return;
+  float s = 0.f;
+  for (int p = 0; p < parts; ++p) s += part[static_cast<int64_t>(p) * n + v];
+  out[v] = s * common_scale(k);
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(uint8_t* p, int64_t bytes) {
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < bytes; i += gridDim.x * 256ll) p[i] = 0;
+}
+
+// ---------------------------------------------------------------------------
+// the gradient's products: out[c][r] = sum_k A[r][k] B[c][k]
+// ---------------------------------------------------------------------------
+
+// Where element (r, c) of a product goes: rows or columns that are tokens lie
+// at (t / inner) s_hi + (t % inner) s_lo.
+struct OutMap {
+  void* out;
+  int64_t r_hi, r_lo, c_hi, c_lo;
+  int32_t r_inner, c_inner;
+  int32_t wide;   // four rows follow each other in memory, aligned
+};
+
+struct ProductArgs {
+  GemmOperand a, b;
+  PlanePairs pairs;
+  int32_t ksteps, tm, tn, splits;
+  OutMap map;
+  float* slab;    // [split][b.rows][slab_ld] partial sums instead of the output, or null
+  int64_t slab_ld;
+  int32_t add;    // the slab already holds a sum
+  Tokens k;       // for the common factor
+};
+
+template <class O>
+__device__ __forceinline__ void store4(const OutMap& m, int r, int c, int rows, f32x4 v) {
+  const int ch = c / m.c_inner, cl = c - ch * m.c_inner;
+  const int64_t at = ch * m.c_hi + cl * m.c_lo;
+  O* out = static_cast<O*>(m.out);
+  if (m.wide) {
+    if (r < rows) {   // (rows is a multiple of four here)
+      using O4 = __attribute__((ext_vector_type(4))) O;
+      const int rh = r / m.r_inner, rl = r - rh * m.r_inner;
+      *reinterpret_cast<O4*>(out + at + rh * m.r_hi + rl * m.r_lo) =
+          O4{static_cast<O>(v[0]), static_cast<O>(v[1]), static_cast<O>(v[2]), static_cast<O>(v[3])};
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (r + e < rows) {
+      const int rh = (r + e) / m.r_inner, rl = r + e - rh * m.r_inner;
+      out[at + rh * m.r_hi + rl * m.r_lo] = static_cast<O>(v[e]);
+    }
+}
+
+template <class Tile, class O>
+__global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
+  __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
+  const int tiles = a.tm * a.tn;
+  const int id = xcd_order(blockIdx.x, tiles * a.splits);
+  const int split = id / tiles;
+  int ti, tj;
+  band_order(id - split * tiles, a.tm, a.tn, &ti, &tj);
+  const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
+  const int steps = a.ksteps * a.pairs.n;
+  const int s0 = static_cast<int>(static_cast<int64_t>(steps) * split / a.splits);
+  const int s1 = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
+  f32x4 acc[Tile::FM][Tile::FN];
+  Tile::run(a.a, a.b, a.pairs, row0, col0, a.ksteps, 0, s0, s1, lds, acc);
+  const float scale = a.slab ? 1.f : common_scale(a.k);
+#pragma unroll
+  for (int j = 0; j < Tile::FN; ++j) {
+    const int c = col0 + Tile::col_of(j);
+    if (c >= a.b.rows) continue;
+#pragma unroll
+    for (int i = 0; i < Tile::FM; ++i) {
+      const int r = row0 + Tile::row_of(i);
+      if (a.slab) {
+        if (r < a.slab_ld) {   // (a multiple of four)
+          f32x4* at = reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.b.rows + c) * a.slab_ld + r);
+          *at = a.add ? *at + acc[i][j] : acc[i][j];
+        }
+      } else {
+        store4<O>(a.map, r, c, a.a.rows, acc[i][j] * scale);
+      }
+    }
+  }
+}
+
+template <class O>
+__global__ __launch_bounds__(256) void slab_kernel(const float* slab, int64_t slab_ld, int32_t rows, int32_t cols,
+                                                   int32_t splits, OutMap map, Tokens tok) {
+  const float scale = common_scale(tok);
+  const int64_t n4 = slab_ld / 4, all = n4 * cols;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
+    const int c = static_cast<int>(i / n4), r = static_cast<int>(i - c * n4) * 4;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; ++k)
+      s += *reinterpret_cast<const f32x4*>(slab + (static_cast<int64_t>(k) * cols + c) * slab_ld + r);
+    store4<O>(map, r, c, rows, s * scale);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+
+using Big = GemmTile<__bf16, 256, 256, 2, 4>;
+using Mid = GemmTile<__bf16, 128, 128, 2, 2>;
+using Small = GemmTile<__bf16, 64, 64, 2, 2>;
+enum { kBig = 0, kMid = 1, kSmall = 2 };
+constexpr int kTileM[] = {256, 128, 64}, kTileN[] = {256, 128, 64};
+
+// The largest tile that still gives most CUs one.
+int pick_tile(int64_t m, int64_t n) {
+  for (int k = 0; k < 2; ++k)
+    if (cdiv(m, kTileM[k]) * cdiv(n, kTileN[k]) >= 200) return k;
+  return kSmall;
+}
+
+// Splits of k for a product whose tiles do not fill the card; each keeps at
+// least 8 steps.
+int pick_splits(int64_t tiles, int64_t steps) {
+  if (tiles >= 200) return 1;
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(cdiv(256, tiles), steps / 8)));
+}
+
+struct Plan {
+  int64_t t = 0, d = 0, v = 0, tp = 0, dp = 0, vp = 0;   // sizes and their paddings
+  int planes = 1;
+  PlanePairs pairs = kPairs1;
+  bool w_direct = false, x_direct = false, fwd = false, bwd = false;
+  int logit = kSmall, parts = 0;
+  int64_t piece = 0, pieces = 0;      // classes a piece
+  int gl = kSmall, dxt = kSmall, dwt = kSmall, dx_splits = 1, dw_splits = 1;
+  bool dx_slab = false, dw_slab = false;
+  int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
+  bool dx_turned = false;             // dx's product has the tokens as rows
+  // workspace offsets
+  size_t x_k = 0, w_k = 0, x_t = 0, w_t = 0, part = 0, tl = 0, loss = 0, weight = 0, g = 0, gt = 0, db = 0, slab = 0, total = 0;
+};
+
+constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of G, both orders
+
+Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool x_aligned, bool w_aligned) {
+  Plan p;
+  p.fwd = fwd, p.bwd = bwd;
+  p.t = d.n * d.hw, p.d = d.d, p.v = d.v;
+  p.tp = pad64(p.t), p.dp = pad64(p.d), p.vp = pad64(p.v);
+  const bool bf16 = d.dtype == PP_BF16;
+  p.planes = bf16 ? 1 : 3;
+  p.pairs = bf16 ? kPairs1 : kPairs6;
+  const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
+  p.x_direct = bf16 && x_aligned && d.x_sc == 1 && p.d % 64 == 0 && step % 8 == 0 && step >= p.d && step <= kMaxLd &&
+               (d.n == 1 || d.hw == 1 || d.x_sn == d.hw * d.x_sp);
+  p.w_direct = bf16 && w_aligned && p.d % 64 == 0 && d.w_ld % 8 == 0 && d.w_ld <= kMaxLd;
+  size_t at = 0;
+  auto take = [&at](size_t n) {
+    const size_t r = at;
+    at += (n + 255) / 256 * 256;
+    return r;
+  };
+  const size_t e = 2 * p.planes;
+  if (!p.x_direct) p.x_k = take(p.t * p.dp * e);
+  if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
+  if (fwd) {
+    p.logit = pick_tile(p.v, p.t);
+    p.parts = static_cast<int>(cdiv(p.v, kTileM[p.logit]) * 2);
+    p.part = take(p.parts * p.t * 8);
+    p.tl = take(p.t * 4), p.loss = take(p.t * 4), p.weight = take(p.t * 4);
+  }
+  if (bwd) {
+    p.x_t = take(p.d * p.tp * e), p.w_t = take(p.d * p.vp * e);
+    p.piece = std::max<int64_t>(256, kPieceBytes / (p.tp * static_cast<int64_t>(2 * e)) / 256 * 256);
+    if (p.piece > p.vp) p.piece = p.vp;
+    p.pieces = cdiv(p.v, p.piece);
+    p.piece = std::min(p.vp, cdiv(cdiv(p.v, p.pieces), 256) * 256);   // pieces of about one size
+    p.pieces = cdiv(p.v, p.piece);
+    p.g = take(p.t * p.piece * e), p.gt = take(p.piece * p.tp * e);
+    p.gl = pick_tile(p.piece, p.t);
+    p.db = take(cdiv(p.t, kTileN[p.gl]) * 4 * p.piece * 4);
+    p.dx_turned = d.dx_sc != 1;
+    const int64_t dm = p.dx_turned ? p.t : p.d, dn = p.dx_turned ? p.d : p.t;
+    p.dxt = pick_tile(dm, dn);
+    p.dx_splits = pick_splits(cdiv(dm, kTileM[p.dxt]) * cdiv(dn, kTileN[p.dxt]), p.piece / 64 * p.pairs.n);
+    p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
+    p.dx_ld = cdiv(dm, 4) * 4;
+    p.dwt = pick_tile(p.d, p.piece);
+    p.dw_splits = pick_splits(cdiv(p.d, kTileM[p.dwt]) * cdiv(p.piece, kTileN[p.dwt]), p.tp / 64 * p.pairs.n);
+    p.dw_slab = p.dw_splits > 1;
+    p.dw_ld = cdiv(p.d, 4) * 4;
+    // dx's slab outlives a piece, dw's does not
+    p.slab = take((p.dx_slab ? p.dx_splits * p.dx_ld * dn * 4 : 0) + 256 + (p.dw_slab ? p.dw_splits * p.dw_ld * p.piece * 4 : 0));
+  }
+  p.total = std::max<size_t>(at, 256);
+  return p;
+}
+
+template <class S, int P>
+void stage(const StageArgs& a, hipStream_t st) {
+  const int64_t blocks = static_cast<int64_t>(a.rows_pad / 64) * (a.cols_pad / 64);
+  hipLaunchKernelGGL((stage_kernel<S, P>), dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, a);
+}
+
+template <bool GRAD, int P>
+void logits(int tile, LogitArgs& a, hipStream_t st) {
+  a.tm = static_cast<int32_t>(cdiv(a.w.rows, kTileM[tile]));
+  a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileN[tile]));
+  const dim3 grid(static_cast<uint32_t>(a.tm * a.tn));
+  if (tile == kBig)
+    hipLaunchKernelGGL((logit_kernel<Big, GRAD, P>), grid, dim3(Big::THREADS), 0, st, a);
+  else if (tile == kMid)
+    hipLaunchKernelGGL((logit_kernel<Mid, GRAD, P>), grid, dim3(Mid::THREADS), 0, st, a);
+  else
+    hipLaunchKernelGGL((logit_kernel<Small, GRAD, P>), grid, dim3(Small::THREADS), 0, st, a);
+}
+
+template <class O>
+void product(int tile, ProductArgs& a, hipStream_t st) {
+  a.tm = static_cast<int32_t>(cdiv(a.a.rows, kTileM[tile]));
+  a.tn = static_cast<int32_t>(cdiv(a.b.rows, kTileN[tile]));
+  const dim3 grid(static_cast<uint32_t>(a.tm * a.tn * a.splits));
+  if (tile == kBig)
+    hipLaunchKernelGGL((product_kernel<Big, O>), grid, dim3(Big::THREADS), 0, st, a);
+  else if (tile == kMid)
+    hipLaunchKernelGGL((product_kernel<Mid, O>), grid, dim3(Mid::THREADS), 0, st, a);
+  else
+    hipLaunchKernelGGL((product_kernel<Small, O>), grid, dim3(Small::THREADS), 0, st, a);
+}
+
+template <class O>
+void join_slab(const ProductArgs& a, hipStream_t st) {
+  const int64_t n = a.slab_ld / 4 * a.b.rows;
+  const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(cdiv(n, 256), 4096));
+  hipLaunchKernelGGL((slab_kernel<O>), dim3(grid), dim3(256), 0, st, a.slab, a.slab_ld, a.a.rows, a.b.rows, a.splits, a.map, a.k);
+}
+
+struct Call {
+  const pp_xent_desc* d;
+  const void *x, *w;
+  const float *bias, *class_weight;
+  const int64_t* target;
+  float *loss, *stats;
+  const float* grad;
+  void *dx, *dw;
+  float* db;
+  uint8_t* ws;
+  hipStream_t st;
+};
+
+template <class S, int P>
+pp_status enqueue(const Plan& p, const Call& c) {
+  const pp_xent_desc& d = *c.d;
+  hipStream_t st = c.st;
+  pp_status s;
+  Tokens tok = {c.target, c.class_weight, c.grad, c.stats, d.ignore_index, static_cast<int32_t>(p.t), static_cast<int32_t>(p.v),
+                d.reduction == PP_NONE};
+  auto bf = [&](size_t off) { return reinterpret_cast<__bf16*>(c.ws + off); };
+  auto f32 = [&](size_t off) { return reinterpret_cast<float*>(c.ws + off); };
+
+  // operands: token rows and class rows, k (channels) contiguous; for the
+  // gradient also turned
+  const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
+  GemmOperand x = p.x_direct ? operand(c.x, 0, step, p.t, 1) : operand(bf(p.x_k), p.t * p.dp, p.dp, p.t, P);
+  GemmOperand w = p.w_direct ? operand(c.w, 0, d.w_ld, p.v, 1) : operand(bf(p.w_k), p.v * p.dp, p.dp, p.v, P);
+  const bool turn_x = p.bwd && c.dw, turn_w = p.bwd && c.dx;
+  if (!p.x_direct || turn_x) {
+    StageArgs a = {c.x, d.x_sn, d.x_sp, d.x_sc, static_cast<int32_t>(d.hw), static_cast<int32_t>(p.t), static_cast<int32_t>(p.d),
+                   c.target, d.ignore_index, p.x_direct ? nullptr : bf(p.x_k), turn_x ? bf(p.x_t) : nullptr,
+                   p.t * p.dp, p.d * p.tp, static_cast<int32_t>(p.dp), static_cast<int32_t>(p.tp)};
+    stage<S, P>(a, st);
+  }
+  if (!p.w_direct || turn_w) {
+    StageArgs a = {c.w, d.w_ld, 0, 1, 1, static_cast<int32_t>(p.v), static_cast<int32_t>(p.d), nullptr, 0,
+                   p.w_direct ? nullptr : bf(p.w_k), turn_w ? bf(p.w_t) : nullptr, p.v * p.dp, p.d * p.vp,
+                   static_cast<int32_t>(p.dp), static_cast<int32_t>(p.vp)};
+    stage<S, P>(a, st);
+  }
+  if ((s = launched()) != PP_OK) return s;
+
+  LogitArgs la = {};
+  la.x = x, la.pairs = p.pairs, la.ksteps = static_cast<int32_t>(p.dp / 64), la.k = tok;
+  if (p.fwd) {
+    la.w = w, la.v0 = 0, la.bias = c.bias;
+    la.part = reinterpret_cast<float2*>(c.ws + p.part), la.target_logit = f32(p.tl);
+    logits<false, P>(p.logit, la, st);
+    const bool each = d.reduction == PP_NONE;
+    JoinArgs ja = {tok, la.part, la.target_logit, p.parts, c.stats, each ? c.loss : f32(p.loss), each ? nullptr : f32(p.weight)};
+    hipLaunchKernelGGL(join_kernel, dim3(static_cast<uint32_t>(cdiv(p.t, 16))), dim3(256), 0, st, ja);
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, each ? nullptr : f32(p.loss), f32(p.weight),
+                       static_cast<int32_t>(p.t), static_cast<int32_t>(d.reduction == PP_MEAN), each ? nullptr : c.loss, c.stats + p.t);
+    if ((s = launched()) != PP_OK) return s;
+  }
+  if (!p.bwd) return PP_OK;
+
+  const GemmOperand xt = operand(bf(p.x_t), p.d * p.tp, p.tp, p.d, P);
+  const GemmOperand wt = operand(bf(p.w_t), p.d * p.vp, p.vp, p.d, P);
+  const int64_t dn = p.dx_turned ? p.d : p.t;
+  float* dx_slab = f32(p.slab);
+  float* dw_slab = dx_slab + (p.dx_slab ? p.dx_splits * p.dx_ld * dn : 0);
+  ProductArgs xa = {}, wa = {};
+  for (int64_t k = 0; k < p.pieces; ++k) {
+    const int64_t v0 = k * p.piece, nv = std::min(p.piece, p.v - v0), nvp = pad64(nv);
+    la.w = rows_from(w, v0, nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
+    la.g = bf(p.g), la.gt = bf(p.gt);
+    la.v_pad = static_cast<int32_t>(nvp), la.t_pad = static_cast<int32_t>(p.tp);
+    la.g_plane = p.t * nvp, la.gt_plane = nv * p.tp;
+    la.db_part = c.db ? f32(p.db) : nullptr;
+    logits<true, P>(p.gl, la, st);
+    if (c.db)
+      hipLaunchKernelGGL(column_sum_kernel, dim3(static_cast<uint32_t>(cdiv(nv, 256))), dim3(256), 0, st, la.db_part,
+                         static_cast<int32_t>(la.tn * (p.gl == kBig ? Big::WN : Mid::WN)), static_cast<int32_t>(nv), tok, c.db + v0);
+    const GemmOperand g = operand(la.g, la.g_plane, nvp, p.t, P), gt = operand(la.gt, la.gt_plane, p.tp, nv, P);
+    if (c.dw) {
+      wa = {};
+      wa.k = tok, wa.a = xt, wa.b = gt, wa.pairs = p.pairs, wa.ksteps = static_cast<int32_t>(p.tp / 64), wa.splits = p.dw_splits;
+      wa.map = {static_cast<S*>(c.dw) + v0 * p.d, 1, 0, p.d, 0, 1, 1, p.d % 4 == 0 && reinterpret_cast<uintptr_t>(c.dw) % 16 == 0};
+      wa.slab = p.dw_slab ? dw_slab : nullptr, wa.slab_ld = p.dw_ld;
+      product<S>(p.dwt, wa, st);
+      if (p.dw_slab) join_slab<S>(wa, st);
+    }
+    if (c.dx) {
+      xa = {};
+      GemmOperand wp = wt;
+      for (auto& q : wp.plane) q = static_cast<const uint8_t*>(q) + v0 * 2;
+      xa.k = tok, xa.pairs = p.pairs, xa.ksteps = static_cast<int32_t>(nvp / 64);
+      xa.splits = p.dx_splits;   // (a last, smaller piece may leave some without a step: they add nothing)
+      const bool aligned = reinterpret_cast<uintptr_t>(c.dx) % 16 == 0;
+      if (p.dx_turned) {
+        xa.a = g, xa.b = wp;
+        xa.map = {c.dx, d.dx_sn, d.dx_sp, d.dx_sc, 0, static_cast<int32_t>(d.hw), 1,
+                  aligned && d.dx_sp == 1 && d.hw % 4 == 0 && d.dx_sn % 4 == 0 && d.dx_sc % 4 == 0};
+      } else {
+        xa.a = wp, xa.b = g;
+        xa.map = {c.dx, 1, 0, d.dx_sn, d.dx_sp, 1, static_cast<int32_t>(d.hw),
+                  aligned && p.d % 4 == 0 && d.dx_sn % 4 == 0 && (d.hw == 1 || d.dx_sp % 4 == 0)};
+      }
+      xa.slab = p.dx_slab ? dx_slab : nullptr, xa.slab_ld = p.dx_ld, xa.add = k > 0;
+      product<S>(p.dxt, xa, st);
+    }
+    if ((s = launched()) != PP_OK) return s;
+  }
+  if (c.dx && p.dx_slab) join_slab<S>(xa, st);
+  return launched();
+}
+
+pp_status check_desc(const pp_xent_desc* d) {
+  if (!d) return fail(PP_EINVAL, "desc is NULL");
+  if (d->dtype != PP_F32 && d->dtype != PP_BF16) return fail(PP_EINVAL, "bad dtype");
+  if (d->reduction != PP_MEAN && d->reduction != PP_SUM && d->reduction != PP_NONE) return fail(PP_EINVAL, "bad reduction");
+  if (d->n < 0 || d->hw < 0 || d->d < 1 || d->v < 1) return fail(PP_EINVAL, "n, hw must be >= 0, d and v >= 1");
+  if (d->d > kMaxLd - 64 || d->v > kMaxLd - 64 || d->n > kMaxLd || d->hw > kMaxLd || d->n * d->hw > kMaxLd - 64)
+    return fail(PP_EUNSUPPORTED, "d, v and the tokens must be below 2^22 - 64 each");
+  if (d->w_ld < d->d) return fail(PP_EINVAL, "w_ld smaller than d");
+  if (d->x_sn < 0 || d->x_sc < 0 || d->x_sp < 0 || d->dx_sn < 0 || d->dx_sc < 0 || d->dx_sp < 0)
+    return fail(PP_EINVAL, "negative stride");
+  return PP_OK;
+}
+
+pp_status xent_call(const Call& c, bool fwd, bool bwd, size_t ws_bytes) {
+  pp_status s = check_desc(c.d);
+  if (s != PP_OK) return s;
+  const pp_xent_desc& d = *c.d;
+  const size_t esz = d.dtype == PP_BF16 ? 2 : 4;
+  const bool empty = d.n * d.hw == 0;
+  if (!c.w || !c.stats || (fwd && !c.loss && !(empty && d.reduction == PP_NONE))) return fail(PP_EINVAL, "NULL pointer");
+  if (!empty && (!c.x || !c.target)) return fail(PP_EINVAL, "NULL pointer");
+  for (const void* q : {c.x, c.w, static_cast<const void*>(c.dx), static_cast<const void*>(c.dw)})
+    if (reinterpret_cast<uintptr_t>(q) % esz) return fail(PP_EINVAL, "misaligned pointer");
+  for (const void* q : {static_cast<const void*>(c.bias), static_cast<const void*>(c.class_weight), static_cast<const void*>(c.loss),
+                        static_cast<const void*>(c.stats), static_cast<const void*>(c.grad), static_cast<const void*>(c.db)})
+    if (reinterpret_cast<uintptr_t>(q) % 4) return fail(PP_EINVAL, "misaligned fp32 pointer");
+  if (reinterpret_cast<uintptr_t>(c.target) % 8) return fail(PP_EINVAL, "misaligned target");
+  if (empty) {   // no token: a loss of 0, and gradients of 0
+    auto zero = [&](void* q, int64_t bytes) {
+      if (q && bytes)
+        hipLaunchKernelGGL(zero_kernel, dim3(static_cast<uint32_t>(std::min<int64_t>(cdiv(bytes, 256), 4096))), dim3(256), 0, c.st,
+                           static_cast<uint8_t*>(q), bytes);
+    };
+    if (fwd)
+      hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, nullptr, nullptr, 0, 0,
+                         d.reduction == PP_NONE ? nullptr : c.loss, c.stats);
+    if (bwd) {
+      zero(c.dw, d.v * d.d * static_cast<int64_t>(esz));
+      zero(c.db, d.v * 4);
+    }
+    return launched();
+  }
+  const Plan p = make_plan(d, fwd, bwd, aligned16(c.x), aligned16(c.w));
+  if (!c.ws || reinterpret_cast<uintptr_t>(c.ws) % 256) return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
+  if (ws_bytes < p.total) return fail(PP_ESIZE, "workspace smaller than pp_xent_workspace says");
+  return d.dtype == PP_BF16 ? enqueue<__bf16, 1>(p, c) : enqueue<float, 3>(p, c);
+}
+
+}  // namespace
+}  // namespace pp
+
+using namespace pp;
+
+extern "C" pp_status pp_xent_workspace(const pp_xent_desc* desc, int32_t parts, size_t* bytes) {
+  clear_error();
+  if (!bytes) return fail(PP_EINVAL, "bytes is NULL");
+  pp_status s = check_desc(desc);
+  if (s != PP_OK) return s;
+  if (parts < 1 || parts > 3) return fail(PP_EINVAL, "parts must be PP_XENT_FWD, PP_XENT_BWD or both");
+  if (desc->n * desc->hw == 0) {
+    *bytes = 0;
+    return PP_OK;
+  }
+  // (operands that are not 16-byte aligned are copied: what the call needs at most)
+  *bytes = make_plan(*desc, parts & 1, parts & 2, false, false).total;
+  return PP_OK;
+}
+
+extern "C" pp_status pp_xent_fwd(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,
+                                 const float* class_weight, const int64_t* target, float* loss, float* stats,
+                                 void* workspace, size_t ws_bytes, void* hip_stream) {
+  clear_error();
+  return xent_call({desc, x, w, bias, class_weight, target, loss, stats, nullptr, nullptr, nullptr, nullptr,
+                    static_cast<uint8_t*>(workspace), static_cast<hipStream_t>(hip_stream)}, true, false, ws_bytes);
+}
+
+extern "C" pp_status pp_xent_bwd(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,
+                                 const float* class_weight, const int64_t* target, const float* stats, const float* grad,
+                                 void* dx, void* dw, float* db, void* workspace, size_t ws_bytes, void* hip_stream) {
+  clear_error();
+  return xent_call({desc, x, w, bias, class_weight, target, nullptr, const_cast<float*>(stats), grad, dx, dw, db,
+                    static_cast<uint8_t*>(workspace), static_cast<hipStream_t>(hip_stream)}, false, true, ws_bytes);
+}
+
+extern "C" pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,
+                                  const float* class_weight, const int64_t* target, const float* grad, float* loss,
+                                  float* stats, void* dx, void* dw, float* db, void* workspace, size_t ws_bytes,
+                                  void* hip_stream) {
+  clear_error();
+  return xent_call({desc, x, w, bias, class_weight, target, loss, stats, grad, dx, dw, db,
+                    static_cast<uint8_t*>(workspace), static_cast<hipStream_t>(hip_stream)}, true, true, ws_bytes);
+}

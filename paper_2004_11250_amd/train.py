@@ -1,0 +1,193 @@
+"""Training operators: the loss of a linear head with its gradient, and the
+orthogonalised weight step of pruned layers (the calls of ``include/pp.h``'s
+training section, on torch tensors).
+
+``linear_xent_fwd`` / ``linear_xent_bwd`` / ``linear_xent_step``
+    softmax cross entropy of a 1x1 convolution or fully connected layer over
+    any number of classes, and its gradients, without keeping the logits.
+
+As elsewhere in this package every computation runs in the library's kernels;
+this module checks and marshals arguments, and allocates outputs and scratch
+on the stream of the call.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+from . import _check, _dtype_code, _stream_ptr, _torch, load_library
+
+PP_MEAN, PP_SUM, PP_NONE = 0, 1, 2
+PP_XENT_FWD, PP_XENT_BWD = 1, 2
+_REDUCTION = {"mean": PP_MEAN, "sum": PP_SUM, "none": PP_NONE}
+
+
+class XentDesc(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("reduction", ctypes.c_int32), ("n", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("hw", ctypes.c_int64), ("v", ctypes.c_int64), ("x_sn", ctypes.c_int64), ("x_sc", ctypes.c_int64),
+                ("x_sp", ctypes.c_int64), ("dx_sn", ctypes.c_int64), ("dx_sc", ctypes.c_int64),
+                ("dx_sp", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("ignore_index", ctypes.c_int64)]
+
+
+def bind(lib):
+    """Argument types of the training calls (a library without them, the
+    host-only one, is left as it is)."""
+    vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
+    desc = ctypes.POINTER(XentDesc)
+    argtypes = {
+        "pp_xent_workspace": [desc, i32, ctypes.POINTER(sz)],
+        "pp_xent_fwd": [desc, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        "pp_xent_bwd": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        "pp_xent_step": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+    }
+    for name, at in argtypes.items():
+        if hasattr(lib, name):
+            fn = getattr(lib, name)
+            fn.argtypes = at
+            fn.restype = i32
+
+
+def _p(t):
+    return None if t is None else t.data_ptr()
+
+
+def _on(stream, device):
+    """Context in which tensors belong to the call's stream."""
+    if stream is None:
+        return contextlib.nullcontext()
+    torch = _torch()
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream.cuda_stream), device))
+
+
+def _flat_pixels(x):
+    """(n, d, hw, strides) of features [n, d, ...]; the pixel axes have to be
+    one axis in memory."""
+    n, d = x.shape[0], x.shape[1]
+    sizes, strides = list(x.shape[2:]), list(x.stride()[2:])
+    hw, sp = 1, 1
+    for size, step in zip(reversed(sizes), reversed(strides)):   # from the innermost axis out
+        if size != 1 and hw != 1 and step != hw * sp and 0 not in x.shape:
+            raise ValueError("the pixel axes of x do not lie as one axis in memory (call contiguous())")
+        if size != 1 and hw == 1:
+            sp = step
+        hw *= size
+    return n, d, hw, (x.stride(0), x.stride(1), sp)
+
+
+def _xent_args(x, w, target, bias, class_weight, ignore_index, reduction):
+    torch = _torch()
+    if reduction not in _REDUCTION:
+        raise ValueError(f"reduction must be one of {sorted(_REDUCTION)}, got {reduction!r}")
+    if x.dim() < 2 or w.dim() < 2 or any(k != 1 for k in w.shape[2:]):
+        raise ValueError("x must be [n, d, ...] and w [v, d] (or [v, d, 1, 1])")
+    dt = _dtype_code(x)
+    if w.dtype != x.dtype:
+        raise TypeError(f"w must be of x's dtype {x.dtype}, got {w.dtype}")
+    if w.dim() > 2:
+        w = w.reshape(w.shape[0], w.shape[1])
+    if w.shape[1] != x.shape[1] or w.shape[0] < 1 or w.shape[1] < 1:
+        raise ValueError(f"w {tuple(w.shape)} does not fit features {tuple(x.shape)}")
+    if w.stride(1) != 1 and w.shape[1] != 1 or w.shape[0] > 1 and w.stride(0) < w.shape[1]:
+        raise ValueError("the rows of w must be contiguous")
+    if tuple(target.shape) != (x.shape[0],) + tuple(x.shape[2:]) or target.dtype != torch.int64:
+        raise ValueError(f"target must be int64 of shape {(x.shape[0],) + tuple(x.shape[2:])}")
+    if not target.is_contiguous():
+        raise ValueError("target must be contiguous")
+    for name, t in (("bias", bias), ("class_weight", class_weight)):
+        if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (w.shape[0],) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous float32 [{w.shape[0]}]")
+    for t in (w, target, bias, class_weight):
+        if t is not None and t.device != x.device:
+            raise ValueError("all tensors must be on x's device")
+    if not x.is_cuda:
+        raise ValueError("the tensors must be on a GPU")
+    n, d, hw, (sn, sc, sp) = _flat_pixels(x)
+    v = w.shape[0]
+    ld = w.stride(0) if v > 1 else d
+    desc = XentDesc(dt, _REDUCTION[reduction], n, d, hw, v, sn, sc, sp, d * hw, hw, 1, ld, int(ignore_index))
+    return desc, w
+
+
+def _xent_grad_arg(grad, target, reduction):
+    torch = _torch()
+    if grad is None:
+        return
+    want = tuple(target.shape) if reduction == "none" else ()
+    if grad.dtype != torch.float32 or (tuple(grad.shape) != want and grad.numel() != (target.numel() if want else 1)) \
+            or not grad.is_contiguous() or grad.device != target.device:
+        raise ValueError(f"grad must be contiguous float32 of shape {want} on the targets' device")
+
+
+def _xent_workspace(desc, parts, device):
+    torch = _torch()
+    nb = ctypes.c_size_t(0)
+    _check(load_library().pp_xent_workspace(ctypes.byref(desc), parts, ctypes.byref(nb)), "pp_xent_workspace")
+    return torch.empty(max(nb.value, 256), dtype=torch.uint8, device=device)
+
+
+def linear_xent_fwd(x, w, target, bias=None, class_weight=None, ignore_index=-100, reduction="mean", stream=None):
+    """pp_xent_fwd: softmax cross entropy of the logits ``w x + bias``.
+
+    x: features [n, d, ...] (float32 or bfloat16; channels first or last, or
+    token rows [t, d]); w: [v, d] or a 1x1 convolution's [v, d, 1, 1]; target:
+    int64 [n, ...].  Returns (loss, stats): loss a float32 scalar, or [n, ...]
+    with reduction="none"; stats, float32 [tokens + 1], each token's
+    log-sum-exp (0 where ignored) and the loss's divisor, for
+    linear_xent_bwd."""
+    torch = _torch()
+    desc, w = _xent_args(x, w, target, bias, class_weight, ignore_index, reduction)
+    with _on(stream, x.device):
+        loss = torch.empty(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
+        stats = torch.empty(desc.n * desc.hw + 1, dtype=torch.float32, device=x.device)
+        ws = _xent_workspace(desc, PP_XENT_FWD, x.device)
+    _check(load_library().pp_xent_fwd(ctypes.byref(desc), _p(x), _p(w), _p(bias), _p(class_weight), _p(target), _p(loss),
+                                      _p(stats), _p(ws), ws.numel(), _stream_ptr(stream)), "pp_xent_fwd")
+    return loss, stats
+
+
+def _xent_outputs(desc, x, w, bias, need):
+    torch = _torch()
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need[0] else None
+    dw = torch.empty(w.shape, dtype=w.dtype, device=x.device) if need[1] else None
+    db = torch.empty(desc.v, dtype=torch.float32, device=x.device) if need[2] and bias is not None else None
+    return dx, dw, db
+
+
+def linear_xent_bwd(x, w, target, stats, grad=None, bias=None, class_weight=None, ignore_index=-100, reduction="mean",
+                    need=(True, True, True), stream=None):
+    """pp_xent_bwd: (dx, dw, db) of the loss that linear_xent_fwd returned with
+    ``stats``, times ``grad`` (a scalar tensor, or one value a token with
+    reduction="none"; None: ones).  dx is contiguous in x's shape, dw in w's;
+    db is None without a bias.  need: which of the three to compute."""
+    torch = _torch()
+    shape = w
+    desc, w = _xent_args(x, w, target, bias, class_weight, ignore_index, reduction)
+    _xent_grad_arg(grad, target, reduction)
+    if stats.dtype != torch.float32 or stats.numel() != desc.n * desc.hw + 1 or not stats.is_contiguous() \
+            or stats.device != x.device:
+        raise ValueError("stats must be what linear_xent_fwd returned for these features")
+    with _on(stream, x.device):
+        dx, dw, db = _xent_outputs(desc, x, shape, bias, need)
+        ws = _xent_workspace(desc, PP_XENT_BWD, x.device)
+    _check(load_library().pp_xent_bwd(ctypes.byref(desc), _p(x), _p(w), _p(bias), _p(class_weight), _p(target), _p(stats),
+                                      _p(grad), _p(dx), _p(dw), _p(db), _p(ws), ws.numel(), _stream_ptr(stream)),
+           "pp_xent_bwd")
+    return dx, dw, db
+
+
+def linear_xent_step(x, w, target, grad=None, bias=None, class_weight=None, ignore_index=-100, reduction="mean",
+                     need=(True, True, True), stream=None):
+    """pp_xent_step: (loss, dx, dw, db), forward and backward in one call."""
+    torch = _torch()
+    shape = w
+    desc, w = _xent_args(x, w, target, bias, class_weight, ignore_index, reduction)
+    _xent_grad_arg(grad, target, reduction)
+    with _on(stream, x.device):
+        loss = torch.empty(target.shape if reduction == "none" else (), dtype=torch.float32, device=x.device)
+        stats = torch.empty(desc.n * desc.hw + 1, dtype=torch.float32, device=x.device)
+        dx, dw, db = _xent_outputs(desc, x, shape, bias, need)
+        ws = _xent_workspace(desc, PP_XENT_FWD | PP_XENT_BWD, x.device)
+    _check(load_library().pp_xent_step(ctypes.byref(desc), _p(x), _p(w), _p(bias), _p(class_weight), _p(target), _p(grad),
+                                       _p(loss), _p(stats), _p(dx), _p(dw), _p(db), _p(ws), ws.numel(),
+                                       _stream_ptr(stream)), "pp_xent_step")
+    return loss, dx, dw, db
