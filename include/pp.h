@@ -562,6 +562,78 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
                        float* stats, void* dx, void* dw, float* db, void* workspace, size_t ws_bytes,
                        void* hip_stream);
 
+/*
+ * Orthogonalised updates.  A layer's update U (rows x cols: output channels by
+ * input channels times taps) is replaced by its Newton-Schulz iterate: with
+ * X = U / (|U| + eps) (|.| the square root of the sum of squares), `steps` times
+ *   A = X X^T,  X <- a X + (b A + c A A) X          (coeffs = {a, b, c})
+ * which keeps U's singular vectors and takes each singular value s of X to
+ * a s + b s^3 + c s^5, towards 1 (a matrix with more rows than columns is
+ * handled as its transpose: the same result).  The values are held as pairs of
+ * fp16 values (22 bits) between the products, whose sums are fp32; for bf16
+ * matrices X enters the products with 11 bits, an error of about 1e-3 of the
+ * result.  The sum of squares is taken in 64 bits.  U = 0 gives 0; a NaN or an
+ * infinity in U makes its result NaN.
+ * Coefficients: those that keep singular values of 0..1 within -2..2 on every
+ * step and |b s^2| and |b s^2 + c s^4| at most 48, e.g. {3.4445, -4.7750,
+ * 2.0315}, {1.875, -1.25, 0.375}, {1.5, -0.5, 0}; others PP_EUNSUPPORTED.
+ *
+ * pp_ortho -- all matrices of a list in one call (each stage of the iteration
+ * is one launch over all of them).  u and o may be the same.
+ *   mats, count   host array (read during the call); a matrix without
+ *                 elements is skipped
+ *   dtype         pp_dtype of every u and o
+ *   steps         1..64
+ *   workspace     256-byte aligned, pp_ortho_workspace() bytes
+ * pp_muon_step -- the weight step of a list of layers:
+ *   M' = momentum M + G
+ *   U  = G + momentum M' (nesterov) or M'
+ *   W' = (1 - lr weight_decay) W - lr sqrt(max(1, rows / cols)) O(U)
+ * with O the iterate above.  A pruned layer gives the 9-bit tap mask of each of
+ * its 3x3 kernels (Sec. 2: the pattern of a kept kernel, 0 for a removed one;
+ * bit t = tap t): taps that are off count as 0 in G, and W' and M' are 0 there
+ * whatever W, M and G hold, so the layer stays on its structure.  All arrays
+ * are contiguous [rows][cols]; w_out may be w and momentum_out may be momentum.
+ *   layers, count  host array (read during the call)
+ *   dtype          pp_dtype of w, g and w_out; momentum is fp32
+ * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, a pruned layer's cols
+ * not a multiple of 9, steps, non-finite parameters, negative strides or eps),
+ * PP_EUNSUPPORTED (sizes above 2^21, or 32768 on the shorter side;
+ * coefficients), PP_ESIZE, PP_EHIP.
+ */
+typedef struct {
+  int64_t rows, cols;
+  const void* u;                       /* device; element (r, c) at r u_rs + c u_cs */
+  int64_t u_rs, u_cs;
+  void* o;                             /* device; element (r, c) at r o_rs + c o_cs */
+  int64_t o_rs, o_cs;
+} pp_ortho_mat;
+
+typedef struct {
+  int64_t rows, cols;
+  const void* w;                       /* device                                   */
+  const void* g;                       /* device                                   */
+  const float* momentum;               /* device                                   */
+  void* w_out;                         /* device                                   */
+  float* momentum_out;                 /* device                                   */
+  const uint16_t* keep;                /* device [rows][cols / 9] tap masks, or NULL */
+} pp_muon_layer;
+
+typedef struct {
+  float lr, momentum, weight_decay;
+  int32_t nesterov;
+  int32_t steps;
+  float coeffs[3];
+  float eps;
+} pp_muon_desc;
+
+pp_status pp_ortho_workspace(const pp_ortho_mat* mats, int32_t count, int32_t dtype, size_t* bytes);
+pp_status pp_ortho(const pp_ortho_mat* mats, int32_t count, int32_t dtype, int32_t steps, const float* coeffs,
+                   float eps, void* workspace, size_t ws_bytes, void* hip_stream);
+pp_status pp_muon_workspace(const pp_muon_layer* layers, int32_t count, int32_t dtype, size_t* bytes);
+pp_status pp_muon_step(const pp_muon_layer* layers, int32_t count, int32_t dtype, const pp_muon_desc* desc,
+                       void* workspace, size_t ws_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,7 +36,8 @@ SYMBOLS = ("pp_pack", "pp_blob_info", "pp_conv2d_fwd", "pp_conv2d_workspace", "p
            "pp_project_patterns", "pp_project_connectivity", "pp_project_columns", "pp_column_library",
            "pp_fold_bn", "pp_jit_library", "pp_conv2d_fwd_noalloc", "pp_net_plan", "pp_round_bf16",
            "pp_conv2d_prepare", "pp_conv2d_fwd_prepared", "pp_conv2d_scratch",
-           "pp_xent_workspace", "pp_xent_fwd", "pp_xent_bwd", "pp_xent_step")
+           "pp_xent_workspace", "pp_xent_fwd", "pp_xent_bwd", "pp_xent_step", "pp_ortho_workspace", "pp_ortho",
+           "pp_muon_workspace", "pp_muon_step")
 
 
 class PPError(RuntimeError):
@@ -624,4 +625,5 @@ class Net:
 
 
 from . import train   # noqa: E402  (uses the helpers above)
-from .train import linear_xent_bwd, linear_xent_fwd, linear_xent_step   # noqa: E402,F401
+from .train import (keep_masks, linear_xent_bwd, linear_xent_fwd, linear_xent_step, muon_step,   # noqa: E402,F401
+                    orthogonalize)

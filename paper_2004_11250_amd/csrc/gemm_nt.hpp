@@ -91,6 +91,12 @@ __device__ __forceinline__ void gemm_dma(u32x4_t rsrc, uint32_t voff, uint32_t l
 // the wave's DMAs have landed and its LDS reads are done; then all waves meet
 __device__ __forceinline__ void gemm_sync() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// A value that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+  return static_cast<uint64_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32))) << 32 |
+         static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
+}
+
 template <class T, int BM_, int BN_, int WM_, int WN_>
 struct GemmTile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
@@ -136,10 +142,19 @@ struct GemmTile {
       vb[i] = col0 + r < B.rows ? static_cast<uint32_t>(r * static_cast<int>(B.ld) * 2) + piece : 0x80000000u;
     }
     const int64_t offa = (static_cast<int64_t>(row0) * A.ld + k0) * 2, offb = (static_cast<int64_t>(col0) * B.ld + k0) * 2;
+    uint64_t pa[kMaxPlanes], pb[kMaxPlanes];
+#pragma unroll
+    for (int q = 0; q < kMaxPlanes; ++q) {
+      pa[q] = uniform64(reinterpret_cast<uint64_t>(A.plane[q]) + offa);
+      pb[q] = uniform64(reinterpret_cast<uint64_t>(B.plane[q]) + offb);
+    }
+    ksteps = __builtin_amdgcn_readfirstlane(ksteps);
     int pair = s0 / ksteps, kk = s0 - pair * ksteps;
 
-    auto rsrc = [](const void* p, int64_t off) {
-      const uint64_t b = reinterpret_cast<uint64_t>(p) + off;
+    // (the base is a sum taken in scalar registers, so the DMA has no vector
+    // instruction's result to wait for)
+    auto rsrc = [](uint64_t p, int64_t off) {
+      const uint64_t b = p + off;
       u32x4_t r;
       r.x = static_cast<uint32_t>(b);
       r.y = static_cast<uint32_t>(b >> 32) & 0xFFFFu;
@@ -150,7 +165,8 @@ struct GemmTile {
     auto fetch = [&](uint32_t buf) {
       const uint32_t c = pairs.code >> (4 * pair);
       const int64_t ko = static_cast<int64_t>(kk) * (kBK * 2);
-      const u32x4_t ra = rsrc(A.plane[c & 3], offa + ko), rb = rsrc(B.plane[c >> 2 & 3], offb + ko);
+      auto plane = [](const uint64_t (&p)[kMaxPlanes], uint32_t q) { return q == 0 ? p[0] : q == 1 ? p[1] : p[2]; };
+      const u32x4_t ra = rsrc(plane(pa, c & 3), ko), rb = rsrc(plane(pb, c >> 2 & 3), ko);
 #pragma unroll
       for (int i = 0; i < QA; ++i) gemm_dma(ra, va[i], buf + 1024u * (NW * i + wv));
 #pragma unroll
@@ -184,6 +200,72 @@ struct GemmTile {
           for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
       }
       cur = LDS_STEP - cur;
+    }
+  }
+
+  // After run(): the accumulators by way of LDS, for stores along rows or
+  // columns (a lane holds four rows of a column, too short a piece for
+  // either).  Each wave has a region of its own, of CR x CC values; f(row,
+  // col, View) is called for each CR x CC part of the wave's tile, whose first
+  // element is (row, col) of the workgroup's tile.
+  static constexpr int CR = TM < 64 ? TM : 64, CC = TN;
+  static constexpr int PIECES = CR * CC / 8 / 64;   // pieces of eight values a lane takes
+  static_assert(CC <= 64 && CR * CC * 4 * NW <= static_cast<int>(LDS_BYTES), "staging area");
+  struct View {
+    float* at;
+    // where element (r, c) lies: columns in groups of 16 are turned round
+    // with r / 4, so that the four row groups a wave writes at once lie in
+    // different banks
+    static __device__ __forceinline__ int place(int r, int c) { return r * CC + (c ^ ((r >> 2 & (CC / 16 - 1)) << 4)); }
+    // the i-th piece of this lane: eight columns of a row ...
+    static __device__ __forceinline__ void row_piece(int i, int* r, int* c) {
+      const int k = i * 64 + lane();
+      *r = k / (CC / 8), *c = k % (CC / 8) * 8;
+    }
+    // ... or eight rows of a column
+    static __device__ __forceinline__ void col_piece(int i, int* r, int* c) {
+      const int k = i * 64 + lane();
+      *c = k / (CR / 8), *r = k % (CR / 8) * 8;
+    }
+    __device__ __forceinline__ void row(int r, int c, float (&v)[8]) const {
+      const f32x4* q = reinterpret_cast<const f32x4*>(at + place(r, c));
+      const f32x4 a = q[0], b = q[1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+    }
+    __device__ __forceinline__ void put_row(int r, int c, const float (&v)[8]) const {
+      f32x4* q = reinterpret_cast<f32x4*>(at + place(r, c));
+      q[0] = f32x4{v[0], v[1], v[2], v[3]};
+      q[1] = f32x4{v[4], v[5], v[6], v[7]};
+    }
+    __device__ __forceinline__ void col(int r, int c, float (&v)[8]) const {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = at[place(r + e, c)];
+    }
+    // what lanes wrote is read by others from here on (one wave's LDS
+    // accesses are done in order: only the compiler has to keep it)
+    static __device__ __forceinline__ void turn() {
+      __builtin_amdgcn_wave_barrier();
+      asm volatile("" ::: "memory");
+    }
+  };
+  template <class F>
+  static __device__ __forceinline__ void staged(uint8_t* lds, const f32x4 (&acc)[FM][FN], F&& f) {
+    gemm_sync();   // (every wave is done with the operands)
+    const int ln = lane(), wv = wave();
+    const View view = {reinterpret_cast<float*>(lds) + wv * (CR * CC)};
+#pragma unroll
+    for (int part = 0; part < TM / CR; ++part) {
+#pragma unroll
+      for (int i = 0; i < CR / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            view.at[View::place(16 * i + 4 * (ln >> 4) + e, 16 * j + (ln & 15))] = acc[part * (CR / 16) + i][j][e];
+      View::turn();
+      f((wv / WN) * TM + part * CR, (wv % WN) * TN, view);
+      View::turn();
     }
   }
 };

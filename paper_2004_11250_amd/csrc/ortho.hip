@@ -1,0 +1,676 @@
+// ortho.hip -- pp_ortho / pp_muon_step: updates orthogonalised by
+// Newton-Schulz products, and the weight step of (pruned) layers with them.
+//
+//   X = U / (|U|_F + eps), turned so that it has m <= n rows, then `steps` times
+//   A = X X^T,  B = b A + c A^2,  X <- a X + B X
+//
+// so every singular value s of X goes to a s + b s^3 + c s^5, towards 1.
+//
+// Numbers.  Small singular values grow by about a factor a a step, and with
+// them what was rounded off X, A and B: 16 bits a value would leave errors of
+// a few per cent.  X, A and B are therefore kept as pairs of fp16 values
+// (22 bits; the values' range is known, so a fixed power of two keeps them
+// clear of fp16's ends), products are summed in fp32, and
+//   fp32 updates   take three plane products each (all but rest x rest);
+//   bf16 updates   use only the upper fp16 value of X inside the products
+//                  (a X is taken from both), and both of A and B: about 1e-3
+//                  of the result, below the output's own rounding.
+//
+// All matrices of a call go through each stage in one launch: a sum of
+// squares, the scaling, and three products a step.  A and B are symmetric:
+// only the tiles on and below the diagonal are computed, and written twice.
+// X is kept in both orders, since A sums over n and B X over m.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <string>
+#include <vector>
+
+#include "api_internal.hpp"
+#include "gemm_nt.hpp"
+#include "train.hpp"
+
+namespace pp {
+namespace {
+
+using half_t = _Float16;
+
+// X, A and B are stored times these
+constexpr float kSX = 8192.f, kSA = 4096.f, kSB = 1024.f;
+
+enum { kStageNorm = 0, kStageFill, kStageGram, kStageApply, kStages };
+
+struct Mat {
+  // the update (r, c), r < rows, c < cols
+  const void* u;
+  int64_t u_rs, u_cs;
+  void* o;
+  int64_t o_rs, o_cs;
+  // the weight step (rows x cols contiguous); g null: only orthogonalise
+  const void* g;
+  const float* mom;
+  const void* w;
+  void* w_out;
+  float* mom_out;
+  const uint16_t* keep;
+  float up;                     // lr times the layer's scale
+  int32_t rows, cols;
+  int32_t turned;               // X is the transpose: m = cols, n = rows
+  int32_t m, n, mp, np;
+  int32_t chunk, chunks;        // elements a workgroup of the sum of squares takes
+  half_t* xr;                   // [2 planes][m][np]
+  half_t* xt[2];                // [planes][n][mp], two in turn
+  half_t* a;                    // [2][m][mp]
+  half_t* b;                    // [2][m][mp]
+  double* part;                 // [chunks]
+};
+
+struct Step {
+  float lr, momentum, decay;
+  int32_t nesterov;
+  float a, b, c, eps;
+  int32_t steps;
+};
+
+constexpr int kSetup = 12;      // matrices a set-up launch brings (kernel arguments hold 4 KB)
+struct Setup {
+  Mat mat[kSetup];
+  int32_t start[kStages][kSetup];
+  int32_t first, count, all;
+};
+
+// The plan in device memory: all matrices, and for each stage the first tile
+// of each.
+struct Table {
+  const Mat* mat;
+  const int32_t* start;         // [kStages][all]
+  int32_t all;
+};
+
+__global__ __launch_bounds__(256) void setup_kernel(Setup s, Mat* mat, int32_t* start) {
+  const int words = s.count * static_cast<int>(sizeof(Mat) / 4);
+  const uint32_t* from = reinterpret_cast<const uint32_t*>(s.mat);
+  uint32_t* to = reinterpret_cast<uint32_t*>(mat + s.first);
+  for (int i = threadIdx.x; i < words; i += 256) to[i] = from[i];
+  for (int i = threadIdx.x; i < kStages * s.count; i += 256) {
+    const int k = i / s.count, j = i - k * s.count;
+    start[k * s.all + s.first + j] = s.start[k][j];
+  }
+}
+
+// The matrix that tile `id` of a stage belongs to; *local: its tile there.
+__device__ __forceinline__ int find(const Table& t, int stage, int id, int* local) {
+  const int32_t* st = t.start + stage * t.all;
+  int at = -1;
+  for (int i = 0; i < t.all; i += 64) {
+    const int k = i + (threadIdx.x & 63);
+    const bool below = k < t.all && st[k] <= id;
+    at += __popcll(__ballot(below));
+  }
+  at = __builtin_amdgcn_readfirstlane(at);
+  *local = id - __builtin_amdgcn_readfirstlane(st[at]);
+  return at;
+}
+
+__device__ __forceinline__ bool kept(const Mat& m, int64_t e) {
+  if (!m.keep) return true;
+  const int64_t k = e / 9;
+  return m.keep[k] >> static_cast<int>(e - 9 * k) & 1;
+}
+
+// element e of a weight step's update, from the new momentum
+template <class S>
+__device__ __forceinline__ float update_of(const Mat& m, const Step& s, int64_t e) {
+  const float mom = m.mom_out[e];
+  if (!s.nesterov) return mom;
+  const float g = kept(m, e) ? static_cast<float>(static_cast<const S*>(m.g)[e]) : 0.f;
+  return g + s.momentum * mom;
+}
+
+// The sum of squares of each matrix, in 64 bits, a chunk a workgroup; a
+// weight step's momentum on the way.
+template <class S>
+__global__ __launch_bounds__(256) void norm_kernel(Table t, Step s) {
+  __shared__ double sums[4];
+  int chunk;
+  const Mat& m = t.mat[find(t, kStageNorm, blockIdx.x, &chunk)];
+  const int64_t all = static_cast<int64_t>(m.rows) * m.cols, e0 = static_cast<int64_t>(chunk) * m.chunk;
+  const int64_t e1 = e0 + m.chunk < all ? e0 + m.chunk : all;
+  double sum = 0.;
+  if (m.g) {
+    for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
+      float g = 0.f, mom = 0.f;
+      if (kept(m, e)) {
+        g = static_cast<float>(static_cast<const S*>(m.g)[e]);
+        mom = s.momentum * m.mom[e] + g;
+      }
+      m.mom_out[e] = mom;
+      const float u = s.nesterov ? g + s.momentum * mom : mom;
+      sum += static_cast<double>(u) * u;
+    }
+  } else {
+    for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
+      const int64_t r = e / m.cols, c = e - r * m.cols;
+      const float u = static_cast<float>(static_cast<const S*>(m.u)[r * m.u_rs + c * m.u_cs]);
+      sum += static_cast<double>(u) * u;
+    }
+  }
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) m.part[chunk] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+__device__ __forceinline__ void split(float x, half_t* h, half_t* l) {
+  *h = static_cast<half_t>(x);
+  *l = static_cast<half_t>(x - static_cast<float>(*h));
+}
+
+// X = U / (|U| + eps), in both orders, padded with zeros.
+template <class S, int P>
+__global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
+  __shared__ float tile[64][65];
+  __shared__ double sums[4];
+  int id;
+  const Mat& m = t.mat[find(t, kStageFill, blockIdx.x, &id)];
+  const int tid = threadIdx.x;
+  double sum = 0.;
+  for (int i = tid; i < m.chunks; i += 256) sum += m.part[i];
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if ((tid & 63) == 0) sums[tid >> 6] = sum;
+  __syncthreads();
+  const float scale = static_cast<float>(kSX / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + static_cast<double>(s.eps)));
+
+  const int tc = m.np / 64, r0 = id / tc * 64, c0 = id % tc * 64;
+  const bool along_n = m.g ? !m.turned : (m.turned ? m.u_rs : m.u_cs) == 1;   // consecutive along n in memory
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int x = tid & 63, y = (tid >> 6) + 4 * i;
+    const int r = along_n ? y : x, c = along_n ? x : y;
+    float u = 0.f;
+    if (r0 + r < m.m && c0 + c < m.n) {
+      const int64_t ur = m.turned ? c0 + c : r0 + r, uc = m.turned ? r0 + r : c0 + c;
+      u = m.g ? update_of<S>(m, s, ur * m.cols + uc) : static_cast<float>(static_cast<const S*>(m.u)[ur * m.u_rs + uc * m.u_cs]);
+    }
+    tile[r][c] = u * scale;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
+    f16x8 h, l;
+    if (r0 + u < m.m) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        half_t a, b;
+        split(tile[u][w + e], &a, &b);
+        h[e] = a, l[e] = b;
+      }
+      half_t* at = m.xr + static_cast<int64_t>(r0 + u) * m.np + c0 + w;
+      *reinterpret_cast<f16x8*>(at) = h;
+      *reinterpret_cast<f16x8*>(at + static_cast<int64_t>(m.m) * m.np) = l;
+    }
+    if (c0 + u < m.n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        half_t a, b;
+        split(tile[w + e][u], &a, &b);
+        h[e] = a, l[e] = b;
+      }
+      if (r0 + w < m.mp) {
+        half_t* at = m.xt[0] + static_cast<int64_t>(c0 + u) * m.mp + r0 + w;
+        *reinterpret_cast<f16x8*>(at) = h;
+        if constexpr (P > 1) *reinterpret_cast<f16x8*>(at + static_cast<int64_t>(m.n) * m.mp) = l;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ GemmOperand planes_of(const half_t* p, int rows, int ld) {
+  GemmOperand o;
+  o.plane[0] = p;
+  o.plane[1] = p + static_cast<int64_t>(rows) * ld;
+  o.plane[2] = p;
+  o.ld = __builtin_amdgcn_readfirstlane(ld);
+  o.rows = __builtin_amdgcn_readfirstlane(rows);
+  return o;
+}
+
+// Tile t of the lower triangle, row by row.
+__device__ __forceinline__ void triangle(int t, int* ti, int* tj) {
+  int r = static_cast<int>((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+  while (r * (r + 1) / 2 > t) --r;
+  while ((r + 1) * (r + 2) / 2 <= t) ++r;
+  *ti = r;
+  *tj = t - r * (r + 1) / 2;
+}
+
+__device__ __forceinline__ void split8(const float (&v)[8], f16x8* h, f16x8* l) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    half_t a, b;
+    split(v[e], &a, &b);
+    (*h)[e] = a, (*l)[e] = b;
+  }
+}
+// a pair of fp16 values as one
+__device__ __forceinline__ void pair8(const half_t* h, int64_t plane, float (&v)[8]) {
+  const f16x8 a = *reinterpret_cast<const f16x8*>(h), b = *reinterpret_cast<const f16x8*>(h + plane);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(a[e]) + static_cast<float>(b[e]);
+}
+
+// A = X X^T (POLY false) or B = b A + c A A^T (POLY true)
+template <class Tile, bool POLY>
+__global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, PlanePairs pairs) {
+  __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
+  int id;
+  const Mat& m = t.mat[find(t, kStageGram, blockIdx.x, &id)];
+  int ti, tj;
+  triangle(id, &ti, &tj);
+  const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
+  const GemmOperand x = POLY ? planes_of(m.a, m.m, m.mp) : planes_of(m.xr, m.m, m.np);
+  const int ksteps = (POLY ? m.mp : m.np) / kBK;
+  f32x4 acc[Tile::FM][Tile::FN];
+  Tile::run(x, x, pairs, row0, col0, ksteps, 0, 0, ksteps * pairs.n, lds, acc);
+  const int mm = m.m, mp = m.mp;
+  const int64_t plane = static_cast<int64_t>(mm) * mp;
+  const half_t* a = m.a;
+  half_t* out = POLY ? m.b : m.a;
+  const float fa = s.b * (kSB / kSA), fc = POLY ? s.c * (kSB / (kSA * kSA)) : kSA / (kSX * kSX);
+  // (rows past m are zeros in both operands, so the padding comes out as zeros)
+  auto store = [&](int64_t at, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= fc;
+    if constexpr (POLY) {
+      float o[8];
+      pair8(a + at, plane, o);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += fa * o[e];
+    }
+    f16x8 h, l;
+    split8(v, &h, &l);
+    *reinterpret_cast<f16x8*>(out + at) = h;
+    *reinterpret_cast<f16x8*>(out + at + plane) = l;
+  };
+  Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
+#pragma unroll 2
+    for (int i = 0; i < Tile::PIECES; ++i) {
+      int r, c;
+      float v[8];
+      view.row_piece(i, &r, &c);
+      view.row(r, c, v);
+      r += row0 + rb, c += col0 + cb;
+      if (r < mm && c < mp) store(static_cast<int64_t>(r) * mp + c, v);
+    }
+    if (ti != tj) {
+#pragma unroll 2
+      for (int i = 0; i < Tile::PIECES; ++i) {
+        int r, c;
+        float v[8];
+        view.col_piece(i, &r, &c);
+        view.col(r, c, v);
+        r += row0 + rb, c += col0 + cb;
+        if (c < mm && r < mp) store(static_cast<int64_t>(c) * mp + r, v);
+      }
+    }
+  });
+}
+
+// results (r, c) .. (r, c + 7) of a matrix, of which n are there
+template <class S>
+__device__ __forceinline__ void put_result(const Mat& m, const Step& s, int r, int c, int n, const float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (e >= n) break;
+    const int ur = r, uc = c + e;
+    if (m.g) {
+      const int64_t k = static_cast<int64_t>(ur) * m.cols + uc;
+      float w = 0.f;
+      if (kept(m, k)) w = (1.f - s.lr * s.decay) * static_cast<float>(static_cast<const S*>(m.w)[k]) - m.up * v[e];
+      static_cast<S*>(m.w_out)[k] = static_cast<S>(w);
+    } else {
+      static_cast<S*>(m.o)[ur * m.o_rs + uc * m.o_cs] = static_cast<S>(v[e]);
+    }
+  }
+}
+
+// X <- a X + B X; the last one writes the result instead: the orthogonalised
+// update, or the weights.
+template <class Tile, class S, int P, bool LAST>
+__global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, PlanePairs pairs, int32_t turn) {
+  __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
+  int id;
+  const Mat& m = t.mat[find(t, kStageApply, blockIdx.x, &id)];
+  const int mm = m.m, nn = m.n, mp = m.mp, np = m.np;
+  int ti, tj;
+  band_order(id, (mm + Tile::BM - 1) / Tile::BM, (nn + Tile::BN - 1) / Tile::BN, &ti, &tj);
+  const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
+  const int ksteps = mp / kBK;
+  f32x4 acc[Tile::FM][Tile::FN];
+  Tile::run(planes_of(m.b, mm, mp), planes_of(m.xt[turn], nn, mp), pairs, row0, col0, ksteps, 0, 0, ksteps * pairs.n, lds, acc);
+  const int64_t plane = static_cast<int64_t>(mm) * np, tplane = static_cast<int64_t>(nn) * mp;
+  half_t *xr = m.xr, *xt = m.xt[turn ^ 1];
+  const bool turned = m.turned;
+  Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
+    rb += row0, cb += col0;
+#pragma unroll 2
+    for (int i = 0; i < Tile::PIECES; ++i) {
+      int r, c;
+      view.row_piece(i, &r, &c);
+      if (rb + r >= mm || cb + c >= np) continue;
+      float v[8], x[8];
+      view.row(r, c, v);
+      const int64_t at = static_cast<int64_t>(rb + r) * np + cb + c;
+      pair8(xr + at, plane, x);
+      const float fb = LAST ? 1.f / (kSB * kSX) : 1.f / kSB, fx = LAST ? s.a / kSX : s.a;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fx * x[e] + fb * v[e];
+      if constexpr (LAST) {
+        if (!turned) put_result<S>(m, s, rb + r, cb + c, nn - (cb + c), v);
+      } else {
+        f16x8 h, l;
+        split8(v, &h, &l);
+        *reinterpret_cast<f16x8*>(xr + at) = h;
+        *reinterpret_cast<f16x8*>(xr + at + plane) = l;
+      }
+      if (!LAST || turned) view.put_row(r, c, v);
+    }
+    if (LAST && !turned) return;
+    view.turn();
+#pragma unroll 2
+    for (int i = 0; i < Tile::PIECES; ++i) {
+      int r, c;
+      float v[8];
+      view.col_piece(i, &r, &c);
+      if (cb + c >= nn || rb + r >= mp) continue;
+      view.col(r, c, v);
+      if constexpr (LAST) {
+        put_result<S>(m, s, cb + c, rb + r, mm - (rb + r), v);
+      } else {
+        f16x8 h, l;   // (rows past m are zeros, as B's are)
+        split8(v, &h, &l);
+        const int64_t at = static_cast<int64_t>(cb + c) * mp + rb + r;
+        *reinterpret_cast<f16x8*>(xt + at) = h;
+        if constexpr (P > 1) *reinterpret_cast<f16x8*>(xt + at + tplane) = l;
+      }
+    }
+  });
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+
+using Big = GemmTile<half_t, 256, 256, 2, 4>;
+using Mid = GemmTile<half_t, 128, 128, 2, 2>;
+using Small = GemmTile<half_t, 64, 64, 2, 2>;
+constexpr int kTile[] = {256, 128, 64};
+
+struct Plan {
+  std::vector<Mat> mats;
+  int gram = 2, apply = 2;      // tiles
+  int64_t blocks[kStages] = {};
+  std::vector<int32_t> start[kStages];
+  size_t table = 0, total = 0;
+};
+
+// The largest tile that gives most CUs one, over all matrices.
+template <class F>
+int pick(F&& tiles) {
+  for (int k = 0; k < 2; ++k)
+    if (tiles(kTile[k]) >= 200) return k;
+  return 2;
+}
+
+// Fills in sizes and workspace places (as offsets from `ws`).
+pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
+  const int planes = dtype == PP_BF16 ? 1 : 2;
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    const size_t r = at;
+    at += (n + 255) / 256 * 256;
+    return r;
+  };
+  for (Mat& m : p->mats) {
+    m.turned = m.rows > m.cols;
+    m.m = std::min(m.rows, m.cols), m.n = std::max(m.rows, m.cols);
+    m.mp = static_cast<int32_t>(pad64(m.m)), m.np = static_cast<int32_t>(pad64(m.n));
+    const int64_t all = static_cast<int64_t>(m.rows) * m.cols;
+    m.chunk = static_cast<int32_t>(std::max<int64_t>(4096, cdiv(cdiv(all, 256), 256) * 256));
+    m.chunks = static_cast<int32_t>(cdiv(all, m.chunk));
+  }
+  // long sums first, so that the longest tiles do not start last
+  std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
+  auto sum = [&](auto&& f) {
+    int64_t n = 0;
+    for (const Mat& m : p->mats) n += f(m);
+    return n;
+  };
+  auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.m, t); return k * (k + 1) / 2; };
+  auto rect = [](const Mat& m, int t) { return cdiv(m.m, t) * cdiv(m.n, t); };
+  p->gram = pick([&](int t) { return sum([&](const Mat& m) { return tri(m, t); }); });
+  p->apply = pick([&](int t) { return sum([&](const Mat& m) { return rect(m, t); }); });
+  for (Mat& m : p->mats) {
+    const int64_t n[kStages] = {m.chunks, static_cast<int64_t>(m.mp / 64) * (m.np / 64), tri(m, kTile[p->gram]), rect(m, kTile[p->apply])};
+    for (int k = 0; k < kStages; ++k) {
+      p->start[k].push_back(static_cast<int32_t>(p->blocks[k]));
+      p->blocks[k] += n[k];
+      if (p->blocks[k] > (1 << 30)) return fail(PP_EUNSUPPORTED, "too many matrices, or too large, for one call");
+    }
+    const size_t xn = static_cast<size_t>(m.m) * m.np * 2, tn = static_cast<size_t>(m.n) * m.mp * 2, an = static_cast<size_t>(m.m) * m.mp * 2;
+    m.xr = reinterpret_cast<half_t*>(ws + take(2 * xn));
+    m.xt[0] = reinterpret_cast<half_t*>(ws + take(planes * tn));
+    m.xt[1] = reinterpret_cast<half_t*>(ws + take(planes * tn));
+    m.a = reinterpret_cast<half_t*>(ws + take(2 * an));
+    m.b = reinterpret_cast<half_t*>(ws + take(2 * an));
+    m.part = reinterpret_cast<double*>(ws + take(m.chunks * 8));
+  }
+  p->table = take(p->mats.size() * (sizeof(Mat) + kStages * 4));
+  p->total = std::max<size_t>(at, 256);
+  return PP_OK;
+}
+
+template <bool POLY>
+void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, hipStream_t st) {
+  const dim3 grid(static_cast<uint32_t>(p.blocks[kStageGram]));
+  if (p.gram == 0)
+    hipLaunchKernelGGL((gram_kernel<Big, POLY>), grid, dim3(Big::THREADS), 0, st, t, s, pairs);
+  else if (p.gram == 1)
+    hipLaunchKernelGGL((gram_kernel<Mid, POLY>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs);
+  else
+    hipLaunchKernelGGL((gram_kernel<Small, POLY>), grid, dim3(Small::THREADS), 0, st, t, s, pairs);
+}
+
+template <class S, int P, bool LAST>
+void apply(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
+  const dim3 grid(static_cast<uint32_t>(p.blocks[kStageApply]));
+  if (p.apply == 0)
+    hipLaunchKernelGGL((apply_kernel<Big, S, P, LAST>), grid, dim3(Big::THREADS), 0, st, t, s, pairs, turn);
+  else if (p.apply == 1)
+    hipLaunchKernelGGL((apply_kernel<Mid, S, P, LAST>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs, turn);
+  else
+    hipLaunchKernelGGL((apply_kernel<Small, S, P, LAST>), grid, dim3(Small::THREADS), 0, st, t, s, pairs, turn);
+}
+
+template <class S, int P>
+pp_status enqueue(const Plan& p, const Step& s, uint8_t* ws, hipStream_t st) {
+  Mat* mats = reinterpret_cast<Mat*>(ws + p.table);
+  int32_t* start = reinterpret_cast<int32_t*>(mats + p.mats.size());
+  const int all = static_cast<int>(p.mats.size());
+  for (int first = 0; first < all; first += kSetup) {
+    Setup su;
+    su.first = first, su.count = std::min(kSetup, all - first), su.all = all;
+    for (int i = 0; i < su.count; ++i) {
+      su.mat[i] = p.mats[first + i];
+      for (int k = 0; k < kStages; ++k) su.start[k][i] = p.start[k][first + i];
+    }
+    hipLaunchKernelGGL(setup_kernel, dim3(1), dim3(256), 0, st, su, mats, start);
+  }
+  const Table t = {mats, start, all};
+  hipLaunchKernelGGL((norm_kernel<S>), dim3(static_cast<uint32_t>(p.blocks[kStageNorm])), dim3(256), 0, st, t, s);
+  hipLaunchKernelGGL((fill_kernel<S, P>), dim3(static_cast<uint32_t>(p.blocks[kStageFill])), dim3(256), 0, st, t, s);
+  for (int k = 0; k < s.steps; ++k) {
+    gram<false>(p, t, s, P == 1 ? kPairs1 : kPairs3, st);
+    gram<true>(p, t, s, kPairs3, st);
+    if (k + 1 < s.steps)
+      apply<S, P, false>(p, t, s, P == 1 ? kPairs2 : kPairs3, k & 1, st);
+    else
+      apply<S, P, true>(p, t, s, P == 1 ? kPairs2 : kPairs3, k & 1, st);
+  }
+  return launched();
+}
+
+// The coefficients have to keep singular values of 0..1 within 0..2 and the
+// intermediate matrices within their stored range.
+pp_status check_step(const Step& s) {
+  if (s.steps < 1 || s.steps > 64) return fail(PP_EINVAL, "steps must be 1..64");
+  for (float v : {s.a, s.b, s.c, s.eps, s.lr, s.momentum, s.decay})
+    if (!std::isfinite(v)) return fail(PP_EINVAL, "parameters must be finite");
+  if (s.eps < 0) return fail(PP_EINVAL, "eps must be >= 0");
+  for (int i = 0; i <= 2048; ++i) {
+    double x = i / 2048.;
+    for (int k = 0; k < s.steps; ++k) {
+      const double g = x * x, b = s.b * g + s.c * g * g;
+      if (std::fabs(b) > 48. || std::fabs(s.b * g) > 48.) return fail(PP_EUNSUPPORTED, "coefficients too large");
+      x = s.a * x + b * x;
+      if (std::fabs(x) > 2.) return fail(PP_EUNSUPPORTED, "the coefficients let singular values leave 0..2");
+    }
+  }
+  return PP_OK;
+}
+
+pp_status run(Plan* p, int32_t dtype, const Step& s, void* workspace, size_t ws_bytes, void* hip_stream) {
+  if (p->mats.empty()) return PP_OK;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256) return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
+  const pp_status st = make_plan(p, dtype, static_cast<uint8_t*>(workspace));
+  if (st != PP_OK) return st;
+  if (ws_bytes < p->total) return fail(PP_ESIZE, "workspace smaller than needed");
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return dtype == PP_BF16 ? enqueue<__bf16, 1>(*p, s, static_cast<uint8_t*>(workspace), stream)
+                          : enqueue<float, 2>(*p, s, static_cast<uint8_t*>(workspace), stream);
+}
+
+pp_status check_size(int64_t rows, int64_t cols) {
+  if (rows < 0 || cols < 0) return fail(PP_EINVAL, "negative size");
+  if (rows > (1 << 21) || cols > (1 << 21) || std::min(rows, cols) > 32768)
+    return fail(PP_EUNSUPPORTED, "a matrix may have up to 2^21 rows or columns, and 32768 of the fewer");
+  return PP_OK;
+}
+
+template <class F>
+pp_status guarded(F&& f) {
+  clear_error();
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return fail(PP_EINVAL, std::string("out of host memory: ") + e.what());
+  }
+}
+
+pp_status collect(Plan* p, const pp_ortho_mat* mats, int32_t count, int32_t dtype, bool pointers) {
+  if (count < 0 || (count && !mats)) return fail(PP_EINVAL, "mats is NULL");
+  if (dtype != PP_F32 && dtype != PP_BF16) return fail(PP_EINVAL, "bad dtype");
+  const size_t esz = dtype == PP_BF16 ? 2 : 4;
+  for (int32_t i = 0; i < count; ++i) {
+    const pp_ortho_mat& q = mats[i];
+    const pp_status s = check_size(q.rows, q.cols);
+    if (s != PP_OK) return s;
+    if (q.rows == 0 || q.cols == 0) continue;
+    if (pointers) {
+      if (!q.u || !q.o) return fail(PP_EINVAL, "NULL pointer");
+      if (reinterpret_cast<uintptr_t>(q.u) % esz || reinterpret_cast<uintptr_t>(q.o) % esz) return fail(PP_EINVAL, "misaligned pointer");
+      if (q.u_rs < 0 || q.u_cs < 0 || q.o_rs < 0 || q.o_cs < 0) return fail(PP_EINVAL, "negative stride");
+    }
+    Mat m;
+    std::memset(&m, 0, sizeof(m));
+    m.u = q.u, m.u_rs = q.u_rs, m.u_cs = q.u_cs, m.o = q.o, m.o_rs = q.o_rs, m.o_cs = q.o_cs;
+    m.rows = static_cast<int32_t>(q.rows), m.cols = static_cast<int32_t>(q.cols);
+    p->mats.push_back(m);
+  }
+  return PP_OK;
+}
+
+pp_status collect(Plan* p, const pp_muon_layer* layers, int32_t count, int32_t dtype, bool pointers, float lr) {
+  if (count < 0 || (count && !layers)) return fail(PP_EINVAL, "layers is NULL");
+  if (dtype != PP_F32 && dtype != PP_BF16) return fail(PP_EINVAL, "bad dtype");
+  const size_t esz = dtype == PP_BF16 ? 2 : 4;
+  for (int32_t i = 0; i < count; ++i) {
+    const pp_muon_layer& q = layers[i];
+    const pp_status s = check_size(q.rows, q.cols);
+    if (s != PP_OK) return s;
+    if (q.keep && q.cols % 9) return fail(PP_EINVAL, "a pruned layer has 9 columns for each input channel");
+    if (q.rows == 0 || q.cols == 0) continue;
+    if (pointers) {
+      if (!q.w || !q.g || !q.momentum || !q.w_out || !q.momentum_out) return fail(PP_EINVAL, "NULL pointer");
+      for (const void* v : {q.w, q.g, static_cast<const void*>(q.w_out)})
+        if (reinterpret_cast<uintptr_t>(v) % esz) return fail(PP_EINVAL, "misaligned pointer");
+      for (const void* v : {static_cast<const void*>(q.momentum), static_cast<const void*>(q.momentum_out)})
+        if (reinterpret_cast<uintptr_t>(v) % 4) return fail(PP_EINVAL, "misaligned momentum");
+      if (reinterpret_cast<uintptr_t>(q.keep) % 2) return fail(PP_EINVAL, "misaligned keep");
+    }
+    Mat m;
+    std::memset(&m, 0, sizeof(m));
+    m.g = q.g, m.mom = q.momentum, m.w = q.w, m.w_out = q.w_out, m.mom_out = q.momentum_out, m.keep = q.keep;
+    m.rows = static_cast<int32_t>(q.rows), m.cols = static_cast<int32_t>(q.cols);
+    m.up = static_cast<float>(lr * std::sqrt(std::max(1., static_cast<double>(q.rows) / q.cols)));
+    p->mats.push_back(m);
+  }
+  return PP_OK;
+}
+
+}  // namespace
+}  // namespace pp
+
+using namespace pp;
+
+extern "C" pp_status pp_ortho_workspace(const pp_ortho_mat* mats, int32_t count, int32_t dtype, size_t* bytes) {
+  return guarded([&]() -> pp_status {
+    if (!bytes) return fail(PP_EINVAL, "bytes is NULL");
+    Plan p;
+    pp_status s = collect(&p, mats, count, dtype, false);
+    if (s == PP_OK) s = make_plan(&p, dtype, nullptr);
+    if (s == PP_OK) *bytes = p.mats.empty() ? 0 : p.total;
+    return s;
+  });
+}
+
+extern "C" pp_status pp_ortho(const pp_ortho_mat* mats, int32_t count, int32_t dtype, int32_t steps, const float* coeffs,
+                              float eps, void* workspace, size_t ws_bytes, void* hip_stream) {
+  return guarded([&]() -> pp_status {
+    if (!coeffs) return fail(PP_EINVAL, "coeffs is NULL");
+    const Step s = {0.f, 0.f, 0.f, 0, coeffs[0], coeffs[1], coeffs[2], eps, steps};
+    pp_status st = check_step(s);
+    if (st != PP_OK) return st;
+    Plan p;
+    st = collect(&p, mats, count, dtype, true);
+    return st == PP_OK ? run(&p, dtype, s, workspace, ws_bytes, hip_stream) : st;
+  });
+}
+
+extern "C" pp_status pp_muon_workspace(const pp_muon_layer* layers, int32_t count, int32_t dtype, size_t* bytes) {
+  return guarded([&]() -> pp_status {
+    if (!bytes) return fail(PP_EINVAL, "bytes is NULL");
+    Plan p;
+    pp_status s = collect(&p, layers, count, dtype, false, 0.f);
+    if (s == PP_OK) s = make_plan(&p, dtype, nullptr);
+    if (s == PP_OK) *bytes = p.mats.empty() ? 0 : p.total;
+    return s;
+  });
+}
+
+extern "C" pp_status pp_muon_step(const pp_muon_layer* layers, int32_t count, int32_t dtype, const pp_muon_desc* desc,
+                                  void* workspace, size_t ws_bytes, void* hip_stream) {
+  return guarded([&]() -> pp_status {
+    if (!desc) return fail(PP_EINVAL, "desc is NULL");
+    const Step s = {desc->lr, desc->momentum, desc->weight_decay, desc->nesterov != 0, desc->coeffs[0], desc->coeffs[1],
+                    desc->coeffs[2], desc->eps, desc->steps};
+    pp_status st = check_step(s);
+    if (st != PP_OK) return st;
+    Plan p;
+    st = collect(&p, layers, count, dtype, true, desc->lr);
+    return st == PP_OK ? run(&p, dtype, s, workspace, ws_bytes, hip_stream) : st;
+  });
+}

@@ -245,29 +245,15 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
       const int r = row0 + Tile::row_of(i);
       float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < Tile::FN; ++j) {
-        const int t = col0 + Tile::col_of(j);
-        __bf16 o[4][P];
+      for (int j = 0; j < Tile::FN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float g = 0.f;
-          if (kept[j] && r + e < rows) g = (fast_exp(acc[i][j][e] - lse[j]) - (hit[j] == 16 * i + e ? 1.f : 0.f)) * s[j];
+          // (classes past the end: exp(-inf); they have no target)
+          float g = (fast_exp(acc[i][j][e] - lse[j]) - (hit[j] == 16 * i + e ? 1.f : 0.f)) * s[j];
+          g = kept[j] && r + e < rows ? g : 0.f;
           sum[e] += g;
-          bf16_planes<P>(g, o[e]);
-          if (r + e < rows && t < a.t_pad) {
-#pragma unroll
-            for (int q = 0; q < P; ++q) a.gt[q * a.gt_plane + static_cast<int64_t>(r + e) * a.t_pad + t] = o[e][q];
-          }
+          acc[i][j][e] = g;
         }
-        if (t < nt && r < a.v_pad) {
-#pragma unroll
-          for (int q = 0; q < P; ++q) {
-            using bf16x4 = __attribute__((ext_vector_type(4))) __bf16;
-            *reinterpret_cast<bf16x4*>(a.g + q * a.g_plane + static_cast<int64_t>(t) * a.v_pad + r) =
-                bf16x4{o[0][q], o[1][q], o[2][q], o[3][q]};
-          }
-        }
-      }
       if (a.db_part) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -278,6 +264,37 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
         }
       }
     }
+    auto store = [&](__bf16* to, int64_t plane, const float (&v)[8]) {
+      bf16x8 o[P];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        __bf16 p[P];
+        bf16_planes<P>(v[e], p);
+#pragma unroll
+        for (int q = 0; q < P; ++q) o[q][e] = p[q];
+      }
+#pragma unroll
+      for (int q = 0; q < P; ++q) *reinterpret_cast<bf16x8*>(to + q * plane) = o[q];
+    };
+    Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
+      rb += row0, cb += col0;
+#pragma unroll 2
+      for (int i = 0; i < Tile::PIECES; ++i) {
+        int r, c;
+        float v[8];
+        view.row_piece(i, &r, &c);
+        view.row(r, c, v);
+        if (rb + r < rows && cb + c < a.t_pad) store(a.gt + static_cast<int64_t>(rb + r) * a.t_pad + cb + c, a.gt_plane, v);
+      }
+#pragma unroll 2
+      for (int i = 0; i < Tile::PIECES; ++i) {
+        int r, c;
+        float v[8];
+        view.col_piece(i, &r, &c);
+        view.col(r, c, v);
+        if (cb + c < nt && rb + r < a.v_pad) store(a.g + static_cast<int64_t>(cb + c) * a.v_pad + rb + r, a.g_plane, v);
+      }
+    });
   }
 }
 
@@ -429,23 +446,31 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
   f32x4 acc[Tile::FM][Tile::FN];
   Tile::run(a.a, a.b, a.pairs, row0, col0, a.ksteps, 0, s0, s1, lds, acc);
   const float scale = a.slab ? 1.f : common_scale(a.k);
-#pragma unroll
-  for (int j = 0; j < Tile::FN; ++j) {
-    const int c = col0 + Tile::col_of(j);
-    if (c >= a.b.rows) continue;
-#pragma unroll
-    for (int i = 0; i < Tile::FM; ++i) {
-      const int r = row0 + Tile::row_of(i);
+  Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
+    rb += row0, cb += col0;
+#pragma unroll 2
+    for (int i = 0; i < Tile::PIECES; ++i) {
+      int r, c;
+      float v[8];
+      view.col_piece(i, &r, &c);
+      view.col(r, c, v);
+      r += rb, c += cb;
+      if (c >= a.b.rows) continue;
       if (a.slab) {
-        if (r < a.slab_ld) {   // (a multiple of four)
-          f32x4* at = reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.b.rows + c) * a.slab_ld + r);
-          *at = a.add ? *at + acc[i][j] : acc[i][j];
-        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (r + 4 * h < a.slab_ld) {   // (a multiple of four)
+            f32x4* at = reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.b.rows + c) * a.slab_ld + r + 4 * h);
+            const f32x4 x = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+            *at = a.add ? *at + x : x;
+          }
       } else {
-        store4<O>(a.map, r, c, a.a.rows, acc[i][j] * scale);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          store4<O>(a.map, r + 4 * h, c, a.a.rows, f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]} * scale);
       }
     }
-  }
+  });
 }
 
 template <class O>

@@ -5,6 +5,12 @@ training section, on torch tensors).
 ``linear_xent_fwd`` / ``linear_xent_bwd`` / ``linear_xent_step``
     softmax cross entropy of a 1x1 convolution or fully connected layer over
     any number of classes, and its gradients, without keeping the logits.
+``orthogonalize``
+    a list of updates, each replaced by its Newton-Schulz iterate (singular
+    values taken towards 1).
+``muon_step``
+    momentum, orthogonalised update and weight step of a list of layers; a
+    pruned 3x3 layer (``keep_masks``) stays on its kept taps.
 
 As elsewhere in this package every computation runs in the library's kernels;
 this module checks and marshals arguments, and allocates outputs and scratch
@@ -14,6 +20,8 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+
+import numpy as np
 
 from . import _check, _dtype_code, _stream_ptr, _torch, load_library
 
@@ -29,6 +37,23 @@ class XentDesc(ctypes.Structure):
                 ("dx_sp", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("ignore_index", ctypes.c_int64)]
 
 
+class OrthoMat(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("u", ctypes.c_void_p), ("u_rs", ctypes.c_int64),
+                ("u_cs", ctypes.c_int64), ("o", ctypes.c_void_p), ("o_rs", ctypes.c_int64), ("o_cs", ctypes.c_int64)]
+
+
+class MuonLayer(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("w", ctypes.c_void_p), ("g", ctypes.c_void_p),
+                ("momentum", ctypes.c_void_p), ("w_out", ctypes.c_void_p), ("momentum_out", ctypes.c_void_p),
+                ("keep", ctypes.c_void_p)]
+
+
+class MuonDesc(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_float), ("momentum", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32), ("coeffs", ctypes.c_float * 3),
+                ("eps", ctypes.c_float)]
+
+
 def bind(lib):
     """Argument types of the training calls (a library without them, the
     host-only one, is left as it is)."""
@@ -39,6 +64,10 @@ def bind(lib):
         "pp_xent_fwd": [desc, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "pp_xent_bwd": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "pp_xent_step": [desc, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        "pp_ortho_workspace": [vp, i32, i32, ctypes.POINTER(sz)],
+        "pp_ortho": [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_float), ctypes.c_float, vp, sz, vp],
+        "pp_muon_workspace": [vp, i32, i32, ctypes.POINTER(sz)],
+        "pp_muon_step": [vp, i32, i32, ctypes.POINTER(MuonDesc), vp, sz, vp],
     }
     for name, at in argtypes.items():
         if hasattr(lib, name):
@@ -191,3 +220,133 @@ def linear_xent_step(x, w, target, grad=None, bias=None, class_weight=None, igno
                                        _p(loss), _p(stats), _p(dx), _p(dw), _p(db), _p(ws), ws.numel(),
                                        _stream_ptr(stream)), "pp_xent_step")
     return loss, dx, dw, db
+
+
+# ---------------------------------------------------------------------------
+# orthogonalised updates
+# ---------------------------------------------------------------------------
+
+COEFFS = (3.4445, -4.7750, 2.0315)
+
+
+def _matrix(t, name):
+    """(rows, cols, row stride, column stride) of [rows, ...] taken as a matrix."""
+    if t.dim() < 2:
+        raise ValueError(f"{name} must have two axes or more, got {tuple(t.shape)}")
+    if t.numel() == 0:
+        return t.shape[0], 0, 0, 1
+    if t.dim() > 2:
+        try:
+            t = t.view(t.shape[0], -1)
+        except RuntimeError:
+            raise ValueError(f"the trailing axes of {name} do not lie as one axis in memory (call contiguous())") from None
+    return t.shape[0], t.shape[1], t.stride(0), t.stride(1)
+
+
+def _one_dtype(tensors, name):
+    if not tensors:
+        raise ValueError(f"{name} is empty")
+    dt, dev = tensors[0].dtype, tensors[0].device
+    code = _dtype_code(tensors[0])
+    for t in tensors:
+        if t.dtype != dt or t.device != dev:
+            raise ValueError(f"{name} must be of one dtype and on one device")
+    return code, dev
+
+
+def _coeffs(coeffs):
+    if len(coeffs) != 3:
+        raise ValueError("coeffs must be three numbers")
+    return (ctypes.c_float * 3)(*(float(c) for c in coeffs))
+
+
+def orthogonalize(mats, steps=5, coeffs=COEFFS, eps=1e-7, out=None, stream=None):
+    """pp_ortho: the Newton-Schulz iterate of each update, a tensor or a list of
+    them ([rows, ...], trailing axes taken together; float32 or bfloat16, any
+    strides), all in one call.  Returns contiguous tensors of the same shapes,
+    or fills ``out`` (which may be the inputs)."""
+    torch = _torch()
+    single = torch.is_tensor(mats)
+    mats = [mats] if single else list(mats)
+    code, dev = _one_dtype(mats, "mats")
+    k = _coeffs(coeffs)
+    if out is not None:
+        out = [out] if torch.is_tensor(out) else list(out)
+        if len(out) != len(mats) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != dev
+                                        for o, t in zip(out, mats)):
+            raise ValueError("out must match mats")
+    shapes = [_matrix(t, "a matrix of mats") for t in mats]
+    if dev.type != "cuda":
+        raise ValueError("the tensors must be on a GPU")
+    lib = load_library()
+    with _on(stream, dev):
+        if out is None:
+            out = [torch.empty(t.shape, dtype=t.dtype, device=dev) for t in mats]
+        arr = (OrthoMat * len(mats))()
+        for e, t, o, (r, c, rs, cs) in zip(arr, mats, out, shapes):
+            _, _, ors, ocs = _matrix(o, "a matrix of out")
+            e.rows, e.cols, e.u, e.u_rs, e.u_cs, e.o, e.o_rs, e.o_cs = r, c, t.data_ptr(), rs, cs, o.data_ptr(), ors, ocs
+        nb = ctypes.c_size_t(0)
+        _check(lib.pp_ortho_workspace(arr, len(mats), code, ctypes.byref(nb)), "pp_ortho_workspace")
+        ws = torch.empty(max(nb.value, 256), dtype=torch.uint8, device=dev)
+    _check(lib.pp_ortho(arr, len(mats), code, int(steps), k, float(eps), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+           "pp_ortho")
+    return out[0] if single else out
+
+
+def keep_masks(pattern_id, conn, lib_masks):
+    """int16 [c_out][c_in]: the tap mask of each kernel of a pruned layer (0 where
+    it is removed), for muon_step's ``keep`` (as a tensor on the GPU)."""
+    pid = np.asarray(pattern_id, dtype=np.int64)
+    on = np.asarray(conn)
+    masks = np.asarray(lib_masks, dtype=np.int64)
+    if pid.shape != on.shape or pid.ndim != 2:
+        raise ValueError("pattern_id and conn must be [c_out][c_in]")
+    if np.any((on != 0) & ((pid < 0) | (pid >= len(masks)))):
+        raise ValueError("a kept kernel's pattern is not in the library")
+    return np.where(on != 0, masks[np.clip(pid, 0, len(masks) - 1)], 0).astype(np.int16)
+
+
+def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_decay=0.0, keep=None, steps=5,
+              coeffs=COEFFS, eps=1e-7, out=None, stream=None):
+    """pp_muon_step on lists of tensors (or single ones): weights and grads
+    [rows, ...] of one dtype (float32 or bfloat16), momenta float32 of the same
+    shapes, all contiguous.  ``keep``: None, or for each layer None or the int16
+    tap masks [c_out][c_in] of a pruned 3x3 layer (keep_masks).  Updates weights
+    and momenta in place, or fills ``out`` = (weights, momenta), and returns
+    them."""
+    torch = _torch()
+    single = torch.is_tensor(weights)
+    if single:
+        weights, grads, momenta, keep = [weights], [grads], [momenta], [keep]
+        out = None if out is None else ([out[0]], [out[1]])
+    weights, grads, momenta = list(weights), list(grads), list(momenta)
+    keep = [None] * len(weights) if keep is None else list(keep)
+    code, dev = _one_dtype(weights, "weights")
+    k = _coeffs(coeffs)
+    wo, mo = (weights, momenta) if out is None else (list(out[0]), list(out[1]))
+    if not len(weights) == len(grads) == len(momenta) == len(keep) == len(wo) == len(mo):
+        raise ValueError("weights, grads, momenta, keep and out must be of one length")
+    arr = (MuonLayer * len(weights))()
+    for e, w, g, m, kp, w2, m2 in zip(arr, weights, grads, momenta, keep, wo, mo):
+        for name, t, dt in (("grads", g, w.dtype), ("momenta", m, torch.float32), ("out weights", w2, w.dtype),
+                            ("out momenta", m2, torch.float32), ("weights", w, w.dtype)):
+            if t.shape != w.shape or t.dtype != dt or t.device != dev or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous {dt} of its weights' shape {tuple(w.shape)} and device")
+        r, c, _, _ = _matrix(w, "a weight")
+        if kp is not None and (kp.dtype != torch.int16 or tuple(kp.shape) != tuple(w.shape[:2]) or c != 9 * kp.shape[1]
+                               or not kp.is_contiguous() or kp.device != dev):
+            raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
+        e.rows, e.cols, e.w, e.g, e.momentum = r, c, w.data_ptr(), g.data_ptr(), m.data_ptr()
+        e.w_out, e.momentum_out, e.keep = w2.data_ptr(), m2.data_ptr(), _p(kp)
+    if dev.type != "cuda":
+        raise ValueError("the tensors must be on a GPU")
+    lib = load_library()
+    nb = ctypes.c_size_t(0)
+    _check(lib.pp_muon_workspace(arr, len(weights), code, ctypes.byref(nb)), "pp_muon_workspace")
+    with _on(stream, dev):
+        ws = torch.empty(max(nb.value, 256), dtype=torch.uint8, device=dev)
+    d = MuonDesc(float(lr), float(momentum), float(weight_decay), int(bool(nesterov)), int(steps), k, float(eps))
+    _check(lib.pp_muon_step(arr, len(weights), code, ctypes.byref(d), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
+           "pp_muon_step")
+    return (wo[0], mo[0]) if single else (wo, mo)
