@@ -571,7 +571,7 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  * a s + b s^3 + c s^5, towards 1 (a matrix with more rows than columns is
  * handled as its transpose: the same result).  The values are held as pairs of
  * fp16 values (22 bits) between the products, whose sums are fp32; for bf16
- * matrices X enters the products with 11 bits, an error of about 1e-3 of the
+ * matrices 11 bits of each enter the products, an error of about 1.3e-3 of the
  * result.  The sum of squares is taken in 64 bits.  U = 0 gives 0; a NaN or an
  * infinity in U makes its result NaN.
  * Coefficients: those that keep singular values of 0..1 within -2..2 on every
@@ -598,8 +598,8 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  *   dtype          pp_dtype of w, g and w_out; momentum is fp32
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, a pruned layer's cols
  * not a multiple of 9, steps, non-finite parameters, negative strides or eps),
- * PP_EUNSUPPORTED (sizes above 2^21, or 32768 on the shorter side;
- * coefficients), PP_ESIZE, PP_EHIP.
+ * PP_EUNSUPPORTED (sizes above 2^21, or 32768 on the shorter side, or
+ * 2^31 elements; coefficients), PP_ESIZE, PP_EHIP.
  */
 typedef struct {
   int64_t rows, cols;

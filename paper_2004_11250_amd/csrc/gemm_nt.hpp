@@ -97,15 +97,17 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
          static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_>
+template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PHASED_ = false>
 struct GemmTile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int STAGES = STAGES_;                // steps held in LDS
+  static constexpr bool PHASED = PHASED_;
   static constexpr int NW = WM * WN, THREADS = NW * 64;
   static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
   static constexpr int FM = TM / 16, FN = TN / 16;      // in 16 x 16 blocks
   static constexpr int QA = BM / (8 * NW), QB = BN / (8 * NW);   // DMAs a wave issues for a step
   static constexpr uint32_t LDS_A = BM * kBK * 2, LDS_STEP = (BM + BN) * kBK * 2;
-  static constexpr uint32_t LDS_BYTES = 2 * LDS_STEP;
+  static constexpr uint32_t LDS_BYTES = STAGES * LDS_STEP;
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 16 == 0 && TN % 16 == 0, "tile");
 
   // Row and column of acc[i][j][e] in the tile.  A lane holds four rows that
@@ -115,45 +117,43 @@ struct GemmTile {
   static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
   static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-  // steps [s0, s1) of the flattened (plane pair, k step) range; ksteps k steps
-  // a pair.  k0: first k (a multiple of 8).  lds: LDS_BYTES of shared memory.
-  static __device__ __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0,
-                                             int col0, int ksteps, int64_t k0, int s0, int s1, uint8_t* lds,
-                                             f32x4 (&acc)[FM][FN]) {
-    using Frag = typename Mfma<T>::Frag;
-    const int ln = lane(), wv = wave();
-    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    // per-lane offsets of the DMAs: row 8 (NW i + wave) + lane / 8 of the tile
-    uint32_t va[QA], vb[QB];
-    const uint32_t piece = static_cast<uint32_t>((ln & 7) ^ (ln >> 3)) * 16u;
-#pragma unroll
-    for (int i = 0; i < QA; ++i) {
-      const int r = 8 * (NW * i + wv) + (ln >> 3);
-      va[i] = row0 + r < A.rows ? static_cast<uint32_t>(r * static_cast<int>(A.ld) * 2) + piece : 0x80000000u;
-    }
-#pragma unroll
-    for (int i = 0; i < QB; ++i) {
-      const int r = 8 * (NW * i + wv) + (ln >> 3);
-      vb[i] = col0 + r < B.rows ? static_cast<uint32_t>(r * static_cast<int>(B.ld) * 2) + piece : 0x80000000u;
-    }
-    const int64_t offa = (static_cast<int64_t>(row0) * A.ld + k0) * 2, offb = (static_cast<int64_t>(col0) * B.ld + k0) * 2;
+  // A lane's part of the addresses, and the DMAs of one step.
+  struct Feed {
     uint64_t pa[kMaxPlanes], pb[kMaxPlanes];
-#pragma unroll
-    for (int q = 0; q < kMaxPlanes; ++q) {
-      pa[q] = uniform64(reinterpret_cast<uint64_t>(A.plane[q]) + offa);
-      pb[q] = uniform64(reinterpret_cast<uint64_t>(B.plane[q]) + offb);
-    }
-    ksteps = __builtin_amdgcn_readfirstlane(ksteps);
-    int pair = s0 / ksteps, kk = s0 - pair * ksteps;
+    uint32_t va[QA], vb[QB];
+    uint32_t code;
+    int ksteps, pair, kk, wv;
+    u32x4_t ra, rb;
 
+    __device__ __forceinline__ Feed(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0, int col0,
+                                    int ksteps_, int64_t k0, int s0) {
+      const int ln = lane();
+      wv = wave();
+      // row of DMA i: group i of the wave's groups of eight, and lane / 8
+      const uint32_t piece = static_cast<uint32_t>((ln & 7) ^ (ln >> 3)) * 16u;
+#pragma unroll
+      for (int i = 0; i < QA; ++i) {
+        const int r = 8 * group_a(i, wv) + (ln >> 3);
+        va[i] = row0 + r < A.rows ? static_cast<uint32_t>(r * static_cast<int>(A.ld) * 2) + piece : 0x80000000u;
+      }
+#pragma unroll
+      for (int i = 0; i < QB; ++i) {
+        const int r = 8 * group_b(i, wv) + (ln >> 3);
+        vb[i] = col0 + r < B.rows ? static_cast<uint32_t>(r * static_cast<int>(B.ld) * 2) + piece : 0x80000000u;
+      }
+      const int64_t offa = (static_cast<int64_t>(row0) * A.ld + k0) * 2, offb = (static_cast<int64_t>(col0) * B.ld + k0) * 2;
+#pragma unroll
+      for (int q = 0; q < kMaxPlanes; ++q) {
+        pa[q] = uniform64(reinterpret_cast<uint64_t>(A.plane[q]) + offa);
+        pb[q] = uniform64(reinterpret_cast<uint64_t>(B.plane[q]) + offb);
+      }
+      code = pairs.code;
+      ksteps = __builtin_amdgcn_readfirstlane(ksteps_);
+      pair = s0 / ksteps, kk = s0 - pair * ksteps;
+    }
     // (the base is a sum taken in scalar registers, so the DMA has no vector
     // instruction's result to wait for)
-    auto rsrc = [](uint64_t p, int64_t off) {
+    static __device__ __forceinline__ u32x4_t rsrc(uint64_t p, int64_t off) {
       const uint64_t b = p + off;
       u32x4_t r;
       r.x = static_cast<uint32_t>(b);
@@ -161,30 +161,85 @@ struct GemmTile {
       r.z = 0x7FFFFFFFu;
       r.w = 0x00020000u;
       return r;
-    };
-    auto fetch = [&](uint32_t buf) {
-      const uint32_t c = pairs.code >> (4 * pair);
+    }
+    static __device__ __forceinline__ uint64_t plane(const uint64_t (&p)[kMaxPlanes], uint32_t q) {
+      return q == 0 ? p[0] : q == 1 ? p[1] : p[2];
+    }
+    // descriptors of the next step
+    __device__ __forceinline__ void next() {
+      const uint32_t c = code >> (4 * pair);
       const int64_t ko = static_cast<int64_t>(kk) * (kBK * 2);
-      auto plane = [](const uint64_t (&p)[kMaxPlanes], uint32_t q) { return q == 0 ? p[0] : q == 1 ? p[1] : p[2]; };
-      const u32x4_t ra = rsrc(plane(pa, c & 3), ko), rb = rsrc(plane(pb, c >> 2 & 3), ko);
-#pragma unroll
-      for (int i = 0; i < QA; ++i) gemm_dma(ra, va[i], buf + 1024u * (NW * i + wv));
-#pragma unroll
-      for (int i = 0; i < QB; ++i) gemm_dma(rb, vb[i], buf + LDS_A + 1024u * (NW * i + wv));
+      ra = rsrc(plane(pa, c & 3), ko), rb = rsrc(plane(pb, c >> 2 & 3), ko);
       if (++kk == ksteps) kk = 0, ++pair;
-    };
+    }
+    template <int I>
+    __device__ __forceinline__ void a(uint32_t buf) const { gemm_dma(ra, va[I], buf + 1024u * group_a(I, wv)); }
+    template <int I>
+    __device__ __forceinline__ void b(uint32_t buf) const { gemm_dma(rb, vb[I], buf + LDS_A + 1024u * group_b(I, wv)); }
+    template <int I = 0>
+    __device__ __forceinline__ void all(uint32_t buf) const {
+      if constexpr (I < QA) a<I>(buf);
+      if constexpr (I < QB) b<I>(buf);
+      if constexpr (I + 1 < QA || I + 1 < QB) all<I + 1>(buf);
+    }
+  };
+  // Which group of eight rows DMA i of wave w brings.  In the phased loop DMA
+  // 0 and 1 bring the halves of every wave's rows (columns) that its first
+  // products read, 2 and 3 the others.
+  static __device__ __forceinline__ int group_a(int i, int w) {
+    if constexpr (PHASED) return (i & 1) * (TM / 8) + (i >> 1) * (TM / 16) + w;
+    return NW * i + w;
+  }
+  static __device__ __forceinline__ int group_b(int i, int w) {
+    if constexpr (PHASED) return (2 * (i & 1) + (w >> 2)) * (TN / 8) + (i >> 1) * (TN / 16) + (w & 3);
+    return NW * i + w;
+  }
 
+  using Frag = typename Mfma<T>::Frag;
+
+  // steps [s0, s1) of the flattened (plane pair, k step) range; ksteps k steps
+  // a pair.  k0: first k (a multiple of 8).  lds: LDS_BYTES of shared memory.
+  static __device__ __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0,
+                                             int col0, int ksteps, int64_t k0, int s0, int s1, uint8_t* lds,
+                                             f32x4 (&acc)[FM][FN]) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (s0 >= s1) return;
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
+    Feed feed(A, B, pairs, row0, col0, ksteps, k0, s0);
+    if constexpr (PHASED)
+      phased(feed, s1 - s0, lds, lds0, acc);
+    else
+      ring(feed, s1 - s0, lds, lds0, acc);
+  }
+
+  // A ring of STAGES steps, STAGES - 1 of them in flight; one barrier a step.
+  static __device__ __forceinline__ void ring(Feed& feed, int n, const uint8_t* lds, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
+    const int ln = lane(), wv = wave();
     // a lane's operand of block i, k half h: row 16 i + lane % 16, piece 4 h + lane / 16
     const uint32_t ar = static_cast<uint32_t>((wv / WN) * TM + (ln & 15)) * 128u;
     const uint32_t br = LDS_A + static_cast<uint32_t>((wv % WN) * TN + (ln & 15)) * 128u;
     const uint32_t p0 = static_cast<uint32_t>((ln >> 4) ^ (ln & 7)) * 16u;
-
-    if (s0 >= s1) return;
-    fetch(lds0);
-    uint32_t cur = 0;
-    for (int s = s0; s < s1; ++s) {
-      gemm_sync();
-      if (s + 1 < s1) fetch(lds0 + (LDS_STEP - cur));
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+      if (i < n) {
+        feed.next();
+        feed.all(lds0 + i * LDS_STEP);
+      }
+    uint32_t cur = 0;                              // the step's place in the ring
+    uint32_t put = (STAGES - 1) * LDS_STEP;        // where the step STAGES - 1 on goes: the last one's place
+    for (int s = 0; s < n; ++s) {
+      // this step has landed once at most the later ones' DMAs are in flight
+      if (s + STAGES - 1 <= n)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * (QA + QB)) : "memory");
+      else
+        gemm_sync();
+      if (s + STAGES - 1 < n) {
+        feed.next();
+        feed.all(lds0 + put);
+      }
       const uint8_t* base = lds + cur;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -199,8 +254,97 @@ struct GemmTile {
 #pragma unroll
           for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
       }
+      put = cur;
+      cur = cur + LDS_STEP == LDS_BYTES ? 0 : cur + LDS_STEP;
+    }
+  }
+
+  // Two groups of four waves, one wave of each on every SIMD, half a phase
+  // apart: while one group's waves feed the matrix cores, the other's read
+  // their next operands from LDS and start DMAs.  A step is four phases, each
+  // a quarter of the wave's tile (2 x 2 blocks of FM/2 x FN/2) over the whole
+  // step's k.  What a phase has read is overwritten from the next phase on by
+  // the step after next, so that a DMA has a step and more to land.
+  static __device__ __forceinline__ void phased(Feed& feed, int n, const uint8_t* lds, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
+    static_assert(!PHASED || (NW == 8 && QA == 4 && QB == 4 && TM / 16 == 8 && TN / 16 == 4), "phases");
+    const int ln = lane(), wv = wave();
+    const uint32_t ar = static_cast<uint32_t>((wv / WN) * TM + (ln & 15)) * 128u;
+    const uint32_t br = LDS_A + static_cast<uint32_t>((wv % WN) * TN + (ln & 15)) * 128u;
+    const uint32_t p0 = static_cast<uint32_t>((ln >> 4) ^ (ln & 7)) * 16u;
+    constexpr int HM = FM / 2, HN = FN / 2;
+    feed.next();
+    feed.all(lds0);
+    if (n > 1) {
+      feed.next();
+      feed.all(lds0 + LDS_STEP);
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(QA + QB) : "memory");
+    } else {
+      gemm_sync();
+    }
+    if (wv >= 4) asm volatile("s_barrier" ::: "memory");
+    uint32_t cur = 0;
+    Frag a[2][HM], b0[2][HN], b1[2][HN];
+    auto read_a = [&](int half) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < HM; ++i)
+          a[h][i] = *reinterpret_cast<const Frag*>(lds + cur + ar + (half * HM + i) * 2048u + (p0 ^ (h * 64u)));
+    };
+    auto read_b = [&](int half, Frag (&b)[2][HN]) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < HN; ++j)
+          b[h][j] = *reinterpret_cast<const Frag*>(lds + cur + br + (half * HN + j) * 2048u + (p0 ^ (h * 64u)));
+    };
+    auto products = [&](int mh, int nh, const Frag (&b)[2][HN]) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < HM; ++i)
+#pragma unroll
+          for (int j = 0; j < HN; ++j)
+            acc[mh * HM + i][nh * HN + j] = Mfma<T>::mul(a[h][i], b[h][j], acc[mh * HM + i][nh * HN + j]);
+      __builtin_amdgcn_s_setprio(0);
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_barrier" ::: "memory");
+    };
+    for (int s = 0; s < n; ++s) {
+      const bool more = s + 2 < n;
+      const uint32_t buf = lds0 + cur;
+      read_b(0, b0);
+      read_a(0);
+      products(0, 0, b0);
+      read_b(1, b1);
+      if (more) {
+        feed.next();
+        feed.template a<0>(buf);
+        feed.template a<1>(buf);
+        feed.template b<0>(buf);
+        feed.template b<1>(buf);
+      }
+      products(0, 1, b1);
+      read_a(1);
+      if (more) {
+        feed.template b<2>(buf);
+        feed.template b<3>(buf);
+      }
+      products(1, 1, b1);
+      if (more) {
+        feed.template a<2>(buf);
+        feed.template a<3>(buf);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(QA + QB) : "memory");   // the next step has landed
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      products(1, 0, b0);
       cur = LDS_STEP - cur;
     }
+    if (wv < 4) asm volatile("s_barrier" ::: "memory");
   }
 
   // After run(): the accumulators by way of LDS, for stores along rows or

@@ -12,9 +12,13 @@
 // (22 bits; the values' range is known, so a fixed power of two keeps them
 // clear of fp16's ends), products are summed in fp32, and
 //   fp32 updates   take three plane products each (all but rest x rest);
-//   bf16 updates   use only the upper fp16 value of X inside the products
-//                  (a X is taken from both), and both of A and B: about 1e-3
-//                  of the result, below the output's own rounding.
+//   bf16 updates   take one: the upper values' product.  The rests enter where
+//                  they cost nothing, in the epilogues: a X and b A use both
+//                  values, and of A's and B's rests, whose largest part by far
+//                  lies on the diagonal, the diagonal is multiplied in
+//                  (A_h D + D A_h, D X).  The error is about 1.3e-3 of the
+//                  result, below the output's own rounding; without the
+//                  diagonals it is 2 to 4e-3.
 //
 // All matrices of a call go through each stage in one launch: a sum of
 // squares, the scaling, and three products a step.  A and B are symmetric:
@@ -40,7 +44,7 @@ using half_t = _Float16;
 // X, A and B are stored times these
 constexpr float kSX = 8192.f, kSA = 4096.f, kSB = 1024.f;
 
-enum { kStageNorm = 0, kStageFill, kStageGram, kStageApply, kStages };
+enum { kStageNorm = 0, kStageFill, kStageGram, kStagePoly, kStageApply, kStages };
 
 struct Mat {
   // the update (r, c), r < rows, c < cols
@@ -59,11 +63,13 @@ struct Mat {
   int32_t rows, cols;
   int32_t turned;               // X is the transpose: m = cols, n = rows
   int32_t m, n, mp, np;
+  int32_t wide, o_wide;         // pieces of eight of a contiguous row are 16-byte aligned
   int32_t chunk, chunks;        // elements a workgroup of the sum of squares takes
   half_t* xr;                   // [2 planes][m][np]
   half_t* xt[2];                // [planes][n][mp], two in turn
   half_t* a;                    // [2][m][mp]
   half_t* b;                    // [2][m][mp]
+  float *da, *db;               // [m]: the diagonals' rests of A and B (bf16)
   double* part;                 // [chunks]
 };
 
@@ -114,19 +120,55 @@ __device__ __forceinline__ int find(const Table& t, int stage, int id, int* loca
   return at;
 }
 
-__device__ __forceinline__ bool kept(const Mat& m, int64_t e) {
-  if (!m.keep) return true;
-  const int64_t k = e / 9;
-  return m.keep[k] >> static_cast<int>(e - 9 * k) & 1;
+// Which of the elements e .. e + 7 of a layer are kept taps (bit by bit).
+__device__ __forceinline__ uint32_t kept8(const Mat& m, uint32_t e, uint32_t all) {
+  if (!m.keep) return 255u;
+  const uint32_t k = e / 9u;
+  uint32_t bits = m.keep[k] & 511u;
+  if ((k + 1u) * 9u < all) bits |= static_cast<uint32_t>(m.keep[k + 1]) << 9;
+  return bits >> (e - 9u * k);
 }
 
-// element e of a weight step's update, from the new momentum
+// Eight values from p on, of which n are there; wide: p is aligned to 16
+// bytes, and all eight are.
 template <class S>
-__device__ __forceinline__ float update_of(const Mat& m, const Step& s, int64_t e) {
-  const float mom = m.mom_out[e];
-  if (!s.nesterov) return mom;
-  const float g = kept(m, e) ? static_cast<float>(static_cast<const S*>(m.g)[e]) : 0.f;
-  return g + s.momentum * mom;
+__device__ __forceinline__ void load8(const S* p, int n, bool wide, float (&v)[8]) {
+  if (wide) {
+    using S8 = __attribute__((ext_vector_type(8))) S;
+    const S8 x = *reinterpret_cast<const S8*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? static_cast<float>(p[e]) : 0.f;
+  }
+}
+template <class S>
+__device__ __forceinline__ void store8(S* p, int n, bool wide, const float (&v)[8]) {
+  if (wide) {
+    using S8 = __attribute__((ext_vector_type(8))) S;
+    S8 x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = static_cast<S>(v[e]);
+    *reinterpret_cast<S8*>(p) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = static_cast<S>(v[e]);
+  }
+}
+
+// elements e .. e + 7 of a weight step's update, from the new momentum
+template <class S>
+__device__ __forceinline__ void update8(const Mat& m, const Step& s, uint32_t e, int n, float (&u)[8]) {
+  const bool wide = m.wide && n == 8 && e % 8 == 0;
+  load8(m.mom_out + e, n, wide, u);
+  if (!s.nesterov) return;
+  const uint32_t on = kept8(m, e, static_cast<uint32_t>(m.rows) * m.cols);
+  float g[8];
+  load8(static_cast<const S*>(m.g) + e, n, wide, g);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) u[i] = (on >> i & 1 ? g[i] : 0.f) + s.momentum * u[i];
 }
 
 // The sum of squares of each matrix, in 64 bits, a chunk a workgroup; a
@@ -136,29 +178,50 @@ __global__ __launch_bounds__(256) void norm_kernel(Table t, Step s) {
   __shared__ double sums[4];
   int chunk;
   const Mat& m = t.mat[find(t, kStageNorm, blockIdx.x, &chunk)];
-  const int64_t all = static_cast<int64_t>(m.rows) * m.cols, e0 = static_cast<int64_t>(chunk) * m.chunk;
-  const int64_t e1 = e0 + m.chunk < all ? e0 + m.chunk : all;
-  double sum = 0.;
+  const uint32_t all = static_cast<uint32_t>(m.rows) * m.cols, e0 = static_cast<uint32_t>(chunk) * m.chunk;
+  const uint32_t e1 = e0 + m.chunk < all ? e0 + m.chunk : all;
+  double sum[2] = {0., 0.};
+  auto add = [&](const float (&u)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i & 1] += static_cast<double>(u[i]) * u[i];
+  };
   if (m.g) {
-    for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
-      float g = 0.f, mom = 0.f;
-      if (kept(m, e)) {
-        g = static_cast<float>(static_cast<const S*>(m.g)[e]);
-        mom = s.momentum * m.mom[e] + g;
+    for (uint32_t e = e0 + 8 * threadIdx.x; e < e1; e += 2048) {
+      const int n = e1 - e < 8 ? static_cast<int>(e1 - e) : 8;
+      const bool wide = m.wide && n == 8;
+      float g[8], mom[8];
+      load8(static_cast<const S*>(m.g) + e, n, wide, g);
+      load8(m.mom + e, n, wide, mom);
+      const uint32_t on = kept8(m, e, all);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        g[i] = on >> i & 1 ? g[i] : 0.f;
+        mom[i] = on >> i & 1 ? s.momentum * mom[i] + g[i] : 0.f;
       }
-      m.mom_out[e] = mom;
-      const float u = s.nesterov ? g + s.momentum * mom : mom;
-      sum += static_cast<double>(u) * u;
+      store8(m.mom_out + e, n, wide, mom);
+      if (s.nesterov) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mom[i] = g[i] + s.momentum * mom[i];
+      }
+      add(mom);
+    }
+  } else if (m.u_cs == 1 && m.u_rs == m.cols) {
+    for (uint32_t e = e0 + 8 * threadIdx.x; e < e1; e += 2048) {
+      const int n = e1 - e < 8 ? static_cast<int>(e1 - e) : 8;
+      float u[8];
+      load8(static_cast<const S*>(m.u) + e, n, m.wide && n == 8, u);
+      add(u);
     }
   } else {
-    for (int64_t e = e0 + threadIdx.x; e < e1; e += 256) {
-      const int64_t r = e / m.cols, c = e - r * m.cols;
+    for (uint32_t e = e0 + threadIdx.x; e < e1; e += 256) {
+      const uint32_t r = e / static_cast<uint32_t>(m.cols), c = e - r * m.cols;
       const float u = static_cast<float>(static_cast<const S*>(m.u)[r * m.u_rs + c * m.u_cs]);
-      sum += static_cast<double>(u) * u;
+      sum[0] += static_cast<double>(u) * u;
     }
   }
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  double x = sum[0] + sum[1];
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
   __syncthreads();
   if (threadIdx.x == 0) m.part[chunk] = sums[0] + sums[1] + sums[2] + sums[3];
 }
@@ -184,17 +247,37 @@ __global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
   const float scale = static_cast<float>(kSX / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + static_cast<double>(s.eps)));
 
   const int tc = m.np / 64, r0 = id / tc * 64, c0 = id % tc * 64;
-  const bool along_n = m.g ? !m.turned : (m.turned ? m.u_rs : m.u_cs) == 1;   // consecutive along n in memory
+  // pieces of eight along the update's own rows, or down them if its columns
+  // are the contiguous ones
+  const bool rows = m.g || m.u_cs <= m.u_rs;
+  const bool along_n = rows != static_cast<bool>(m.turned);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int x = tid & 63, y = (tid >> 6) + 4 * i;
-    const int r = along_n ? y : x, c = along_n ? x : y;
-    float u = 0.f;
-    if (r0 + r < m.m && c0 + c < m.n) {
-      const int64_t ur = m.turned ? c0 + c : r0 + r, uc = m.turned ? r0 + r : c0 + c;
-      u = m.g ? update_of<S>(m, s, ur * m.cols + uc) : static_cast<float>(static_cast<const S*>(m.u)[ur * m.u_rs + uc * m.u_cs]);
+  for (int i = 0; i < 2; ++i) {
+    const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
+    const int r = r0 + (along_n ? u : w), c = c0 + (along_n ? w : u);
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (r < m.m && c < m.n) {
+      const int left = along_n ? m.n - c : m.m - r, n = left < 8 ? left : 8;
+      const int ur = m.turned ? c : r, uc = m.turned ? r : c;
+      if (m.g) {
+        update8<S>(m, s, static_cast<uint32_t>(ur) * m.cols + uc, n, x);
+      } else if (rows && m.u_cs == 1) {
+        load8(static_cast<const S*>(m.u) + ur * m.u_rs + uc, n, m.wide && n == 8, x);
+      } else {
+        const S* at = static_cast<const S*>(m.u) + ur * m.u_rs + uc * m.u_cs;
+        const int64_t step = rows ? m.u_cs : m.u_rs;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e < n ? static_cast<float>(at[e * step]) : 0.f;
+      }
     }
-    tile[r][c] = u * scale;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = x[e] * scale;
+      if (along_n)
+        tile[u][w + e] = c + e < m.n ? v : 0.f;
+      else
+        tile[w + e][u] = r + e < m.m ? v : 0.f;
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -262,12 +345,13 @@ __device__ __forceinline__ void pair8(const half_t* h, int64_t plane, float (&v)
   for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(a[e]) + static_cast<float>(b[e]);
 }
 
-// A = X X^T (POLY false) or B = b A + c A A^T (POLY true)
-template <class Tile, bool POLY>
+// A = X X^T (POLY false) or B = b A + c A A^T (POLY true); P: values of X, A
+// and B in the products
+template <class Tile, int P, bool POLY>
 __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, PlanePairs pairs) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
   int id;
-  const Mat& m = t.mat[find(t, kStageGram, blockIdx.x, &id)];
+  const Mat& m = t.mat[find(t, POLY ? kStagePoly : kStageGram, blockIdx.x, &id)];
   int ti, tj;
   triangle(id, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
@@ -281,19 +365,31 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
   half_t* out = POLY ? m.b : m.a;
   const float fa = s.b * (kSB / kSA), fc = POLY ? s.c * (kSB / (kSA * kSA)) : kSA / (kSX * kSX);
   // (rows past m are zeros in both operands, so the padding comes out as zeros)
-  auto store = [&](int64_t at, float (&v)[8]) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= fc;
+  auto store = [&](int r, int c, float (&v)[8]) {
+    const int64_t at = static_cast<int64_t>(r) * mp + c;
     if constexpr (POLY) {
-      float o[8];
-      pair8(a + at, plane, o);
+      const f16x8 h = *reinterpret_cast<const f16x8*>(a + at), l = *reinterpret_cast<const f16x8*>(a + at + plane);
+      if constexpr (P == 1) {
+        const float d = m.da[r];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += fa * o[e];
+        for (int e = 0; e < 8; ++e) v[e] += static_cast<float>(h[e]) * (d + m.da[c + e < mm ? c + e : mm - 1]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fc * v[e] + fa * (static_cast<float>(h[e]) + static_cast<float>(l[e]));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= fc;
     }
     f16x8 h, l;
     split8(v, &h, &l);
     *reinterpret_cast<f16x8*>(out + at) = h;
-    *reinterpret_cast<f16x8*>(out + at + plane) = l;
+    if (!POLY || P > 1) *reinterpret_cast<f16x8*>(out + at + plane) = l;
+    if (P == 1 && r >= c && r < c + 8) {
+      float* d = POLY ? m.db : m.da;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (r == c + e) d[r] = static_cast<float>(l[e]);
+    }
   };
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
 #pragma unroll 2
@@ -303,7 +399,7 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
       view.row_piece(i, &r, &c);
       view.row(r, c, v);
       r += row0 + rb, c += col0 + cb;
-      if (r < mm && c < mp) store(static_cast<int64_t>(r) * mp + c, v);
+      if (r < mm && c < mp) store(r, c, v);
     }
     if (ti != tj) {
 #pragma unroll 2
@@ -313,7 +409,7 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
         view.col_piece(i, &r, &c);
         view.col(r, c, v);
         r += row0 + rb, c += col0 + cb;
-        if (c < mm && r < mp) store(static_cast<int64_t>(c) * mp + r, v);
+        if (c < mm && r < mp) store(c, r, v);
       }
     }
   });
@@ -322,18 +418,24 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
 // results (r, c) .. (r, c + 7) of a matrix, of which n are there
 template <class S>
 __device__ __forceinline__ void put_result(const Mat& m, const Step& s, int r, int c, int n, const float (&v)[8]) {
+  n = n < 8 ? n : 8;
+  if (m.g) {
+    const uint32_t e = static_cast<uint32_t>(r) * m.cols + c;
+    const bool wide = m.wide && n == 8 && e % 8 == 0;
+    const uint32_t on = kept8(m, e, static_cast<uint32_t>(m.rows) * m.cols);
+    const float decay = 1.f - s.lr * s.decay;
+    float w[8];
+    load8(static_cast<const S*>(m.w) + e, n, wide, w);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (e >= n) break;
-    const int ur = r, uc = c + e;
-    if (m.g) {
-      const int64_t k = static_cast<int64_t>(ur) * m.cols + uc;
-      float w = 0.f;
-      if (kept(m, k)) w = (1.f - s.lr * s.decay) * static_cast<float>(static_cast<const S*>(m.w)[k]) - m.up * v[e];
-      static_cast<S*>(m.w_out)[k] = static_cast<S>(w);
-    } else {
-      static_cast<S*>(m.o)[ur * m.o_rs + uc * m.o_cs] = static_cast<S>(v[e]);
-    }
+    for (int i = 0; i < 8; ++i) w[i] = on >> i & 1 ? decay * w[i] - m.up * v[i] : 0.f;
+    store8(static_cast<S*>(m.w_out) + e, n, wide, w);
+  } else if (m.o_cs == 1) {
+    store8(static_cast<S*>(m.o) + r * m.o_rs + c, n, m.o_wide && n == 8, v);
+  } else {
+    S* at = static_cast<S*>(m.o) + r * m.o_rs + c * m.o_cs;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) at[e * m.o_cs] = static_cast<S>(v[e]);
   }
 }
 
@@ -366,6 +468,11 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
       const int64_t at = static_cast<int64_t>(rb + r) * np + cb + c;
       pair8(xr + at, plane, x);
       const float fb = LAST ? 1.f / (kSB * kSX) : 1.f / kSB, fx = LAST ? s.a / kSX : s.a;
+      if constexpr (P == 1) {
+        const float d = m.db[rb + r];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += d * x[e];
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fx * x[e] + fb * v[e];
       if constexpr (LAST) {
@@ -404,25 +511,34 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
 // host
 // ---------------------------------------------------------------------------
 
-using Big = GemmTile<half_t, 256, 256, 2, 4>;
-using Mid = GemmTile<half_t, 128, 128, 2, 2>;
-using Small = GemmTile<half_t, 64, 64, 2, 2>;
-constexpr int kTile[] = {256, 128, 64};
+using Big = BigTile<half_t>;
+using Mid = MidTile<half_t>;
+using Small = SmallTile<half_t>;
 
 struct Plan {
   std::vector<Mat> mats;
-  int gram = 2, apply = 2;      // tiles
+  int gram = kSmall, poly = kSmall, apply = kSmall;   // tiles
   int64_t blocks[kStages] = {};
   std::vector<int32_t> start[kStages];
   size_t table = 0, total = 0;
 };
 
-// The largest tile that gives most CUs one, over all matrices.
-template <class F>
-int pick(F&& tiles) {
-  for (int k = 0; k < 2; ++k)
-    if (tiles(kTile[k]) >= 200) return k;
-  return 2;
+// The tile that takes the least modelled time for a stage over all matrices;
+// tiles(m, edge) and steps(m) of each.
+template <class F, class G>
+int pick(const std::vector<Mat>& mats, F&& tiles, G&& steps) {
+  int best = kSmall;
+  double least = 1e300;
+  for (int k : {kSmall, kMid, kBig}) {
+    double n = 0., work = 0., most = 0.;
+    for (const Mat& m : mats) {
+      const double t = static_cast<double>(tiles(m, kTileEdge[k])), s = steps(m);
+      n += t, work += t * s, most = std::max(most, s);
+    }
+    const double t = tile_time(k, n, work / n, most);
+    if (t < least) least = t, best = k;
+  }
+  return best;
 }
 
 // Fills in sizes and workspace places (as offsets from `ws`).
@@ -439,22 +555,24 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     m.m = std::min(m.rows, m.cols), m.n = std::max(m.rows, m.cols);
     m.mp = static_cast<int32_t>(pad64(m.m)), m.np = static_cast<int32_t>(pad64(m.n));
     const int64_t all = static_cast<int64_t>(m.rows) * m.cols;
+    auto piece = [&](const void* q, int64_t pitch) { return aligned16(q) && pitch % 8 == 0; };
+    m.wide = m.g ? aligned16(m.g) && aligned16(m.w) && aligned16(m.w_out) && aligned16(m.mom) && aligned16(m.mom_out)
+                 : piece(m.u, m.u_rs);
+    m.o_wide = piece(m.o, m.o_rs);
     m.chunk = static_cast<int32_t>(std::max<int64_t>(4096, cdiv(cdiv(all, 256), 256) * 256));
     m.chunks = static_cast<int32_t>(cdiv(all, m.chunk));
   }
   // long sums first, so that the longest tiles do not start last
   std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
-  auto sum = [&](auto&& f) {
-    int64_t n = 0;
-    for (const Mat& m : p->mats) n += f(m);
-    return n;
-  };
   auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.m, t); return k * (k + 1) / 2; };
   auto rect = [](const Mat& m, int t) { return cdiv(m.m, t) * cdiv(m.n, t); };
-  p->gram = pick([&](int t) { return sum([&](const Mat& m) { return tri(m, t); }); });
-  p->apply = pick([&](int t) { return sum([&](const Mat& m) { return rect(m, t); }); });
+  const int pairs = planes == 1 ? 1 : 3;
+  p->gram = pick(p->mats, tri, [&](const Mat& m) { return m.np / 64 * pairs; });
+  p->poly = pick(p->mats, tri, [&](const Mat& m) { return m.mp / 64 * pairs; });
+  p->apply = pick(p->mats, rect, [&](const Mat& m) { return m.mp / 64 * pairs; });
   for (Mat& m : p->mats) {
-    const int64_t n[kStages] = {m.chunks, static_cast<int64_t>(m.mp / 64) * (m.np / 64), tri(m, kTile[p->gram]), rect(m, kTile[p->apply])};
+    const int64_t n[kStages] = {m.chunks, static_cast<int64_t>(m.mp / 64) * (m.np / 64), tri(m, kTileEdge[p->gram]),
+                                tri(m, kTileEdge[p->poly]), rect(m, kTileEdge[p->apply])};
     for (int k = 0; k < kStages; ++k) {
       p->start[k].push_back(static_cast<int32_t>(p->blocks[k]));
       p->blocks[k] += n[k];
@@ -466,6 +584,8 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     m.xt[1] = reinterpret_cast<half_t*>(ws + take(planes * tn));
     m.a = reinterpret_cast<half_t*>(ws + take(2 * an));
     m.b = reinterpret_cast<half_t*>(ws + take(2 * an));
+    m.da = reinterpret_cast<float*>(ws + take(m.m * 4));
+    m.db = reinterpret_cast<float*>(ws + take(m.m * 4));
     m.part = reinterpret_cast<double*>(ws + take(m.chunks * 8));
   }
   p->table = take(p->mats.size() * (sizeof(Mat) + kStages * 4));
@@ -473,23 +593,24 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
   return PP_OK;
 }
 
-template <bool POLY>
+template <int P, bool POLY>
 void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, hipStream_t st) {
-  const dim3 grid(static_cast<uint32_t>(p.blocks[kStageGram]));
-  if (p.gram == 0)
-    hipLaunchKernelGGL((gram_kernel<Big, POLY>), grid, dim3(Big::THREADS), 0, st, t, s, pairs);
-  else if (p.gram == 1)
-    hipLaunchKernelGGL((gram_kernel<Mid, POLY>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs);
+  const dim3 grid(static_cast<uint32_t>(p.blocks[POLY ? kStagePoly : kStageGram]));
+  const int tile = POLY ? p.poly : p.gram;
+  if (tile == kBig)
+    hipLaunchKernelGGL((gram_kernel<Big, P, POLY>), grid, dim3(Big::THREADS), 0, st, t, s, pairs);
+  else if (tile == kMid)
+    hipLaunchKernelGGL((gram_kernel<Mid, P, POLY>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs);
   else
-    hipLaunchKernelGGL((gram_kernel<Small, POLY>), grid, dim3(Small::THREADS), 0, st, t, s, pairs);
+    hipLaunchKernelGGL((gram_kernel<Small, P, POLY>), grid, dim3(Small::THREADS), 0, st, t, s, pairs);
 }
 
 template <class S, int P, bool LAST>
 void apply(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
   const dim3 grid(static_cast<uint32_t>(p.blocks[kStageApply]));
-  if (p.apply == 0)
+  if (p.apply == kBig)
     hipLaunchKernelGGL((apply_kernel<Big, S, P, LAST>), grid, dim3(Big::THREADS), 0, st, t, s, pairs, turn);
-  else if (p.apply == 1)
+  else if (p.apply == kMid)
     hipLaunchKernelGGL((apply_kernel<Mid, S, P, LAST>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs, turn);
   else
     hipLaunchKernelGGL((apply_kernel<Small, S, P, LAST>), grid, dim3(Small::THREADS), 0, st, t, s, pairs, turn);
@@ -512,13 +633,14 @@ pp_status enqueue(const Plan& p, const Step& s, uint8_t* ws, hipStream_t st) {
   const Table t = {mats, start, all};
   hipLaunchKernelGGL((norm_kernel<S>), dim3(static_cast<uint32_t>(p.blocks[kStageNorm])), dim3(256), 0, st, t, s);
   hipLaunchKernelGGL((fill_kernel<S, P>), dim3(static_cast<uint32_t>(p.blocks[kStageFill])), dim3(256), 0, st, t, s);
+  const PlanePairs pairs = P == 1 ? kPairs1 : kPairs3;
   for (int k = 0; k < s.steps; ++k) {
-    gram<false>(p, t, s, P == 1 ? kPairs1 : kPairs3, st);
-    gram<true>(p, t, s, kPairs3, st);
+    gram<P, false>(p, t, s, pairs, st);
+    gram<P, true>(p, t, s, pairs, st);
     if (k + 1 < s.steps)
-      apply<S, P, false>(p, t, s, P == 1 ? kPairs2 : kPairs3, k & 1, st);
+      apply<S, P, false>(p, t, s, pairs, k & 1, st);
     else
-      apply<S, P, true>(p, t, s, P == 1 ? kPairs2 : kPairs3, k & 1, st);
+      apply<S, P, true>(p, t, s, pairs, k & 1, st);
   }
   return launched();
 }
@@ -557,6 +679,7 @@ pp_status check_size(int64_t rows, int64_t cols) {
   if (rows < 0 || cols < 0) return fail(PP_EINVAL, "negative size");
   if (rows > (1 << 21) || cols > (1 << 21) || std::min(rows, cols) > 32768)
     return fail(PP_EUNSUPPORTED, "a matrix may have up to 2^21 rows or columns, and 32768 of the fewer");
+  if (rows * cols >= (int64_t(1) << 31)) return fail(PP_EUNSUPPORTED, "a matrix must have fewer than 2^31 elements");
   return PP_OK;
 }
 

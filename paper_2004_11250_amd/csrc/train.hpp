@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <string>
 
 #include "gemm_nt.hpp"
@@ -31,6 +32,59 @@ inline GemmOperand rows_from(GemmOperand o, int64_t r0, int64_t rows) {
   for (auto& p : o.plane) p = static_cast<const uint8_t*>(p) + r0 * o.ld * 2;
   o.rows = static_cast<int32_t>(rows);
   return o;
+}
+
+// The tiles of the products, and when each is used.  Measured on MI355X (us a
+// step of 64 k, a workgroup on every CU / alone on its CU; us at either end of
+// a tile): 256 x 256 phased 1.68 / 1.68 (1280 TFLOP/s at 8192^3), 6;
+// 128 x 128, two workgroups a CU, 0.52 / 0.62 (1020 TFLOP/s), 3.5; 64 x 64 with
+// four steps in flight 0.195 / 0.31 (690 TFLOP/s), 2.5.  So the large tile wins
+// wherever it fills the card, and the small ones where it would leave CUs
+// without work: 1024 x 8192 x 7168 takes 146, 118 and 205 us, 512 x 512 x 4608
+// 83, 45 and 22 us.
+enum { kBig = 0, kMid = 1, kSmall = 2 };
+template <class T> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, true>;
+template <class T> using MidTile = GemmTile<T, 128, 128, 2, 2, 2>;
+template <class T> using SmallTile = GemmTile<T, 64, 64, 2, 2, 4>;
+constexpr int kTileEdge[] = {256, 128, 64};
+constexpr int kCUs = 256;
+
+// Modelled time in us of `tiles` tiles of `steps` steps on average, `most` at
+// most.
+inline double tile_time(int tile, double tiles, double steps, double most) {
+  constexpr double full[] = {1.68, 0.52, 0.195}, alone[] = {1.68, 0.62, 0.31}, ends[] = {6., 3.5, 2.5};
+  const double n = static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs));
+  return std::max(most * alone[tile], n * steps * full[tile]) + ends[tile] * (tile == kBig ? n : 0.5 + 0.5 * n);
+}
+
+inline int pick_tile(int64_t m, int64_t n, int64_t steps) {
+  int best = kSmall;
+  double least = 1e300;
+  for (int k : {kSmall, kMid, kBig}) {
+    const double t = tile_time(k, static_cast<double>(cdiv(m, kTileEdge[k]) * cdiv(n, kTileEdge[k])), steps, steps);
+    if (t < least) least = t, best = k;
+  }
+  return best;
+}
+
+// The same for a product whose sum over k may be split over workgroups: the
+// partial sums are written to and read from memory (at about 3 TB/s) by one
+// more launch (about 4 us).
+struct SplitTile {
+  int tile, splits;
+};
+inline SplitTile pick_split(int64_t m, int64_t n, int64_t steps) {
+  SplitTile best = {kSmall, 1};
+  double least = 1e300;
+  for (int k : {kSmall, kMid, kBig})
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (s > 1 && (steps / s < 4 || static_cast<double>(s) * m * n * 4 > 256e6)) break;
+      const double per = static_cast<double>(cdiv(steps, s));
+      double t = tile_time(k, static_cast<double>(cdiv(m, kTileEdge[k]) * cdiv(n, kTileEdge[k]) * s), per, per);
+      if (s > 1) t += 4. + s * static_cast<double>(m) * n * 8e-6 / 3.;
+      if (t < least) least = t, best = {k, s};
+    }
+  return best;
 }
 
 }  // namespace pp

@@ -78,6 +78,8 @@ struct StageArgs {
   __bf16* turned;              // [cols][rows padded] planes, or null
   int64_t direct_plane, turned_plane;   // elements between planes
   int32_t cols_pad, rows_pad;
+  int32_t along_cols;          // columns lie closer in memory than rows
+  int32_t wide;                // pieces of eight on that axis are contiguous and 16-byte aligned
 };
 
 // An fp32 value as a sum of three bf16 values: 8 bits of it each.
@@ -98,18 +100,47 @@ __global__ __launch_bounds__(256) void stage_kernel(StageArgs a) {
   const int tc = a.cols_pad / 64;
   const int r0 = blockIdx.x / tc * 64, c0 = blockIdx.x % tc * 64, tid = threadIdx.x;
   const S* src = static_cast<const S*>(a.src);
-  const bool along_cols = a.s_col == 1;
+  // a piece of eight values along the axis that is contiguous in memory
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int u = tid & 63, w = (tid >> 6) + 4 * i;
-    const int r = along_cols ? w : u, c = along_cols ? u : w;
-    const int row = r0 + r, col = c0 + c;
-    float x = 0.f;
-    if (row < a.rows && col < a.cols && !(a.target && a.target[row] == a.ignore)) {
-      const int hi = row / a.inner, lo = row - hi * a.inner;
-      x = static_cast<float>(src[hi * a.s_hi + lo * a.s_lo + col * a.s_col]);
+  for (int i = 0; i < 2; ++i) {
+    const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
+    const int r = r0 + (a.along_cols ? u : w), c = c0 + (a.along_cols ? w : u);
+    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (r < a.rows && c < a.cols) {
+      const int hi = r / a.inner;
+      int lo = r - hi * a.inner;
+      int64_t row = hi * a.s_hi + lo * a.s_lo;
+      if (a.wide && (a.along_cols ? c : lo) + 8 <= (a.along_cols ? a.cols : a.inner)) {
+        using S8 = __attribute__((ext_vector_type(8))) S;
+        const S8 v = *reinterpret_cast<const S8*>(src + row + c * a.s_col);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = static_cast<float>(v[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (r + (a.along_cols ? 0 : e) < a.rows && c + (a.along_cols ? e : 0) < a.cols)
+            x[e] = static_cast<float>(src[row + (c + (a.along_cols ? e : 0)) * a.s_col]);
+          if (!a.along_cols) {
+            row += a.s_lo;
+            if (++lo == a.inner) lo = 0, row += a.s_hi - a.inner * a.s_lo;
+          }
+        }
+      }
+      if (a.target) {   // ignored tokens
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int t = r + (a.along_cols ? 0 : e);
+          if (t < a.rows && a.target[t] == a.ignore) x[e] = 0.f;
+        }
+      }
     }
-    tile[r][c] = x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (a.along_cols)
+        tile[u][w + e] = x[e];
+      else
+        tile[w + e][u] = x[e];
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -308,61 +339,63 @@ struct JoinArgs {
   const float* target_logit;
   int32_t parts;
   float* lse;       // [token]
-  float* loss;      // [token]
-  float* weight;    // [token], or null
+  float* loss;      // [token], or null
+  double2* sums;    // [workgroup]: sums of the losses and of the weights, or null
 };
 
-// 16 tokens a workgroup, 16 threads each taking every 16th part.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.f : top;
+  return make_float2(top, a.y * fast_exp(a.x - ref) + b.y * fast_exp(b.x - ref));
+}
+
+// 256 / W tokens a workgroup, W threads each taking every W-th part.
+template <int W>
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
-  __shared__ float2 got[16][17];
-  const int u = threadIdx.x & 15, w = threadIdx.x >> 4, t = blockIdx.x * 16 + u;
-  float m = -INFINITY, s = 0.f;
+  constexpr int N = 256 / W;
+  __shared__ float2 got[W][N];
+  const int u = threadIdx.x % N, w = threadIdx.x / N, t = blockIdx.x * N + u;
+  float2 s = make_float2(-INFINITY, 0.f);
   if (t < a.k.t)
-    for (int p = w; p < a.parts; p += 16) {
-      const float2 q = a.part[static_cast<int64_t>(p) * a.k.t + t];
-      const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
-      s = s * fast_exp(m - ref) + q.y * fast_exp(q.x - ref);
-      m = top;
-    }
-  got[w][u] = make_float2(m, s);
+    for (int p = w; p < a.parts; p += W) s = join(s, a.part[static_cast<int64_t>(p) * a.k.t + t]);
+  got[w][u] = s;
   __syncthreads();
-  if (w || t >= a.k.t) return;
-  for (int p = 1; p < 16; ++p) {
-    const float2 q = got[p][u];
-    const float top = fmaxf(m, q.x), ref = top == -INFINITY ? 0.f : top;
-    s = s * fast_exp(m - ref) + q.y * fast_exp(q.x - ref);
-    m = top;
-  }
-  const int64_t y = a.k.target[t];
-  float lse = 0.f, loss = 0.f, weight = 0.f;
-  if (y != a.k.ignore) {
-    lse = m + logf(s);
-    if (y < 0 || y >= a.k.v) {
-      loss = weight = __builtin_nanf("");
-    } else {
-      weight = a.k.class_weight ? a.k.class_weight[y] : 1.f;
-      loss = weight * (lse - a.target_logit[t]);
+  if (w) return;
+  float loss = 0.f, weight = 0.f;
+  if (t < a.k.t) {
+#pragma unroll
+    for (int p = 1; p < W; ++p) s = join(s, got[p][u]);
+    const int64_t y = a.k.target[t];
+    float lse = 0.f;
+    if (y != a.k.ignore) {
+      lse = s.x + logf(s.y);
+      if (y < 0 || y >= a.k.v) {
+        loss = weight = __builtin_nanf("");
+      } else {
+        weight = a.k.class_weight ? a.k.class_weight[y] : 1.f;
+        loss = weight * (lse - a.target_logit[t]);
+      }
     }
+    a.lse[t] = lse;
+    if (a.loss) a.loss[t] = loss;
   }
-  a.lse[t] = lse;
-  a.loss[t] = loss;
-  if (a.weight) a.weight[t] = weight;
+  if (!a.sums) return;
+  // (N lanes of one wave)
+  double x = loss, y = weight;
+#pragma unroll
+  for (int d = N / 2; d; d >>= 1) x += __shfl_xor(x, d), y += __shfl_xor(y, d);
+  if (u == 0) a.sums[blockIdx.x] = make_double2(x, y);
 }
 
 // the loss and its divisor (sums in 64 bits, in a fixed order)
-__global__ __launch_bounds__(1024) void loss_kernel(const float* loss, const float* weight, int32_t n, int32_t mean,
-                                                    float* out, float* divisor) {
+__global__ __launch_bounds__(1024) void loss_kernel(const double2* sums, int32_t n, int32_t mean, float* out, float* divisor) {
   __shared__ double a[16], b[16];
   double x = 0., w = 0.;
-  if (loss)
-    for (int i = threadIdx.x; i < n; i += 1024) {
-      x += loss[i];
-      w += weight[i];
-    }
-  for (int d = 32; d; d >>= 1) {
-    x += __shfl_xor(x, d);
-    w += __shfl_xor(w, d);
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += 1024) {
+    const double2 s = sums[i];
+    x += s.x, w += s.y;
   }
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d), w += __shfl_xor(w, d);
   if ((threadIdx.x & 63) == 0) a[threadIdx.x >> 6] = x, b[threadIdx.x >> 6] = w;
   __syncthreads();
   if (threadIdx.x) return;
@@ -373,11 +406,20 @@ __global__ __launch_bounds__(1024) void loss_kernel(const float* loss, const flo
   *divisor = static_cast<float>(div);
 }
 
-__global__ __launch_bounds__(256) void column_sum_kernel(const float* part, int32_t parts, int32_t n, Tokens k, float* out) {
-  const int v = blockIdx.x * 256 + threadIdx.x;
-  if (v >= n) return;
+// 64 columns a workgroup, 16 rows of threads each taking every 16th part
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int32_t parts, int32_t n, Tokens k, float* out) {
+  __shared__ float got[16][64];
+  const int u = threadIdx.x & 63, w = threadIdx.x >> 6, v = blockIdx.x * 64 + u;
   float s = 0.f;
-  for (int p = 0; p < parts; ++p) s += part[static_cast<int64_t>(p) * n + v];
+  if (v < n) {
+#pragma unroll 4
+    for (int p = w; p < parts; p += 16) s += part[static_cast<int64_t>(p) * n + v];
+  }
+  got[w][u] = s;
+  __syncthreads();
+  if (w || v >= n) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += got[i][u];
   out[v] = s * common_scale(k);
 }
 
@@ -491,25 +533,9 @@ __global__ __launch_bounds__(256) void slab_kernel(const float* slab, int64_t sl
 // host
 // ---------------------------------------------------------------------------
 
-using Big = GemmTile<__bf16, 256, 256, 2, 4>;
-using Mid = GemmTile<__bf16, 128, 128, 2, 2>;
-using Small = GemmTile<__bf16, 64, 64, 2, 2>;
-enum { kBig = 0, kMid = 1, kSmall = 2 };
-constexpr int kTileM[] = {256, 128, 64}, kTileN[] = {256, 128, 64};
-
-// The largest tile that still gives most CUs one.
-int pick_tile(int64_t m, int64_t n) {
-  for (int k = 0; k < 2; ++k)
-    if (cdiv(m, kTileM[k]) * cdiv(n, kTileN[k]) >= 200) return k;
-  return kSmall;
-}
-
-// Splits of k for a product whose tiles do not fill the card; each keeps at
-// least 8 steps.
-int pick_splits(int64_t tiles, int64_t steps) {
-  if (tiles >= 200) return 1;
-  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(cdiv(256, tiles), steps / 8)));
-}
+using Big = BigTile<__bf16>;
+using Mid = MidTile<__bf16>;
+using Small = SmallTile<__bf16>;
 
 struct Plan {
   int64_t t = 0, d = 0, v = 0, tp = 0, dp = 0, vp = 0;   // sizes and their paddings
@@ -523,7 +549,7 @@ struct Plan {
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
   // workspace offsets
-  size_t x_k = 0, w_k = 0, x_t = 0, w_t = 0, part = 0, tl = 0, loss = 0, weight = 0, g = 0, gt = 0, db = 0, slab = 0, total = 0;
+  size_t x_k = 0, w_k = 0, x_t = 0, w_t = 0, part = 0, tl = 0, sums = 0, g = 0, gt = 0, db = 0, slab = 0, total = 0;
 };
 
 constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of G, both orders
@@ -550,10 +576,10 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool x_aligned, bool w
   if (!p.x_direct) p.x_k = take(p.t * p.dp * e);
   if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
   if (fwd) {
-    p.logit = pick_tile(p.v, p.t);
-    p.parts = static_cast<int>(cdiv(p.v, kTileM[p.logit]) * 2);
+    p.logit = pick_tile(p.v, p.t, p.dp / 64 * p.pairs.n);
+    p.parts = static_cast<int>(cdiv(p.v, kTileEdge[p.logit]) * 2);
     p.part = take(p.parts * p.t * 8);
-    p.tl = take(p.t * 4), p.loss = take(p.t * 4), p.weight = take(p.t * 4);
+    p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
   }
   if (bwd) {
     p.x_t = take(p.d * p.tp * e), p.w_t = take(p.d * p.vp * e);
@@ -563,16 +589,15 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool x_aligned, bool w
     p.piece = std::min(p.vp, cdiv(cdiv(p.v, p.pieces), 256) * 256);   // pieces of about one size
     p.pieces = cdiv(p.v, p.piece);
     p.g = take(p.t * p.piece * e), p.gt = take(p.piece * p.tp * e);
-    p.gl = pick_tile(p.piece, p.t);
-    p.db = take(cdiv(p.t, kTileN[p.gl]) * 4 * p.piece * 4);
+    p.gl = pick_tile(p.piece, p.t, p.dp / 64 * p.pairs.n);
+    p.db = take(cdiv(p.t, kTileEdge[p.gl]) * 4 * p.piece * 4);
     p.dx_turned = d.dx_sc != 1;
     const int64_t dm = p.dx_turned ? p.t : p.d, dn = p.dx_turned ? p.d : p.t;
-    p.dxt = pick_tile(dm, dn);
-    p.dx_splits = pick_splits(cdiv(dm, kTileM[p.dxt]) * cdiv(dn, kTileN[p.dxt]), p.piece / 64 * p.pairs.n);
+    const SplitTile x = pick_split(dm, dn, p.piece / 64 * p.pairs.n), w = pick_split(p.d, p.piece, p.tp / 64 * p.pairs.n);
+    p.dxt = x.tile, p.dx_splits = x.splits;
     p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
     p.dx_ld = cdiv(dm, 4) * 4;
-    p.dwt = pick_tile(p.d, p.piece);
-    p.dw_splits = pick_splits(cdiv(p.d, kTileM[p.dwt]) * cdiv(p.piece, kTileN[p.dwt]), p.tp / 64 * p.pairs.n);
+    p.dwt = w.tile, p.dw_splits = w.splits;
     p.dw_slab = p.dw_splits > 1;
     p.dw_ld = cdiv(p.d, 4) * 4;
     // dx's slab outlives a piece, dw's does not
@@ -590,8 +615,8 @@ void stage(const StageArgs& a, hipStream_t st) {
 
 template <bool GRAD, int P>
 void logits(int tile, LogitArgs& a, hipStream_t st) {
-  a.tm = static_cast<int32_t>(cdiv(a.w.rows, kTileM[tile]));
-  a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileN[tile]));
+  a.tm = static_cast<int32_t>(cdiv(a.w.rows, kTileEdge[tile]));
+  a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileEdge[tile]));
   const dim3 grid(static_cast<uint32_t>(a.tm * a.tn));
   if (tile == kBig)
     hipLaunchKernelGGL((logit_kernel<Big, GRAD, P>), grid, dim3(Big::THREADS), 0, st, a);
@@ -603,8 +628,8 @@ void logits(int tile, LogitArgs& a, hipStream_t st) {
 
 template <class O>
 void product(int tile, ProductArgs& a, hipStream_t st) {
-  a.tm = static_cast<int32_t>(cdiv(a.a.rows, kTileM[tile]));
-  a.tn = static_cast<int32_t>(cdiv(a.b.rows, kTileN[tile]));
+  a.tm = static_cast<int32_t>(cdiv(a.a.rows, kTileEdge[tile]));
+  a.tn = static_cast<int32_t>(cdiv(a.b.rows, kTileEdge[tile]));
   const dim3 grid(static_cast<uint32_t>(a.tm * a.tn * a.splits));
   if (tile == kBig)
     hipLaunchKernelGGL((product_kernel<Big, O>), grid, dim3(Big::THREADS), 0, st, a);
@@ -654,12 +679,17 @@ pp_status enqueue(const Plan& p, const Call& c) {
     StageArgs a = {c.x, d.x_sn, d.x_sp, d.x_sc, static_cast<int32_t>(d.hw), static_cast<int32_t>(p.t), static_cast<int32_t>(p.d),
                    c.target, d.ignore_index, p.x_direct ? nullptr : bf(p.x_k), turn_x ? bf(p.x_t) : nullptr,
                    p.t * p.dp, p.d * p.tp, static_cast<int32_t>(p.dp), static_cast<int32_t>(p.tp)};
+    a.along_cols = d.x_sc <= step;
+    a.wide = aligned16(c.x) && (a.along_cols ? d.x_sc == 1 && step % 8 == 0 && (d.hw == 1 || d.x_sn % 8 == 0)
+                                             : d.x_sp == 1 && d.hw % 8 == 0 && d.x_sc % 8 == 0 && d.x_sn % 8 == 0);
     stage<S, P>(a, st);
   }
   if (!p.w_direct || turn_w) {
     StageArgs a = {c.w, d.w_ld, 0, 1, 1, static_cast<int32_t>(p.v), static_cast<int32_t>(p.d), nullptr, 0,
                    p.w_direct ? nullptr : bf(p.w_k), turn_w ? bf(p.w_t) : nullptr, p.v * p.dp, p.d * p.vp,
                    static_cast<int32_t>(p.dp), static_cast<int32_t>(p.vp)};
+    a.along_cols = 1;
+    a.wide = aligned16(c.w) && d.w_ld % 8 == 0;
     stage<S, P>(a, st);
   }
   if ((s = launched()) != PP_OK) return s;
@@ -671,10 +701,17 @@ pp_status enqueue(const Plan& p, const Call& c) {
     la.part = reinterpret_cast<float2*>(c.ws + p.part), la.target_logit = f32(p.tl);
     logits<false, P>(p.logit, la, st);
     const bool each = d.reduction == PP_NONE;
-    JoinArgs ja = {tok, la.part, la.target_logit, p.parts, c.stats, each ? c.loss : f32(p.loss), each ? nullptr : f32(p.weight)};
-    hipLaunchKernelGGL(join_kernel, dim3(static_cast<uint32_t>(cdiv(p.t, 16))), dim3(256), 0, st, ja);
-    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, each ? nullptr : f32(p.loss), f32(p.weight),
-                       static_cast<int32_t>(p.t), static_cast<int32_t>(d.reduction == PP_MEAN), each ? nullptr : c.loss, c.stats + p.t);
+    // (few parts: more tokens a workgroup)
+    const int n = p.parts > 8 ? 16 : 64;
+    const uint32_t grid = static_cast<uint32_t>(cdiv(p.t, n));
+    double2* sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
+    const JoinArgs ja = {tok, la.part, la.target_logit, p.parts, c.stats, each ? c.loss : nullptr, sums};
+    if (n == 16)
+      hipLaunchKernelGGL((join_kernel<16>), dim3(grid), dim3(256), 0, st, ja);
+    else
+      hipLaunchKernelGGL((join_kernel<4>), dim3(grid), dim3(256), 0, st, ja);
+    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, sums, each ? 0 : static_cast<int32_t>(grid),
+                       static_cast<int32_t>(d.reduction == PP_MEAN), each ? nullptr : c.loss, c.stats + p.t);
     if ((s = launched()) != PP_OK) return s;
   }
   if (!p.bwd) return PP_OK;
@@ -694,7 +731,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     la.db_part = c.db ? f32(p.db) : nullptr;
     logits<true, P>(p.gl, la, st);
     if (c.db)
-      hipLaunchKernelGGL(column_sum_kernel, dim3(static_cast<uint32_t>(cdiv(nv, 256))), dim3(256), 0, st, la.db_part,
+      hipLaunchKernelGGL(column_sum_kernel, dim3(static_cast<uint32_t>(cdiv(nv, 64))), dim3(1024), 0, st, la.db_part,
                          static_cast<int32_t>(la.tn * (p.gl == kBig ? Big::WN : Mid::WN)), static_cast<int32_t>(nv), tok, c.db + v0);
     const GemmOperand g = operand(la.g, la.g_plane, nvp, p.t, P), gt = operand(la.gt, la.gt_plane, p.tp, nv, P);
     if (c.dw) {
@@ -764,7 +801,7 @@ pp_status xent_call(const Call& c, bool fwd, bool bwd, size_t ws_bytes) {
                            static_cast<uint8_t*>(q), bytes);
     };
     if (fwd)
-      hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, nullptr, nullptr, 0, 0,
+      hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, static_cast<const double2*>(nullptr), 0, 0,
                          d.reduction == PP_NONE ? nullptr : c.loss, c.stats);
     if (bwd) {
       zero(c.dw, d.v * d.d * static_cast<int64_t>(esz));
