@@ -97,17 +97,19 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
          static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, bool PHASED_ = false>
+template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, int WK_ = 1, bool PHASED_ = false>
 struct GemmTile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int STAGES = STAGES_;                // steps held in LDS
   static constexpr bool PHASED = PHASED_;
-  static constexpr int NW = WM * WN, THREADS = NW * 64;
+  // WK groups of WM x WN waves: each takes every WK-th step, on operands of its
+  // own, and the groups' sums are added in LDS at the end
+  static constexpr int WK = WK_, NW = WM * WN, THREADS = NW * WK * 64;
   static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
   static constexpr int FM = TM / 16, FN = TN / 16;      // in 16 x 16 blocks
   static constexpr int QA = BM / (8 * NW), QB = BN / (8 * NW);   // DMAs a wave issues for a step
   static constexpr uint32_t LDS_A = BM * kBK * 2, LDS_STEP = (BM + BN) * kBK * 2;
-  static constexpr uint32_t LDS_BYTES = STAGES * LDS_STEP;
+  static constexpr uint32_t LDS_RING = STAGES * LDS_STEP, LDS_BYTES = WK * LDS_RING;
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 16 == 0 && TN % 16 == 0, "tile");
 
   // Row and column of acc[i][j][e] in the tile.  A lane holds four rows that
@@ -115,7 +117,9 @@ struct GemmTile {
   static __device__ __forceinline__ int row_of(int i) { return (wave() / WN) * TM + 16 * i + (lane() >> 4) * 4; }
   static __device__ __forceinline__ int col_of(int j) { return (wave() % WN) * TN + 16 * j + (lane() & 15); }
   static __device__ __forceinline__ int lane() { return threadIdx.x & 63; }
-  static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+  // the wave's place in its group, and its group
+  static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW; }
+  static __device__ __forceinline__ int group() { return WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW; }
 
   // A lane's part of the addresses, and the DMAs of one step.
   struct Feed {
@@ -170,7 +174,8 @@ struct GemmTile {
       const uint32_t c = code >> (4 * pair);
       const int64_t ko = static_cast<int64_t>(kk) * (kBK * 2);
       ra = rsrc(plane(pa, c & 3), ko), rb = rsrc(plane(pb, c >> 2 & 3), ko);
-      if (++kk == ksteps) kk = 0, ++pair;
+      kk += WK;
+      while (kk >= ksteps) kk -= ksteps, ++pair;
     }
     template <int I>
     __device__ __forceinline__ void a(uint32_t buf) const { gemm_dma(ra, va[I], buf + 1024u * group_a(I, wv)); }
@@ -208,15 +213,19 @@ struct GemmTile {
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (s0 >= s1) return;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
-    Feed feed(A, B, pairs, row0, col0, ksteps, k0, s0);
+    const int g = group();
+    Feed feed(A, B, pairs, row0, col0, ksteps, k0, s0 + g);
     if constexpr (PHASED)
       phased(feed, s1 - s0, lds, lds0, acc);
     else
-      ring(feed, s1 - s0, lds, lds0, acc);
+      ring(feed, s1 - s0, g, lds + g * LDS_RING, lds0 + g * LDS_RING, acc);
   }
 
-  // A ring of STAGES steps, STAGES - 1 of them in flight; one barrier a step.
-  static __device__ __forceinline__ void ring(Feed& feed, int n, const uint8_t* lds, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
+  // A ring of STAGES steps a group, STAGES - 1 of them in flight; one barrier
+  // for a step of every group.
+  static __device__ __forceinline__ void ring(Feed& feed, int steps, int g, const uint8_t* lds, uint32_t lds0,
+                                              f32x4 (&acc)[FM][FN]) {
+    const int rounds = (steps + WK - 1) / WK, n = WK == 1 ? steps : (steps - g + WK - 1) / WK;   // this group's steps
     const int ln = lane(), wv = wave();
     // a lane's operand of block i, k half h: row 16 i + lane % 16, piece 4 h + lane / 16
     const uint32_t ar = static_cast<uint32_t>((wv / WN) * TM + (ln & 15)) * 128u;
@@ -230,7 +239,7 @@ struct GemmTile {
       }
     uint32_t cur = 0;                              // the step's place in the ring
     uint32_t put = (STAGES - 1) * LDS_STEP;        // where the step STAGES - 1 on goes: the last one's place
-    for (int s = 0; s < n; ++s) {
+    for (int s = 0; s < rounds; ++s) {
       // this step has landed once at most the later ones' DMAs are in flight
       if (s + STAGES - 1 <= n)
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * (QA + QB)) : "memory");
@@ -240,6 +249,7 @@ struct GemmTile {
         feed.next();
         feed.all(lds0 + put);
       }
+      if (WK > 1 && s >= n) break;   // (the last round, for groups without a step in it)
       const uint8_t* base = lds + cur;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -255,7 +265,7 @@ struct GemmTile {
           for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
       }
       put = cur;
-      cur = cur + LDS_STEP == LDS_BYTES ? 0 : cur + LDS_STEP;
+      cur = cur + LDS_STEP == LDS_RING ? 0 : cur + LDS_STEP;
     }
   }
 
@@ -347,14 +357,39 @@ struct GemmTile {
     if (wv < 4) asm volatile("s_barrier" ::: "memory");
   }
 
+  // After run(), for what is done with the accumulators in registers: the
+  // groups' sums in the first group's, zeros in the others'.
+  static __device__ __forceinline__ void reduce(uint8_t* lds, f32x4 (&acc)[FM][FN]) {
+    if constexpr (WK > 1) {
+      gemm_sync();   // (every wave is done with the operands)
+      const int g = group();
+      f32x4* at = reinterpret_cast<f32x4*>(lds) + (wave() * FM * FN) * 64 + lane();
+      constexpr int STRIDE = NW * FM * FN * 64;
+      if (g > 0) {
+#pragma unroll
+        for (int k = 0; k < FM * FN; ++k) {
+          at[(g - 1) * STRIDE + k * 64] = acc[k / FN][k % FN];
+          acc[k / FN][k % FN] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      gemm_sync();
+      if (g == 0) {
+#pragma unroll
+        for (int k = 0; k < FM * FN; ++k)
+#pragma unroll
+          for (int q = 0; q < WK - 1; ++q) acc[k / FN][k % FN] += at[q * STRIDE + k * 64];
+      }
+    }
+  }
+
   // After run(): the accumulators by way of LDS, for stores along rows or
   // columns (a lane holds four rows of a column, too short a piece for
   // either).  Each wave has a region of its own, of CR x CC values; f(row,
   // col, View) is called for each CR x CC part of the wave's tile, whose first
   // element is (row, col) of the workgroup's tile.
   static constexpr int CR = TM < 64 ? TM : 64, CC = TN;
-  static constexpr int PIECES = CR * CC / 8 / 64;   // pieces of eight values a lane takes
-  static_assert(CC <= 64 && CR * CC * 4 * NW <= static_cast<int>(LDS_BYTES), "staging area");
+  static constexpr int PIECES = CR * CC / 8 / 64 / WK;   // pieces of eight values a lane takes
+  static_assert(CC <= 64 && CR * CC * 4 * NW * WK <= static_cast<int>(LDS_BYTES) && PIECES >= 1 && (WK == 1 || TM <= 64), "staging area");
   struct View {
     float* at;
     // where element (r, c) lies: columns in groups of 16 are turned round
@@ -363,12 +398,12 @@ struct GemmTile {
     static __device__ __forceinline__ int place(int r, int c) { return r * CC + (c ^ ((r >> 2 & (CC / 16 - 1)) << 4)); }
     // the i-th piece of this lane: eight columns of a row ...
     static __device__ __forceinline__ void row_piece(int i, int* r, int* c) {
-      const int k = i * 64 + lane();
+      const int k = (i * WK + group()) * 64 + lane();
       *r = k / (CC / 8), *c = k % (CC / 8) * 8;
     }
     // ... or eight rows of a column
     static __device__ __forceinline__ void col_piece(int i, int* r, int* c) {
-      const int k = i * 64 + lane();
+      const int k = (i * WK + group()) * 64 + lane();
       *c = k / (CR / 8), *r = k % (CR / 8) * 8;
     }
     __device__ __forceinline__ void row(int r, int c, float (&v)[8]) const {
@@ -389,15 +424,20 @@ struct GemmTile {
     // what lanes wrote is read by others from here on (one wave's LDS
     // accesses are done in order: only the compiler has to keep it)
     static __device__ __forceinline__ void turn() {
-      __builtin_amdgcn_wave_barrier();
-      asm volatile("" ::: "memory");
+      if constexpr (WK > 1) {
+        gemm_sync();   // (the groups share a region)
+      } else {
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+      }
     }
   };
   template <class F>
   static __device__ __forceinline__ void staged(uint8_t* lds, const f32x4 (&acc)[FM][FN], F&& f) {
     gemm_sync();   // (every wave is done with the operands)
     const int ln = lane(), wv = wave();
-    const View view = {reinterpret_cast<float*>(lds) + wv * (CR * CC)};
+    float* region = reinterpret_cast<float*>(lds) + wv * (CR * CC);
+    const View view = {region}, mine = {region + group() * (NW * CR * CC)};
 #pragma unroll
     for (int part = 0; part < TM / CR; ++part) {
 #pragma unroll
@@ -406,8 +446,26 @@ struct GemmTile {
         for (int j = 0; j < FN; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            view.at[View::place(16 * i + 4 * (ln >> 4) + e, 16 * j + (ln & 15))] = acc[part * (CR / 16) + i][j][e];
+            mine.at[View::place(16 * i + 4 * (ln >> 4) + e, 16 * j + (ln & 15))] = acc[part * (CR / 16) + i][j][e];
       View::turn();
+      if constexpr (WK > 1) {   // the groups' sums
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          int r, c;
+          float v[8];
+          View::row_piece(i, &r, &c);
+          view.row(r, c, v);
+#pragma unroll
+          for (int q = 1; q < WK; ++q) {
+            float x[8];
+            View{region + q * (NW * CR * CC)}.row(r, c, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += x[e];
+          }
+          view.put_row(r, c, v);
+        }
+        View::turn();
+      }
       f((wv / WN) * TM + part * CR, (wv % WN) * TN, view);
       View::turn();
     }

@@ -21,7 +21,8 @@
 //                  diagonals it is 2 to 4e-3.
 //
 // All matrices of a call go through each stage in one launch: a sum of
-// squares, the scaling, and three products a step.  A and B are symmetric:
+// squares, the scaling, and three products a step.  (Small ones are done whole by
+// a workgroup each.)  A and B are symmetric:
 // only the tiles on and below the diagonal are computed, and written twice.
 // X is kept in both orders, since A sums over n and B X over m.
 #include <hip/hip_runtime.h>
@@ -106,8 +107,24 @@ __global__ __launch_bounds__(256) void setup_kernel(Setup s, Mat* mat, int32_t* 
   }
 }
 
+// A matrix of the plan, by scalar loads (an earlier kernel wrote it: constant
+// here).
+__device__ __forceinline__ Mat get(const Table& t, int i) {
+  struct Words {
+    uint32_t w[sizeof(Mat) / 4];
+  } x;
+  const auto* p = (const __attribute__((address_space(4))) uint32_t*)reinterpret_cast<uintptr_t>(t.mat + i);
+#pragma unroll
+  for (int k = 0; k < static_cast<int>(sizeof(Mat) / 4); ++k) x.w[k] = p[k];
+  return __builtin_bit_cast(Mat, x);
+}
+
 // The matrix that tile `id` of a stage belongs to; *local: its tile there.
 __device__ __forceinline__ int find(const Table& t, int stage, int id, int* local) {
+  if (t.all == 1) {
+    *local = id;
+    return 0;
+  }
   const int32_t* st = t.start + stage * t.all;
   int at = -1;
   for (int i = 0; i < t.all; i += 64) {
@@ -177,7 +194,7 @@ template <class S>
 __global__ __launch_bounds__(256) void norm_kernel(Table t, Step s) {
   __shared__ double sums[4];
   int chunk;
-  const Mat& m = t.mat[find(t, kStageNorm, blockIdx.x, &chunk)];
+  const Mat m = get(t, find(t, kStageNorm, blockIdx.x, &chunk));
   const uint32_t all = static_cast<uint32_t>(m.rows) * m.cols, e0 = static_cast<uint32_t>(chunk) * m.chunk;
   const uint32_t e1 = e0 + m.chunk < all ? e0 + m.chunk : all;
   double sum[2] = {0., 0.};
@@ -237,7 +254,7 @@ __global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
   __shared__ float tile[64][65];
   __shared__ double sums[4];
   int id;
-  const Mat& m = t.mat[find(t, kStageFill, blockIdx.x, &id)];
+  const Mat m = get(t, find(t, kStageFill, blockIdx.x, &id));
   const int tid = threadIdx.x;
   double sum = 0.;
   for (int i = tid; i < m.chunks; i += 256) sum += m.part[i];
@@ -351,7 +368,7 @@ template <class Tile, int P, bool POLY>
 __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, PlanePairs pairs) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
   int id;
-  const Mat& m = t.mat[find(t, POLY ? kStagePoly : kStageGram, blockIdx.x, &id)];
+  const Mat m = get(t, find(t, POLY ? kStagePoly : kStageGram, blockIdx.x, &id));
   int ti, tj;
   triangle(id, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
@@ -445,7 +462,7 @@ template <class Tile, class S, int P, bool LAST>
 __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, PlanePairs pairs, int32_t turn) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
   int id;
-  const Mat& m = t.mat[find(t, kStageApply, blockIdx.x, &id)];
+  const Mat m = get(t, find(t, kStageApply, blockIdx.x, &id));
   const int mm = m.m, nn = m.n, mp = m.mp, np = m.np;
   int ti, tj;
   band_order(id, (mm + Tile::BM - 1) / Tile::BM, (nn + Tile::BN - 1) / Tile::BN, &ti, &tj);
@@ -508,15 +525,161 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
 }
 
 // ---------------------------------------------------------------------------
+// small matrices: a workgroup does all steps of one, in LDS and in fp32
+// ---------------------------------------------------------------------------
+
+// A launch costs 3 us and more on the card, and a matrix of the staged path
+// three of them a step.  Up to the sizes of tiny_fits() one CU's fp32 matrix
+// instructions take less than that, and need no pairs of values.
+constexpr int kTinyWaves = 8, kTinyRows = 64, kTinyFloats = 28000;
+constexpr int kTinyLd = 68;     // row pitch of A and B: 4 past a multiple of the banks
+__host__ __device__ constexpr int tiny_ld(int n) { return (n + 63) / 64 * 64 + 4; }
+
+bool tiny_fits(int m, int n) {
+  const int64_t m16 = (m + 15) / 16 * 16, n16 = (n + 15) / 16 * 16;
+  return m16 <= kTinyRows && m16 * tiny_ld(n) <= kTinyFloats && m16 * m16 * n16 <= 600000;
+}
+
+template <class S>
+__global__ __launch_bounds__(kTinyWaves * 64) void tiny_kernel(Setup su, Step s) {
+  __shared__ float x[kTinyFloats];
+  __shared__ float a[kTinyRows * kTinyLd], b[kTinyRows * kTinyLd];
+  __shared__ f32x4 part[kTinyWaves][64];
+  __shared__ double sums[kTinyWaves];
+  constexpr int kThreads = kTinyWaves * 64;
+  const Mat& m = su.mat[blockIdx.x];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int mt = (m.m + 15) / 16, nt = (m.n + 15) / 16, ld = tiny_ld(m.n);
+  const int all = m.rows * m.cols, cols = m.cols;
+
+  // the update, and its sum of squares
+  for (int e = tid; e < mt * 16 * ld; e += kThreads) x[e] = 0.f;
+  __syncthreads();
+  double sum = 0.;
+  for (int e = tid; e < all; e += kThreads) {
+    const int r = e / cols, c = e - r * cols;
+    float u;
+    if (m.g) {
+      const bool on = kept8(m, static_cast<uint32_t>(e), static_cast<uint32_t>(all)) & 1;
+      const float g = on ? static_cast<float>(static_cast<const S*>(m.g)[e]) : 0.f;
+      const float mom = on ? s.momentum * m.mom[e] + g : 0.f;
+      m.mom_out[e] = mom;
+      u = s.nesterov ? g + s.momentum * mom : mom;
+    } else {
+      u = static_cast<float>(static_cast<const S*>(m.u)[r * m.u_rs + c * m.u_cs]);
+    }
+    sum += static_cast<double>(u) * u;
+    x[m.turned ? c * ld + r : r * ld + c] = u;
+  }
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  sum = 0.;
+  for (int i = 0; i < kTinyWaves; ++i) sum += sums[i];
+  const float scale = static_cast<float>(1. / (sqrt(sum) + static_cast<double>(s.eps)));
+  for (int e = tid; e < mt * 16 * ld; e += kThreads) x[e] *= scale;
+  __syncthreads();
+
+  // a lane's operand values: row or column lane % 16, k lane / 16
+  const int l16 = lane & 15, lk = lane >> 4;
+  const int tiles = mt * (mt + 1) / 2, parts = tiles < kTinyWaves ? kTinyWaves / tiles : 1;
+  for (int step = 0; step < s.steps; ++step) {
+    // A: tiles on and below the diagonal, k in `parts` parts
+    for (int job = wave; job < tiles * parts; job += kTinyWaves) {
+      const int t = job / parts, p = job - t * parts;
+      int ti, tj;
+      triangle(t, &ti, &tj);
+      const int k0 = nt * p / parts * 16, k1 = nt * (p + 1) / parts * 16;
+      f32x4 acc[4] = {};
+      for (int k = k0; k < k1; k += 16)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[(ti * 16 + l16) * ld + k + 4 * q + lk], x[(tj * 16 + l16) * ld + k + 4 * q + lk],
+                                                        acc[q], 0, 0, 0);
+      const f32x4 v = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+      if (parts > 1) {
+        part[job][lane] = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[(ti * 16 + 4 * lk + e) * kTinyLd + tj * 16 + l16] = v[e];
+          a[(tj * 16 + l16) * kTinyLd + ti * 16 + 4 * lk + e] = v[e];
+        }
+      }
+    }
+    __syncthreads();
+    if (parts > 1) {
+      if (wave < tiles) {
+        f32x4 v = part[wave * parts][lane];
+        for (int p = 1; p < parts; ++p) v += part[wave * parts + p][lane];
+        int ti, tj;
+        triangle(wave, &ti, &tj);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[(ti * 16 + 4 * lk + e) * kTinyLd + tj * 16 + l16] = v[e];
+          a[(tj * 16 + l16) * kTinyLd + ti * 16 + 4 * lk + e] = v[e];
+        }
+      }
+      __syncthreads();
+    }
+    for (int job = wave; job < mt * mt; job += kTinyWaves) {
+      const int ti = job / mt, tj = job - ti * mt;
+      f32x4 acc[4] = {};
+      for (int k = 0; k < mt * 16; k += 16)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          acc[q] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[(ti * 16 + l16) * kTinyLd + k + 4 * q + lk],
+                                                        a[(tj * 16 + l16) * kTinyLd + k + 4 * q + lk], acc[q], 0, 0, 0);
+      const f32x4 v = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = (ti * 16 + 4 * lk + e) * kTinyLd + tj * 16 + l16;
+        b[at] = s.b * a[at] + s.c * v[e];
+      }
+    }
+    __syncthreads();
+    // X: a strip of 16 columns, all rows; no one else reads or writes it
+    for (int job = wave; job < nt; job += kTinyWaves) {
+      const int c = job * 16 + l16;
+      f32x4 acc[kTinyRows / 16] = {};
+      for (int k = 0; k < mt * 16; k += 4) {
+        const float v = x[(k + lk) * ld + c];
+#pragma unroll
+        for (int i = 0; i < kTinyRows / 16; ++i)
+          if (i < mt) acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[(i * 16 + l16) * kTinyLd + k + lk], v, acc[i], 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kTinyRows / 16; ++i)
+        if (i < mt) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float* at = x + (i * 16 + 4 * lk + e) * ld + c;
+            *at = s.a * *at + acc[i][e];
+          }
+        }
+    }
+    __syncthreads();
+  }
+  for (int e = tid; e < all; e += kThreads) {
+    const int r = e / cols, c = e - r * cols;
+    const float v = x[m.turned ? c * ld + r : r * ld + c];
+    if (m.g) {
+      const bool on = kept8(m, static_cast<uint32_t>(e), static_cast<uint32_t>(all)) & 1;
+      const float w = on ? (1.f - s.lr * s.decay) * static_cast<float>(static_cast<const S*>(m.w)[e]) - m.up * v : 0.f;
+      static_cast<S*>(m.w_out)[e] = static_cast<S>(w);
+    } else {
+      static_cast<S*>(m.o)[r * m.o_rs + c * m.o_cs] = static_cast<S>(v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
 
-using Big = BigTile<half_t>;
-using Mid = MidTile<half_t>;
-using Small = SmallTile<half_t>;
-
 struct Plan {
-  std::vector<Mat> mats;
+  std::vector<Mat> mats;        // those of the staged path
+  std::vector<Mat> tiny;
   int gram = kSmall, poly = kSmall, apply = kSmall;   // tiles
   int64_t blocks[kStages] = {};
   std::vector<int32_t> start[kStages];
@@ -529,7 +692,7 @@ template <class F, class G>
 int pick(const std::vector<Mat>& mats, F&& tiles, G&& steps) {
   int best = kSmall;
   double least = 1e300;
-  for (int k : {kSmall, kMid, kBig}) {
+  for (int k = 0; k < kTiles; ++k) {
     double n = 0., work = 0., most = 0.;
     for (const Mat& m : mats) {
       const double t = static_cast<double>(tiles(m, kTileEdge[k])), s = steps(m);
@@ -550,7 +713,9 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     at += (n + 255) / 256 * 256;
     return r;
   };
-  for (Mat& m : p->mats) {
+  std::vector<Mat> given;
+  given.swap(p->mats);
+  for (Mat& m : given) {
     m.turned = m.rows > m.cols;
     m.m = std::min(m.rows, m.cols), m.n = std::max(m.rows, m.cols);
     m.mp = static_cast<int32_t>(pad64(m.m)), m.np = static_cast<int32_t>(pad64(m.n));
@@ -561,6 +726,7 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     m.o_wide = piece(m.o, m.o_rs);
     m.chunk = static_cast<int32_t>(std::max<int64_t>(4096, cdiv(cdiv(all, 256), 256) * 256));
     m.chunks = static_cast<int32_t>(cdiv(all, m.chunk));
+    (tiny_fits(m.m, m.n) ? p->tiny : p->mats).push_back(m);
   }
   // long sums first, so that the longest tiles do not start last
   std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
@@ -596,28 +762,30 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
 template <int P, bool POLY>
 void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, hipStream_t st) {
   const dim3 grid(static_cast<uint32_t>(p.blocks[POLY ? kStagePoly : kStageGram]));
-  const int tile = POLY ? p.poly : p.gram;
-  if (tile == kBig)
-    hipLaunchKernelGGL((gram_kernel<Big, P, POLY>), grid, dim3(Big::THREADS), 0, st, t, s, pairs);
-  else if (tile == kMid)
-    hipLaunchKernelGGL((gram_kernel<Mid, P, POLY>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs);
-  else
-    hipLaunchKernelGGL((gram_kernel<Small, P, POLY>), grid, dim3(Small::THREADS), 0, st, t, s, pairs);
+  with_tile<half_t>(POLY ? p.poly : p.gram, [&](auto k) {
+    using Tile = decltype(k);
+    hipLaunchKernelGGL((gram_kernel<Tile, P, POLY>), grid, dim3(Tile::THREADS), 0, st, t, s, pairs);
+  });
 }
 
 template <class S, int P, bool LAST>
 void apply(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
   const dim3 grid(static_cast<uint32_t>(p.blocks[kStageApply]));
-  if (p.apply == kBig)
-    hipLaunchKernelGGL((apply_kernel<Big, S, P, LAST>), grid, dim3(Big::THREADS), 0, st, t, s, pairs, turn);
-  else if (p.apply == kMid)
-    hipLaunchKernelGGL((apply_kernel<Mid, S, P, LAST>), grid, dim3(Mid::THREADS), 0, st, t, s, pairs, turn);
-  else
-    hipLaunchKernelGGL((apply_kernel<Small, S, P, LAST>), grid, dim3(Small::THREADS), 0, st, t, s, pairs, turn);
+  with_tile<half_t>(p.apply, [&](auto k) {
+    using Tile = decltype(k);
+    hipLaunchKernelGGL((apply_kernel<Tile, S, P, LAST>), grid, dim3(Tile::THREADS), 0, st, t, s, pairs, turn);
+  });
 }
 
 template <class S, int P>
 pp_status enqueue(const Plan& p, const Step& s, uint8_t* ws, hipStream_t st) {
+  for (size_t first = 0; first < p.tiny.size(); first += kSetup) {
+    Setup su = {};
+    su.count = static_cast<int32_t>(std::min<size_t>(kSetup, p.tiny.size() - first));
+    std::copy_n(p.tiny.begin() + first, su.count, su.mat);
+    hipLaunchKernelGGL((tiny_kernel<S>), dim3(static_cast<uint32_t>(su.count)), dim3(kTinyWaves * 64), 0, st, su, s);
+  }
+  if (p.mats.empty()) return launched();
   Mat* mats = reinterpret_cast<Mat*>(ws + p.table);
   int32_t* start = reinterpret_cast<int32_t*>(mats + p.mats.size());
   const int all = static_cast<int>(p.mats.size());

@@ -35,32 +35,48 @@ inline GemmOperand rows_from(GemmOperand o, int64_t r0, int64_t rows) {
 }
 
 // The tiles of the products, and when each is used.  Measured on MI355X (us a
-// step of 64 k, a workgroup on every CU / alone on its CU; us at either end of
-// a tile): 256 x 256 phased 1.68 / 1.68 (1280 TFLOP/s at 8192^3), 6;
-// 128 x 128, two workgroups a CU, 0.52 / 0.62 (1020 TFLOP/s), 3.5; 64 x 64 with
-// four steps in flight 0.195 / 0.31 (690 TFLOP/s), 2.5.  So the large tile wins
-// wherever it fills the card, and the small ones where it would leave CUs
-// without work: 1024 x 8192 x 7168 takes 146, 118 and 205 us, 512 x 512 x 4608
-// 83, 45 and 22 us.
-enum { kBig = 0, kMid = 1, kSmall = 2 };
-template <class T> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, true>;
+// step of 64 k, with every CU full / alone on its CU; us at either end of a
+// tile): 256 x 256 phased 1.68 / 1.68 (1280 TFLOP/s at 8192^3), 6; 128 x 128,
+// two workgroups a CU, 0.52 / 0.62 (1020 TFLOP/s), 3.5; 64 x 64 with four steps
+// in flight, two a CU, 0.195 / 0.31 (690 TFLOP/s), 2.5; 64 x 64 with two groups
+// of waves that share the steps, one a CU, 0.24 / 0.2, 3.  So the large tile
+// wins wherever it fills the card, and the small ones where it would leave CUs
+// without work: 1024 x 8192 x 7168 takes 146, 118, 205 and 290 us,
+// 512 x 512 x 4608 83, 45, 23 and 18 us, 1000 x 256 x 1000 11, 6.1, 4.1 and 4.4.
+enum { kBig = 0, kMid = 1, kSmall = 2, kDeep = 3, kTiles = 4 };
+template <class T> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, 1, true>;
 template <class T> using MidTile = GemmTile<T, 128, 128, 2, 2, 2>;
 template <class T> using SmallTile = GemmTile<T, 64, 64, 2, 2, 4>;
-constexpr int kTileEdge[] = {256, 128, 64};
+template <class T> using DeepTile = GemmTile<T, 64, 64, 2, 2, 4, 2>;
+constexpr int kTileEdge[kTiles] = {256, 128, 64, 64};
 constexpr int kCUs = 256;
+
+// f(tile's type) for tile k
+template <class T, class F>
+void with_tile(int k, F&& f) {
+  if (k == kBig)
+    f(BigTile<T>());
+  else if (k == kMid)
+    f(MidTile<T>());
+  else if (k == kSmall)
+    f(SmallTile<T>());
+  else
+    f(DeepTile<T>());
+}
 
 // Modelled time in us of `tiles` tiles of `steps` steps on average, `most` at
 // most.
 inline double tile_time(int tile, double tiles, double steps, double most) {
-  constexpr double full[] = {1.68, 0.52, 0.195}, alone[] = {1.68, 0.62, 0.31}, ends[] = {6., 3.5, 2.5};
+  constexpr double full[kTiles] = {1.68, 0.52, 0.195, 0.24}, alone[kTiles] = {1.68, 0.62, 0.31, 0.2}, ends[kTiles] = {6., 3.5, 2.5, 3.};
   const double n = static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs));
-  return std::max(most * alone[tile], n * steps * full[tile]) + ends[tile] * (tile == kBig ? n : 0.5 + 0.5 * n);
+  const bool single = tile == kBig || tile == kDeep;   // one workgroup a CU
+  return std::max(most * alone[tile], n * steps * full[tile]) + ends[tile] * (single ? n : 0.5 + 0.5 * n);
 }
 
 inline int pick_tile(int64_t m, int64_t n, int64_t steps) {
   int best = kSmall;
   double least = 1e300;
-  for (int k : {kSmall, kMid, kBig}) {
+  for (int k = 0; k < kTiles; ++k) {
     const double t = tile_time(k, static_cast<double>(cdiv(m, kTileEdge[k]) * cdiv(n, kTileEdge[k])), steps, steps);
     if (t < least) least = t, best = k;
   }
@@ -76,7 +92,7 @@ struct SplitTile {
 inline SplitTile pick_split(int64_t m, int64_t n, int64_t steps) {
   SplitTile best = {kSmall, 1};
   double least = 1e300;
-  for (int k : {kSmall, kMid, kBig})
+  for (int k = 0; k < kTiles; ++k)
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
       if (s > 1 && (steps / s < 4 || static_cast<double>(s) * m * n * 4 > 256e6)) break;
       const double per = static_cast<double>(cdiv(steps, s));

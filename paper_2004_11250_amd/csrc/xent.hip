@@ -205,6 +205,7 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
   f32x4 acc[Tile::FM][Tile::FN];
   Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, 0, a.ksteps * a.pairs.n, lds, acc);
+  Tile::reduce(lds, acc);
 
   const int lane = Tile::lane(), wave = Tile::wave();
   const int rows = a.w.rows, nt = a.k.t;
@@ -220,6 +221,7 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
     }
   }
   if constexpr (!GRAD) {
+    if (Tile::group() > 0) return;
 #pragma unroll
     for (int j = 0; j < Tile::FN; ++j) {
       const int t = col0 + Tile::col_of(j);
@@ -265,7 +267,7 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
       hit[j] = -1;
       if (t < nt) {
         const int64_t y = a.k.target[t];
-        kept[j] = token_scale(a.k, t, y, &s[j]);
+        kept[j] = token_scale(a.k, t, y, &s[j]) && Tile::group() == 0;
         lse[j] = a.k.stats[t];
         const int64_t d = y - a.v0 - (row0 + Tile::row_of(0));
         if (d >= 0 && d < Tile::TM) hit[j] = static_cast<int>(d);
@@ -285,7 +287,7 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
           sum[e] += g;
           acc[i][j][e] = g;
         }
-      if (a.db_part) {
+      if (a.db_part && Tile::group() == 0) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
 #pragma unroll
@@ -533,10 +535,6 @@ __global__ __launch_bounds__(256) void slab_kernel(const float* slab, int64_t sl
 // host
 // ---------------------------------------------------------------------------
 
-using Big = BigTile<__bf16>;
-using Mid = MidTile<__bf16>;
-using Small = SmallTile<__bf16>;
-
 struct Plan {
   int64_t t = 0, d = 0, v = 0, tp = 0, dp = 0, vp = 0;   // sizes and their paddings
   int planes = 1;
@@ -617,26 +615,20 @@ template <bool GRAD, int P>
 void logits(int tile, LogitArgs& a, hipStream_t st) {
   a.tm = static_cast<int32_t>(cdiv(a.w.rows, kTileEdge[tile]));
   a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileEdge[tile]));
-  const dim3 grid(static_cast<uint32_t>(a.tm * a.tn));
-  if (tile == kBig)
-    hipLaunchKernelGGL((logit_kernel<Big, GRAD, P>), grid, dim3(Big::THREADS), 0, st, a);
-  else if (tile == kMid)
-    hipLaunchKernelGGL((logit_kernel<Mid, GRAD, P>), grid, dim3(Mid::THREADS), 0, st, a);
-  else
-    hipLaunchKernelGGL((logit_kernel<Small, GRAD, P>), grid, dim3(Small::THREADS), 0, st, a);
+  with_tile<__bf16>(tile, [&](auto t) {
+    using Tile = decltype(t);
+    hipLaunchKernelGGL((logit_kernel<Tile, GRAD, P>), dim3(static_cast<uint32_t>(a.tm * a.tn)), dim3(Tile::THREADS), 0, st, a);
+  });
 }
 
 template <class O>
 void product(int tile, ProductArgs& a, hipStream_t st) {
   a.tm = static_cast<int32_t>(cdiv(a.a.rows, kTileEdge[tile]));
   a.tn = static_cast<int32_t>(cdiv(a.b.rows, kTileEdge[tile]));
-  const dim3 grid(static_cast<uint32_t>(a.tm * a.tn * a.splits));
-  if (tile == kBig)
-    hipLaunchKernelGGL((product_kernel<Big, O>), grid, dim3(Big::THREADS), 0, st, a);
-  else if (tile == kMid)
-    hipLaunchKernelGGL((product_kernel<Mid, O>), grid, dim3(Mid::THREADS), 0, st, a);
-  else
-    hipLaunchKernelGGL((product_kernel<Small, O>), grid, dim3(Small::THREADS), 0, st, a);
+  with_tile<__bf16>(tile, [&](auto t) {
+    using Tile = decltype(t);
+    hipLaunchKernelGGL((product_kernel<Tile, O>), dim3(static_cast<uint32_t>(a.tm * a.tn * a.splits)), dim3(Tile::THREADS), 0, st, a);
+  });
 }
 
 template <class O>
@@ -732,7 +724,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     logits<true, P>(p.gl, la, st);
     if (c.db)
       hipLaunchKernelGGL(column_sum_kernel, dim3(static_cast<uint32_t>(cdiv(nv, 64))), dim3(1024), 0, st, la.db_part,
-                         static_cast<int32_t>(la.tn * (p.gl == kBig ? Big::WN : Mid::WN)), static_cast<int32_t>(nv), tok, c.db + v0);
+                         static_cast<int32_t>(la.tn * (p.gl == kBig ? 4 : 2)), static_cast<int32_t>(nv), tok, c.db + v0);
     const GemmOperand g = operand(la.g, la.g_plane, nvp, p.t, P), gt = operand(la.gt, la.gt_plane, p.tp, nv, P);
     if (c.dw) {
       wa = {};
