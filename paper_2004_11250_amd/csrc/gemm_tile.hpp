@@ -1,22 +1,27 @@
-// gemm_nt.hpp -- the matrix-core product the training operators are built on:
+// gemm_tile.hpp -- the matrix-core product the training operators are built on:
 //
 //   acc[r][c] = sum over plane pairs (p, q), sum over k of A_p[r][k] B_q[c][k]
 //
-// with both operands stored with k contiguous.  16-bit operands multiply at
-// the full matrix-core rate; an operand that needs more bits than one 16-bit
-// value holds is stored as a sum of two or three such values ("planes", the
-// first the rounded value, the next the rounded rest), and the product is the
-// sum of the plane products that matter, taken one after the other along a
-// longer k into the same fp32 accumulators.
+// Each operand is stored either with k contiguous ([row][k]) or by rows of k
+// ([k][row]), so that no operand has to be kept in two orders.  16-bit operands
+// multiply at the full matrix-core rate; an operand that needs more bits than
+// one 16-bit value holds is stored as a sum of two or three such values
+// ("planes", the first the rounded value, the next the rounded rest), and the
+// product is the sum of the plane products that matter, taken one after the
+// other along a longer k into the same fp32 accumulators.
 //
-// A workgroup of WM x WN waves owns a BM x BN tile and walks k in steps of 64.
-// A step's operands go from global memory straight into LDS (16 bytes a lane;
-// no registers), one step ahead of the products; two LDS buffers, one barrier
-// a step.  A row of 64 values is 128 bytes, the whole of the LDS banks, so the
-// 16-byte pieces of row r are stored at piece position p ^ (r & 7): the eight
-// rows that a quarter of a wave reads at once then lie in different banks.
+// A workgroup owns a BM x BN tile and walks k in steps of 64.  A step's
+// operands go from global memory straight into LDS (16 bytes a lane; no
+// registers), steps ahead of the products.  Two layouts there:
+//   k contiguous: a row of 64 values is 128 bytes; its 16-byte pieces lie at
+//     position piece ^ (row & 7), so that the eight rows that an eighth of a
+//     wave reads at once lie in different banks.
+//   rows of k: a k holds BM (BN) values; 32-byte pieces of 16 rows lie at
+//     position piece ^ swizzle(k), so that the eight k that are read at once
+//     do, and the hardware's transposing LDS read gives each lane four k of
+//     its row.
 // The permutation is applied to the global address, since the LDS side of the
-// DMA is fixed (lane after lane).  Rows past the operand's end are read
+// DMA is fixed (lane after lane).  What lies past an operand's end is read
 // through an offset outside the descriptor's range, which gives zeros.
 #pragma once
 
@@ -33,14 +38,16 @@ using u32x4_t = __attribute__((ext_vector_type(4))) uint32_t;
 
 constexpr int kBK = 64;              // k per step; operands are padded with zeros to a multiple of it
 constexpr int kMaxPlanes = 3;
-constexpr int64_t kMaxLd = 1 << 22;  // row pitch limit: a tile's rows stay within 31-bit byte offsets
+constexpr int64_t kMaxLd = 1 << 22;  // pitch limit: a tile stays within 31-bit byte offsets
 
-// one operand: up to three planes of [rows][ld], k contiguous, 16-byte aligned
-// rows
+// One operand: up to three planes of [rows][ld] with k contiguous and padded
+// with zeros to whole steps, or of [k][ld] with rows contiguous, rows a
+// multiple of 8.  16-byte aligned, ld a multiple of 8.
 struct GemmOperand {
   const void* plane[kMaxPlanes];
   int64_t ld;
   int32_t rows;
+  int32_t k;      // rows of k that are there (the second form)
 };
 
 // Which planes are multiplied, in order (the smallest products first, so that
@@ -97,11 +104,13 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
          static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
 }
 
-template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, int WK_ = 1, bool PHASED_ = false>
+template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, int WK_ = 1, bool PHASED_ = false, bool AR_ = false,
+          bool BR_ = false>
 struct GemmTile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int STAGES = STAGES_;                // steps held in LDS
   static constexpr bool PHASED = PHASED_;
+  static constexpr bool AR = AR_, BR = BR_;             // the operand is stored by rows of k
   // WK groups of WM x WN waves: each takes every WK-th step, on operands of its
   // own, and the groups' sums are added in LDS at the end
   static constexpr int WK = WK_, NW = WM * WN, THREADS = NW * WK * 64;
@@ -111,6 +120,7 @@ struct GemmTile {
   static constexpr uint32_t LDS_A = BM * kBK * 2, LDS_STEP = (BM + BN) * kBK * 2;
   static constexpr uint32_t LDS_RING = STAGES * LDS_STEP, LDS_BYTES = WK * LDS_RING;
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 16 == 0 && TN % 16 == 0, "tile");
+  static_assert((FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0 && FM <= 8 && FN <= 8, "blocks");
 
   // Row and column of acc[i][j][e] in the tile.  A lane holds four rows that
   // follow each other of one column.
@@ -121,92 +131,152 @@ struct GemmTile {
   static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % NW; }
   static __device__ __forceinline__ int group() { return WK == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW; }
 
-  // A lane's part of the addresses, and the DMAs of one step.
-  struct Feed {
-    uint64_t pa[kMaxPlanes], pb[kMaxPlanes];
-    uint32_t va[QA], vb[QB];
-    uint32_t code;
-    int ksteps, pair, kk, wv;
-    u32x4_t ra, rb;
+  using Frag = typename Mfma<T>::Frag;
 
-    __device__ __forceinline__ Feed(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0, int col0,
-                                    int ksteps_, int64_t k0, int s0) {
-      const int ln = lane();
-      wv = wave();
-      // row of DMA i: group i of the wave's groups of eight, and lane / 8
-      const uint32_t piece = static_cast<uint32_t>((ln & 7) ^ (ln >> 3)) * 16u;
-#pragma unroll
-      for (int i = 0; i < QA; ++i) {
-        const int r = 8 * group_a(i, wv) + (ln >> 3);
-        va[i] = row0 + r < A.rows ? static_cast<uint32_t>(r * static_cast<int>(A.ld) * 2) + piece : 0x80000000u;
-      }
-#pragma unroll
-      for (int i = 0; i < QB; ++i) {
-        const int r = 8 * group_b(i, wv) + (ln >> 3);
-        vb[i] = col0 + r < B.rows ? static_cast<uint32_t>(r * static_cast<int>(B.ld) * 2) + piece : 0x80000000u;
-      }
-      const int64_t offa = (static_cast<int64_t>(row0) * A.ld + k0) * 2, offb = (static_cast<int64_t>(col0) * B.ld + k0) * 2;
-#pragma unroll
-      for (int q = 0; q < kMaxPlanes; ++q) {
-        pa[q] = uniform64(reinterpret_cast<uint64_t>(A.plane[q]) + offa);
-        pb[q] = uniform64(reinterpret_cast<uint64_t>(B.plane[q]) + offb);
-      }
-      code = pairs.code;
-      ksteps = __builtin_amdgcn_readfirstlane(ksteps_);
-      pair = s0 / ksteps, kk = s0 - pair * ksteps;
+  // One operand's DMAs and LDS reads; E: rows of the tile, Q: DMAs a wave
+  // issues for a step, R: stored by rows of k.
+  template <int E, int Q, bool R, int TW>
+  struct Side {
+    static constexpr int LPR = R ? E / 8 : 8, RPI = 64 / LPR;   // lanes a stored row takes, stored rows a DMA brings
+    uint64_t base[kMaxPlanes];
+    int64_t step, left;       // bytes from a step to the next; bytes from the first step on (rows of k)
+    uint64_t now;             // the next step's address
+    int64_t rest;             // and bytes from there on
+    uint32_t off[Q];          // per lane
+    uint32_t at;              // of this lane's LDS reads
+
+    static __device__ __forceinline__ int swizzle(int k) {
+      return E >= 128 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
     }
-    // (the base is a sum taken in scalar registers, so the DMA has no vector
-    // instruction's result to wait for)
-    static __device__ __forceinline__ u32x4_t rsrc(uint64_t p, int64_t off) {
-      const uint64_t b = p + off;
+    // first: first row of the tile; which(i): the group of eight rows (k
+    // contiguous) that DMA i of this wave brings; wrow: first row of the
+    // wave's part
+    template <class F>
+    __device__ __forceinline__ void init(const GemmOperand& o, int first, int wrow, F&& which) {
+      const int ln = lane();
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        const int r = RPI * which(i) + ln / LPR, pos = ln % LPR;
+        if constexpr (R) {
+          const int piece = ((pos >> 1 ^ swizzle(r)) << 1 | (pos & 1)) * 8;
+          off[i] = first + piece < o.rows ? static_cast<uint32_t>((r * static_cast<int>(o.ld) + piece) * 2) : 0x80000000u;
+        } else {
+          off[i] = first + r < o.rows ? static_cast<uint32_t>(r * static_cast<int>(o.ld) * 2 + (pos ^ (r & 7)) * 16) : 0x80000000u;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kMaxPlanes; ++q)
+        base[q] = uniform64(reinterpret_cast<uint64_t>(o.plane[q]) + 2 * static_cast<uint64_t>(R ? first : first * o.ld));
+      step = static_cast<int64_t>(uniform64(R ? kBK * 2 * o.ld : kBK * 2));
+      left = static_cast<int64_t>(uniform64(2 * (o.k * o.ld - first)));
+      if constexpr (R) {
+        // (k = 8 (lane / 16) + lane % 16 / 4, four rows from 4 (lane % 4) on)
+        const int k = 8 * (ln >> 4) + (ln >> 2 & 3);
+        at = static_cast<uint32_t>(k * (E * 2) + ((wrow / 16) ^ swizzle(k)) * 32 + (ln & 3) * 8);
+      } else {
+        // row lane % 16, piece lane / 16
+        at = static_cast<uint32_t>((wrow + (ln & 15)) * 128 + ((ln >> 4) ^ (ln & 7)) * 16);
+      }
+    }
+    // The descriptor moves on by scalar additions, so a DMA has no vector
+    // instruction's result to wait for.
+    __device__ __forceinline__ void go(uint32_t plane, int kk) {
+      now = (plane == 0 ? base[0] : plane == 1 ? base[1] : base[2]) + static_cast<uint64_t>(kk * step);
+      if constexpr (R) rest = left - kk * step;
+    }
+    __device__ __forceinline__ void move() {
+      now += WK * step;
+      if constexpr (R) rest -= WK * step;
+    }
+    __device__ __forceinline__ u32x4_t rsrc() const {
       u32x4_t r;
-      r.x = static_cast<uint32_t>(b);
-      r.y = static_cast<uint32_t>(b >> 32) & 0xFFFFu;
+      r.x = static_cast<uint32_t>(now);
+      r.y = static_cast<uint32_t>(now >> 32) & 0xFFFFu;
       r.z = 0x7FFFFFFFu;
+      if constexpr (R) r.z = rest <= 0 ? 0u : rest < 0x7FFFFFFF ? static_cast<uint32_t>(rest) : 0x7FFFFFFFu;   // (k past the end reads zeros)
       r.w = 0x00020000u;
       return r;
     }
-    static __device__ __forceinline__ uint64_t plane(const uint64_t (&p)[kMaxPlanes], uint32_t q) {
-      return q == 0 ? p[0] : q == 1 ? p[1] : p[2];
+    // operand block i (16 rows of the wave's part), half h of the step's k,
+    // from the operand's place `buf` in LDS
+    // (constant parts are added to a pointer, so that they become the reads'
+    // immediate offsets)
+    __device__ __forceinline__ Frag read(uint32_t buf, int i, int h) const {
+      using Bytes = const __attribute__((address_space(3))) uint8_t*;
+      if constexpr (R) {
+        using Half = __attribute__((ext_vector_type(4))) short;
+        using Ptr = __attribute__((address_space(3))) Half*;
+        const Bytes p = (Bytes)(buf + (at ^ (i * 32u)));
+        const Half lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + h * (32 * E * 2)));
+        const Half hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + h * (32 * E * 2) + 4 * E * 2));
+        return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      } else {
+        const Bytes p = (Bytes)(buf + (at ^ (h * 64u)));
+        return *(const __attribute__((address_space(3))) Frag*)(p + i * 2048);
+      }
+    }
+  };
+
+  struct Feed {
+    Side<BM, QA, AR, TM> a;
+    Side<BN, QB, BR, TN> b;
+    u32x4_t ra, rb;
+    uint32_t code;
+    int ksteps, pair, kk, wv;
+
+    __device__ __forceinline__ Feed(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0, int col0,
+                                    int ksteps_, int s0) {
+      wv = wave();
+      a.init(A, row0, (wv / WN) * TM, [&](int i) { return group_a(i, wv); });
+      b.init(B, col0, (wv % WN) * TN, [&](int i) { return group_b(i, wv); });
+      b.at += LDS_A;   // (a multiple of a kilobyte: the permutations are of lower bits)
+      code = pairs.code;
+      ksteps = __builtin_amdgcn_readfirstlane(ksteps_);
+      pair = s0 / ksteps, kk = s0 - pair * ksteps;
+      a.go(code >> (4 * pair) & 3, kk), b.go(code >> (4 * pair + 2) & 3, kk);
     }
     // descriptors of the next step
     __device__ __forceinline__ void next() {
-      const uint32_t c = code >> (4 * pair);
-      const int64_t ko = static_cast<int64_t>(kk) * (kBK * 2);
-      ra = rsrc(plane(pa, c & 3), ko), rb = rsrc(plane(pb, c >> 2 & 3), ko);
+      ra = a.rsrc(), rb = b.rsrc();
       kk += WK;
-      while (kk >= ksteps) kk -= ksteps, ++pair;
+      if (kk < ksteps) {
+        a.move(), b.move();
+      } else {   // the next plane pair
+        while (kk >= ksteps) kk -= ksteps, ++pair;
+        a.go(code >> (4 * pair) & 3, kk), b.go(code >> (4 * pair + 2) & 3, kk);
+      }
     }
     template <int I>
-    __device__ __forceinline__ void a(uint32_t buf) const { gemm_dma(ra, va[I], buf + 1024u * group_a(I, wv)); }
+    __device__ __forceinline__ void dma_a(uint32_t buf) const {
+      gemm_dma(ra, a.off[I], buf + 1024u * group_a(I, wv));
+    }
     template <int I>
-    __device__ __forceinline__ void b(uint32_t buf) const { gemm_dma(rb, vb[I], buf + LDS_A + 1024u * group_b(I, wv)); }
+    __device__ __forceinline__ void dma_b(uint32_t buf) const {
+      gemm_dma(rb, b.off[I], buf + LDS_A + 1024u * group_b(I, wv));
+    }
     template <int I = 0>
     __device__ __forceinline__ void all(uint32_t buf) const {
-      if constexpr (I < QA) a<I>(buf);
-      if constexpr (I < QB) b<I>(buf);
+      if constexpr (I < QA) dma_a<I>(buf);
+      if constexpr (I < QB) dma_b<I>(buf);
       if constexpr (I + 1 < QA || I + 1 < QB) all<I + 1>(buf);
     }
   };
-  // Which group of eight rows DMA i of wave w brings.  In the phased loop DMA
-  // 0 and 1 bring the halves of every wave's rows (columns) that its first
-  // products read, 2 and 3 the others.
+  // Which kilobyte of the operand's place DMA i of wave w brings.  In the
+  // phased loop, k contiguous: DMAs 0 and 1 bring the halves of every wave's
+  // rows (columns) that its first products read, 2 and 3 the others.
   static __device__ __forceinline__ int group_a(int i, int w) {
-    if constexpr (PHASED) return (i & 1) * (TM / 8) + (i >> 1) * (TM / 16) + w;
+    if constexpr (PHASED && !AR) return (i & 1) * (TM / 8) + (i >> 1) * (TM / 16) + w;
     return NW * i + w;
   }
   static __device__ __forceinline__ int group_b(int i, int w) {
-    if constexpr (PHASED) return (2 * (i & 1) + (w >> 2)) * (TN / 8) + (i >> 1) * (TN / 16) + (w & 3);
+    if constexpr (PHASED && !BR) return (2 * (i & 1) + (w >> 2)) * (TN / 8) + (i >> 1) * (TN / 16) + (w & 3);
     return NW * i + w;
   }
 
-  using Frag = typename Mfma<T>::Frag;
-
   // steps [s0, s1) of the flattened (plane pair, k step) range; ksteps k steps
-  // a pair.  k0: first k (a multiple of 8).  lds: LDS_BYTES of shared memory.
+  // a pair.  lds: LDS_BYTES of shared memory.
   static __device__ __forceinline__ void run(const GemmOperand& A, const GemmOperand& B, PlanePairs pairs, int row0,
-                                             int col0, int ksteps, int64_t k0, int s0, int s1, uint8_t* lds,
-                                             f32x4 (&acc)[FM][FN]) {
+                                             int col0, int ksteps, int s0, int s1, uint8_t* lds, f32x4 (&acc)[FM][FN]) {
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -214,23 +284,17 @@ struct GemmTile {
     if (s0 >= s1) return;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
     const int g = group();
-    Feed feed(A, B, pairs, row0, col0, ksteps, k0, s0 + g);
+    Feed feed(A, B, pairs, row0, col0, ksteps, s0 + g);
     if constexpr (PHASED)
-      phased(feed, s1 - s0, lds, lds0, acc);
+      phased(feed, s1 - s0, lds0, acc);
     else
-      ring(feed, s1 - s0, g, lds + g * LDS_RING, lds0 + g * LDS_RING, acc);
+      ring(feed, s1 - s0, g, lds0 + g * LDS_RING, acc);
   }
 
   // A ring of STAGES steps a group, STAGES - 1 of them in flight; one barrier
   // for a step of every group.
-  static __device__ __forceinline__ void ring(Feed& feed, int steps, int g, const uint8_t* lds, uint32_t lds0,
-                                              f32x4 (&acc)[FM][FN]) {
+  static __device__ __forceinline__ void ring(Feed& feed, int steps, int g, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
     const int rounds = (steps + WK - 1) / WK, n = WK == 1 ? steps : (steps - g + WK - 1) / WK;   // this group's steps
-    const int ln = lane(), wv = wave();
-    // a lane's operand of block i, k half h: row 16 i + lane % 16, piece 4 h + lane / 16
-    const uint32_t ar = static_cast<uint32_t>((wv / WN) * TM + (ln & 15)) * 128u;
-    const uint32_t br = LDS_A + static_cast<uint32_t>((wv % WN) * TN + (ln & 15)) * 128u;
-    const uint32_t p0 = static_cast<uint32_t>((ln >> 4) ^ (ln & 7)) * 16u;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i)
       if (i < n) {
@@ -250,15 +314,14 @@ struct GemmTile {
         feed.all(lds0 + put);
       }
       if (WK > 1 && s >= n) break;   // (the last round, for groups without a step in it)
-      const uint8_t* base = lds + cur;
+      const uint32_t la = lds0 + cur;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t p = p0 ^ (h * 64u);
         Frag a[FM], b[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) b[j] = *reinterpret_cast<const Frag*>(base + br + j * 2048u + p);
+        for (int j = 0; j < FN; ++j) b[j] = feed.b.read(la, j, h);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) a[i] = *reinterpret_cast<const Frag*>(base + ar + i * 2048u + p);
+        for (int i = 0; i < FM; ++i) a[i] = feed.a.read(la, i, h);
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -273,40 +336,38 @@ struct GemmTile {
   // apart: while one group's waves feed the matrix cores, the other's read
   // their next operands from LDS and start DMAs.  A step is four phases, each
   // a quarter of the wave's tile (2 x 2 blocks of FM/2 x FN/2) over the whole
-  // step's k.  What a phase has read is overwritten from the next phase on by
-  // the step after next, so that a DMA has a step and more to land.
-  static __device__ __forceinline__ void phased(Feed& feed, int n, const uint8_t* lds, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
-    static_assert(!PHASED || (NW == 8 && QA == 4 && QB == 4 && TM / 16 == 8 && TN / 16 == 4), "phases");
-    const int ln = lane(), wv = wave();
-    const uint32_t ar = static_cast<uint32_t>((wv / WN) * TM + (ln & 15)) * 128u;
-    const uint32_t br = LDS_A + static_cast<uint32_t>((wv % WN) * TN + (ln & 15)) * 128u;
-    const uint32_t p0 = static_cast<uint32_t>((ln >> 4) ^ (ln & 7)) * 16u;
+  // step's k.  What has been read is overwritten from the next phase on by the
+  // step after next, so that a DMA has a step and more to land.
+  static __device__ __forceinline__ void phased(Feed& feed, int n, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
+    static_assert(!PHASED || (NW == 8 && WK == 1 && STAGES == 2 && QA == 4 && QB == 4 && FM == 8 && FN == 4), "phases");
+    const int wv = wave();
     constexpr int HM = FM / 2, HN = FN / 2;
-    feed.next();
-    feed.all(lds0);
-    if (n > 1) {
+    auto fetch = [&](uint32_t buf) {   // (columns first: the counts below)
       feed.next();
-      feed.all(lds0 + LDS_STEP);
+      feed.template dma_b<0>(buf), feed.template dma_b<1>(buf), feed.template dma_b<2>(buf), feed.template dma_b<3>(buf);
+      feed.template dma_a<0>(buf), feed.template dma_a<1>(buf), feed.template dma_a<2>(buf), feed.template dma_a<3>(buf);
+    };
+    fetch(lds0);
+    if (n > 1) {
+      fetch(lds0 + LDS_STEP);
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(QA + QB) : "memory");
     } else {
       gemm_sync();
     }
     if (wv >= 4) asm volatile("s_barrier" ::: "memory");
-    uint32_t cur = 0;
+    uint32_t cur = lds0;
     Frag a[2][HM], b0[2][HN], b1[2][HN];
     auto read_a = [&](int half) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < HM; ++i)
-          a[h][i] = *reinterpret_cast<const Frag*>(lds + cur + ar + (half * HM + i) * 2048u + (p0 ^ (h * 64u)));
+        for (int i = 0; i < HM; ++i) a[h][i] = feed.a.read(cur, half * HM + i, h);
     };
-    auto read_b = [&](int half, Frag (&b)[2][HN]) {
+    auto read_b = [&](uint32_t buf, int half, Frag (&b)[2][HN]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < HN; ++j)
-          b[h][j] = *reinterpret_cast<const Frag*>(lds + cur + br + (half * HN + j) * 2048u + (p0 ^ (h * 64u)));
+        for (int j = 0; j < HN; ++j) b[h][j] = feed.b.read(buf, half * HN + j, h);
     };
     auto products = [&](int mh, int nh, const Frag (&b)[2][HN]) {
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -325,34 +386,31 @@ struct GemmTile {
     };
     for (int s = 0; s < n; ++s) {
       const bool more = s + 2 < n;
-      const uint32_t buf = lds0 + cur;
-      read_b(0, b0);
+      read_b(cur, 0, b0);
       read_a(0);
       products(0, 0, b0);
-      read_b(1, b1);
+      read_b(cur, 1, b1);
       if (more) {
         feed.next();
-        feed.template a<0>(buf);
-        feed.template a<1>(buf);
-        feed.template b<0>(buf);
-        feed.template b<1>(buf);
+        if constexpr (!AR) feed.template dma_a<0>(cur), feed.template dma_a<1>(cur);
+        if constexpr (!BR) feed.template dma_b<0>(cur), feed.template dma_b<1>(cur);
       }
       products(0, 1, b1);
       read_a(1);
       if (more) {
-        feed.template b<2>(buf);
-        feed.template b<3>(buf);
+        if constexpr (BR) feed.template dma_b<0>(cur), feed.template dma_b<1>(cur);
+        feed.template dma_b<2>(cur), feed.template dma_b<3>(cur);
       }
       products(1, 1, b1);
       if (more) {
-        feed.template a<2>(buf);
-        feed.template a<3>(buf);
+        if constexpr (AR) feed.template dma_a<0>(cur), feed.template dma_a<1>(cur);
+        feed.template dma_a<2>(cur), feed.template dma_a<3>(cur);
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(QA + QB) : "memory");   // the next step has landed
       } else {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       }
       products(1, 0, b0);
-      cur = LDS_STEP - cur;
+      cur = lds0 + (LDS_STEP - (cur - lds0));
     }
     if (wv < 4) asm volatile("s_barrier" ::: "memory");
   }

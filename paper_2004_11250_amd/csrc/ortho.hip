@@ -24,7 +24,6 @@
 // squares, the scaling, and three products a step.  (Small ones are done whole by
 // a workgroup each.)  A and B are symmetric:
 // only the tiles on and below the diagonal are computed, and written twice.
-// X is kept in both orders, since A sums over n and B X over m.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -34,7 +33,7 @@
 #include <vector>
 
 #include "api_internal.hpp"
-#include "gemm_nt.hpp"
+#include "gemm_tile.hpp"
 #include "train.hpp"
 
 namespace pp {
@@ -66,8 +65,7 @@ struct Mat {
   int32_t m, n, mp, np;
   int32_t wide, o_wide;         // pieces of eight of a contiguous row are 16-byte aligned
   int32_t chunk, chunks;        // elements a workgroup of the sum of squares takes
-  half_t* xr;                   // [2 planes][m][np]
-  half_t* xt[2];                // [planes][n][mp], two in turn
+  half_t* x[2];                 // [2 planes][m][np], two in turn
   half_t* a;                    // [2][m][mp]
   half_t* b;                    // [2][m][mp]
   float *da, *db;               // [m]: the diagonals' rests of A and B (bf16)
@@ -119,8 +117,19 @@ __device__ __forceinline__ Mat get(const Table& t, int i) {
   return __builtin_bit_cast(Mat, x);
 }
 
+// A product stage's tiles over the workgroups: workgroups are dealt to the
+// eight XCDs (each with an L2 of its own) in turn, so runs of `chunk`
+// consecutive tiles, which share operands, go to one XCD each.
+struct Spread {
+  int32_t total, chunk;
+};
+__device__ __forceinline__ int spread(const Spread& s, int block) {
+  const int slot = block >> 3;
+  return (slot / s.chunk * 8 + (block & 7)) * s.chunk + slot % s.chunk;
+}
+
 // The matrix that tile `id` of a stage belongs to; *local: its tile there.
-__device__ __forceinline__ int find(const Table& t, int stage, int id, int* local) {
+__device__ __forceinline__ int find(const Table& t, int stage, const int id, int* local) {
   if (t.all == 1) {
     *local = id;
     return 0;
@@ -248,8 +257,8 @@ __device__ __forceinline__ void split(float x, half_t* h, half_t* l) {
   *l = static_cast<half_t>(x - static_cast<float>(*h));
 }
 
-// X = U / (|U| + eps), in both orders, padded with zeros.
-template <class S, int P>
+// X = U / (|U| + eps), padded with zeros.
+template <class S>
 __global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
   __shared__ float tile[64][65];
   __shared__ double sums[4];
@@ -300,41 +309,29 @@ __global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
+    if (r0 + u >= m.m) continue;
     f16x8 h, l;
-    if (r0 + u < m.m) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        half_t a, b;
-        split(tile[u][w + e], &a, &b);
-        h[e] = a, l[e] = b;
-      }
-      half_t* at = m.xr + static_cast<int64_t>(r0 + u) * m.np + c0 + w;
-      *reinterpret_cast<f16x8*>(at) = h;
-      *reinterpret_cast<f16x8*>(at + static_cast<int64_t>(m.m) * m.np) = l;
+    for (int e = 0; e < 8; ++e) {
+      half_t a, b;
+      split(tile[u][w + e], &a, &b);
+      h[e] = a, l[e] = b;
     }
-    if (c0 + u < m.n) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        half_t a, b;
-        split(tile[w + e][u], &a, &b);
-        h[e] = a, l[e] = b;
-      }
-      if (r0 + w < m.mp) {
-        half_t* at = m.xt[0] + static_cast<int64_t>(c0 + u) * m.mp + r0 + w;
-        *reinterpret_cast<f16x8*>(at) = h;
-        if constexpr (P > 1) *reinterpret_cast<f16x8*>(at + static_cast<int64_t>(m.n) * m.mp) = l;
-      }
-    }
+    half_t* at = m.x[0] + static_cast<int64_t>(r0 + u) * m.np + c0 + w;
+    *reinterpret_cast<f16x8*>(at) = h;
+    *reinterpret_cast<f16x8*>(at + static_cast<int64_t>(m.m) * m.np) = l;
   }
 }
 
-__device__ __forceinline__ GemmOperand planes_of(const half_t* p, int rows, int ld) {
+// planes [2][count][ld] as an operand whose rows (or k, by_k) are the count
+__device__ __forceinline__ GemmOperand planes_of(const half_t* p, int count, int ld, bool by_k = false) {
   GemmOperand o;
   o.plane[0] = p;
-  o.plane[1] = p + static_cast<int64_t>(rows) * ld;
+  o.plane[1] = p + static_cast<int64_t>(count) * ld;
   o.plane[2] = p;
   o.ld = __builtin_amdgcn_readfirstlane(ld);
-  o.rows = __builtin_amdgcn_readfirstlane(rows);
+  o.rows = __builtin_amdgcn_readfirstlane(by_k ? ld : count);
+  o.k = __builtin_amdgcn_readfirstlane(by_k ? count : ld);
   return o;
 }
 
@@ -365,17 +362,18 @@ __device__ __forceinline__ void pair8(const half_t* h, int64_t plane, float (&v)
 // A = X X^T (POLY false) or B = b A + c A A^T (POLY true); P: values of X, A
 // and B in the products
 template <class Tile, int P, bool POLY>
-__global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, PlanePairs pairs) {
+__global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, PlanePairs pairs, int32_t turn, Spread sp) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
-  int id;
-  const Mat m = get(t, find(t, POLY ? kStagePoly : kStageGram, blockIdx.x, &id));
+  int id = spread(sp, blockIdx.x);
+  if (id >= sp.total) return;
+  const Mat m = get(t, find(t, POLY ? kStagePoly : kStageGram, id, &id));
   int ti, tj;
   triangle(id, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
-  const GemmOperand x = POLY ? planes_of(m.a, m.m, m.mp) : planes_of(m.xr, m.m, m.np);
+  const GemmOperand x = POLY ? planes_of(m.a, m.m, m.mp) : planes_of(m.x[turn], m.m, m.np);
   const int ksteps = (POLY ? m.mp : m.np) / kBK;
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(x, x, pairs, row0, col0, ksteps, 0, 0, ksteps * pairs.n, lds, acc);
+  Tile::run(x, x, pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
   const int mm = m.m, mp = m.mp;
   const int64_t plane = static_cast<int64_t>(mm) * mp;
   const half_t* a = m.a;
@@ -459,19 +457,21 @@ __device__ __forceinline__ void put_result(const Mat& m, const Step& s, int r, i
 // X <- a X + B X; the last one writes the result instead: the orthogonalised
 // update, or the weights.
 template <class Tile, class S, int P, bool LAST>
-__global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, PlanePairs pairs, int32_t turn) {
+__global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, PlanePairs pairs, int32_t turn, Spread sp) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
-  int id;
-  const Mat m = get(t, find(t, kStageApply, blockIdx.x, &id));
+  int id = spread(sp, blockIdx.x);
+  if (id >= sp.total) return;
+  const Mat m = get(t, find(t, kStageApply, id, &id));
   const int mm = m.m, nn = m.n, mp = m.mp, np = m.np;
   int ti, tj;
   band_order(id, (mm + Tile::BM - 1) / Tile::BM, (nn + Tile::BN - 1) / Tile::BN, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
   const int ksteps = mp / kBK;
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(planes_of(m.b, mm, mp), planes_of(m.xt[turn], nn, mp), pairs, row0, col0, ksteps, 0, 0, ksteps * pairs.n, lds, acc);
-  const int64_t plane = static_cast<int64_t>(mm) * np, tplane = static_cast<int64_t>(nn) * mp;
-  half_t *xr = m.xr, *xt = m.xt[turn ^ 1];
+  Tile::run(planes_of(m.b, mm, mp), planes_of(m.x[turn], mm, np, true), pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
+  const int64_t plane = static_cast<int64_t>(mm) * np;
+  const half_t* from = m.x[turn];
+  half_t* to = m.x[turn ^ 1];
   const bool turned = m.turned;
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
     rb += row0, cb += col0;
@@ -483,7 +483,7 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
       float v[8], x[8];
       view.row(r, c, v);
       const int64_t at = static_cast<int64_t>(rb + r) * np + cb + c;
-      pair8(xr + at, plane, x);
+      pair8(from + at, plane, x);
       const float fb = LAST ? 1.f / (kSB * kSX) : 1.f / kSB, fx = LAST ? s.a / kSX : s.a;
       if constexpr (P == 1) {
         const float d = m.db[rb + r];
@@ -497,12 +497,12 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
       } else {
         f16x8 h, l;
         split8(v, &h, &l);
-        *reinterpret_cast<f16x8*>(xr + at) = h;
-        *reinterpret_cast<f16x8*>(xr + at + plane) = l;
+        *reinterpret_cast<f16x8*>(to + at) = h;
+        *reinterpret_cast<f16x8*>(to + at + plane) = l;
       }
-      if (!LAST || turned) view.put_row(r, c, v);
+      if (LAST && turned) view.put_row(r, c, v);
     }
-    if (LAST && !turned) return;
+    if (!LAST || !turned) return;
     view.turn();
 #pragma unroll 2
     for (int i = 0; i < Tile::PIECES; ++i) {
@@ -511,15 +511,7 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
       view.col_piece(i, &r, &c);
       if (cb + c >= nn || rb + r >= mp) continue;
       view.col(r, c, v);
-      if constexpr (LAST) {
-        put_result<S>(m, s, cb + c, rb + r, mm - (rb + r), v);
-      } else {
-        f16x8 h, l;   // (rows past m are zeros, as B's are)
-        split8(v, &h, &l);
-        const int64_t at = static_cast<int64_t>(cb + c) * mp + rb + r;
-        *reinterpret_cast<f16x8*>(xt + at) = h;
-        if constexpr (P > 1) *reinterpret_cast<f16x8*>(xt + at + tplane) = l;
-      }
+      put_result<S>(m, s, cb + c, rb + r, mm - (rb + r), v);
     }
   });
 }
@@ -744,10 +736,9 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
       p->blocks[k] += n[k];
       if (p->blocks[k] > (1 << 30)) return fail(PP_EUNSUPPORTED, "too many matrices, or too large, for one call");
     }
-    const size_t xn = static_cast<size_t>(m.m) * m.np * 2, tn = static_cast<size_t>(m.n) * m.mp * 2, an = static_cast<size_t>(m.m) * m.mp * 2;
-    m.xr = reinterpret_cast<half_t*>(ws + take(2 * xn));
-    m.xt[0] = reinterpret_cast<half_t*>(ws + take(planes * tn));
-    m.xt[1] = reinterpret_cast<half_t*>(ws + take(planes * tn));
+    const size_t xn = static_cast<size_t>(m.m) * m.np * 2, an = static_cast<size_t>(m.m) * m.mp * 2;
+    m.x[0] = reinterpret_cast<half_t*>(ws + take(2 * xn));
+    m.x[1] = reinterpret_cast<half_t*>(ws + take(2 * xn));
     m.a = reinterpret_cast<half_t*>(ws + take(2 * an));
     m.b = reinterpret_cast<half_t*>(ws + take(2 * an));
     m.da = reinterpret_cast<float*>(ws + take(m.m * 4));
@@ -759,21 +750,26 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
   return PP_OK;
 }
 
+Spread spread_of(int64_t tiles) {
+  return {static_cast<int32_t>(tiles), static_cast<int32_t>(std::min<int64_t>(32, cdiv(tiles, 8)))};
+}
+dim3 grid_of(const Spread& s) { return dim3(static_cast<uint32_t>(cdiv(s.total, 8 * s.chunk) * 8 * s.chunk)); }
+
 template <int P, bool POLY>
-void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, hipStream_t st) {
-  const dim3 grid(static_cast<uint32_t>(p.blocks[POLY ? kStagePoly : kStageGram]));
-  with_tile<half_t>(POLY ? p.poly : p.gram, [&](auto k) {
+void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
+  const Spread sp = spread_of(p.blocks[POLY ? kStagePoly : kStageGram]);
+  with_tile<half_t, false, false>(POLY ? p.poly : p.gram, [&](auto k) {
     using Tile = decltype(k);
-    hipLaunchKernelGGL((gram_kernel<Tile, P, POLY>), grid, dim3(Tile::THREADS), 0, st, t, s, pairs);
+    hipLaunchKernelGGL((gram_kernel<Tile, P, POLY>), grid_of(sp), dim3(Tile::THREADS), 0, st, t, s, pairs, turn, sp);
   });
 }
 
 template <class S, int P, bool LAST>
 void apply(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
-  const dim3 grid(static_cast<uint32_t>(p.blocks[kStageApply]));
-  with_tile<half_t>(p.apply, [&](auto k) {
+  const Spread sp = spread_of(p.blocks[kStageApply]);
+  with_tile<half_t, false, true>(p.apply, [&](auto k) {
     using Tile = decltype(k);
-    hipLaunchKernelGGL((apply_kernel<Tile, S, P, LAST>), grid, dim3(Tile::THREADS), 0, st, t, s, pairs, turn);
+    hipLaunchKernelGGL((apply_kernel<Tile, S, P, LAST>), grid_of(sp), dim3(Tile::THREADS), 0, st, t, s, pairs, turn, sp);
   });
 }
 
@@ -800,11 +796,11 @@ pp_status enqueue(const Plan& p, const Step& s, uint8_t* ws, hipStream_t st) {
   }
   const Table t = {mats, start, all};
   hipLaunchKernelGGL((norm_kernel<S>), dim3(static_cast<uint32_t>(p.blocks[kStageNorm])), dim3(256), 0, st, t, s);
-  hipLaunchKernelGGL((fill_kernel<S, P>), dim3(static_cast<uint32_t>(p.blocks[kStageFill])), dim3(256), 0, st, t, s);
+  hipLaunchKernelGGL((fill_kernel<S>), dim3(static_cast<uint32_t>(p.blocks[kStageFill])), dim3(256), 0, st, t, s);
   const PlanePairs pairs = P == 1 ? kPairs1 : kPairs3;
   for (int k = 0; k < s.steps; ++k) {
-    gram<P, false>(p, t, s, pairs, st);
-    gram<P, true>(p, t, s, pairs, st);
+    gram<P, false>(p, t, s, pairs, k & 1, st);
+    gram<P, true>(p, t, s, pairs, 0, st);
     if (k + 1 < s.steps)
       apply<S, P, false>(p, t, s, pairs, k & 1, st);
     else

@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <string>
 
-#include "gemm_nt.hpp"
+#include "gemm_tile.hpp"
 #include "ppk1.hpp"
 
 namespace pp {
@@ -20,54 +20,53 @@ inline pp_status launched() {
   return e == hipSuccess ? PP_OK : fail(PP_EHIP, std::string("launch: ") + hipGetErrorString(e));
 }
 
-inline GemmOperand operand(const void* base, int64_t plane_elems, int64_t ld, int64_t rows, int planes) {
+// `planes` planes of [..][ld], plane_elems elements apart; rows, k as
+// GemmOperand has them
+inline GemmOperand operand(const void* base, int64_t plane_elems, int64_t ld, int64_t rows, int64_t k, int planes) {
   GemmOperand o;
   for (int q = 0; q < kMaxPlanes; ++q)
     o.plane[q] = static_cast<const uint8_t*>(base) + (q < planes ? q : 0) * plane_elems * 2;
   o.ld = ld;
   o.rows = static_cast<int32_t>(rows);
-  return o;
-}
-inline GemmOperand rows_from(GemmOperand o, int64_t r0, int64_t rows) {
-  for (auto& p : o.plane) p = static_cast<const uint8_t*>(p) + r0 * o.ld * 2;
-  o.rows = static_cast<int32_t>(rows);
+  o.k = static_cast<int32_t>(k);
   return o;
 }
 
 // The tiles of the products, and when each is used.  Measured on MI355X (us a
 // step of 64 k, with every CU full / alone on its CU; us at either end of a
-// tile): 256 x 256 phased 1.68 / 1.68 (1280 TFLOP/s at 8192^3), 6; 128 x 128,
-// two workgroups a CU, 0.52 / 0.62 (1020 TFLOP/s), 3.5; 64 x 64 with four steps
-// in flight, two a CU, 0.195 / 0.31 (690 TFLOP/s), 2.5; 64 x 64 with two groups
-// of waves that share the steps, one a CU, 0.24 / 0.2, 3.  So the large tile
+// tile): 256 x 256 phased 1.6 / 1.15 (1310 TFLOP/s at 8192^3), 6; 128 x 128,
+// two workgroups a CU, 0.52 / 0.58 (1040 TFLOP/s), 3.5; 64 x 64 with four steps
+// in flight, two a CU, 0.19 / 0.27 (720 TFLOP/s), 2.5; 64 x 64 with two groups
+// of waves that share the steps, one a CU, 0.23 / 0.19, 3.  So the large tile
 // wins wherever it fills the card, and the small ones where it would leave CUs
-// without work: 1024 x 8192 x 7168 takes 146, 118, 205 and 290 us,
-// 512 x 512 x 4608 83, 45, 23 and 18 us, 1000 x 256 x 1000 11, 6.1, 4.1 and 4.4.
+// without work: 4096^3 takes 104, 141, 218 and 267 us, 2048^3 43, 27, 28 and
+// 35, 512 x 512 x 4608 80, 42, 20 and 17.  Operands stored by rows of k cost 5
+// to 10 % each.
 enum { kBig = 0, kMid = 1, kSmall = 2, kDeep = 3, kTiles = 4 };
-template <class T> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, 1, true>;
-template <class T> using MidTile = GemmTile<T, 128, 128, 2, 2, 2>;
-template <class T> using SmallTile = GemmTile<T, 64, 64, 2, 2, 4>;
-template <class T> using DeepTile = GemmTile<T, 64, 64, 2, 2, 4, 2>;
+template <class T, bool AR, bool BR> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, 1, true, AR, BR>;
+template <class T, bool AR, bool BR> using MidTile = GemmTile<T, 128, 128, 2, 2, 2, 1, false, AR, BR>;
+template <class T, bool AR, bool BR> using SmallTile = GemmTile<T, 64, 64, 2, 2, 4, 1, false, AR, BR>;
+template <class T, bool AR, bool BR> using DeepTile = GemmTile<T, 64, 64, 2, 2, 4, 2, false, AR, BR>;
 constexpr int kTileEdge[kTiles] = {256, 128, 64, 64};
 constexpr int kCUs = 256;
 
-// f(tile's type) for tile k
-template <class T, class F>
+// f(tile's type) for tile k; AR, BR: operands stored by rows of k
+template <class T, bool AR, bool BR, class F>
 void with_tile(int k, F&& f) {
   if (k == kBig)
-    f(BigTile<T>());
+    f(BigTile<T, AR, BR>());
   else if (k == kMid)
-    f(MidTile<T>());
+    f(MidTile<T, AR, BR>());
   else if (k == kSmall)
-    f(SmallTile<T>());
+    f(SmallTile<T, AR, BR>());
   else
-    f(DeepTile<T>());
+    f(DeepTile<T, AR, BR>());
 }
 
 // Modelled time in us of `tiles` tiles of `steps` steps on average, `most` at
 // most.
 inline double tile_time(int tile, double tiles, double steps, double most) {
-  constexpr double full[kTiles] = {1.68, 0.52, 0.195, 0.24}, alone[kTiles] = {1.68, 0.62, 0.31, 0.2}, ends[kTiles] = {6., 3.5, 2.5, 3.};
+  constexpr double full[kTiles] = {1.6, 0.52, 0.19, 0.23}, alone[kTiles] = {1.15, 0.58, 0.27, 0.19}, ends[kTiles] = {6., 3.5, 2.5, 3.};
   const double n = static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs));
   const bool single = tile == kBig || tile == kDeep;   // one workgroup a CU
   return std::max(most * alone[tile], n * steps * full[tile]) + ends[tile] * (single ? n : 0.5 + 0.5 * n);

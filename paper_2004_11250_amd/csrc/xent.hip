@@ -12,9 +12,9 @@
 // exponentials per token (a few bytes per token and 64 to 128 classes), and a
 // second kernel joins those.  Backward: the logits are computed again, a
 // piece of the classes at a time, turned into G in the epilogue (the logits
-// themselves are not rounded), rounded to the operands' type and stored in
-// both orders, since one product sums over classes and the other over tokens;
-// then the two products.  The piece bounds what the workspace holds.
+// themselves are not rounded), rounded to the operands' type and stored; then
+// the two products, one over classes and one over tokens.  The piece bounds
+// what the workspace holds.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,7 +22,7 @@
 #include <string>
 
 #include "api_internal.hpp"
-#include "gemm_nt.hpp"
+#include "gemm_tile.hpp"
 #include "train.hpp"
 
 namespace pp {
@@ -64,8 +64,8 @@ __device__ __forceinline__ bool token_scale(const Tokens& k, int t, int64_t y, f
 }
 
 // ---------------------------------------------------------------------------
-// operands: [rows][cols] of any strides -> 16-bit planes, k contiguous, padded
-// with zeros to multiples of 64, in one or both orders
+// operands: [rows][cols] of any strides -> 16-bit planes, columns contiguous and
+// padded with zeros to a multiple of 64
 // ---------------------------------------------------------------------------
 
 struct StageArgs {
@@ -74,10 +74,9 @@ struct StageArgs {
   int32_t inner, rows, cols;
   const int64_t* target;       // rows whose target is `ignore` become zeros (null: none)
   int64_t ignore;
-  __bf16* direct;              // [rows][cols padded] planes, or null
-  __bf16* turned;              // [cols][rows padded] planes, or null
-  int64_t direct_plane, turned_plane;   // elements between planes
-  int32_t cols_pad, rows_pad;
+  __bf16* out;                 // [rows][cols_pad] planes
+  int64_t plane;               // elements between planes
+  int32_t cols_pad;
   int32_t along_cols;          // columns lie closer in memory than rows
   int32_t wide;                // pieces of eight on that axis are contiguous and 16-byte aligned
 };
@@ -146,32 +145,18 @@ __global__ __launch_bounds__(256) void stage_kernel(StageArgs a) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
-    if (a.direct && r0 + u < a.rows) {
-      bf16x8 o[P];
+    if (r0 + u >= a.rows) continue;
+    bf16x8 o[P];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        __bf16 p[P];
-        bf16_planes<P>(tile[u][w + e], p);
+    for (int e = 0; e < 8; ++e) {
+      __bf16 p[P];
+      bf16_planes<P>(tile[u][w + e], p);
 #pragma unroll
-        for (int q = 0; q < P; ++q) o[q][e] = p[q];
-      }
-#pragma unroll
-      for (int q = 0; q < P; ++q)
-        *reinterpret_cast<bf16x8*>(a.direct + q * a.direct_plane + static_cast<int64_t>(r0 + u) * a.cols_pad + c0 + w) = o[q];
+      for (int q = 0; q < P; ++q) o[q][e] = p[q];
     }
-    if (a.turned && c0 + u < a.cols) {
-      bf16x8 o[P];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        __bf16 p[P];
-        bf16_planes<P>(tile[w + e][u], p);
-#pragma unroll
-        for (int q = 0; q < P; ++q) o[q][e] = p[q];
-      }
-#pragma unroll
-      for (int q = 0; q < P; ++q)
-        *reinterpret_cast<bf16x8*>(a.turned + q * a.turned_plane + static_cast<int64_t>(c0 + u) * a.rows_pad + r0 + w) = o[q];
-    }
+    for (int q = 0; q < P; ++q)
+      *reinterpret_cast<bf16x8*>(a.out + q * a.plane + static_cast<int64_t>(r0 + u) * a.cols_pad + c0 + w) = o[q];
   }
 }
 
@@ -191,9 +176,8 @@ struct LogitArgs {
   float* target_logit;     // [token]
   // gradient
   __bf16* g;               // [token][v_pad] planes
-  __bf16* gt;              // [class][t_pad] planes
-  int64_t g_plane, gt_plane;
-  int32_t v_pad, t_pad;
+  int64_t g_plane;
+  int32_t v_pad;
   float* db_part;          // [token part][w.rows], or null
 };
 
@@ -204,7 +188,7 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   band_order(xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, 0, a.ksteps * a.pairs.n, lds, acc);
+  Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, a.ksteps * a.pairs.n, lds, acc);
   Tile::reduce(lds, acc);
 
   const int lane = Tile::lane(), wave = Tile::wave();
@@ -311,14 +295,6 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
     };
     Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
       rb += row0, cb += col0;
-#pragma unroll 2
-      for (int i = 0; i < Tile::PIECES; ++i) {
-        int r, c;
-        float v[8];
-        view.row_piece(i, &r, &c);
-        view.row(r, c, v);
-        if (rb + r < rows && cb + c < a.t_pad) store(a.gt + static_cast<int64_t>(rb + r) * a.t_pad + cb + c, a.gt_plane, v);
-      }
 #pragma unroll 2
       for (int i = 0; i < Tile::PIECES; ++i) {
         int r, c;
@@ -445,9 +421,10 @@ struct OutMap {
 struct ProductArgs {
   GemmOperand a, b;
   PlanePairs pairs;
+  int32_t m, n;   // the output's size
   int32_t ksteps, tm, tn, splits;
   OutMap map;
-  float* slab;    // [split][b.rows][slab_ld] partial sums instead of the output, or null
+  float* slab;    // [split][n][slab_ld] partial sums instead of the output, or null
   int64_t slab_ld;
   int32_t add;    // the slab already holds a sum
   Tokens k;       // for the common factor
@@ -488,7 +465,7 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
   const int s0 = static_cast<int>(static_cast<int64_t>(steps) * split / a.splits);
   const int s1 = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(a.a, a.b, a.pairs, row0, col0, a.ksteps, 0, s0, s1, lds, acc);
+  Tile::run(a.a, a.b, a.pairs, row0, col0, a.ksteps, s0, s1, lds, acc);
   const float scale = a.slab ? 1.f : common_scale(a.k);
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
     rb += row0, cb += col0;
@@ -499,19 +476,19 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
       view.col_piece(i, &r, &c);
       view.col(r, c, v);
       r += rb, c += cb;
-      if (c >= a.b.rows) continue;
+      if (c >= a.n) continue;
       if (a.slab) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           if (r + 4 * h < a.slab_ld) {   // (a multiple of four)
-            f32x4* at = reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.b.rows + c) * a.slab_ld + r + 4 * h);
+            f32x4* at = reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.n + c) * a.slab_ld + r + 4 * h);
             const f32x4 x = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
             *at = a.add ? *at + x : x;
           }
       } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-          store4<O>(a.map, r + 4 * h, c, a.a.rows, f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]} * scale);
+          store4<O>(a.map, r + 4 * h, c, a.m, f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]} * scale);
       }
     }
   });
@@ -536,7 +513,7 @@ __global__ __launch_bounds__(256) void slab_kernel(const float* slab, int64_t sl
 // ---------------------------------------------------------------------------
 
 struct Plan {
-  int64_t t = 0, d = 0, v = 0, tp = 0, dp = 0, vp = 0;   // sizes and their paddings
+  int64_t t = 0, d = 0, v = 0, dp = 0, vp = 0;   // sizes and their paddings
   int planes = 1;
   PlanePairs pairs = kPairs1;
   bool w_direct = false, x_direct = false, fwd = false, bwd = false;
@@ -547,21 +524,22 @@ struct Plan {
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
   // workspace offsets
-  size_t x_k = 0, w_k = 0, x_t = 0, w_t = 0, part = 0, tl = 0, sums = 0, g = 0, gt = 0, db = 0, slab = 0, total = 0;
+  size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
 };
 
-constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of G, both orders
+constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of G
 
-Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool x_aligned, bool w_aligned) {
+Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligned, bool w_aligned) {
   Plan p;
   p.fwd = fwd, p.bwd = bwd;
   p.t = d.n * d.hw, p.d = d.d, p.v = d.v;
-  p.tp = pad64(p.t), p.dp = pad64(p.d), p.vp = pad64(p.v);
+  p.dp = pad64(p.d), p.vp = pad64(p.v);
   const bool bf16 = d.dtype == PP_BF16;
   p.planes = bf16 ? 1 : 3;
   p.pairs = bf16 ? kPairs1 : kPairs6;
   const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
-  p.x_direct = bf16 && x_aligned && d.x_sc == 1 && p.d % 64 == 0 && step % 8 == 0 && step >= p.d && step <= kMaxLd &&
+  // (dw's product reads every token's features: ignored ones are copied as zeros)
+  p.x_direct = !dw && bf16 && x_aligned && d.x_sc == 1 && p.d % 64 == 0 && step % 8 == 0 && step >= p.d && step <= kMaxLd &&
                (d.n == 1 || d.hw == 1 || d.x_sn == d.hw * d.x_sp);
   p.w_direct = bf16 && w_aligned && p.d % 64 == 0 && d.w_ld % 8 == 0 && d.w_ld <= kMaxLd;
   size_t at = 0;
@@ -580,18 +558,17 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool x_aligned, bool w
     p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
   }
   if (bwd) {
-    p.x_t = take(p.d * p.tp * e), p.w_t = take(p.d * p.vp * e);
-    p.piece = std::max<int64_t>(256, kPieceBytes / (p.tp * static_cast<int64_t>(2 * e)) / 256 * 256);
+    p.piece = std::max<int64_t>(256, kPieceBytes / (p.t * static_cast<int64_t>(e)) / 256 * 256);
     if (p.piece > p.vp) p.piece = p.vp;
     p.pieces = cdiv(p.v, p.piece);
     p.piece = std::min(p.vp, cdiv(cdiv(p.v, p.pieces), 256) * 256);   // pieces of about one size
     p.pieces = cdiv(p.v, p.piece);
-    p.g = take(p.t * p.piece * e), p.gt = take(p.piece * p.tp * e);
+    p.g = take(p.t * p.piece * e);
     p.gl = pick_tile(p.piece, p.t, p.dp / 64 * p.pairs.n);
     p.db = take(cdiv(p.t, kTileEdge[p.gl]) * 4 * p.piece * 4);
     p.dx_turned = d.dx_sc != 1;
     const int64_t dm = p.dx_turned ? p.t : p.d, dn = p.dx_turned ? p.d : p.t;
-    const SplitTile x = pick_split(dm, dn, p.piece / 64 * p.pairs.n), w = pick_split(p.d, p.piece, p.tp / 64 * p.pairs.n);
+    const SplitTile x = pick_split(dm, dn, p.piece / 64 * p.pairs.n), w = pick_split(p.d, p.piece, cdiv(p.t, 64) * p.pairs.n);
     p.dxt = x.tile, p.dx_splits = x.splits;
     p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
     p.dx_ld = cdiv(dm, 4) * 4;
@@ -607,7 +584,7 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool x_aligned, bool w
 
 template <class S, int P>
 void stage(const StageArgs& a, hipStream_t st) {
-  const int64_t blocks = static_cast<int64_t>(a.rows_pad / 64) * (a.cols_pad / 64);
+  const int64_t blocks = cdiv(a.rows, 64) * (a.cols_pad / 64);
   hipLaunchKernelGGL((stage_kernel<S, P>), dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, a);
 }
 
@@ -615,17 +592,17 @@ template <bool GRAD, int P>
 void logits(int tile, LogitArgs& a, hipStream_t st) {
   a.tm = static_cast<int32_t>(cdiv(a.w.rows, kTileEdge[tile]));
   a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileEdge[tile]));
-  with_tile<__bf16>(tile, [&](auto t) {
+  with_tile<__bf16, false, false>(tile, [&](auto t) {
     using Tile = decltype(t);
     hipLaunchKernelGGL((logit_kernel<Tile, GRAD, P>), dim3(static_cast<uint32_t>(a.tm * a.tn)), dim3(Tile::THREADS), 0, st, a);
   });
 }
 
-template <class O>
+template <class O, bool AR, bool BR>
 void product(int tile, ProductArgs& a, hipStream_t st) {
-  a.tm = static_cast<int32_t>(cdiv(a.a.rows, kTileEdge[tile]));
-  a.tn = static_cast<int32_t>(cdiv(a.b.rows, kTileEdge[tile]));
-  with_tile<__bf16>(tile, [&](auto t) {
+  a.tm = static_cast<int32_t>(cdiv(a.m, kTileEdge[tile]));
+  a.tn = static_cast<int32_t>(cdiv(a.n, kTileEdge[tile]));
+  with_tile<__bf16, AR, BR>(tile, [&](auto t) {
     using Tile = decltype(t);
     hipLaunchKernelGGL((product_kernel<Tile, O>), dim3(static_cast<uint32_t>(a.tm * a.tn * a.splits)), dim3(Tile::THREADS), 0, st, a);
   });
@@ -633,9 +610,9 @@ void product(int tile, ProductArgs& a, hipStream_t st) {
 
 template <class O>
 void join_slab(const ProductArgs& a, hipStream_t st) {
-  const int64_t n = a.slab_ld / 4 * a.b.rows;
+  const int64_t n = a.slab_ld / 4 * a.n;
   const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(cdiv(n, 256), 4096));
-  hipLaunchKernelGGL((slab_kernel<O>), dim3(grid), dim3(256), 0, st, a.slab, a.slab_ld, a.a.rows, a.b.rows, a.splits, a.map, a.k);
+  hipLaunchKernelGGL((slab_kernel<O>), dim3(grid), dim3(256), 0, st, a.slab, a.slab_ld, a.m, a.n, a.splits, a.map, a.k);
 }
 
 struct Call {
@@ -661,25 +638,21 @@ pp_status enqueue(const Plan& p, const Call& c) {
   auto bf = [&](size_t off) { return reinterpret_cast<__bf16*>(c.ws + off); };
   auto f32 = [&](size_t off) { return reinterpret_cast<float*>(c.ws + off); };
 
-  // operands: token rows and class rows, k (channels) contiguous; for the
-  // gradient also turned
+  // operands: token rows and class rows, channels contiguous
   const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
-  GemmOperand x = p.x_direct ? operand(c.x, 0, step, p.t, 1) : operand(bf(p.x_k), p.t * p.dp, p.dp, p.t, P);
-  GemmOperand w = p.w_direct ? operand(c.w, 0, d.w_ld, p.v, 1) : operand(bf(p.w_k), p.v * p.dp, p.dp, p.v, P);
-  const bool turn_x = p.bwd && c.dw, turn_w = p.bwd && c.dx;
-  if (!p.x_direct || turn_x) {
+  const GemmOperand x = p.x_direct ? operand(c.x, 0, step, p.t, p.dp, 1) : operand(bf(p.x_k), p.t * p.dp, p.dp, p.t, p.dp, P);
+  const GemmOperand w = p.w_direct ? operand(c.w, 0, d.w_ld, p.v, p.dp, 1) : operand(bf(p.w_k), p.v * p.dp, p.dp, p.v, p.dp, P);
+  if (!p.x_direct) {
     StageArgs a = {c.x, d.x_sn, d.x_sp, d.x_sc, static_cast<int32_t>(d.hw), static_cast<int32_t>(p.t), static_cast<int32_t>(p.d),
-                   c.target, d.ignore_index, p.x_direct ? nullptr : bf(p.x_k), turn_x ? bf(p.x_t) : nullptr,
-                   p.t * p.dp, p.d * p.tp, static_cast<int32_t>(p.dp), static_cast<int32_t>(p.tp)};
+                   c.target, d.ignore_index, bf(p.x_k), p.t * p.dp, static_cast<int32_t>(p.dp)};
     a.along_cols = d.x_sc <= step;
     a.wide = aligned16(c.x) && (a.along_cols ? d.x_sc == 1 && step % 8 == 0 && (d.hw == 1 || d.x_sn % 8 == 0)
                                              : d.x_sp == 1 && d.hw % 8 == 0 && d.x_sc % 8 == 0 && d.x_sn % 8 == 0);
     stage<S, P>(a, st);
   }
-  if (!p.w_direct || turn_w) {
+  if (!p.w_direct) {
     StageArgs a = {c.w, d.w_ld, 0, 1, 1, static_cast<int32_t>(p.v), static_cast<int32_t>(p.d), nullptr, 0,
-                   p.w_direct ? nullptr : bf(p.w_k), turn_w ? bf(p.w_t) : nullptr, p.v * p.dp, p.d * p.vp,
-                   static_cast<int32_t>(p.dp), static_cast<int32_t>(p.vp)};
+                   bf(p.w_k), p.v * p.dp, static_cast<int32_t>(p.dp)};
     a.along_cols = 1;
     a.wide = aligned16(c.w) && d.w_ld % 8 == 0;
     stage<S, P>(a, st);
@@ -708,50 +681,58 @@ pp_status enqueue(const Plan& p, const Call& c) {
   }
   if (!p.bwd) return PP_OK;
 
-  const GemmOperand xt = operand(bf(p.x_t), p.d * p.tp, p.tp, p.d, P);
-  const GemmOperand wt = operand(bf(p.w_t), p.d * p.vp, p.vp, p.d, P);
   const int64_t dn = p.dx_turned ? p.d : p.t;
   float* dx_slab = f32(p.slab);
   float* dw_slab = dx_slab + (p.dx_slab ? p.dx_splits * p.dx_ld * dn : 0);
+  // an operand's rows from r0 on
+  auto from = [](GemmOperand o, int64_t r0) {
+    for (auto& q : o.plane) q = static_cast<const uint8_t*>(q) + r0 * o.ld * 2;
+    return o;
+  };
+  // the same array as [k][rows]
+  auto by_k = [](GemmOperand o, int64_t rows, int64_t k) {
+    o.rows = static_cast<int32_t>(rows), o.k = static_cast<int32_t>(k);
+    return o;
+  };
   ProductArgs xa = {}, wa = {};
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t v0 = k * p.piece, nv = std::min(p.piece, p.v - v0), nvp = pad64(nv);
-    la.w = rows_from(w, v0, nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
-    la.g = bf(p.g), la.gt = bf(p.gt);
-    la.v_pad = static_cast<int32_t>(nvp), la.t_pad = static_cast<int32_t>(p.tp);
-    la.g_plane = p.t * nvp, la.gt_plane = nv * p.tp;
+    la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
+    la.g = bf(p.g), la.v_pad = static_cast<int32_t>(nvp), la.g_plane = p.t * nvp;
     la.db_part = c.db ? f32(p.db) : nullptr;
     logits<true, P>(p.gl, la, st);
     if (c.db)
       hipLaunchKernelGGL(column_sum_kernel, dim3(static_cast<uint32_t>(cdiv(nv, 64))), dim3(1024), 0, st, la.db_part,
                          static_cast<int32_t>(la.tn * (p.gl == kBig ? 4 : 2)), static_cast<int32_t>(nv), tok, c.db + v0);
-    const GemmOperand g = operand(la.g, la.g_plane, nvp, p.t, P), gt = operand(la.gt, la.gt_plane, p.tp, nv, P);
-    if (c.dw) {
+    const GemmOperand g = operand(la.g, la.g_plane, nvp, p.t, nvp, P);
+    if (c.dw) {   // d x classes, over tokens
       wa = {};
-      wa.k = tok, wa.a = xt, wa.b = gt, wa.pairs = p.pairs, wa.ksteps = static_cast<int32_t>(p.tp / 64), wa.splits = p.dw_splits;
+      wa.a = by_k(x, p.dp, p.t), wa.b = by_k(g, nvp, p.t);
+      wa.m = static_cast<int32_t>(p.d), wa.n = static_cast<int32_t>(nv);
+      wa.k = tok, wa.pairs = p.pairs, wa.ksteps = static_cast<int32_t>(cdiv(p.t, 64)), wa.splits = p.dw_splits;
       wa.map = {static_cast<S*>(c.dw) + v0 * p.d, 1, 0, p.d, 0, 1, 1, p.d % 4 == 0 && reinterpret_cast<uintptr_t>(c.dw) % 16 == 0};
       wa.slab = p.dw_slab ? dw_slab : nullptr, wa.slab_ld = p.dw_ld;
-      product<S>(p.dwt, wa, st);
+      product<S, true, true>(p.dwt, wa, st);
       if (p.dw_slab) join_slab<S>(wa, st);
     }
-    if (c.dx) {
+    if (c.dx) {   // over classes
       xa = {};
-      GemmOperand wp = wt;
-      for (auto& q : wp.plane) q = static_cast<const uint8_t*>(q) + v0 * 2;
+      const GemmOperand wp = by_k(from(w, v0), p.dp, nv);
       xa.k = tok, xa.pairs = p.pairs, xa.ksteps = static_cast<int32_t>(nvp / 64);
       xa.splits = p.dx_splits;   // (a last, smaller piece may leave some without a step: they add nothing)
+      xa.slab = p.dx_slab ? dx_slab : nullptr, xa.slab_ld = p.dx_ld, xa.add = k > 0;
       const bool aligned = reinterpret_cast<uintptr_t>(c.dx) % 16 == 0;
-      if (p.dx_turned) {
-        xa.a = g, xa.b = wp;
+      if (p.dx_turned) {   // tokens x d
+        xa.a = g, xa.b = wp, xa.m = static_cast<int32_t>(p.t), xa.n = static_cast<int32_t>(p.d);
         xa.map = {c.dx, d.dx_sn, d.dx_sp, d.dx_sc, 0, static_cast<int32_t>(d.hw), 1,
                   aligned && d.dx_sp == 1 && d.hw % 4 == 0 && d.dx_sn % 4 == 0 && d.dx_sc % 4 == 0};
-      } else {
-        xa.a = wp, xa.b = g;
+        product<S, false, true>(p.dxt, xa, st);
+      } else {             // d x tokens
+        xa.a = wp, xa.b = g, xa.m = static_cast<int32_t>(p.d), xa.n = static_cast<int32_t>(p.t);
         xa.map = {c.dx, 1, 0, d.dx_sn, d.dx_sp, 1, static_cast<int32_t>(d.hw),
                   aligned && p.d % 4 == 0 && d.dx_sn % 4 == 0 && (d.hw == 1 || d.dx_sp % 4 == 0)};
+        product<S, true, false>(p.dxt, xa, st);
       }
-      xa.slab = p.dx_slab ? dx_slab : nullptr, xa.slab_ld = p.dx_ld, xa.add = k > 0;
-      product<S>(p.dxt, xa, st);
     }
     if ((s = launched()) != PP_OK) return s;
   }
@@ -801,7 +782,7 @@ pp_status xent_call(const Call& c, bool fwd, bool bwd, size_t ws_bytes) {
     }
     return launched();
   }
-  const Plan p = make_plan(d, fwd, bwd, aligned16(c.x), aligned16(c.w));
+  const Plan p = make_plan(d, fwd, bwd, bwd && c.dw, aligned16(c.x), aligned16(c.w));
   if (!c.ws || reinterpret_cast<uintptr_t>(c.ws) % 256) return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
   if (ws_bytes < p.total) return fail(PP_ESIZE, "workspace smaller than pp_xent_workspace says");
   return d.dtype == PP_BF16 ? enqueue<__bf16, 1>(p, c) : enqueue<float, 3>(p, c);
@@ -823,7 +804,7 @@ extern "C" pp_status pp_xent_workspace(const pp_xent_desc* desc, int32_t parts, 
     return PP_OK;
   }
   // (operands that are not 16-byte aligned are copied: what the call needs at most)
-  *bytes = make_plan(*desc, parts & 1, parts & 2, false, false).total;
+  *bytes = make_plan(*desc, parts & 1, parts & 2, parts & 2, false, false).total;
   return PP_OK;
 }
 
