@@ -133,6 +133,8 @@ struct GemmTile {
 
   using Frag = typename Mfma<T>::Frag;
 
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Wint-to-pointer-cast"   // (LDS addresses are 32 bits; the host pass does not know)
   // One operand's DMAs and LDS reads; E: rows of the tile, Q: DMAs a wave
   // issues for a step, R: stored by rows of k.
   template <int E, int Q, bool R, int TW>
@@ -217,6 +219,8 @@ struct GemmTile {
     }
   };
 
+#pragma clang diagnostic pop
+
   struct Feed {
     Side<BM, QA, AR, TM> a;
     Side<BN, QB, BR, TN> b;
@@ -281,6 +285,7 @@ struct GemmTile {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    s0 = __builtin_amdgcn_readfirstlane(s0), s1 = __builtin_amdgcn_readfirstlane(s1);
     if (s0 >= s1) return;
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)lds));
     const int g = group();
@@ -440,9 +445,8 @@ struct GemmTile {
     }
   }
 
-  // After run(): the accumulators by way of LDS, for stores along rows or
-  // columns (a lane holds four rows of a column, too short a piece for
-  // either).  Each wave has a region of its own, of CR x CC values; f(row,
+  // After run(): the accumulators by way of LDS, for stores along columns or
+  // rows (a lane holds four rows of a column, too short a piece for either).  Each wave has a region of its own, of CR x CC values; f(row,
   // col, View) is called for each CR x CC part of the wave's tile, whose first
   // element is (row, col) of the workgroup's tile.
   static constexpr int CR = TM < 64 ? TM : 64, CC = TN;
@@ -450,34 +454,32 @@ struct GemmTile {
   static_assert(CC <= 64 && CR * CC * 4 * NW * WK <= static_cast<int>(LDS_BYTES) && PIECES >= 1 && (WK == 1 || TM <= 64), "staging area");
   struct View {
     float* at;
-    // where element (r, c) lies: columns in groups of 16 are turned round
-    // with r / 4, so that the four row groups a wave writes at once lie in
-    // different banks
-    static __device__ __forceinline__ int place(int r, int c) { return r * CC + (c ^ ((r >> 2 & (CC / 16 - 1)) << 4)); }
-    // the i-th piece of this lane: eight columns of a row ...
-    static __device__ __forceinline__ void row_piece(int i, int* r, int* c) {
-      const int k = (i * WK + group()) * 64 + lane();
-      *r = k / (CC / 8), *c = k % (CC / 8) * 8;
-    }
-    // ... or eight rows of a column
+    // Element (r, c): columns one after the other, rows in groups of four
+    // (what a lane's accumulator holds) that are turned round with the column,
+    // so that 16 lanes with one row group of 16 columns reach all banks.
+    static __device__ __forceinline__ int place(int r, int c) { return c * CR + ((r >> 2 ^ (c & (CR / 4 - 1))) << 2) + (r & 3); }
+    // the i-th piece of this lane: eight rows of a column ...
     static __device__ __forceinline__ void col_piece(int i, int* r, int* c) {
       const int k = (i * WK + group()) * 64 + lane();
       *c = k / (CR / 8), *r = k % (CR / 8) * 8;
     }
-    __device__ __forceinline__ void row(int r, int c, float (&v)[8]) const {
-      const f32x4* q = reinterpret_cast<const f32x4*>(at + place(r, c));
-      const f32x4 a = q[0], b = q[1];
+    // ... or eight columns of a row
+    static __device__ __forceinline__ void row_piece(int i, int* r, int* c) {
+      const int k = (i * WK + group()) * 64 + lane();
+      *r = k / (CC / 8), *c = k % (CC / 8) * 8;
+    }
+    __device__ __forceinline__ void col(int r, int c, float (&v)[8]) const {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(at + place(r, c)), b = *reinterpret_cast<const f32x4*>(at + place(r + 4, c));
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
     }
-    __device__ __forceinline__ void put_row(int r, int c, const float (&v)[8]) const {
-      f32x4* q = reinterpret_cast<f32x4*>(at + place(r, c));
-      q[0] = f32x4{v[0], v[1], v[2], v[3]};
-      q[1] = f32x4{v[4], v[5], v[6], v[7]};
+    __device__ __forceinline__ void put_col(int r, int c, const float (&v)[8]) const {
+      *reinterpret_cast<f32x4*>(at + place(r, c)) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(at + place(r + 4, c)) = f32x4{v[4], v[5], v[6], v[7]};
     }
-    __device__ __forceinline__ void col(int r, int c, float (&v)[8]) const {
+    __device__ __forceinline__ void row(int r, int c, float (&v)[8]) const {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = at[place(r + e, c)];
+      for (int e = 0; e < 8; ++e) v[e] = at[place(r, c + e)];
     }
     // what lanes wrote is read by others from here on (one wave's LDS
     // accesses are done in order: only the compiler has to keep it)
@@ -502,25 +504,23 @@ struct GemmTile {
       for (int i = 0; i < CR / 16; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            mine.at[View::place(16 * i + 4 * (ln >> 4) + e, 16 * j + (ln & 15))] = acc[part * (CR / 16) + i][j][e];
+          *reinterpret_cast<f32x4*>(mine.at + View::place(16 * i + 4 * (ln >> 4), 16 * j + (ln & 15))) = acc[part * (CR / 16) + i][j];
       View::turn();
       if constexpr (WK > 1) {   // the groups' sums
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
           int r, c;
           float v[8];
-          View::row_piece(i, &r, &c);
-          view.row(r, c, v);
+          View::col_piece(i, &r, &c);
+          view.col(r, c, v);
 #pragma unroll
           for (int q = 1; q < WK; ++q) {
             float x[8];
-            View{region + q * (NW * CR * CC)}.row(r, c, x);
+            View{region + q * (NW * CR * CC)}.col(r, c, x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += x[e];
           }
-          view.put_row(r, c, v);
+          view.put_col(r, c, v);
         }
         View::turn();
       }

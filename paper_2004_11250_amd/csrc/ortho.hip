@@ -92,6 +92,7 @@ struct Table {
   const Mat* mat;
   const int32_t* start;         // [kStages][all]
   int32_t all;
+  Mat one;                      // the matrix, if there is only one
 };
 
 __global__ __launch_bounds__(256) void setup_kernel(Setup s, Mat* mat, int32_t* start) {
@@ -108,6 +109,7 @@ __global__ __launch_bounds__(256) void setup_kernel(Setup s, Mat* mat, int32_t* 
 // A matrix of the plan, by scalar loads (an earlier kernel wrote it: constant
 // here).
 __device__ __forceinline__ Mat get(const Table& t, int i) {
+  if (t.all == 1) return t.one;
   struct Words {
     uint32_t w[sizeof(Mat) / 4];
   } x;
@@ -406,25 +408,25 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
         if (r == c + e) d[r] = static_cast<float>(l[e]);
     }
   };
+  // element (r, c) of the tile is also element (c, r) of the matrix
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
+    rb += row0, cb += col0;
 #pragma unroll 2
     for (int i = 0; i < Tile::PIECES; ++i) {
       int r, c;
       float v[8];
-      view.row_piece(i, &r, &c);
-      view.row(r, c, v);
-      r += row0 + rb, c += col0 + cb;
-      if (r < mm && c < mp) store(r, c, v);
+      view.col_piece(i, &r, &c);
+      view.col(r, c, v);
+      if (cb + c < mm && rb + r < mp) store(cb + c, rb + r, v);
     }
     if (ti != tj) {
 #pragma unroll 2
       for (int i = 0; i < Tile::PIECES; ++i) {
         int r, c;
         float v[8];
-        view.col_piece(i, &r, &c);
-        view.col(r, c, v);
-        r += row0 + rb, c += col0 + cb;
-        if (c < mm && r < mp) store(c, r, v);
+        view.row_piece(i, &r, &c);
+        view.row(r, c, v);
+        if (rb + r < mm && cb + c < mp) store(rb + r, cb + c, v);
       }
     }
   });
@@ -463,12 +465,14 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
   if (id >= sp.total) return;
   const Mat m = get(t, find(t, kStageApply, id, &id));
   const int mm = m.m, nn = m.n, mp = m.mp, np = m.np;
+  // the tile's rows are X's columns: a lane's eight rows of a tile's column
+  // follow each other in X
   int ti, tj;
-  band_order(id, (mm + Tile::BM - 1) / Tile::BM, (nn + Tile::BN - 1) / Tile::BN, &ti, &tj);
+  band_order(id, (nn + Tile::BM - 1) / Tile::BM, (mm + Tile::BN - 1) / Tile::BN, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
   const int ksteps = mp / kBK;
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(planes_of(m.b, mm, mp), planes_of(m.x[turn], mm, np, true), pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
+  Tile::run(planes_of(m.x[turn], mm, np, true), planes_of(m.b, mm, mp), pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
   const int64_t plane = static_cast<int64_t>(mm) * np;
   const half_t* from = m.x[turn];
   half_t* to = m.x[turn ^ 1];
@@ -478,29 +482,31 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
 #pragma unroll 2
     for (int i = 0; i < Tile::PIECES; ++i) {
       int r, c;
-      view.row_piece(i, &r, &c);
-      if (rb + r >= mm || cb + c >= np) continue;
+      view.col_piece(i, &r, &c);
+      if (cb + c >= mm || rb + r >= np) continue;
       float v[8], x[8];
-      view.row(r, c, v);
-      const int64_t at = static_cast<int64_t>(rb + r) * np + cb + c;
+      view.col(r, c, v);
+      const int64_t at = static_cast<int64_t>(cb + c) * np + rb + r;
       pair8(from + at, plane, x);
       const float fb = LAST ? 1.f / (kSB * kSX) : 1.f / kSB, fx = LAST ? s.a / kSX : s.a;
       if constexpr (P == 1) {
-        const float d = m.db[rb + r];
+        const float d = m.db[cb + c];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += d * x[e];
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = fx * x[e] + fb * v[e];
       if constexpr (LAST) {
-        if (!turned) put_result<S>(m, s, rb + r, cb + c, nn - (cb + c), v);
+        if (turned)
+          view.put_col(r, c, v);
+        else
+          put_result<S>(m, s, cb + c, rb + r, nn - (rb + r), v);
       } else {
         f16x8 h, l;
         split8(v, &h, &l);
         *reinterpret_cast<f16x8*>(to + at) = h;
         *reinterpret_cast<f16x8*>(to + at + plane) = l;
       }
-      if (LAST && turned) view.put_row(r, c, v);
     }
     if (!LAST || !turned) return;
     view.turn();
@@ -508,10 +514,10 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
     for (int i = 0; i < Tile::PIECES; ++i) {
       int r, c;
       float v[8];
-      view.col_piece(i, &r, &c);
-      if (cb + c >= nn || rb + r >= mp) continue;
-      view.col(r, c, v);
-      put_result<S>(m, s, cb + c, rb + r, mm - (rb + r), v);
+      view.row_piece(i, &r, &c);
+      if (rb + r >= nn || cb + c >= mm) continue;
+      view.row(r, c, v);
+      put_result<S>(m, s, rb + r, cb + c, mm - (cb + c), v);
     }
   });
 }
@@ -723,7 +729,7 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
   // long sums first, so that the longest tiles do not start last
   std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
   auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.m, t); return k * (k + 1) / 2; };
-  auto rect = [](const Mat& m, int t) { return cdiv(m.m, t) * cdiv(m.n, t); };
+  auto rect = [](const Mat& m, int t) { return cdiv(m.n, t) * cdiv(m.m, t); };
   const int pairs = planes == 1 ? 1 : 3;
   p->gram = pick(p->mats, tri, [&](const Mat& m) { return m.np / 64 * pairs; });
   p->poly = pick(p->mats, tri, [&](const Mat& m) { return m.mp / 64 * pairs; });
@@ -767,7 +773,7 @@ void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int tu
 template <class S, int P, bool LAST>
 void apply(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
   const Spread sp = spread_of(p.blocks[kStageApply]);
-  with_tile<half_t, false, true>(p.apply, [&](auto k) {
+  with_tile<half_t, true, false>(p.apply, [&](auto k) {
     using Tile = decltype(k);
     hipLaunchKernelGGL((apply_kernel<Tile, S, P, LAST>), grid_of(sp), dim3(Tile::THREADS), 0, st, t, s, pairs, turn, sp);
   });
@@ -785,7 +791,7 @@ pp_status enqueue(const Plan& p, const Step& s, uint8_t* ws, hipStream_t st) {
   Mat* mats = reinterpret_cast<Mat*>(ws + p.table);
   int32_t* start = reinterpret_cast<int32_t*>(mats + p.mats.size());
   const int all = static_cast<int>(p.mats.size());
-  for (int first = 0; first < all; first += kSetup) {
+  for (int first = 0; first < all && all > 1; first += kSetup) {
     Setup su;
     su.first = first, su.count = std::min(kSetup, all - first), su.all = all;
     for (int i = 0; i < su.count; ++i) {
@@ -794,7 +800,7 @@ pp_status enqueue(const Plan& p, const Step& s, uint8_t* ws, hipStream_t st) {
     }
     hipLaunchKernelGGL(setup_kernel, dim3(1), dim3(256), 0, st, su, mats, start);
   }
-  const Table t = {mats, start, all};
+  const Table t = {mats, start, all, p.mats[0]};
   hipLaunchKernelGGL((norm_kernel<S>), dim3(static_cast<uint32_t>(p.blocks[kStageNorm])), dim3(256), 0, st, t, s);
   hipLaunchKernelGGL((fill_kernel<S>), dim3(static_cast<uint32_t>(p.blocks[kStageFill])), dim3(256), 0, st, t, s);
   const PlanePairs pairs = P == 1 ? kPairs1 : kPairs3;

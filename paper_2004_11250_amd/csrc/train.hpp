@@ -68,8 +68,10 @@ void with_tile(int k, F&& f) {
 inline double tile_time(int tile, double tiles, double steps, double most) {
   constexpr double full[kTiles] = {1.6, 0.52, 0.19, 0.23}, alone[kTiles] = {1.15, 0.58, 0.27, 0.19}, ends[kTiles] = {6., 3.5, 2.5, 3.};
   const double n = static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs));
+  // (a card in part idle clocks higher and shares its caches among fewer)
+  const double step = alone[tile] + (std::max(full[tile], alone[tile]) - alone[tile]) * std::min(1., tiles / kCUs);
   const bool single = tile == kBig || tile == kDeep;   // one workgroup a CU
-  return std::max(most * alone[tile], n * steps * full[tile]) + ends[tile] * (single ? n : 0.5 + 0.5 * n);
+  return std::max(most * step, n > 1 ? n * steps * full[tile] : 0.) + ends[tile] * (single ? n : 0.5 + 0.5 * n);
 }
 
 inline int pick_tile(int64_t m, int64_t n, int64_t steps) {

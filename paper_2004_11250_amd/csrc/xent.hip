@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <cmath>
 #include <string>
+#include <type_traits>
 
 #include "api_internal.hpp"
 #include "gemm_tile.hpp"
@@ -93,11 +94,15 @@ __device__ __forceinline__ void bf16_planes(float x, __bf16 (&p)[P]) {
   }
 }
 
+// two arrays in one launch: the second's tiles from workgroup `first` on
 template <class S, int P>
-__global__ __launch_bounds__(256) void stage_kernel(StageArgs a) {
+__global__ __launch_bounds__(256) void stage_kernel(StageArgs one, StageArgs two, int32_t first) {
   __shared__ float tile[64][65];
+  const bool second = static_cast<int>(blockIdx.x) >= first;
+  const StageArgs& a = second ? two : one;
+  const int id = second ? blockIdx.x - first : blockIdx.x;
   const int tc = a.cols_pad / 64;
-  const int r0 = blockIdx.x / tc * 64, c0 = blockIdx.x % tc * 64, tid = threadIdx.x;
+  const int r0 = id / tc * 64, c0 = id % tc * 64, tid = threadIdx.x;
   const S* src = static_cast<const S*>(a.src);
   // a piece of eight values along the axis that is contiguous in memory
 #pragma unroll
@@ -160,6 +165,50 @@ __global__ __launch_bounds__(256) void stage_kernel(StageArgs a) {
   }
 }
 
+// The loss and its divisor (sums in 64 bits, in a fixed order), by a workgroup.
+struct LossArgs {
+  const double2* sums;   // of n workgroups of the join
+  int32_t n, mean;
+  float *out, *divisor;  // (out null: each token has its loss)
+};
+__device__ __forceinline__ void loss_sum(const LossArgs& l, double2* wave_sums) {
+  double x = 0., w = 0.;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < l.n; i += blockDim.x) {
+    const double2 s = l.sums[i];
+    x += s.x, w += s.y;
+  }
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d), w += __shfl_xor(w, d);
+  if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = make_double2(x, w);
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (unsigned i = 1; i < blockDim.x / 64; ++i) x += wave_sums[i].x, w += wave_sums[i].y;
+  // (a mean over no token: a loss of 0)
+  const double div = l.mean && !(w == 0.) ? w : 1.;
+  if (l.out) *l.out = static_cast<float>(x / div);
+  *l.divisor = static_cast<float>(div);
+}
+
+// db: 64 classes a workgroup, each wave taking every n-th part
+struct ClassSums {
+  const float* part;   // [parts][n]
+  int32_t parts, n;
+  float* out;
+};
+__device__ __forceinline__ void class_sum(const ClassSums& a, const Tokens& k, int block, float* wave_sums) {
+  const int u = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x / 64, v = block * 64 + u;
+  float s = 0.f;
+  if (v < a.n) {
+#pragma unroll 4
+    for (int p = w; p < a.parts; p += waves) s += a.part[static_cast<int64_t>(p) * a.n + v];
+  }
+  wave_sums[w * 64 + u] = s;
+  __syncthreads();
+  if (w || v >= a.n) return;
+  for (int i = 1; i < waves; ++i) s += wave_sums[i * 64 + u];
+  a.out[v] = s * common_scale(k);
+}
+
 // ---------------------------------------------------------------------------
 // the logits' product, rows = classes [v0, v0 + A.rows), columns = tokens
 // ---------------------------------------------------------------------------
@@ -170,6 +219,7 @@ struct LogitArgs {
   int32_t ksteps, tm, tn;
   int32_t v0;
   const float* bias;
+  int32_t bias_wide;       // bias + v0 is 16-byte aligned
   Tokens k;
   // statistics
   float2* part;            // [class part][token]: maximum, sum of exp(l - maximum)
@@ -179,29 +229,83 @@ struct LogitArgs {
   int64_t g_plane;
   int32_t v_pad;
   float* db_part;          // [token part][w.rows], or null
+  LossArgs loss;           // done by a workgroup past the tiles, if there is one
 };
+
+// the sum over a row of 16 lanes, in all of them
+__device__ __forceinline__ float sum16(float v) {
+  auto turned = [](float x, auto n) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + decltype(n)::value, 0xF, 0xF, true));
+  };
+  v += turned(v, std::integral_constant<int, 8>());   // (row_ror)
+  v += turned(v, std::integral_constant<int, 4>());
+  v += turned(v, std::integral_constant<int, 2>());
+  v += turned(v, std::integral_constant<int, 1>());
+  return v;
+}
 
 template <class Tile, bool GRAD, int P>
 __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
+  if (GRAD && static_cast<int>(blockIdx.x) >= a.tm * a.tn) {
+    loss_sum(a.loss, reinterpret_cast<double2*>(lds));
+    return;
+  }
   int ti, tj;
   band_order(xcd_order(blockIdx.x, a.tm * a.tn), a.tm, a.tn, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
+  const int lane = Tile::lane(), wave = Tile::wave();
+  const int rows = a.w.rows, nt = a.k.t;
+
+  // This lane's columns: what the gradient needs of each token, fetched ahead
+  // of the product.
+  float scale[Tile::FN], lse[Tile::FN];
+  int hit[Tile::FN];   // the target's row, from this lane's first one on (-1: not in the wave's)
+#pragma unroll
+  for (int j = 0; j < Tile::FN; ++j) {
+    const int t = col0 + Tile::col_of(j);
+    scale[j] = lse[j] = 0.f;
+    hit[j] = -1;
+    if (t < nt) {
+      const int64_t y = a.k.target[t];
+      const int64_t d = y - a.v0 - (row0 + Tile::row_of(0));
+      if (d >= 0 && d < Tile::TM && y - a.v0 < rows) hit[j] = static_cast<int>(d);
+      if constexpr (GRAD) {
+        if (token_scale(a.k, t, y, &scale[j])) lse[j] = a.k.stats[t];
+      }
+    }
+  }
+
   f32x4 acc[Tile::FM][Tile::FN];
   Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, a.ksteps * a.pairs.n, lds, acc);
   Tile::reduce(lds, acc);
 
-  const int lane = Tile::lane(), wave = Tile::wave();
-  const int rows = a.w.rows, nt = a.k.t;
   // the logits: bias added; classes past the end take no part
+  if (a.bias) {
+    const bool wide = a.bias_wide;
 #pragma unroll
-  for (int i = 0; i < Tile::FM; ++i) {
-    const int r = row0 + Tile::row_of(i);
+    for (int i = 0; i < Tile::FM; ++i) {
+      const int r = row0 + Tile::row_of(i);
+      f32x4 b = {0.f, 0.f, 0.f, 0.f};
+      if (wide && r + 3 < rows) {
+        b = *reinterpret_cast<const f32x4*>(a.bias + a.v0 + r);
+      } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float b = r + e < rows ? (a.bias ? a.bias[a.v0 + r + e] : 0.f) : -INFINITY;
+        for (int e = 0; e < 4; ++e)
+          if (r + e < rows) b[e] = a.bias[a.v0 + r + e];
+      }
 #pragma unroll
-      for (int j = 0; j < Tile::FN; ++j) acc[i][j][e] = r + e < rows ? acc[i][j][e] + b : -INFINITY;
+      for (int j = 0; j < Tile::FN; ++j) acc[i][j] += b;
+    }
+  }
+  if (row0 + Tile::BM > rows) {
+#pragma unroll
+    for (int i = 0; i < Tile::FM; ++i) {
+      const int r = row0 + Tile::row_of(i);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < Tile::FN; ++j) acc[i][j][e] = r + e < rows ? acc[i][j][e] : -INFINITY;
     }
   }
   if constexpr (!GRAD) {
@@ -225,57 +329,45 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
         for (int e = 0; e < 4; ++e) s += fast_exp(acc[i][j][e] - ref);
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
-      if (t < nt) {
-        if (lane < 16) a.part[static_cast<int64_t>(ti * Tile::WM + wave / Tile::WN) * nt + t] = make_float2(m, s);
-        const int64_t y = a.k.target[t] - a.v0;
-        const int64_t first = row0 + Tile::row_of(0);
-        if (y >= first && y < first + Tile::TM && y < rows) {
-          const int d = static_cast<int>(y - first);
+      if (t < nt && lane < 16) a.part[static_cast<int64_t>(ti * Tile::WM + wave / Tile::WN) * nt + t] = make_float2(m, s);
+      if (__ballot(hit[j] >= 0)) {   // (few tiles have a target's class)
 #pragma unroll
-          for (int i = 0; i < Tile::FM; ++i)
+        for (int i = 0; i < Tile::FM; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (d == 16 * i + e) a.target_logit[t] = acc[i][j][e];
-        }
+          for (int e = 0; e < 4; ++e)
+            if (hit[j] == 16 * i + e) a.target_logit[t] = acc[i][j][e];
       }
     }
   } else {
-    float s[Tile::FN], lse[Tile::FN];
-    int hit[Tile::FN];   // target's row in this lane's rows, or out of them
-    bool kept[Tile::FN];
+    const bool mine = Tile::group() == 0;
 #pragma unroll
     for (int j = 0; j < Tile::FN; ++j) {
-      const int t = col0 + Tile::col_of(j);
-      kept[j] = false;
-      s[j] = lse[j] = 0.f;
-      hit[j] = -1;
-      if (t < nt) {
-        const int64_t y = a.k.target[t];
-        kept[j] = token_scale(a.k, t, y, &s[j]) && Tile::group() == 0;
-        lse[j] = a.k.stats[t];
-        const int64_t d = y - a.v0 - (row0 + Tile::row_of(0));
-        if (d >= 0 && d < Tile::TM) hit[j] = static_cast<int>(d);
+      const bool on = mine && scale[j] != 0.f;   // (an ignored token, whatever its logits are)
+#pragma unroll
+      for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = fast_exp(acc[i][j][e] - lse[j]) * scale[j];
+          acc[i][j][e] = on ? p : 0.f;
+        }
+      if (__ballot(hit[j] >= 0)) {
+#pragma unroll
+        for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (on && hit[j] == 16 * i + e) acc[i][j][e] -= scale[j];
       }
     }
+    if (a.db_part && mine) {
 #pragma unroll
-    for (int i = 0; i < Tile::FM; ++i) {
-      const int r = row0 + Tile::row_of(i);
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < Tile::FM; ++i) {
+        const int r = row0 + Tile::row_of(i);
+        f32x4 sum = acc[i][0];
 #pragma unroll
-      for (int j = 0; j < Tile::FN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // (classes past the end: exp(-inf); they have no target)
-          float g = (fast_exp(acc[i][j][e] - lse[j]) - (hit[j] == 16 * i + e ? 1.f : 0.f)) * s[j];
-          g = kept[j] && r + e < rows ? g : 0.f;
-          sum[e] += g;
-          acc[i][j][e] = g;
-        }
-      if (a.db_part && Tile::group() == 0) {
+        for (int j = 1; j < Tile::FN; ++j) sum += acc[i][j];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-#pragma unroll
-          for (int d = 1; d < 16; d <<= 1) sum[e] += __shfl_xor(sum[e], d);
+          sum[e] = sum16(sum[e]);
           if ((lane & 15) == 0 && r + e < rows)
             a.db_part[static_cast<int64_t>(tj * Tile::WN + wave % Tile::WN) * rows + r + e] = sum[e];
         }
@@ -364,41 +456,14 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
   if (u == 0) a.sums[blockIdx.x] = make_double2(x, y);
 }
 
-// the loss and its divisor (sums in 64 bits, in a fixed order)
-__global__ __launch_bounds__(1024) void loss_kernel(const double2* sums, int32_t n, int32_t mean, float* out, float* divisor) {
-  __shared__ double a[16], b[16];
-  double x = 0., w = 0.;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += 1024) {
-    const double2 s = sums[i];
-    x += s.x, w += s.y;
-  }
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d), w += __shfl_xor(w, d);
-  if ((threadIdx.x & 63) == 0) a[threadIdx.x >> 6] = x, b[threadIdx.x >> 6] = w;
-  __syncthreads();
-  if (threadIdx.x) return;
-  for (int i = 1; i < 16; ++i) x += a[i], w += b[i];
-  // (a mean over no token: a loss of 0)
-  const double div = mean && !(w == 0.) ? w : 1.;
-  if (out) *out = static_cast<float>(x / div);
-  *divisor = static_cast<float>(div);
+__global__ __launch_bounds__(1024) void loss_kernel(LossArgs l) {
+  __shared__ double2 wave_sums[16];
+  loss_sum(l, wave_sums);
 }
 
-// 64 columns a workgroup, 16 rows of threads each taking every 16th part
-__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int32_t parts, int32_t n, Tokens k, float* out) {
-  __shared__ float got[16][64];
-  const int u = threadIdx.x & 63, w = threadIdx.x >> 6, v = blockIdx.x * 64 + u;
-  float s = 0.f;
-  if (v < n) {
-#pragma unroll 4
-    for (int p = w; p < parts; p += 16) s += part[static_cast<int64_t>(p) * n + v];
-  }
-  got[w][u] = s;
-  __syncthreads();
-  if (w || v >= n) return;
-#pragma unroll
-  for (int i = 1; i < 16; ++i) s += got[i][u];
-  out[v] = s * common_scale(k);
+__global__ __launch_bounds__(1024) void class_sum_kernel(ClassSums a, Tokens k) {
+  __shared__ float wave_sums[16 * 64];
+  class_sum(a, k, blockIdx.x, wave_sums);
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint8_t* p, int64_t bytes) {
@@ -418,6 +483,14 @@ struct OutMap {
   int32_t wide;   // four rows follow each other in memory, aligned
 };
 
+// Partial sums to be joined: [split][n][ld] -> the output.
+struct Slab {
+  float* at;
+  int64_t ld;
+  int32_t m, n, splits;
+  OutMap map;
+};
+
 struct ProductArgs {
   GemmOperand a, b;
   PlanePairs pairs;
@@ -428,6 +501,11 @@ struct ProductArgs {
   int64_t slab_ld;
   int32_t add;    // the slab already holds a sum
   Tokens k;       // for the common factor
+  // done by workgroups past the tiles: db's sums, and another product's slab
+  ClassSums db;
+  int32_t db_blocks;
+  Slab join;
+  int32_t join_blocks;
 };
 
 template <class O>
@@ -452,10 +530,32 @@ __device__ __forceinline__ void store4(const OutMap& m, int r, int c, int rows, 
     }
 }
 
+template <class O>
+__device__ __forceinline__ void join_slab(const Slab& j, const Tokens& k, int block, int blocks) {
+  const float scale = common_scale(k);
+  const int64_t n4 = j.ld / 4, all = n4 * j.n, step = static_cast<int64_t>(blocks) * blockDim.x;
+  for (int64_t i = static_cast<int64_t>(block) * blockDim.x + threadIdx.x; i < all; i += step) {
+    const int c = static_cast<int>(i / n4), r = static_cast<int>(i - c * n4) * 4;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int q = 0; q < j.splits; ++q)
+      s += *reinterpret_cast<const f32x4*>(j.at + (static_cast<int64_t>(q) * j.n + c) * j.ld + r);
+    store4<O>(j.map, r, c, j.m, s * scale);
+  }
+}
+
 template <class Tile, class O>
 __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
   __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
   const int tiles = a.tm * a.tn;
+  const int past = static_cast<int>(blockIdx.x) - tiles * a.splits;
+  if (past >= 0) {
+    if (past < a.db_blocks)
+      class_sum(a.db, a.k, past, reinterpret_cast<float*>(lds));
+    else
+      join_slab<O>(a.join, a.k, past - a.db_blocks, a.join_blocks);
+    return;
+  }
   const int id = xcd_order(blockIdx.x, tiles * a.splits);
   const int split = id / tiles;
   int ti, tj;
@@ -495,17 +595,8 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
 }
 
 template <class O>
-__global__ __launch_bounds__(256) void slab_kernel(const float* slab, int64_t slab_ld, int32_t rows, int32_t cols,
-                                                   int32_t splits, OutMap map, Tokens tok) {
-  const float scale = common_scale(tok);
-  const int64_t n4 = slab_ld / 4, all = n4 * cols;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < all; i += gridDim.x * 256ll) {
-    const int c = static_cast<int>(i / n4), r = static_cast<int>(i - c * n4) * 4;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int k = 0; k < splits; ++k)
-      s += *reinterpret_cast<const f32x4*>(slab + (static_cast<int64_t>(k) * cols + c) * slab_ld + r);
-    store4<O>(map, r, c, rows, s * scale);
-  }
+__global__ __launch_bounds__(256) void slab_kernel(Slab j, Tokens k) {
+  join_slab<O>(j, k, blockIdx.x, gridDim.x);
 }
 
 // ---------------------------------------------------------------------------
@@ -583,9 +674,11 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
 }
 
 template <class S, int P>
-void stage(const StageArgs& a, hipStream_t st) {
-  const int64_t blocks = cdiv(a.rows, 64) * (a.cols_pad / 64);
-  hipLaunchKernelGGL((stage_kernel<S, P>), dim3(static_cast<uint32_t>(blocks)), dim3(256), 0, st, a);
+void stage(const StageArgs* a, int n, hipStream_t st) {
+  int64_t blocks[2] = {0, 0};
+  for (int i = 0; i < n; ++i) blocks[i] = cdiv(a[i].rows, 64) * (a[i].cols_pad / 64);
+  hipLaunchKernelGGL((stage_kernel<S, P>), dim3(static_cast<uint32_t>(blocks[0] + blocks[1])), dim3(256), 0, st, a[0], a[n - 1],
+                     static_cast<int32_t>(blocks[0]));
 }
 
 template <bool GRAD, int P>
@@ -594,7 +687,8 @@ void logits(int tile, LogitArgs& a, hipStream_t st) {
   a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileEdge[tile]));
   with_tile<__bf16, false, false>(tile, [&](auto t) {
     using Tile = decltype(t);
-    hipLaunchKernelGGL((logit_kernel<Tile, GRAD, P>), dim3(static_cast<uint32_t>(a.tm * a.tn)), dim3(Tile::THREADS), 0, st, a);
+    hipLaunchKernelGGL((logit_kernel<Tile, GRAD, P>), dim3(static_cast<uint32_t>(a.tm * a.tn + (a.loss.divisor ? 1 : 0))),
+                       dim3(Tile::THREADS), 0, st, a);
   });
 }
 
@@ -604,15 +698,17 @@ void product(int tile, ProductArgs& a, hipStream_t st) {
   a.tn = static_cast<int32_t>(cdiv(a.n, kTileEdge[tile]));
   with_tile<__bf16, AR, BR>(tile, [&](auto t) {
     using Tile = decltype(t);
-    hipLaunchKernelGGL((product_kernel<Tile, O>), dim3(static_cast<uint32_t>(a.tm * a.tn * a.splits)), dim3(Tile::THREADS), 0, st, a);
+    hipLaunchKernelGGL((product_kernel<Tile, O>), dim3(static_cast<uint32_t>(a.tm * a.tn * a.splits + a.db_blocks + a.join_blocks)),
+                       dim3(Tile::THREADS), 0, st, a);
   });
 }
 
+Slab slab_of(const ProductArgs& a) { return {a.slab, a.slab_ld, a.m, a.n, a.splits, a.map}; }
+
 template <class O>
-void join_slab(const ProductArgs& a, hipStream_t st) {
-  const int64_t n = a.slab_ld / 4 * a.n;
-  const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(cdiv(n, 256), 4096));
-  hipLaunchKernelGGL((slab_kernel<O>), dim3(grid), dim3(256), 0, st, a.slab, a.slab_ld, a.m, a.n, a.splits, a.map, a.k);
+void launch_slab(const Slab& j, const Tokens& k, hipStream_t st) {
+  const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(cdiv(j.ld / 4 * j.n, 256), 4096));
+  hipLaunchKernelGGL((slab_kernel<O>), dim3(grid), dim3(256), 0, st, j, k);
 }
 
 struct Call {
@@ -642,27 +738,30 @@ pp_status enqueue(const Plan& p, const Call& c) {
   const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
   const GemmOperand x = p.x_direct ? operand(c.x, 0, step, p.t, p.dp, 1) : operand(bf(p.x_k), p.t * p.dp, p.dp, p.t, p.dp, P);
   const GemmOperand w = p.w_direct ? operand(c.w, 0, d.w_ld, p.v, p.dp, 1) : operand(bf(p.w_k), p.v * p.dp, p.dp, p.v, p.dp, P);
+  StageArgs staged[2];
+  int copies = 0;
   if (!p.x_direct) {
     StageArgs a = {c.x, d.x_sn, d.x_sp, d.x_sc, static_cast<int32_t>(d.hw), static_cast<int32_t>(p.t), static_cast<int32_t>(p.d),
                    c.target, d.ignore_index, bf(p.x_k), p.t * p.dp, static_cast<int32_t>(p.dp)};
     a.along_cols = d.x_sc <= step;
     a.wide = aligned16(c.x) && (a.along_cols ? d.x_sc == 1 && step % 8 == 0 && (d.hw == 1 || d.x_sn % 8 == 0)
                                              : d.x_sp == 1 && d.hw % 8 == 0 && d.x_sc % 8 == 0 && d.x_sn % 8 == 0);
-    stage<S, P>(a, st);
+    staged[copies++] = a;
   }
   if (!p.w_direct) {
     StageArgs a = {c.w, d.w_ld, 0, 1, 1, static_cast<int32_t>(p.v), static_cast<int32_t>(p.d), nullptr, 0,
                    bf(p.w_k), p.v * p.dp, static_cast<int32_t>(p.dp)};
     a.along_cols = 1;
     a.wide = aligned16(c.w) && d.w_ld % 8 == 0;
-    stage<S, P>(a, st);
+    staged[copies++] = a;
   }
+  if (copies) stage<S, P>(staged, copies, st);
   if ((s = launched()) != PP_OK) return s;
 
   LogitArgs la = {};
   la.x = x, la.pairs = p.pairs, la.ksteps = static_cast<int32_t>(p.dp / 64), la.k = tok;
   if (p.fwd) {
-    la.w = w, la.v0 = 0, la.bias = c.bias;
+    la.w = w, la.v0 = 0, la.bias = c.bias, la.bias_wide = aligned16(c.bias);
     la.part = reinterpret_cast<float2*>(c.ws + p.part), la.target_logit = f32(p.tl);
     logits<false, P>(p.logit, la, st);
     const bool each = d.reduction == PP_NONE;
@@ -675,8 +774,13 @@ pp_status enqueue(const Plan& p, const Call& c) {
       hipLaunchKernelGGL((join_kernel<16>), dim3(grid), dim3(256), 0, st, ja);
     else
       hipLaunchKernelGGL((join_kernel<4>), dim3(grid), dim3(256), 0, st, ja);
-    hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, sums, each ? 0 : static_cast<int32_t>(grid),
-                       static_cast<int32_t>(d.reduction == PP_MEAN), each ? nullptr : c.loss, c.stats + p.t);
+    // (what the loss's divisor scales comes after the gradient's first
+    // product, which takes this along)
+    const LossArgs loss = {sums, each ? 0 : static_cast<int32_t>(grid), d.reduction == PP_MEAN, each ? nullptr : c.loss, c.stats + p.t};
+    if (p.bwd)
+      la.loss = loss;
+    else
+      hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, loss);
     if ((s = launched()) != PP_OK) return s;
   }
   if (!p.bwd) return PP_OK;
@@ -697,13 +801,17 @@ pp_status enqueue(const Plan& p, const Call& c) {
   ProductArgs xa = {}, wa = {};
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t v0 = k * p.piece, nv = std::min(p.piece, p.v - v0), nvp = pad64(nv);
-    la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
+    la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias,
+    la.bias_wide = aligned16(c.bias);
     la.g = bf(p.g), la.v_pad = static_cast<int32_t>(nvp), la.g_plane = p.t * nvp;
     la.db_part = c.db ? f32(p.db) : nullptr;
     logits<true, P>(p.gl, la, st);
-    if (c.db)
-      hipLaunchKernelGGL(column_sum_kernel, dim3(static_cast<uint32_t>(cdiv(nv, 64))), dim3(1024), 0, st, la.db_part,
-                         static_cast<int32_t>(la.tn * (p.gl == kBig ? 4 : 2)), static_cast<int32_t>(nv), tok, c.db + v0);
+    la.loss = {};
+    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * (p.gl == kBig ? 4 : 2)), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
+    const int32_t db_blocks = c.db ? static_cast<int32_t>(cdiv(nv, 64)) : 0;
+    if (db_blocks && !c.dw) hipLaunchKernelGGL(class_sum_kernel, dim3(static_cast<uint32_t>(db_blocks)), dim3(1024), 0, st, db, tok);
+    // a small slab of dw is joined by dx's product, which comes after it
+    bool riding = false;
     const GemmOperand g = operand(la.g, la.g_plane, nvp, p.t, nvp, P);
     if (c.dw) {   // d x classes, over tokens
       wa = {};
@@ -712,8 +820,10 @@ pp_status enqueue(const Plan& p, const Call& c) {
       wa.k = tok, wa.pairs = p.pairs, wa.ksteps = static_cast<int32_t>(cdiv(p.t, 64)), wa.splits = p.dw_splits;
       wa.map = {static_cast<S*>(c.dw) + v0 * p.d, 1, 0, p.d, 0, 1, 1, p.d % 4 == 0 && reinterpret_cast<uintptr_t>(c.dw) % 16 == 0};
       wa.slab = p.dw_slab ? dw_slab : nullptr, wa.slab_ld = p.dw_ld;
+      wa.db = db, wa.db_blocks = db_blocks;
       product<S, true, true>(p.dwt, wa, st);
-      if (p.dw_slab) join_slab<S>(wa, st);
+      riding = p.dw_slab && c.dx && p.dw_splits * p.dw_ld * nv <= (4 << 20);
+      if (p.dw_slab && !riding) launch_slab<S>(slab_of(wa), tok, st);
     }
     if (c.dx) {   // over classes
       xa = {};
@@ -721,6 +831,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
       xa.k = tok, xa.pairs = p.pairs, xa.ksteps = static_cast<int32_t>(nvp / 64);
       xa.splits = p.dx_splits;   // (a last, smaller piece may leave some without a step: they add nothing)
       xa.slab = p.dx_slab ? dx_slab : nullptr, xa.slab_ld = p.dx_ld, xa.add = k > 0;
+      if (riding) xa.join = slab_of(wa), xa.join_blocks = static_cast<int32_t>(std::min<int64_t>(cdiv(p.dw_ld / 4 * nv, 512), 128));
       const bool aligned = reinterpret_cast<uintptr_t>(c.dx) % 16 == 0;
       if (p.dx_turned) {   // tokens x d
         xa.a = g, xa.b = wp, xa.m = static_cast<int32_t>(p.t), xa.n = static_cast<int32_t>(p.d);
@@ -736,7 +847,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     }
     if ((s = launched()) != PP_OK) return s;
   }
-  if (c.dx && p.dx_slab) join_slab<S>(xa, st);
+  if (c.dx && p.dx_slab) launch_slab<S>(slab_of(xa), tok, st);
   return launched();
 }
 
@@ -754,6 +865,7 @@ pp_status check_desc(const pp_xent_desc* d) {
 }
 
 pp_status xent_call(const Call& c, bool fwd, bool bwd, size_t ws_bytes) {
+  bwd = bwd && (c.dx || c.dw || c.db);
   pp_status s = check_desc(c.d);
   if (s != PP_OK) return s;
   const pp_xent_desc& d = *c.d;
@@ -774,14 +886,14 @@ pp_status xent_call(const Call& c, bool fwd, bool bwd, size_t ws_bytes) {
                            static_cast<uint8_t*>(q), bytes);
     };
     if (fwd)
-      hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, static_cast<const double2*>(nullptr), 0, 0,
-                         d.reduction == PP_NONE ? nullptr : c.loss, c.stats);
+      hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, LossArgs{nullptr, 0, 0, d.reduction == PP_NONE ? nullptr : c.loss, c.stats});
     if (bwd) {
       zero(c.dw, d.v * d.d * static_cast<int64_t>(esz));
       zero(c.db, d.v * 4);
     }
     return launched();
   }
+  if (!fwd && !bwd) return PP_OK;
   const Plan p = make_plan(d, fwd, bwd, bwd && c.dw, aligned16(c.x), aligned16(c.w));
   if (!c.ws || reinterpret_cast<uintptr_t>(c.ws) % 256) return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
   if (ws_bytes < p.total) return fail(PP_ESIZE, "workspace smaller than pp_xent_workspace says");
