@@ -148,7 +148,7 @@ struct GemmTile {
     uint32_t at;              // of this lane's LDS reads
 
     static __device__ __forceinline__ int swizzle(int k) {
-      return E >= 128 ? (k & 3) | (k >> 3 & 1) << 2 : (k >> 1 & 1) | (k >> 3 & 1) << 1;
+      return E >= 128 ? (k & 3) | (k >> 3 & 1) << 2 : E == 64 ? (k >> 1 & 1) | (k >> 3 & 1) << 1 : k >> 3 & 1;
     }
     // first: first row of the tile; which(i): the group of eight rows (k
     // contiguous) that DMA i of this wave brings; wrow: first row of the
@@ -450,22 +450,26 @@ struct GemmTile {
   // col, View) is called for each CR x CC part of the wave's tile, whose first
   // element is (row, col) of the workgroup's tile.
   static constexpr int CR = TM < 64 ? TM : 64, CC = TN;
-  static constexpr int PIECES = CR * CC / 8 / 64 / WK;   // pieces of eight values a lane takes
-  static_assert(CC <= 64 && CR * CC * 4 * NW * WK <= static_cast<int>(LDS_BYTES) && PIECES >= 1 && (WK == 1 || TM <= 64), "staging area");
+  // pieces of eight values a lane takes (a small part has work for SHARERS
+  // groups only)
+  static constexpr int SHARERS = CR * CC / 512 < WK ? CR * CC / 512 : WK, PIECES = CR * CC / 512 / SHARERS;
+  static_assert(CC <= 64 && CR * CC * 4 * NW * WK <= static_cast<int>(LDS_BYTES) && (WK == 1 || TM <= 64), "staging area");
   struct View {
     float* at;
     // Element (r, c): columns one after the other, rows in groups of four
     // (what a lane's accumulator holds) that are turned round with the column,
     // so that 16 lanes with one row group of 16 columns reach all banks.
     static __device__ __forceinline__ int place(int r, int c) { return c * CR + ((r >> 2 ^ (c & (CR / 4 - 1))) << 2) + (r & 3); }
-    // the i-th piece of this lane: eight rows of a column ...
+    // how many pieces this lane takes
+    static __device__ __forceinline__ int pieces() { return SHARERS == WK || group() < SHARERS ? PIECES : 0; }
+    // the i-th of them: eight rows of a column ...
     static __device__ __forceinline__ void col_piece(int i, int* r, int* c) {
-      const int k = (i * WK + group()) * 64 + lane();
+      const int k = (i * SHARERS + group()) * 64 + lane();
       *c = k / (CR / 8), *r = k % (CR / 8) * 8;
     }
     // ... or eight columns of a row
     static __device__ __forceinline__ void row_piece(int i, int* r, int* c) {
-      const int k = (i * WK + group()) * 64 + lane();
+      const int k = (i * SHARERS + group()) * 64 + lane();
       *r = k / (CC / 8), *c = k % (CC / 8) * 8;
     }
     __device__ __forceinline__ void col(int r, int c, float (&v)[8]) const {
@@ -507,8 +511,7 @@ struct GemmTile {
           *reinterpret_cast<f32x4*>(mine.at + View::place(16 * i + 4 * (ln >> 4), 16 * j + (ln & 15))) = acc[part * (CR / 16) + i][j];
       View::turn();
       if constexpr (WK > 1) {   // the groups' sums
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
+        for (int i = 0; i < View::pieces(); ++i) {
           int r, c;
           float v[8];
           View::col_piece(i, &r, &c);

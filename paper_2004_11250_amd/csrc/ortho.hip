@@ -372,7 +372,7 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
   int ti, tj;
   triangle(id, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
-  const GemmOperand x = POLY ? planes_of(m.a, m.m, m.mp) : planes_of(m.x[turn], m.m, m.np);
+  const GemmOperand x = POLY ? planes_of(m.a, m.m, m.mp) : planes_of(turn ? m.x[1] : m.x[0], m.m, m.np);
   const int ksteps = (POLY ? m.mp : m.np) / kBK;
   f32x4 acc[Tile::FM][Tile::FN];
   Tile::run(x, x, pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
@@ -381,53 +381,62 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
   const half_t* a = m.a;
   half_t* out = POLY ? m.b : m.a;
   const float fa = s.b * (kSB / kSA), fc = POLY ? s.c * (kSB / (kSA * kSA)) : kSA / (kSX * kSX);
-  // (rows past m are zeros in both operands, so the padding comes out as zeros)
-  auto store = [&](int r, int c, float (&v)[8]) {
-    const int64_t at = static_cast<int64_t>(r) * mp + c;
-    if constexpr (POLY) {
-      const f16x8 h = *reinterpret_cast<const f16x8*>(a + at), l = *reinterpret_cast<const f16x8*>(a + at + plane);
-      if constexpr (P == 1) {
-        const float d = m.da[r];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += static_cast<float>(h[e]) * (d + m.da[c + e < mm ? c + e : mm - 1]);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fc * v[e] + fa * (static_cast<float>(h[e]) + static_cast<float>(l[e]));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= fc;
-    }
-    f16x8 h, l;
-    split8(v, &h, &l);
-    *reinterpret_cast<f16x8*>(out + at) = h;
-    if (!POLY || P > 1) *reinterpret_cast<f16x8*>(out + at + plane) = l;
-    if (P == 1 && r >= c && r < c + 8) {
-      float* d = POLY ? m.db : m.da;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (r == c + e) d[r] = static_cast<float>(l[e]);
-    }
-  };
-  // element (r, c) of the tile is also element (c, r) of the matrix
+  // Element (r, c) of the tile is also element (c, r) of the matrix: columns are
+  // stored first, by their finished values, which then go out again as rows.
+  // (Rows past m are zeros in both operands, so the padding comes out as zeros.)
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
     rb += row0, cb += col0;
-#pragma unroll 2
-    for (int i = 0; i < Tile::PIECES; ++i) {
+#pragma unroll 4
+    for (int i = 0; i < view.pieces(); ++i) {
       int r, c;
-      float v[8];
       view.col_piece(i, &r, &c);
+      const int y = cb + c, x = rb + r;   // (y, x .. x + 7) of the matrix
+      if (y >= mm || x >= mp) continue;
+      float v[8];
       view.col(r, c, v);
-      if (cb + c < mm && rb + r < mp) store(cb + c, rb + r, v);
-    }
-    if (ti != tj) {
-#pragma unroll 2
-      for (int i = 0; i < Tile::PIECES; ++i) {
-        int r, c;
-        float v[8];
-        view.row_piece(i, &r, &c);
-        view.row(r, c, v);
-        if (rb + r < mm && cb + c < mp) store(rb + r, cb + c, v);
+      const int64_t at = static_cast<int64_t>(y) * mp + x;
+      if constexpr (POLY) {
+        const f16x8 h = *reinterpret_cast<const f16x8*>(a + at), l = *reinterpret_cast<const f16x8*>(a + at + plane);
+        if constexpr (P == 1) {
+          const float d = m.da[y];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += static_cast<float>(h[e]) * (d + m.da[x + e < mm ? x + e : mm - 1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fc * v[e] + fa * (static_cast<float>(h[e]) + static_cast<float>(l[e]));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= fc;
       }
+      if (ti != tj) view.put_col(r, c, v);
+      f16x8 h, l;
+      split8(v, &h, &l);
+      *reinterpret_cast<f16x8*>(out + at) = h;
+      if (!POLY || P > 1) *reinterpret_cast<f16x8*>(out + at + plane) = l;
+      if (P == 1 && y >= x && y < x + 8) {
+        float* d = POLY ? m.db : m.da;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (y == x + e) d[y] = static_cast<float>(l[e]);
+      }
+    }
+    if (ti == tj) return;
+    view.turn();
+#pragma unroll 4
+    for (int i = 0; i < view.pieces(); ++i) {
+      int r, c;
+      view.row_piece(i, &r, &c);
+      if (rb + r >= mm || cb + c >= mp) continue;
+      float v[8];
+      view.row(r, c, v);
+      f16x8 h, l;
+      split8(v, &h, &l);
+      const int64_t at = static_cast<int64_t>(rb + r) * mp + cb + c;
+      *reinterpret_cast<f16x8*>(out + at) = h;
+      // (else only this half's rests that share a tile of the next product with
+      // the diagonal are read)
+      if (P > 1 || (!POLY && (rb + r) / kTileEdge[kBig] == (cb + c) / kTileEdge[kBig]))
+        *reinterpret_cast<f16x8*>(out + at + plane) = l;
     }
   });
 }
@@ -468,19 +477,19 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
   // the tile's rows are X's columns: a lane's eight rows of a tile's column
   // follow each other in X
   int ti, tj;
-  band_order(id, (nn + Tile::BM - 1) / Tile::BM, (mm + Tile::BN - 1) / Tile::BN, &ti, &tj);
+  band_order(id, (np + Tile::BM - 1) / Tile::BM, (mm + Tile::BN - 1) / Tile::BN, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
   const int ksteps = mp / kBK;
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(planes_of(m.x[turn], mm, np, true), planes_of(m.b, mm, mp), pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
+  const half_t* from = turn ? m.x[1] : m.x[0];
+  half_t* to = turn ? m.x[0] : m.x[1];
+  Tile::run(planes_of(from, mm, np, true), planes_of(m.b, mm, mp), pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
   const int64_t plane = static_cast<int64_t>(mm) * np;
-  const half_t* from = m.x[turn];
-  half_t* to = m.x[turn ^ 1];
   const bool turned = m.turned;
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
     rb += row0, cb += col0;
-#pragma unroll 2
-    for (int i = 0; i < Tile::PIECES; ++i) {
+#pragma unroll 4
+    for (int i = 0; i < view.pieces(); ++i) {
       int r, c;
       view.col_piece(i, &r, &c);
       if (cb + c >= mm || rb + r >= np) continue;
@@ -510,8 +519,8 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
     }
     if (!LAST || !turned) return;
     view.turn();
-#pragma unroll 2
-    for (int i = 0; i < Tile::PIECES; ++i) {
+#pragma unroll 4
+    for (int i = 0; i < view.pieces(); ++i) {
       int r, c;
       float v[8];
       view.row_piece(i, &r, &c);
@@ -728,8 +737,8 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
   }
   // long sums first, so that the longest tiles do not start last
   std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
-  auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.m, t); return k * (k + 1) / 2; };
-  auto rect = [](const Mat& m, int t) { return cdiv(m.n, t) * cdiv(m.m, t); };
+  auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.mp, t); return k * (k + 1) / 2; };   // (the padding is written too)
+  auto rect = [](const Mat& m, int t) { return cdiv(m.np, t) * cdiv(m.m, t); };
   const int pairs = planes == 1 ? 1 : 3;
   p->gram = pick(p->mats, tri, [&](const Mat& m) { return m.np / 64 * pairs; });
   p->poly = pick(p->mats, tri, [&](const Mat& m) { return m.mp / 64 * pairs; });

@@ -50,18 +50,14 @@ __device__ __forceinline__ float common_scale(const Tokens& k) {
   return (k.grad && !k.grad_each ? k.grad[0] : 1.f) / k.stats[k.t];
 }
 
-// Token t's own factor of G; false: ignored.  A target outside the classes
-// makes it NaN.
-__device__ __forceinline__ bool token_scale(const Tokens& k, int t, int64_t y, float* s) {
-  if (y == k.ignore) return false;
-  if (y < 0 || y >= k.v) {
-    *s = __builtin_nanf("");
-    return true;
-  }
+// Token t's own factor of G: 0 where it is ignored, NaN where its target is
+// outside the classes.
+__device__ __forceinline__ float token_scale(const Tokens& k, int t, int64_t y) {
+  if (y == k.ignore) return 0.f;
+  if (y < 0 || y >= k.v) return __builtin_nanf("");
   float g = k.grad && k.grad_each ? k.grad[t] : 1.f;
   if (k.class_weight) g *= k.class_weight[y];
-  *s = g;
-  return true;
+  return g;
 }
 
 // ---------------------------------------------------------------------------
@@ -257,29 +253,33 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   const int lane = Tile::lane(), wave = Tile::wave();
   const int rows = a.w.rows, nt = a.k.t;
 
-  // This lane's columns: what the gradient needs of each token, fetched ahead
-  // of the product.
-  float scale[Tile::FN], lse[Tile::FN];
+  // this lane's columns: their targets, and for the gradient the statistics,
+  // fetched ahead of the product and used after it
+  int64_t target[Tile::FN];
+  float lse[Tile::FN], scale[Tile::FN];
   int hit[Tile::FN];   // the target's row, from this lane's first one on (-1: not in the wave's)
 #pragma unroll
   for (int j = 0; j < Tile::FN; ++j) {
-    const int t = col0 + Tile::col_of(j);
-    scale[j] = lse[j] = 0.f;
-    hit[j] = -1;
-    if (t < nt) {
-      const int64_t y = a.k.target[t];
-      const int64_t d = y - a.v0 - (row0 + Tile::row_of(0));
-      if (d >= 0 && d < Tile::TM && y - a.v0 < rows) hit[j] = static_cast<int>(d);
-      if constexpr (GRAD) {
-        if (token_scale(a.k, t, y, &scale[j])) lse[j] = a.k.stats[t];
-      }
-    }
+    const int t = min(col0 + Tile::col_of(j), nt - 1);
+    target[j] = a.k.target[t];
+    if constexpr (GRAD) lse[j] = a.k.stats[t];
   }
 
   f32x4 acc[Tile::FM][Tile::FN];
   Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, a.ksteps * a.pairs.n, lds, acc);
   Tile::reduce(lds, acc);
 
+#pragma unroll
+  for (int j = 0; j < Tile::FN; ++j) {
+    const int t = col0 + Tile::col_of(j);
+    scale[j] = 0.f;
+    hit[j] = -1;
+    if (t < nt) {
+      const int64_t c = target[j] - a.v0, d = c - (row0 + Tile::row_of(0));
+      if (d >= 0 && d < Tile::TM && c < rows) hit[j] = static_cast<int>(d);
+      if constexpr (GRAD) scale[j] = token_scale(a.k, t, target[j]);
+    }
+  }
   // the logits: bias added; classes past the end take no part
   if (a.bias) {
     const bool wide = a.bias_wide;
@@ -387,8 +387,8 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
     };
     Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
       rb += row0, cb += col0;
-#pragma unroll 2
-      for (int i = 0; i < Tile::PIECES; ++i) {
+#pragma unroll 4
+      for (int i = 0; i < view.pieces(); ++i) {
         int r, c;
         float v[8];
         view.col_piece(i, &r, &c);
@@ -569,8 +569,8 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
   const float scale = a.slab ? 1.f : common_scale(a.k);
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
     rb += row0, cb += col0;
-#pragma unroll 2
-    for (int i = 0; i < Tile::PIECES; ++i) {
+#pragma unroll 4
+    for (int i = 0; i < view.pieces(); ++i) {
       int r, c;
       float v[8];
       view.col_piece(i, &r, &c);
@@ -644,7 +644,7 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
   if (fwd) {
     p.logit = pick_tile(p.v, p.t, p.dp / 64 * p.pairs.n);
-    p.parts = static_cast<int>(cdiv(p.v, kTileEdge[p.logit]) * 2);
+    p.parts = static_cast<int>(cdiv(p.vp, kTileEdge[p.logit]) * kTileWM[p.logit]);
     p.part = take(p.parts * p.t * 8);
     p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
   }
@@ -656,7 +656,7 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     p.pieces = cdiv(p.v, p.piece);
     p.g = take(p.t * p.piece * e);
     p.gl = pick_tile(p.piece, p.t, p.dp / 64 * p.pairs.n);
-    p.db = take(cdiv(p.t, kTileEdge[p.gl]) * 4 * p.piece * 4);
+    p.db = take(cdiv(p.t, kTileEdge[p.gl]) * kTileWN[p.gl] * p.piece * 4);
     p.dx_turned = d.dx_sc != 1;
     const int64_t dm = p.dx_turned ? p.t : p.d, dn = p.dx_turned ? p.d : p.t;
     const SplitTile x = pick_split(dm, dn, p.piece / 64 * p.pairs.n), w = pick_split(p.d, p.piece, cdiv(p.t, 64) * p.pairs.n);
@@ -683,7 +683,7 @@ void stage(const StageArgs* a, int n, hipStream_t st) {
 
 template <bool GRAD, int P>
 void logits(int tile, LogitArgs& a, hipStream_t st) {
-  a.tm = static_cast<int32_t>(cdiv(a.w.rows, kTileEdge[tile]));
+  a.tm = static_cast<int32_t>(cdiv(pad64(a.w.rows), kTileEdge[tile]));   // (G's padding is written too)
   a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileEdge[tile]));
   with_tile<__bf16, false, false>(tile, [&](auto t) {
     using Tile = decltype(t);
@@ -807,7 +807,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     la.db_part = c.db ? f32(p.db) : nullptr;
     logits<true, P>(p.gl, la, st);
     la.loss = {};
-    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * (p.gl == kBig ? 4 : 2)), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
+    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * kTileWN[p.gl]), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
     const int32_t db_blocks = c.db ? static_cast<int32_t>(cdiv(nv, 64)) : 0;
     if (db_blocks && !c.dw) hipLaunchKernelGGL(class_sum_kernel, dim3(static_cast<uint32_t>(db_blocks)), dim3(1024), 0, st, db, tok);
     // a small slab of dw is joined by dx's product, which comes after it
