@@ -99,7 +99,7 @@ inline int pick_tile(int64_t m, int64_t n, int64_t steps) {
 struct SplitTile {
   int tile, splits;
 };
-inline SplitTile pick_split(int64_t m, int64_t n, int64_t steps) {
+inline SplitTile pick_split(int64_t m, int64_t n, int64_t steps, double* time = nullptr) {
   SplitTile best = {kSmall, 1};
   double least = 1e300;
   for (int k = 0; k < kTiles; ++k)
@@ -110,6 +110,7 @@ inline SplitTile pick_split(int64_t m, int64_t n, int64_t steps) {
       if (s > 1) t += 4. + s * static_cast<double>(m) * n * 8e-6 / 3.;
       if (t < least) least = t, best = {k, s};
     }
+  if (time) *time = least;
   return best;
 }
 

@@ -50,14 +50,10 @@ __device__ __forceinline__ float common_scale(const Tokens& k) {
   return (k.grad && !k.grad_each ? k.grad[0] : 1.f) / k.stats[k.t];
 }
 
-// Token t's own factor of G: 0 where it is ignored, NaN where its target is
-// outside the classes.
-__device__ __forceinline__ float token_scale(const Tokens& k, int t, int64_t y) {
-  if (y == k.ignore) return 0.f;
-  if (y < 0 || y >= k.v) return __builtin_nanf("");
-  float g = k.grad && k.grad_each ? k.grad[t] : 1.f;
-  if (k.class_weight) g *= k.class_weight[y];
-  return g;
+// Token t's own factor of G, given its class weight and its incoming gradient:
+// 0 where it is ignored, NaN where its target is outside the classes.
+__device__ __forceinline__ float token_scale(const Tokens& k, int64_t y, float weight, float grad) {
+  return y == k.ignore ? 0.f : y < 0 || y >= k.v ? __builtin_nanf("") : weight * grad;
 }
 
 // ---------------------------------------------------------------------------
@@ -167,6 +163,12 @@ struct LossArgs {
   int32_t n, mean;
   float *out, *divisor;  // (out null: each token has its loss)
 };
+__device__ __forceinline__ void put_loss(const LossArgs& l, double x, double w) {
+  // (a mean over no token: a loss of 0)
+  const double div = l.mean && !(w == 0.) ? w : 1.;
+  if (l.out) *l.out = static_cast<float>(x / div);
+  *l.divisor = static_cast<float>(div);
+}
 __device__ __forceinline__ void loss_sum(const LossArgs& l, double2* wave_sums) {
   double x = 0., w = 0.;
 #pragma unroll 4
@@ -179,10 +181,7 @@ __device__ __forceinline__ void loss_sum(const LossArgs& l, double2* wave_sums) 
   __syncthreads();
   if (threadIdx.x) return;
   for (unsigned i = 1; i < blockDim.x / 64; ++i) x += wave_sums[i].x, w += wave_sums[i].y;
-  // (a mean over no token: a loss of 0)
-  const double div = l.mean && !(w == 0.) ? w : 1.;
-  if (l.out) *l.out = static_cast<float>(x / div);
-  *l.divisor = static_cast<float>(div);
+  put_loss(l, x, w);
 }
 
 // db: 64 classes a workgroup, each wave taking every n-th part
@@ -215,7 +214,6 @@ struct LogitArgs {
   int32_t ksteps, tm, tn;
   int32_t v0;
   const float* bias;
-  int32_t bias_wide;       // bias + v0 is 16-byte aligned
   Tokens k;
   // statistics
   float2* part;            // [class part][token]: maximum, sum of exp(l - maximum)
@@ -269,34 +267,44 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, a.ksteps * a.pairs.n, lds, acc);
   Tile::reduce(lds, acc);
 
+  // (everything that has to be fetched first, without branches between)
+  f32x4 bias[Tile::FM];
+  if (a.bias) {
+    const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.bias) + a.v0, 0, rows * 4, 0x00020000);   // (0 past the end)
+#pragma unroll
+    for (int i = 0; i < Tile::FM; ++i)
+      bias[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (row0 + Tile::row_of(i)) * 4, 0, 0));
+  }
+  if constexpr (GRAD) {
+    float weight[Tile::FN], grad[Tile::FN];
+#pragma unroll
+    for (int j = 0; j < Tile::FN; ++j) weight[j] = grad[j] = 1.f;
+    if (a.k.class_weight) {
+#pragma unroll
+      for (int j = 0; j < Tile::FN; ++j) {
+        const int64_t y = target[j];
+        weight[j] = a.k.class_weight[y < 0 || y >= a.k.v ? 0 : y];
+      }
+    }
+    if (a.k.grad && a.k.grad_each) {
+#pragma unroll
+      for (int j = 0; j < Tile::FN; ++j) grad[j] = a.k.grad[min(col0 + Tile::col_of(j), nt - 1)];
+    }
+#pragma unroll
+    for (int j = 0; j < Tile::FN; ++j)
+      scale[j] = col0 + Tile::col_of(j) < nt ? token_scale(a.k, target[j], weight[j], grad[j]) : 0.f;
+  }
 #pragma unroll
   for (int j = 0; j < Tile::FN; ++j) {
-    const int t = col0 + Tile::col_of(j);
-    scale[j] = 0.f;
-    hit[j] = -1;
-    if (t < nt) {
-      const int64_t c = target[j] - a.v0, d = c - (row0 + Tile::row_of(0));
-      if (d >= 0 && d < Tile::TM && c < rows) hit[j] = static_cast<int>(d);
-      if constexpr (GRAD) scale[j] = token_scale(a.k, t, target[j]);
-    }
+    const int64_t c = target[j] - a.v0, d = c - (row0 + Tile::row_of(0));
+    hit[j] = d >= 0 && d < Tile::TM && c < rows && col0 + Tile::col_of(j) < nt ? static_cast<int>(d) : -1;
   }
   // the logits: bias added; classes past the end take no part
   if (a.bias) {
-    const bool wide = a.bias_wide;
 #pragma unroll
-    for (int i = 0; i < Tile::FM; ++i) {
-      const int r = row0 + Tile::row_of(i);
-      f32x4 b = {0.f, 0.f, 0.f, 0.f};
-      if (wide && r + 3 < rows) {
-        b = *reinterpret_cast<const f32x4*>(a.bias + a.v0 + r);
-      } else {
+    for (int i = 0; i < Tile::FM; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (r + e < rows) b[e] = a.bias[a.v0 + r + e];
-      }
-#pragma unroll
-      for (int j = 0; j < Tile::FN; ++j) acc[i][j] += b;
-    }
+      for (int j = 0; j < Tile::FN; ++j) acc[i][j] += bias[i];
   }
   if (row0 + Tile::BM > rows) {
 #pragma unroll
@@ -411,6 +419,7 @@ struct JoinArgs {
   float* lse;       // [token]
   float* loss;      // [token], or null
   double2* sums;    // [workgroup]: sums of the losses and of the weights, or null
+  LossArgs whole;   // one workgroup: the loss and its divisor right away (divisor null: not)
 };
 
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
@@ -448,12 +457,16 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
     a.lse[t] = lse;
     if (a.loss) a.loss[t] = loss;
   }
-  if (!a.sums) return;
+  if (!a.sums && !a.whole.divisor) return;
   // (N lanes of one wave)
   double x = loss, y = weight;
 #pragma unroll
   for (int d = N / 2; d; d >>= 1) x += __shfl_xor(x, d), y += __shfl_xor(y, d);
-  if (u == 0) a.sums[blockIdx.x] = make_double2(x, y);
+  if (u) return;
+  if (a.whole.divisor)
+    put_loss(a.whole, x, y);
+  else
+    a.sums[blockIdx.x] = make_double2(x, y);
 }
 
 __global__ __launch_bounds__(1024) void loss_kernel(LossArgs l) {
@@ -564,9 +577,9 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
   const int steps = a.ksteps * a.pairs.n;
   const int s0 = static_cast<int>(static_cast<int64_t>(steps) * split / a.splits);
   const int s1 = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
+  const float scale = a.slab ? 1.f : common_scale(a.k);
   f32x4 acc[Tile::FM][Tile::FN];
   Tile::run(a.a, a.b, a.pairs, row0, col0, a.ksteps, s0, s1, lds, acc);
-  const float scale = a.slab ? 1.f : common_scale(a.k);
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
     rb += row0, cb += col0;
 #pragma unroll 4
@@ -618,7 +631,40 @@ struct Plan {
   size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
 };
 
-constexpr int64_t kPieceBytes = int64_t(256) << 20;   // of G
+constexpr int64_t kPieceBytes = int64_t(512) << 20;   // of G
+
+// Modelled time of the gradient's products for nv classes.
+double piece_time(const Plan& p, int64_t nv, bool turned) {
+  const int64_t steps = p.dp / 64 * p.pairs.n;
+  const int k = pick_tile(nv, p.t, steps);
+  const double tiles = static_cast<double>(cdiv(nv, kTileEdge[k]) * cdiv(p.t, kTileEdge[k])), s = static_cast<double>(steps);
+  // (G's epilogue: about 10 us a round of large tiles)
+  double t = tile_time(k, tiles, s, s) + (k == kBig ? 10. * static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs)) : 0.);
+  double x;
+  pick_split(turned ? p.t : p.d, turned ? p.d : p.t, cdiv(nv, 64) * p.pairs.n, &x);
+  t += x;
+  pick_split(p.d, nv, cdiv(p.t, 64) * p.pairs.n, &x);
+  return t + x;
+}
+
+// Classes a piece: all, if G fits the workspace; else the size, among a few
+// that fit, whose tiles waste the least of their last rounds.
+int64_t pick_piece(const Plan& p, bool turned) {
+  const int64_t most = std::max<int64_t>(256, kPieceBytes / (p.t * 2 * p.planes) / 256 * 256);
+  if (p.vp <= most) return p.vp;
+  int64_t best = most;
+  double least = 1e300;
+  auto look = [&](int64_t piece) {
+    if (piece < 256 || piece > most) return;
+    const int64_t n = p.v / piece, rest = p.v - n * piece;
+    const double t = n * piece_time(p, piece, turned) + (rest ? piece_time(p, rest, turned) : 0.);
+    if (t < least) least = t, best = piece;
+  };
+  const int64_t few = cdiv(p.v, most);
+  for (int64_t n = few; n < few + 6; ++n) look(cdiv(cdiv(p.v, n), 256) * 256);
+  for (int64_t n = most / 2048 * 2048, i = 0; n > 0 && i < 12; n -= 2048, ++i) look(n);
+  return best;
+}
 
 Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligned, bool w_aligned) {
   Plan p;
@@ -649,10 +695,7 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
   }
   if (bwd) {
-    p.piece = std::max<int64_t>(256, kPieceBytes / (p.t * static_cast<int64_t>(e)) / 256 * 256);
-    if (p.piece > p.vp) p.piece = p.vp;
-    p.pieces = cdiv(p.v, p.piece);
-    p.piece = std::min(p.vp, cdiv(cdiv(p.v, p.pieces), 256) * 256);   // pieces of about one size
+    p.piece = pick_piece(p, d.dx_sc != 1);
     p.pieces = cdiv(p.v, p.piece);
     p.g = take(p.t * p.piece * e);
     p.gl = pick_tile(p.piece, p.t, p.dp / 64 * p.pairs.n);
@@ -761,7 +804,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
   LogitArgs la = {};
   la.x = x, la.pairs = p.pairs, la.ksteps = static_cast<int32_t>(p.dp / 64), la.k = tok;
   if (p.fwd) {
-    la.w = w, la.v0 = 0, la.bias = c.bias, la.bias_wide = aligned16(c.bias);
+    la.w = w, la.v0 = 0, la.bias = c.bias;
     la.part = reinterpret_cast<float2*>(c.ws + p.part), la.target_logit = f32(p.tl);
     logits<false, P>(p.logit, la, st);
     const bool each = d.reduction == PP_NONE;
@@ -769,17 +812,19 @@ pp_status enqueue(const Plan& p, const Call& c) {
     const int n = p.parts > 8 ? 16 : 64;
     const uint32_t grid = static_cast<uint32_t>(cdiv(p.t, n));
     double2* sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
-    const JoinArgs ja = {tok, la.part, la.target_logit, p.parts, c.stats, each ? c.loss : nullptr, sums};
+    // The loss and its divisor: by the join, if that is one workgroup; by the
+    // gradient's first product, if there is one (what the divisor scales comes
+    // after it).
+    const LossArgs loss = {sums, each ? 0 : static_cast<int32_t>(grid), d.reduction == PP_MEAN, each ? nullptr : c.loss, c.stats + p.t};
+    const bool whole = grid == 1;
+    const JoinArgs ja = {tok, la.part, la.target_logit, p.parts, c.stats, each ? c.loss : nullptr, sums, whole ? loss : LossArgs{}};
     if (n == 16)
       hipLaunchKernelGGL((join_kernel<16>), dim3(grid), dim3(256), 0, st, ja);
     else
       hipLaunchKernelGGL((join_kernel<4>), dim3(grid), dim3(256), 0, st, ja);
-    // (what the loss's divisor scales comes after the gradient's first
-    // product, which takes this along)
-    const LossArgs loss = {sums, each ? 0 : static_cast<int32_t>(grid), d.reduction == PP_MEAN, each ? nullptr : c.loss, c.stats + p.t};
-    if (p.bwd)
+    if (p.bwd && !whole)
       la.loss = loss;
-    else
+    else if (!whole)
       hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, loss);
     if ((s = launched()) != PP_OK) return s;
   }
@@ -801,8 +846,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
   ProductArgs xa = {}, wa = {};
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t v0 = k * p.piece, nv = std::min(p.piece, p.v - v0), nvp = pad64(nv);
-    la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias,
-    la.bias_wide = aligned16(c.bias);
+    la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
     la.g = bf(p.g), la.v_pad = static_cast<int32_t>(nvp), la.g_plane = p.t * nvp;
     la.db_part = c.db ? f32(p.db) : nullptr;
     logits<true, P>(p.gl, la, st);
