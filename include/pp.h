@@ -524,7 +524,7 @@ typedef struct {
 /*
  * pp_xent_workspace -- device bytes a call needs (parts: PP_XENT_FWD for
  * pp_xent_fwd, PP_XENT_BWD for pp_xent_bwd, both for pp_xent_step), which do
- * not grow with v times the tokens beyond about 0.3 GB.  Host-only.
+ * not grow with v times the tokens beyond about 0.6 GB.  Host-only.
  *
  * pp_xent_fwd -- the loss, and the statistics pp_xent_bwd needs.
  *   x, w          device [n][d][hw] (by strides) and [v][d] (rows w_ld apart)
@@ -547,8 +547,8 @@ typedef struct {
  * 24 bits (fp32) for the products with w and x, and sums in fp32.
  * n hw = 0 is a loss of 0 and zero gradients.
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, reduction, dtype,
- * negative strides), PP_EUNSUPPORTED (d, v or the tokens 2^22 - 64 or more),
- * PP_ESIZE (workspace too small), PP_EHIP.
+ * negative strides), PP_EUNSUPPORTED (d, v or the tokens 2^22 - 64 or more, x or
+ * w of 2^35 elements or more), PP_ESIZE (workspace too small), PP_EHIP.
  */
 pp_status pp_xent_workspace(const pp_xent_desc* desc, int32_t parts, size_t* bytes);
 pp_status pp_xent_fwd(const pp_xent_desc* desc, const void* x, const void* w, const float* bias,

@@ -749,7 +749,7 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     for (int k = 0; k < kStages; ++k) {
       p->start[k].push_back(static_cast<int32_t>(p->blocks[k]));
       p->blocks[k] += n[k];
-      if (p->blocks[k] > (1 << 30)) return fail(PP_EUNSUPPORTED, "too many matrices, or too large, for one call");
+      if (p->blocks[k] > (1 << 22)) return fail(PP_EUNSUPPORTED, "too many matrices, or too large, for one call");
     }
     const size_t xn = static_cast<size_t>(m.m) * m.np * 2, an = static_cast<size_t>(m.m) * m.mp * 2;
     m.x[0] = reinterpret_cast<half_t*>(ws + take(2 * xn));

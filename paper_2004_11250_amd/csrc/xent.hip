@@ -415,7 +415,8 @@ struct JoinArgs {
   Tokens k;
   const float2* part;
   const float* target_logit;
-  int32_t parts;
+  int32_t first, parts;   // the parts [first, parts)
+  float2* carry;    // [token]: the joined part goes there, and nothing else is done (or null)
   float* lse;       // [token]
   float* loss;      // [token], or null
   double2* sums;    // [workgroup]: sums of the losses and of the weights, or null
@@ -435,7 +436,7 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
   const int u = threadIdx.x % N, w = threadIdx.x / N, t = blockIdx.x * N + u;
   float2 s = make_float2(-INFINITY, 0.f);
   if (t < a.k.t)
-    for (int p = w; p < a.parts; p += W) s = join(s, a.part[static_cast<int64_t>(p) * a.k.t + t]);
+    for (int p = a.first + w; p < a.parts; p += W) s = join(s, a.part[static_cast<int64_t>(p) * a.k.t + t]);
   got[w][u] = s;
   __syncthreads();
   if (w) return;
@@ -443,6 +444,10 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
   if (t < a.k.t) {
 #pragma unroll
     for (int p = 1; p < W; ++p) s = join(s, got[p][u]);
+    if (a.carry) a.carry[t] = s;
+  }
+  if (a.carry) return;
+  if (t < a.k.t) {
     const int64_t y = a.k.target[t];
     float lse = 0.f;
     if (y != a.k.ignore) {
@@ -621,7 +626,8 @@ struct Plan {
   int planes = 1;
   PlanePairs pairs = kPairs1;
   bool w_direct = false, x_direct = false, fwd = false, bwd = false;
-  int logit = kSmall, parts = 0;
+  int logit = kSmall, parts = 0;      // of a forward piece
+  int64_t fwd_piece = 0;              // classes of one
   int64_t piece = 0, pieces = 0;      // classes a piece
   int gl = kSmall, dxt = kSmall, dwt = kSmall, dx_splits = 1, dw_splits = 1;
   bool dx_slab = false, dw_slab = false;
@@ -631,6 +637,7 @@ struct Plan {
   size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
 };
 
+constexpr int64_t kPartBytes = int64_t(64) << 20;     // of the forward pass's statistics
 constexpr int64_t kPieceBytes = int64_t(512) << 20;   // of G
 
 // Modelled time of the gradient's products for nv classes.
@@ -690,8 +697,10 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
   if (fwd) {
     p.logit = pick_tile(p.v, p.t, p.dp / 64 * p.pairs.n);
-    p.parts = static_cast<int>(cdiv(p.vp, kTileEdge[p.logit]) * kTileWM[p.logit]);
-    p.part = take(p.parts * p.t * 8);
+    const int64_t edge = kTileEdge[p.logit], wm = kTileWM[p.logit];
+    p.fwd_piece = std::min(p.vp, std::max<int64_t>(256, kPartBytes / (p.t * 8) / wm * edge / 256 * 256));
+    p.parts = static_cast<int>(cdiv(p.fwd_piece, edge) * wm);
+    p.part = take((p.parts + 1) * p.t * 8);   // (and what the pieces before left)
     p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
   }
   if (bwd) {
@@ -801,12 +810,17 @@ pp_status enqueue(const Plan& p, const Call& c) {
   if (copies) stage<S, P>(staged, copies, st);
   if ((s = launched()) != PP_OK) return s;
 
+  // an operand's rows from r0 on
+  auto from = [](GemmOperand o, int64_t r0) {
+    for (auto& q : o.plane) q = static_cast<const uint8_t*>(q) + r0 * o.ld * 2;
+    return o;
+  };
   LogitArgs la = {};
   la.x = x, la.pairs = p.pairs, la.ksteps = static_cast<int32_t>(p.dp / 64), la.k = tok;
   if (p.fwd) {
-    la.w = w, la.v0 = 0, la.bias = c.bias;
-    la.part = reinterpret_cast<float2*>(c.ws + p.part), la.target_logit = f32(p.tl);
-    logits<false, P>(p.logit, la, st);
+    la.bias = c.bias, la.target_logit = f32(p.tl);
+    float2* carry = reinterpret_cast<float2*>(c.ws + p.part);
+    la.part = carry + p.t;
     const bool each = d.reduction == PP_NONE;
     // (few parts: more tokens a workgroup)
     const int n = p.parts > 8 ? 16 : 64;
@@ -817,11 +831,19 @@ pp_status enqueue(const Plan& p, const Call& c) {
     // after it).
     const LossArgs loss = {sums, each ? 0 : static_cast<int32_t>(grid), d.reduction == PP_MEAN, each ? nullptr : c.loss, c.stats + p.t};
     const bool whole = grid == 1;
-    const JoinArgs ja = {tok, la.part, la.target_logit, p.parts, c.stats, each ? c.loss : nullptr, sums, whole ? loss : LossArgs{}};
-    if (n == 16)
-      hipLaunchKernelGGL((join_kernel<16>), dim3(grid), dim3(256), 0, st, ja);
-    else
-      hipLaunchKernelGGL((join_kernel<4>), dim3(grid), dim3(256), 0, st, ja);
+    for (int64_t v0 = 0; v0 < p.v; v0 += p.fwd_piece) {
+      const int64_t nv = std::min(p.fwd_piece, p.v - v0);
+      const bool last = v0 + nv == p.v;
+      la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0);
+      logits<false, P>(p.logit, la, st);
+      const int32_t parts = static_cast<int32_t>(cdiv(pad64(nv), kTileEdge[p.logit]) * kTileWM[p.logit]);
+      const JoinArgs ja = {tok, carry, la.target_logit, v0 ? 0 : 1, parts + 1, last ? nullptr : carry, c.stats, each ? c.loss : nullptr,
+                           sums, whole ? loss : LossArgs{}};
+      if (n == 16)
+        hipLaunchKernelGGL((join_kernel<16>), dim3(grid), dim3(256), 0, st, ja);
+      else
+        hipLaunchKernelGGL((join_kernel<4>), dim3(grid), dim3(256), 0, st, ja);
+    }
     if (p.bwd && !whole)
       la.loss = loss;
     else if (!whole)
@@ -833,11 +855,6 @@ pp_status enqueue(const Plan& p, const Call& c) {
   const int64_t dn = p.dx_turned ? p.d : p.t;
   float* dx_slab = f32(p.slab);
   float* dw_slab = dx_slab + (p.dx_slab ? p.dx_splits * p.dx_ld * dn : 0);
-  // an operand's rows from r0 on
-  auto from = [](GemmOperand o, int64_t r0) {
-    for (auto& q : o.plane) q = static_cast<const uint8_t*>(q) + r0 * o.ld * 2;
-    return o;
-  };
   // the same array as [k][rows]
   auto by_k = [](GemmOperand o, int64_t rows, int64_t k) {
     o.rows = static_cast<int32_t>(rows), o.k = static_cast<int32_t>(k);
@@ -902,6 +919,8 @@ pp_status check_desc(const pp_xent_desc* d) {
   if (d->n < 0 || d->hw < 0 || d->d < 1 || d->v < 1) return fail(PP_EINVAL, "n, hw must be >= 0, d and v >= 1");
   if (d->d > kMaxLd - 64 || d->v > kMaxLd - 64 || d->n > kMaxLd || d->hw > kMaxLd || d->n * d->hw > kMaxLd - 64)
     return fail(PP_EUNSUPPORTED, "d, v and the tokens must be below 2^22 - 64 each");
+  if (d->n * d->hw * pad64(d->d) > (int64_t(1) << 35) || d->v * pad64(d->d) > (int64_t(1) << 35))
+    return fail(PP_EUNSUPPORTED, "x and w must have fewer than 2^35 elements each");
   if (d->w_ld < d->d) return fail(PP_EINVAL, "w_ld smaller than d");
   if (d->x_sn < 0 || d->x_sc < 0 || d->x_sp < 0 || d->dx_sn < 0 || d->dx_sc < 0 || d->dx_sp < 0)
     return fail(PP_EINVAL, "negative stride");

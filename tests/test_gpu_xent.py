@@ -162,6 +162,20 @@ def test_several_pieces(n, d, hw, v, layout):
     check(5, n, d, hw, v, "bf16", layout=layout, ignored=0.1)
 
 
+def test_statistics_in_several_pieces():
+    # more classes and tokens than the forward pass keeps statistics of at once
+    x, w, t, b, cw, _ = make(18, 16400, 64, 1, 70000, "bf16", layout="tokens", ignored=0.01)
+    # (only the loss: the gradients' bounds would take tens of GB)
+    l = x.double() @ w.double().t() + b.double()
+    lim = (64 + 64) * U * (x.double().abs() @ w.double().abs().t() + b.double().abs()).amax(1)
+    lse = torch.logsumexp(l, 1)
+    keep = t != -100
+    each = torch.where(keep, lse - l.gather(1, t.clamp(min=0)[:, None])[:, 0], torch.zeros_like(lse))
+    loss, stats = pp.linear_xent_fwd(x, w, t, bias=b, reduction="none")
+    near(loss, each, 2 * lim + 2e-6 + 4 * U * (each.abs() + lse.abs()), "loss")
+    near(stats[:-1], torch.where(keep, lse, torch.zeros_like(lse)), lim + 2e-6 + 2 * U * lse.abs(), "lse")
+
+
 def test_long_sums_are_split():
     # many tokens, few classes and features; few tokens, many classes
     check(6, 4, 32, 5000, 40, "bf16", weighted=True)
