@@ -575,7 +575,8 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  * result.  The sum of squares is taken in 64 bits.  U = 0 gives 0; a NaN or an
  * infinity in U makes its result NaN.
  * Coefficients: those that keep singular values of 0..1 within -2..2 on every
- * step and |b s^2| and |b s^2 + c s^4| at most 48, e.g. {3.4445, -4.7750,
+ * step (every step for all values up to the largest that the one before can
+ * give) and |b s^2| and |b s^2 + c s^4| at most 48, e.g. {3.4445, -4.7750,
  * 2.0315}, {1.875, -1.25, 0.375}, {1.5, -0.5, 0}; others PP_EUNSUPPORTED.
  *
  * pp_ortho -- all matrices of a list in one call (each stage of the iteration

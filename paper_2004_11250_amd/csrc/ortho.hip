@@ -831,14 +831,28 @@ pp_status check_step(const Step& s) {
   for (float v : {s.a, s.b, s.c, s.eps, s.lr, s.momentum, s.decay})
     if (!std::isfinite(v)) return fail(PP_EINVAL, "parameters must be finite");
   if (s.eps < 0) return fail(PP_EINVAL, "eps must be >= 0");
-  for (int i = 0; i <= 2048; ++i) {
-    double x = i / 2048.;
-    for (int k = 0; k < s.steps; ++k) {
-      const double g = x * x, b = s.b * g + s.c * g * g;
-      if (std::fabs(b) > 48. || std::fabs(s.b * g) > 48.) return fail(PP_EUNSUPPORTED, "coefficients too large");
-      x = s.a * x + b * x;
-      if (std::fabs(x) > 2.) return fail(PP_EUNSUPPORTED, "the coefficients let singular values leave 0..2");
+  // Over t = x^2 in 0..r^2, r the largest |x| the steps before can give:
+  // f(x) = x (a + b t + c t^2) is largest at an end or where a + 3 b t + 5 c t^2 = 0,
+  // g(t) = b t + c t^2 at an end or at -b / 2c.
+  const double a = s.a, b = s.b, c = s.c;
+  double r = 1.;
+  for (int k = 0; k < s.steps; ++k) {
+    const double end = r * r;
+    double most = 0., g = 0.;
+    auto f = [&](double t) { if (t >= 0. && t <= end) most = std::max(most, std::sqrt(t) * std::fabs(a + b * t + c * t * t)); };
+    auto h = [&](double t) { if (t >= 0. && t <= end) g = std::max(g, std::max(std::fabs(b * t + c * t * t), std::fabs(b * t))); };
+    f(end), h(end);
+    if (c != 0.) {
+      const double d = 9. * b * b - 20. * a * c;
+      if (d >= 0.) f((-3. * b + std::sqrt(d)) / (10. * c)), f((-3. * b - std::sqrt(d)) / (10. * c));
+      h(-b / (2. * c));
+    } else if (b != 0.) {
+      f(-a / (3. * b));
     }
+    if (!(most <= 2.)) return fail(PP_EUNSUPPORTED, "the coefficients let singular values leave 0..2");
+    if (!(g <= 48.)) return fail(PP_EUNSUPPORTED, "coefficients too large");
+    if (most <= r) break;   // (the range does not grow any more)
+    r = most;
   }
   return PP_OK;
 }

@@ -629,8 +629,12 @@ struct Plan {
   int logit = kSmall, parts = 0;      // of a forward piece
   int64_t fwd_piece = 0;              // classes of one
   int64_t piece = 0, pieces = 0;      // classes a piece
-  int gl = kSmall, dxt = kSmall, dwt = kSmall, dx_splits = 1, dw_splits = 1;
-  bool dx_slab = false, dw_slab = false;
+  struct Piece {
+    int logit = kSmall, dx = kSmall;  // tiles
+    SplitTile dw = {kSmall, 1};
+  } of[2];                            // the pieces, and the last one, which may be smaller
+  int dx_splits = 1;
+  bool dx_slab = false;
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
   // workspace offsets
@@ -707,19 +711,25 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     p.piece = pick_piece(p, d.dx_sc != 1);
     p.pieces = cdiv(p.v, p.piece);
     p.g = take(p.t * p.piece * e);
-    p.gl = pick_tile(p.piece, p.t, p.dp / 64 * p.pairs.n);
-    p.db = take(cdiv(p.t, kTileEdge[p.gl]) * kTileWN[p.gl] * p.piece * 4);
     p.dx_turned = d.dx_sc != 1;
     const int64_t dm = p.dx_turned ? p.t : p.d, dn = p.dx_turned ? p.d : p.t;
-    const SplitTile x = pick_split(dm, dn, p.piece / 64 * p.pairs.n), w = pick_split(p.d, p.piece, cdiv(p.t, 64) * p.pairs.n);
-    p.dxt = x.tile, p.dx_splits = x.splits;
-    p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
     p.dx_ld = cdiv(dm, 4) * 4;
-    p.dwt = w.tile, p.dw_splits = w.splits;
-    p.dw_slab = p.dw_splits > 1;
     p.dw_ld = cdiv(p.d, 4) * 4;
-    // dx's slab outlives a piece, dw's does not
-    p.slab = take((p.dx_slab ? p.dx_splits * p.dx_ld * dn * 4 : 0) + 256 + (p.dw_slab ? p.dw_splits * p.dw_ld * p.piece * 4 : 0));
+    int64_t db = 0, dw_slab = 0;
+    for (int i = 0; i < 2; ++i) {
+      const int64_t nv = i ? p.v - (p.pieces - 1) * p.piece : std::min(p.piece, p.v);
+      Plan::Piece& q = p.of[i];
+      q.logit = pick_tile(nv, p.t, p.dp / 64 * p.pairs.n);
+      db = std::max(db, cdiv(p.t, kTileEdge[q.logit]) * kTileWN[q.logit] * nv * 4);
+      const SplitTile x = pick_split(dm, dn, cdiv(nv, 64) * p.pairs.n);
+      q.dx = x.tile;
+      if (i == 0) p.dx_splits = x.splits;   // (dx's partial sums are kept over the pieces)
+      q.dw = pick_split(p.d, nv, cdiv(p.t, 64) * p.pairs.n);
+      if (q.dw.splits > 1) dw_slab = std::max(dw_slab, q.dw.splits * p.dw_ld * nv * 4);
+    }
+    p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
+    p.db = take(db);
+    p.slab = take((p.dx_slab ? p.dx_splits * p.dx_ld * dn * 4 : 0) + dw_slab);
   }
   p.total = std::max<size_t>(at, 256);
   return p;
@@ -854,7 +864,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
 
   const int64_t dn = p.dx_turned ? p.d : p.t;
   float* dx_slab = f32(p.slab);
-  float* dw_slab = dx_slab + (p.dx_slab ? p.dx_splits * p.dx_ld * dn : 0);
+  float* dw_slab = dx_slab + (p.dx_slab ? p.dx_splits * p.dx_ld * dn : 0);   // (of one piece at a time)
   // the same array as [k][rows]
   auto by_k = [](GemmOperand o, int64_t rows, int64_t k) {
     o.rows = static_cast<int32_t>(rows), o.k = static_cast<int32_t>(k);
@@ -863,12 +873,13 @@ pp_status enqueue(const Plan& p, const Call& c) {
   ProductArgs xa = {}, wa = {};
   for (int64_t k = 0; k < p.pieces; ++k) {
     const int64_t v0 = k * p.piece, nv = std::min(p.piece, p.v - v0), nvp = pad64(nv);
+    const Plan::Piece& q = p.of[k + 1 == p.pieces];
     la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
     la.g = bf(p.g), la.v_pad = static_cast<int32_t>(nvp), la.g_plane = p.t * nvp;
     la.db_part = c.db ? f32(p.db) : nullptr;
-    logits<true, P>(p.gl, la, st);
+    logits<true, P>(q.logit, la, st);
     la.loss = {};
-    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * kTileWN[p.gl]), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
+    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * kTileWN[q.logit]), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
     const int32_t db_blocks = c.db ? static_cast<int32_t>(cdiv(nv, 64)) : 0;
     if (db_blocks && !c.dw) hipLaunchKernelGGL(class_sum_kernel, dim3(static_cast<uint32_t>(db_blocks)), dim3(1024), 0, st, db, tok);
     // a small slab of dw is joined by dx's product, which comes after it
@@ -878,13 +889,13 @@ pp_status enqueue(const Plan& p, const Call& c) {
       wa = {};
       wa.a = by_k(x, p.dp, p.t), wa.b = by_k(g, nvp, p.t);
       wa.m = static_cast<int32_t>(p.d), wa.n = static_cast<int32_t>(nv);
-      wa.k = tok, wa.pairs = p.pairs, wa.ksteps = static_cast<int32_t>(cdiv(p.t, 64)), wa.splits = p.dw_splits;
+      wa.k = tok, wa.pairs = p.pairs, wa.ksteps = static_cast<int32_t>(cdiv(p.t, 64)), wa.splits = q.dw.splits;
       wa.map = {static_cast<S*>(c.dw) + v0 * p.d, 1, 0, p.d, 0, 1, 1, p.d % 4 == 0 && reinterpret_cast<uintptr_t>(c.dw) % 16 == 0};
-      wa.slab = p.dw_slab ? dw_slab : nullptr, wa.slab_ld = p.dw_ld;
+      wa.slab = wa.splits > 1 ? dw_slab : nullptr, wa.slab_ld = p.dw_ld;
       wa.db = db, wa.db_blocks = db_blocks;
-      product<S, true, true>(p.dwt, wa, st);
-      riding = p.dw_slab && c.dx && p.dw_splits * p.dw_ld * nv <= (4 << 20);
-      if (p.dw_slab && !riding) launch_slab<S>(slab_of(wa), tok, st);
+      product<S, true, true>(q.dw.tile, wa, st);
+      riding = wa.slab && c.dx && wa.splits * p.dw_ld * nv <= (4 << 20);
+      if (wa.slab && !riding) launch_slab<S>(slab_of(wa), tok, st);
     }
     if (c.dx) {   // over classes
       xa = {};
@@ -898,12 +909,12 @@ pp_status enqueue(const Plan& p, const Call& c) {
         xa.a = g, xa.b = wp, xa.m = static_cast<int32_t>(p.t), xa.n = static_cast<int32_t>(p.d);
         xa.map = {c.dx, d.dx_sn, d.dx_sp, d.dx_sc, 0, static_cast<int32_t>(d.hw), 1,
                   aligned && d.dx_sp == 1 && d.hw % 4 == 0 && d.dx_sn % 4 == 0 && d.dx_sc % 4 == 0};
-        product<S, false, true>(p.dxt, xa, st);
+        product<S, false, true>(q.dx, xa, st);
       } else {             // d x tokens
         xa.a = wp, xa.b = g, xa.m = static_cast<int32_t>(p.d), xa.n = static_cast<int32_t>(p.t);
         xa.map = {c.dx, 1, 0, d.dx_sn, d.dx_sp, 1, static_cast<int32_t>(d.hw),
                   aligned && p.d % 4 == 0 && d.dx_sn % 4 == 0 && (d.hw == 1 || d.dx_sp % 4 == 0)};
-        product<S, true, false>(p.dxt, xa, st);
+        product<S, true, false>(q.dx, xa, st);
       }
     }
     if ((s = launched()) != PP_OK) return s;

@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 
 import numpy as np
 
@@ -147,11 +148,17 @@ def _xent_grad_arg(grad, target, reduction):
         raise ValueError(f"grad must be contiguous float32 of shape {want} on the targets' device")
 
 
-def _xent_workspace(desc, parts, device):
-    torch = _torch()
+@functools.lru_cache(maxsize=256)
+def _xent_bytes(desc, parts):
+    """pp_xent_workspace of a description (as bytes): a function of it alone."""
     nb = ctypes.c_size_t(0)
-    _check(load_library().pp_xent_workspace(ctypes.byref(desc), parts, ctypes.byref(nb)), "pp_xent_workspace")
-    return torch.empty(max(nb.value, 256), dtype=torch.uint8, device=device)
+    _check(load_library().pp_xent_workspace(ctypes.byref(XentDesc.from_buffer_copy(desc)), parts, ctypes.byref(nb)),
+           "pp_xent_workspace")
+    return max(nb.value, 256)
+
+
+def _xent_workspace(desc, parts, device):
+    return _torch().empty(_xent_bytes(bytes(desc), parts), dtype=_torch().uint8, device=device)
 
 
 def linear_xent_fwd(x, w, target, bias=None, class_weight=None, ignore_index=-100, reduction="mean", stream=None):
