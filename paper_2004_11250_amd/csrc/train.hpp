@@ -39,19 +39,19 @@ inline GemmOperand operand(const void* base, int64_t plane_elems, int64_t ld, in
 //   128 x 128, two workgroups a CU                       0.52 / 0.58     3.5
 //   64 x 64, four steps in flight, two a CU              0.19 / 0.27     2.5
 //   64 x 64, two groups of waves share the steps         0.23 / 0.19     4
-//   32 x 32, eight waves share the steps, each one's own 0.13 / 0.1      3.2
+//   32 x 32, four waves share the steps, two a CU        0.1 / 0.12      2.8
 // The large tile wins wherever it fills the card (1310 TFLOP/s at 8192^3; the
 // others 1040, 720, 630), the small ones where it would leave CUs without work:
-// 4096^3 takes 104, 141, 218 and 267 us, 2048^3 43, 27, 28, 35 and 86,
-// 1000 x 3008 x 1000 -, 35, 16, 14 and 30, 512 x 4608 x 512 80, 42, 20, 17 and 10,
-// 256 x 960 x 256 -, 13, 6.5, 6.1 and 4.3.  Operands stored by rows of k cost 5 to
+// 4096^3 takes 104, 141, 218 and 267 us, 2048^3 43, 27, 28, 35 and 58,
+// 1000 x 3008 x 1000 -, 35, 16, 14 and 21, 512 x 4608 x 512 80, 42, 20, 17 and 11,
+// 256 x 960 x 256 -, 13, 6.5, 6.1 and 4.5.  Operands stored by rows of k cost 5 to
 // 10 % each.
 enum { kBig = 0, kMid = 1, kSmall = 2, kDeep = 3, kNarrow = 4, kTiles = 5 };
 template <class T, bool AR, bool BR> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, 1, true, AR, BR>;
 template <class T, bool AR, bool BR> using MidTile = GemmTile<T, 128, 128, 2, 2, 2, 1, false, AR, BR>;
 template <class T, bool AR, bool BR> using SmallTile = GemmTile<T, 64, 64, 2, 2, 4, 1, false, AR, BR>;
 template <class T, bool AR, bool BR> using DeepTile = GemmTile<T, 64, 64, 2, 2, 4, 2, false, AR, BR>;
-template <class T, bool AR, bool BR> using NarrowTile = GemmTile<T, 32, 32, 1, 1, 2, 8, false, AR, BR>;
+template <class T, bool AR, bool BR> using NarrowTile = GemmTile<T, 32, 32, 1, 1, 2, 4, false, AR, BR>;
 constexpr int kTileEdge[kTiles] = {256, 128, 64, 64, 32};
 constexpr int kTileWM[kTiles] = {2, 2, 2, 2, 1}, kTileWN[kTiles] = {4, 2, 2, 2, 1};   // waves' parts of a tile
 constexpr int kCUs = 256;
@@ -74,12 +74,12 @@ void with_tile(int k, F&& f) {
 // Modelled time in us of `tiles` tiles of `steps` steps on average, `most` at
 // most.
 inline double tile_time(int tile, double tiles, double steps, double most) {
-  constexpr double full[kTiles] = {1.6, 0.52, 0.19, 0.23, 0.13}, alone[kTiles] = {1.15, 0.58, 0.27, 0.19, 0.1},
-                   ends[kTiles] = {6., 3.5, 2.5, 4., 3.2};
+  constexpr double full[kTiles] = {1.6, 0.52, 0.19, 0.23, 0.1}, alone[kTiles] = {1.15, 0.58, 0.27, 0.19, 0.12},
+                   ends[kTiles] = {6., 3.5, 2.5, 4., 2.8};
   const double n = static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs));
   // (a card in part idle clocks higher and shares its caches among fewer)
   const double step = alone[tile] + (std::max(full[tile], alone[tile]) - alone[tile]) * std::min(1., tiles / kCUs);
-  const bool single = tile == kBig || tile >= kDeep;   // one workgroup a CU
+  const bool single = tile == kBig || tile == kDeep;   // one workgroup a CU
   return std::max(most * step, n > 1 ? n * steps * full[tile] : 0.) + ends[tile] * (single ? n : 0.5 + 0.5 * n);
 }
 
