@@ -90,12 +90,14 @@ __device__ __forceinline__ void bf16_planes(float x, __bf16 (&p)[P]) {
 template <class S, int P>
 __global__ __launch_bounds__(256) void stage_kernel(StageArgs one, StageArgs two, int32_t first) {
   __shared__ float tile[64][65];
+  __shared__ int32_t ignored[64];
   const bool second = static_cast<int>(blockIdx.x) >= first;
   const StageArgs& a = second ? two : one;
   const int id = second ? blockIdx.x - first : blockIdx.x;
   const int tc = a.cols_pad / 64;
   const int r0 = id / tc * 64, c0 = id % tc * 64, tid = threadIdx.x;
   const S* src = static_cast<const S*>(a.src);
+  if (tid < 64) ignored[tid] = a.target && r0 + tid < a.rows && a.target[r0 + tid] == a.ignore;
   // a piece of eight values along the axis that is contiguous in memory
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -122,13 +124,6 @@ __global__ __launch_bounds__(256) void stage_kernel(StageArgs one, StageArgs two
           }
         }
       }
-      if (a.target) {   // ignored tokens
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int t = r + (a.along_cols ? 0 : e);
-          if (t < a.rows && a.target[t] == a.ignore) x[e] = 0.f;
-        }
-      }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -143,11 +138,12 @@ __global__ __launch_bounds__(256) void stage_kernel(StageArgs one, StageArgs two
   for (int i = 0; i < 2; ++i) {
     const int u = (tid >> 3) + 32 * i, w = (tid & 7) * 8;
     if (r0 + u >= a.rows) continue;
+    const bool off = ignored[u];
     bf16x8 o[P];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       __bf16 p[P];
-      bf16_planes<P>(tile[u][w + e], p);
+      bf16_planes<P>(off ? 0.f : tile[u][w + e], p);
 #pragma unroll
       for (int q = 0; q < P; ++q) o[q][e] = p[q];
     }
@@ -339,11 +335,13 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
       s += __shfl_xor(s, 32);
       if (t < nt && lane < 16) a.part[static_cast<int64_t>(ti * Tile::WM + wave / Tile::WN) * nt + t] = make_float2(m, s);
       if (__ballot(hit[j] >= 0)) {   // (few tiles have a target's class)
+        float l = 0.f;
 #pragma unroll
         for (int i = 0; i < Tile::FM; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (hit[j] == 16 * i + e) a.target_logit[t] = acc[i][j][e];
+          for (int e = 0; e < 4; ++e) l = hit[j] == 16 * i + e ? acc[i][j][e] : l;
+        // (a lane has the rows 16 i + 4 (lane / 16) + 0..3: of the others' it finds none)
+        if (hit[j] >= 0 && (hit[j] & 15) < 4) a.target_logit[t] = l;
       }
     }
   } else {
@@ -359,11 +357,11 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
           acc[i][j][e] = on ? p : 0.f;
         }
       if (__ballot(hit[j] >= 0)) {
+        const float less = on ? scale[j] : 0.f;
 #pragma unroll
         for (int i = 0; i < Tile::FM; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (on && hit[j] == 16 * i + e) acc[i][j][e] -= scale[j];
+          for (int e = 0; e < 4; ++e) acc[i][j][e] -= hit[j] == 16 * i + e ? less : 0.f;
       }
     }
     if (a.db_part && mine) {
