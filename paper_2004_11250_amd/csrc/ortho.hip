@@ -11,7 +11,8 @@
 // a few per cent.  X, A and B are therefore kept as pairs of fp16 values
 // (22 bits; the values' range is known, so a fixed power of two keeps them
 // clear of fp16's ends), products are summed in fp32, and
-//   fp32 updates   take three plane products each (all but rest x rest);
+//   fp32 updates   take three plane products each (all but rest x rest), and
+//                  a is added to B's diagonal: X <- (a + B) X;
 //   bf16 updates   take one: the upper values' product.  The rests enter where
 //                  they cost nothing, in the epilogues: a X and b A use both
 //                  values, and of A's and B's rests, whose largest part by far
@@ -404,6 +405,10 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = fc * v[e] + fa * (static_cast<float>(h[e]) + static_cast<float>(l[e]));
+        if constexpr (P > 1) {   // a X comes with B X
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += x + e == y ? s.a * kSB : 0.f;
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= fc;
@@ -493,18 +498,20 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
       int r, c;
       view.col_piece(i, &r, &c);
       if (cb + c >= mm || rb + r >= np) continue;
-      float v[8], x[8];
+      float v[8];
       view.col(r, c, v);
       const int64_t at = static_cast<int64_t>(cb + c) * np + rb + r;
-      pair8(from + at, plane, x);
       const float fb = LAST ? 1.f / (kSB * kSX) : 1.f / kSB, fx = LAST ? s.a / kSX : s.a;
       if constexpr (P == 1) {
+        float x[8];
+        pair8(from + at, plane, x);
         const float d = m.db[cb + c];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += d * x[e];
-      }
+        for (int e = 0; e < 8; ++e) v[e] = fx * x[e] + fb * (v[e] + d * x[e]);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fx * x[e] + fb * v[e];
+        for (int e = 0; e < 8; ++e) v[e] *= fb;
+      }
       if constexpr (LAST) {
         if (turned)
           view.put_col(r, c, v);
