@@ -104,20 +104,46 @@ __device__ __forceinline__ uint64_t uniform64(uint64_t v) {
          static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v)));
 }
 
+// The plane products of operands of n planes each, in the order in which they
+// are added (as kPairs1, 3 and 6).
+struct PlanePair {
+  int a, b;
+};
+template <int N>
+struct PlaneProducts;
+template <>
+struct PlaneProducts<1> {
+  static constexpr int COUNT = 1;
+  static constexpr PlanePair LIST[] = {{0, 0}};
+};
+template <>
+struct PlaneProducts<2> {
+  static constexpr int COUNT = 3;
+  static constexpr PlanePair LIST[] = {{1, 0}, {0, 1}, {0, 0}};
+};
+template <>
+struct PlaneProducts<3> {
+  static constexpr int COUNT = 6;
+  static constexpr PlanePair LIST[] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+};
+
 template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, int WK_ = 1, bool PHASED_ = false, bool AR_ = false,
-          bool BR_ = false>
+          bool BR_ = false, int NP_ = 1>
 struct GemmTile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int STAGES = STAGES_;                // steps held in LDS
   static constexpr bool PHASED = PHASED_;
   static constexpr bool AR = AR_, BR = BR_;             // the operand is stored by rows of k
+  // Planes of each operand that a step brings; it makes all their products.
+  // 1: one plane pair after the other along a longer k, as run() is told.
+  static constexpr int NP = NP_;
   // WK groups of WM x WN waves: each takes every WK-th step, on operands of its
   // own, and the groups' sums are added in LDS at the end
   static constexpr int WK = WK_, NW = WM * WN, THREADS = NW * WK * 64;
   static constexpr int TM = BM / WM, TN = BN / WN;      // a wave's part
   static constexpr int FM = TM / 16, FN = TN / 16;      // in 16 x 16 blocks
   static constexpr int QA = BM / (8 * NW), QB = BN / (8 * NW);   // DMAs a wave issues for a step
-  static constexpr uint32_t LDS_A = BM * kBK * 2, LDS_STEP = (BM + BN) * kBK * 2;
+  static constexpr uint32_t PLANE_A = BM * kBK * 2, PLANE_B = BN * kBK * 2, LDS_A = NP * PLANE_A, LDS_STEP = NP * (PLANE_A + PLANE_B);
   static constexpr uint32_t LDS_RING = STAGES * LDS_STEP, LDS_BYTES = WK * LDS_RING;
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 16 == 0 && TN % 16 == 0, "tile");
   static_assert((FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0 && FM <= 8 && FN <= 8, "blocks");
@@ -142,8 +168,7 @@ struct GemmTile {
     static constexpr int LPR = R ? E / 8 : 8, RPI = 64 / LPR;   // lanes a stored row takes, stored rows a DMA brings
     uint64_t base[kMaxPlanes];
     int64_t step, left;       // bytes from a step to the next; bytes from the first step on (rows of k)
-    uint64_t now;             // the next step's address
-    int64_t rest;             // and bytes from there on
+    int64_t now;              // bytes from the first step to the next one
     uint32_t off[Q];          // per lane
     uint32_t at;              // of this lane's LDS reads
 
@@ -180,22 +205,18 @@ struct GemmTile {
         at = static_cast<uint32_t>((wrow + (ln & 15)) * 128 + ((ln >> 4) ^ (ln & 7)) * 16);
       }
     }
-    // The descriptor moves on by scalar additions, so a DMA has no vector
-    // instruction's result to wait for.
-    __device__ __forceinline__ void go(uint32_t plane, int kk) {
-      now = (plane == 0 ? base[0] : plane == 1 ? base[1] : base[2]) + static_cast<uint64_t>(kk * step);
-      if constexpr (R) rest = left - kk * step;
-    }
-    __device__ __forceinline__ void move() {
-      now += WK * step;
-      if constexpr (R) rest -= WK * step;
-    }
-    __device__ __forceinline__ u32x4_t rsrc() const {
+    // The descriptor's base is a sum taken in scalar registers, so a DMA has no
+    // vector instruction's result to wait for.
+    __device__ __forceinline__ u32x4_t rsrc(uint32_t plane) const {
+      const uint64_t b = (plane == 0 ? base[0] : plane == 1 ? base[1] : base[2]) + static_cast<uint64_t>(now);
       u32x4_t r;
-      r.x = static_cast<uint32_t>(now);
-      r.y = static_cast<uint32_t>(now >> 32) & 0xFFFFu;
+      r.x = static_cast<uint32_t>(b);
+      r.y = static_cast<uint32_t>(b >> 32) & 0xFFFFu;
       r.z = 0x7FFFFFFFu;
-      if constexpr (R) r.z = rest <= 0 ? 0u : rest < 0x7FFFFFFF ? static_cast<uint32_t>(rest) : 0x7FFFFFFFu;   // (k past the end reads zeros)
+      if constexpr (R) {   // (k past the end reads zeros)
+        const int64_t rest = left - now;
+        r.z = rest <= 0 ? 0u : rest < 0x7FFFFFFF ? static_cast<uint32_t>(rest) : 0x7FFFFFFFu;
+      }
       r.w = 0x00020000u;
       return r;
     }
@@ -224,7 +245,7 @@ struct GemmTile {
   struct Feed {
     Side<BM, QA, AR, TM> a;
     Side<BN, QB, BR, TN> b;
-    u32x4_t ra, rb;
+    u32x4_t ra[NP], rb[NP];
     uint32_t code;
     int ksteps, pair, kk, wv;
 
@@ -237,26 +258,34 @@ struct GemmTile {
       code = pairs.code;
       ksteps = __builtin_amdgcn_readfirstlane(ksteps_);
       pair = s0 / ksteps, kk = s0 - pair * ksteps;
-      a.go(code >> (4 * pair) & 3, kk), b.go(code >> (4 * pair + 2) & 3, kk);
+      a.now = kk * a.step, b.now = kk * b.step;
     }
     // descriptors of the next step
     __device__ __forceinline__ void next() {
-      ra = a.rsrc(), rb = b.rsrc();
-      kk += WK;
-      if (kk < ksteps) {
-        a.move(), b.move();
-      } else {   // the next plane pair
-        while (kk >= ksteps) kk -= ksteps, ++pair;
-        a.go(code >> (4 * pair) & 3, kk), b.go(code >> (4 * pair + 2) & 3, kk);
+      if constexpr (NP > 1) {
+#pragma unroll
+        for (int q = 0; q < NP; ++q) ra[q] = a.rsrc(q), rb[q] = b.rsrc(q);
+        a.now += WK * a.step, b.now += WK * b.step;
+      } else {
+        ra[0] = a.rsrc(code >> (4 * pair) & 3), rb[0] = b.rsrc(code >> (4 * pair + 2) & 3);
+        kk += WK;
+        if (kk < ksteps) {
+          a.now += WK * a.step, b.now += WK * b.step;
+        } else {   // the next plane pair
+          while (kk >= ksteps) kk -= ksteps, ++pair;
+          a.now = kk * a.step, b.now = kk * b.step;
+        }
       }
     }
     template <int I>
     __device__ __forceinline__ void dma_a(uint32_t buf) const {
-      gemm_dma(ra, a.off[I], buf + 1024u * group_a(I, wv));
+#pragma unroll
+      for (int q = 0; q < NP; ++q) gemm_dma(ra[q], a.off[I], buf + q * PLANE_A + 1024u * group_a(I, wv));
     }
     template <int I>
     __device__ __forceinline__ void dma_b(uint32_t buf) const {
-      gemm_dma(rb, b.off[I], buf + LDS_A + 1024u * group_b(I, wv));
+#pragma unroll
+      for (int q = 0; q < NP; ++q) gemm_dma(rb[q], b.off[I], buf + LDS_A + q * PLANE_B + 1024u * group_b(I, wv));
     }
     template <int I = 0>
     __device__ __forceinline__ void all(uint32_t buf) const {
@@ -276,6 +305,9 @@ struct GemmTile {
     if constexpr (PHASED && !BR) return (2 * (i & 1) + (w >> 2)) * (TN / 8) + (i >> 1) * (TN / 16) + (w & 3);
     return NW * i + w;
   }
+
+  // how many steps a product of ksteps k steps takes
+  static __device__ __forceinline__ int steps_of(int ksteps, PlanePairs pairs) { return NP > 1 ? ksteps : ksteps * pairs.n; }
 
   // steps [s0, s1) of the flattened (plane pair, k step) range; ksteps k steps
   // a pair.  lds: LDS_BYTES of shared memory.
@@ -311,7 +343,7 @@ struct GemmTile {
     for (int s = 0; s < rounds; ++s) {
       // this step has landed once at most the later ones' DMAs are in flight
       if (s + STAGES - 1 <= n)
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * (QA + QB)) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((STAGES - 2) * NP * (QA + QB)) : "memory");
       else
         gemm_sync();
       if (s + STAGES - 1 < n) {
@@ -322,15 +354,21 @@ struct GemmTile {
       const uint32_t la = lds0 + cur;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        Frag a[FM], b[FN];
+        Frag a[NP][FM], b[NP][FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j) b[j] = feed.b.read(la, j, h);
+        for (int q = NP - 1; q >= 0; --q) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i) a[i] = feed.a.read(la, i, h);
+          for (int j = 0; j < FN; ++j) b[q][j] = feed.b.read(la + q * PLANE_B, j, h);
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
+          for (int i = 0; i < FM; ++i) a[q][i] = feed.a.read(la + q * PLANE_A, i, h);
+        }
 #pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = Mfma<T>::mul(a[i], b[j], acc[i][j]);
+        for (int k = 0; k < PlaneProducts<NP>::COUNT; ++k)
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+              acc[i][j] = Mfma<T>::mul(a[PlaneProducts<NP>::LIST[k].a][i], b[PlaneProducts<NP>::LIST[k].b][j], acc[i][j]);
       }
       put = cur;
       cur = cur + LDS_STEP == LDS_RING ? 0 : cur + LDS_STEP;
@@ -344,7 +382,7 @@ struct GemmTile {
   // step's k.  What has been read is overwritten from the next phase on by the
   // step after next, so that a DMA has a step and more to land.
   static __device__ __forceinline__ void phased(Feed& feed, int n, uint32_t lds0, f32x4 (&acc)[FM][FN]) {
-    static_assert(!PHASED || (NW == 8 && WK == 1 && STAGES == 2 && QA == 4 && QB == 4 && FM == 8 && FN == 4), "phases");
+    static_assert(!PHASED || (NP == 1 && NW == 8 && WK == 1 && STAGES == 2 && QA == 4 && QB == 4 && FM == 8 && FN == 4), "phases");
     const int wv = wave();
     constexpr int HM = FM / 2, HN = FN / 2;
     auto fetch = [&](uint32_t buf) {   // (columns first: the counts below)

@@ -376,7 +376,7 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
   const GemmOperand x = POLY ? planes_of(m.a, m.m, m.mp) : planes_of(turn ? m.x[1] : m.x[0], m.m, m.np);
   const int ksteps = (POLY ? m.mp : m.np) / kBK;
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(x, x, pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
+  Tile::run(x, x, pairs, row0, col0, ksteps, 0, Tile::steps_of(ksteps, pairs), lds, acc);
   const int mm = m.m, mp = m.mp;
   const int64_t plane = static_cast<int64_t>(mm) * mp;
   const half_t* a = m.a;
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
       *reinterpret_cast<f16x8*>(out + at) = h;
       // (else only this half's rests that share a tile of the next product with
       // the diagonal are read)
-      if (P > 1 || (!POLY && (rb + r) / kTileEdge[kBig] == (cb + c) / kTileEdge[kBig]))
+      if (P > 1 || (!POLY && (rb + r) / tile_m(1, kBig) == (cb + c) / tile_m(1, kBig)))
         *reinterpret_cast<f16x8*>(out + at + plane) = l;
     }
   });
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(Tile::THREADS) void apply_kernel(Table t, Step s, P
   f32x4 acc[Tile::FM][Tile::FN];
   const half_t* from = turn ? m.x[1] : m.x[0];
   half_t* to = turn ? m.x[0] : m.x[1];
-  Tile::run(planes_of(from, mm, np, true), planes_of(m.b, mm, mp), pairs, row0, col0, ksteps, 0, ksteps * pairs.n, lds, acc);
+  Tile::run(planes_of(from, mm, np, true), planes_of(m.b, mm, mp), pairs, row0, col0, ksteps, 0, Tile::steps_of(ksteps, pairs), lds, acc);
   const int64_t plane = static_cast<int64_t>(mm) * np;
   const bool turned = m.turned;
   Tile::staged(lds, acc, [&](int rb, int cb, typename Tile::View view) {
@@ -703,16 +703,16 @@ struct Plan {
 // The tile that takes the least modelled time for a stage over all matrices;
 // tiles(m, edge) and steps(m) of each.
 template <class F, class G>
-int pick(const std::vector<Mat>& mats, F&& tiles, G&& steps) {
+int pick(int np, const std::vector<Mat>& mats, F&& tiles, G&& steps) {
   int best = kSmall;
   double least = 1e300;
   for (int k = 0; k < kTiles; ++k) {
     double n = 0., work = 0., most = 0.;
     for (const Mat& m : mats) {
-      const double t = static_cast<double>(tiles(m, kTileEdge[k])), s = steps(m);
+      const double t = static_cast<double>(tiles(m, tile_m(np, k))), s = steps(m);
       n += t, work += t * s, most = std::max(most, s);
     }
-    const double t = tile_time(k, n, work / n, most);
+    const double t = tile_time(np, k, n, work / n, most);
     if (t < least) least = t, best = k;
   }
   return best;
@@ -746,13 +746,12 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
   std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
   auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.mp, t); return k * (k + 1) / 2; };   // (the padding is written too)
   auto rect = [](const Mat& m, int t) { return cdiv(m.np, t) * cdiv(m.m, t); };
-  const int pairs = planes == 1 ? 1 : 3;
-  p->gram = pick(p->mats, tri, [&](const Mat& m) { return m.np / 64 * pairs; });
-  p->poly = pick(p->mats, tri, [&](const Mat& m) { return m.mp / 64 * pairs; });
-  p->apply = pick(p->mats, rect, [&](const Mat& m) { return m.mp / 64 * pairs; });
+  p->gram = pick(planes, p->mats, tri, [](const Mat& m) { return m.np / 64; });
+  p->poly = pick(planes, p->mats, tri, [](const Mat& m) { return m.mp / 64; });
+  p->apply = pick(planes, p->mats, rect, [](const Mat& m) { return m.mp / 64; });
   for (Mat& m : p->mats) {
-    const int64_t n[kStages] = {m.chunks, static_cast<int64_t>(m.mp / 64) * (m.np / 64), tri(m, kTileEdge[p->gram]),
-                                tri(m, kTileEdge[p->poly]), rect(m, kTileEdge[p->apply])};
+    const int64_t n[kStages] = {m.chunks, static_cast<int64_t>(m.mp / 64) * (m.np / 64), tri(m, tile_m(planes, p->gram)),
+                                tri(m, tile_m(planes, p->poly)), rect(m, tile_m(planes, p->apply))};
     for (int k = 0; k < kStages; ++k) {
       p->start[k].push_back(static_cast<int32_t>(p->blocks[k]));
       p->blocks[k] += n[k];
@@ -780,7 +779,7 @@ dim3 grid_of(const Spread& s) { return dim3(static_cast<uint32_t>(cdiv(s.total, 
 template <int P, bool POLY>
 void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
   const Spread sp = spread_of(p.blocks[POLY ? kStagePoly : kStageGram]);
-  with_tile<half_t, false, false>(POLY ? p.poly : p.gram, [&](auto k) {
+  with_tile<half_t, false, false, P>(POLY ? p.poly : p.gram, [&](auto k) {
     using Tile = decltype(k);
     hipLaunchKernelGGL((gram_kernel<Tile, P, POLY>), grid_of(sp), dim3(Tile::THREADS), 0, st, t, s, pairs, turn, sp);
   });
@@ -789,7 +788,7 @@ void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int tu
 template <class S, int P, bool LAST>
 void apply(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
   const Spread sp = spread_of(p.blocks[kStageApply]);
-  with_tile<half_t, true, false>(p.apply, [&](auto k) {
+  with_tile<half_t, true, false, P>(p.apply, [&](auto k) {
     using Tile = decltype(k);
     hipLaunchKernelGGL((apply_kernel<Tile, S, P, LAST>), grid_of(sp), dim3(Tile::THREADS), 0, st, t, s, pairs, turn, sp);
   });

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "gemm_tile.hpp"
 #include "ppk1.hpp"
@@ -32,62 +33,80 @@ inline GemmOperand operand(const void* base, int64_t plane_elems, int64_t ld, in
   return o;
 }
 
-// The tiles of the products, and when each is used.  Measured on MI355X (us a
-// step of 64 k, with every CU full / alone on its CU; us at either end of a
-// tile):
-//   256 x 256 phased                                     1.6 / 1.15      6
-//   128 x 128, two workgroups a CU                       0.52 / 0.58     3.5
-//   64 x 64, four steps in flight, two a CU              0.19 / 0.27     2.5
-//   64 x 64, two groups of waves share the steps         0.23 / 0.19     4
-//   32 x 32, four waves share the steps, two a CU        0.1 / 0.12      2.8
-// The large tile wins wherever it fills the card (1310 TFLOP/s at 8192^3; the
-// others 1040, 720, 630), the small ones where it would leave CUs without work:
-// 4096^3 takes 104, 141, 218 and 267 us, 2048^3 43, 27, 28, 35 and 58,
-// 1000 x 3008 x 1000 -, 35, 16, 14 and 21, 512 x 4608 x 512 80, 42, 20, 17 and 11,
-// 256 x 960 x 256 -, 13, 6.5, 6.1 and 4.5.  Operands stored by rows of k cost 5 to
-// 10 % each.
+// The tiles of the products, and when each is used.  Measured on MI355X, us a
+// step of 64 k with every CU full / alone on its CU, and us at either end of a
+// tile; with one plane an operand, with two (three products), with three (six):
+//   256 x 256 phased            1.6 / 1.15   6     4.8 / 3.45    6     9.6 / 6.9   6
+//   128 x 128                   0.52 / 0.58  3.5   1.37 / 1.16   4.5   -
+//   128 x 64                    -                  -                   1.5 / 1.25  2.5
+//   64 x 64                     0.19 / 0.27  2.5   0.41 / 0.62   2.8   1.03 / 0.92 2
+//   64 x 64, two groups of
+//     waves share the steps     0.23 / 0.19  4     0.55 / 0.5    4     -
+//   32 x 32, a wave's own steps 0.1 / 0.12   2.8   0.27 / 0.25   2.8   0.46 / 0.43 2.8
+// The large tile wins wherever it fills the card (one plane, 8192^3: 1310
+// TFLOP/s; 128 x 128 1040, 64 x 64 720), the small ones where it would leave CUs
+// without work (512 x 512, k 4608: 80, 42, 20, 17 and 11 us).  All but the
+// largest bring all planes of a step together: half the traffic and one barrier
+// for three or six products, but as much LDS as there are planes.  512 x 512, k
+// 4608, three products: 64 x 64 tiles 49 us, 32 x 32 21; one after the other 65
+// and 39.  2048^3, six products: 128 x 64 98 us, 64 x 64 135; 128 x 128, one
+// after the other, 145.  Operands stored by rows of k cost 5 to 10 % each.
 enum { kBig = 0, kMid = 1, kSmall = 2, kDeep = 3, kNarrow = 4, kTiles = 5 };
-template <class T, bool AR, bool BR> using BigTile = GemmTile<T, 256, 256, 2, 4, 2, 1, true, AR, BR>;
-template <class T, bool AR, bool BR> using MidTile = GemmTile<T, 128, 128, 2, 2, 2, 1, false, AR, BR>;
-template <class T, bool AR, bool BR> using SmallTile = GemmTile<T, 64, 64, 2, 2, 4, 1, false, AR, BR>;
-template <class T, bool AR, bool BR> using DeepTile = GemmTile<T, 64, 64, 2, 2, 4, 2, false, AR, BR>;
-template <class T, bool AR, bool BR> using NarrowTile = GemmTile<T, 32, 32, 1, 1, 2, 4, false, AR, BR>;
-constexpr int kTileEdge[kTiles] = {256, 128, 64, 64, 32};
-constexpr int kTileWM[kTiles] = {2, 2, 2, 2, 1}, kTileWN[kTiles] = {4, 2, 2, 2, 1};   // waves' parts of a tile
+template <class T, bool AR, bool BR, int NP>
+struct Tiles {
+  using Big = GemmTile<T, 256, 256, 2, 4, 2, 1, true, AR, BR>;
+  using Mid = std::conditional_t<NP == 2, GemmTile<T, 128, 128, 2, 4, 2, 1, false, AR, BR, 2>,
+                                 std::conditional_t<NP == 3, GemmTile<T, 128, 64, 4, 2, 2, 1, false, AR, BR, 3>,
+                                                    GemmTile<T, 128, 128, 2, 2, 2, 1, false, AR, BR>>>;
+  using Small = GemmTile<T, 64, 64, 2, 2, NP == 1 ? 4 : 2, 1, false, AR, BR, NP>;
+  using Deep = GemmTile<T, 64, 64, 2, 2, NP == 1 ? 4 : 2, 2, false, AR, BR, NP == 3 ? 1 : NP>;
+  using Narrow = GemmTile<T, 32, 32, 1, 1, 2, NP == 3 ? 3 : 4, false, AR, BR, NP>;
+};
+// rows and columns of a tile, and its waves' parts of them
+constexpr int tile_m(int, int k) { return k == kBig ? 256 : k == kMid ? 128 : k == kNarrow ? 32 : 64; }
+constexpr int tile_n(int np, int k) { return k == kMid && np == 3 ? 64 : tile_m(np, k); }
+constexpr int tile_wm(int np, int k) { return k == kMid && np == 3 ? 4 : k == kNarrow ? 1 : 2; }
+constexpr int tile_wn(int np, int k) { return k == kBig || (k == kMid && np == 2) ? 4 : k == kNarrow ? 1 : 2; }
 constexpr int kCUs = 256;
 
-// f(tile's type) for tile k; AR, BR: operands stored by rows of k
-template <class T, bool AR, bool BR, class F>
+// f(tile's type) for tile k; AR, BR: operands stored by rows of k; NP: planes
+template <class T, bool AR, bool BR, int NP, class F>
 void with_tile(int k, F&& f) {
+  using X = Tiles<T, AR, BR, NP>;
   if (k == kBig)
-    f(BigTile<T, AR, BR>());
+    f(typename X::Big());
   else if (k == kMid)
-    f(MidTile<T, AR, BR>());
+    f(typename X::Mid());
   else if (k == kSmall)
-    f(SmallTile<T, AR, BR>());
-  else if (k == kDeep)
-    f(DeepTile<T, AR, BR>());
-  else
-    f(NarrowTile<T, AR, BR>());
+    f(typename X::Small());
+  else if constexpr (NP < 3) {
+    if (k == kDeep)
+      f(typename X::Deep());
+    else
+      f(typename X::Narrow());
+  } else
+    f(typename X::Narrow());
 }
 
-// Modelled time in us of `tiles` tiles of `steps` steps on average, `most` at
-// most.
-inline double tile_time(int tile, double tiles, double steps, double most) {
-  constexpr double full[kTiles] = {1.6, 0.52, 0.19, 0.23, 0.1}, alone[kTiles] = {1.15, 0.58, 0.27, 0.19, 0.12},
-                   ends[kTiles] = {6., 3.5, 2.5, 4., 2.8};
+// Modelled time in us of `tiles` tiles of `steps` k steps on average, `most` at
+// most, with np planes an operand.
+inline double tile_time(int np, int tile, double tiles, double steps, double most) {
+  constexpr double full[3][kTiles] = {{1.6, 0.52, 0.19, 0.23, 0.1}, {4.8, 1.37, 0.41, 0.55, 0.27}, {9.6, 1.5, 1.03, 1e9, 0.46}};
+  constexpr double alone[3][kTiles] = {{1.15, 0.58, 0.27, 0.19, 0.12}, {3.45, 1.16, 0.62, 0.5, 0.25}, {6.9, 1.25, 0.92, 1e9, 0.43}};
+  constexpr double ends[3][kTiles] = {{6., 3.5, 2.5, 4., 2.8}, {6., 4.5, 2.8, 4., 2.8}, {6., 2.5, 2., 0., 2.8}};
+  constexpr bool single[3][kTiles] = {{true, false, false, true, false}, {true, true, false, true, true}, {true, true, true, true, true}};
+  const int q = np - 1;   // (single: one workgroup a CU)
   const double n = static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs));
   // (a card in part idle clocks higher and shares its caches among fewer)
-  const double step = alone[tile] + (std::max(full[tile], alone[tile]) - alone[tile]) * std::min(1., tiles / kCUs);
-  const bool single = tile == kBig || tile == kDeep;   // one workgroup a CU
-  return std::max(most * step, n > 1 ? n * steps * full[tile] : 0.) + ends[tile] * (single ? n : 0.5 + 0.5 * n);
+  const double step = alone[q][tile] + (std::max(full[q][tile], alone[q][tile]) - alone[q][tile]) * std::min(1., tiles / kCUs);
+  return std::max(most * step, n > 1 ? n * steps * full[q][tile] : 0.) + ends[q][tile] * (single[q][tile] ? n : 0.5 + 0.5 * n);
 }
 
-inline int pick_tile(int64_t m, int64_t n, int64_t steps) {
+inline int pick_tile(int np, int64_t m, int64_t n, int64_t steps) {
   int best = kSmall;
   double least = 1e300;
   for (int k = 0; k < kTiles; ++k) {
-    const double t = tile_time(k, static_cast<double>(cdiv(m, kTileEdge[k]) * cdiv(n, kTileEdge[k])), steps, steps);
+    const double t = tile_time(np, k, static_cast<double>(cdiv(m, tile_m(np, k)) * cdiv(n, tile_n(np, k))), steps, steps);
     if (t < least) least = t, best = k;
   }
   return best;
@@ -99,14 +118,14 @@ inline int pick_tile(int64_t m, int64_t n, int64_t steps) {
 struct SplitTile {
   int tile, splits;
 };
-inline SplitTile pick_split(int64_t m, int64_t n, int64_t steps, double* time = nullptr) {
+inline SplitTile pick_split(int np, int64_t m, int64_t n, int64_t steps, double* time = nullptr) {
   SplitTile best = {kSmall, 1};
   double least = 1e300;
   for (int k = 0; k < kTiles; ++k)
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (s > 1 && (steps / s < 4 || static_cast<double>(s) * m * n * 4 > 256e6)) break;
+      if (s > 1 && (steps / s < (np > 1 ? 2 : 4) || static_cast<double>(s) * m * n * 4 > 256e6)) break;
       const double per = static_cast<double>(cdiv(steps, s));
-      double t = tile_time(k, static_cast<double>(cdiv(m, kTileEdge[k]) * cdiv(n, kTileEdge[k]) * s), per, per);
+      double t = tile_time(np, k, static_cast<double>(cdiv(m, tile_m(np, k)) * cdiv(n, tile_n(np, k)) * s), per, per);
       if (s > 1) t += 4. + s * static_cast<double>(m) * n * 8e-6 / 3.;
       if (t < least) least = t, best = {k, s};
     }

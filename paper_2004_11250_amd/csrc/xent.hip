@@ -260,7 +260,7 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   }
 
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, a.ksteps * a.pairs.n, lds, acc);
+  Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, Tile::steps_of(a.ksteps, a.pairs), lds, acc);
   Tile::reduce(lds, acc);
 
   // (everything that has to be fetched first, without branches between)
@@ -577,7 +577,7 @@ __global__ __launch_bounds__(Tile::THREADS) void product_kernel(ProductArgs a) {
   int ti, tj;
   band_order(id - split * tiles, a.tm, a.tn, &ti, &tj);
   const int row0 = ti * Tile::BM, col0 = tj * Tile::BN;
-  const int steps = a.ksteps * a.pairs.n;
+  const int steps = Tile::steps_of(a.ksteps, a.pairs);
   const int s0 = static_cast<int>(static_cast<int64_t>(steps) * split / a.splits);
   const int s1 = static_cast<int>(static_cast<int64_t>(steps) * (split + 1) / a.splits);
   const float scale = a.slab ? 1.f : common_scale(a.k);
@@ -644,15 +644,15 @@ constexpr int64_t kPieceBytes = int64_t(512) << 20;   // of G
 
 // Modelled time of the gradient's products for nv classes.
 double piece_time(const Plan& p, int64_t nv, bool turned) {
-  const int64_t steps = p.dp / 64 * p.pairs.n;
-  const int k = pick_tile(nv, p.t, steps);
-  const double tiles = static_cast<double>(cdiv(nv, kTileEdge[k]) * cdiv(p.t, kTileEdge[k])), s = static_cast<double>(steps);
+  const int64_t steps = p.dp / 64;
+  const int k = pick_tile(p.planes, nv, p.t, steps);
+  const double tiles = static_cast<double>(cdiv(nv, tile_m(p.planes, k)) * cdiv(p.t, tile_n(p.planes, k))), s = static_cast<double>(steps);
   // (G's epilogue: about 10 us a round of large tiles)
-  double t = tile_time(k, tiles, s, s) + (k == kBig ? 10. * static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs)) : 0.);
+  double t = tile_time(p.planes, k, tiles, s, s) + (k == kBig ? 10. * static_cast<double>(cdiv(static_cast<int64_t>(tiles), kCUs)) : 0.);
   double x;
-  pick_split(turned ? p.t : p.d, turned ? p.d : p.t, cdiv(nv, 64) * p.pairs.n, &x);
+  pick_split(p.planes, turned ? p.t : p.d, turned ? p.d : p.t, cdiv(nv, 64), &x);
   t += x;
-  pick_split(p.d, nv, cdiv(p.t, 64) * p.pairs.n, &x);
+  pick_split(p.planes, p.d, nv, cdiv(p.t, 64), &x);
   return t + x;
 }
 
@@ -698,8 +698,8 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   if (!p.x_direct) p.x_k = take(p.t * p.dp * e);
   if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
   if (fwd) {
-    p.logit = pick_tile(p.v, p.t, p.dp / 64 * p.pairs.n);
-    const int64_t edge = kTileEdge[p.logit], wm = kTileWM[p.logit];
+    p.logit = pick_tile(p.planes, p.v, p.t, p.dp / 64);
+    const int64_t edge = tile_m(p.planes, p.logit), wm = tile_wm(p.planes, p.logit);
     p.fwd_piece = std::min(p.vp, std::max<int64_t>(256, kPartBytes / (p.t * 8) / wm * edge / 256 * 256));
     p.parts = static_cast<int>(cdiv(p.fwd_piece, edge) * wm);
     p.part = take((p.parts + 1) * p.t * 8);   // (and what the pieces before left)
@@ -717,12 +717,12 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     for (int i = 0; i < 2; ++i) {
       const int64_t nv = i ? p.v - (p.pieces - 1) * p.piece : std::min(p.piece, p.v);
       Plan::Piece& q = p.of[i];
-      q.logit = pick_tile(nv, p.t, p.dp / 64 * p.pairs.n);
-      db = std::max(db, cdiv(p.t, kTileEdge[q.logit]) * kTileWN[q.logit] * nv * 4);
-      const SplitTile x = pick_split(dm, dn, cdiv(nv, 64) * p.pairs.n);
+      q.logit = pick_tile(p.planes, nv, p.t, p.dp / 64);
+      db = std::max(db, cdiv(p.t, tile_n(p.planes, q.logit)) * tile_wn(p.planes, q.logit) * nv * 4);
+      const SplitTile x = pick_split(p.planes, dm, dn, cdiv(nv, 64));
       q.dx = x.tile;
       if (i == 0) p.dx_splits = x.splits;   // (dx's partial sums are kept over the pieces)
-      q.dw = pick_split(p.d, nv, cdiv(p.t, 64) * p.pairs.n);
+      q.dw = pick_split(p.planes, p.d, nv, cdiv(p.t, 64));
       if (q.dw.splits > 1) dw_slab = std::max(dw_slab, q.dw.splits * p.dw_ld * nv * 4);
     }
     p.dx_slab = p.dx_splits > 1 || p.pieces > 1;
@@ -743,9 +743,9 @@ void stage(const StageArgs* a, int n, hipStream_t st) {
 
 template <bool GRAD, int P>
 void logits(int tile, LogitArgs& a, hipStream_t st) {
-  a.tm = static_cast<int32_t>(cdiv(pad64(a.w.rows), kTileEdge[tile]));   // (G's padding is written too)
-  a.tn = static_cast<int32_t>(cdiv(a.x.rows, kTileEdge[tile]));
-  with_tile<__bf16, false, false>(tile, [&](auto t) {
+  a.tm = static_cast<int32_t>(cdiv(pad64(a.w.rows), tile_m(P, tile)));   // (G's padding is written too)
+  a.tn = static_cast<int32_t>(cdiv(a.x.rows, tile_n(P, tile)));
+  with_tile<__bf16, false, false, P>(tile, [&](auto t) {
     using Tile = decltype(t);
     hipLaunchKernelGGL((logit_kernel<Tile, GRAD, P>), dim3(static_cast<uint32_t>(a.tm * a.tn + (a.loss.divisor ? 1 : 0))),
                        dim3(Tile::THREADS), 0, st, a);
@@ -754,9 +754,10 @@ void logits(int tile, LogitArgs& a, hipStream_t st) {
 
 template <class O, bool AR, bool BR>
 void product(int tile, ProductArgs& a, hipStream_t st) {
-  a.tm = static_cast<int32_t>(cdiv(a.m, kTileEdge[tile]));
-  a.tn = static_cast<int32_t>(cdiv(a.n, kTileEdge[tile]));
-  with_tile<__bf16, AR, BR>(tile, [&](auto t) {
+  constexpr int P = std::is_same_v<O, float> ? 3 : 1;
+  a.tm = static_cast<int32_t>(cdiv(a.m, tile_m(P, tile)));
+  a.tn = static_cast<int32_t>(cdiv(a.n, tile_n(P, tile)));
+  with_tile<__bf16, AR, BR, P>(tile, [&](auto t) {
     using Tile = decltype(t);
     hipLaunchKernelGGL((product_kernel<Tile, O>), dim3(static_cast<uint32_t>(a.tm * a.tn * a.splits + a.db_blocks + a.join_blocks)),
                        dim3(Tile::THREADS), 0, st, a);
@@ -844,7 +845,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
       const bool last = v0 + nv == p.v;
       la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0);
       logits<false, P>(p.logit, la, st);
-      const int32_t parts = static_cast<int32_t>(cdiv(pad64(nv), kTileEdge[p.logit]) * kTileWM[p.logit]);
+      const int32_t parts = static_cast<int32_t>(cdiv(pad64(nv), tile_m(P, p.logit)) * tile_wm(P, p.logit));
       const JoinArgs ja = {tok, carry, la.target_logit, v0 ? 0 : 1, parts + 1, last ? nullptr : carry, c.stats, each ? c.loss : nullptr,
                            sums, whole ? loss : LossArgs{}};
       if (n == 16)
@@ -877,7 +878,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     la.db_part = c.db ? f32(p.db) : nullptr;
     logits<true, P>(q.logit, la, st);
     la.loss = {};
-    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * kTileWN[q.logit]), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
+    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * tile_wn(P, q.logit)), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
     const int32_t db_blocks = c.db ? static_cast<int32_t>(cdiv(nv, 64)) : 0;
     if (db_blocks && !c.dw) hipLaunchKernelGGL(class_sum_kernel, dim3(static_cast<uint32_t>(db_blocks)), dim3(1024), 0, st, db, tok);
     // a small slab of dw is joined by dx's product, which comes after it
