@@ -615,6 +615,8 @@ __global__ __launch_bounds__(256) void slab_kernel(Slab j, Tokens k) {
   join_slab<O>(j, k, blockIdx.x, gridDim.x);
 }
 
+#include "xent_few.hpp"
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
@@ -635,6 +637,8 @@ struct Plan {
   bool dx_slab = false;
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
+  bool few = false, few_wide = false; // few tokens: kernels of their own
+  int few_splits = 1;
   // workspace offsets
   size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
 };
@@ -694,6 +698,23 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     at += (n + 255) / 256 * 256;
     return r;
   };
+  p.few = p.t <= kFewTokens;
+  if (p.few) {
+    const int64_t n = bf16 ? 8 : 4;
+    p.few_wide = w_aligned && p.d % n == 0 && d.w_ld % n == 0;
+    if (fwd) {
+      p.parts = static_cast<int>(cdiv(p.v, 128));
+      p.part = take((p.parts + 1) * p.t * 8), p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
+    }
+    if (bwd) {
+      // two workgroups a CU, 64 classes at least
+      p.few_splits = static_cast<int>(std::max<int64_t>(1, std::min(cdiv(p.v, 64), 2 * kCUs / cdiv(p.d, 256))));
+      p.dx_ld = cdiv(p.d, 4) * 4;
+      p.g = take(p.t * p.vp * 4), p.slab = take(p.few_splits * p.t * p.dx_ld * 4);
+    }
+    p.total = std::max<size_t>(at, 256);
+    return p;
+  }
   const size_t e = 2 * p.planes;
   if (!p.x_direct) p.x_k = take(p.t * p.dp * e);
   if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
@@ -772,6 +793,9 @@ void launch_slab(const Slab& j, const Tokens& k, hipStream_t st) {
   hipLaunchKernelGGL((slab_kernel<O>), dim3(grid), dim3(256), 0, st, j, k);
 }
 
+// tokens a workgroup of the join (few parts: more)
+int join_tokens(const Plan& p) { return p.parts > 8 ? 16 : 64; }
+
 struct Call {
   const pp_xent_desc* d;
   const void *x, *w;
@@ -785,13 +809,77 @@ struct Call {
   hipStream_t st;
 };
 
+Tokens tokens_of(const Plan& p, const Call& c) {
+  return {c.target, c.class_weight, c.grad, c.stats, c.d->ignore_index, static_cast<int32_t>(p.t), static_cast<int32_t>(p.v),
+          c.d->reduction == PP_NONE};
+}
+
+void launch_join(const Plan& p, const JoinArgs& a, hipStream_t st) {
+  const uint32_t n = static_cast<uint32_t>(join_tokens(p));
+  const dim3 grid((static_cast<uint32_t>(p.t) + n - 1) / n);
+  if (n == 16)
+    hipLaunchKernelGGL((join_kernel<16>), grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL((join_kernel<4>), grid, dim3(256), 0, st, a);
+}
+
+template <class S, int NT, bool WIDE>
+pp_status enqueue_few(const Plan& p, const Call& c) {
+  const pp_xent_desc& d = *c.d;
+  constexpr int64_t N = 16 / sizeof(S);
+  auto f32 = [&](size_t off) { return reinterpret_cast<float*>(c.ws + off); };
+  const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
+  FewArgs a = {};
+  a.w = c.w, a.w_ld = d.w_ld, a.x = c.x, a.x_sn = d.x_sn, a.x_sp = d.x_sp, a.x_sc = d.x_sc;
+  a.hw = static_cast<int32_t>(d.hw), a.d = static_cast<int32_t>(d.d), a.k = tokens_of(p, c), a.bias = c.bias;
+  a.x_wide = aligned16(c.x) && d.x_sc == 1 && step % N == 0 && (d.hw == 1 || d.x_sn % N == 0);
+  if (p.bwd) a.logits = f32(p.g), a.l_ld = p.vp;
+  if (p.fwd) a.part = reinterpret_cast<float2*>(c.ws + p.part) + p.t, a.target_logit = f32(p.tl);
+  hipLaunchKernelGGL((few_logit_kernel<S, NT, WIDE>), dim3(static_cast<uint32_t>(cdiv(p.v, 128))), dim3(512), 0, c.st, a);
+  if (p.fwd) {
+    const bool each = d.reduction == PP_NONE;
+    double2* sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
+    const int32_t grid = static_cast<int32_t>(cdiv(p.t, join_tokens(p)));
+    const LossArgs loss = {sums, each ? 0 : grid, d.reduction == PP_MEAN, each ? nullptr : c.loss, c.stats + p.t};
+    const JoinArgs ja = {a.k, reinterpret_cast<float2*>(c.ws + p.part), a.target_logit, 1, p.parts + 1, nullptr, c.stats,
+                         each ? c.loss : nullptr, sums, grid == 1 ? loss : LossArgs{}};
+    launch_join(p, ja, c.st);
+    if (grid > 1) hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, loss);
+  }
+  if (!p.bwd) return launched();
+  a.dw = c.dw, a.dw_wide = d.d % 4 == 0 && reinterpret_cast<uintptr_t>(c.dw) % 16 == 0, a.db = c.db;
+  a.slab = c.dx ? f32(p.slab) : nullptr, a.slab_ld = p.dx_ld;
+  a.splits = p.few_splits, a.groups = static_cast<int32_t>(cdiv(p.d, 256));
+  hipLaunchKernelGGL((few_grad_kernel<S, NT, WIDE>), dim3(static_cast<uint32_t>(a.splits * a.groups)), dim3(256), 0, c.st, a);
+  if (c.dx) {
+    const Slab s = {a.slab, p.dx_ld, a.d, static_cast<int32_t>(p.t), a.splits,
+                    {c.dx, d.dx_sc, 0, d.dx_sn, d.dx_sp, 1, a.hw,
+                     d.dx_sc == 1 && reinterpret_cast<uintptr_t>(c.dx) % 16 == 0 && p.d % 4 == 0 && d.dx_sn % 4 == 0 &&
+                         (d.hw == 1 || d.dx_sp % 4 == 0)}};
+    hipLaunchKernelGGL((few_sum_kernel<S>), dim3(static_cast<uint32_t>(cdiv(p.dx_ld / 4 * p.t, 16))), dim3(256), 0, c.st, s, a.k);
+  }
+  return launched();
+}
+
+template <class S>
+pp_status enqueue_few(const Plan& p, const Call& c) {
+  auto run = [&](auto nt) {
+    constexpr int NT = decltype(nt)::value;
+    return p.few_wide ? enqueue_few<S, NT, true>(p, c) : enqueue_few<S, NT, false>(p, c);
+  };
+  if (p.t <= 16) return run(std::integral_constant<int, 1>());
+  if (p.t <= 32) return run(std::integral_constant<int, 2>());
+  if (p.t <= 48) return run(std::integral_constant<int, 3>());
+  return run(std::integral_constant<int, 4>());
+}
+
 template <class S, int P>
 pp_status enqueue(const Plan& p, const Call& c) {
+  if (p.few) return enqueue_few<S>(p, c);
   const pp_xent_desc& d = *c.d;
   hipStream_t st = c.st;
   pp_status s;
-  Tokens tok = {c.target, c.class_weight, c.grad, c.stats, d.ignore_index, static_cast<int32_t>(p.t), static_cast<int32_t>(p.v),
-                d.reduction == PP_NONE};
+  const Tokens tok = tokens_of(p, c);
   auto bf = [&](size_t off) { return reinterpret_cast<__bf16*>(c.ws + off); };
   auto f32 = [&](size_t off) { return reinterpret_cast<float*>(c.ws + off); };
 
@@ -831,9 +919,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     float2* carry = reinterpret_cast<float2*>(c.ws + p.part);
     la.part = carry + p.t;
     const bool each = d.reduction == PP_NONE;
-    // (few parts: more tokens a workgroup)
-    const int n = p.parts > 8 ? 16 : 64;
-    const uint32_t grid = static_cast<uint32_t>(cdiv(p.t, n));
+    const uint32_t grid = static_cast<uint32_t>(cdiv(p.t, join_tokens(p)));
     double2* sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
     // The loss and its divisor: by the join, if that is one workgroup; by the
     // gradient's first product, if there is one (what the divisor scales comes
@@ -848,10 +934,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
       const int32_t parts = static_cast<int32_t>(cdiv(pad64(nv), tile_m(P, p.logit)) * tile_wm(P, p.logit));
       const JoinArgs ja = {tok, carry, la.target_logit, v0 ? 0 : 1, parts + 1, last ? nullptr : carry, c.stats, each ? c.loss : nullptr,
                            sums, whole ? loss : LossArgs{}};
-      if (n == 16)
-        hipLaunchKernelGGL((join_kernel<16>), dim3(grid), dim3(256), 0, st, ja);
-      else
-        hipLaunchKernelGGL((join_kernel<4>), dim3(grid), dim3(256), 0, st, ja);
+      launch_join(p, ja, st);
     }
     if (p.bwd && !whole)
       la.loss = loss;

@@ -1,0 +1,406 @@
+// xent_few.hpp -- the head for few tokens (at most 64), where reading w is the
+// work.  w is read in its own type and not copied; the logits of all classes
+// are kept (they are small), so that the gradient's kernel reads w once.
+//
+// Both kernels use the matrix cores on what the lanes load, sixteen bytes each:
+// which of the k positions of an instruction a lane's values take is free as
+// long as both operands agree, so lane (r, g) = (lane % 16, lane / 16) gives
+// four (or eight) neighbouring channels, one (or all) to an instruction.  fp32
+// values are multiplied in fp32: at these sizes its rate is enough.
+// (Included by xent.hip, inside its namespace.)
+
+constexpr int kFewTokens = 64;
+
+struct FewArgs {
+  const void* w;        // [v][w_ld]
+  int64_t w_ld;
+  const void* x;        // token t, channel c at (t / hw) x_sn + (t % hw) x_sp + c x_sc
+  int64_t x_sn, x_sp, x_sc;
+  int32_t hw, d, x_wide;   // x_wide: pieces of a lane are contiguous and aligned
+  Tokens k;
+  float* logits;        // [token][l_ld], or null
+  int64_t l_ld;
+  // forward
+  const float* bias;
+  float2* part;         // [128 classes][token], or null
+  float* target_logit;
+  // gradient
+  void* dw;             // [v][d], or null
+  int32_t dw_wide;
+  float* db;            // or null
+  float* slab;          // [split][token][slab_ld], or null
+  int64_t slab_ld;
+  int32_t splits, groups;   // of the classes; of the channels (256 each)
+};
+
+constexpr uint32_t kNowhere = 0x80000000u;   // past the end of any buffer made here
+
+// N values from a buffer, at byte offset `at`; 0 past column `cols`
+template <class S, int N, bool WIDE>
+__device__ __forceinline__ auto few_load(__amdgpu_buffer_rsrc_t r, bool row, uint32_t at, int col, int cols) {
+  using V = __attribute__((ext_vector_type(N))) S;
+  if constexpr (WIDE) {   // (cols is a multiple of N)
+    const uint32_t off = row && col < cols ? at : kNowhere;
+    if constexpr (sizeof(V) == 16)
+      return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+    else
+      return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+  } else {
+    V v;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const uint32_t off = row && col + e < cols ? at + e * static_cast<uint32_t>(sizeof(S)) : kNowhere;
+      if constexpr (sizeof(S) == 4)
+        v[e] = __builtin_bit_cast(S, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+      else
+        v[e] = __builtin_bit_cast(S, __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
+    }
+    return v;
+  }
+}
+
+// sixteen rows of w from class c on (the same in all lanes)
+template <class S>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rows(const FewArgs& a, int c) {
+  const S* base = static_cast<const S*>(a.w) + static_cast<int64_t>(c) * a.w_ld;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<S*>(base), 0, static_cast<int>(16 * a.w_ld * sizeof(S)), 0x00020000);
+}
+
+// N channels of a token's features, 0 past the end and for an ignored token
+template <class S, int N>
+__device__ __forceinline__ auto few_x(const FewArgs& a, int t, int c) {
+  using V = __attribute__((ext_vector_type(N))) S;
+  V v = {};
+  if (t >= a.k.t || c >= a.d || a.k.target[t] == a.k.ignore) return v;
+  const int hi = t / a.hw;
+  const S* at = static_cast<const S*>(a.x) + hi * a.x_sn + (t - hi * a.hw) * a.x_sp + c * a.x_sc;
+  if (a.x_wide && c + N <= a.d) return *reinterpret_cast<const V*>(at);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (c + e < a.d) v[e] = at[e * a.x_sc];
+  return v;
+}
+
+// The logits of 128 classes, 16 a wave, with their statistics: a stream of w
+// against the features in LDS, a chunk of the channels at a time.
+template <class S, int NT, bool WIDE>
+__global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
+  constexpr int N = 16 / sizeof(S), KS = 4 * N, U = 4;
+  constexpr int KC = 4096 / (NT * static_cast<int>(sizeof(S))) / (KS * U) * (KS * U);   // (64 KB)
+  static_assert(KC % (KS * U) == 0);
+  using V = __attribute__((ext_vector_type(N))) S;
+  // (rows sixteen bytes apart modulo the banks)
+  __shared__ __align__(16) S xs[16 * NT][KC + N];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c0 = blockIdx.x * 128 + wave * 16, v = a.k.v, d = a.d;
+  const auto rows = few_rows<S>(a, c0);
+  const bool mine = c0 + r < v;
+  const uint32_t at = static_cast<uint32_t>((r * a.w_ld + N * g) * sizeof(S));
+  V cur[U];
+  auto load = [&](int k, V (&to)[U]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      to[u] = few_load<S, N, WIDE>(rows, mine, at + static_cast<uint32_t>((k + u * KS) * sizeof(S)), k + u * KS + N * g, d);
+  };
+  load(0, cur);
+  f32x4 acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bool along = a.x_sc <= (a.hw == 1 ? a.x_sn : a.x_sp);
+  for (int kc = 0; kc < d; kc += KC) {
+    const int kn = min(KC, (d - kc + KS * U - 1) / (KS * U) * (KS * U));
+    if (kc) __syncthreads();
+    for (int i = tid; i < kn / N * 16 * NT; i += 512) {
+      const int t = along ? i / (kn / N) : i % (16 * NT), k = (along ? i % (kn / N) : i / (16 * NT)) * N;
+      *reinterpret_cast<V*>(&xs[t][k]) = few_x<S, N>(a, t, kc + k);
+    }
+    __syncthreads();
+    for (int k = 0; k < kn; k += KS * U) {
+      V next[U];
+      load(kc + k + KS * U, next);   // (nothing past the last channel)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        V b[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = *reinterpret_cast<const V*>(&xs[16 * j + r][k + u * KS + N * g]);
+        if constexpr (sizeof(S) == 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(cur[u][e], b[j][e], acc[j], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cur[u], b[j], acc[j], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) cur[u] = next[u];
+    }
+  }
+  // lane (r, g) has the classes c0 + 4 g + 0..3 of the tokens 16 j + r
+  const int c = c0 + 4 * g;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float bias = a.bias && c + e < v ? a.bias[c + e] : 0.f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j][e] = c + e < v ? acc[j][e] + bias : -INFINITY;
+  }
+  __syncthreads();
+  float2(*red)[16 * NT] = reinterpret_cast<float2(*)[16 * NT]>(&xs[0][0]);   // [wave][token]
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int t = 16 * j + r;
+    if (t < a.k.t && a.logits && c < a.l_ld) *reinterpret_cast<f32x4*>(a.logits + t * a.l_ld + c) = acc[j];
+    if (!a.part) continue;
+    float m = fmaxf(fmaxf(acc[j][0], acc[j][1]), fmaxf(acc[j][2], acc[j][3]));
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s += fast_exp(acc[j][e] - ref);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (g == 0) red[wave][t] = make_float2(m, s);
+    const int64_t y = t < a.k.t ? a.k.target[t] : -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (y == c + e && c + e < v) a.target_logit[t] = acc[j][e];
+  }
+  if (!a.part) return;
+  __syncthreads();
+  if (tid >= a.k.t) return;
+  float2 s = red[0][tid];
+#pragma unroll
+  for (int w = 1; w < 8; ++w) s = join(s, red[w][tid]);
+  a.part[static_cast<int64_t>(blockIdx.x) * a.k.t + tid] = s;
+}
+
+// G of 64 classes at a time in LDS; each wave has 64 channels, for which it adds
+// G w to dx's sums in registers and stores G^T x.  bf16 operands: G is rounded
+// to bf16 (db is summed before), a lane gives four tokens or classes to one
+// instruction, and the four channels that it loads of each of four classes are
+// turned in its registers.
+template <class S, int NT>
+struct FewG {   // [class][token] for dw, [token][class] for dx
+  __bf16 by_class[64][16 * NT + 4], by_token[16 * NT][64 + 4];
+};
+template <int NT>
+struct FewG<float, NT> {
+  float by_class[64][16 * NT + 4];
+};
+
+template <class S, int NT, bool WIDE>
+__global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
+  using S4 = __attribute__((ext_vector_type(4))) S;
+  constexpr bool F = sizeof(S) == 4;
+  __shared__ __align__(16) FewG<S, NT> gs[2];
+  __shared__ float db_part[2][4][64];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col0 = group * 256 + wave * 64, col = col0 + 4 * r, v = a.k.v, d = a.d;
+  const bool on = col0 < d, dx = a.slab && on, dw = a.dw && on, db = a.db && group == 0;
+  const int blocks = (v + 15) / 16;
+  const int b0 = static_cast<int>(static_cast<int64_t>(blocks) * split / a.splits);
+  const int b1 = static_cast<int>(static_cast<int64_t>(blocks) * (split + 1) / a.splits);
+  const float scale = common_scale(a.k);
+  // a lane's class of load s: 4 s + g, bf16 4 g + s
+  constexpr int kG = F ? 1 : 4, kS = F ? 4 : 1;
+  const uint32_t at = static_cast<uint32_t>((kG * g * a.w_ld + col) * sizeof(S));
+  auto load = [&](int b, S4 (&to)[4]) {
+    const auto rows = few_rows<S>(a, 16 * b);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      to[s] = few_load<S, 4, WIDE>(rows, b < b1 && 16 * b + kS * s + kG * g < v, at + static_cast<uint32_t>(kS * s * a.w_ld * sizeof(S)),
+                                   col, d);
+  };
+  S4 cur[4] = {};
+  if (dx) load(b0, cur);
+  // this thread's part of G: classes 4 q + 0..3 of a chunk, the tokens t0 + 16 i
+  const int q = tid & 15, t0 = tid >> 4;
+  float lse[NT], factor[NT];
+  int64_t target[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int t = t0 + 16 * i;
+    lse[i] = factor[i] = 0.f, target[i] = -1;
+    if (t < a.k.t) {
+      const int64_t y = a.k.target[t];
+      const float weight = a.k.class_weight && y >= 0 && y < v ? a.k.class_weight[y] : 1.f;
+      lse[i] = a.k.stats[t], target[i] = y;
+      factor[i] = token_scale(a.k, y, weight, a.k.grad && a.k.grad_each ? a.k.grad[t] : 1.f);
+    }
+  }
+  f32x4 logit[NT];
+  auto fetch = [&](int b) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int t = t0 + 16 * i, c = 16 * b + 4 * q;
+      logit[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (t < a.k.t && c < 16 * b1) logit[i] = *reinterpret_cast<const f32x4*>(a.logits + t * a.l_ld + c);
+    }
+  };
+  fetch(b0);
+  // x: a lane's four channels of the tokens 16 i + 4 s + g, bf16 16 i + 4 g + s
+  S4 x[NT][4];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) x[i][s] = dw ? few_x<S, 4>(a, 16 * i + kS * s + kG * g, col) : S4{};
+  }
+  // four values of each of four rows -> of each of four columns
+  auto turn = [](const S4 (&u)[4], S4 (&to)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) to[e] = S4{u[0][e], u[1][e], u[2][e], u[3][e]};
+  };
+  if constexpr (!F) {
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      S4 to[4];
+      turn(x[i], to);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[i][e] = to[e];
+    }
+  }
+  f32x4 sum[NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[j][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  using I4 = __attribute__((ext_vector_type(4))) short;
+  auto product = [](auto m, auto n, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(I4, m), __builtin_bit_cast(I4, n), c, 0, 0, 0);
+  };
+
+  int buf = 0;
+  for (int b = b0; b < b1; b += 4, buf ^= 1) {
+    FewG<S, NT>& now = gs[buf];
+    f32x4 all = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      f32x4 p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = 16 * b + 4 * q + e;
+        p[e] = fast_exp(logit[i][e] - lse[i]) * factor[i];
+        if (target[i] == c) p[e] -= factor[i];
+        p[e] = factor[i] != 0.f && c < v ? p[e] : 0.f;
+        now.by_class[4 * q + e][t0 + 16 * i] = static_cast<S>(p[e]);
+      }
+      all += p;
+      if constexpr (!F)
+        *reinterpret_cast<S4*>(&now.by_token[t0 + 16 * i][4 * q]) =
+            S4{static_cast<S>(p[0]), static_cast<S>(p[1]), static_cast<S>(p[2]), static_cast<S>(p[3])};
+    }
+    if (db) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        all[e] += __shfl_xor(all[e], 16);
+        all[e] += __shfl_xor(all[e], 32);
+      }
+      if (lane < 16) *reinterpret_cast<f32x4*>(&db_part[buf][wave][4 * q]) = all;
+    }
+    fetch(b + 4);
+    __syncthreads();   // (the other half is written again after the next one)
+    if (db && tid < 64 && tid < 16 * (b1 - b) && 16 * b + tid < v)
+      a.db[16 * b + tid] = (db_part[buf][0][tid] + db_part[buf][1][tid] + db_part[buf][2][tid] + db_part[buf][3][tid]) * scale;
+    if (!on) continue;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      if (b + n >= b1) break;
+      S4 next[4] = {};
+      if (dx) load(b + n + 1, next);
+      if (dw) {
+        f32x4 out[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          if constexpr (F) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+              const float m = now.by_class[16 * n + r][16 * i + 4 * s + g];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) out[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(m, x[i][s][e], out[e], 0, 0, 0);
+            }
+          } else {
+            const S4 m = *reinterpret_cast<const S4*>(&now.by_class[16 * n + r][16 * i + 4 * g]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[e] = product(m, x[i][e], out[e]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = 16 * (b + n) + 4 * g + e;
+          if (c >= v || col >= d) continue;
+          S* to = static_cast<S*>(a.dw) + static_cast<int64_t>(c) * d + col;
+          S4 o;
+#pragma unroll
+          for (int f = 0; f < 4; ++f) o[f] = static_cast<S>(out[f][e] * scale);
+          if (a.dw_wide) {   // (d is a multiple of four)
+            *reinterpret_cast<S4*>(to) = o;
+          } else {
+#pragma unroll
+            for (int f = 0; f < 4; ++f)
+              if (col + f < d) to[f] = o[f];
+          }
+        }
+      }
+      if (dx) {
+        if constexpr (F) {
+#pragma unroll
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              const float m = now.by_class[16 * n + 4 * s + g][16 * j + r];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sum[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(m, cur[s][e], sum[j][e], 0, 0, 0);
+            }
+        } else {
+          S4 w[4];
+          turn(cur, w);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const S4 m = *reinterpret_cast<const S4*>(&now.by_token[16 * j + r][16 * n + 4 * g]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[j][e] = product(m, w[e], sum[j][e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 4; ++s) cur[s] = next[s];
+    }
+  }
+  if (!dx || col >= a.slab_ld) return;
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int t = 16 * j + 4 * g + e;
+      if (t < a.k.t)
+        *reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.k.t + t) * a.slab_ld + col) =
+            f32x4{sum[j][0][e], sum[j][1][e], sum[j][2][e], sum[j][3][e]};
+    }
+}
+
+// dx of few tokens: 16 pieces of four channels a workgroup, 16 threads each
+// taking every 16th partial sum
+template <class O>
+__global__ __launch_bounds__(256) void few_sum_kernel(Slab s, Tokens k) {
+  __shared__ f32x4 got[16][16];
+  const int u = threadIdx.x & 15, w = threadIdx.x >> 4;
+  const int64_t n4 = s.ld / 4, i = blockIdx.x * 16ll + u, c = i / n4, r = (i - c * n4) * 4;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  if (c < s.n) {
+#pragma unroll 4
+    for (int q = w; q < s.splits; q += 16) x += *reinterpret_cast<const f32x4*>(s.at + (static_cast<int64_t>(q) * s.n + c) * s.ld + r);
+  }
+  got[w][u] = x;
+  __syncthreads();
+  if (w || c >= s.n) return;
+#pragma unroll
+  for (int q = 1; q < 16; ++q) x += got[q][u];
+  store4<O>(s.map, static_cast<int>(r), static_cast<int>(c), s.m, x * common_scale(k));
+}
