@@ -637,7 +637,7 @@ struct Plan {
   bool dx_slab = false;
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
-  bool few = false, few_wide = false; // few tokens: kernels of their own
+  bool few = false, few_odd = false;  // few tokens: kernels of their own
   int few_splits = 1;
   // workspace offsets
   size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
@@ -679,7 +679,7 @@ int64_t pick_piece(const Plan& p, bool turned) {
   return best;
 }
 
-Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligned, bool w_aligned) {
+Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligned, bool w_aligned, bool w_words) {
   Plan p;
   p.fwd = fwd, p.bwd = bwd;
   p.t = d.n * d.hw, p.d = d.d, p.v = d.v;
@@ -698,10 +698,9 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     at += (n + 255) / 256 * 256;
     return r;
   };
-  p.few = p.t <= kFewTokens;
+  p.few = p.t <= kFewTokens && p.d >= 8;
   if (p.few) {
-    const int64_t n = bf16 ? 8 : 4;
-    p.few_wide = w_aligned && p.d % n == 0 && d.w_ld % n == 0;
+    p.few_odd = bf16 && (!w_words || p.d % 2 || d.w_ld % 2);
     if (fwd) {
       p.parts = static_cast<int>(cdiv(p.v, 128));
       p.part = take((p.parts + 1) * p.t * 8), p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
@@ -823,7 +822,7 @@ void launch_join(const Plan& p, const JoinArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((join_kernel<4>), grid, dim3(256), 0, st, a);
 }
 
-template <class S, int NT, bool WIDE>
+template <class S, int NT, bool ODD>
 pp_status enqueue_few(const Plan& p, const Call& c) {
   const pp_xent_desc& d = *c.d;
   constexpr int64_t N = 16 / sizeof(S);
@@ -835,7 +834,7 @@ pp_status enqueue_few(const Plan& p, const Call& c) {
   a.x_wide = aligned16(c.x) && d.x_sc == 1 && step % N == 0 && (d.hw == 1 || d.x_sn % N == 0);
   if (p.bwd) a.logits = f32(p.g), a.l_ld = p.vp;
   if (p.fwd) a.part = reinterpret_cast<float2*>(c.ws + p.part) + p.t, a.target_logit = f32(p.tl);
-  hipLaunchKernelGGL((few_logit_kernel<S, NT, WIDE>), dim3(static_cast<uint32_t>(cdiv(p.v, 128))), dim3(512), 0, c.st, a);
+  hipLaunchKernelGGL((few_logit_kernel<S, NT, ODD>), dim3(static_cast<uint32_t>(cdiv(p.v, 128))), dim3(512), 0, c.st, a);
   if (p.fwd) {
     const bool each = d.reduction == PP_NONE;
     double2* sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
@@ -847,10 +846,10 @@ pp_status enqueue_few(const Plan& p, const Call& c) {
     if (grid > 1) hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, c.st, loss);
   }
   if (!p.bwd) return launched();
-  a.dw = c.dw, a.dw_wide = d.d % 4 == 0 && reinterpret_cast<uintptr_t>(c.dw) % 16 == 0, a.db = c.db;
+  a.dw = c.dw, a.db = c.db;
   a.slab = c.dx ? f32(p.slab) : nullptr, a.slab_ld = p.dx_ld;
   a.splits = p.few_splits, a.groups = static_cast<int32_t>(cdiv(p.d, 256));
-  hipLaunchKernelGGL((few_grad_kernel<S, NT, WIDE>), dim3(static_cast<uint32_t>(a.splits * a.groups)), dim3(256), 0, c.st, a);
+  hipLaunchKernelGGL((few_grad_kernel<S, NT, ODD>), dim3(static_cast<uint32_t>(a.splits * a.groups)), dim3(256), 0, c.st, a);
   if (c.dx) {
     const Slab s = {a.slab, p.dx_ld, a.d, static_cast<int32_t>(p.t), a.splits,
                     {c.dx, d.dx_sc, 0, d.dx_sn, d.dx_sp, 1, a.hw,
@@ -865,7 +864,10 @@ template <class S>
 pp_status enqueue_few(const Plan& p, const Call& c) {
   auto run = [&](auto nt) {
     constexpr int NT = decltype(nt)::value;
-    return p.few_wide ? enqueue_few<S, NT, true>(p, c) : enqueue_few<S, NT, false>(p, c);
+    if constexpr (sizeof(S) == 2) {
+      if (p.few_odd) return enqueue_few<S, NT, true>(p, c);
+    }
+    return enqueue_few<S, NT, false>(p, c);
   };
   if (p.t <= 16) return run(std::integral_constant<int, 1>());
   if (p.t <= 32) return run(std::integral_constant<int, 2>());
@@ -1050,7 +1052,7 @@ pp_status xent_call(const Call& c, bool fwd, bool bwd, size_t ws_bytes) {
     return launched();
   }
   if (!fwd && !bwd) return PP_OK;
-  const Plan p = make_plan(d, fwd, bwd, bwd && c.dw, aligned16(c.x), aligned16(c.w));
+  const Plan p = make_plan(d, fwd, bwd, bwd && c.dw, aligned16(c.x), aligned16(c.w), reinterpret_cast<uintptr_t>(c.w) % 4 == 0);
   if (!c.ws || reinterpret_cast<uintptr_t>(c.ws) % 256) return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
   if (ws_bytes < p.total) return fail(PP_ESIZE, "workspace smaller than pp_xent_workspace says");
   return d.dtype == PP_BF16 ? enqueue<__bf16, 1>(p, c) : enqueue<float, 3>(p, c);
@@ -1072,7 +1074,7 @@ extern "C" pp_status pp_xent_workspace(const pp_xent_desc* desc, int32_t parts, 
     return PP_OK;
   }
   // (operands that are not 16-byte aligned are copied: what the call needs at most)
-  *bytes = make_plan(*desc, parts & 1, parts & 2, parts & 2, false, false).total;
+  *bytes = make_plan(*desc, parts & 1, parts & 2, parts & 2, false, false, false).total;
   return PP_OK;
 }
 

@@ -26,7 +26,6 @@ struct FewArgs {
   float* target_logit;
   // gradient
   void* dw;             // [v][d], or null
-  int32_t dw_wide;
   float* db;            // or null
   float* slab;          // [split][token][slab_ld], or null
   int64_t slab_ld;
@@ -35,35 +34,49 @@ struct FewArgs {
 
 constexpr uint32_t kNowhere = 0x80000000u;   // past the end of any buffer made here
 
-// N values from a buffer, at byte offset `at`; 0 past column `cols`
-template <class S, int N, bool WIDE>
-__device__ __forceinline__ auto few_load(__amdgpu_buffer_rsrc_t r, bool row, uint32_t at, int col, int cols) {
+// N values of a row of w, from byte `at` of the buffer on, which is the row's
+// column `col`.  A row's last values are fetched as its last N and moved down
+// when they are used (few_tail): nothing is read outside the rows, and columns
+// past the end count as zeros whatever is there.  Words are fetched through the
+// buffer; rows of bf16 values that do not begin at words (ODD) from memory.
+template <class S, int N, bool ODD>
+__device__ __forceinline__ auto few_load(__amdgpu_buffer_rsrc_t r, const S* rows, bool row, uint32_t at, int col, int cols) {
   using V = __attribute__((ext_vector_type(N))) S;
-  if constexpr (WIDE) {   // (cols is a multiple of N)
-    const uint32_t off = row && col < cols ? at : kNowhere;
-    if constexpr (sizeof(V) == 16)
-      return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
-    else
-      return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+  const uint32_t off = at - static_cast<uint32_t>(max(col + N - cols, 0) * static_cast<int>(sizeof(S)));
+  if constexpr (ODD) {
+    using U = __attribute__((ext_vector_type(N), aligned(2))) S;
+    V v = {};
+    if (row && col < cols) v = *reinterpret_cast<const U*>(reinterpret_cast<const uint8_t*>(rows) + off);
+    return v;
+  } else if constexpr (sizeof(V) == 16) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b128(r, row && col < cols ? off : kNowhere, 0, 0));
   } else {
-    V v;
+    return __builtin_bit_cast(V, __builtin_amdgcn_raw_buffer_load_b64(r, row && col < cols ? off : kNowhere, 0, 0));
+  }
+}
+template <class V>
+__device__ __forceinline__ V few_tail(V v, int col, int cols) {
+  constexpr int N = sizeof(V) / sizeof(v[0]);
+  const int by = max(col + N - cols, 0);
+#pragma unroll
+  for (int n = 1; n < N; n *= 2) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      const uint32_t off = row && col + e < cols ? at + e * static_cast<uint32_t>(sizeof(S)) : kNowhere;
-      if constexpr (sizeof(S) == 4)
-        v[e] = __builtin_bit_cast(S, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
-      else
-        v[e] = __builtin_bit_cast(S, __builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
+      const auto moved = e + n < N ? v[e + n < N ? e + n : 0] : static_cast<decltype(v[0] + v[0])>(0);
+      v[e] = by & n ? moved : v[e];
     }
-    return v;
   }
+  return col < cols ? v : V{};
 }
 
 // sixteen rows of w from class c on (the same in all lanes)
 template <class S>
+__device__ __forceinline__ const S* few_base(const FewArgs& a, int c) {
+  return static_cast<const S*>(a.w) + static_cast<int64_t>(c) * a.w_ld;
+}
+template <class S>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rows(const FewArgs& a, int c) {
-  const S* base = static_cast<const S*>(a.w) + static_cast<int64_t>(c) * a.w_ld;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<S*>(base), 0, static_cast<int>(16 * a.w_ld * sizeof(S)), 0x00020000);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<S*>(few_base<S>(a, c)), 0, static_cast<int>(16 * a.w_ld * sizeof(S)), 0x00020000);
 }
 
 // N channels of a token's features, 0 past the end and for an ignored token
@@ -83,7 +96,7 @@ __device__ __forceinline__ auto few_x(const FewArgs& a, int t, int c) {
 
 // The logits of 128 classes, 16 a wave, with their statistics: a stream of w
 // against the features in LDS, a chunk of the channels at a time.
-template <class S, int NT, bool WIDE>
+template <class S, int NT, bool ODD>
 __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
   constexpr int N = 16 / sizeof(S), KS = 4 * N, U = 4;
   constexpr int KC = 4096 / (NT * static_cast<int>(sizeof(S))) / (KS * U) * (KS * U);   // (64 KB)
@@ -95,13 +108,14 @@ __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c0 = blockIdx.x * 128 + wave * 16, v = a.k.v, d = a.d;
   const auto rows = few_rows<S>(a, c0);
+  const S* base = few_base<S>(a, c0);
   const bool mine = c0 + r < v;
   const uint32_t at = static_cast<uint32_t>((r * a.w_ld + N * g) * sizeof(S));
   V cur[U];
   auto load = [&](int k, V (&to)[U]) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      to[u] = few_load<S, N, WIDE>(rows, mine, at + static_cast<uint32_t>((k + u * KS) * sizeof(S)), k + u * KS + N * g, d);
+      to[u] = few_load<S, N, ODD>(rows, base, mine, at + static_cast<uint32_t>((k + u * KS) * sizeof(S)), k + u * KS + N * g, d);
   };
   load(0, cur);
   f32x4 acc[NT];
@@ -119,6 +133,10 @@ __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
     for (int k = 0; k < kn; k += KS * U) {
       V next[U];
       load(kc + k + KS * U, next);   // (nothing past the last channel)
+      if (kc + k + KS * U > d) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) cur[u] = few_tail(cur[u], kc + k + u * KS + N * g, d);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         V b[NT];
@@ -191,7 +209,7 @@ struct FewG<float, NT> {
   float by_class[64][16 * NT + 4];
 };
 
-template <class S, int NT, bool WIDE>
+template <class S, int NT, bool ODD>
 __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
   using S4 = __attribute__((ext_vector_type(4))) S;
   constexpr bool F = sizeof(S) == 4;
@@ -213,8 +231,8 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
     const auto rows = few_rows<S>(a, 16 * b);
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      to[s] = few_load<S, 4, WIDE>(rows, b < b1 && 16 * b + kS * s + kG * g < v, at + static_cast<uint32_t>(kS * s * a.w_ld * sizeof(S)),
-                                   col, d);
+      to[s] = few_load<S, 4, ODD>(rows, few_base<S>(a, 16 * b), b < b1 && 16 * b + kS * s + kG * g < v,
+                                  at + static_cast<uint32_t>(kS * s * a.w_ld * sizeof(S)), col, d);
   };
   S4 cur[4] = {};
   if (dx) load(b0, cur);
@@ -339,8 +357,9 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
           S4 o;
 #pragma unroll
           for (int f = 0; f < 4; ++f) o[f] = static_cast<S>(out[f][e] * scale);
-          if (a.dw_wide) {   // (d is a multiple of four)
-            *reinterpret_cast<S4*>(to) = o;
+          if (col + 4 <= d) {
+            using U4 = __attribute__((ext_vector_type(4), aligned(sizeof(S)))) S;
+            *reinterpret_cast<U4*>(to) = o;
           } else {
 #pragma unroll
             for (int f = 0; f < 4; ++f)
@@ -349,6 +368,10 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
         }
       }
       if (dx) {
+        if (col0 + 64 > d) {
+#pragma unroll
+          for (int s = 0; s < 4; ++s) cur[s] = few_tail(cur[s], col, d);
+        }
         if constexpr (F) {
 #pragma unroll
           for (int s = 0; s < 4; ++s)
