@@ -638,7 +638,7 @@ struct Plan {
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
   bool few = false, few_odd = false;  // few tokens: kernels of their own
-  int few_splits = 1;
+  int few_classes = 128, few_lane = 4, few_splits = 1;   // classes a workgroup; of the gradient: channels a lane, parts of the classes
   // workspace offsets
   size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
 };
@@ -698,16 +698,25 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     at += (n + 255) / 256 * 256;
     return r;
   };
-  p.few = p.t <= kFewTokens && p.d >= 8;
+  // Few tokens: where reading w is the work.  1024 channels, 50000 classes, step:
+  // fp32 1, 64, 128 tokens 125, 225, 420 us, by the products 438, 458, 646; bf16
+  // 1, 64 tokens 72, 105, by the products 146, 154.  With few classes a token the
+  // workgroups are too few: 64 tokens, 2048 channels, 1000 classes 108 us, 68.
+  p.few = p.t <= kFewTokens[bf16] && p.v >= 128 * p.t && p.d >= 8;
   if (p.few) {
+    p.few_lane = p.t <= 64 ? 4 : 2;
+    // 64 a workgroup where that leaves CUs without one (1 token, 2048 channels,
+    // 8000 classes, fp32: 33 us, with 128 39; 500 channels, 20000 classes: 22, 19)
+    p.few_classes = (!bf16 && p.t > 16) || p.v > 64 * kCUs ? 128 : 64;
+    if (!bf16 && p.t > 16) p.x_k = take(3 * p.t * p.dp * 2);
     p.few_odd = bf16 && (!w_words || p.d % 2 || d.w_ld % 2);
     if (fwd) {
-      p.parts = static_cast<int>(cdiv(p.v, 128));
+      p.parts = static_cast<int>(cdiv(p.v, p.few_classes));
       p.part = take((p.parts + 1) * p.t * 8), p.tl = take(p.t * 4), p.sums = take(cdiv(p.t, 16) * 16);
     }
     if (bwd) {
-      // two workgroups a CU, 64 classes at least
-      p.few_splits = static_cast<int>(std::max<int64_t>(1, std::min(cdiv(p.v, 64), 2 * kCUs / cdiv(p.d, 256))));
+      // two workgroups a CU, 32 classes at least
+      p.few_splits = static_cast<int>(std::max<int64_t>(1, std::min(cdiv(p.v, 32), 2 * kCUs / cdiv(p.d, 64 * p.few_lane))));
       p.dx_ld = cdiv(p.d, 4) * 4;
       p.g = take(p.t * p.vp * 4), p.slab = take(p.few_splits * p.t * p.dx_ld * 4);
     }
@@ -822,10 +831,22 @@ void launch_join(const Plan& p, const JoinArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((join_kernel<4>), grid, dim3(256), 0, st, a);
 }
 
+StageArgs stage_x(const Plan& p, const Call& c) {
+  const pp_xent_desc& d = *c.d;
+  const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
+  StageArgs a = {c.x, d.x_sn, d.x_sp, d.x_sc, static_cast<int32_t>(d.hw), static_cast<int32_t>(p.t), static_cast<int32_t>(p.d),
+                 c.target, d.ignore_index, reinterpret_cast<__bf16*>(c.ws + p.x_k), p.t * p.dp, static_cast<int32_t>(p.dp)};
+  a.along_cols = d.x_sc <= step;
+  a.wide = aligned16(c.x) && (a.along_cols ? d.x_sc == 1 && step % 8 == 0 && (d.hw == 1 || d.x_sn % 8 == 0)
+                                           : d.x_sp == 1 && d.hw % 8 == 0 && d.x_sc % 8 == 0 && d.x_sn % 8 == 0);
+  return a;
+}
+
 template <class S, int NT, bool ODD>
 pp_status enqueue_few(const Plan& p, const Call& c) {
   const pp_xent_desc& d = *c.d;
   constexpr int64_t N = 16 / sizeof(S);
+  constexpr int C = NT > 4 ? 2 : 4;
   auto f32 = [&](size_t off) { return reinterpret_cast<float*>(c.ws + off); };
   const int64_t step = d.hw == 1 ? d.x_sn : d.x_sp;
   FewArgs a = {};
@@ -834,7 +855,16 @@ pp_status enqueue_few(const Plan& p, const Call& c) {
   a.x_wide = aligned16(c.x) && d.x_sc == 1 && step % N == 0 && (d.hw == 1 || d.x_sn % N == 0);
   if (p.bwd) a.logits = f32(p.g), a.l_ld = p.vp;
   if (p.fwd) a.part = reinterpret_cast<float2*>(c.ws + p.part) + p.t, a.target_logit = f32(p.tl);
-  hipLaunchKernelGGL((few_logit_kernel<S, NT, ODD>), dim3(static_cast<uint32_t>(cdiv(p.v, 128))), dim3(512), 0, c.st, a);
+  const dim3 blocks(static_cast<uint32_t>(cdiv(p.v, p.few_classes)));
+  if constexpr (sizeof(S) == 4 && NT > 1) {
+    const StageArgs sa = stage_x(p, c);
+    stage<S, 3>(&sa, 1, c.st);
+    FewArgs b = a;
+    b.x = sa.out, b.x_sn = p.dp, b.x_sp = sa.plane;
+    hipLaunchKernelGGL((few_logit3_kernel<NT>), blocks, dim3(256), 0, c.st, b);
+  } else {
+    hipLaunchKernelGGL((few_logit_kernel<S, NT, ODD>), blocks, dim3(static_cast<uint32_t>(4 * p.few_classes)), 0, c.st, a);
+  }
   if (p.fwd) {
     const bool each = d.reduction == PP_NONE;
     double2* sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
@@ -848,8 +878,8 @@ pp_status enqueue_few(const Plan& p, const Call& c) {
   if (!p.bwd) return launched();
   a.dw = c.dw, a.db = c.db;
   a.slab = c.dx ? f32(p.slab) : nullptr, a.slab_ld = p.dx_ld;
-  a.splits = p.few_splits, a.groups = static_cast<int32_t>(cdiv(p.d, 256));
-  hipLaunchKernelGGL((few_grad_kernel<S, NT, ODD>), dim3(static_cast<uint32_t>(a.splits * a.groups)), dim3(256), 0, c.st, a);
+  a.splits = p.few_splits, a.groups = static_cast<int32_t>(cdiv(p.d, 64 * C));
+  hipLaunchKernelGGL((few_grad_kernel<S, NT, C, ODD>), dim3(static_cast<uint32_t>(a.splits * a.groups)), dim3(256), 0, c.st, a);
   if (c.dx) {
     const Slab s = {a.slab, p.dx_ld, a.d, static_cast<int32_t>(p.t), a.splits,
                     {c.dx, d.dx_sc, 0, d.dx_sn, d.dx_sp, 1, a.hw,
@@ -872,6 +902,10 @@ pp_status enqueue_few(const Plan& p, const Call& c) {
   if (p.t <= 16) return run(std::integral_constant<int, 1>());
   if (p.t <= 32) return run(std::integral_constant<int, 2>());
   if (p.t <= 48) return run(std::integral_constant<int, 3>());
+  if constexpr (sizeof(S) == 4) {
+    if (p.t > 96) return run(std::integral_constant<int, 8>());
+    if (p.t > 64) return run(std::integral_constant<int, 6>());
+  }
   return run(std::integral_constant<int, 4>());
 }
 
@@ -891,14 +925,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
   const GemmOperand w = p.w_direct ? operand(c.w, 0, d.w_ld, p.v, p.dp, 1) : operand(bf(p.w_k), p.v * p.dp, p.dp, p.v, p.dp, P);
   StageArgs staged[2];
   int copies = 0;
-  if (!p.x_direct) {
-    StageArgs a = {c.x, d.x_sn, d.x_sp, d.x_sc, static_cast<int32_t>(d.hw), static_cast<int32_t>(p.t), static_cast<int32_t>(p.d),
-                   c.target, d.ignore_index, bf(p.x_k), p.t * p.dp, static_cast<int32_t>(p.dp)};
-    a.along_cols = d.x_sc <= step;
-    a.wide = aligned16(c.x) && (a.along_cols ? d.x_sc == 1 && step % 8 == 0 && (d.hw == 1 || d.x_sn % 8 == 0)
-                                             : d.x_sp == 1 && d.hw % 8 == 0 && d.x_sc % 8 == 0 && d.x_sn % 8 == 0);
-    staged[copies++] = a;
-  }
+  if (!p.x_direct) staged[copies++] = stage_x(p, c);
   if (!p.w_direct) {
     StageArgs a = {c.w, d.w_ld, 0, 1, 1, static_cast<int32_t>(p.v), static_cast<int32_t>(p.d), nullptr, 0,
                    bf(p.w_k), p.v * p.dp, static_cast<int32_t>(p.dp)};

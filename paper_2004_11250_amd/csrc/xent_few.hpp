@@ -9,7 +9,7 @@
 // values are multiplied in fp32: at these sizes its rate is enough.
 // (Included by xent.hip, inside its namespace.)
 
-constexpr int kFewTokens = 64;
+constexpr int kFewTokens[2] = {128, 64};   // fp32, bf16
 
 struct FewArgs {
   const void* w;        // [v][w_ld]
@@ -22,14 +22,14 @@ struct FewArgs {
   int64_t l_ld;
   // forward
   const float* bias;
-  float2* part;         // [128 classes][token], or null
+  float2* part;         // [workgroup][token], or null
   float* target_logit;
   // gradient
   void* dw;             // [v][d], or null
   float* db;            // or null
   float* slab;          // [split][token][slab_ld], or null
   int64_t slab_ld;
-  int32_t splits, groups;   // of the classes; of the channels (256 each)
+  int32_t splits, groups;   // of the classes; of the channels (64 C each)
 };
 
 constexpr uint32_t kNowhere = 0x80000000u;   // past the end of any buffer made here
@@ -79,14 +79,19 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t few_rows(const FewArgs& a, int
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<S*>(few_base<S>(a, c)), 0, static_cast<int>(16 * a.w_ld * sizeof(S)), 0x00020000);
 }
 
-// N channels of a token's features, 0 past the end and for an ignored token
+// A token's features: their offset, or -1 for one that is ignored or past the end
+__device__ __forceinline__ int64_t few_token(const FewArgs& a, int t) {
+  if (t >= a.k.t || a.k.target[t] == a.k.ignore) return -1;
+  const int hi = t / a.hw;
+  return hi * a.x_sn + (t - hi * a.hw) * a.x_sp;
+}
+// N channels of them, 0 past the end
 template <class S, int N>
-__device__ __forceinline__ auto few_x(const FewArgs& a, int t, int c) {
+__device__ __forceinline__ auto few_x(const FewArgs& a, int64_t token, int c) {
   using V = __attribute__((ext_vector_type(N))) S;
   V v = {};
-  if (t >= a.k.t || c >= a.d || a.k.target[t] == a.k.ignore) return v;
-  const int hi = t / a.hw;
-  const S* at = static_cast<const S*>(a.x) + hi * a.x_sn + (t - hi * a.hw) * a.x_sp + c * a.x_sc;
+  if (token < 0 || c >= a.d) return v;
+  const S* at = static_cast<const S*>(a.x) + token + c * a.x_sc;
   if (a.x_wide && c + N <= a.d) return *reinterpret_cast<const V*>(at);
 #pragma unroll
   for (int e = 0; e < N; ++e)
@@ -94,8 +99,54 @@ __device__ __forceinline__ auto few_x(const FewArgs& a, int t, int c) {
   return v;
 }
 
-// The logits of 128 classes, 16 a wave, with their statistics: a stream of w
-// against the features in LDS, a chunk of the channels at a time.
+// Sixteen classes' logits: lane (r, g) has the classes c .. c + 3, c = c0 + 4 g,
+// of the tokens 16 j + r.  Bias, the logits' store, and the maximum and sum of
+// each token, to red[token].
+template <int NT>
+__device__ __forceinline__ void few_logits_out(const FewArgs& a, f32x4 (&acc)[NT], int c, float2* red) {
+  const int r = threadIdx.x & 15, v = a.k.v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float bias = a.bias && c + e < v ? a.bias[c + e] : 0.f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[j][e] = c + e < v ? acc[j][e] + bias : -INFINITY;
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int t = 16 * j + r;
+    if (t < a.k.t && a.logits && c < a.l_ld) *reinterpret_cast<f32x4*>(a.logits + t * a.l_ld + c) = acc[j];
+    if (!a.part) continue;
+    float m = fmaxf(fmaxf(acc[j][0], acc[j][1]), fmaxf(acc[j][2], acc[j][3]));
+    m = fmaxf(m, __shfl_xor(m, 16));
+    m = fmaxf(m, __shfl_xor(m, 32));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s += fast_exp(acc[j][e] - ref);
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if ((threadIdx.x & 48) == 0) red[t] = make_float2(m, s);
+    const int64_t y = t < a.k.t ? a.k.target[t] : -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (y == c + e && c + e < v) a.target_logit[t] = acc[j][e];
+  }
+}
+
+// the sixteens of a workgroup joined
+template <int NT>
+__device__ __forceinline__ void few_part_out(const FewArgs& a, float2 (*red)[16 * NT], int n) {
+  if (!a.part) return;
+  __syncthreads();
+  const int t = threadIdx.x;
+  if (t >= a.k.t) return;
+  float2 s = red[0][t];
+  for (int w = 1; w < n; ++w) s = join(s, red[w][t]);
+  a.part[static_cast<int64_t>(blockIdx.x) * a.k.t + t] = s;
+}
+
+// The logits of 128 or 64 classes, 16 a wave, with their statistics: a stream of
+// w against the features in LDS, a chunk of the channels at a time.
 template <class S, int NT, bool ODD>
 __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
   constexpr int N = 16 / sizeof(S), KS = 4 * N, U = 4;
@@ -106,7 +157,7 @@ __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
   __shared__ __align__(16) S xs[16 * NT][KC + N];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int c0 = blockIdx.x * 128 + wave * 16, v = a.k.v, d = a.d;
+  const int threads = blockDim.x, c0 = blockIdx.x * (threads / 4) + wave * 16, v = a.k.v, d = a.d;
   const auto rows = few_rows<S>(a, c0);
   const S* base = few_base<S>(a, c0);
   const bool mine = c0 + r < v;
@@ -118,6 +169,9 @@ __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
       to[u] = few_load<S, N, ODD>(rows, base, mine, at + static_cast<uint32_t>((k + u * KS) * sizeof(S)), k + u * KS + N * g, d);
   };
   load(0, cur);
+  __shared__ int64_t token[16 * NT];
+  if (tid < 16 * NT) token[tid] = few_token(a, tid);
+  __syncthreads();
   f32x4 acc[NT];
 #pragma unroll
   for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -125,9 +179,19 @@ __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
   for (int kc = 0; kc < d; kc += KC) {
     const int kn = min(KC, (d - kc + KS * U - 1) / (KS * U) * (KS * U));
     if (kc) __syncthreads();
-    for (int i = tid; i < kn / N * 16 * NT; i += 512) {
-      const int t = along ? i / (kn / N) : i % (16 * NT), k = (along ? i % (kn / N) : i / (16 * NT)) * N;
-      *reinterpret_cast<V*>(&xs[t][k]) = few_x<S, N>(a, t, kc + k);
+    // (four pieces at a time, all fetched before the first is put away)
+    const int row = kn / N, all = row * 16 * NT;
+    for (int i0 = tid; i0 < all; i0 += 4 * threads) {
+      V got[4];
+      int t[4], k[4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int i = min(i0 + n * threads, all - 1);
+        t[n] = along ? i / row : i % (16 * NT), k[n] = (along ? i - t[n] * row : i / (16 * NT)) * N;
+        got[n] = few_x<S, N>(a, token[t[n]], kc + k[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) *reinterpret_cast<V*>(&xs[t[n]][k[n]]) = got[n];
     }
     __syncthreads();
     for (int k = 0; k < kn; k += KS * U) {
@@ -156,46 +220,127 @@ __global__ __launch_bounds__(512) void few_logit_kernel(FewArgs a) {
       for (int u = 0; u < U; ++u) cur[u] = next[u];
     }
   }
-  // lane (r, g) has the classes c0 + 4 g + 0..3 of the tokens 16 j + r
-  const int c = c0 + 4 * g;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float bias = a.bias && c + e < v ? a.bias[c + e] : 0.f;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[j][e] = c + e < v ? acc[j][e] + bias : -INFINITY;
-  }
   __syncthreads();
-  float2(*red)[16 * NT] = reinterpret_cast<float2(*)[16 * NT]>(&xs[0][0]);   // [wave][token]
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int t = 16 * j + r;
-    if (t < a.k.t && a.logits && c < a.l_ld) *reinterpret_cast<f32x4*>(a.logits + t * a.l_ld + c) = acc[j];
-    if (!a.part) continue;
-    float m = fmaxf(fmaxf(acc[j][0], acc[j][1]), fmaxf(acc[j][2], acc[j][3]));
-    m = fmaxf(m, __shfl_xor(m, 16));
-    m = fmaxf(m, __shfl_xor(m, 32));
-    const float ref = m == -INFINITY ? 0.f : m;
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s += fast_exp(acc[j][e] - ref);
-    s += __shfl_xor(s, 16);
-    s += __shfl_xor(s, 32);
-    if (g == 0) red[wave][t] = make_float2(m, s);
-    const int64_t y = t < a.k.t ? a.k.target[t] : -1;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (y == c + e && c + e < v) a.target_logit[t] = acc[j][e];
-  }
-  if (!a.part) return;
-  __syncthreads();
-  if (tid >= a.k.t) return;
-  float2 s = red[0][tid];
-#pragma unroll
-  for (int w = 1; w < 8; ++w) s = join(s, red[w][tid]);
-  a.part[static_cast<int64_t>(blockIdx.x) * a.k.t + tid] = s;
+  float2(*red)[16 * NT] = reinterpret_cast<float2(*)[16 * NT]>(&xs[0][0]);
+  few_logits_out<NT>(a, acc, c0 + 4 * g, red[wave]);
+  few_part_out<NT>(a, red, threads / 64);
 }
 
-// G of 64 classes at a time in LDS; each wave has 64 channels, for which it adds
+// The same for fp32 and more tokens, where the fp32 instructions' rate would be
+// the bound: w's values are split into three of bf16 as they come, x's were
+// before (x: its planes, x_sn apart a token, x_sp a plane), and six products of
+// them are summed.  32 classes a wave.
+template <int NT>
+__global__ __launch_bounds__(256, 2) void few_logit3_kernel(FewArgs a) {
+  constexpr int U = 2, KS = 32, KC = 512 / NT / (KS * U) * (KS * U);
+  __shared__ __align__(16) __bf16 xs[3][16 * NT][KC + 8];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c0 = blockIdx.x * 128 + wave * 32, v = a.k.v, d = a.d;
+  const float* base = few_base<float>(a, c0);
+  const auto rows = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base), 0, static_cast<int>(32 * a.w_ld * 4), 0x00020000);
+  f32x4 cur[U][2][2];   // [step][sixteen classes][half]
+  auto load = [&](int k, f32x4 (&to)[U][2][2]) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int col = k + u * KS + 8 * g + 4 * h;
+          to[u][i][h] = few_load<float, 4, false>(rows, base, c0 + 16 * i + r < v, static_cast<uint32_t>(((16 * i + r) * a.w_ld + col) * 4), col, d);
+        }
+  };
+  load(0, cur);
+  f32x4 acc[2][NT];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const __bf16* x = static_cast<const __bf16*>(a.x);
+  const int dp = (d + 63) / 64 * 64;
+  // x's next chunk, fetched during a chunk
+  constexpr int PIECES = 3 * 16 * NT * (KC / 8) / 256;
+  static_assert(3 * 16 * NT * (KC / 8) % 256 == 0);
+  bf16x8 ahead[PIECES];
+  auto fetch = [&](int kc) {
+#pragma unroll
+    for (int n = 0; n < PIECES; ++n) {
+      const int i = n * 256 + tid, row = i / (KC / 8), k = kc + i % (KC / 8) * 8, p = row / (16 * NT), t = row % (16 * NT);
+      ahead[n] = bf16x8{};
+      if (t < a.k.t && k < dp) ahead[n] = *reinterpret_cast<const bf16x8*>(x + p * a.x_sp + t * a.x_sn + k);
+    }
+  };
+  fetch(0);
+  for (int kc = 0; kc < dp; kc += KC) {
+    const int kn = min(KC, dp - kc);
+    if (kc) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < PIECES; ++n) {
+      const int i = n * 256 + tid, row = i / (KC / 8);
+      *reinterpret_cast<bf16x8*>(&xs[row / (16 * NT)][row % (16 * NT)][i % (KC / 8) * 8]) = ahead[n];
+    }
+    __syncthreads();
+    fetch(kc + KC);
+    for (int k = 0; k < kn; k += KS * U) {
+      f32x4 next[U][2][2];
+      load(kc + k + KS * U, next);   // (nothing past the last channel)
+      if (kc + k + KS * U > d) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) cur[u][i][h] = few_tail(cur[u][i][h], kc + k + u * KS + 8 * g + 4 * h, d);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        bf16x8 w[2][3];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            __bf16 q[3];
+            bf16_planes<3>(cur[u][i][e / 4][e % 4], q);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) w[i][p][e] = q[p];
+          }
+        // (two sixteens of tokens in turn: four sums, so that none waits for itself)
+#pragma unroll
+        for (int j0 = 0; j0 < NT; j0 += 2) {
+          bf16x8 b[2][3];
+#pragma unroll
+          for (int j = j0; j < NT && j < j0 + 2; ++j)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) b[j - j0][p] = *reinterpret_cast<const bf16x8*>(&xs[p][16 * j + r][k + u * KS + 8 * g]);
+          // (the smallest products first)
+#pragma unroll
+          for (int p = 2; p >= 0; --p)
+#pragma unroll
+            for (int q = 0; q <= p; ++q)
+#pragma unroll
+              for (int j = j0; j < NT && j < j0 + 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                  acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i][q], b[j - j0][p - q], acc[i][j], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) cur[u][i][h] = next[u][i][h];
+    }
+  }
+  __syncthreads();
+  float2(*red)[16 * NT] = reinterpret_cast<float2(*)[16 * NT]>(&xs[0][0][0]);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) few_logits_out<NT>(a, acc[i], c0 + 16 * i + 4 * g, red[2 * wave + i]);
+  few_part_out<NT>(a, red, 8);
+}
+
+// G of 64 classes at a time in LDS; each wave has 16 C channels, for which it adds
 // G w to dx's sums in registers and stores G^T x.  bf16 operands: G is rounded
 // to bf16 (db is summed before), a lane gives four tokens or classes to one
 // instruction, and the four channels that it loads of each of four classes are
@@ -209,16 +354,18 @@ struct FewG<float, NT> {
   float by_class[64][16 * NT + 4];
 };
 
-template <class S, int NT, bool ODD>
+template <class S, int NT, int C, bool ODD>
 __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
   using S4 = __attribute__((ext_vector_type(4))) S;
+  using SC = __attribute__((ext_vector_type(C))) S;
+  static_assert(C == 4 || sizeof(S) == 4);
   constexpr bool F = sizeof(S) == 4;
   __shared__ __align__(16) FewG<S, NT> gs[2];
   __shared__ float db_part[2][4][64];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int group = blockIdx.x % a.groups, split = blockIdx.x / a.groups;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col0 = group * 256 + wave * 64, col = col0 + 4 * r, v = a.k.v, d = a.d;
+  const int col0 = (group * 4 + wave) * 16 * C, col = col0 + C * r, v = a.k.v, d = a.d;
   const bool on = col0 < d, dx = a.slab && on, dw = a.dw && on, db = a.db && group == 0;
   const int blocks = (v + 15) / 16;
   const int b0 = static_cast<int>(static_cast<int64_t>(blocks) * split / a.splits);
@@ -227,14 +374,14 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
   // a lane's class of load s: 4 s + g, bf16 4 g + s
   constexpr int kG = F ? 1 : 4, kS = F ? 4 : 1;
   const uint32_t at = static_cast<uint32_t>((kG * g * a.w_ld + col) * sizeof(S));
-  auto load = [&](int b, S4 (&to)[4]) {
+  auto load = [&](int b, SC (&to)[4]) {
     const auto rows = few_rows<S>(a, 16 * b);
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      to[s] = few_load<S, 4, ODD>(rows, few_base<S>(a, 16 * b), b < b1 && 16 * b + kS * s + kG * g < v,
+      to[s] = few_load<S, C, ODD>(rows, few_base<S>(a, 16 * b), b < b1 && 16 * b + kS * s + kG * g < v,
                                   at + static_cast<uint32_t>(kS * s * a.w_ld * sizeof(S)), col, d);
   };
-  S4 cur[4] = {};
+  SC cur[4] = {};
   if (dx) load(b0, cur);
   // this thread's part of G: classes 4 q + 0..3 of a chunk, the tokens t0 + 16 i
   const int q = tid & 15, t0 = tid >> 4;
@@ -262,14 +409,14 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
   };
   fetch(b0);
   // x: a lane's four channels of the tokens 16 i + 4 s + g, bf16 16 i + 4 g + s
-  S4 x[NT][4];
+  SC x[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) x[i][s] = dw ? few_x<S, 4>(a, 16 * i + kS * s + kG * g, col) : S4{};
+    for (int s = 0; s < 4; ++s) x[i][s] = dw ? few_x<S, C>(a, few_token(a, 16 * i + kS * s + kG * g), col) : SC{};
   }
   // four values of each of four rows -> of each of four columns
-  auto turn = [](const S4 (&u)[4], S4 (&to)[4]) {
+  [[maybe_unused]] auto turn = [](const auto (&u)[4], S4 (&to)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) to[e] = S4{u[0][e], u[1][e], u[2][e], u[3][e]};
   };
@@ -282,13 +429,13 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
       for (int e = 0; e < 4; ++e) x[i][e] = to[e];
     }
   }
-  f32x4 sum[NT][4];
+  f32x4 sum[NT][C];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[j][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < C; ++e) sum[j][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   using I4 = __attribute__((ext_vector_type(4))) short;
-  auto product = [](auto m, auto n, f32x4 c) {
+  [[maybe_unused]] auto product = [](auto m, auto n, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(I4, m), __builtin_bit_cast(I4, n), c, 0, 0, 0);
   };
 
@@ -328,12 +475,12 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       if (b + n >= b1) break;
-      S4 next[4] = {};
+      SC next[4] = {};
       if (dx) load(b + n + 1, next);
       if (dw) {
-        f32x4 out[4];
+        f32x4 out[C];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < C; ++e) out[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
           if constexpr (F) {
@@ -341,12 +488,12 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
             for (int s = 0; s < 4; ++s) {
               const float m = now.by_class[16 * n + r][16 * i + 4 * s + g];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) out[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(m, x[i][s][e], out[e], 0, 0, 0);
+              for (int e = 0; e < C; ++e) out[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(m, x[i][s][e], out[e], 0, 0, 0);
             }
           } else {
             const S4 m = *reinterpret_cast<const S4*>(&now.by_class[16 * n + r][16 * i + 4 * g]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) out[e] = product(m, x[i][e], out[e]);
+            for (int e = 0; e < C; ++e) out[e] = product(m, x[i][e], out[e]);
           }
         }
 #pragma unroll
@@ -354,21 +501,21 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
           const int c = 16 * (b + n) + 4 * g + e;
           if (c >= v || col >= d) continue;
           S* to = static_cast<S*>(a.dw) + static_cast<int64_t>(c) * d + col;
-          S4 o;
+          SC o;
 #pragma unroll
-          for (int f = 0; f < 4; ++f) o[f] = static_cast<S>(out[f][e] * scale);
-          if (col + 4 <= d) {
-            using U4 = __attribute__((ext_vector_type(4), aligned(sizeof(S)))) S;
-            *reinterpret_cast<U4*>(to) = o;
+          for (int f = 0; f < C; ++f) o[f] = static_cast<S>(out[f][e] * scale);
+          if (col + C <= d) {
+            using U = __attribute__((ext_vector_type(C), aligned(sizeof(S)))) S;
+            *reinterpret_cast<U*>(to) = o;
           } else {
 #pragma unroll
-            for (int f = 0; f < 4; ++f)
+            for (int f = 0; f < C; ++f)
               if (col + f < d) to[f] = o[f];
           }
         }
       }
       if (dx) {
-        if (col0 + 64 > d) {
+        if (col0 + 16 * C > d) {
 #pragma unroll
           for (int s = 0; s < 4; ++s) cur[s] = few_tail(cur[s], col, d);
         }
@@ -379,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
             for (int j = 0; j < NT; ++j) {
               const float m = now.by_class[16 * n + 4 * s + g][16 * j + r];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) sum[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(m, cur[s][e], sum[j][e], 0, 0, 0);
+              for (int e = 0; e < C; ++e) sum[j][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(m, cur[s][e], sum[j][e], 0, 0, 0);
             }
         } else {
           S4 w[4];
@@ -388,7 +535,7 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
           for (int j = 0; j < NT; ++j) {
             const S4 m = *reinterpret_cast<const S4*>(&now.by_token[16 * j + r][16 * n + 4 * g]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum[j][e] = product(m, w[e], sum[j][e]);
+            for (int e = 0; e < C; ++e) sum[j][e] = product(m, w[e], sum[j][e]);
           }
         }
       }
@@ -402,9 +549,11 @@ __global__ __launch_bounds__(256, 2) void few_grad_kernel(FewArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int t = 16 * j + 4 * g + e;
-      if (t < a.k.t)
-        *reinterpret_cast<f32x4*>(a.slab + (static_cast<int64_t>(split) * a.k.t + t) * a.slab_ld + col) =
-            f32x4{sum[j][0][e], sum[j][1][e], sum[j][2][e], sum[j][3][e]};
+      if (t >= a.k.t) continue;
+      __attribute__((ext_vector_type(C))) float o;
+#pragma unroll
+      for (int f = 0; f < C; ++f) o[f] = sum[j][f][e];
+      *reinterpret_cast<decltype(o)*>(a.slab + (static_cast<int64_t>(split) * a.k.t + t) * a.slab_ld + col) = o;
     }
 }
 

@@ -1,4 +1,4 @@
-"""The head of few tokens (up to 64, whose kernels read w where it lies):
+"""The head of few tokens (up to 64, in fp32 128, whose kernels read w where it lies):
 token counts around the kernels' sixteens, odd channels and classes, rows of w
 inside wider and misaligned ones.  Error bounds as for any number of tokens."""
 import pytest
@@ -11,29 +11,30 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 32, 33, 48, 49, 64, 65])
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 32, 33, 48, 49, 64, 65, 96, 97, 128, 129])
 def test_token_counts(dtype, n):
     check(n, n, 72, 1, 130, dtype, layout="tokens", weighted=n % 2 == 0, reduction="none" if n % 3 == 0 else "mean")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [7, 8, 9, 10, 11, 12, 63, 66, 129, 255, 256, 257, 1030])
-@pytest.mark.parametrize("n,v", [(3, 1), (20, 17), (64, 1000)])
+@pytest.mark.parametrize("n,v", [(3, 1), (20, 17), (64, 1000), (90, 300), (128, 515)])
 def test_channels_and_classes(dtype, d, n, v):
     check(d, n, d, 1, v, dtype, layout="tokens")
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("images", [3, 8])
 @pytest.mark.parametrize("layout", ["first", "last", "rows", "slice"])
-def test_layouts(dtype, layout):
-    n, hw = (30, 1) if layout == "rows" else (3, 13)
+def test_layouts(dtype, images, layout):
+    n, hw = (10 * images, 1) if layout == "rows" else (images, 13)
     check(5, n, 100, hw, 313, dtype, layout=layout, ignored=0.3)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d,left,pitch", [(64, 0, 64), (64, 1, 67), (64, 2, 68), (37, 3, 41), (38, 2, 46), (40, 8, 56)])
 def test_rows_of_w(dtype, d, left, pitch):
-    n, v = 21, 150
+    n, v = {"f32": 101, "bf16": 21}[dtype], 150
     x, w, t, b, cw, gr = make(6, n, d, 1, v, dtype, layout="tokens")
     wide = torch.full((v, pitch), float("nan"), device="cuda", dtype=DT[dtype])
     wide[:, left:left + d] = w
