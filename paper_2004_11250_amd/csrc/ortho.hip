@@ -738,7 +738,8 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     m.wide = m.g ? aligned16(m.g) && aligned16(m.w) && aligned16(m.w_out) && aligned16(m.mom) && aligned16(m.mom_out)
                  : piece(m.u, m.u_rs);
     m.o_wide = piece(m.o, m.o_rs);
-    m.chunk = static_cast<int32_t>(std::max<int64_t>(4096, cdiv(cdiv(all, 256), 256) * 256));
+    // (at most 1024, whose sums each workgroup of the next kernel adds up)
+    m.chunk = static_cast<int32_t>(std::max<int64_t>(4096, cdiv(cdiv(all, 1024), 2048) * 2048));
     m.chunks = static_cast<int32_t>(cdiv(all, m.chunk));
     (tiny_fits(m.m, m.n) ? p->tiny : p->mats).push_back(m);
   }
