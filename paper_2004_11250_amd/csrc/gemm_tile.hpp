@@ -146,7 +146,7 @@ struct GemmTile {
   static constexpr uint32_t PLANE_A = BM * kBK * 2, PLANE_B = BN * kBK * 2, LDS_A = NP * PLANE_A, LDS_STEP = NP * (PLANE_A + PLANE_B);
   static constexpr uint32_t LDS_RING = STAGES * LDS_STEP, LDS_BYTES = WK * LDS_RING;
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0 && TM % 16 == 0 && TN % 16 == 0, "tile");
-  static_assert((FM & (FM - 1)) == 0 && (FN & (FN - 1)) == 0 && FM <= 8 && FN <= 8, "blocks");
+  static_assert((!AR || (FM & (FM - 1)) == 0) && (!BR || (FN & (FN - 1)) == 0) && FM <= 8 && FN <= 8, "blocks");
 
   // Row and column of acc[i][j][e] in the tile.  A lane holds four rows that
   // follow each other of one column.
@@ -487,7 +487,7 @@ struct GemmTile {
   // rows (a lane holds four rows of a column, too short a piece for either).  Each wave has a region of its own, of CR x CC values; f(row,
   // col, View) is called for each CR x CC part of the wave's tile, whose first
   // element is (row, col) of the workgroup's tile.
-  static constexpr int CR = TM < 64 ? TM : 64, CC = TN;
+  static constexpr int CR = TM % 64 == 0 ? 64 : TM % 32 == 0 ? 32 : 16, CC = TN;
   // pieces of eight values a lane takes (a small part has work for SHARERS
   // groups only)
   static constexpr int SHARERS = CR * CC / 512 < WK ? CR * CC / 512 : WK, PIECES = CR * CC / 512 / SHARERS;

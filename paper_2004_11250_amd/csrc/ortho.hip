@@ -438,9 +438,9 @@ __global__ __launch_bounds__(Tile::THREADS) void gram_kernel(Table t, Step s, Pl
       split8(v, &h, &l);
       const int64_t at = static_cast<int64_t>(rb + r) * mp + cb + c;
       *reinterpret_cast<f16x8*>(out + at) = h;
-      // (else only this half's rests that share a tile of the next product with
-      // the diagonal are read)
-      if (P > 1 || (!POLY && (rb + r) / tile_m(1, kBig) == (cb + c) / tile_m(1, kBig)))
+      // (else only this half's rests that may share a tile of the next product
+      // with the diagonal are read)
+      if (P > 1 || (!POLY && abs(rb + r - cb - c) < tile_m(1, kBig)))
         *reinterpret_cast<f16x8*>(out + at + plane) = l;
     }
   });
@@ -703,10 +703,10 @@ struct Plan {
 // The tile that takes the least modelled time for a stage over all matrices;
 // tiles(m, edge) and steps(m) of each.
 template <class F, class G>
-int pick(int np, const std::vector<Mat>& mats, F&& tiles, G&& steps) {
+int pick(int np, int kinds, const std::vector<Mat>& mats, F&& tiles, G&& steps) {
   int best = kSmall;
   double least = 1e300;
-  for (int k = 0; k < kTiles; ++k) {
+  for (int k = 0; k < kinds; ++k) {
     double n = 0., work = 0., most = 0.;
     for (const Mat& m : mats) {
       const double t = static_cast<double>(tiles(m, tile_m(np, k))), s = steps(m);
@@ -747,9 +747,9 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
   std::stable_sort(p->mats.begin(), p->mats.end(), [](const Mat& a, const Mat& b) { return a.n > b.n; });
   auto tri = [](const Mat& m, int t) { const int64_t k = cdiv(m.mp, t); return k * (k + 1) / 2; };   // (the padding is written too)
   auto rect = [](const Mat& m, int t) { return cdiv(m.np, t) * cdiv(m.m, t); };
-  p->gram = pick(planes, p->mats, tri, [](const Mat& m) { return m.np / 64; });
-  p->poly = pick(planes, p->mats, tri, [](const Mat& m) { return m.mp / 64; });
-  p->apply = pick(planes, p->mats, rect, [](const Mat& m) { return m.mp / 64; });
+  p->gram = pick(planes, kTiles, p->mats, tri, [](const Mat& m) { return m.np / 64; });
+  p->poly = pick(planes, kTiles, p->mats, tri, [](const Mat& m) { return m.mp / 64; });
+  p->apply = pick(planes, kFit, p->mats, rect, [](const Mat& m) { return m.mp / 64; });
   for (Mat& m : p->mats) {
     const int64_t n[kStages] = {m.chunks, static_cast<int64_t>(m.mp / 64) * (m.np / 64), tri(m, tile_m(planes, p->gram)),
                                 tri(m, tile_m(planes, p->poly)), rect(m, tile_m(planes, p->apply))};
