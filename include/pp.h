@@ -508,8 +508,10 @@ enum { PP_XENT_FWD = 1, PP_XENT_BWD = 2 };               /* parts of pp_xent_wor
  * neither ignore_index nor in 0..v-1 makes the loss (PP_NONE: its own) and the
  * gradients it reaches NaN.  A class whose logits are -inf (a bias of -inf)
  * has probability 0; a token all of whose logits are -inf has loss NaN.
- * The logits are accumulated in fp32 and are neither rounded nor stored; fp32
- * features are multiplied as sums of three bf16 values each (24 bits).
+ * The logits are accumulated in fp32 and not rounded.  They are not stored,
+ * except those of few tokens (64, in fp32 128) by a call that computes
+ * gradients, in the workspace.  fp32 features are multiplied in fp32 (few
+ * tokens) or as sums of three bf16 values each (24 bits).
  */
 typedef struct {
   int32_t dtype;                       /* pp_dtype of x, w, dx and dw                 */
@@ -544,7 +546,8 @@ typedef struct {
  * pp_xent_step -- both in one call, sharing what they prepare of x and w.
  *
  * The backward pass rounds the logits' gradient to bf16 (bf16 features) or to
- * 24 bits (fp32) for the products with w and x, and sums in fp32.
+ * 24 bits (fp32; few tokens: not) for the products with w and x, and sums in
+ * fp32.
  * n hw = 0 is a loss of 0 and zero gradients.
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, reduction, dtype,
  * negative strides), PP_EUNSUPPORTED (d, v or the tokens 2^22 - 64 or more, x or
