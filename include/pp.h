@@ -509,8 +509,8 @@ enum { PP_XENT_FWD = 1, PP_XENT_BWD = 2 };               /* parts of pp_xent_wor
  * gradients it reaches NaN.  A class whose logits are -inf (a bias of -inf)
  * has probability 0; a token all of whose logits are -inf has loss NaN.
  * The logits are accumulated in fp32 and not rounded.  They are not stored,
- * except those of few tokens (64, in fp32 128) by a call that computes
- * gradients, in the workspace.  fp32 features are multiplied in fp32 (few
+ * except in the workspace, up to 512 MB: those of few tokens (64, in fp32 128)
+ * by a call that computes gradients, and in fp32 by pp_xent_step.  fp32 features are multiplied in fp32 (few
  * tokens) or as sums of three bf16 values each (24 bits).
  */
 typedef struct {
@@ -526,7 +526,7 @@ typedef struct {
 /*
  * pp_xent_workspace -- device bytes a call needs (parts: PP_XENT_FWD for
  * pp_xent_fwd, PP_XENT_BWD for pp_xent_bwd, both for pp_xent_step), which do
- * not grow with v times the tokens beyond about 0.6 GB.  Host-only.
+ * not grow with v times the tokens beyond about 1.1 GB.  Host-only.
  *
  * pp_xent_fwd -- the loss, and the statistics pp_xent_bwd needs.
  *   x, w          device [n][d][hw] (by strides) and [v][d] (rows w_ld apart)

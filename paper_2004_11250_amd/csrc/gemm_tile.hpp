@@ -491,7 +491,8 @@ struct GemmTile {
   // pieces of eight values a lane takes (a small part has work for SHARERS
   // groups only)
   static constexpr int SHARERS = CR * CC / 512 < WK ? CR * CC / 512 : WK, PIECES = CR * CC / 512 / SHARERS;
-  static_assert(CC <= 64 && CR * CC * 4 * NW * WK <= static_cast<int>(LDS_BYTES) && (WK == 1 || TM <= 64), "staging area");
+  static constexpr uint32_t STAGING = CR * CC * 4 * NW * WK;   // bytes of LDS
+  static_assert(CC <= 64 && STAGING <= LDS_BYTES && (WK == 1 || TM <= 64), "staging area");
   struct View {
     float* at;
     // Element (r, c): columns one after the other, rows in groups of four

@@ -1,6 +1,6 @@
 // xent.hip -- pp_xent_fwd / pp_xent_bwd / pp_xent_step: softmax cross entropy
 // of a linear (1x1) head over a large number of classes, with its gradient,
-// without keeping the logits.
+// without keeping the logits where they are many.
 //
 //   l[t][v] = x[t] . w[v] + b[v],  lse[t] = log sum_v exp l[t][v]
 //   loss[t] = c[y] (lse[t] - l[t][y]),            y = target[t]
@@ -10,8 +10,8 @@
 // Forward: the logits are a product on the matrix cores whose tiles never
 // leave the registers: each wave reduces its tile to a maximum and a sum of
 // exponentials per token (a few bytes per token and 64 to 128 classes), and a
-// second kernel joins those.  Backward: the logits are computed again, a
-// piece of the classes at a time, turned into G in the epilogue (the logits
+// second kernel joins those.  Backward: the logits are computed again (a step
+// in fp32 may keep them), a piece of the classes at a time, turned into G in the epilogue (the logits
 // themselves are not rounded), rounded to the operands' type and stored; then
 // the two products, one over classes and one over tokens.  The piece bounds
 // what the workspace holds.  (Few tokens: xent_few.hpp.)
@@ -213,6 +213,8 @@ struct LogitArgs {
   int32_t v0;
   const float* bias;
   Tokens k;
+  float* logits;           // [token][l_ld], without the bias: kept, or taken from there; or null
+  int64_t l_ld;
   // statistics
   float2* part;            // [class part][token]: maximum, sum of exp(l - maximum)
   float* target_logit;     // [token]
@@ -240,9 +242,13 @@ __device__ __forceinline__ float sum16(float v) {
 // 1.25 PFLOP/s; G of 8192 tokens, 16384 classes: 290 us, 0.95 PFLOP/s, of which
 // G's store through LDS takes 45.  Sums of a few steps are short of that: fp32,
 // 8192 tokens, 313 classes, 256 channels, six products: 18 us, 0.45 PFLOP/s.
-template <class Tile, bool GRAD, int P>
+// kKept: G again, of logits that the statistics' kernel kept, by the same tiles
+// and so with the same sums.
+enum { kStats = 0, kGrad = 1, kKept = 2 };
+template <class Tile, int MODE, int P>
 __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
-  __shared__ __align__(1024) uint8_t lds[Tile::LDS_BYTES];
+  constexpr bool GRAD = MODE != kStats;
+  __shared__ __align__(1024) uint8_t lds[MODE == kKept ? Tile::STAGING : Tile::LDS_BYTES];
   if (GRAD && static_cast<int>(blockIdx.x) >= a.tm * a.tn) {
     loss_sum(a.loss, reinterpret_cast<double2*>(lds));
     return;
@@ -266,8 +272,30 @@ __global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
   }
 
   f32x4 acc[Tile::FM][Tile::FN];
-  Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, Tile::steps_of(a.ksteps, a.pairs), lds, acc);
-  Tile::reduce(lds, acc);
+  if constexpr (MODE == kKept) {
+#pragma unroll
+    for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+      for (int j = 0; j < Tile::FN; ++j) {
+        const int t = min(col0 + Tile::col_of(j), nt - 1), r = row0 + Tile::row_of(i);
+        acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (Tile::group() == 0 && r < a.v_pad) acc[i][j] = *reinterpret_cast<const f32x4*>(a.logits + t * a.l_ld + a.v0 + r);
+      }
+  } else {
+    Tile::run(a.w, a.x, a.pairs, row0, col0, a.ksteps, 0, Tile::steps_of(a.ksteps, a.pairs), lds, acc);
+    Tile::reduce(lds, acc);
+  }
+  if constexpr (MODE == kStats && P > 1) {
+    if (a.logits && Tile::group() == 0) {
+#pragma unroll
+      for (int i = 0; i < Tile::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < Tile::FN; ++j) {
+          const int t = col0 + Tile::col_of(j), r = row0 + Tile::row_of(i);
+          if (t < nt && r < (rows + 63) / 64 * 64) *reinterpret_cast<f32x4*>(a.logits + t * a.l_ld + a.v0 + r) = acc[i][j];
+        }
+    }
+  }
 
   // (everything that has to be fetched first, without branches between)
   f32x4 bias[Tile::FM];
@@ -649,12 +677,13 @@ struct Plan {
   } of[2];                            // the pieces, and the last one, which may be smaller
   int dx_splits = 1;
   bool dx_slab = false;
+  bool keep = false;                  // the logits are kept for the gradient
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
   bool few = false, few_odd = false;  // few tokens: kernels of their own
   int few_classes = 128, few_lane = 4, few_splits = 1;   // classes a workgroup; of the gradient: channels a lane, parts of the classes
   // workspace offsets
-  size_t x_k = 0, w_k = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
+  size_t x_k = 0, w_k = 0, logits = 0, part = 0, tl = 0, sums = 0, g = 0, db = 0, slab = 0, total = 0;
 };
 
 constexpr int64_t kPartBytes = int64_t(64) << 20;     // of the forward pass's statistics
@@ -752,6 +781,13 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     p.piece = pick_piece(p, d.dx_sc != 1);
     p.pieces = cdiv(p.v, p.piece);
     p.g = take(p.t * p.piece * e);
+    // A step in fp32 keeps its logits, where G fits one piece and six products
+    // cost more than a store and a load: 4096 tokens, 5000 classes, 64, 128, 256
+    // channels 159, 190, 256 us, computed twice 146, 190, 291; 512 tokens, 1024
+    // channels, 50000 classes 1055, 1265.  (bf16: 23 us for G of the products,
+    // about as many for the store and the load.)
+    p.keep = fwd && !bf16 && p.dp >= 192 && p.pieces == 1 && p.t * p.vp * 4 <= kPieceBytes;
+    if (p.keep) p.logits = take(p.t * p.vp * 4);
     p.dx_turned = d.dx_sc != 1;
     const int64_t dm = p.dx_turned ? p.t : p.d, dn = p.dx_turned ? p.d : p.t;
     p.dx_ld = cdiv(dm, 4) * 4;
@@ -784,13 +820,13 @@ void stage(const StageArgs* a, int n, hipStream_t st) {
                      static_cast<int32_t>(blocks[0]));
 }
 
-template <bool GRAD, int P>
+template <int MODE, int P>
 void logits(int tile, LogitArgs& a, hipStream_t st) {
   a.tm = static_cast<int32_t>(cdiv(pad64(a.w.rows), tile_m(P, tile)));   // (G's padding is written too)
   a.tn = static_cast<int32_t>(cdiv(a.x.rows, tile_n(P, tile)));
   with_tile<__bf16, false, false, P>(tile, [&](auto t) {
     using Tile = decltype(t);
-    hipLaunchKernelGGL((logit_kernel<Tile, GRAD, P>), dim3(static_cast<uint32_t>(a.tm * a.tn + (a.loss.divisor ? 1 : 0))),
+    hipLaunchKernelGGL((logit_kernel<Tile, MODE, P>), dim3(static_cast<uint32_t>(a.tm * a.tn + (a.loss.divisor ? 1 : 0))),
                        dim3(Tile::THREADS), 0, st, a);
   });
 }
@@ -956,6 +992,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     return o;
   };
   LogitArgs la = {};
+  if (p.keep) la.logits = f32(p.logits), la.l_ld = p.vp;
   la.x = x, la.pairs = p.pairs, la.ksteps = static_cast<int32_t>(p.dp / 64), la.k = tok;
   if (p.fwd) {
     la.bias = c.bias, la.target_logit = f32(p.tl);
@@ -973,7 +1010,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
       const int64_t nv = std::min(p.fwd_piece, p.v - v0);
       const bool last = v0 + nv == p.v;
       la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0);
-      logits<false, P>(p.logit, la, st);
+      logits<kStats, P>(p.logit, la, st);
       const int32_t parts = static_cast<int32_t>(cdiv(pad64(nv), tile_m(P, p.logit)) * tile_wm(P, p.logit));
       const JoinArgs ja = {tok, carry, la.target_logit, v0 ? 0 : 1, parts + 1, last ? nullptr : carry, c.stats, each ? c.loss : nullptr,
                            sums, whole ? loss : LossArgs{}};
@@ -1002,7 +1039,10 @@ pp_status enqueue(const Plan& p, const Call& c) {
     la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0), la.bias = c.bias;
     la.g = bf(p.g), la.v_pad = static_cast<int32_t>(nvp), la.g_plane = p.t * nvp;
     la.db_part = c.db ? f32(p.db) : nullptr;
-    logits<true, P>(q.logit, la, st);
+    if (P > 1 && p.keep)
+      logits<P == 1 ? kGrad : kKept, P>(q.logit, la, st);
+    else
+      logits<kGrad, P>(q.logit, la, st);
     la.loss = {};
     const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * tile_wn(P, q.logit)), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
     const int32_t db_blocks = c.db ? static_cast<int32_t>(cdiv(nv, 64)) : 0;
