@@ -790,7 +790,7 @@ dim3 grid_of(const Spread& s) { return dim3(static_cast<uint32_t>(cdiv(s.total, 
 template <int P, bool POLY>
 void gram(const Plan& p, const Table& t, const Step& s, PlanePairs pairs, int turn, hipStream_t st) {
   const Spread sp = spread_of(p.blocks[POLY ? kStagePoly : kStageGram]);
-  with_tile<half_t, false, false, P>(POLY ? p.poly : p.gram, [&](auto k) {
+  with_tile<half_t, false, false, P, P == 1>(POLY ? p.poly : p.gram, [&](auto k) {
     using Tile = decltype(k);
     hipLaunchKernelGGL((gram_kernel<Tile, P, POLY>), grid_of(sp), dim3(Tile::THREADS), 0, st, t, s, pairs, turn, sp);
   });
