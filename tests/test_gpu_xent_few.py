@@ -75,3 +75,30 @@ def test_target_outside(dtype):
     t[2] = 70
     loss, dx, dw, db = pp.linear_xent_step(x, w, t, bias=b)
     assert bool(loss.isnan()) and bool(dx[2].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_offsets_past_32_bits(dtype):
+    # (w and dw have more than 2^32 bytes, in bf16 more than 2^32 elements)
+    d, v = 65536, {"f32": 17000, "bf16": 66000}[dtype]
+    x, _, t, _, _, _ = make(10, 2, d, 1, v, dtype, layout="tokens", bias=False)
+    t[0], t[1] = v - 1, 5
+    w = torch.empty(v, d, device="cuda", dtype=DT[dtype])
+    for i in range(0, v, 2000):
+        w[i:i + 2000] = make(11 + i, 1, d, 1, min(2000, v - i), dtype, layout="tokens", bias=False)[1]
+    loss, dx, dw, _ = pp.linear_xent_step(x, w, t)
+    lse = torch.logsumexp(torch.cat([x.double() @ w[i:i + 2000].double().t().contiguous() for i in range(0, v, 2000)], 1), 1)
+    for rows in (slice(0, 40), slice(v - 40, v)):
+        lim = Ref(x, w[rows], torch.zeros_like(t))     # (its bound on a logit)
+        l = x.double() @ w[rows].double().t().contiguous()
+        G = torch.exp(l - lse[:, None]) / 2
+        for i in range(2):
+            at = int(t[i]) - (rows.start or 0)
+            if 0 <= at < 40:
+                G[i, at] -= 0.5
+        want = G.t().contiguous() @ x.double()
+        u = {"f32": 2.0 ** -21, "bf16": 2.0 ** -7}[dtype]
+        bound = (2 * lim.lse_lim.max() + 1e-5) * (G.abs().t().contiguous() @ x.double().abs()) + u * (G.abs().t().contiguous() @ x.double().abs())
+        near(dw[rows], want, bound, "dw")
+    each = lse - torch.stack([(x[i].double() * w[int(t[i])].double()).sum() for i in range(2)])
+    near(loss, each.mean(), 2 * lim.lse_lim.max() + 1e-5, "loss")
