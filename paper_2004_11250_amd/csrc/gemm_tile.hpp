@@ -128,7 +128,7 @@ struct PlaneProducts<3> {
 };
 
 template <class T, int BM_, int BN_, int WM_, int WN_, int STAGES_, int WK_ = 1, bool PHASED_ = false, bool AR_ = false,
-          bool BR_ = false, int NP_ = 1>
+          bool BR_ = false, int NP_ = 1, int CR_ = 64>
 struct GemmTile {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int STAGES = STAGES_;                // steps held in LDS
@@ -487,7 +487,7 @@ struct GemmTile {
   // rows (a lane holds four rows of a column, too short a piece for either).  Each wave has a region of its own, of CR x CC values; f(row,
   // col, View) is called for each CR x CC part of the wave's tile, whose first
   // element is (row, col) of the workgroup's tile.
-  static constexpr int CR = TM % 64 == 0 ? 64 : TM % 32 == 0 ? 32 : 16, CC = TN;
+  static constexpr int CR = TM % 64 == 0 && CR_ >= 64 ? 64 : TM % 32 == 0 ? 32 : 16, CC = TN;
   // pieces of eight values a lane takes (a small part has work for SHARERS
   // groups only)
   static constexpr int SHARERS = CR * CC / 512 < WK ? CR * CC / 512 : WK, PIECES = CR * CC / 512 / SHARERS;

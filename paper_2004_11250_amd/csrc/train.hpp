@@ -44,8 +44,6 @@ inline GemmOperand operand(const void* base, int64_t plane_elems, int64_t ld, in
 //   64 x 64, two groups of
 //     waves share the steps     0.23 / 0.19  4     0.55 / 0.5    4     -
 //   32 x 32, a wave's own steps 0.1 / 0.12   2.8   0.27 / 0.25   2.8   0.46 / 0.43 2.8
-// (kAll256, kAll512, not in the table: tiles with all of up to 256 or 512 rows,
-// for what has to see a whole column.)
 // (192 x 192: one plane, operands that are not stored by rows of k; for a
 // triangle of tiles, which the large ones cover badly: 4096 x 4096 has 136 large
 // ones, in a whole round with 120 CUs idle, and 253 of these.)
@@ -57,7 +55,7 @@ inline GemmOperand operand(const void* base, int64_t plane_elems, int64_t ld, in
 // 4608, three products: 64 x 64 tiles 49 us, 32 x 32 21; one after the other 65
 // and 39.  2048^3, six products: 128 x 64 98 us, 64 x 64 135; 128 x 128, one
 // after the other, 145.  Operands stored by rows of k cost 5 to 10 % each.
-enum { kBig = 0, kMid = 1, kSmall = 2, kDeep = 3, kNarrow = 4, kFit = 5, kTiles = 6, kAll256 = 6, kAll512 = 7 };
+enum { kBig = 0, kMid = 1, kSmall = 2, kDeep = 3, kNarrow = 4, kFit = 5, kTiles = 6 };
 template <class T, bool AR, bool BR, int NP>
 struct Tiles {
   using Big = GemmTile<T, 256, 256, 2, 4, 2, 1, true, AR, BR>;
@@ -69,10 +67,10 @@ struct Tiles {
   using Narrow = GemmTile<T, 32, 32, 1, 1, 2, NP == 3 ? 3 : 4, false, AR, BR, NP>;
 };
 // rows and columns of a tile, and its waves' parts of them
-constexpr int tile_m(int, int k) { return k == kAll512 ? 512 : k == kBig || k == kAll256 ? 256 : k == kFit ? 192 : k == kMid ? 128 : k == kNarrow ? 32 : 64; }
-constexpr int tile_n(int np, int k) { return k == kAll512 || (k == kMid && np == 3) ? 64 : k == kAll256 ? 128 : tile_m(np, k); }
-constexpr int tile_wm(int np, int k) { return k == kAll512 ? 8 : k == kAll256 ? 4 : k == kMid && np == 3 ? 4 : k == kNarrow ? 1 : 2; }
-constexpr int tile_wn(int np, int k) { return k == kBig || k == kFit || (k == kMid && np == 2) ? 4 : k == kNarrow || k == kAll512 ? 1 : 2; }
+constexpr int tile_m(int, int k) { return k == kBig ? 256 : k == kFit ? 192 : k == kMid ? 128 : k == kNarrow ? 32 : 64; }
+constexpr int tile_n(int np, int k) { return k == kMid && np == 3 ? 64 : tile_m(np, k); }
+constexpr int tile_wm(int np, int k) { return k == kMid && np == 3 ? 4 : k == kNarrow ? 1 : 2; }
+constexpr int tile_wn(int np, int k) { return k == kBig || k == kFit || (k == kMid && np == 2) ? 4 : k == kNarrow ? 1 : 2; }
 constexpr int kCUs = 256;
 
 // f(tile's type) for tile k; AR, BR: operands stored by rows of k; NP: planes;
@@ -95,15 +93,6 @@ void with_tile(int k, F&& f) {
       f(typename X::Narrow());
   } else
     f(typename X::Narrow());
-}
-
-// the same for kAll256 and kAll512
-template <class T, class F>
-void with_all(int k, F&& f) {
-  if (k == kAll256)
-    f(GemmTile<T, 256, 128, 4, 2, 3>());
-  else
-    f(GemmTile<T, 512, 64, 8, 1, 2>());
 }
 
 // Modelled time in us of `tiles` tiles of `steps` k steps on average, `most` at

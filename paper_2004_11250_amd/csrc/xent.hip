@@ -268,12 +268,71 @@ __device__ __forceinline__ float sum16(float v) {
 // 8192 tokens, 313 classes, 256 channels, six products: 18 to 20 us, 0.4 PFLOP/s
 // (G of kept logits: 11 us, 2.8 TB/s).  With all classes in a tile, bf16, 32768
 // tokens, 313 classes, 256 channels: 33 us, where statistics, join and G took 43.
+// A tile with all classes of 64 tokens: 8 waves of 16 FM classes each, whose rows
+// of w no other wave needs: they come from memory (most of them from the L2) into
+// the lanes' registers, a step ahead, and only the tokens' features, all
+// channels at once, are in LDS.  So it has no barrier in its loop, and two
+// workgroups fit a CU.
+constexpr int kAllTokens = 64, kAllClasses = 512, kAllChannels = 512;
+template <int F>
+struct AllTile : GemmTile<__bf16, 128 * F, kAllTokens, 8, 1, 2, 1, false, false, false, 1, 32> {
+  using Base = GemmTile<__bf16, 128 * F, kAllTokens, 8, 1, 2, 1, false, false, false, 1, 32>;
+  static constexpr uint32_t FEATURES = kAllTokens * (kAllChannels + 8) * 2;
+  static constexpr uint32_t LDS_BYTES = FEATURES > Base::STAGING ? FEATURES : Base::STAGING;
+  static __device__ __forceinline__ void run(const GemmOperand& w, const GemmOperand& x, PlanePairs, int row0, int col0, int ksteps, int,
+                                             int, uint8_t* lds, f32x4 (&acc)[Base::FM][Base::FN]) {
+    const int tid = threadIdx.x, r = tid & 15, g = tid >> 4 & 3, pitch = ksteps * 64 + 8;   // (16 bytes past a multiple of the banks)
+    __bf16* xs = reinterpret_cast<__bf16*>(lds);
+    const __bf16* rows[Base::FM];
+#pragma unroll
+    for (int i = 0; i < Base::FM; ++i) {   // (what is past the last class is not used)
+      const int row = min(row0 + Base::wave() * Base::TM + 16 * i + r, w.rows - 1);
+      rows[i] = static_cast<const __bf16*>(w.plane[0]) + row * w.ld + 8 * g;
+    }
+    bf16x8 cur[Base::FM], next[Base::FM];
+#pragma unroll
+    for (int i = 0; i < Base::FM; ++i) cur[i] = *reinterpret_cast<const bf16x8*>(rows[i]);
+    {
+      const int t = tid >> 3;
+      const bool on = col0 + t < x.rows;
+      const __bf16* from = static_cast<const __bf16*>(x.plane[0]) + (on ? col0 + t : 0) * x.ld + (tid & 7) * 8;
+      __bf16* to = xs + t * pitch + (tid & 7) * 8;
+#pragma unroll 4
+      for (int n = 0; n < ksteps; ++n) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(from + 64 * n);
+        *reinterpret_cast<bf16x8*>(to + 64 * n) = on ? v : bf16x8{};
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < Base::FM; ++i)
+#pragma unroll
+      for (int j = 0; j < Base::FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int steps = ksteps * 2;
+    for (int s = 0; s < steps; ++s) {
+      const int ahead = min(s + 1, steps - 1) * 32;
+#pragma unroll
+      for (int i = 0; i < Base::FM; ++i) next[i] = *reinterpret_cast<const bf16x8*>(rows[i] + ahead);
+      bf16x8 b[Base::FN];
+#pragma unroll
+      for (int j = 0; j < Base::FN; ++j) b[j] = *reinterpret_cast<const bf16x8*>(xs + (16 * j + r) * pitch + 32 * s + 8 * g);
+#pragma unroll
+      for (int i = 0; i < Base::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < Base::FN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(cur[i], b[j], acc[i][j], 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < Base::FM; ++i) cur[i] = next[i];
+    }
+  }
+};
+
 // kKept: G again, of logits that the statistics' kernel kept, by the same tiles
 // and so with the same sums.  kWhole: a tile has all classes, so the statistics,
-// the loss and G (if there is room for it: g) are one kernel's work.
-enum { kStats = 0, kGrad = 1, kKept = 2, kWhole = 3 };
+// the loss and G (if there is room for it: g) are one kernel's work; kWholeGrad:
+// G by such tiles, given the statistics.
+enum { kStats = 0, kGrad = 1, kKept = 2, kWhole = 3, kWholeGrad = 4 };
 template <class Tile, int MODE, int P>
-__global__ __launch_bounds__(Tile::THREADS) void logit_kernel(LogitArgs a) {
+__global__ __launch_bounds__(Tile::THREADS, MODE >= kWhole ? 4 : 1) void logit_kernel(LogitArgs a) {
   constexpr bool GRAD = MODE != kStats, WHOLE = MODE == kWhole;
   __shared__ __align__(1024) uint8_t lds[MODE == kKept ? Tile::STAGING : Tile::LDS_BYTES];
   if (GRAD && !WHOLE && static_cast<int>(blockIdx.x) >= a.tm * a.tn) {
@@ -741,7 +800,7 @@ struct Plan {
   } of[2];                            // the pieces, and the last one, which may be smaller
   int dx_splits = 1;
   bool dx_slab = false;
-  int all = 0;                        // the tile that has all classes, or 0
+  int all = 0;                        // tiles with all classes: their 128s (else 0)
   bool keep = false;                  // the logits are kept for the gradient
   int64_t dx_ld = 0, dw_ld = 0;       // slab pitches: the product's rows rounded up to four
   bool dx_turned = false;             // dx's product has the tokens as rows
@@ -835,7 +894,8 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   // joined where they are.  8 x 4096 pixels, 256 channels, 313 classes: step 75 us,
   // 81 with the logits twice; 512 channels, 200 classes 88, 100.  Its loop has one
   // step in flight, so long sums are slower: 2048 channels, 256 classes 85, 76.
-  if (bf16 && p.v <= 512 && p.dp <= 512 && (!bwd || p.t * p.vp * 2 <= kPieceBytes)) p.all = p.v <= 256 ? kAll256 : kAll512;
+  if (bf16 && p.v <= kAllClasses && p.dp <= kAllChannels && (!bwd || p.t * p.vp * 2 <= kPieceBytes))
+    p.all = static_cast<int>(cdiv(p.v, 128));
   const size_t e = 2 * p.planes;
   if (!p.x_direct) p.x_k = take(p.t * p.dp * e);
   if (!p.w_direct) p.w_k = take(p.v * p.dp * e);
@@ -868,8 +928,8 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     for (int i = 0; i < 2; ++i) {
       const int64_t nv = i ? p.v - (p.pieces - 1) * p.piece : std::min(p.piece, p.v);
       Plan::Piece& q = p.of[i];
-      q.logit = p.all ? p.all : pick_tile(p.planes, nv, p.t, p.dp / 64);
-      db = std::max(db, cdiv(p.t, tile_n(p.planes, q.logit)) * tile_wn(p.planes, q.logit) * nv * 4);
+      q.logit = pick_tile(p.planes, nv, p.t, p.dp / 64);
+      db = std::max(db, (p.all ? cdiv(p.t, kAllTokens) : cdiv(p.t, tile_n(p.planes, q.logit)) * tile_wn(p.planes, q.logit)) * nv * 4);
       const SplitTile x = pick_split(p.planes, dm, dn, cdiv(nv, 64));
       q.dx = x.tile;
       if (i == 0) p.dx_splits = x.splits;   // (dx's partial sums are kept over the pieces)
@@ -903,20 +963,22 @@ void logits(int tile, LogitArgs& a, hipStream_t st) {
   });
 }
 
-void whole(int tile, LogitArgs& a, hipStream_t st) {
-  a.tm = 1, a.tn = static_cast<int32_t>(cdiv(a.x.rows, tile_n(1, tile)));
-  with_all<__bf16>(tile, [&](auto t) {
+// f128: classes in units of 128
+template <int MODE>
+void whole(int f128, LogitArgs& a, hipStream_t st) {
+  a.tm = 1, a.tn = static_cast<int32_t>(cdiv(a.x.rows, kAllTokens));
+  auto run = [&](auto t) {
     using Tile = decltype(t);
-    hipLaunchKernelGGL((logit_kernel<Tile, kWhole, 1>), dim3(static_cast<uint32_t>(a.tn)), dim3(Tile::THREADS), 0, st, a);
-  });
-}
-// G alone, by the same tiles
-void whole_grad(int tile, LogitArgs& a, hipStream_t st) {
-  a.tm = 1, a.tn = static_cast<int32_t>(cdiv(a.x.rows, tile_n(1, tile)));
-  with_all<__bf16>(tile, [&](auto t) {
-    using Tile = decltype(t);
-    hipLaunchKernelGGL((logit_kernel<Tile, kGrad, 1>), dim3(static_cast<uint32_t>(a.tn)), dim3(Tile::THREADS), 0, st, a);
-  });
+    hipLaunchKernelGGL((logit_kernel<Tile, MODE, 1>), dim3(static_cast<uint32_t>(a.tn)), dim3(Tile::THREADS), 0, st, a);
+  };
+  if (f128 == 1)
+    run(AllTile<1>());
+  else if (f128 == 2)
+    run(AllTile<2>());
+  else if (f128 == 3)
+    run(AllTile<3>());
+  else
+    run(AllTile<4>());
 }
 
 template <class O, bool AR, bool BR>
@@ -1088,7 +1150,7 @@ pp_status enqueue(const Plan& p, const Call& c) {
     const bool each = d.reduction == PP_NONE;
     la.w = w, la.lse_out = c.stats, la.each = each ? c.loss : nullptr;
     la.sums = each ? nullptr : reinterpret_cast<double2*>(c.ws + p.sums);
-    whole(p.all, la, st);
+    whole<kWhole>(p.all, la, st);
     const LossArgs loss = {la.sums, each ? 0 : static_cast<int32_t>(cdiv(p.t, 64)), d.reduction == PP_MEAN, each ? nullptr : c.loss,
                            c.stats + p.t};
     hipLaunchKernelGGL(loss_kernel, dim3(1), dim3(1024), 0, st, loss);
@@ -1137,16 +1199,14 @@ pp_status enqueue(const Plan& p, const Call& c) {
     la.w = from(w, v0), la.w.rows = static_cast<int32_t>(nv), la.v0 = static_cast<int32_t>(v0);
     la.g = bf(p.g), la.v_pad = static_cast<int32_t>(nvp), la.g_plane = p.t * nvp;
     la.db_part = c.db ? f32(p.db) : nullptr;
-    if (p.all && p.fwd)
-      la.tn = static_cast<int32_t>(cdiv(p.t, tile_n(1, p.all)));   // (G is there)
-    else if (p.all)
-      whole_grad(p.all, la, st);
-    else if (P > 1 && p.keep)
+    if (p.all) {
+      if (!p.fwd) whole<kWholeGrad>(p.all, la, st);   // (else G is there)
+    } else if (P > 1 && p.keep)
       logits<P == 1 ? kGrad : kKept, P>(q.logit, la, st);
     else
       logits<kGrad, P>(q.logit, la, st);
     la.loss = {};
-    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * tile_wn(P, q.logit)), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
+    const ClassSums db = {la.db_part, static_cast<int32_t>(la.tn * (p.all ? 1 : tile_wn(P, q.logit))), static_cast<int32_t>(nv), c.db ? c.db + v0 : nullptr};
     const int32_t db_blocks = c.db ? static_cast<int32_t>(cdiv(nv, 64)) : 0;
     if (db_blocks && !c.dw) hipLaunchKernelGGL(class_sum_kernel, dim3(static_cast<uint32_t>(db_blocks)), dim3(1024), 0, st, db, tok);
     // a small slab of dw is joined by dx's product, which comes after it
