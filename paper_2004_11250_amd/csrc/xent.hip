@@ -267,7 +267,9 @@ __device__ __forceinline__ float sum16(float v) {
 // G's store through LDS takes 45.  Sums of a few steps are short of that: fp32,
 // 8192 tokens, 313 classes, 256 channels, six products: 18 to 20 us, 0.4 PFLOP/s
 // (G of kept logits: 11 us, 2.8 TB/s).  With all classes in a tile, bf16, 32768
-// tokens, 313 classes, 256 channels: 33 us, where statistics, join and G took 43.
+// tokens, 313 classes, 256 channels: 29 us, where statistics, join and G took 43;
+// that is neither the products' time (4 us) nor the bytes' (8), but a chain of
+// fetches and joins with every workgroup resident.
 // A tile with all classes of 64 tokens: 8 waves of 16 FM classes each, whose rows
 // of w no other wave needs: they come from memory (most of them from the L2) into
 // the lanes' registers, a step ahead, and only the tokens' features, all
@@ -332,7 +334,7 @@ struct AllTile : GemmTile<__bf16, 128 * F, kAllTokens, 8, 1, 2, 1, false, false,
 // G by such tiles, given the statistics.
 enum { kStats = 0, kGrad = 1, kKept = 2, kWhole = 3, kWholeGrad = 4 };
 template <class Tile, int MODE, int P>
-__global__ __launch_bounds__(Tile::THREADS, MODE >= kWhole ? 4 : 1) void logit_kernel(LogitArgs a) {
+__global__ __launch_bounds__(Tile::THREADS, MODE < kWhole ? 1 : Tile::FM < 4 ? 4 : 2) void logit_kernel(LogitArgs a) {
   constexpr bool GRAD = MODE != kStats, WHOLE = MODE == kWhole;
   __shared__ __align__(1024) uint8_t lds[MODE == kKept ? Tile::STAGING : Tile::LDS_BYTES];
   if (GRAD && !WHOLE && static_cast<int>(blockIdx.x) >= a.tm * a.tn) {
@@ -891,10 +893,11 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
     return p;
   }
   // Few classes: a tile that has them all, whose logits are computed once and
-  // joined where they are.  8 x 4096 pixels, 256 channels, 313 classes: step 75 us,
-  // 81 with the logits twice; 512 channels, 200 classes 88, 100.  Its loop has one
-  // step in flight, so long sums are slower: 2048 channels, 256 classes 85, 76.
-  if (bf16 && p.v <= kAllClasses && p.dp <= kAllChannels && (!bwd || p.t * p.vp * 2 <= kPieceBytes))
+  // joined where they are.  8 x 4096 pixels, 256 channels, 313 classes: step 71 us,
+  // 81 with the logits twice; 3000 tokens, 128 channels, 130 classes 31, 37.  A tile's
+  // time grows with the channels, so few tokens keep to the products: 200 tokens,
+  // 512 channels, 500 classes 43, 37.
+  if (bf16 && p.t >= 512 && p.v <= kAllClasses && p.dp <= kAllChannels && (!bwd || p.t * p.vp * 2 <= kPieceBytes))
     p.all = static_cast<int>(cdiv(p.v, 128));
   const size_t e = 2 * p.planes;
   if (!p.x_direct) p.x_k = take(p.t * p.dp * e);
