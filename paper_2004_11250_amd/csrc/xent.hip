@@ -872,8 +872,9 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   // 1, 64 tokens 72, 105, by the products 146, 154.  With few classes a token the
   // workgroups are too few: fp32, 64 tokens, 2048 channels, 1000 classes 108 us,
   // 68; 128 tokens, 256 channels, 17000 classes 101, 89 (96 tokens, 64 channels,
-  // 20000 classes: 65, 66).
-  p.few = p.t <= kFewTokens[bf16] && p.v >= 192 * p.t && p.d >= 8 && p.t * p.vp * 4 <= kPieceBytes;
+  // 20000 classes: 65, 66).  Rows of w too far apart for the kernels' descriptors
+  // (32 rows, 32-bit offsets) are left to the products, which copy them.
+  p.few = p.t <= kFewTokens[bf16] && p.v >= 192 * p.t && p.d >= 8 && p.t * p.vp * 4 <= kPieceBytes && d.w_ld <= kMaxLd;
   if (p.few) {
     p.few_lane = p.t <= 64 ? 4 : 2;
     // 64 a workgroup where that leaves CUs without one (1 token, 2048 channels,

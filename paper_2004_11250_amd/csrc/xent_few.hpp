@@ -33,6 +33,7 @@ struct FewArgs {
 };
 
 constexpr uint32_t kNowhere = 0x80000000u;   // past the end of any buffer made here
+static_assert(32 * kMaxLd * 4 < int64_t(kNowhere), "32 rows of w in one descriptor");
 
 // N values of a row of w, from byte `at` of the buffer on, which is the row's
 // column `col`.  A row's last values are fetched as its last N and moved down
