@@ -588,7 +588,8 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  *                 elements is skipped
  *   dtype         pp_dtype of every u and o
  *   steps         1..64
- *   workspace     256-byte aligned, pp_ortho_workspace() bytes
+ *   workspace     256-byte aligned, pp_ortho_workspace() bytes (0 where every
+ *                 matrix is small: it may be NULL then)
  * pp_muon_step -- the weight step of a list of layers:
  *   M' = momentum M + G
  *   U  = G + momentum M' (nesterov) or M'

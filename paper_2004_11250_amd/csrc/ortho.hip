@@ -778,7 +778,7 @@ pp_status make_plan(Plan* p, int32_t dtype, uint8_t* ws) {
     m.part = reinterpret_cast<double*>(ws + take(m.chunks * 8));
   }
   p->table = take(p->mats.size() * (sizeof(Mat) + kStages * 4));
-  p->total = std::max<size_t>(at, 256);
+  p->total = at;   // (0: small matrices need none)
   return PP_OK;
 }
 
@@ -876,9 +876,10 @@ pp_status check_step(const Step& s) {
 
 pp_status run(Plan* p, int32_t dtype, const Step& s, void* workspace, size_t ws_bytes, void* hip_stream) {
   if (p->mats.empty()) return PP_OK;
-  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256) return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
   const pp_status st = make_plan(p, dtype, static_cast<uint8_t*>(workspace));
   if (st != PP_OK) return st;
+  if (p->total && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256))
+    return fail(PP_EINVAL, "the workspace must be 256-byte aligned");
   if (ws_bytes < p->total) return fail(PP_ESIZE, "workspace smaller than needed");
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   return dtype == PP_BF16 ? enqueue<__bf16, 1>(*p, s, static_cast<uint8_t*>(workspace), stream)
@@ -965,7 +966,7 @@ extern "C" pp_status pp_ortho_workspace(const pp_ortho_mat* mats, int32_t count,
     Plan p;
     pp_status s = collect(&p, mats, count, dtype, false);
     if (s == PP_OK) s = make_plan(&p, dtype, nullptr);
-    if (s == PP_OK) *bytes = p.mats.empty() ? 0 : p.total;
+    if (s == PP_OK) *bytes = p.total;
     return s;
   });
 }
@@ -989,7 +990,7 @@ extern "C" pp_status pp_muon_workspace(const pp_muon_layer* layers, int32_t coun
     Plan p;
     pp_status s = collect(&p, layers, count, dtype, false, 0.f);
     if (s == PP_OK) s = make_plan(&p, dtype, nullptr);
-    if (s == PP_OK) *bytes = p.mats.empty() ? 0 : p.total;
+    if (s == PP_OK) *bytes = p.total;
     return s;
   });
 }
