@@ -256,6 +256,20 @@ __global__ __launch_bounds__(256) void norm_kernel(Table t, Step s) {
   if (threadIdx.x == 0) m.part[chunk] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
+// X = U times / (|U| + eps), for any norm of finite fp32 values: fp32 holds the
+// factor itself from norms of 2^-115 on (below it is infinite) up to 2^126 (above
+// it loses bits), so a power of two goes first, which is exact.  (Where that
+// takes bits from an element, the element is 2^-100 of the norm.)  0 where U is.
+struct Scale {
+  float first, then;
+  __device__ __forceinline__ float operator()(float x) const { return x * first * then; }
+};
+__device__ __forceinline__ Scale scale_of(double squares, float eps, float times) {
+  const double norm = sqrt(squares) + static_cast<double>(eps);
+  const double first = norm < 0x1p-64 ? 0x1p80 : norm > 0x1p64 ? 0x1p-64 : 1.;
+  return {static_cast<float>(first), norm == 0. ? 0.f : static_cast<float>(times / (norm * first))};
+}
+
 __device__ __forceinline__ void split(float x, half_t* h, half_t* l) {
   *h = static_cast<half_t>(x);
   *l = static_cast<half_t>(x - static_cast<float>(*h));
@@ -276,7 +290,7 @@ __global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
   if ((tid & 63) == 0) sums[tid >> 6] = sum;
   __syncthreads();
-  const float scale = static_cast<float>(kSX / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + static_cast<double>(s.eps)));
+  const Scale scale = scale_of(sums[0] + sums[1] + sums[2] + sums[3], s.eps, kSX);
 
   const int tc = m.np / 64, r0 = id / tc * 64, c0 = id % tc * 64;
   // pieces of eight along the update's own rows, or down them if its columns
@@ -304,7 +318,7 @@ __global__ __launch_bounds__(256) void fill_kernel(Table t, Step s) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float v = x[e] * scale;
+      const float v = scale(x[e]);
       if (along_n)
         tile[u][w + e] = c + e < m.n ? v : 0.f;
       else
@@ -600,8 +614,8 @@ __global__ __launch_bounds__(kTinyWaves * 64) void tiny_kernel(Setup su, Step s)
   __syncthreads();
   sum = 0.;
   for (int i = 0; i < kTinyWaves; ++i) sum += sums[i];
-  const float scale = static_cast<float>(1. / (sqrt(sum) + static_cast<double>(s.eps)));
-  for (int e = tid; e < mt * 16 * ld; e += kThreads) x[e] *= scale;
+  const Scale scale = scale_of(sum, s.eps, 1.f);
+  for (int e = tid; e < mt * 16 * ld; e += kThreads) x[e] = scale(x[e]);
   __syncthreads();
 
   // a lane's operand values: row or column lane % 16, k lane / 16
