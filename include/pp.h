@@ -548,6 +548,12 @@ typedef struct {
  * The backward pass rounds the logits' gradient to bf16 (bf16 features) or to
  * 24 bits (fp32; few tokens: not) for the products with w and x, and sums in
  * fp32.
+ * A loss is taken from its token's largest logit and the logarithm of its sum
+ * apart (2^-24 absolute for a token that is sure of its class, however large the
+ * logits).  The gradients are taken from stats, in pp_xent_step too (the two
+ * agree bit by bit): a probability is exp(l - lse) of the fp32 lse, off by up to
+ * |lse| 2^-24 of itself, so the target's own p - 1 of a token whose loss is below
+ * that is not resolved.
  * n hw = 0 is a loss of 0 and zero gradients.
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, reduction, dtype,
  * negative strides), PP_EUNSUPPORTED (d, v or the tokens 2^22 - 64 or more, x or

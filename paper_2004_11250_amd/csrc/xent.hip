@@ -67,14 +67,16 @@ __device__ __forceinline__ float token_loss(const Tokens& k, int t, float2 s, fl
   const int64_t y = k.target[t];
   *loss = *weight = 0.f;
   if (y == k.ignore) return 0.f;
-  const float lse = s.x + logf(s.y);
+  // (the loss from the maximum and the sum's logarithm, not from their sum: that
+  // is rounded to 2^-24 of itself, which may be more than the loss)
+  const float rest = logf(s.y);
   if (y < 0 || y >= k.v) {
     *loss = *weight = __builtin_nanf("");
   } else {
     *weight = k.class_weight ? k.class_weight[y] : 1.f;
-    *loss = *weight * (lse - target_logit);
+    *loss = *weight * (s.x - target_logit + rest);
   }
-  return lse;
+  return s.x + rest;
 }
 
 // ---------------------------------------------------------------------------
