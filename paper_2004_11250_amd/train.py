@@ -15,6 +15,12 @@ training section, on torch tensors).
 As elsewhere in this package every computation runs in the library's kernels;
 this module checks and marshals arguments, and allocates outputs and scratch
 on the stream of the call.
+
+No call records an autograd graph.  Tensors that require a gradient are read as
+they are, and no result requires one: the gradients that ``linear_xent_bwd`` and
+``linear_xent_step`` return are passed on by hand (``features.backward(dx)``).
+Tensors that a call writes in place count as changed: a graph that has saved one
+refuses its backward pass.
 """
 from __future__ import annotations
 
@@ -87,6 +93,11 @@ def _on(stream, device):
         return contextlib.nullcontext()
     torch = _torch()
     return torch.cuda.stream(torch.cuda.ExternalStream(int(stream.cuda_stream), device))
+
+
+def _changed(tensors):
+    """Tell autograd that a call has written these."""
+    _torch().autograd.graph.increment_version(tensors)
 
 
 def _flat_pixels(x):
@@ -286,8 +297,9 @@ def orthogonalize(mats, steps=5, coeffs=COEFFS, eps=1e-7, out=None, stream=None)
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     lib = load_library()
+    given = out is not None
     with _on(stream, dev):
-        if out is None:
+        if not given:
             out = [torch.empty(t.shape, dtype=t.dtype, device=dev) for t in mats]
         arr = (OrthoMat * len(mats))()
         for e, t, o, (r, c, rs, cs) in zip(arr, mats, out, shapes):
@@ -298,6 +310,8 @@ def orthogonalize(mats, steps=5, coeffs=COEFFS, eps=1e-7, out=None, stream=None)
         ws = torch.empty(max(nb.value, 256), dtype=torch.uint8, device=dev)
     _check(lib.pp_ortho(arr, len(mats), code, int(steps), k, float(eps), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
            "pp_ortho")
+    if given:
+        _changed(out)
     return out[0] if single else out
 
 
@@ -356,4 +370,5 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
     d = MuonDesc(float(lr), float(momentum), float(weight_decay), int(bool(nesterov)), int(steps), k, float(eps))
     _check(lib.pp_muon_step(arr, len(weights), code, ctypes.byref(d), ws.data_ptr(), ws.numel(), _stream_ptr(stream)),
            "pp_muon_step")
+    _changed(wo + mo)
     return (wo[0], mo[0]) if single else (wo, mo)
