@@ -589,7 +589,8 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  * 2.0315}, {1.875, -1.25, 0.375}, {1.5, -0.5, 0}; others PP_EUNSUPPORTED.
  *
  * pp_ortho -- all matrices of a list in one call (each stage of the iteration
- * is one launch over all of them).  u and o may be the same.
+ * is one launch over all of them).  A matrix's o may be its own u; it may not
+ * overlap another's u or o, since they are read and written in no order.
  *   mats, count   host array (read during the call); a matrix without
  *                 elements is skipped
  *   dtype         pp_dtype of every u and o
@@ -604,7 +605,8 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  * its 3x3 kernels (Sec. 2: the pattern of a kept kernel, 0 for a removed one;
  * bit t = tap t): taps that are off count as 0 in G, and W' and M' are 0 there
  * whatever W, M and G hold, so the layer stays on its structure.  All arrays
- * are contiguous [rows][cols]; w_out may be w and momentum_out may be momentum.
+ * are contiguous [rows][cols]; a layer's w_out may be its w and its momentum_out
+ * its momentum, and they may overlap no other array of the call.
  *   layers, count  host array (read during the call)
  *   dtype          pp_dtype of w, g and w_out; momentum is fp32
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, a pruned layer's cols

@@ -272,6 +272,21 @@ def _one_dtype(tensors, name):
     return code, dev
 
 
+def _own_places(outs, ins, more=()):
+    """outs[i] may be ins[i] and no other tensor of a call: the matrices of a list
+    are read and written in no order.  (By where they begin.)"""
+    at = {}
+    for i, t in enumerate(outs):
+        if t.numel() and at.setdefault(t.data_ptr(), i) != i:
+            raise ValueError("two outputs are the same tensor")
+    for i, t in enumerate(ins):
+        if t.numel() and at.get(t.data_ptr(), i) != i:
+            raise ValueError("an output is another matrix's input")
+    for t in more:
+        if t.numel() and t.data_ptr() in at:
+            raise ValueError("an output is another tensor of the call")
+
+
 def _coeffs(coeffs):
     if len(coeffs) != 3:
         raise ValueError("coeffs must be three numbers")
@@ -282,7 +297,7 @@ def orthogonalize(mats, steps=5, coeffs=COEFFS, eps=1e-7, out=None, stream=None)
     """pp_ortho: the Newton-Schulz iterate of each update, a tensor or a list of
     them ([rows, ...], trailing axes taken together; float32 or bfloat16, any
     strides), all in one call.  Returns contiguous tensors of the same shapes,
-    or fills ``out`` (which may be the inputs)."""
+    or fills ``out``, each of which may be its own input."""
     torch = _torch()
     single = torch.is_tensor(mats)
     mats = [mats] if single else list(mats)
@@ -293,6 +308,7 @@ def orthogonalize(mats, steps=5, coeffs=COEFFS, eps=1e-7, out=None, stream=None)
         if len(out) != len(mats) or any(o.shape != t.shape or o.dtype != t.dtype or o.device != dev
                                         for o, t in zip(out, mats)):
             raise ValueError("out must match mats")
+        _own_places(out, mats)
     shapes = [_matrix(t, "a matrix of mats") for t in mats]
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
@@ -335,7 +351,7 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
     shapes, all contiguous.  ``keep``: None, or for each layer None or the int16
     tap masks [c_out][c_in] of a pruned 3x3 layer (keep_masks).  Updates weights
     and momenta in place, or fills ``out`` = (weights, momenta), and returns
-    them."""
+    them.  What is written is each layer's own: a weight may be listed once."""
     torch = _torch()
     single = torch.is_tensor(weights)
     if single:
@@ -360,6 +376,7 @@ def muon_step(weights, grads, momenta, lr, momentum=0.95, nesterov=True, weight_
             raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
         e.rows, e.cols, e.w, e.g, e.momentum = r, c, w.data_ptr(), g.data_ptr(), m.data_ptr()
         e.w_out, e.momentum_out, e.keep = w2.data_ptr(), m2.data_ptr(), _p(kp)
+    _own_places(wo + mo, weights + momenta, grads)
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     lib = load_library()
