@@ -501,7 +501,7 @@ enum { PP_XENT_FWD = 1, PP_XENT_BWD = 2 };               /* parts of pp_xent_wor
  *   lse[t]  = log sum_j exp l[t][j]
  *   loss[t] = class_weight[y] (lse[t] - l[t][y]),  y = target[t]
  * PP_SUM sums loss over the tokens, PP_MEAN divides that by the sum of
- * class_weight[y] (a mean over no token is 0), PP_NONE stores each.  A token
+ * class_weight[y] (by 1 where that is 0: a mean over no token is 0), PP_NONE stores each.  A token
  * whose target is ignore_index contributes nothing to the loss or to any
  * gradient, whatever its features hold; its dx is 0 (NaN where the incoming
  * gradient or the mean's divisor is not finite).  A token whose target is
@@ -509,9 +509,11 @@ enum { PP_XENT_FWD = 1, PP_XENT_BWD = 2 };               /* parts of pp_xent_wor
  * gradients it reaches NaN.  A class whose logits are -inf (a bias of -inf)
  * has probability 0; a token all of whose logits are -inf has loss NaN.
  * The logits are accumulated in fp32 and not rounded.  They are not stored,
- * except in the workspace, up to 512 MB: those of few tokens (64, in fp32 128)
- * by a call that computes gradients, and in fp32 by pp_xent_step.  fp32 features are multiplied in fp32 (few
- * tokens) or as sums of three bf16 values each (24 bits).
+ * except in the workspace, up to 512 MB: those of few tokens (64, in fp32 128,
+ * with 192 classes a token or more) by a call that computes gradients, and in
+ * fp32 by pp_xent_step.  fp32 features are multiplied as sums of three bf16
+ * values each (24 bits); those of few tokens in fp32, but for the logits of more
+ * than 16.
  */
 typedef struct {
   int32_t dtype;                       /* pp_dtype of x, w, dx and dw                 */
@@ -536,7 +538,7 @@ typedef struct {
  *   loss          device fp32: one value, or [n][hw] with PP_NONE
  *   stats         device fp32 [n hw + 1]: lse of each token (0 where ignored),
  *                 then what PP_MEAN divides by (1 for PP_SUM and PP_NONE, and
- *                 for a mean over no token)
+ *                 for a mean whose weights sum to 0)
  *   workspace     256-byte aligned
  * pp_xent_bwd -- the gradients of sum_t grad[t] loss[t] (PP_NONE), or of
  * grad[0] loss; stats as pp_xent_fwd left it for the same inputs.
@@ -580,8 +582,11 @@ pp_status pp_xent_step(const pp_xent_desc* desc, const void* x, const void* w, c
  * a s + b s^3 + c s^5, towards 1 (a matrix with more rows than columns is
  * handled as its transpose: the same result).  The values are held as pairs of
  * fp16 values (22 bits) between the products, whose sums are fp32; for bf16
- * matrices 11 bits of each enter the products, an error of about 1.3e-3 of the
- * result.  The sum of squares is taken in 64 bits.  U = 0 gives 0; a NaN or an
+ * matrices 11 bits of each enter the products.  That errs, beside the rounding of
+ * the result to bf16 (1.7e-3 of its norm), by 1.0e-3 to 1.7e-3 of it for five
+ * steps on updates whose directions are all of a size, the more the fewer rows,
+ * and by less where some dominate; small matrices, done in fp32, by nothing
+ * beside it.  The sum of squares is taken in 64 bits.  U = 0 gives 0; a NaN or an
  * infinity in U makes its result NaN.
  * Coefficients: those that keep singular values of 0..1 within -2..2 on every
  * step (every step for all values up to the largest that the one before can
