@@ -59,8 +59,6 @@ struct PlanePairs {
 constexpr uint32_t plane_pair(int p, int q, int i) { return static_cast<uint32_t>(p | q << 2) << (4 * i); }
 // one plane each: 16-bit operands
 constexpr PlanePairs kPairs1 = {plane_pair(0, 0, 0), 1};
-// two planes of A, one of B
-constexpr PlanePairs kPairs2 = {plane_pair(1, 0, 0) | plane_pair(0, 0, 1), 2};
 // two planes each; what is left out is the product of the two rests
 constexpr PlanePairs kPairs3 = {plane_pair(1, 0, 0) | plane_pair(0, 1, 1) | plane_pair(0, 0, 2), 3};
 // three bf16 planes each hold all 24 bits of an fp32 value; what is left out

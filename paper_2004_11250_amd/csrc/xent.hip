@@ -46,6 +46,13 @@ struct Tokens {   // what the kernels know of the tokens
 // loss over the divisor.  It is left out of G and multiplied into the fp32
 // sums: most of G's weight lies in the values near -1 at the targets, which
 // 16 bits hold well and which a common factor would round all alike.
+//
+// G's other rounding is a choice too: with bf16 features it enters the products
+// with w and x as one bf16 value, like those.  It errs by 2^-8 of each value at
+// most, independently, as does the output's own rounding: gradients of 8 x 4096 pixels,
+// 256 channels, 313 classes are off by 2.4e-3 of their norm, with G in fp32 by
+// 1.7e-3.  A second value for the rest would make either product two (1.6 of the
+// 3.0 ms of 8192 tokens, 1024 channels, 50000 classes are those).
 __device__ __forceinline__ float common_scale(const Tokens& k) {
   return (k.grad && !k.grad_each ? k.grad[0] : 1.f) / k.stats[k.t];
 }
@@ -872,9 +879,18 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   // Few tokens: where reading w is the work.  1024 channels, 50000 classes, step:
   // fp32 1, 64, 128 tokens 125, 225, 420 us, by the products 438, 458, 646; bf16
   // 1, 64 tokens 72, 105, by the products 146, 154.  With few classes a token the
-  // workgroups are too few: fp32, 64 tokens, 2048 channels, 1000 classes 108 us,
-  // 68; 128 tokens, 256 channels, 17000 classes 101, 89 (96 tokens, 64 channels,
-  // 20000 classes: 65, 66).  Rows of w too far apart for the kernels' descriptors
+  // workgroups are too few, and the two ways meet at about 192 (step, us, here and
+  // by the products; 96, 192, 384 classes a token):
+  //   bf16 64 tokens, 256 channels      40, 46   47, 45   49, 55
+  //   bf16 64 tokens, 1024 channels     59, 49   64, 61   71, 88
+  //   bf16 64 tokens, 2048 channels     74, 62   84, 82   105, 126
+  //   fp32 64 tokens, 256 channels      53, 49   61, 65   70, 89
+  //   fp32 64 tokens, 1024 channels     91, 76   105, 105 134, 183
+  //   fp32 64 tokens, 2048 channels     135, 111 163, 180 223, 377
+  //   fp32 128 tokens, 256 channels     92, 71   110, 107 152, 166
+  //   fp32 128 tokens, 1024 channels    185, 126 251, 240 417, 491
+  // Up to 16 tokens a step is 34 to 36 us here at any of these, by the products 41
+  // to 46 (launches), so the rule's lower side gives up to 10 us away there.  Rows of w too far apart for the kernels' descriptors
   // (32 rows, 32-bit offsets) are left to the products, which copy them.
   p.few = p.t <= kFewTokens[bf16] && p.v >= 192 * p.t && p.d >= 8 && p.t * p.vp * 4 <= kPieceBytes && d.w_ld <= kMaxLd;
   if (p.few) {
@@ -899,9 +915,16 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   }
   // Few classes: a tile that has them all, whose logits are computed once and
   // joined where they are.  8 x 4096 pixels, 256 channels, 313 classes: step 71 us,
-  // 81 with the logits twice; 3000 tokens, 128 channels, 130 classes 31, 37.  A tile's
-  // time grows with the channels, so few tokens keep to the products: 200 tokens,
-  // 512 channels, 500 classes 43, 37.
+  // 81 with the logits twice.  A tile's time grows with channels and classes, and
+  // few tokens leave CUs idle that the products use (step of token rows, us, here
+  // and by the products; 512, 1024, 3000, 8192 tokens):
+  //   130 classes, 128 channels   38, 41   38, 41   38, 41   38, 41
+  //   313 classes, 256 channels   38, 41   39, 42   46, 43   44, 49
+  //   313 classes, 512 channels   40, 42   43, 42   53, 49   55, 59
+  //   500 classes, 256 channels   39, 42   41, 42   51, 45   51, 52
+  //   500 classes, 512 channels   45, 42   49, 42   61, 51   65, 64
+  // (below 512 tokens 0 to 3 us either way.)  So it loses up to a fifth in a part
+  // of its range, many classes and channels of some thousand tokens.
   if (bf16 && p.t >= 512 && p.v <= kAllClasses && p.dp <= kAllChannels && (!bwd || p.t * p.vp * 2 <= kPieceBytes))
     p.all = static_cast<int>(cdiv(p.v, 128));
   const size_t e = 2 * p.planes;

@@ -6,7 +6,8 @@
 // which of the k positions of an instruction a lane's values take is free as
 // long as both operands agree, so lane (r, g) = (lane % 16, lane / 16) gives
 // four (or eight) neighbouring channels, one (or all) to an instruction.  fp32
-// values are multiplied in fp32: at these sizes its rate is enough.
+// values are multiplied in fp32, whose rate is enough for that up to 16 tokens; the
+// logits of more take w in three bf16 values (few_logit3_kernel).
 // (Included by xent.hip, inside its namespace.)
 
 constexpr int kFewTokens[2] = {128, 64};   // fp32, bf16
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(256, 2) void few_logit3_kernel(FewArgs a) {
 
 // G of 64 classes at a time in LDS; each wave has 16 C channels, for which it adds
 // G w to dx's sums in registers and stores G^T x.  bf16 operands: G is rounded
-// to bf16 (db is summed before), a lane gives four tokens or classes to one
+// to bf16, as by the products (db is summed before), a lane gives four tokens or classes to one
 // instruction, and the four channels that it loads of each of four classes are
 // turned in its registers.  Bound by memory up to 16 tokens (1024 channels, 50000
 // classes, fp32: about 75 us for w read and dw written, 5.4 TB/s), by the fp32
