@@ -889,8 +889,10 @@ Plan make_plan(const pp_xent_desc& d, bool fwd, bool bwd, bool dw, bool x_aligne
   //   fp32 64 tokens, 2048 channels     135, 111 163, 180 223, 377
   //   fp32 128 tokens, 256 channels     92, 71   110, 107 152, 166
   //   fp32 128 tokens, 1024 channels    185, 126 251, 240 417, 491
-  // Up to 16 tokens a step is 34 to 36 us here at any of these, by the products 41
-  // to 46 (launches), so the rule's lower side gives up to 10 us away there.  Rows of w too far apart for the kernels' descriptors
+  // Up to 16 tokens the kernels here are ahead from 24 classes a token on (bf16 35
+  // us, 42 to 46; fp32, 2048 channels, 96 a token 50, 62), so the rule gives up to
+  // 12 us away there; the forward pass alone of 64 bf16 tokens with 2048 channels
+  // loses by it up to 384 a token (42, 27 at 192; 42, 42).  Rows of w too far apart for the kernels' descriptors
   // (32 rows, 32-bit offsets) are left to the products, which copy them.
   p.few = p.t <= kFewTokens[bf16] && p.v >= 192 * p.t && p.d >= 8 && p.t * p.vp * 4 <= kPieceBytes && d.w_ld <= kMaxLd;
   if (p.few) {
