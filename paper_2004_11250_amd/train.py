@@ -277,6 +277,8 @@ def _own_places(outs, ins, more=()):
     are read and written in no order.  (By where they begin.)"""
     at = {}
     for i, t in enumerate(outs):
+        if any(step == 0 and size > 1 for step, size in zip(t.stride(), t.shape)):
+            raise ValueError("elements of an output share their memory")
         if t.numel() and at.setdefault(t.data_ptr(), i) != i:
             raise ValueError("two outputs are the same tensor")
     for i, t in enumerate(ins):

@@ -44,3 +44,14 @@ def test_weight_steps():
     for out in (None, ([w, w2], [m, m2]), ([x, w2], [m, m2])):
         with refused("GPU"):
             pp.muon_step([w, w2], [g, g], [m, m2], lr=0.1, out=out)
+
+
+def test_outputs_that_share_their_elements():
+    u = torch.zeros(8, 8)
+    for out in (torch.zeros(8, 1).expand(8, 8), torch.zeros(1, 8).expand(8, 8), torch.zeros(1, 1).expand(8, 8)):
+        with refused("share their memory"):
+            pp.orthogonalize(u, out=out)
+        with refused("GPU"):      # (an input may)
+            pp.orthogonalize(out)
+    with refused("GPU"):
+        pp.orthogonalize(torch.zeros(1, 8), out=torch.zeros(8).expand(1, 8))
