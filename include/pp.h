@@ -482,7 +482,8 @@ const char* pp_last_error(void);
 /* ------------------------------------------------------------------------
  * Training operators.  Structured pruning alternates training steps with the
  * projections above (Sec. 2: min f(W) subject to W_i in S_i); these are the
- * loss with its gradient of a network's linear head, and the weight step.
+ * loss with its gradient of a network's linear head, a table of embeddings with
+ * its gradient, and the weight steps.
  * Conventions as above: caller-owned device buffers, caller's stream, no
  * synchronisation, no allocation, fixed summation orders (repeated calls are
  * bitwise identical).  All can be recorded into a HIP graph.
@@ -650,6 +651,139 @@ pp_status pp_ortho(const pp_ortho_mat* mats, int32_t count, int32_t dtype, int32
                    float eps, void* workspace, size_t ws_bytes, void* hip_stream);
 pp_status pp_muon_workspace(const pp_muon_layer* layers, int32_t count, int32_t dtype, size_t* bytes);
 pp_status pp_muon_step(const pp_muon_layer* layers, int32_t count, int32_t dtype, const pp_muon_desc* desc,
+                       void* workspace, size_t ws_bytes, void* hip_stream);
+
+/*
+ * A table of embeddings: v rows of d features, looked up by id.
+ *   y[t]  = scale w[ids[t]]                              (pp_embed_fwd)
+ *   dw[j] = add[j] + scale sum over t, ids[t] = j, of dy[t]   (pp_embed_bwd)
+ * A token whose id is ignore_index (in 0..v-1 or not) has a row of zeros and
+ * reaches no gradient, whatever its dy holds.  A token whose id is neither that
+ * nor in 0..v-1 has a row of NaN and reaches no gradient.
+ * Sums are fp32, in an order that the ids alone fix, and rounded once, after scale
+ * and add.
+ */
+typedef struct {
+  int32_t w_dtype;                     /* pp_dtype of w, dw and add                   */
+  int32_t y_dtype;                     /* pp_dtype of y and dy                        */
+  int64_t t, v, d;                     /* tokens, rows of the table, features         */
+  int64_t w_ld;                        /* elements from one row of w, dw, add to the next */
+  int64_t y_ld;                        /* elements from one row of y, dy to the next  */
+  int64_t ignore_index;
+  float scale;
+} pp_embed_desc;
+
+/*
+ * pp_embed_fwd
+ *   ids   device int64 [t]
+ *   w, y  device [v][d] and [t][d] (rows w_ld and y_ld apart)
+ * pp_embed_workspace -- device bytes pp_embed_bwd needs: 4 (v + t), and up to
+ * 2048 rows of d fp32 values for rows of the table that many tokens share.
+ * pp_embed_bwd
+ *   dy         device [t][d]
+ *   add        device [v][d], or NULL; may be dw: then only rows that tokens
+ *              reach are written (and read)
+ *   dw         device [v][d]; every row is written.  It may overlap no other
+ *              array of the call (but be add)
+ *   workspace  256-byte aligned
+ * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, dtypes, rows closer
+ * than d), PP_EUNSUPPORTED (2^30 tokens or rows of the table or more, d of 2^24
+ * or more, rows 2^32 elements apart or more), PP_ESIZE, PP_EHIP.
+ */
+pp_status pp_embed_fwd(const pp_embed_desc* desc, const int64_t* ids, const void* w, void* y, void* hip_stream);
+pp_status pp_embed_workspace(const pp_embed_desc* desc, size_t* bytes);
+pp_status pp_embed_bwd(const pp_embed_desc* desc, const int64_t* ids, const void* dy, const void* add, void* dw,
+                       void* workspace, size_t ws_bytes, void* hip_stream);
+
+/*
+ * AdamW steps of lists of tensors, for what pp_muon_step is not for (biases,
+ * tables, heads) or in its place:
+ *   g  = grad_scale G
+ *   m' = beta1 m + (1 - beta1) g        v' = beta2 v + (1 - beta2) g^2
+ *   W' = (1 - lr weight_decay) W - lr (m' / (1 - beta1^step)) / (sqrt(v' / (1 - beta2^step)) + eps)
+ * in fp32, whatever the types.  A pruned layer's taps that are off (keep, as for
+ * pp_muon_step) count as 0 in G, and W', m' and v' are 0 there whatever W, m and
+ * v hold.
+ *
+ * The moments of all tensors of a list lie in one array each: tensor i's from
+ * element `at` on, a multiple of PP_ADAMW_BLOCK; what follows them up to the next
+ * multiple is written as 0.  With 32 bits they are fp32.  With 8 bits each
+ * block of PP_ADAMW_BLOCK elements has a scale for each moment, and a code an
+ * element:
+ *   m   e4m3 (OCP, 448 at most), times the block's scale: its largest |m'| / 448
+ *   v   c > 0: r = 2^(q / 16 - 127) (1 + (q mod 16) / 16), q = c + 1777 (whole
+ *       division: 4 bits of the exponent and 4 after the leading one, c = 255
+ *       being 1); c = 0: r = 0; and v = (r times the block's scale)^2, the scale
+ *       being the largest sqrt(v')
+ * rounded to the nearest, ties to even codes.  A v' above 0 has a code of 1 at
+ * least (2^-16 1.125), so that a small second moment is held too large, never as
+ * 0.  A scale is at least 2^-100.  W' is taken from m' and v' before they are
+ * rounded.  An element whose m' is not finite keeps a NaN as m (the others of its
+ * block are held as if it were not there); a v' above fp32's range is held as
+ * its largest value.
+ */
+#define PP_ADAMW_BLOCK 128
+
+typedef struct {
+  int64_t n;                           /* elements; 0: skipped                        */
+  const void* w;                       /* device [n]                                  */
+  const void* g;                       /* device [n]                                  */
+  void* w_out;                         /* device [n]; may be w                        */
+  void* copy;                          /* device bf16 [n]: W' rounded; or NULL        */
+  const uint16_t* keep;                /* device [n / 9] tap masks, or NULL           */
+  int64_t at;                          /* the first element of its moments            */
+  double weight_decay;
+} pp_adamw_tensor;
+
+typedef struct {
+  int32_t w_dtype, g_dtype;            /* pp_dtype of w and w_out, and of g           */
+  int32_t bits;                        /* of the moments: 32 or 8                     */
+  double lr, beta1, beta2, eps;
+  int64_t step;                        /* 1, 2, ...                                   */
+  const float* d_lr;                   /* device, or NULL: read in place of lr        */
+  const int64_t* d_step;               /* device, or NULL: read in place of step (below 1: as 1) */
+  const float* d_grad_scale;           /* device, or NULL for 1                       */
+  const void *m, *v;                   /* device: fp32, or 8-bit codes; 16-byte aligned */
+  const float *m_scale, *v_scale;      /* device, 8 bits: a value a block             */
+  void *m_out, *v_out;                 /* may be m, v                                 */
+  float *m_scale_out, *v_scale_out;    /* may be m_scale, v_scale                     */
+} pp_adamw_desc;
+
+/*
+ * pp_adamw_step -- one step of a list.  Where *d_grad_scale is not finite
+ * (pp_grad_norm of gradients that are not) no step is taken: what is written is
+ * what was read.
+ *   tensors, count  host array (read during the call)
+ * Arrays that are written may overlap no other array of the call, but be their
+ * own input.
+ * pp_adamw_values -- the moments that codes of 8 bits stand for.
+ *   elements  of the arrays, a multiple of PP_ADAMW_BLOCK
+ *   m, v, m_scale, v_scale   as pp_adamw_step left them
+ *   m_out, v_out             device [elements] of dtype; either may be NULL
+ * pp_grad_norm -- the norm of all gradients of a list, and the factor that brings
+ * it to max_norm at most.
+ *   grads, count    host array (read during the call)
+ *   dtype           pp_dtype of the gradients
+ *   max_norm        > 0; INFINITY: the factor is 1
+ *   out             device fp32 [2]: the norm; 1 if it is at most max_norm,
+ *                   max_norm / norm above it, NaN where a gradient is not finite
+ *   workspace       256-byte aligned, pp_grad_norm_workspace() bytes
+ * The squares are summed in 64 bits.
+ * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, places, dtypes, bits,
+ * step, parameters: lr and weight_decay finite, 0 <= beta < 1, 0 <= eps finite),
+ * PP_EUNSUPPORTED (a tensor of 2^40 elements or more, more than 2^31 workgroups),
+ * PP_ESIZE, PP_EHIP.
+ */
+typedef struct {
+  const void* g;                       /* device [n]                                  */
+  int64_t n;
+} pp_grad;
+
+pp_status pp_adamw_step(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_desc* desc, void* hip_stream);
+pp_status pp_adamw_values(const void* m, const void* v, const float* m_scale, const float* v_scale, int64_t elements,
+                          int32_t dtype, void* m_out, void* v_out, void* hip_stream);
+pp_status pp_grad_norm_workspace(const pp_grad* grads, int32_t count, int32_t dtype, size_t* bytes);
+pp_status pp_grad_norm(const pp_grad* grads, int32_t count, int32_t dtype, float max_norm, float* out,
                        void* workspace, size_t ws_bytes, void* hip_stream);
 
 #ifdef __cplusplus

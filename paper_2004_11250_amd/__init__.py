@@ -37,7 +37,8 @@ SYMBOLS = ("pp_pack", "pp_blob_info", "pp_conv2d_fwd", "pp_conv2d_workspace", "p
            "pp_fold_bn", "pp_jit_library", "pp_conv2d_fwd_noalloc", "pp_net_plan", "pp_round_bf16",
            "pp_conv2d_prepare", "pp_conv2d_fwd_prepared", "pp_conv2d_scratch",
            "pp_xent_workspace", "pp_xent_fwd", "pp_xent_bwd", "pp_xent_step", "pp_ortho_workspace", "pp_ortho",
-           "pp_muon_workspace", "pp_muon_step")
+           "pp_muon_workspace", "pp_muon_step", "pp_embed_fwd", "pp_embed_workspace", "pp_embed_bwd", "pp_adamw_step",
+           "pp_adamw_values", "pp_grad_norm_workspace", "pp_grad_norm")
 
 
 class PPError(RuntimeError):
@@ -105,7 +106,8 @@ def load_library(path: str = LIB_PATH):
             fn = getattr(lib, name)
             fn.argtypes = at
             fn.restype = ctypes.c_char_p if name in ("pp_status_str", "pp_last_error") else i32
-    train.bind(lib)
+    for part in (train, embed, adamw):
+        part.bind(lib)
     _lib = lib
     return lib
 
@@ -627,3 +629,6 @@ class Net:
 from . import train   # noqa: E402  (uses the helpers above)
 from .train import (keep_masks, linear_xent_bwd, linear_xent_fwd, linear_xent_step, muon_step,   # noqa: E402,F401
                     orthogonalize)
+from . import adamw, embed   # noqa: E402
+from .adamw import AdamWState, adamw_step, grad_norm   # noqa: E402,F401
+from .embed import embed_bwd, embed_fwd   # noqa: E402,F401

@@ -1,0 +1,272 @@
+"""AdamW steps of lists of tensors, and the norm of their gradients, on torch
+tensors (``pp_adamw_*`` and ``pp_grad_norm`` of ``include/pp.h``).
+
+``AdamWState``   the moments of a list, in 32 bits or in 8
+``adamw_step``   one step of all tensors of the list
+``grad_norm``    the norm of a list of gradients and the factor that clips it
+
+For what ``muon_step`` is not for (biases, tables, heads), or in its place.  Step
+count, learning rate and gradient scale may be tensors on the GPU, so that a
+recorded graph can be replayed with others.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import numpy as np
+
+from . import _check, _torch, load_library
+from .train import _changed, _on, _p, _stream_of
+
+BLOCK = 128     # PP_ADAMW_BLOCK
+
+_TENSOR = np.dtype([("n", "i8"), ("w", "u8"), ("g", "u8"), ("w_out", "u8"), ("copy", "u8"), ("keep", "u8"), ("at", "i8"),
+                    ("weight_decay", "f8")])
+_GRAD = np.dtype([("g", "u8"), ("n", "i8")])
+
+
+class AdamWDesc(ctypes.Structure):
+    _fields_ = [("w_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32), ("bits", ctypes.c_int32), ("lr", ctypes.c_double),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int64),
+                ("d_lr", ctypes.c_void_p), ("d_step", ctypes.c_void_p), ("d_grad_scale", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("m_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p), ("m_scale_out", ctypes.c_void_p),
+                ("v_scale_out", ctypes.c_void_p)]
+
+
+def bind(lib):
+    vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    for name, at in {"pp_adamw_step": [vp, i32, ctypes.POINTER(AdamWDesc), vp],
+                     "pp_adamw_values": [vp, vp, vp, vp, i64, i32, vp, vp, vp],
+                     "pp_grad_norm_workspace": [vp, i32, i32, ctypes.POINTER(sz)],
+                     "pp_grad_norm": [vp, i32, i32, ctypes.c_float, vp, vp, sz, vp]}.items():
+        if hasattr(lib, name):
+            fn = getattr(lib, name)
+            fn.argtypes, fn.restype = at, i32
+
+
+class AdamWState:
+    """The moments of a list of tensors: zeros, before the first step.
+
+    m, v             flat tensors of all moments.  Tensor i's are the elements from
+                     ``places[i]`` on (a multiple of 128), 0 up to the next tensor.
+                     float32 with bits=32; with bits=8 codes, float8_e4m3fn and uint8
+    m_scale, v_scale with bits=8: float32, for each block of 128 codes (else None)
+
+    Saving these four and copying them into a new state continues a run.
+    ``tensors``: the list, or its shapes (then ``device`` says where)."""
+
+    def __init__(self, tensors, bits=32, device=None):
+        torch = _torch()
+        if bits not in (32, 8):
+            raise ValueError(f"bits must be 32 or 8, got {bits}")
+        tensors = [tensors] if torch.is_tensor(tensors) else list(tensors)
+        if not tensors:
+            raise ValueError("tensors is empty")
+        if device is None:
+            device = tensors[0].device if torch.is_tensor(tensors[0]) else torch.device("cuda", torch.cuda.current_device())
+        self.bits = bits
+        self.shapes = [torch.Size(t.shape if torch.is_tensor(t) else t) for t in tensors]
+        self.sizes = [math.prod(s) for s in self.shapes]
+        self.places, at = [], 0
+        for n in self.sizes:
+            self.places.append(at)
+            at += -(-n // BLOCK) * BLOCK
+        self.elements = at
+
+        def zeros(n, dtype):
+            return torch.zeros(n, dtype=torch.uint8, device=device).view(dtype)
+
+        if bits == 32:
+            self.m, self.v = zeros(4 * at, torch.float32), zeros(4 * at, torch.float32)
+            self.m_scale = self.v_scale = None
+        else:
+            self.m, self.v = zeros(at, torch.float8_e4m3fn), zeros(at, torch.uint8)
+            self.m_scale, self.v_scale = (zeros(4 * (at // BLOCK), torch.float32) for _ in range(2))
+
+    def buffers(self):
+        """(m, v, m_scale, v_scale), checked: whoever holds a state may have put others in their places."""
+        torch = _torch()
+        if self.bits == 32:
+            want = ((self.m, torch.float32, self.elements), (self.v, torch.float32, self.elements))
+        else:
+            blocks = self.elements // BLOCK
+            want = ((self.m, torch.float8_e4m3fn, self.elements), (self.v, torch.uint8, self.elements),
+                    (self.m_scale, torch.float32, blocks), (self.v_scale, torch.float32, blocks))
+        for t, dtype, n in want:
+            if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.m.device:
+                raise ValueError(f"the state's buffers must be contiguous, of {n} {dtype} and on one device")
+        return self.m, self.v, self.m_scale, self.v_scale
+
+    def split(self, flat):
+        """Views of a flat tensor of the moments' layout, one in each tensor's shape."""
+        return [flat[a:a + n].view(s) for a, n, s in zip(self.places, self.sizes, self.shapes)]
+
+    def values(self, dtype=None, stream=None):
+        """pp_adamw_values: the moments (m, v) as flat tensors of ``dtype`` (float32
+        if None, or bfloat16).  With bits=32 and float32 they are the state's own."""
+        torch = _torch()
+        dtype = torch.float32 if dtype is None else dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"dtype must be float32 or bfloat16, got {dtype}")
+        m, v, ms, vs = self.buffers()
+        if not m.is_cuda:
+            raise ValueError("the tensors must be on a GPU")
+        if self.bits == 32:
+            with _on(stream, m.device):
+                return m.to(dtype), v.to(dtype)
+        with _stream_of(stream, m.device) as sp:
+            with _on(stream, m.device):
+                out = [torch.empty(self.elements, dtype=dtype, device=m.device) for _ in range(2)]
+            _check(load_library().pp_adamw_values(m.data_ptr(), v.data_ptr(), ms.data_ptr(), vs.data_ptr(), self.elements,
+                                                  int(dtype == torch.bfloat16), out[0].data_ptr(), out[1].data_ptr(), sp),
+                   "pp_adamw_values")
+        return tuple(out)
+
+
+def _list(t):
+    return [t] if _torch().is_tensor(t) else list(t)
+
+
+def _pointers(name, tensors, shapes, dtype, device):
+    """Addresses of a list that fits the state's, checked in few passes: a list may
+    have hundreds of tensors, and each costs the host."""
+    if [t.shape for t in tensors] != shapes:
+        raise ValueError(f"{name} must be of the state's shapes")
+    if {t.dtype for t in tensors} != {dtype} or {t.device for t in tensors} != {device} \
+            or not all([t.is_contiguous() for t in tensors]):
+        raise ValueError(f"{name} must be contiguous {dtype} on the state's device {device}")
+    return [t.data_ptr() for t in tensors]
+
+
+def _scalar(name, t, dtype, device):
+    if t.dtype != dtype or t.numel() != 1 or t.device != device:
+        raise ValueError(f"{name} must be one {dtype} on the state's device")
+    return t.data_ptr()
+
+
+def _own(outs, wp, op, gp):
+    """Outputs are each their own, but an element's weight may be written in place.
+    (By where the tensors begin.)"""
+    at = set(outs)
+    if len(at) != len(outs):
+        raise ValueError("two outputs are the same tensor")
+    if not at.isdisjoint(gp):
+        raise ValueError("an output is another tensor of the call")
+    for w, o in zip(wp, op):
+        if w != o and w in at:
+            raise ValueError("an output is another tensor's input")
+
+
+def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, keep=None, copies=None,
+               grad_scale=None, out=None, stream=None):
+    """pp_adamw_step on a list of tensors (or a single one) and its AdamWState.
+
+    weights and grads: contiguous, of the state's shapes, each list float32 or
+    bfloat16.  ``step`` counts from 1; ``weight_decay``: one number or one a tensor;
+    ``keep``: None, or for each tensor None or the int16 tap masks [c_out][c_in] of
+    a pruned 3x3 layer (keep_masks); ``copies``: bfloat16 tensors that get the new
+    weights, rounded.  ``lr``, ``step`` and ``grad_scale`` (that ``grad_norm``
+    returns) may be tensors of one float32, int64 and float32 on the GPU.  Where
+    grad_scale is not finite no step is taken.
+
+    Updates weights and state in place, or fills ``out`` = (weights, state), and
+    returns them."""
+    torch = _torch()
+    single = torch.is_tensor(weights)
+    weights, grads = _list(weights), _list(grads)
+    if single and keep is not None and torch.is_tensor(keep):
+        keep = [keep]
+    shapes, count = state.shapes, len(state.shapes)
+    if len(weights) != count or len(grads) != count:
+        raise ValueError(f"weights and grads must be of the state's length {count}")
+    bufs = state.buffers()
+    dev, wt, gt = bufs[0].device, weights[0].dtype, grads[0].dtype
+    for name, dt in (("weights", wt), ("grads", gt)):
+        if dt not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
+    table = np.zeros(count, _TENSOR)
+    wp, gp = _pointers("weights", weights, shapes, wt, dev), _pointers("grads", grads, shapes, gt, dev)
+    if out is None:
+        new, state_out, op, bufs_out = weights, state, wp, bufs
+    else:
+        new, state_out = _list(out[0]), out[1]
+        if len(new) != count or state_out.bits != state.bits or state_out.shapes != shapes:
+            raise ValueError("out must be weights and a state of the same shapes and bits")
+        op, bufs_out = _pointers("out weights", new, shapes, wt, dev), state_out.buffers()
+        if bufs_out[0].device != dev:
+            raise ValueError("out must be on the state's device")
+    outs = [p for p, n in zip(op, state.sizes) if n]
+    if copies is not None:
+        copies = _list(copies)
+        if len(copies) != count:
+            raise ValueError(f"copies must be of the state's length {count}")
+        cp = _pointers("copies", copies, shapes, torch.bfloat16, dev)
+        table["copy"] = cp
+        outs += [p for p, n in zip(cp, state.sizes) if n]
+    _own(outs, wp, op, gp)
+    if keep is not None:
+        keep = list(keep)
+        if len(keep) != count:
+            raise ValueError(f"keep must be of the state's length {count}")
+        for i, (k, s) in enumerate(zip(keep, shapes)):
+            if k is None:
+                continue
+            if len(s) < 2 or k.dtype != torch.int16 or tuple(k.shape) != tuple(s[:2]) or state.sizes[i] != 9 * k.numel() \
+                    or not k.is_contiguous() or k.device != dev:
+                raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
+            table["keep"][i] = k.data_ptr()
+    table["n"], table["at"], table["w"], table["g"], table["w_out"] = state.sizes, state.places, wp, gp, op
+    table["weight_decay"] = weight_decay
+    d = AdamWDesc(w_dtype=int(wt == torch.bfloat16), g_dtype=int(gt == torch.bfloat16), bits=state.bits,
+                  beta1=float(betas[0]), beta2=float(betas[1]), eps=float(eps))
+    if torch.is_tensor(lr):
+        d.d_lr = _scalar("lr", lr, torch.float32, dev)
+    else:
+        d.lr = float(lr)
+    if torch.is_tensor(step):
+        d.d_step = _scalar("step", step, torch.int64, dev)
+    else:
+        d.step = int(step)
+    if grad_scale is not None:
+        d.d_grad_scale = _scalar("grad_scale", grad_scale, torch.float32, dev)
+    d.m, d.v, d.m_scale, d.v_scale = (_p(t) for t in bufs)
+    d.m_out, d.v_out, d.m_scale_out, d.v_scale_out = (_p(t) for t in bufs_out)
+    if dev.type != "cuda":
+        raise ValueError("the tensors must be on a GPU")
+    with _stream_of(stream, dev) as sp:
+        _check(load_library().pp_adamw_step(table.ctypes.data, count, ctypes.byref(d), sp), "pp_adamw_step")
+    _changed(new + [t for t in bufs_out if t is not None] + (copies or []))
+    return (new[0], state_out) if single else (new, state_out)
+
+
+def grad_norm(grads, max_norm=None, stream=None):
+    """pp_grad_norm: (norm, scale) of a list of gradients (or one), float32 or
+    bfloat16 and contiguous: the square root of the sum of all squares, and the
+    factor that brings it to ``max_norm`` at most (1 if None; NaN where a gradient
+    is not finite), for adamw_step's ``grad_scale``.  Both stay on the GPU."""
+    torch = _torch()
+    grads = _list(grads)
+    if not grads:
+        raise ValueError("grads is empty")
+    dt, dev = grads[0].dtype, grads[0].device
+    if dt not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"grads must be float32 or bfloat16, got {dt}")
+    most = math.inf if max_norm is None else float(max_norm)
+    if not most > 0:
+        raise ValueError(f"max_norm must be above 0, got {max_norm}")
+    table = np.zeros(len(grads), _GRAD)
+    table["g"] = _pointers("grads", grads, [t.shape for t in grads], dt, dev)
+    table["n"] = [t.numel() for t in grads]
+    if dev.type != "cuda":
+        raise ValueError("the tensors must be on a GPU")
+    code, lib, nb = int(dt == torch.bfloat16), load_library(), ctypes.c_size_t(0)
+    _check(lib.pp_grad_norm_workspace(table.ctypes.data, len(grads), code, ctypes.byref(nb)), "pp_grad_norm_workspace")
+    with _stream_of(stream, dev) as sp:
+        with _on(stream, dev):
+            both = torch.empty(2, dtype=torch.float32, device=dev)
+            ws = torch.empty(max(nb.value, 256), dtype=torch.uint8, device=dev)
+        _check(lib.pp_grad_norm(table.ctypes.data, len(grads), code, most, both.data_ptr(), ws.data_ptr(), ws.numel(), sp),
+               "pp_grad_norm")
+    return both[0], both[1]

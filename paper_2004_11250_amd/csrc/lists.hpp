@@ -1,0 +1,64 @@
+// lists.hpp -- eight values at a time, and lists of tensors brought to a kernel
+// in its arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace pp {
+
+// Eight consecutive values; the hardware loads and stores 16 bytes at any
+// address of the element's own alignment.
+template <class S>
+using Eight = __attribute__((ext_vector_type(8), aligned(sizeof(S)))) S;
+
+// n values from p on (n >= 8: eight), 0 in the place of the others
+template <class S>
+__device__ __forceinline__ void load8(const S* p, int64_t n, float (&v)[8]) {
+  if (n >= 8) {
+    const Eight<S> x = *reinterpret_cast<const Eight<S>*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? static_cast<float>(p[e]) : 0.f;
+  }
+}
+template <class S>
+__device__ __forceinline__ void store8(S* p, int64_t n, const float (&v)[8]) {
+  if (n >= 8) {
+    Eight<S> x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = static_cast<S>(v[e]);
+    *reinterpret_cast<Eight<S>*>(p) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = static_cast<S>(v[e]);
+  }
+}
+
+// A list's tensors in a kernel's arguments (which hold 4 KB), each with the
+// first of its workgroups.
+template <class Item, int N>
+struct List {
+  Item item[N];
+  int32_t first[N];
+  int32_t count;
+};
+// The tensor that workgroup `id` is of; *local: which of its workgroups it is.
+template <class Item, int N>
+__device__ __forceinline__ int find(const List<Item, N>& t, int id, int* local) {
+  int at = -1;
+#pragma unroll
+  for (int i = 0; i < N; i += 64) {
+    const int k = i + (threadIdx.x & 63);
+    at += __popcll(__ballot(k < t.count && t.first[k < N ? k : 0] <= id));
+  }
+  at = __builtin_amdgcn_readfirstlane(at);
+  *local = id - t.first[at];
+  return at;
+}
+
+}  // namespace pp

@@ -911,16 +911,6 @@ pp_status check_size(int64_t rows, int64_t cols) {
   return PP_OK;
 }
 
-template <class F>
-pp_status guarded(F&& f) {
-  clear_error();
-  try {
-    return f();
-  } catch (const std::exception& e) {
-    return fail(PP_EINVAL, std::string("out of host memory: ") + e.what());
-  }
-}
-
 pp_status collect(Plan* p, const pp_ortho_mat* mats, int32_t count, int32_t dtype, bool pointers) {
   if (count < 0 || (count && !mats)) return fail(PP_EINVAL, "mats is NULL");
   if (dtype != PP_F32 && dtype != PP_BF16) return fail(PP_EINVAL, "bad dtype");

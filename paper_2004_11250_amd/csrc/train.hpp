@@ -16,6 +16,17 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t pad64(int64_t n) { return cdiv(n, 64) * 64; }
 inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+// An entry point's body: no exception leaves it.
+template <class F>
+inline pp_status guarded(F&& f) {
+  clear_error();
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return fail(PP_EINVAL, std::string("out of host memory: ") + e.what());
+  }
+}
+
 inline pp_status launched() {
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? PP_OK : fail(PP_EHIP, std::string("launch: ") + hipGetErrorString(e));

@@ -95,6 +95,30 @@ def _on(stream, device):
     return torch.cuda.stream(torch.cuda.ExternalStream(int(stream.cuda_stream), device))
 
 
+class _stream_of:
+    """Context of a call's launches on ``device``, the current one or not: gives the
+    stream's handle (of ``stream``, or of the device's current one)."""
+    __slots__ = ("stream", "device", "guard")
+
+    def __init__(self, stream, device):
+        self.stream, self.device, self.guard = stream, device, None
+
+    def __enter__(self):
+        cuda = _torch().cuda
+        at = self.device.index
+        if self.stream is not None and getattr(self.stream, "device", self.device).index != at:
+            raise ValueError("the stream is of another device than the tensors")
+        if cuda.current_device() != at:
+            self.guard = cuda.device(at)
+            self.guard.__enter__()
+        s = self.stream if self.stream is not None else cuda.current_stream(at)
+        return int(s.cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
 def _changed(tensors):
     """Tell autograd that a call has written these."""
     _torch().autograd.graph.increment_version(tensors)
