@@ -4,9 +4,10 @@
 //   y[t] = scale w[ids[t]],   dw[j] = add[j] + scale sum over t, ids[t] = j, of dy[t]
 //
 // The gradient goes by tokens sorted by id (sort_kernel), so that each row of the
-// table is summed in an order that the ids alone fix, without atomics: a row of up
-// to `piece` tokens by one group of lanes, and a longer one by a workgroup for
-// each `piece` places of the sorted list, whose sums a last kernel adds up.
+// table is summed in an order that the ids alone fix, without atomics, and all
+// workgroups have equally many tokens, however many share a row: sum_kernel goes
+// by pieces of the sorted list, and join_kernel adds up the sums of rows that lie
+// in more than one.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -81,68 +82,80 @@ __global__ __launch_bounds__(256) void look_kernel(const Look a) {
 }
 
 // ---------------------------------------------------------------------------
-// tokens in the order of their ids
+// tokens in the order of their ids, and the rows that have none
 // ---------------------------------------------------------------------------
 
-constexpr int kSortWaves = 16, kSortRows = 1024, kOwn = 256;
+constexpr int kSortWaves = 16, kSortRows = 1024, kOwn = 1024, kOwnBits = 10;
+
+struct Place {
+  int32_t token, row;
+};
 
 struct Sort {
   const int64_t* ids;
   int32_t* start;               // [v + 1]: where each row's tokens begin
-  int32_t* order;               // tokens, by row and then by token
-  int64_t v, ignore;
+  Place* order;                 // tokens, by row and then by token
+  const void* add;
+  void* dw;
+  int64_t w_ld;
+  uint32_t v, ignore;           // (ignore: v where it is no row)
   int32_t t, per;               // rows of the table a workgroup has: kSortRows at most
+  int32_t d, lanes;
 };
 
 // A workgroup has `per` rows of the table and reads all ids: it counts those of
 // rows before its own, which is where its part of the list begins, and puts its
 // own tokens there, all in one launch and without a word from another workgroup.
 // A wave has consecutive tokens; counts by row and wave, summed up, give each wave
-// the places of its tokens of each row, which it then fills in order.
+// the places of its tokens of each row, which it then fills in order.  It also
+// writes the rows without a token.
+template <class W>
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
-  __shared__ uint32_t count[kSortWaves][kSortRows];
-  __shared__ uint2 own[kSortWaves][kOwn];       // token, row: a wave's first ones
+  __shared__ uint32_t count[kSortWaves * kSortRows];
+  __shared__ uint32_t own[kSortWaves][kOwn];    // a wave's first tokens: (token - t0) << 10 | row
   __shared__ uint32_t sums[kSortWaves], belows[kSortWaves];
+  __shared__ bool empty[kSortRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t lo = static_cast<int64_t>(blockIdx.x) * a.per;
-  const int per = static_cast<int>(a.v - lo < a.per ? a.v - lo : a.per);
+  const uint32_t lo = blockIdx.x * static_cast<uint32_t>(a.per);
+  const int per = static_cast<int>(min(a.v - lo, static_cast<uint32_t>(a.per)));
   const uint64_t before = (uint64_t(1) << lane) - 1;
   const int64_t each = (a.t + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
   const int t0 = static_cast<int>(min(each * wave, static_cast<int64_t>(a.t)));
   const int t1 = static_cast<int>(min(each * (wave + 1), static_cast<int64_t>(a.t)));
+  const uint32_t most = t1 - t0 <= 1 << (32 - kOwnBits) ? kOwn : 0u;
 
-  for (int i = threadIdx.x; i < kSortWaves * kSortRows; i += kSortWaves * 64) count[0][i] = 0;
+  for (int i = threadIdx.x; i < kSortWaves * per; i += kSortWaves * 64) count[i] = 0;
   __syncthreads();
 
-  // the row of an id among the workgroup's, or -1; *below: it is of a row before them
-  auto row_of = [&](int64_t id, bool* below) {
-    const bool live = static_cast<uint64_t>(id) < static_cast<uint64_t>(a.v) && id != a.ignore;
-    *below = live && id < lo;
-    return live && id >= lo && id < lo + per ? static_cast<int>(id - lo) : -1;
-  };
-
+  // f(token, row among the workgroup's or -1, whether of a row before them) for
+  // each of a wave's tokens, a lane each
   constexpr int kAtOnce = 4;
-  uint32_t below = 0, mine = 0;
-  for (int t = t0; t < t1; t += 64 * kAtOnce) {
-    int64_t id[kAtOnce];
+  auto each_token = [&](auto&& f) {
+    for (int t = t0 + lane; t - lane < t1; t += 64 * kAtOnce) {
+      int64_t id[kAtOnce];
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) id[u] = t + 64 * u + lane < t1 ? a.ids[t + 64 * u + lane] : a.ignore;
+      for (int u = 0; u < kAtOnce; ++u) id[u] = t + 64 * u < t1 ? a.ids[t + 64 * u] : -1;
 #pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      bool under;
-      const int r = row_of(id[u], &under);
-      below += under;
-      const uint64_t here = __ballot(r >= 0);
-      if (here) {
-        const uint32_t at = mine + __popcll(here & before);
-        if (r >= 0) {
-          atomicAdd(&count[wave][r], 1u);
-          if (at < kOwn) own[wave][at] = {static_cast<uint32_t>(t + 64 * u + lane), static_cast<uint32_t>(r)};
-        }
-        mine += __popcll(here);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const uint32_t i = static_cast<uint32_t>(id[u]);
+        const bool live = (id[u] >> 32) == 0 && i < a.v && i != a.ignore;
+        f(t + 64 * u, live && i - lo < static_cast<uint32_t>(per) ? static_cast<int>(i - lo) : -1, live && i < lo);
       }
     }
-  }
+  };
+  uint32_t below = 0, mine = 0;
+  each_token([&](int t, int r, bool under) {
+    below += under;
+    const uint64_t here = __ballot(r >= 0);
+    if (here) {
+      const uint32_t at = mine + __popcll(here & before);
+      if (r >= 0) {
+        atomicAdd(&count[wave * per + r], 1u);
+        if (at < most) own[wave][at] = static_cast<uint32_t>(t - t0) << kOwnBits | r;
+      }
+      mine += __popcll(here);
+    }
+  });
   for (int d = 32; d; d >>= 1) below += __shfl_xor(below, d);
   if (lane == 0) belows[wave] = below;
   __syncthreads();
@@ -152,7 +165,8 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   uint32_t n = 0;
   if (row < per) {
 #pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) n += count[w][row];
+    for (int w = 0; w < kSortWaves; ++w) n += count[w * per + row];
+    empty[row] = n == 0;
   }
   uint32_t at = n;              // inclusive sum over the wave
   for (int d = 1; d < 64; d <<= 1) {
@@ -173,8 +187,8 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
     uint32_t place = at;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t x = count[w][row];
-      count[w][row] = place;
+      const uint32_t x = count[w * per + row];
+      count[w * per + row] = place;
       place += x;
     }
   }
@@ -184,31 +198,49 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   // a wave's tokens to their places, 64 at a time: a token's place among those of
   // its row is how many of the lanes before it have the same row
   const int bits = 32 - __clz(per - 1);
-  volatile uint32_t* next = count[wave];
-  auto place = [&](int r, uint32_t token) {
+  volatile uint32_t* next = count + wave * per;
+  auto put = [&](int r, int token) {
     uint64_t same = __ballot(r >= 0);
+    if (!same) return;
     for (int b = 0; b < bits; ++b) {
       const uint64_t set = __ballot(r >> b & 1);
       same &= r >> b & 1 ? set : ~set;
     }
     if (r >= 0) {
       const uint32_t base = next[r];
-      a.order[base + __popcll(same & before)] = static_cast<int32_t>(token);
+      a.order[base + __popcll(same & before)] = {token, static_cast<int32_t>(lo) + r};
       if ((same & before) == 0) next[r] = base + __popcll(same);
     }
     __builtin_amdgcn_wave_barrier();
   };
-  if (mine <= kOwn) {
+  if (mine <= most) {
     for (uint32_t i = 0; i < mine; i += 64) {
       const bool on = i + lane < mine;
-      const uint2 x = own[wave][on ? i + lane : 0];
-      place(on ? static_cast<int>(x.y) : -1, x.x);
+      const uint32_t x = own[wave][on ? i + lane : 0];
+      put(on ? static_cast<int>(x & ((1u << kOwnBits) - 1)) : -1, t0 + static_cast<int>(x >> kOwnBits));
     }
   } else {
-    for (int t = t0; t < t1; t += 64) {
-      bool under;
-      const int r = row_of(t + lane < t1 ? a.ids[t + lane] : a.ignore, &under);
-      if (__ballot(r >= 0)) place(r, static_cast<uint32_t>(t + lane));
+    each_token([&](int t, int r, bool) { put(r, t); });
+  }
+
+  // the rows without a token, four of a group of lanes at a time
+  if (a.add == a.dw) return;
+  constexpr int kRows = 4;
+  const int groups = kSortWaves * 64 >> a.lanes, g = threadIdx.x >> a.lanes;
+  for (int c = (threadIdx.x & ((1 << a.lanes) - 1)) * 8; c < a.d; c += 8 << a.lanes) {
+    const int cols = a.d - c;
+    W* dw = static_cast<W*>(a.dw) + lo * a.w_ld + c;
+    const W* add = static_cast<const W*>(a.add) + lo * a.w_ld + c;
+    for (int r = g; r < per; r += kRows * groups) {
+      float x[kRows][8] = {};
+      if (a.add) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+          if (r + u * groups < per && empty[r + u * groups]) load8(add + (r + u * groups) * a.w_ld, cols, x[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kRows; ++u)
+        if (r + u * groups < per && empty[r + u * groups]) store8(dw + (r + u * groups) * a.w_ld, cols, x[u]);
     }
   }
 }
@@ -218,40 +250,20 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
 // ---------------------------------------------------------------------------
 
 struct Sum {
-  const int64_t* ids;
   const int32_t* start;
-  const int32_t* order;
+  const Place* order;
   const void* dy;
   const void* add;
   void* dw;
   float* part;                  // [pieces][2][part_ld]
   int64_t y_ld, w_ld;
-  int32_t v, d, lanes, rows;    // rows: of a group of lanes
-  int32_t piece, pieces, part_ld;
+  int32_t v, d, lanes;
+  int32_t batches, piece;       // of a group of lanes: batches of kBatch tokens; of a workgroup: tokens
+  int32_t part_ld;
   float scale;
 };
 
-// Adds dy's rows order[i], i = i0, i0 + by, .. < i1.
-template <class Y>
-__device__ __forceinline__ void add_rows(const Sum& a, int i0, int i1, int by, int c, float (&acc)[8]) {
-  constexpr int kAtOnce = 4;
-  const int cols = a.d - c;
-  const Y* dy = static_cast<const Y*>(a.dy) + c;
-  for (int i = i0; i < i1; i += kAtOnce * by) {
-    float x[kAtOnce][8];
-    int32_t t[kAtOnce];
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) t[u] = a.order[min(i + u * by, i1 - 1)];
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) load8(dy + t[u] * a.y_ld, cols, x[u]);
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u)
-      if (i + u * by < i1) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
-      }
-  }
-}
+constexpr int kBatch = 8;
 
 template <class W>
 __device__ __forceinline__ void put_row(const Sum& a, int64_t row, int c, const float (&acc)[8]) {
@@ -263,72 +275,109 @@ __device__ __forceinline__ void put_row(const Sum& a, int64_t row, int c, const 
   store8(static_cast<W*>(a.dw) + at, a.d - c, x);
 }
 
-// The first `pieces` workgroups: each its places of the list, for rows of more than
-// `piece` tokens (of which it can hold the end of one, or all, and the beginning of
-// another).  The others: `rows` rows of the table for each group of lanes, but for
-// those.
+// A workgroup sums a piece of the list, a group of lanes a part of it.  A run of
+// one row's tokens that begins and ends inside a group's part is written by the
+// group; a part's first and last run meet their neighbours' in LDS; what goes on
+// past the piece's ends is left for join_kernel: the sum of a run that goes on from
+// the piece before in part[piece][0], of one that begins here in part[piece][1].
 template <class Y, class W>
 __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
-  __shared__ float shared[256 * 8];
+  __shared__ float edge[2 * 256][8];            // [2 group + (not the first run)][lane]
+  __shared__ int32_t edge_row[2 * 256];
+  const int total = a.start[a.v];
+  const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = min(p0 + a.piece, total);
+  if (p0 >= p1) return;
   const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes, lane = threadIdx.x & ((1 << a.lanes) - 1);
-  const int c = ((blockIdx.y << a.lanes) + lane) * 8;
-  if (static_cast<int>(blockIdx.x) >= a.pieces) {
-    if (c >= a.d) return;
-    const int64_t first = (static_cast<int64_t>(blockIdx.x - a.pieces) * groups + g) * a.rows;
-    const int64_t last = min(first + a.rows, static_cast<int64_t>(a.v));
-    if (first >= last) return;
-    int i0 = a.start[first];
-    for (int64_t row = first; row < last; ++row) {
-      const int i1 = a.start[row + 1], n = i1 - i0;
-      if (n <= a.piece && (n > 0 || a.add != a.dw)) {
-        float acc[8] = {};
-        add_rows<Y>(a, i0, i1, 1, c, acc);
-        put_row<W>(a, row, c, acc);
+  const int c = ((blockIdx.y << a.lanes) + lane) * 8, cols = a.d - c;
+  const Y* dy = static_cast<const Y*>(a.dy) + c;
+  const int i0 = p0 + g * a.batches * kBatch, i1 = min(i0 + a.batches * kBatch, p1);
+
+  float acc[8];
+  int cur = -1;
+  bool first = true;
+  auto to_edge = [&](int slot) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) edge[(slot << a.lanes) + lane][e] = acc[e];
+    if (lane == 0) edge_row[slot] = cur;
+  };
+  for (int i = i0; i < i1; i += kBatch) {
+    Place at[kBatch];
+    float x[kBatch][8];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i + u, i1 - 1)];
+    if (cols > 0) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) load8(dy + at[u].token * a.y_ld, cols, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (i + u >= i1) break;
+      if (at[u].row != cur) {
+        if (cur >= 0) {
+          if (first)
+            to_edge(2 * g), first = false;
+          else if (cols > 0)
+            put_row<W>(a, cur, c, acc);
+        }
+        cur = at[u].row;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
       }
-      i0 = i1;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
     }
-    return;
   }
-  const int total = a.start[a.v], i0 = static_cast<int>(blockIdx.x) * a.piece, i1 = min(i0 + a.piece, total);
-  if (i0 >= i1) return;
+  if (lane == 0) {
+    if (first) edge_row[2 * g] = -1;
+    edge_row[2 * g + 1] = -1;
+  }
+  if (cur >= 0) to_edge(2 * g + (first ? 0 : 1));
+  __syncthreads();
+  if (cols <= 0) return;
+
+  // the runs that begin at this group's edges
+  for (int s = 2 * g; s < 2 * g + 2; ++s) {
+    const int32_t row = edge_row[s];
+    if (row < 0) continue;
+    const int32_t prev = s == 0 ? -1 : edge_row[s - 1] >= 0 ? edge_row[s - 1] : s > 1 ? edge_row[s - 2] : -1;
+    if (prev == row) continue;
 #pragma unroll
-  for (int slot = 0; slot < 2; ++slot) {
-    const int64_t row = a.ids[a.order[slot ? i1 - 1 : i0]];
-    const int b = a.start[row], e = a.start[row + 1];
-    if (e - b <= a.piece || (slot && b <= i0)) continue;      // (all of these are the workgroup's)
-    float acc[8] = {};
-    if (c < a.d) add_rows<Y>(a, max(b, i0) + g, min(e, i1), groups, c, acc);
+    for (int e = 0; e < 8; ++e) acc[e] = edge[(s << a.lanes) + lane][e];
+    bool ends = false;          // another run follows in this piece
+    for (int q = s + 1; q < 2 * groups && !ends; ++q) {
+      const int32_t r = edge_row[q];
+      if (r == row) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) shared[threadIdx.x * 8 + k] = acc[k];
-    __syncthreads();
-    if (g == 0 && c < a.d) {
-      for (int q = 1; q < groups; ++q)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) acc[k] += shared[((q << a.lanes) + lane) * 8 + k];
-      store8(a.part + (static_cast<int64_t>(blockIdx.x) * 2 + slot) * a.part_ld + c, 8, acc);
+        for (int e = 0; e < 8; ++e) acc[e] += edge[(q << a.lanes) + lane][e];
+      } else if (r >= 0) {
+        ends = true;
+      }
     }
-    __syncthreads();
+    const bool from = s == 0 && p0 > 0 && a.order[p0 - 1].row == row, on = !ends && p1 < total && a.order[p1].row == row;
+    if (from || on)
+      store8(a.part + (static_cast<int64_t>(blockIdx.x) * 2 + !from) * a.part_ld + c, 8, acc);
+    else
+      put_row<W>(a, row, c, acc);
   }
 }
 
-// Rows of more than `piece` tokens from their pieces' sums: a workgroup for each
-// piece that such a row begins in, and 256 features.
+// Rows whose tokens lie in more than one piece, from the pieces' sums: a workgroup
+// for each piece that such a row may begin in, and 256 features.
 constexpr int kJoinGroups = 16;
 template <class W>
 __global__ __launch_bounds__(kJoinGroups * 64) void join_kernel(const Sum a) {
   using F4 = __attribute__((ext_vector_type(4))) float;
   __shared__ F4 shared[kJoinGroups][64];
-  const int total = a.start[a.v], i0 = static_cast<int>(blockIdx.x) * a.piece, i1 = min(i0 + a.piece, total);
-  if (i0 >= i1) return;
-  const int64_t row = a.ids[a.order[i1 - 1]];
-  const int b = a.start[row], e = a.start[row + 1];
-  if (e - b <= a.piece || b < i0) return;
+  const int total = a.start[a.v], p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = p0 + a.piece;
+  if (p1 >= total) return;
+  const int64_t row = a.order[p1 - 1].row;
+  if (a.order[p1].row != row || a.start[row] < p0) return;
   const int g = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (static_cast<int>(blockIdx.y) * 64 + lane) * 4;
-  const int p0 = blockIdx.x, p1 = (e - 1) / a.piece + 1;
+  const int last = (a.start[row + 1] - 1) / a.piece;
   F4 acc = {0.f, 0.f, 0.f, 0.f};
   if (c < a.d)
-    for (int p = p0 + g; p < p1; p += kJoinGroups)
-      acc += *reinterpret_cast<const F4*>(a.part + (static_cast<int64_t>(p) * 2 + (p == p0 && b > i0)) * a.part_ld + c);
+    for (int p = static_cast<int>(blockIdx.x) + g; p <= last; p += kJoinGroups)
+      acc += *reinterpret_cast<const F4*>(a.part + (static_cast<int64_t>(p) * 2 + (p == static_cast<int>(blockIdx.x))) * a.part_ld + c);
   shared[g][lane] = acc;
   __syncthreads();
   if (g > 0 || c >= a.d) return;
@@ -363,16 +412,21 @@ pp_status check(const pp_embed_desc* desc) {
   return PP_OK;
 }
 
-// Tokens of a piece: at least 32, and at most 1024 pieces.
+// Tokens of a group's part: kBatch, or as many times that as keep the pieces
+// to kPieces.
+constexpr int64_t kPieces = 2048;
 struct Plan {
-  int32_t piece = 0, pieces = 0, part_ld = 0;
+  Lanes lanes;
+  int32_t batches = 1, piece = 0, pieces = 0, part_ld = 0;
   size_t order = 0, part = 0, total = 0;
 };
 Plan plan_of(const pp_embed_desc& d) {
   Plan p;
-  p.piece = 32;
-  while (static_cast<int64_t>(p.piece) * 1024 < d.t) p.piece *= 2;
-  p.pieces = d.t > p.piece ? static_cast<int32_t>(cdiv(d.t, p.piece)) : 0;   // (no row can have more)
+  p.lanes = lanes_for(d.d);
+  const int64_t groups = 256 >> p.lanes.log;
+  p.batches = static_cast<int32_t>(std::max<int64_t>(1, cdiv(d.t, groups * kBatch * kPieces)));
+  p.piece = static_cast<int32_t>(groups) * kBatch * p.batches;
+  p.pieces = static_cast<int32_t>(cdiv(d.t, p.piece));
   p.part_ld = static_cast<int32_t>(cdiv(d.d, 8) * 8);
   auto take = [&](int64_t n) {
     const size_t at = p.total;
@@ -380,8 +434,8 @@ Plan plan_of(const pp_embed_desc& d) {
     return at;
   };
   take(4 * (d.v + 1));
-  p.order = take(4 * d.t);
-  p.part = take(static_cast<int64_t>(p.pieces) * 2 * p.part_ld * 4);
+  p.order = take(static_cast<int64_t>(sizeof(Place)) * d.t);
+  p.part = take(p.pieces > 1 ? static_cast<int64_t>(p.pieces) * 2 * p.part_ld * 4 : 0);
   return p;
 }
 
@@ -420,23 +474,24 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   if (bytes < p.total) return fail(PP_ESIZE, "workspace smaller than needed");
   uint8_t* base = static_cast<uint8_t*>(ws);
   int32_t* start = reinterpret_cast<int32_t*>(base);
-  int32_t* order = reinterpret_cast<int32_t*>(base + p.order);
+  Place* order = reinterpret_cast<Place*>(base + p.order);
 
   // as many workgroups as CUs, or more where a workgroup's rows would be too many
   const int64_t per = std::min<int64_t>(kSortRows, cdiv(d.v, kCUs));
-  const Sort s = {ids, start, order, d.v, d.ignore_index, static_cast<int32_t>(d.t), static_cast<int32_t>(per)};
-  hipLaunchKernelGGL(sort_kernel, dim3(static_cast<uint32_t>(cdiv(d.v, per))), dim3(kSortWaves * 64), 0, st, s);
-
-  const Lanes l = lanes_for(d.d);
-  const int64_t groups = 256 >> l.log;
-  const int64_t rows = std::min<int64_t>(8, std::max<int64_t>(1, d.v / (groups * 4096)));
-  const Sum a = {ids,    start,  order, dy,      add,      dw,        reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.v),
-                 static_cast<int32_t>(d.d), l.log, static_cast<int32_t>(rows), p.piece, p.pieces, p.part_ld, d.scale};
-  const dim3 grid(static_cast<uint32_t>(p.pieces + cdiv(d.v, groups * rows)), static_cast<uint32_t>(l.columns));
+  const bool row = d.ignore_index >= 0 && d.ignore_index < d.v;
+  const Sort s = {ids, start, order, add, dw, d.w_ld, static_cast<uint32_t>(d.v), static_cast<uint32_t>(row ? d.ignore_index : d.v),
+                  static_cast<int32_t>(d.t), static_cast<int32_t>(per), static_cast<int32_t>(d.d), p.lanes.log};
+  const Sum a = {start, order, dy, add, dw, reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.v),
+                 static_cast<int32_t>(d.d), p.lanes.log, p.batches, p.piece, p.part_ld, d.scale};
+  const dim3 sorts(static_cast<uint32_t>(cdiv(d.v, per)));
+  const dim3 sums(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(p.lanes.columns));
   const dim3 joins(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(cdiv(d.d, 256)));
   with_types(d.y_dtype, d.w_dtype, [&](auto yt, auto wt) {
-    hipLaunchKernelGGL((sum_kernel<decltype(yt), decltype(wt)>), grid, dim3(256), 0, st, a);
-    if (p.pieces) hipLaunchKernelGGL((join_kernel<decltype(wt)>), joins, dim3(kJoinGroups * 64), 0, st, a);
+    using Y = decltype(yt);
+    using W = decltype(wt);
+    hipLaunchKernelGGL((sort_kernel<W>), sorts, dim3(kSortWaves * 64), 0, st, s);
+    if (p.pieces) hipLaunchKernelGGL((sum_kernel<Y, W>), sums, dim3(256), 0, st, a);
+    if (p.pieces > 1) hipLaunchKernelGGL((join_kernel<W>), joins, dim3(kJoinGroups * 64), 0, st, a);
   });
   return launched();
 }
