@@ -85,78 +85,125 @@ __global__ __launch_bounds__(256) void look_kernel(const Look a) {
 // tokens in the order of their ids, and the rows that have none
 // ---------------------------------------------------------------------------
 
-constexpr int kSortWaves = 16, kSortRows = 1024, kOwn = 1024, kOwnBits = 10;
+constexpr int kSortWaves = 16, kOwnBits = 10, kSortRows = 1 << kOwnBits, kSortWords = 2400;
 
 struct Place {
   int32_t token, row;
 };
 
+// Rows are dealt to 2^log workgroups, 2^run consecutive ones at a time, so that
+// rows that occur often, which tend to lie together, come to different ones.
+struct Deal {
+  int32_t log, run, per;        // per: rows of a workgroup, kSortRows at most
+  __device__ __forceinline__ uint32_t group(uint32_t row) const { return row >> run & ((1u << log) - 1); }
+  __device__ __forceinline__ uint32_t local(uint32_t row) const { return (row >> (run + log)) << run | (row & ((1u << run) - 1)); }
+  __device__ __forceinline__ uint32_t row(uint32_t group, uint32_t local) const {
+    return (local >> run) << (run + log) | group << run | (local & ((1u << run) - 1));
+  }
+  // where a row's entry of `start` is
+  __device__ __forceinline__ int64_t at(uint32_t row) const { return static_cast<int64_t>(group(row)) * per + local(row); }
+  __host__ __device__ int64_t entries() const { return (static_cast<int64_t>(per) << log) + 1; }
+};
+
 struct Sort {
   const int64_t* ids;
-  int32_t* start;               // [v + 1]: where each row's tokens begin
-  Place* order;                 // tokens, by row and then by token
+  int32_t* start;               // [deal.entries()]: where each row's tokens begin
+  Place* order;                 // tokens, by row (in the order of `start`)
   const void* add;
   void* dw;
   int64_t w_ld;
   uint32_t v, ignore;           // (ignore: v where it is no row)
-  int32_t t, per;               // rows of the table a workgroup has: kSortRows at most
-  int32_t d, lanes;
+  int32_t t, d, lanes;
+  Deal deal;
 };
 
-// A workgroup has `per` rows of the table and reads all ids: it counts those of
-// rows before its own, which is where its part of the list begins, and puts its
+// A workgroup has its rows of the table and reads all ids: it counts those of the
+// workgroups before it, which is where its part of the list begins, and puts its
 // own tokens there, all in one launch and without a word from another workgroup.
 // A wave has consecutive tokens; counts by row and wave, summed up, give each wave
 // the places of its tokens of each row, which it then fills in order.  It also
 // writes the rows without a token.
 template <class W>
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
-  __shared__ uint32_t count[kSortWaves * kSortRows];
-  __shared__ uint32_t own[kSortWaves][kOwn];    // a wave's first tokens: (token - t0) << 10 | row
+  // for each wave a count of each row's tokens, then a list of tokens:
+  // (token - base) << kOwnBits | row
+  __shared__ uint32_t words[kSortWaves * kSortWords];
   __shared__ uint32_t sums[kSortWaves], belows[kSortWaves];
   __shared__ bool empty[kSortRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t lo = blockIdx.x * static_cast<uint32_t>(a.per);
-  const int per = static_cast<int>(min(a.v - lo, static_cast<uint32_t>(a.per)));
+  const uint32_t me = blockIdx.x;
+  const Deal deal = a.deal;
+  const int per = deal.per;
   const uint64_t before = (uint64_t(1) << lane) - 1;
   const int64_t each = (a.t + kSortWaves * 64 - 1) / (kSortWaves * 64) * 64;
   const int t0 = static_cast<int>(min(each * wave, static_cast<int64_t>(a.t)));
   const int t1 = static_cast<int>(min(each * (wave + 1), static_cast<int64_t>(a.t)));
-  const uint32_t most = t1 - t0 <= 1 << (32 - kOwnBits) ? kOwn : 0u;
-
+  uint32_t* count = words;
+  uint32_t* own = words + kSortWaves * per + wave * (kSortWords - per);
+  const uint32_t most = kSortWords - per;
   for (int i = threadIdx.x; i < kSortWaves * per; i += kSortWaves * 64) count[i] = 0;
   __syncthreads();
 
-  // f(token, row among the workgroup's or -1, whether of a row before them) for
-  // each of a wave's tokens, a lane each
-  constexpr int kAtOnce = 4;
-  auto each_token = [&](auto&& f) {
-    for (int t = t0 + lane; t - lane < t1; t += 64 * kAtOnce) {
-      int64_t id[kAtOnce];
+  // All of a wave's tokens: those of the workgroup's rows go on a list in LDS, and
+  // `use(list's length, the token that its entries count from)` takes it when it is
+  // full (the last list is left to the caller).
+  constexpr int kAtOnce = 8, kStep = 64 * kAtOnce;
+  uint32_t below = 0, mine = 0;
+  int base = t0;
+  bool whole = true;
+  auto scan = [&](auto&& use, auto first) {
+    mine = 0, base = t0;
+    for (int t = t0; t < t1; t += kStep) {
+      const uint2* p = reinterpret_cast<const uint2*>(a.ids) + t;   // (an id's upper half: y)
+      uint2 id[kAtOnce];
+      if (t + kStep <= t1) {
 #pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) id[u] = t + 64 * u < t1 ? a.ids[t + 64 * u] : -1;
+        for (int u = 0; u < kAtOnce; ++u) id[u] = p[64 * u + lane];
+      } else {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) id[u] = t + 64 * u + lane < t1 ? p[64 * u + lane] : uint2{0u, 1u};
+      }
 #pragma unroll
       for (int u = 0; u < kAtOnce; ++u) {
-        const uint32_t i = static_cast<uint32_t>(id[u]);
-        const bool live = (id[u] >> 32) == 0 && i < a.v && i != a.ignore;
-        f(t + 64 * u, live && i - lo < static_cast<uint32_t>(per) ? static_cast<int>(i - lo) : -1, live && i < lo);
+        const uint32_t i = id[u].x;
+        const bool live = id[u].y == 0 && i < a.v && i != a.ignore;
+        const uint32_t g = live ? deal.group(i) : ~0u;
+        if constexpr (decltype(first)::value) below += __popcll(__ballot(g < me));
+        const uint64_t here = __ballot(g == me);
+        if (here) {
+          if (g == me) own[mine + __popcll(here & before)] = static_cast<uint32_t>(t + 64 * u + lane - base) << kOwnBits | deal.local(i);
+          mine += __popcll(here);
+        }
+      }
+      if (mine > most - kStep || t + 2 * kStep - base > 1 << (32 - kOwnBits)) {
+        use();
+        mine = 0, base = t + kStep, whole = false;
       }
     }
   };
-  uint32_t below = 0, mine = 0;
-  each_token([&](int t, int r, bool under) {
-    below += under;
-    const uint64_t here = __ballot(r >= 0);
-    if (here) {
-      const uint32_t at = mine + __popcll(here & before);
-      if (r >= 0) {
-        atomicAdd(&count[wave * per + r], 1u);
-        if (at < most) own[wave][at] = static_cast<uint32_t>(t - t0) << kOwnBits | r;
+  // f(row, the token's bits of its entry, lanes of the same row) for 64 entries at a
+  // time (a step's lanes add to each row once: additions to one address take turns)
+  const int bits = 32 - __clz(per - 1);
+  auto each_entry = [&](auto&& f) {
+    for (uint32_t i = 0; i < mine; i += 64) {
+      const bool on = i + lane < mine;
+      const uint32_t x = own[on ? i + lane : 0], r = x & (kSortRows - 1);
+      uint64_t same = __ballot(on);
+      for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(r >> b & 1);
+        same &= r >> b & 1 ? set : ~set;
       }
-      mine += __popcll(here);
+      if (on) f(r, x >> kOwnBits, same);
+      __builtin_amdgcn_wave_barrier();
     }
-  });
-  for (int d = 32; d; d >>= 1) below += __shfl_xor(below, d);
+  };
+  auto tally = [&] {
+    each_entry([&](uint32_t r, uint32_t, uint64_t same) {
+      if ((same & before) == 0) atomicAdd(&count[wave * per + r], static_cast<uint32_t>(__popcll(same)));
+    });
+  };
+  scan(tally, std::true_type());
+  tally();
   if (lane == 0) belows[wave] = below;
   __syncthreads();
 
@@ -183,7 +230,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
     all += belows[w] + sums[w];
   }
   if (row < per) {
-    a.start[lo + row] = static_cast<int32_t>(at);
+    a.start[static_cast<int64_t>(me) * per + row] = static_cast<int32_t>(at);
     uint32_t place = at;
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
@@ -192,36 +239,21 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
       place += x;
     }
   }
-  if (row == 0 && lo + per == a.v) a.start[a.v] = static_cast<int32_t>(all);
+  if (row == 0 && me + 1 == gridDim.x) a.start[deal.entries() - 1] = static_cast<int32_t>(all);
   __syncthreads();
 
   // a wave's tokens to their places, 64 at a time: a token's place among those of
   // its row is how many of the lanes before it have the same row
-  const int bits = 32 - __clz(per - 1);
   volatile uint32_t* next = count + wave * per;
-  auto put = [&](int r, int token) {
-    uint64_t same = __ballot(r >= 0);
-    if (!same) return;
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot(r >> b & 1);
-      same &= r >> b & 1 ? set : ~set;
-    }
-    if (r >= 0) {
-      const uint32_t base = next[r];
-      a.order[base + __popcll(same & before)] = {token, static_cast<int32_t>(lo) + r};
-      if ((same & before) == 0) next[r] = base + __popcll(same);
-    }
-    __builtin_amdgcn_wave_barrier();
+  auto place = [&] {
+    each_entry([&](uint32_t r, uint32_t token, uint64_t same) {
+      const uint32_t at = next[r];
+      a.order[at + __popcll(same & before)] = {base + static_cast<int>(token), static_cast<int32_t>(deal.row(me, r))};
+      if ((same & before) == 0) next[r] = at + __popcll(same);
+    });
   };
-  if (mine <= most) {
-    for (uint32_t i = 0; i < mine; i += 64) {
-      const bool on = i + lane < mine;
-      const uint32_t x = own[wave][on ? i + lane : 0];
-      put(on ? static_cast<int>(x & ((1u << kOwnBits) - 1)) : -1, t0 + static_cast<int>(x >> kOwnBits));
-    }
-  } else {
-    each_token([&](int t, int r, bool) { put(r, t); });
-  }
+  if (!whole) scan(place, std::false_type());
+  place();
 
   // the rows without a token, four of a group of lanes at a time
   if (a.add == a.dw) return;
@@ -229,18 +261,23 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   const int groups = kSortWaves * 64 >> a.lanes, g = threadIdx.x >> a.lanes;
   for (int c = (threadIdx.x & ((1 << a.lanes) - 1)) * 8; c < a.d; c += 8 << a.lanes) {
     const int cols = a.d - c;
-    W* dw = static_cast<W*>(a.dw) + lo * a.w_ld + c;
-    const W* add = static_cast<const W*>(a.add) + lo * a.w_ld + c;
-    for (int r = g; r < per; r += kRows * groups) {
+    for (int l = g; l < per; l += kRows * groups) {
       float x[kRows][8] = {};
+      int64_t at[kRows];
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) {
+        const int k = l + u * groups;
+        const uint32_t row = deal.row(me, k);
+        at[u] = k < per && row < a.v && empty[k] ? row * a.w_ld + c : -1;
+      }
       if (a.add) {
 #pragma unroll
         for (int u = 0; u < kRows; ++u)
-          if (r + u * groups < per && empty[r + u * groups]) load8(add + (r + u * groups) * a.w_ld, cols, x[u]);
+          if (at[u] >= 0) load8(static_cast<const W*>(a.add) + at[u], cols, x[u]);
       }
 #pragma unroll
       for (int u = 0; u < kRows; ++u)
-        if (r + u * groups < per && empty[r + u * groups]) store8(dw + (r + u * groups) * a.w_ld, cols, x[u]);
+        if (at[u] >= 0) store8(static_cast<W*>(a.dw) + at[u], cols, x[u]);
     }
   }
 }
@@ -257,7 +294,8 @@ struct Sum {
   void* dw;
   float* part;                  // [pieces][2][part_ld]
   int64_t y_ld, w_ld;
-  int32_t v, d, lanes;
+  int32_t t, d, lanes;
+  Deal deal;
   int32_t batches, piece;       // of a group of lanes: batches of kBatch tokens; of a workgroup: tokens
   int32_t part_ld;
   float scale;
@@ -284,13 +322,19 @@ template <class Y, class W>
 __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
   __shared__ float edge[2 * 256][8];            // [2 group + (not the first run)][lane]
   __shared__ int32_t edge_row[2 * 256];
-  const int total = a.start[a.v];
+  const int total = a.start[a.deal.entries() - 1];
   const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = min(p0 + a.piece, total);
-  if (p0 >= p1) return;
   const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes, lane = threadIdx.x & ((1 << a.lanes) - 1);
   const int c = ((blockIdx.y << a.lanes) + lane) * 8, cols = a.d - c;
   const Y* dy = static_cast<const Y*>(a.dy) + c;
   const int i0 = p0 + g * a.batches * kBatch, i1 = min(i0 + a.batches * kBatch, p1);
+
+  // (the first batch's places do not wait for the total; behind it they hold nothing)
+  Place at[kBatch];
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i0 + u, a.t - 1)];
+  const int32_t prev_row = a.order[max(p0 - 1, 0)].row, next_row = a.order[min(p0 + a.piece, a.t - 1)].row;
+  if (p0 >= p1) return;
 
   float acc[8];
   int cur = -1;
@@ -301,13 +345,14 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
     if (lane == 0) edge_row[slot] = cur;
   };
   for (int i = i0; i < i1; i += kBatch) {
-    Place at[kBatch];
     float x[kBatch][8];
+    if (i > i0) {
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i + u, i1 - 1)];
+      for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i + u, i1 - 1)];
+    }
     if (cols > 0) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) load8(dy + at[u].token * a.y_ld, cols, x[u]);
+      for (int u = 0; u < kBatch; ++u) load8(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols, x[u]);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -353,7 +398,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
         ends = true;
       }
     }
-    const bool from = s == 0 && p0 > 0 && a.order[p0 - 1].row == row, on = !ends && p1 < total && a.order[p1].row == row;
+    const bool from = s == 0 && p0 > 0 && prev_row == row, on = !ends && p1 < total && next_row == row;
     if (from || on)
       store8(a.part + (static_cast<int64_t>(blockIdx.x) * 2 + !from) * a.part_ld + c, 8, acc);
     else
@@ -363,21 +408,37 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
 
 // Rows whose tokens lie in more than one piece, from the pieces' sums: a workgroup
 // for each piece that such a row may begin in, and 256 features.
-constexpr int kJoinGroups = 16;
+constexpr int kJoinGroups = 4;
 template <class W>
 __global__ __launch_bounds__(kJoinGroups * 64) void join_kernel(const Sum a) {
   using F4 = __attribute__((ext_vector_type(4))) float;
   __shared__ F4 shared[kJoinGroups][64];
-  const int total = a.start[a.v], p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = p0 + a.piece;
-  if (p1 >= total) return;
-  const int64_t row = a.order[p1 - 1].row;
-  if (a.order[p1].row != row || a.start[row] < p0) return;
+  const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = p0 + a.piece;
+  if (p1 >= a.t) return;
+  const int total = a.start[a.deal.entries() - 1];
+  const int64_t row = a.order[p1 - 1].row, next = a.order[p1].row;
+  if (p1 >= total || next != row) return;
+  const int64_t at_row = a.deal.at(static_cast<uint32_t>(row));
+  const int b = a.start[at_row], e = a.start[at_row + 1];
+  if (b < p0) return;
   const int g = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (static_cast<int>(blockIdx.y) * 64 + lane) * 4;
-  const int last = (a.start[row + 1] - 1) / a.piece;
+  const int first = blockIdx.x, last = (e - 1) / a.piece;
   F4 acc = {0.f, 0.f, 0.f, 0.f};
-  if (c < a.d)
-    for (int p = static_cast<int>(blockIdx.x) + g; p <= last; p += kJoinGroups)
-      acc += *reinterpret_cast<const F4*>(a.part + (static_cast<int64_t>(p) * 2 + (p == static_cast<int>(blockIdx.x))) * a.part_ld + c);
+  if (c < a.d) {
+    constexpr int kAtOnce = 8;
+    const float* part = a.part + c;
+    for (int p = first + g; p <= last; p += kAtOnce * kJoinGroups) {
+      F4 x[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t q = min(p + u * kJoinGroups, last);
+        x[u] = *reinterpret_cast<const F4*>(part + (2 * q + (q == first)) * a.part_ld);
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        if (p + u * kJoinGroups <= last) acc += x[u];
+    }
+  }
   shared[g][lane] = acc;
   __syncthreads();
   if (g > 0 || c >= a.d) return;
@@ -414,15 +475,25 @@ pp_status check(const pp_embed_desc* desc) {
 
 // Tokens of a group's part: kBatch, or as many times that as keep the pieces
 // to kPieces.
-constexpr int64_t kPieces = 2048;
+constexpr int64_t kPieces = 1024;
 struct Plan {
   Lanes lanes;
+  Deal deal;
   int32_t batches = 1, piece = 0, pieces = 0, part_ld = 0;
   size_t order = 0, part = 0, total = 0;
 };
 Plan plan_of(const pp_embed_desc& d) {
   Plan p;
   p.lanes = lanes_for(d.d);
+  // as many workgroups as CUs, or more where a workgroup's rows would be too many;
+  // of narrow rows some at a time, 256 bytes, so that whole lines of memory are written by one
+  const int64_t bytes = d.d * (d.w_dtype == PP_BF16 ? 2 : 4);
+  p.deal.run = 0, p.deal.log = 0;
+  while (bytes << p.deal.run < 256) ++p.deal.run;
+  const int64_t runs = cdiv(d.v, int64_t(1) << p.deal.run);
+  while (int64_t(1) << p.deal.log < std::min<int64_t>(runs, kCUs) || cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run > kSortRows)
+    ++p.deal.log;
+  p.deal.per = static_cast<int32_t>(cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run);
   const int64_t groups = 256 >> p.lanes.log;
   p.batches = static_cast<int32_t>(std::max<int64_t>(1, cdiv(d.t, groups * kBatch * kPieces)));
   p.piece = static_cast<int32_t>(groups) * kBatch * p.batches;
@@ -433,7 +504,7 @@ Plan plan_of(const pp_embed_desc& d) {
     p.total += static_cast<size_t>(cdiv(n, 256) * 256);
     return at;
   };
-  take(4 * (d.v + 1));
+  take(4 * p.deal.entries());
   p.order = take(static_cast<int64_t>(sizeof(Place)) * d.t);
   p.part = take(p.pieces > 1 ? static_cast<int64_t>(p.pieces) * 2 * p.part_ld * 4 : 0);
   return p;
@@ -476,14 +547,12 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   int32_t* start = reinterpret_cast<int32_t*>(base);
   Place* order = reinterpret_cast<Place*>(base + p.order);
 
-  // as many workgroups as CUs, or more where a workgroup's rows would be too many
-  const int64_t per = std::min<int64_t>(kSortRows, cdiv(d.v, kCUs));
   const bool row = d.ignore_index >= 0 && d.ignore_index < d.v;
   const Sort s = {ids, start, order, add, dw, d.w_ld, static_cast<uint32_t>(d.v), static_cast<uint32_t>(row ? d.ignore_index : d.v),
-                  static_cast<int32_t>(d.t), static_cast<int32_t>(per), static_cast<int32_t>(d.d), p.lanes.log};
-  const Sum a = {start, order, dy, add, dw, reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.v),
-                 static_cast<int32_t>(d.d), p.lanes.log, p.batches, p.piece, p.part_ld, d.scale};
-  const dim3 sorts(static_cast<uint32_t>(cdiv(d.v, per)));
+                  static_cast<int32_t>(d.t), static_cast<int32_t>(d.d), p.lanes.log, p.deal};
+  const Sum a = {start, order, dy, add, dw, reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.t),
+                 static_cast<int32_t>(d.d), p.lanes.log, p.deal, p.batches, p.piece, p.part_ld, d.scale};
+  const dim3 sorts(1u << p.deal.log);
   const dim3 sums(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(p.lanes.columns));
   const dim3 joins(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(cdiv(d.d, 256)));
   with_types(d.y_dtype, d.w_dtype, [&](auto yt, auto wt) {

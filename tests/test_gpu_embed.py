@@ -47,12 +47,20 @@ def ref_fwd(ids, w, scale, dtype, ignore=IGNORE):
 def check_bwd(got, ids, dy, v, scale=1.0, add=None, ignore=IGNORE):
     live = (ids != ignore) & (ids >= 0) & (ids < v)
     at, x = ids[live], dy.reshape(-1, dy.shape[-1])[live.reshape(-1)].double()
-    want = torch.zeros(v, dy.shape[-1], dtype=torch.float64, device="cuda").index_add_(0, at, x) * scale
-    size = torch.zeros_like(want).index_add_(0, at, x.abs()) * abs(scale)
-    n = torch.zeros(v, dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
+    # (sorted, as differences of running sums: many additions to one row are slow in 64 bits)
+    at, order = at.sort(stable=True)
+    ends = torch.searchsorted(at, torch.arange(v + 1, device="cuda"))
+    n = (ends[1:] - ends[:-1]).double()
+
+    def rows(x):
+        x = torch.cat([torch.zeros_like(x[:1]), x]).cumsum(0) if len(x) else torch.zeros(1, x.shape[1], dtype=x.dtype, device="cuda")
+        return torch.where(n[:, None] > 0, x[ends[1:]] - x[ends[:-1]], 0.0)
+
+    want, size = rows(x[order]) * scale, rows(x[order].abs()) * abs(scale)
+    slack = x.abs().sum(0) * abs(scale) * 2.0 ** -44      # (of the running sums: at most 2^-53 of all, 2^9 times over)
     if add is not None:
         want, size = want + add.double(), size + add.double().abs()
-    lim = (n[:, None] + 2) * 2.0 ** -24 * size
+    lim = (n[:, None] + 2) * 2.0 ** -24 * size + slack * (n[:, None] > 0)
     if got.dtype == torch.bfloat16:
         lim = lim + 2.0 ** -8 * (want.abs() + lim)
     bad = ~((got.double() - want).abs() <= lim)
