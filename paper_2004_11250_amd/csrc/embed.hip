@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256) void look_kernel(const Look a) {
 }
 
 // ---------------------------------------------------------------------------
-// tokens in the order of their ids, and the rows that have none
+// tokens in the order of their ids
 // ---------------------------------------------------------------------------
 
 constexpr int kSortWaves = 16, kOwnBits = 10, kSortRows = 1 << kOwnBits, kSortWords = 2400;
@@ -109,11 +109,8 @@ struct Sort {
   const int64_t* ids;
   int32_t* start;               // [deal.entries()]: where each row's tokens begin
   Place* order;                 // tokens, by row (in the order of `start`)
-  const void* add;
-  void* dw;
-  int64_t w_ld;
   uint32_t v, ignore;           // (ignore: v where it is no row)
-  int32_t t, d, lanes;
+  int32_t t;
   Deal deal;
 };
 
@@ -121,15 +118,12 @@ struct Sort {
 // workgroups before it, which is where its part of the list begins, and puts its
 // own tokens there, all in one launch and without a word from another workgroup.
 // A wave has consecutive tokens; counts by row and wave, summed up, give each wave
-// the places of its tokens of each row, which it then fills in order.  It also
-// writes the rows without a token.
-template <class W>
+// the places of its tokens of each row, which it then fills in order.
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   // for each wave a count of each row's tokens, then a list of tokens:
   // (token - base) << kOwnBits | row
   __shared__ uint32_t words[kSortWaves * kSortWords];
   __shared__ uint32_t sums[kSortWaves], belows[kSortWaves];
-  __shared__ bool empty[kSortRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t me = blockIdx.x;
   const Deal deal = a.deal;
@@ -213,7 +207,6 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   if (row < per) {
 #pragma unroll
     for (int w = 0; w < kSortWaves; ++w) n += count[w * per + row];
-    empty[row] = n == 0;
   }
   uint32_t at = n;              // inclusive sum over the wave
   for (int d = 1; d < 64; d <<= 1) {
@@ -254,32 +247,6 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   };
   if (!whole) scan(place, std::false_type());
   place();
-
-  // the rows without a token, four of a group of lanes at a time
-  if (a.add == a.dw) return;
-  constexpr int kRows = 4;
-  const int groups = kSortWaves * 64 >> a.lanes, g = threadIdx.x >> a.lanes;
-  for (int c = (threadIdx.x & ((1 << a.lanes) - 1)) * 8; c < a.d; c += 8 << a.lanes) {
-    const int cols = a.d - c;
-    for (int l = g; l < per; l += kRows * groups) {
-      float x[kRows][8] = {};
-      int64_t at[kRows];
-#pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        const int k = l + u * groups;
-        const uint32_t row = deal.row(me, k);
-        at[u] = k < per && row < a.v && empty[k] ? row * a.w_ld + c : -1;
-      }
-      if (a.add) {
-#pragma unroll
-        for (int u = 0; u < kRows; ++u)
-          if (at[u] >= 0) load8(static_cast<const W*>(a.add) + at[u], cols, x[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < kRows; ++u)
-        if (at[u] >= 0) store8(static_cast<W*>(a.dw) + at[u], cols, x[u]);
-    }
-  }
 }
 
 // ---------------------------------------------------------------------------
@@ -294,9 +261,9 @@ struct Sum {
   void* dw;
   float* part;                  // [pieces][2][part_ld]
   int64_t y_ld, w_ld;
-  int32_t t, d, lanes;
+  int32_t t, v, d, lanes;
   Deal deal;
-  int32_t batches, piece;       // of a group of lanes: batches of kBatch tokens; of a workgroup: tokens
+  int32_t pieces, batches, piece;       // of a group of lanes: batches of kBatch tokens; of a workgroup: tokens
   int32_t part_ld;
   float scale;
 };
@@ -313,7 +280,35 @@ __device__ __forceinline__ void put_row(const Sum& a, int64_t row, int c, const 
   store8(static_cast<W*>(a.dw) + at, a.d - c, x);
 }
 
-// A workgroup sums a piece of the list, a group of lanes a part of it.  A run of
+// Rows without a token, of kFillRows a group of lanes: what they are added to.
+constexpr int kFillRows = 8;
+template <class W>
+__device__ __forceinline__ void fill_rows(const Sum& a, int block) {
+  const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes;
+  const int c = ((blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1))) * 8, cols = a.d - c;
+  if (cols <= 0) return;
+  const int64_t first = static_cast<int64_t>(block) * groups * kFillRows + g;
+  int64_t at[kFillRows];
+#pragma unroll
+  for (int u = 0; u < kFillRows; ++u) {
+    const int64_t row = first + u * groups, i = a.deal.at(static_cast<uint32_t>(min(row, static_cast<int64_t>(a.v - 1))));
+    at[u] = a.start[i] == a.start[i + 1] && row < a.v ? row * a.w_ld + c : -1;
+  }
+#pragma unroll
+  for (int h = 0; h < kFillRows; h += 4) {
+    float x[4][8] = {};
+    if (a.add) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (at[h + u] >= 0) load8(static_cast<const W*>(a.add) + at[h + u], cols, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (at[h + u] >= 0) store8(static_cast<W*>(a.dw) + at[h + u], cols, x[u]);
+  }
+}
+
+// The first `pieces` workgroups: a workgroup sums a piece of the list, a group of lanes a part of it.  A run of
 // one row's tokens that begins and ends inside a group's part is written by the
 // group; a part's first and last run meet their neighbours' in LDS; what goes on
 // past the piece's ends is left for join_kernel: the sum of a run that goes on from
@@ -322,6 +317,10 @@ template <class Y, class W>
 __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
   __shared__ float edge[2 * 256][8];            // [2 group + (not the first run)][lane]
   __shared__ int32_t edge_row[2 * 256];
+  if (static_cast<int>(blockIdx.x) >= a.pieces) {
+    fill_rows<W>(a, static_cast<int>(blockIdx.x) - a.pieces);
+    return;
+  }
   const int total = a.start[a.deal.entries() - 1];
   const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = min(p0 + a.piece, total);
   const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes, lane = threadIdx.x & ((1 << a.lanes) - 1);
@@ -548,18 +547,19 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   Place* order = reinterpret_cast<Place*>(base + p.order);
 
   const bool row = d.ignore_index >= 0 && d.ignore_index < d.v;
-  const Sort s = {ids, start, order, add, dw, d.w_ld, static_cast<uint32_t>(d.v), static_cast<uint32_t>(row ? d.ignore_index : d.v),
-                  static_cast<int32_t>(d.t), static_cast<int32_t>(d.d), p.lanes.log, p.deal};
+  const Sort s = {ids, start, order, static_cast<uint32_t>(d.v), static_cast<uint32_t>(row ? d.ignore_index : d.v),
+                  static_cast<int32_t>(d.t), p.deal};
   const Sum a = {start, order, dy, add, dw, reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.t),
-                 static_cast<int32_t>(d.d), p.lanes.log, p.deal, p.batches, p.piece, p.part_ld, d.scale};
-  const dim3 sorts(1u << p.deal.log);
-  const dim3 sums(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(p.lanes.columns));
+                 static_cast<int32_t>(d.v), static_cast<int32_t>(d.d), p.lanes.log, p.deal, p.pieces, p.batches, p.piece, p.part_ld, d.scale};
+  // (a gradient that is added to in place: rows without a token stay as they are)
+  const int64_t fills = add == dw ? 0 : cdiv(d.v, (256 >> p.lanes.log) * kFillRows);
+  const dim3 sums(static_cast<uint32_t>(p.pieces + fills), static_cast<uint32_t>(p.lanes.columns));
   const dim3 joins(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(cdiv(d.d, 256)));
   with_types(d.y_dtype, d.w_dtype, [&](auto yt, auto wt) {
     using Y = decltype(yt);
     using W = decltype(wt);
-    hipLaunchKernelGGL((sort_kernel<W>), sorts, dim3(kSortWaves * 64), 0, st, s);
-    if (p.pieces) hipLaunchKernelGGL((sum_kernel<Y, W>), sums, dim3(256), 0, st, a);
+    hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
+    if (sums.x) hipLaunchKernelGGL((sum_kernel<Y, W>), sums, dim3(256), 0, st, a);
     if (p.pieces > 1) hipLaunchKernelGGL((join_kernel<W>), joins, dim3(kJoinGroups * 64), 0, st, a);
   });
   return launched();
