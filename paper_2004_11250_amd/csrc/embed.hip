@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void look_kernel(const Look a) {
   const int cols = a.d - c;
   if (cols <= 0) return;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * groups * kLookRows + g;
-  float x[kLookRows][8];
+  Eight<W> x[kLookRows];
   int64_t id[kLookRows];
 #pragma unroll
   for (int u = 0; u < kLookRows; ++u) {
@@ -62,21 +62,20 @@ __global__ __launch_bounds__(256) void look_kernel(const Look a) {
   for (int u = 0; u < kLookRows; ++u) {
     const bool in = static_cast<uint64_t>(id[u]) < static_cast<uint64_t>(a.v);
     if (in && id[u] != a.ignore) {
-      load8(static_cast<const W*>(a.w) + id[u] * a.w_ld + c, cols, x[u]);
+      x[u] = get8(static_cast<const W*>(a.w) + id[u] * a.w_ld + c, cols);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[u][e] = id[u] == a.ignore ? 0.f : __builtin_nanf("");
+      for (int e = 0; e < 8; ++e) x[u][e] = static_cast<W>(id[u] == a.ignore ? 0.f : __builtin_nanf(""));
     }
   }
 #pragma unroll
   for (int u = 0; u < kLookRows; ++u) {
     const int64_t t = first + u * groups;
     if (t < a.t) {
-      if (id[u] != a.ignore) {
+      float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[u][e] *= a.scale;
-      }
-      store8(static_cast<Y*>(a.y) + t * a.y_ld + c, cols, x[u]);
+      for (int e = 0; e < 8; ++e) y[e] = id[u] == a.ignore ? 0.f : a.scale * static_cast<float>(x[u][e]);
+      store8(static_cast<Y*>(a.y) + t * a.y_ld + c, cols, y);
     }
   }
 }
@@ -296,15 +295,15 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
   }
 #pragma unroll
   for (int h = 0; h < kFillRows; h += 4) {
-    float x[4][8] = {};
+    Eight<W> x[4] = {};
     if (a.add) {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (at[h + u] >= 0) load8(static_cast<const W*>(a.add) + at[h + u], cols, x[u]);
+        if (at[h + u] >= 0) x[u] = get8<true>(static_cast<const W*>(a.add) + at[h + u], cols);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (at[h + u] >= 0) store8(static_cast<W*>(a.dw) + at[h + u], cols, x[u]);
+      if (at[h + u] >= 0) put8<true>(static_cast<W*>(a.dw) + at[h + u], cols, x[u]);
   }
 }
 
@@ -344,14 +343,14 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
     if (lane == 0) edge_row[slot] = cur;
   };
   for (int i = i0; i < i1; i += kBatch) {
-    float x[kBatch][8];
+    Eight<Y> x[kBatch];
     if (i > i0) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i + u, i1 - 1)];
     }
     if (cols > 0) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) load8(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols, x[u]);
+      for (int u = 0; u < kBatch; ++u) x[u] = get8<true>(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -368,7 +367,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
+      for (int e = 0; e < 8; ++e) acc[e] += static_cast<float>(x[u][e]);
     }
   }
   if (lane == 0) {

@@ -13,30 +13,47 @@ namespace pp {
 template <class S>
 using Eight = __attribute__((ext_vector_type(8), aligned(sizeof(S)))) S;
 
-// n values from p on (n >= 8: eight), 0 in the place of the others
-template <class S>
-__device__ __forceinline__ void load8(const S* p, int64_t n, float (&v)[8]) {
+// n values from p on (n >= 8: eight), 0 in the place of the others.  ONCE: they
+// are not read again soon, and take no room in the caches.
+template <bool ONCE = false, class S>
+__device__ __forceinline__ Eight<S> get8(const S* p, int64_t n) {
   if (n >= 8) {
-    const Eight<S> x = *reinterpret_cast<const Eight<S>*>(p);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? static_cast<float>(p[e]) : 0.f;
+    const Eight<S>* q = reinterpret_cast<const Eight<S>*>(p);
+    if constexpr (ONCE) return __builtin_nontemporal_load(q);
+    return *q;
   }
-}
-template <class S>
-__device__ __forceinline__ void store8(S* p, int64_t n, const float (&v)[8]) {
-  if (n >= 8) {
-    Eight<S> x;
+  Eight<S> x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = static_cast<S>(v[e]);
-    *reinterpret_cast<Eight<S>*>(p) = x;
+  for (int e = 0; e < 8; ++e) x[e] = e < n ? p[e] : static_cast<S>(0.f);
+  return x;
+}
+template <bool ONCE = false, class S>
+__device__ __forceinline__ void put8(S* p, int64_t n, const Eight<S>& x) {
+  if (n >= 8) {
+    Eight<S>* q = reinterpret_cast<Eight<S>*>(p);
+    if constexpr (ONCE)
+      __builtin_nontemporal_store(x, q);
+    else
+      *q = x;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (e < n) p[e] = static_cast<S>(v[e]);
+      if (e < n) p[e] = x[e];
   }
+}
+// the same by way of fp32
+template <bool ONCE = false, class S>
+__device__ __forceinline__ void load8(const S* p, int64_t n, float (&v)[8]) {
+  const Eight<S> x = get8<ONCE>(p, n);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
+}
+template <bool ONCE = false, class S>
+__device__ __forceinline__ void store8(S* p, int64_t n, const float (&v)[8]) {
+  Eight<S> x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = static_cast<S>(v[e]);
+  put8<ONCE>(p, n, x);
 }
 
 // A list's tensors in a kernel's arguments (which hold 4 KB), each with the
