@@ -17,7 +17,7 @@ import math
 import numpy as np
 
 from . import _check, _torch, load_library
-from .train import _changed, _on, _p, _stream_of
+from .train import _changed, _empty, _on, _p, _stream_of
 
 BLOCK = 128     # PP_ADAMW_BLOCK
 
@@ -117,8 +117,7 @@ class AdamWState:
             with _on(stream, m.device):
                 return m.to(dtype), v.to(dtype)
         with _stream_of(stream, m.device) as sp:
-            with _on(stream, m.device):
-                out = [torch.empty(self.elements, dtype=dtype, device=m.device) for _ in range(2)]
+            out = [_empty(self.elements, dtype, m.device, stream) for _ in range(2)]
             _check(load_library().pp_adamw_values(m.data_ptr(), v.data_ptr(), ms.data_ptr(), vs.data_ptr(), self.elements,
                                                   int(dtype == torch.bfloat16), out[0].data_ptr(), out[1].data_ptr(), sp),
                    "pp_adamw_values")
@@ -129,15 +128,16 @@ def _list(t):
     return [t] if _torch().is_tensor(t) else list(t)
 
 
-def _pointers(name, tensors, shapes, dtype, device):
+def _pointers(name, tensors, dtype, device, shapes=None):
     """Addresses of a list that fits the state's, checked in few passes: a list may
     have hundreds of tensors, and each costs the host."""
-    if [t.shape for t in tensors] != shapes:
+    tensor = _torch().Tensor
+    if shapes is not None and [t.shape for t in tensors] != shapes:
         raise ValueError(f"{name} must be of the state's shapes")
-    if {t.dtype for t in tensors} != {dtype} or {t.device for t in tensors} != {device} \
-            or not all([t.is_contiguous() for t in tensors]):
-        raise ValueError(f"{name} must be contiguous {dtype} on the state's device {device}")
-    return [t.data_ptr() for t in tensors]
+    there = set(map(tensor.get_device, tensors)) == {device.index} if device.type == "cuda" else {t.device for t in tensors} == {device}
+    if not there or {t.dtype for t in tensors} != {dtype} or not all(map(tensor.is_contiguous, tensors)):
+        raise ValueError(f"{name} must be contiguous {dtype} on one device, {device}")
+    return list(map(tensor.data_ptr, tensors))
 
 
 def _scalar(name, t, dtype, device):
@@ -154,9 +154,8 @@ def _own(outs, wp, op, gp):
         raise ValueError("two outputs are the same tensor")
     if not at.isdisjoint(gp):
         raise ValueError("an output is another tensor of the call")
-    for w, o in zip(wp, op):
-        if w != o and w in at:
-            raise ValueError("an output is another tensor's input")
+    if any(w != o and w in at for w, o in zip(wp, op)):
+        raise ValueError("an output is another tensor's input")
 
 
 def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, keep=None, copies=None,
@@ -187,24 +186,24 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
         if dt not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
     table = np.zeros(count, _TENSOR)
-    wp, gp = _pointers("weights", weights, shapes, wt, dev), _pointers("grads", grads, shapes, gt, dev)
+    wp, gp = _pointers("weights", weights, wt, dev, shapes), _pointers("grads", grads, gt, dev, shapes)
     if out is None:
         new, state_out, op, bufs_out = weights, state, wp, bufs
     else:
         new, state_out = _list(out[0]), out[1]
         if len(new) != count or state_out.bits != state.bits or state_out.shapes != shapes:
             raise ValueError("out must be weights and a state of the same shapes and bits")
-        op, bufs_out = _pointers("out weights", new, shapes, wt, dev), state_out.buffers()
+        op, bufs_out = _pointers("out weights", new, wt, dev, shapes), state_out.buffers()
         if bufs_out[0].device != dev:
             raise ValueError("out must be on the state's device")
-    outs = [p for p, n in zip(op, state.sizes) if n]
+    outs = [p for p, n in zip(op, state.sizes) if n] if 0 in state.sizes else list(op)
     if copies is not None:
         copies = _list(copies)
         if len(copies) != count:
             raise ValueError(f"copies must be of the state's length {count}")
-        cp = _pointers("copies", copies, shapes, torch.bfloat16, dev)
+        cp = _pointers("copies", copies, torch.bfloat16, dev, shapes)
         table["copy"] = cp
-        outs += [p for p, n in zip(cp, state.sizes) if n]
+        outs += [p for p, n in zip(cp, state.sizes) if n] if 0 in state.sizes else cp
     _own(outs, wp, op, gp)
     if keep is not None:
         keep = list(keep)
@@ -257,16 +256,15 @@ def grad_norm(grads, max_norm=None, stream=None):
     if not most > 0:
         raise ValueError(f"max_norm must be above 0, got {max_norm}")
     table = np.zeros(len(grads), _GRAD)
-    table["g"] = _pointers("grads", grads, [t.shape for t in grads], dt, dev)
-    table["n"] = [t.numel() for t in grads]
+    table["g"] = _pointers("grads", grads, dt, dev)
+    table["n"] = list(map(torch.Tensor.numel, grads))
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     code, lib, nb = int(dt == torch.bfloat16), load_library(), ctypes.c_size_t(0)
     _check(lib.pp_grad_norm_workspace(table.ctypes.data, len(grads), code, ctypes.byref(nb)), "pp_grad_norm_workspace")
     with _stream_of(stream, dev) as sp:
-        with _on(stream, dev):
-            both = torch.empty(2, dtype=torch.float32, device=dev)
-            ws = torch.empty(max(nb.value, 256), dtype=torch.uint8, device=dev)
+        both = _empty(2, torch.float32, dev, stream)
+        ws = _empty(max(nb.value, 256), torch.uint8, dev, stream)
         _check(lib.pp_grad_norm(table.ctypes.data, len(grads), code, most, both.data_ptr(), ws.data_ptr(), ws.numel(), sp),
                "pp_grad_norm")
-    return both[0], both[1]
+    return both.unbind()

@@ -25,6 +25,8 @@ constexpr int kBlock = PP_ADAMW_BLOCK;   // elements that share their scales: 16
 constexpr float kTiny = 0x1p-100f;       // the least scale
 constexpr int kFirstCode = 1777;         // v: code c stands for the float whose bits are (c + 1777) << 19
 
+using Codes = __attribute__((ext_vector_type(2))) uint32_t;
+
 struct Tensor {
   const void* w;
   const void* g;
@@ -80,7 +82,7 @@ __device__ __forceinline__ uint32_t code_of(float r) {
 }
 __device__ __forceinline__ float value_of(uint32_t c) { return __builtin_bit_cast(float, c ? (c + kFirstCode) << 19 : 0u); }
 
-__device__ __forceinline__ void m_values(uint2 c, float s, float (&m)[8]) {
+__device__ __forceinline__ void m_values(Codes c, float s, float (&m)[8]) {
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int w = h ? c.y : c.x;
@@ -88,7 +90,7 @@ __device__ __forceinline__ void m_values(uint2 c, float s, float (&m)[8]) {
     m[4 * h] = a[0] * s, m[4 * h + 1] = a[1] * s, m[4 * h + 2] = b[0] * s, m[4 * h + 3] = b[1] * s;
   }
 }
-__device__ __forceinline__ void v_values(uint2 c, float s, float (&v)[8]) {
+__device__ __forceinline__ void v_values(Codes c, float s, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float r = value_of(((e < 4 ? c.x : c.y) >> (8 * (e & 3))) & 255u) * s;
@@ -107,8 +109,24 @@ __device__ __forceinline__ uint32_t kept8(const uint16_t* keep, int64_t cell, in
   return bits >> (y - 9u * k);
 }
 
+template <bool ONCE>
+__device__ __forceinline__ Codes codes8(const void* p, int64_t at) {
+  const Codes* q = reinterpret_cast<const Codes*>(static_cast<const uint8_t*>(p) + at);
+  if constexpr (ONCE) return __builtin_nontemporal_load(q);
+  return *q;
+}
+template <bool ONCE>
+__device__ __forceinline__ void put_codes8(void* p, int64_t at, Codes c) {
+  Codes* q = reinterpret_cast<Codes*>(static_cast<uint8_t*>(p) + at);
+  if constexpr (ONCE)
+    __builtin_nontemporal_store(c, q);
+  else
+    *q = c;
+}
+
 template <class W, class G, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const Step s) {
+  constexpr bool ONCE = BITS == 8;
   int chunk;
   const Tensor& t = list.item[find(list, blockIdx.x, &chunk)];
   const int64_t e0 = static_cast<int64_t>(chunk) * s.chunk, n = t.n, left = n - e0;
@@ -119,7 +137,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
   bf16* copy = t.copy ? t.copy + e0 : nullptr;
   const int64_t at = t.at + e0, block = at / kBlock;
   const uint16_t* keep = t.keep;
-  const int64_t cell = e0 / 9, cells = n / 9;
+  const int64_t cell = keep ? e0 / 9 : 0, cells = keep ? n / 9 : 0;
   const int tap = static_cast<int>(e0 - 9 * cell);
 
   const float scale = s.d_scale ? *s.d_scale : 1.f;
@@ -138,16 +156,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
   for (int x = 8 * threadIdx.x; x < len; x += 2048) {
     const int64_t there = left - x;     // elements from here on
     float w[8], g[8], m[8], v[8];
-    uint2 mc, vc;
+    Codes mc, vc;
     float ms, vs;
-    load8(w_in + x, there, w);
-    load8(g_in + x, there, g);
+    load8<ONCE>(w_in + x, there, w);
+    load8<ONCE>(g_in + x, there, g);
     if constexpr (BITS == 32) {
-      load8(static_cast<const float*>(s.m) + at + x, 8, m);
-      load8(static_cast<const float*>(s.v) + at + x, 8, v);
+      load8<ONCE>(static_cast<const float*>(s.m) + at + x, 8, m);
+      load8<ONCE>(static_cast<const float*>(s.v) + at + x, 8, v);
     } else {
-      mc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.m) + at + x);
-      vc = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.v) + at + x);
+      mc = codes8<ONCE>(s.m, at + x);
+      vc = codes8<ONCE>(s.v, at + x);
       ms = s.ms[block + x / kBlock], vs = s.vs[block + x / kBlock];
     }
     const uint32_t on = keep ? kept8(keep, cell, tap, cells, x) : 255u;
@@ -190,15 +208,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       }
     }
     if (there > 0) {
-      store8(w_out + x, there, w);
-      if (copy) store8(copy + x, there, w);
+      store8<ONCE>(w_out + x, there, w);
+      if (copy) store8<ONCE>(copy + x, there, w);
     }
     if constexpr (BITS == 32) {
-      store8(static_cast<float*>(s.m_out) + at + x, 8, m);
-      store8(static_cast<float*>(s.v_out) + at + x, 8, v);
+      store8<ONCE>(static_cast<float*>(s.m_out) + at + x, 8, m);
+      store8<ONCE>(static_cast<float*>(s.v_out) + at + x, 8, v);
     } else {
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(s.m_out) + at + x) = mc;
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(s.v_out) + at + x) = vc;
+      put_codes8<ONCE>(s.m_out, at + x, mc);
+      put_codes8<ONCE>(s.v_out, at + x, vc);
       if (threadIdx.x % 16 == 0) s.ms_out[block + x / kBlock] = ms, s.vs_out[block + x / kBlock] = vs;
     }
   }
@@ -211,11 +229,11 @@ __global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const uin
   for (int64_t x = 8 * (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x); x < all; x += static_cast<int64_t>(gridDim.x) * 2048) {
     float a[8];
     if (m_out) {
-      m_values(*reinterpret_cast<const uint2*>(m + x), ms[x / kBlock], a);
+      m_values(codes8<false>(m, x), ms[x / kBlock], a);
       store8(m_out + x, 8, a);
     }
     if (v_out) {
-      v_values(*reinterpret_cast<const uint2*>(v + x), vs[x / kBlock], a);
+      v_values(codes8<false>(v, x), vs[x / kBlock], a);
       store8(v_out + x, 8, a);
     }
   }
@@ -291,7 +309,10 @@ pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill,
   constexpr int N = sizeof(L::first) / 4;
   L list;
   std::memset(&list, 0, sizeof(list));
-  int64_t blocks = 0;
+  // (of equal length: a short one would leave the card idle)
+  int64_t live = 0, blocks = 0;
+  for (int32_t i = 0; i < count; ++i) live += tensors[i].n != 0;
+  const int64_t most = live ? cdiv(live, cdiv(live, N)) : N;
   auto flush = [&]() -> pp_status {
     if (!list.count) return PP_OK;
     go(list, static_cast<uint32_t>(blocks));
@@ -301,7 +322,7 @@ pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill,
   for (int32_t i = 0; i < count; ++i) {
     if (tensors[i].n == 0) continue;
     const int64_t b = cdiv(tensors[i].n, per);
-    if (list.count == N || blocks + b > (1 << 30)) {
+    if (list.count == most || blocks + b > (1 << 30)) {
       const pp_status s = flush();
       if (s != PP_OK) return s;
     }
@@ -364,7 +385,7 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   s.d_lr = d.d_lr, s.d_step = d.d_step, s.d_scale = d.d_grad_scale;
   s.m = d.m, s.v = d.v, s.ms = d.m_scale, s.vs = d.v_scale;
   s.m_out = d.m_out, s.v_out = d.v_out, s.ms_out = d.m_scale_out, s.vs_out = d.v_scale_out;
-  s.chunk = chunk_of(total, 8192);
+  s.chunk = chunk_of(total, d.bits == 8 ? 4096 : 2048);
   auto fill = [](Tensor& x, const pp_adamw_tensor& t) {
     x = {t.w, t.g, t.w_out, static_cast<bf16*>(t.copy), t.keep, t.n, t.at, static_cast<float>(t.weight_decay)};
   };

@@ -13,7 +13,7 @@ import ctypes
 import functools
 
 from . import _check, _dtype_code, _torch, load_library
-from .train import _changed, _on, _p, _stream_of
+from .train import _changed, _empty, _p, _stream_of
 
 
 class EmbedDesc(ctypes.Structure):
@@ -55,7 +55,7 @@ def _rows(t, name, shape, device):
     if t.device != device:
         raise ValueError(f"{name} must be on the ids' device")
     d = shape[-1]
-    if t.numel() == 0:
+    if t.numel() == 0 or t.is_contiguous():
         return d
     if d > 1 and t.stride(-1) != 1:
         raise ValueError(f"the rows of {name} must be contiguous")
@@ -104,8 +104,7 @@ def embed_fwd(ids, w, scale=1.0, ignore_index=-100, dtype=None, out=None, stream
     given = out is not None
     with _stream_of(stream, ids.device) as sp:
         if not given:
-            with _on(stream, ids.device):
-                out = torch.empty(shape, dtype=torch.bfloat16 if yc else torch.float32, device=ids.device)
+            out = _empty(shape, torch.bfloat16 if yc else torch.float32, ids.device, stream)
         _check(load_library().pp_embed_fwd(ctypes.byref(desc), ids.data_ptr(), w.data_ptr(), out.data_ptr(), sp),
                "pp_embed_fwd")
     if given:
@@ -155,11 +154,10 @@ def embed_bwd(ids, dy, v, scale=1.0, ignore_index=-100, dtype=None, add=None, ou
     desc = EmbedDesc(wc, yc, ids.numel(), int(v), d, w_ld or d, y_ld, int(ignore_index), float(scale))
     given = out is not None
     with _stream_of(stream, ids.device) as sp:
-        with _on(stream, ids.device):
-            if not given:
-                out = torch.empty(shape, dtype=torch.bfloat16 if wc else torch.float32, device=ids.device)
-            nb = _bytes(bytes(desc))
-            ws = torch.empty(nb, dtype=torch.uint8, device=ids.device)
+        if not given:
+            out = _empty(shape, torch.bfloat16 if wc else torch.float32, ids.device, stream)
+        nb = _bytes(bytes(desc))
+        ws = _empty(nb, torch.uint8, ids.device, stream)
         _check(load_library().pp_embed_bwd(ctypes.byref(desc), ids.data_ptr(), dy.data_ptr(), _p(add), out.data_ptr(),
                                            ws.data_ptr(), nb, sp), "pp_embed_bwd")
     if given:
