@@ -13,31 +13,24 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import numpy as np
 
 from . import _check, _torch, load_library
-from .train import _changed, _empty, _on, _p, _stream_of
+from .train import _changed, _empty, _on, _stream_of
 
 BLOCK = 128     # PP_ADAMW_BLOCK
 
-_TENSOR = np.dtype([("n", "i8"), ("w", "u8"), ("g", "u8"), ("w_out", "u8"), ("copy", "u8"), ("keep", "u8"), ("at", "i8"),
-                    ("weight_decay", "f8")])
-_GRAD = np.dtype([("g", "u8"), ("n", "i8")])
-
-
-class AdamWDesc(ctypes.Structure):
-    _fields_ = [("w_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32), ("bits", ctypes.c_int32), ("lr", ctypes.c_double),
-                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int64),
-                ("d_lr", ctypes.c_void_p), ("d_step", ctypes.c_void_p), ("d_grad_scale", ctypes.c_void_p),
-                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
-                ("m_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p), ("m_scale_out", ctypes.c_void_p),
-                ("v_scale_out", ctypes.c_void_p)]
+# pp_adamw_tensor (as eight words), pp_adamw_desc and pp_grad as the library lays them out
+_TENSOR = ("n", "w", "g", "w_out", "copy", "keep", "at", "weight_decay")
+_N, _W, _G, _W_OUT, _COPY, _KEEP, _AT, _DECAY = range(8)
+_DESC = struct.Struct("@3i4dq11Q")
 
 
 def bind(lib):
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-    for name, at in {"pp_adamw_step": [vp, i32, ctypes.POINTER(AdamWDesc), vp],
+    for name, at in {"pp_adamw_step": [vp, i32, vp, vp],
                      "pp_adamw_values": [vp, vp, vp, vp, i64, i32, vp, vp, vp],
                      "pp_grad_norm_workspace": [vp, i32, i32, ctypes.POINTER(sz)],
                      "pp_grad_norm": [vp, i32, i32, ctypes.c_float, vp, vp, sz, vp]}.items():
@@ -74,6 +67,9 @@ class AdamWState:
             self.places.append(at)
             at += -(-n // BLOCK) * BLOCK
         self.elements = at
+        # the list as the library takes it, without addresses
+        self._table = np.zeros((len(self.sizes), len(_TENSOR)), np.int64)
+        self._table[:, _N], self._table[:, _AT] = self.sizes, self.places
 
         def zeros(n, dtype):
             return torch.zeros(n, dtype=torch.uint8, device=device).view(dtype)
@@ -87,17 +83,17 @@ class AdamWState:
 
     def buffers(self):
         """(m, v, m_scale, v_scale), checked: whoever holds a state may have put others in their places."""
-        torch = _torch()
+        torch, n, blocks = _torch(), self.elements, self.elements // BLOCK
+        got = (self.m, self.v, self.m_scale, self.v_scale)
         if self.bits == 32:
-            want = ((self.m, torch.float32, self.elements), (self.v, torch.float32, self.elements))
+            want = ((torch.float32, n), (torch.float32, n))
         else:
-            blocks = self.elements // BLOCK
-            want = ((self.m, torch.float8_e4m3fn, self.elements), (self.v, torch.uint8, self.elements),
-                    (self.m_scale, torch.float32, blocks), (self.v_scale, torch.float32, blocks))
-        for t, dtype, n in want:
-            if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != self.m.device:
+            want = ((torch.float8_e4m3fn, n), (torch.uint8, n), (torch.float32, blocks), (torch.float32, blocks))
+        device = self.m.device
+        for t, (dtype, n) in zip(got, want):
+            if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
                 raise ValueError(f"the state's buffers must be contiguous, of {n} {dtype} and on one device")
-        return self.m, self.v, self.m_scale, self.v_scale
+        return got
 
     def split(self, flat):
         """Views of a flat tensor of the moments' layout, one in each tensor's shape."""
@@ -185,7 +181,7 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
     for name, dt in (("weights", wt), ("grads", gt)):
         if dt not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
-    table = np.zeros(count, _TENSOR)
+    table = state._table.copy()
     wp, gp = _pointers("weights", weights, wt, dev, shapes), _pointers("grads", grads, gt, dev, shapes)
     if out is None:
         new, state_out, op, bufs_out = weights, state, wp, bufs
@@ -202,7 +198,7 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
         if len(copies) != count:
             raise ValueError(f"copies must be of the state's length {count}")
         cp = _pointers("copies", copies, torch.bfloat16, dev, shapes)
-        table["copy"] = cp
+        table[:, _COPY] = cp
         outs += [p for p, n in zip(cp, state.sizes) if n] if 0 in state.sizes else cp
     _own(outs, wp, op, gp)
     if keep is not None:
@@ -215,27 +211,18 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
             if len(s) < 2 or k.dtype != torch.int16 or tuple(k.shape) != tuple(s[:2]) or state.sizes[i] != 9 * k.numel() \
                     or not k.is_contiguous() or k.device != dev:
                 raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
-            table["keep"][i] = k.data_ptr()
-    table["n"], table["at"], table["w"], table["g"], table["w_out"] = state.sizes, state.places, wp, gp, op
-    table["weight_decay"] = weight_decay
-    d = AdamWDesc(w_dtype=int(wt == torch.bfloat16), g_dtype=int(gt == torch.bfloat16), bits=state.bits,
-                  beta1=float(betas[0]), beta2=float(betas[1]), eps=float(eps))
-    if torch.is_tensor(lr):
-        d.d_lr = _scalar("lr", lr, torch.float32, dev)
-    else:
-        d.lr = float(lr)
-    if torch.is_tensor(step):
-        d.d_step = _scalar("step", step, torch.int64, dev)
-    else:
-        d.step = int(step)
-    if grad_scale is not None:
-        d.d_grad_scale = _scalar("grad_scale", grad_scale, torch.float32, dev)
-    d.m, d.v, d.m_scale, d.v_scale = (_p(t) for t in bufs)
-    d.m_out, d.v_out, d.m_scale_out, d.v_scale_out = (_p(t) for t in bufs_out)
+            table[i, _KEEP] = k.data_ptr()
+    table[:, _W], table[:, _G], table[:, _W_OUT] = wp, gp, op
+    table.view(np.float64)[:, _DECAY] = weight_decay
+    d_lr = _scalar("lr", lr, torch.float32, dev) if torch.is_tensor(lr) else 0
+    d_step = _scalar("step", step, torch.int64, dev) if torch.is_tensor(step) else 0
+    d_scale = 0 if grad_scale is None else _scalar("grad_scale", grad_scale, torch.float32, dev)
+    desc = _DESC.pack(int(wt == torch.bfloat16), int(gt == torch.bfloat16), state.bits, 0.0 if d_lr else lr, betas[0], betas[1], eps,
+                      0 if d_step else int(step), d_lr, d_step, d_scale, *[t.data_ptr() if t is not None else 0 for t in bufs + bufs_out])
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     with _stream_of(stream, dev) as sp:
-        _check(load_library().pp_adamw_step(table.ctypes.data, count, ctypes.byref(d), sp), "pp_adamw_step")
+        _check(load_library().pp_adamw_step(table.ctypes.data, count, desc, sp), "pp_adamw_step")
     _changed(new + [t for t in bufs_out if t is not None] + (copies or []))
     return (new[0], state_out) if single else (new, state_out)
 
@@ -255,9 +242,8 @@ def grad_norm(grads, max_norm=None, stream=None):
     most = math.inf if max_norm is None else float(max_norm)
     if not most > 0:
         raise ValueError(f"max_norm must be above 0, got {max_norm}")
-    table = np.zeros(len(grads), _GRAD)
-    table["g"] = _pointers("grads", grads, dt, dev)
-    table["n"] = list(map(torch.Tensor.numel, grads))
+    table = np.empty((len(grads), 2), np.int64)      # (pp_grad: address, elements)
+    table[:, 0], table[:, 1] = _pointers("grads", grads, dt, dev), list(map(torch.Tensor.numel, grads))
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     code, lib, nb = int(dt == torch.bfloat16), load_library(), ctypes.c_size_t(0)

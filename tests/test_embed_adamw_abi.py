@@ -65,8 +65,27 @@ def test_embed_calls(lib):
     assert lib.pp_embed_fwd(ctypes.byref(desc(t=0)), None, None, None, None) == pp.PP_OK
 
 
+TENSOR = np.dtype([("n", "i8"), ("w", "u8"), ("g", "u8"), ("w_out", "u8"), ("copy", "u8"), ("keep", "u8"), ("at", "i8"),
+                   ("weight_decay", "f8")])
+GRAD = np.dtype([("g", "u8"), ("n", "i8")])
+
+
+class AdamWDesc(ctypes.Structure):
+    _fields_ = [("w_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32), ("bits", ctypes.c_int32), ("lr", ctypes.c_double),
+                ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int64),
+                ("d_lr", ctypes.c_void_p), ("d_step", ctypes.c_void_p), ("d_grad_scale", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("m_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p), ("m_scale_out", ctypes.c_void_p),
+                ("v_scale_out", ctypes.c_void_p)]
+
+
+def test_layouts():
+    assert ctypes.sizeof(AdamWDesc) == adamw._DESC.size and TENSOR.itemsize == 8 * len(adamw._TENSOR)
+    assert TENSOR.names == adamw._TENSOR
+
+
 def table(count=1, **kw):
-    t = np.zeros(count, adamw._TENSOR)
+    t = np.zeros(count, TENSOR)
     t["n"], t["w"], t["g"], t["w_out"] = 100, A, A, A
     for k, v in kw.items():
         t[k] = v
@@ -74,8 +93,8 @@ def table(count=1, **kw):
 
 
 def step(lib, t, count=None, **kw):
-    d = adamw.AdamWDesc(w_dtype=0, g_dtype=0, bits=32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, m=A, v=A, m_out=A, v_out=A,
-                        m_scale=A, v_scale=A, m_scale_out=A, v_scale_out=A)
+    d = AdamWDesc(w_dtype=0, g_dtype=0, bits=32, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, m=A, v=A, m_out=A, v_out=A,
+                  m_scale=A, v_scale=A, m_scale_out=A, v_scale_out=A)
     for k, v in kw.items():
         setattr(d, k, v)
     return lib.pp_adamw_step(None if t is None else t.ctypes.data, len(t) if count is None else count, ctypes.byref(d), None)
@@ -112,7 +131,7 @@ def test_values_calls(lib):
 
 
 def test_norm_calls(lib):
-    t = np.zeros(2, adamw._GRAD)
+    t = np.zeros(2, GRAD)
     t["g"], t["n"] = A, 1000
     nb = ctypes.c_size_t(0)
     assert lib.pp_grad_norm_workspace(t.ctypes.data, 2, 0, ctypes.byref(nb)) == pp.PP_OK and nb.value >= 16
