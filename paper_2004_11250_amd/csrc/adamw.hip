@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
     float w[8], g[8], m[8], v[8];
     Codes mc, vc;
     float ms, vs;
-    load8<ONCE>(w_in + x, there, w);
-    load8<ONCE>(g_in + x, there, g);
+    load8<ONCE && sizeof(W) == 2>(w_in + x, there, w);
+    load8<ONCE && sizeof(G) == 2>(g_in + x, there, g);
     if constexpr (BITS == 32) {
       load8<ONCE>(static_cast<const float*>(s.m) + at + x, 8, m);
       load8<ONCE>(static_cast<const float*>(s.v) + at + x, 8, v);
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       }
     }
     if (there > 0) {
-      store8<ONCE>(w_out + x, there, w);
+      store8<ONCE && sizeof(W) == 2>(w_out + x, there, w);
       if (copy) store8<ONCE>(copy + x, there, w);
     }
     if constexpr (BITS == 32) {
@@ -309,10 +309,7 @@ pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill,
   constexpr int N = sizeof(L::first) / 4;
   L list;
   std::memset(&list, 0, sizeof(list));
-  // (of equal length: a short one would leave the card idle)
-  int64_t live = 0, blocks = 0;
-  for (int32_t i = 0; i < count; ++i) live += tensors[i].n != 0;
-  const int64_t most = live ? cdiv(live, cdiv(live, N)) : N;
+  int64_t blocks = 0;
   auto flush = [&]() -> pp_status {
     if (!list.count) return PP_OK;
     go(list, static_cast<uint32_t>(blocks));
@@ -322,7 +319,7 @@ pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill,
   for (int32_t i = 0; i < count; ++i) {
     if (tensors[i].n == 0) continue;
     const int64_t b = cdiv(tensors[i].n, per);
-    if (list.count == most || blocks + b > (1 << 30)) {
+    if (list.count == N || blocks + b > (1 << 30)) {
       const pp_status s = flush();
       if (s != PP_OK) return s;
     }

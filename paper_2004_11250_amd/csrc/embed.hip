@@ -299,40 +299,28 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
     if (a.add) {
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        if (at[h + u] >= 0) x[u] = get8<true>(static_cast<const W*>(a.add) + at[h + u], cols);
+        if (at[h + u] >= 0) x[u] = get8<sizeof(W) == 2>(static_cast<const W*>(a.add) + at[h + u], cols);
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (at[h + u] >= 0) put8<true>(static_cast<W*>(a.dw) + at[h + u], cols, x[u]);
+      if (at[h + u] >= 0) put8<sizeof(W) == 2>(static_cast<W*>(a.dw) + at[h + u], cols, x[u]);
   }
 }
 
-// The first `pieces` workgroups: a workgroup sums a piece of the list, a group of lanes a part of it.  A run of
-// one row's tokens that begins and ends inside a group's part is written by the
-// group; a part's first and last run meet their neighbours' in LDS; what goes on
-// past the piece's ends is left for join_kernel: the sum of a run that goes on from
-// the piece before in part[piece][0], of one that begins here in part[piece][1].
-template <class Y, class W>
-__global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
-  __shared__ float edge[2 * 256][8];            // [2 group + (not the first run)][lane]
-  __shared__ int32_t edge_row[2 * 256];
-  if (static_cast<int>(blockIdx.x) >= a.pieces) {
-    fill_rows<W>(a, static_cast<int>(blockIdx.x) - a.pieces);
-    return;
-  }
-  const int total = a.start[a.deal.entries() - 1];
-  const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = min(p0 + a.piece, total);
-  const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes, lane = threadIdx.x & ((1 << a.lanes) - 1);
+// A workgroup sums the piece p0 .. p1 of a list, a group of lanes a part of it, of
+// `batches` batches of kBatch tokens; `at`: the group's first batch.  A run of one
+// row's tokens that begins and ends inside a group's part is written by the group;
+// a part's first and last run meet their neighbours' in LDS.  What goes on past the
+// piece's ends (row `prev` before it, `next` behind it, -1: none) goes to part: the
+// sum of a run that goes on from the piece before to row 0, of one that begins here
+// to row 1.
+template <class Y, class W, int THREADS>
+__device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int p0, int p1, int batches, Place (&at)[kBatch],
+                                          int32_t prev, int32_t next, float* part, float (*edge)[8], int32_t* edge_row) {
+  const int groups = THREADS >> a.lanes, g = threadIdx.x >> a.lanes, lane = threadIdx.x & ((1 << a.lanes) - 1);
   const int c = ((blockIdx.y << a.lanes) + lane) * 8, cols = a.d - c;
   const Y* dy = static_cast<const Y*>(a.dy) + c;
-  const int i0 = p0 + g * a.batches * kBatch, i1 = min(i0 + a.batches * kBatch, p1);
-
-  // (the first batch's places do not wait for the total; behind it they hold nothing)
-  Place at[kBatch];
-#pragma unroll
-  for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i0 + u, a.t - 1)];
-  const int32_t prev_row = a.order[max(p0 - 1, 0)].row, next_row = a.order[min(p0 + a.piece, a.t - 1)].row;
-  if (p0 >= p1) return;
+  const int i0 = p0 + g * batches * kBatch, i1 = min(i0 + batches * kBatch, p1);
 
   float acc[8];
   int cur = -1;
@@ -346,11 +334,11 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
     Eight<Y> x[kBatch];
     if (i > i0) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(i + u, i1 - 1)];
+      for (int u = 0; u < kBatch; ++u) at[u] = order[min(i + u, i1 - 1)];
     }
     if (cols > 0) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) x[u] = get8<true>(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols);
+      for (int u = 0; u < kBatch; ++u) x[u] = get8<sizeof(Y) == 2>(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -382,8 +370,8 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
   for (int s = 2 * g; s < 2 * g + 2; ++s) {
     const int32_t row = edge_row[s];
     if (row < 0) continue;
-    const int32_t prev = s == 0 ? -1 : edge_row[s - 1] >= 0 ? edge_row[s - 1] : s > 1 ? edge_row[s - 2] : -1;
-    if (prev == row) continue;
+    const int32_t left = s == 0 ? -1 : edge_row[s - 1] >= 0 ? edge_row[s - 1] : s > 1 ? edge_row[s - 2] : -1;
+    if (left == row) continue;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = edge[(s << a.lanes) + lane][e];
     bool ends = false;          // another run follows in this piece
@@ -396,11 +384,123 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
         ends = true;
       }
     }
-    const bool from = s == 0 && p0 > 0 && prev_row == row, on = !ends && p1 < total && next_row == row;
+    const bool from = s == 0 && prev == row, on = !ends && next == row;
     if (from || on)
-      store8(a.part + (static_cast<int64_t>(blockIdx.x) * 2 + !from) * a.part_ld + c, 8, acc);
+      store8(part + static_cast<int64_t>(!from) * a.part_ld + c, 8, acc);
     else
       put_row<W>(a, row, c, acc);
+  }
+}
+
+// The first `pieces` workgroups: a piece of the sorted list each.  The others: rows
+// without a token.
+template <class Y, class W>
+__global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
+  __shared__ float edge[2 * 256][8];            // [2 group + (not the first run)][lane]
+  __shared__ int32_t edge_row[2 * 256];
+  if (static_cast<int>(blockIdx.x) >= a.pieces) {
+    fill_rows<W>(a, static_cast<int>(blockIdx.x) - a.pieces);
+    return;
+  }
+  const int total = a.start[a.deal.entries() - 1];
+  const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = min(p0 + a.piece, total);
+  // (the places do not wait for the total; behind it they hold nothing)
+  Place at[kBatch];
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) at[u] = a.order[min(p0 + static_cast<int>(threadIdx.x >> a.lanes) * a.batches * kBatch + u, a.t - 1)];
+  const int32_t prev = a.order[max(p0 - 1, 0)].row, next = a.order[min(p0 + a.piece, a.t - 1)].row;
+  if (p0 >= p1) return;
+  sum_piece<Y, W, 256>(a, a.order, p0, p1, a.batches, at, p0 > 0 ? prev : -1, p1 < total ? next : -1,
+                       a.part + static_cast<int64_t>(blockIdx.x) * 2 * a.part_ld, edge, edge_row);
+}
+
+// Up to kFewTokens tokens: a workgroup has its rows of the table, finds their tokens,
+// a thread an id, sorts them in LDS, sums them, and fills its rows without a token,
+// all in one launch.
+constexpr int kFewTokens = 1024, kFewRanks = 256;
+template <class Y, class W>
+__global__ __launch_bounds__(kFewTokens) void few_kernel(const Sort s, const Sum a) {
+  __shared__ float edge[2 * kFewTokens][8];
+  __shared__ int32_t edge_row[2 * kFewTokens];
+  __shared__ uint32_t keys[kFewTokens];
+  __shared__ Place order[kFewTokens];
+  __shared__ bool found[kSortRows];
+  __shared__ int32_t counts[kFewTokens / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t me = blockIdx.x;
+  const uint2 id = tid < s.t ? reinterpret_cast<const uint2*>(s.ids)[tid] : uint2{0u, 1u};
+  const bool own = id.y == 0 && id.x < s.v && id.x != s.ignore && s.deal.group(id.x) == me;
+  const uint64_t here = __ballot(own);
+  if (lane == 0) counts[wave] = __popcll(here);
+  found[tid] = false;
+  __syncthreads();
+  int n = 0, at = __popcll(here & ((uint64_t(1) << lane) - 1));
+  for (int w = 0; w < kFewTokens / 64; ++w) {
+    at += w < wave ? counts[w] : 0;
+    n += counts[w];
+  }
+  if (own) {
+    keys[at] = s.deal.local(id.x) << kOwnBits | static_cast<uint32_t>(tid);   // (by row, then by token)
+    found[s.deal.local(id.x)] = true;
+  }
+  if (tid >= n) keys[tid] = ~0u;
+  __syncthreads();
+  if (n) {
+    const auto put = [&](int rank, uint32_t key) {
+      order[rank] = {static_cast<int32_t>(key & (kFewTokens - 1)), static_cast<int32_t>(s.deal.row(me, key >> kOwnBits))};
+    };
+    if (n <= kFewRanks) {
+      // a token's place is how many come before it
+      if (tid < n) {
+        const uint32_t mine = keys[tid];
+        int rank = 0;
+        for (int j = 0; j < n; j += 4)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) rank += keys[j + k] < mine;
+        put(rank, mine);
+      }
+    } else {
+      // exchanges in runs that double (n^2 / 256 reads of LDS take longer from here on)
+      for (int run = 2; run < 2 * n; run *= 2)
+        for (int step = run / 2; step > 0; step /= 2) {
+          const int other = tid ^ step;
+          if (other > tid && tid < 2 * n) {
+            const uint32_t x = keys[tid], y = keys[other];
+            if ((x > y) == ((tid & run) == 0)) keys[tid] = y, keys[other] = x;
+          }
+          __syncthreads();
+        }
+      if (tid < n) put(tid, keys[tid]);
+    }
+    __syncthreads();
+    const int groups = kFewTokens >> a.lanes, batches = (n + groups * kBatch - 1) / (groups * kBatch);
+    Place first[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) first[u] = order[min((tid >> a.lanes) * batches * kBatch + u, n - 1)];
+    sum_piece<Y, W, kFewTokens>(a, order, 0, n, batches, first, -1, -1, nullptr, edge, edge_row);
+  }
+
+  if (a.add == a.dw) return;
+  constexpr int kRows = 4;
+  const int groups = kFewTokens >> a.lanes, c = ((blockIdx.y << a.lanes) + (tid & ((1 << a.lanes) - 1))) * 8, cols = a.d - c;
+  if (cols <= 0) return;
+  for (int l = tid >> a.lanes; l < s.deal.per; l += kRows * groups) {
+    Eight<W> x[kRows] = {};
+    int64_t to[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int k = l + u * groups;
+      const uint32_t row = s.deal.row(me, k);
+      to[u] = k < s.deal.per && row < s.v && !found[k] ? row * a.w_ld + c : -1;
+    }
+    if (a.add) {
+#pragma unroll
+      for (int u = 0; u < kRows; ++u)
+        if (to[u] >= 0) x[u] = get8<sizeof(W) == 2>(static_cast<const W*>(a.add) + to[u], cols);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+      if (to[u] >= 0) put8<sizeof(W) == 2>(static_cast<W*>(a.dw) + to[u], cols, x[u]);
   }
 }
 
@@ -554,9 +654,18 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   const int64_t fills = add == dw ? 0 : cdiv(d.v, (256 >> p.lanes.log) * kFillRows);
   const dim3 sums(static_cast<uint32_t>(p.pieces + fills), static_cast<uint32_t>(p.lanes.columns));
   const dim3 joins(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(cdiv(d.d, 256)));
+  // One launch instead of two or three, at the risk that one row has all tokens, whose
+  // features one workgroup then reads (at 100 GB/s).  us a call, one launch / three:
+  // 777 tokens into 5003 x 203 fp32 12 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
+  // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
+  const bool few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
   with_types(d.y_dtype, d.w_dtype, [&](auto yt, auto wt) {
     using Y = decltype(yt);
     using W = decltype(wt);
+    if (few) {
+      hipLaunchKernelGGL((few_kernel<Y, W>), dim3(1u << p.deal.log, static_cast<uint32_t>(p.lanes.columns)), dim3(kFewTokens), 0, st, s, a);
+      return;
+    }
     hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
     if (sums.x) hipLaunchKernelGGL((sum_kernel<Y, W>), sums, dim3(256), 0, st, a);
     if (p.pieces > 1) hipLaunchKernelGGL((join_kernel<W>), joins, dim3(kJoinGroups * 64), 0, st, a);
