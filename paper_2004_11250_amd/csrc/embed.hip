@@ -3,8 +3,8 @@
 //
 //   y[t] = scale w[ids[t]],   dw[j] = add[j] + scale sum over t, ids[t] = j, of dy[t]
 //
-// The gradient goes by tokens sorted by id (sort_kernel), so that each row of the
-// table is summed in an order that the ids alone fix, without atomics, and all
+// The gradient goes by tokens sorted by id (sort_kernel, or count_kernel and
+// place_kernel; few_kernel does all of a small call), so that each row of the table is summed in an order that the ids alone fix, without atomics, and all
 // workgroups have equally many tokens, however many share a row: sum_kernel goes
 // by pieces of the sorted list, and join_kernel adds up the sums of rows that lie
 // in more than one.
@@ -246,6 +246,117 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   };
   if (!whole) scan(place, std::false_type());
   place();
+}
+
+// The same for tables of up to kSortRows rows, without a workgroup that has all
+// tokens of a row: a workgroup has `each` tokens.  The first launch counts its
+// tokens of each row; the second adds up the counts, which gives each workgroup the
+// places of its tokens of each row, and puts them there.
+constexpr int64_t kCounts = 128;                // workgroups at most
+struct Narrow {
+  const int64_t* ids;
+  uint32_t* count;              // [workgroups][v]
+  int32_t* start;               // [v + 1]
+  Place* order;
+  uint32_t v, ignore;
+  int32_t t, each;              // each: a multiple of 1024
+};
+
+// f(token, row or -1) for the tokens of a wave of the workgroup, a lane each
+template <class F>
+__device__ __forceinline__ void wave_tokens(const Narrow& a, F&& f) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = a.each / kSortWaves;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.each + wave * part;
+  const uint2* p = reinterpret_cast<const uint2*>(a.ids) + t0 + lane;
+  const int64_t left = a.t - t0 - lane;
+  for (int i = 0; i < part; i += 64) {
+    const uint2 id = i < left ? p[i] : uint2{0u, 1u};
+    const bool live = id.y == 0 && id.x < a.v && id.x != a.ignore;
+    f(static_cast<int>(t0 + i + lane), live ? static_cast<int>(id.x) : -1);
+  }
+}
+
+__global__ __launch_bounds__(kSortWaves * 64) void count_kernel(const Narrow a) {
+  __shared__ uint32_t count[kSortRows];
+  count[threadIdx.x] = 0;
+  __syncthreads();
+  wave_tokens(a, [&](int, int r) {
+    if (r >= 0) atomicAdd(&count[r], 1u);
+  });
+  __syncthreads();
+  if (threadIdx.x < a.v) a.count[static_cast<int64_t>(blockIdx.x) * a.v + threadIdx.x] = count[threadIdx.x];
+}
+
+__global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Narrow a) {
+  __shared__ uint32_t count[kSortWaves][kSortRows];
+  __shared__ uint32_t sums[kSortWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint64_t before = (uint64_t(1) << lane) - 1;
+  // a thread a row: its tokens in all, and in the workgroups before this one
+  uint32_t n = 0, earlier = 0;
+  if (tid < static_cast<int>(a.v)) {
+    const int groups = gridDim.x;
+    for (int g = 0; g < groups; g += 8) {
+      uint32_t x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = a.count[static_cast<int64_t>(min(g + u, groups - 1)) * a.v + tid];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        n += g + u < groups ? x[u] : 0u;
+        earlier += g + u < static_cast<int>(blockIdx.x) ? x[u] : 0u;
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) count[w][tid] = 0;
+  }
+  uint32_t at = n;              // inclusive sum over the wave
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t x = __shfl_up(at, d);
+    if (lane >= d) at += x;
+  }
+  if (lane == 63) sums[wave] = at;
+  __syncthreads();
+
+  // lanes with the same row
+  const int bits = 32 - __clz(static_cast<int>(a.v) - 1);
+  auto same_row = [&](int r) {
+    uint64_t same = __ballot(r >= 0);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot(r >> b & 1);
+      same &= r >> b & 1 ? set : ~set;
+    }
+    return same;
+  };
+  wave_tokens(a, [&](int, int r) {
+    const uint64_t same = same_row(r);
+    if (r >= 0 && (same & before) == 0) atomicAdd(&count[wave][r], static_cast<uint32_t>(__popcll(same)));
+  });
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) at += sums[w];
+  if (tid < static_cast<int>(a.v)) {
+    if (blockIdx.x == 0) {
+      a.start[tid] = static_cast<int32_t>(at - n);
+      if (tid + 1 == static_cast<int>(a.v)) a.start[a.v] = static_cast<int32_t>(at);
+    }
+    uint32_t place = at - n + earlier;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t x = count[w][tid];
+      count[w][tid] = place;
+      place += x;
+    }
+  }
+  __syncthreads();
+  volatile uint32_t* next = count[wave];
+  wave_tokens(a, [&](int t, int r) {
+    const uint64_t same = same_row(r);
+    if (r >= 0) {
+      const uint32_t place = next[r];
+      a.order[place + __popcll(same & before)] = {t, r};
+      if ((same & before) == 0) next[r] = place + __popcll(same);
+    }
+    __builtin_amdgcn_wave_barrier();
+  });
 }
 
 // ---------------------------------------------------------------------------
@@ -577,21 +688,38 @@ constexpr int64_t kPieces = 1024;
 struct Plan {
   Lanes lanes;
   Deal deal;
-  int32_t batches = 1, piece = 0, pieces = 0, part_ld = 0;
-  size_t order = 0, part = 0, total = 0;
+  bool few, narrow;             // one launch; sorted by count_kernel and place_kernel
+  int32_t batches = 1, piece = 0, pieces = 0, part_ld = 0, each = 0, counts = 0;
+  size_t order = 0, part = 0, count = 0, total = 0;
 };
 Plan plan_of(const pp_embed_desc& d) {
   Plan p;
   p.lanes = lanes_for(d.d);
-  // as many workgroups as CUs, or more where a workgroup's rows would be too many;
-  // of narrow rows some at a time, 256 bytes, so that whole lines of memory are written by one
-  const int64_t bytes = d.d * (d.w_dtype == PP_BF16 ? 2 : 4);
+  // One launch instead of two or three, at the risk that one row has all tokens, whose
+  // features one workgroup then reads (at 100 GB/s).  us a call, one launch / three:
+  // 777 tokens into 5003 x 203 fp32 12 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
+  // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
+  p.few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
+  // The sort in two launches, without a workgroup that has all tokens of a row.  us a
+  // call, one launch / two, 313 rows of 256 bf16 features, ids of which three in ten are
+  // the same: 8192 tokens 17 / 18, 32768 tokens 28 / 22, 2^20 tokens 675 / 132.
+  p.narrow = !p.few && d.v <= kSortRows && d.t > 16384;
+  // Workgroups of sort_kernel and few_kernel: as many as CUs, or more where one's rows
+  // would be too many; of narrow rows some at a time, 256 bytes, so that whole lines of
+  // memory are written by one.
+  const int64_t bytes = d.d * static_cast<int64_t>(size_of(d.w_dtype));
   p.deal.run = 0, p.deal.log = 0;
-  while (bytes << p.deal.run < 256) ++p.deal.run;
-  const int64_t runs = cdiv(d.v, int64_t(1) << p.deal.run);
-  while (int64_t(1) << p.deal.log < std::min<int64_t>(runs, kCUs) || cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run > kSortRows)
-    ++p.deal.log;
-  p.deal.per = static_cast<int32_t>(cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run);
+  if (!p.narrow) {
+    while (bytes << p.deal.run < 256) ++p.deal.run;
+    const int64_t runs = cdiv(d.v, int64_t(1) << p.deal.run);
+    while (int64_t(1) << p.deal.log < std::min<int64_t>(runs, kCUs) || cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run > kSortRows)
+      ++p.deal.log;
+    p.deal.per = static_cast<int32_t>(cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run);
+  } else {
+    p.deal.per = static_cast<int32_t>(d.v);
+    p.each = static_cast<int32_t>(cdiv(d.t, kCounts * 1024) * 1024);
+    p.counts = static_cast<int32_t>(cdiv(d.t, p.each));
+  }
   const int64_t groups = 256 >> p.lanes.log;
   p.batches = static_cast<int32_t>(std::max<int64_t>(1, cdiv(d.t, groups * kBatch * kPieces)));
   p.piece = static_cast<int32_t>(groups) * kBatch * p.batches;
@@ -605,6 +733,7 @@ Plan plan_of(const pp_embed_desc& d) {
   take(4 * p.deal.entries());
   p.order = take(static_cast<int64_t>(sizeof(Place)) * d.t);
   p.part = take(p.pieces > 1 ? static_cast<int64_t>(p.pieces) * 2 * p.part_ld * 4 : 0);
+  p.count = take(4 * static_cast<int64_t>(p.counts) * d.v);
   return p;
 }
 
@@ -654,19 +783,20 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   const int64_t fills = add == dw ? 0 : cdiv(d.v, (256 >> p.lanes.log) * kFillRows);
   const dim3 sums(static_cast<uint32_t>(p.pieces + fills), static_cast<uint32_t>(p.lanes.columns));
   const dim3 joins(static_cast<uint32_t>(p.pieces), static_cast<uint32_t>(cdiv(d.d, 256)));
-  // One launch instead of two or three, at the risk that one row has all tokens, whose
-  // features one workgroup then reads (at 100 GB/s).  us a call, one launch / three:
-  // 777 tokens into 5003 x 203 fp32 12 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
-  // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
-  const bool few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
   with_types(d.y_dtype, d.w_dtype, [&](auto yt, auto wt) {
     using Y = decltype(yt);
     using W = decltype(wt);
-    if (few) {
+    if (p.few) {
       hipLaunchKernelGGL((few_kernel<Y, W>), dim3(1u << p.deal.log, static_cast<uint32_t>(p.lanes.columns)), dim3(kFewTokens), 0, st, s, a);
       return;
     }
-    hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
+    if (p.narrow) {
+      const Narrow f = {ids, reinterpret_cast<uint32_t*>(base + p.count), start, order, s.v, s.ignore, s.t, p.each};
+      hipLaunchKernelGGL(count_kernel, dim3(p.counts), dim3(kSortWaves * 64), 0, st, f);
+      hipLaunchKernelGGL(place_kernel, dim3(p.counts), dim3(kSortWaves * 64), 0, st, f);
+    } else {
+      hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
+    }
     if (sums.x) hipLaunchKernelGGL((sum_kernel<Y, W>), sums, dim3(256), 0, st, a);
     if (p.pieces > 1) hipLaunchKernelGGL((join_kernel<W>), joins, dim3(kJoinGroups * 64), 0, st, a);
   });
