@@ -677,8 +677,9 @@ typedef struct {
  * pp_embed_fwd
  *   ids   device int64 [t]
  *   w, y  device [v][d] and [t][d] (rows w_ld and y_ld apart)
- * pp_embed_workspace -- device bytes pp_embed_bwd needs: about 4 v + 8 t, and up to
- * 2048 rows of d fp32 values for rows of the table that many tokens share.
+ * pp_embed_workspace -- device bytes pp_embed_bwd needs: up to 8 v + 16 t, about
+ * 0.5 MB, and up to 2048 rows of d fp32 values for rows of the table that many
+ * tokens share.
  * pp_embed_bwd
  *   dy         device [t][d]
  *   add        device [v][d], or NULL; may be dw: then only rows that tokens

@@ -4,10 +4,11 @@
 //   y[t] = scale w[ids[t]],   dw[j] = add[j] + scale sum over t, ids[t] = j, of dy[t]
 //
 // The gradient goes by tokens sorted by id (sort_kernel, or count_kernel and
-// place_kernel; few_kernel does all of a small call), so that each row of the table is summed in an order that the ids alone fix, without atomics, and all
-// workgroups have equally many tokens, however many share a row: sum_kernel goes
-// by pieces of the sorted list, and join_kernel adds up the sums of rows that lie
-// in more than one.
+// place_kernel; few_kernel does all of a small call), so that each row of the table
+// is summed in an order that the ids alone fix, without atomics, and all workgroups
+// have equally many tokens, however many share a row: sum_kernel goes by pieces of
+// the sorted list, and join_kernel adds up the sums of rows that lie in more than
+// one.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -248,58 +249,72 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   place();
 }
 
-// The same for tables of up to kSortRows rows, without a workgroup that has all
-// tokens of a row: a workgroup has `each` tokens.  The first launch counts its
-// tokens of each row; the second adds up the counts, which gives each workgroup the
-// places of its tokens of each row, and puts them there.
+// The same by digits of the row's number, without a workgroup that has all tokens of
+// a row: one digit for tables of up to kSortRows rows, two for others, the lower
+// first.  A workgroup has `each` places of the list so far.  count_kernel counts its
+// tokens of each digit; place_kernel adds up the counts, which gives each workgroup
+// the places of its tokens of each digit, and puts them there, in their order.
 constexpr int64_t kCounts = 128;                // workgroups at most
-struct Narrow {
-  const int64_t* ids;
-  uint32_t* count;              // [workgroups][v]
-  int32_t* start;               // [v + 1]
+struct Digit {
+  const int64_t* ids;           // the first digit's list
+  const Place* in;              // the second's, and its length
+  const int32_t* in_total;
+  int32_t* clear;               // [cleared] values that the first digit's count_kernel sets to 0
+  int64_t cleared;
+  uint32_t* count;              // [workgroups][values]
+  int32_t* start;               // [values + 1]: where each value's tokens begin
   Place* order;
   uint32_t v, ignore;
   int32_t t, each;              // each: a multiple of 1024
+  int32_t shift, values;        // the digit: row >> shift & (2^bits - 1), below `values`
+  int32_t bits;
 };
 
-// f(token, row or -1) for the tokens of a wave of the workgroup, a lane each
-template <class F>
-__device__ __forceinline__ void wave_tokens(const Narrow& a, F&& f) {
+// f(token, row, digit or -1) for the places of a wave of the workgroup, a lane each
+template <bool FIRST, class F>
+__device__ __forceinline__ void wave_tokens(const Digit& a, F&& f) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = a.each / kSortWaves;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.each + wave * part;
-  const uint2* p = reinterpret_cast<const uint2*>(a.ids) + t0 + lane;
-  const int64_t left = a.t - t0 - lane;
+  const uint2* p = (FIRST ? reinterpret_cast<const uint2*>(a.ids) : reinterpret_cast<const uint2*>(a.in)) + t0 + lane;
+  const int64_t left = (FIRST ? a.t : *a.in_total) - t0 - lane;
   for (int i = 0; i < part; i += 64) {
-    const uint2 id = i < left ? p[i] : uint2{0u, 1u};
-    const bool live = id.y == 0 && id.x < a.v && id.x != a.ignore;
-    f(static_cast<int>(t0 + i + lane), live ? static_cast<int>(id.x) : -1);
+    const uint2 x = i < left ? p[i] : uint2{0u, 1u};
+    const uint32_t row = FIRST ? x.x : x.y;
+    const bool live = FIRST ? x.y == 0 && row < a.v && row != a.ignore : i < left;
+    f(FIRST ? static_cast<int>(t0 + i + lane) : static_cast<int>(x.x), static_cast<int>(row),
+      live ? static_cast<int>(row >> a.shift & ((1u << a.bits) - 1)) : -1);
   }
 }
 
-__global__ __launch_bounds__(kSortWaves * 64) void count_kernel(const Narrow a) {
+template <bool FIRST>
+__global__ __launch_bounds__(kSortWaves * 64) void count_kernel(const Digit a) {
   __shared__ uint32_t count[kSortRows];
   count[threadIdx.x] = 0;
   __syncthreads();
-  wave_tokens(a, [&](int, int r) {
-    if (r >= 0) atomicAdd(&count[r], 1u);
+  if constexpr (FIRST)
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kSortWaves * 64 + threadIdx.x; i < a.cleared; i += static_cast<int64_t>(gridDim.x) * kSortWaves * 64)
+      a.clear[i] = 0;
+  wave_tokens<FIRST>(a, [&](int, int, int k) {
+    if (k >= 0) atomicAdd(&count[k], 1u);
   });
   __syncthreads();
-  if (threadIdx.x < a.v) a.count[static_cast<int64_t>(blockIdx.x) * a.v + threadIdx.x] = count[threadIdx.x];
+  if (static_cast<int>(threadIdx.x) < a.values) a.count[static_cast<int64_t>(blockIdx.x) * a.values + threadIdx.x] = count[threadIdx.x];
 }
 
-__global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Narrow a) {
+template <bool FIRST>
+__global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Digit a) {
   __shared__ uint32_t count[kSortWaves][kSortRows];
   __shared__ uint32_t sums[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint64_t before = (uint64_t(1) << lane) - 1;
-  // a thread a row: its tokens in all, and in the workgroups before this one
+  // a thread a value: its tokens in all, and in the workgroups before this one
   uint32_t n = 0, earlier = 0;
-  if (tid < static_cast<int>(a.v)) {
+  if (tid < a.values) {
     const int groups = gridDim.x;
     for (int g = 0; g < groups; g += 8) {
       uint32_t x[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = a.count[static_cast<int64_t>(min(g + u, groups - 1)) * a.v + tid];
+      for (int u = 0; u < 8; ++u) x[u] = a.count[static_cast<int64_t>(min(g + u, groups - 1)) * a.values + tid];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         n += g + u < groups ? x[u] : 0u;
@@ -317,26 +332,25 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Narrow a) 
   if (lane == 63) sums[wave] = at;
   __syncthreads();
 
-  // lanes with the same row
-  const int bits = 32 - __clz(static_cast<int>(a.v) - 1);
-  auto same_row = [&](int r) {
-    uint64_t same = __ballot(r >= 0);
-    for (int b = 0; b < bits; ++b) {
-      const uint64_t set = __ballot(r >> b & 1);
-      same &= r >> b & 1 ? set : ~set;
+  // lanes with the same digit
+  auto same_digit = [&](int k) {
+    uint64_t same = __ballot(k >= 0);
+    for (int b = 0; b < a.bits; ++b) {
+      const uint64_t set = __ballot(k >> b & 1);
+      same &= k >> b & 1 ? set : ~set;
     }
     return same;
   };
-  wave_tokens(a, [&](int, int r) {
-    const uint64_t same = same_row(r);
-    if (r >= 0 && (same & before) == 0) atomicAdd(&count[wave][r], static_cast<uint32_t>(__popcll(same)));
+  wave_tokens<FIRST>(a, [&](int, int, int k) {
+    const uint64_t same = same_digit(k);
+    if (k >= 0 && (same & before) == 0) atomicAdd(&count[wave][k], static_cast<uint32_t>(__popcll(same)));
   });
   __syncthreads();
   for (int w = 0; w < wave; ++w) at += sums[w];
-  if (tid < static_cast<int>(a.v)) {
+  if (tid < a.values) {
     if (blockIdx.x == 0) {
       a.start[tid] = static_cast<int32_t>(at - n);
-      if (tid + 1 == static_cast<int>(a.v)) a.start[a.v] = static_cast<int32_t>(at);
+      if (tid + 1 == a.values) a.start[a.values] = static_cast<int32_t>(at);
     }
     uint32_t place = at - n + earlier;
 #pragma unroll
@@ -348,15 +362,26 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Narrow a) 
   }
   __syncthreads();
   volatile uint32_t* next = count[wave];
-  wave_tokens(a, [&](int t, int r) {
-    const uint64_t same = same_row(r);
-    if (r >= 0) {
-      const uint32_t place = next[r];
-      a.order[place + __popcll(same & before)] = {t, r};
-      if ((same & before) == 0) next[r] = place + __popcll(same);
+  wave_tokens<FIRST>(a, [&](int t, int row, int k) {
+    const uint64_t same = same_digit(k);
+    if (k >= 0) {
+      const uint32_t place = next[k];
+      a.order[place + __popcll(same & before)] = {t, row};
+      if ((same & before) == 0) next[k] = place + __popcll(same);
     }
     __builtin_amdgcn_wave_barrier();
   });
+}
+
+// Where each row's tokens begin and end in a list sorted by two digits; rows without
+// tokens have 0 and 0 already.
+__global__ __launch_bounds__(256) void bounds_kernel(const Place* order, const int32_t* total, int32_t* begin, int32_t* end) {
+  const int n = *total;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int32_t row = order[i].row;
+  if (i == 0 || order[i - 1].row != row) begin[row] = static_cast<int32_t>(i);
+  if (i + 1 == n || order[i + 1].row != row) end[row] = static_cast<int32_t>(i) + 1;
 }
 
 // ---------------------------------------------------------------------------
@@ -364,7 +389,8 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Narrow a) 
 // ---------------------------------------------------------------------------
 
 struct Sum {
-  const int32_t* start;
+  const int32_t *begin, *end;   // of a row's tokens, at deal.at(row)
+  const int32_t* total;         // of the list
   const Place* order;
   const void* dy;
   const void* add;
@@ -402,7 +428,7 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
 #pragma unroll
   for (int u = 0; u < kFillRows; ++u) {
     const int64_t row = first + u * groups, i = a.deal.at(static_cast<uint32_t>(min(row, static_cast<int64_t>(a.v - 1))));
-    at[u] = a.start[i] == a.start[i + 1] && row < a.v ? row * a.w_ld + c : -1;
+    at[u] = a.begin[i] == a.end[i] && row < a.v ? row * a.w_ld + c : -1;
   }
 #pragma unroll
   for (int h = 0; h < kFillRows; h += 4) {
@@ -513,7 +539,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
     fill_rows<W>(a, static_cast<int>(blockIdx.x) - a.pieces);
     return;
   }
-  const int total = a.start[a.deal.entries() - 1];
+  const int total = *a.total;
   const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = min(p0 + a.piece, total);
   // (the places do not wait for the total; behind it they hold nothing)
   Place at[kBatch];
@@ -624,11 +650,11 @@ __global__ __launch_bounds__(kJoinGroups * 64) void join_kernel(const Sum a) {
   __shared__ F4 shared[kJoinGroups][64];
   const int p0 = static_cast<int>(blockIdx.x) * a.piece, p1 = p0 + a.piece;
   if (p1 >= a.t) return;
-  const int total = a.start[a.deal.entries() - 1];
+  const int total = *a.total;
   const int64_t row = a.order[p1 - 1].row, next = a.order[p1].row;
   if (p1 >= total || next != row) return;
   const int64_t at_row = a.deal.at(static_cast<uint32_t>(row));
-  const int b = a.start[at_row], e = a.start[at_row + 1];
+  const int b = a.begin[at_row], e = a.end[at_row];
   if (b < p0) return;
   const int g = threadIdx.x >> 6, lane = threadIdx.x & 63, c = (static_cast<int>(blockIdx.y) * 64 + lane) * 4;
   const int first = blockIdx.x, last = (e - 1) / a.piece;
@@ -688,9 +714,11 @@ constexpr int64_t kPieces = 1024;
 struct Plan {
   Lanes lanes;
   Deal deal;
-  bool few, narrow;             // one launch; sorted by count_kernel and place_kernel
+  bool few;                     // one launch
+  int digits = 0;               // sorted by so many digits (0: by sort_kernel)
+  int32_t values[2] = {}, bits[2] = {};
   int32_t batches = 1, piece = 0, pieces = 0, part_ld = 0, each = 0, counts = 0;
-  size_t order = 0, part = 0, count = 0, total = 0;
+  size_t order = 0, part = 0, count = 0, start2 = 0, order2 = 0, total = 0;
 };
 Plan plan_of(const pp_embed_desc& d) {
   Plan p;
@@ -700,16 +728,22 @@ Plan plan_of(const pp_embed_desc& d) {
   // 777 tokens into 5003 x 203 fp32 12 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
   // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
   p.few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
-  // The sort in two launches, without a workgroup that has all tokens of a row.  us a
-  // call, one launch / two, 313 rows of 256 bf16 features, ids of which three in ten are
-  // the same: 8192 tokens 17 / 18, 32768 tokens 28 / 22, 2^20 tokens 675 / 132.
-  p.narrow = !p.few && d.v <= kSortRows && d.t > 16384;
+  // The sort by digits: two launches (five for two digits), but no workgroup that reads
+  // all ids or has all tokens of a row.  us a call, sort_kernel / digits: 313 rows of 256
+  // bf16 features, three in ten ids the same, 8192 tokens 17 / 18, 32768 28 / 22, 2^20
+  // 675 / 132; 50000 rows of 64 features, 32768 tokens: ids log-uniform 32 / 38, uniform
+  // 20 / 34, three in ten the same 40 / 37; 65536: 42 / 42, 25 / 36, 60 / 43; 2^20: 575 /
+  // 108, 177 / 100, 861 / 118.
+  if (!p.few && d.t > 16384 && d.v <= kSortRows)
+    p.digits = 1;
+  else if (!p.few && d.t >= 65536 && d.v <= kSortRows * kSortRows)
+    p.digits = 2;
   // Workgroups of sort_kernel and few_kernel: as many as CUs, or more where one's rows
   // would be too many; of narrow rows some at a time, 256 bytes, so that whole lines of
   // memory are written by one.
   const int64_t bytes = d.d * static_cast<int64_t>(size_of(d.w_dtype));
   p.deal.run = 0, p.deal.log = 0;
-  if (!p.narrow) {
+  if (!p.digits) {
     while (bytes << p.deal.run < 256) ++p.deal.run;
     const int64_t runs = cdiv(d.v, int64_t(1) << p.deal.run);
     while (int64_t(1) << p.deal.log < std::min<int64_t>(runs, kCUs) || cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run > kSortRows)
@@ -719,6 +753,11 @@ Plan plan_of(const pp_embed_desc& d) {
     p.deal.per = static_cast<int32_t>(d.v);
     p.each = static_cast<int32_t>(cdiv(d.t, kCounts * 1024) * 1024);
     p.counts = static_cast<int32_t>(cdiv(d.t, p.each));
+    int all = 0;
+    while (int64_t(1) << all < d.v) ++all;
+    p.bits[0] = p.digits == 1 ? all : all / 2, p.bits[1] = all - p.bits[0];
+    p.values[0] = p.digits == 1 ? static_cast<int32_t>(d.v) : 1 << p.bits[0];
+    p.values[1] = static_cast<int32_t>(cdiv(d.v, int64_t(1) << p.bits[0]));
   }
   const int64_t groups = 256 >> p.lanes.log;
   p.batches = static_cast<int32_t>(std::max<int64_t>(1, cdiv(d.t, groups * kBatch * kPieces)));
@@ -730,10 +769,14 @@ Plan plan_of(const pp_embed_desc& d) {
     p.total += static_cast<size_t>(cdiv(n, 256) * 256);
     return at;
   };
-  take(4 * p.deal.entries());
+  take(4 * (p.digits == 2 ? 2 * d.v : p.deal.entries()));
   p.order = take(static_cast<int64_t>(sizeof(Place)) * d.t);
   p.part = take(p.pieces > 1 ? static_cast<int64_t>(p.pieces) * 2 * p.part_ld * 4 : 0);
-  p.count = take(4 * static_cast<int64_t>(p.counts) * d.v);
+  p.count = take(4 * static_cast<int64_t>(p.counts) * std::max(p.values[0], p.digits == 2 ? p.values[1] : 0));
+  if (p.digits == 2) {
+    p.start2 = take(4 * (p.values[0] + 1 + p.values[1] + 1));
+    p.order2 = take(static_cast<int64_t>(sizeof(Place)) * d.t);
+  }
   return p;
 }
 
@@ -777,8 +820,11 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   const bool row = d.ignore_index >= 0 && d.ignore_index < d.v;
   const Sort s = {ids, start, order, static_cast<uint32_t>(d.v), static_cast<uint32_t>(row ? d.ignore_index : d.v),
                   static_cast<int32_t>(d.t), p.deal};
-  const Sum a = {start, order, dy, add, dw, reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.t),
-                 static_cast<int32_t>(d.v), static_cast<int32_t>(d.d), p.lanes.log, p.deal, p.pieces, p.batches, p.piece, p.part_ld, d.scale};
+  int32_t* start2 = reinterpret_cast<int32_t*>(base + p.start2);
+  const bool two = p.digits == 2;
+  const Sum a = {start, start + (two ? d.v : 1), two ? start2 + p.values[0] + 1 + p.values[1] : start + p.deal.entries() - 1, order, dy, add, dw,
+                 reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.t), static_cast<int32_t>(d.v),
+                 static_cast<int32_t>(d.d), p.lanes.log, p.deal, p.pieces, p.batches, p.piece, p.part_ld, d.scale};
   // (a gradient that is added to in place: rows without a token stay as they are)
   const int64_t fills = add == dw ? 0 : cdiv(d.v, (256 >> p.lanes.log) * kFillRows);
   const dim3 sums(static_cast<uint32_t>(p.pieces + fills), static_cast<uint32_t>(p.lanes.columns));
@@ -790,10 +836,20 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
       hipLaunchKernelGGL((few_kernel<Y, W>), dim3(1u << p.deal.log, static_cast<uint32_t>(p.lanes.columns)), dim3(kFewTokens), 0, st, s, a);
       return;
     }
-    if (p.narrow) {
-      const Narrow f = {ids, reinterpret_cast<uint32_t*>(base + p.count), start, order, s.v, s.ignore, s.t, p.each};
-      hipLaunchKernelGGL(count_kernel, dim3(p.counts), dim3(kSortWaves * 64), 0, st, f);
-      hipLaunchKernelGGL(place_kernel, dim3(p.counts), dim3(kSortWaves * 64), 0, st, f);
+    if (p.digits) {
+      Place* order2 = reinterpret_cast<Place*>(base + p.order2);
+      Digit f = {ids, nullptr, nullptr, two ? start : nullptr, two ? 2 * d.v : 0, reinterpret_cast<uint32_t*>(base + p.count),
+                 two ? start2 : start, two ? order2 : order, s.v, s.ignore, s.t, p.each, 0, p.values[0], p.bits[0]};
+      const dim3 grid(p.counts), block(kSortWaves * 64);
+      hipLaunchKernelGGL((count_kernel<true>), grid, block, 0, st, f);
+      hipLaunchKernelGGL((place_kernel<true>), grid, block, 0, st, f);
+      if (two) {
+        f.in = order2, f.in_total = start2 + p.values[0], f.start = start2 + p.values[0] + 1, f.order = order;
+        f.shift = p.bits[0], f.values = p.values[1], f.bits = p.bits[1];
+        hipLaunchKernelGGL((count_kernel<false>), grid, block, 0, st, f);
+        hipLaunchKernelGGL((place_kernel<false>), grid, block, 0, st, f);
+        hipLaunchKernelGGL(bounds_kernel, dim3(static_cast<uint32_t>(cdiv(d.t, 256))), dim3(256), 0, st, order, a.total, start, start + d.v);
+      }
     } else {
       hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
     }

@@ -143,6 +143,16 @@ def test_token_counts(t, v, how):
     assert same(got, pp.embed_bwd(ids, dy, v, add=add, out=add))
 
 
+@pytest.mark.parametrize("v", [1023, 1024, 1025, 2047, 65536, 1 << 20, (1 << 20) + 1])
+@pytest.mark.parametrize("t", [16384, 16385, 65535, 65536, 200003])
+def test_sorts(v, t):
+    # one digit and two, the largest of each, and what lies beside them
+    ids, dy = make_ids(t, t, v, "heavy" if v % 2 else "uniform", ignored=0.1), normal(t, t, 5)
+    got = pp.embed_bwd(ids, dy, v, ignore_index=v // 2)
+    check_bwd(got, ids, dy, v, ignore=v // 2)
+    assert same(got, pp.embed_bwd(ids, dy, v, ignore_index=v // 2))
+
+
 def test_ids_that_reach_no_row():
     ids = torch.tensor([-1, 10, 1 << 33, -100, 4, 4, 9, -(1 << 63), (1 << 63) - 1], device="cuda")
     dy = normal(2, 9, 40)
