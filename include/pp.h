@@ -772,7 +772,7 @@ typedef struct {
  * The squares are summed in 64 bits.
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, places, dtypes, bits,
  * step, parameters: lr and weight_decay finite, 0 <= beta < 1, 0 <= eps finite),
- * PP_EUNSUPPORTED (a tensor of 2^40 elements or more, more than 2^31 workgroups),
+ * PP_EUNSUPPORTED (a tensor of 2^34 elements or more, moments of 2^40 or more),
  * PP_ESIZE, PP_EHIP.
  */
 typedef struct {

@@ -294,7 +294,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(const double* part, int64_t 
 bool off(const void* p, size_t by) { return reinterpret_cast<uintptr_t>(p) % by != 0; }
 size_t size_of(int32_t dtype) { return dtype == PP_BF16 ? 2 : 4; }
 bool known(int32_t dtype) { return dtype == PP_F32 || dtype == PP_BF16; }
-constexpr int64_t kMost = int64_t(1) << 40;
+constexpr int64_t kMost = int64_t(1) << 34;   // (a launch has fewer than 2^32 threads, eight elements each at least)
 
 // Elements a workgroup takes: enough workgroups for the card where there is
 // little to do, long ones where there is much.
@@ -319,7 +319,7 @@ pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill,
   for (int32_t i = 0; i < count; ++i) {
     if (tensors[i].n == 0) continue;
     const int64_t b = cdiv(tensors[i].n, per);
-    if (list.count == N || blocks + b > (1 << 30)) {
+    if (list.count == N || blocks + b > (1 << 23)) {
       const pp_status s = flush();
       if (s != PP_OK) return s;
     }
@@ -332,7 +332,7 @@ pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill,
 
 pp_status check_tensor(const pp_adamw_tensor& t, const pp_adamw_desc& d) {
   if (t.n < 0 || t.at < 0 || t.at % kBlock) return fail(PP_EINVAL, "bad size, or moments that do not begin at a block");
-  if (t.n >= kMost || t.at >= kMost) return fail(PP_EUNSUPPORTED, "a tensor must have fewer than 2^40 elements");
+  if (t.n >= kMost || t.at >= int64_t(1) << 40) return fail(PP_EUNSUPPORTED, "a tensor must have fewer than 2^34 elements, and the moments fewer than 2^40");
   if (!std::isfinite(t.weight_decay)) return fail(PP_EINVAL, "weight_decay must be finite");
   if (t.keep && t.n % 9) return fail(PP_EINVAL, "a pruned layer has 9 elements for each tap mask");
   if (t.n == 0) return PP_OK;
@@ -402,7 +402,7 @@ pp_status values(const void* m, const void* v, const float* ms, const float* vs,
                  void* v_out, hipStream_t st) {
   if (!known(dtype)) return fail(PP_EINVAL, "bad dtype");
   if (all < 0 || all % kBlock) return fail(PP_EINVAL, "elements must be whole blocks");
-  if (all >= kMost) return fail(PP_EUNSUPPORTED, "too many elements");
+  if (all >= int64_t(1) << 40) return fail(PP_EUNSUPPORTED, "too many elements");
   if (!all || (!m_out && !v_out)) return PP_OK;
   if ((m_out && (!m || !ms || off(m, 16) || off(ms, 4))) || (v_out && (!v || !vs || off(v, 16) || off(vs, 4))))
     return fail(PP_EINVAL, "codes must be 16-byte aligned, with their scales");
@@ -424,7 +424,7 @@ pp_status norm_plan(const pp_grad* grads, int32_t count, int32_t dtype, int64_t*
   int64_t total = 0;
   for (int32_t i = 0; i < count; ++i) {
     if (grads[i].n < 0) return fail(PP_EINVAL, "negative size");
-    if (grads[i].n >= kMost) return fail(PP_EUNSUPPORTED, "a tensor must have fewer than 2^40 elements");
+    if (grads[i].n >= kMost) return fail(PP_EUNSUPPORTED, "a tensor must have fewer than 2^34 elements");
     total += grads[i].n;
   }
   *chunk = chunk_of(total, 16384);

@@ -135,8 +135,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   uint32_t* count = words;
   uint32_t* own = words + kSortWaves * per + wave * (kSortWords - per);
   const uint32_t most = kSortWords - per;
-  for (int i = threadIdx.x; i < kSortWaves * per; i += kSortWaves * 64) count[i] = 0;
-  __syncthreads();
+  for (int i = lane; i < per; i += 64) count[wave * per + i] = 0;   // (a wave's own until all have counted)
 
   // All of a wave's tokens: those of the workgroup's rows go on a list in LDS, and
   // `use(list's length, the token that its entries count from)` takes it when it is
