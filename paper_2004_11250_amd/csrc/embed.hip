@@ -641,9 +641,11 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(const Sort s, const Sum
 }
 
 // Rows whose tokens lie in more than one piece, from the pieces' sums: a workgroup
-// for each piece that such a row may begin in, and 256 features.
-constexpr int kJoinGroups = 4;
-template <class W>
+// for each piece that such a row may begin in, and 256 features.  Most end at once, so
+// that its time is the workgroups' (1024 pieces of 1024 features 6.3 us with 4 waves
+// each, 8.8 with 8) and the longest row's (313 rows of 256 features, 32768 pixels: 5.3,
+// 4.1 with 8).
+template <class W, int kJoinGroups>
 __global__ __launch_bounds__(kJoinGroups * 64) void join_kernel(const Sum a) {
   using F4 = __attribute__((ext_vector_type(4))) float;
   __shared__ F4 shared[kJoinGroups][64];
@@ -853,7 +855,11 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
       hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
     }
     if (sums.x) hipLaunchKernelGGL((sum_kernel<Y, W>), sums, dim3(256), 0, st, a);
-    if (p.pieces > 1) hipLaunchKernelGGL((join_kernel<W>), joins, dim3(kJoinGroups * 64), 0, st, a);
+    if (p.pieces < 2) return;
+    if (joins.y == 1)
+      hipLaunchKernelGGL((join_kernel<W, 8>), joins, dim3(8 * 64), 0, st, a);
+    else
+      hipLaunchKernelGGL((join_kernel<W, 4>), joins, dim3(4 * 64), 0, st, a);
   });
   return launched();
 }
