@@ -44,41 +44,26 @@ struct Look {
   float scale;
 };
 
-constexpr int kLookRows = 4;    // rows of a group of lanes, read together
+// A group of lanes a token.  Bound by memory: 8192 tokens of 1024 bf16 features from a
+// table of 50000 6.4 us (5.2 TB/s), 65536 39.6 (two, four and eight tokens of a group,
+// read together: 6.6, 7.0 and 7.9, the last ones' waves leave the card too early);
+// one token 1.8, the launch.
 template <class W, class Y>
 __global__ __launch_bounds__(256) void look_kernel(const Look a) {
-  const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes;
-  const int c = ((blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1))) * 8;
-  const int cols = a.d - c;
-  if (cols <= 0) return;
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * groups * kLookRows + g;
-  Eight<W> x[kLookRows];
-  int64_t id[kLookRows];
+  const int c = ((blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1))) * 8, cols = a.d - c;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * (256 >> a.lanes) + (threadIdx.x >> a.lanes);
+  if (cols <= 0 || t >= a.t) return;
+  const int64_t id = a.ids[t];
+  float y[8];
+  if (id != a.ignore && static_cast<uint64_t>(id) < static_cast<uint64_t>(a.v)) {
+    load8(static_cast<const W*>(a.w) + id * a.w_ld + c, cols, y);
 #pragma unroll
-  for (int u = 0; u < kLookRows; ++u) {
-    const int64_t t = first + u * groups;
-    id[u] = t < a.t ? a.ids[t] : a.ignore;
+    for (int e = 0; e < 8; ++e) y[e] *= a.scale;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = id == a.ignore ? 0.f : __builtin_nanf("");
   }
-#pragma unroll
-  for (int u = 0; u < kLookRows; ++u) {
-    const bool in = static_cast<uint64_t>(id[u]) < static_cast<uint64_t>(a.v);
-    if (in && id[u] != a.ignore) {
-      x[u] = get8(static_cast<const W*>(a.w) + id[u] * a.w_ld + c, cols);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[u][e] = static_cast<W>(id[u] == a.ignore ? 0.f : __builtin_nanf(""));
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < kLookRows; ++u) {
-    const int64_t t = first + u * groups;
-    if (t < a.t) {
-      float y[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = id[u] == a.ignore ? 0.f : a.scale * static_cast<float>(x[u][e]);
-      store8(static_cast<Y*>(a.y) + t * a.y_ld + c, cols, y);
-    }
-  }
+  store8(static_cast<Y*>(a.y) + t * a.y_ld + c, cols, y);
 }
 
 // ---------------------------------------------------------------------------
@@ -119,6 +104,10 @@ struct Sort {
 // own tokens there, all in one launch and without a word from another workgroup.
 // A wave has consecutive tokens; counts by row and wave, summed up, give each wave
 // the places of its tokens of each row, which it then fills in order.
+// Bound by the instructions of the scan, some ten an id and workgroup, and by its fixed
+// part: 777 tokens 5.5 us, 8192 7.3, 32768 10.4 with uniform ids; and by the workgroup of
+// the most frequent row (32768 log-uniform ids 14).  (Rows dealt in consecutive ranges
+// instead: 131072 log-uniform ids 130 us, now 57.)
 __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   // for each wave a count of each row's tokens, then a list of tokens:
   // (token - base) << kOwnBits | row
@@ -252,7 +241,8 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
 // a row: one digit for tables of up to kSortRows rows, two for others, the lower
 // first.  A workgroup has `each` places of the list so far.  count_kernel counts its
 // tokens of each digit; place_kernel adds up the counts, which gives each workgroup
-// the places of its tokens of each digit, and puts them there, in their order.
+// the places of its tokens of each digit, and puts them there, in their order.  32768
+// pixels 2.7 and 5.4 us, latency: of the counts, two scans and an exchange.
 constexpr int64_t kCounts = 128;                // workgroups at most
 struct Digit {
   const int64_t* ids;           // the first digit's list
@@ -415,8 +405,15 @@ __device__ __forceinline__ void put_row(const Sum& a, int64_t row, int c, const 
   store8(static_cast<W*>(a.dw) + at, a.d - c, x);
 }
 
-// Rows without a token, of kFillRows a group of lanes: what they are added to.
-constexpr int kFillRows = 8;
+// Rows without a token, of kFillRows a group of lanes: what they are added to, or 0.
+// They lie between the tokens' workgroups in one launch, which is bound by memory then:
+// 8192 tokens into 50000 x 1024 bf16 21 us, 5.7 TB/s (in a launch before it, together
+// with the sort: 22 + 9.5 in place of 7.5 + 21); added to another gradient, 32768 tokens,
+// 47 us, 6 TB/s, 67 without the hint that what is copied is not read again.  (The hint
+// only for values of two bytes: a lane's eight of four bytes are two accesses, and the
+// second would fetch the same lines again, 205 MB 99 us in place of 46.  Rows of a group:
+// 4; 8 and 16 take 49 and 54 us.)
+constexpr int kFillRows = 4;
 template <class W>
 __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
   const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes;
@@ -429,18 +426,15 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
     const int64_t row = first + u * groups, i = a.deal.at(static_cast<uint32_t>(min(row, static_cast<int64_t>(a.v - 1))));
     at[u] = a.begin[i] == a.end[i] && row < a.v ? row * a.w_ld + c : -1;
   }
+  Eight<W> x[kFillRows] = {};
+  if (a.add) {
 #pragma unroll
-  for (int h = 0; h < kFillRows; h += 4) {
-    Eight<W> x[4] = {};
-    if (a.add) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (at[h + u] >= 0) x[u] = get8<sizeof(W) == 2>(static_cast<const W*>(a.add) + at[h + u], cols);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (at[h + u] >= 0) put8<sizeof(W) == 2>(static_cast<W*>(a.dw) + at[h + u], cols, x[u]);
+    for (int u = 0; u < kFillRows; ++u)
+      if (at[u] >= 0) x[u] = get8<sizeof(W) == 2>(static_cast<const W*>(a.add) + at[u], cols);
   }
+#pragma unroll
+  for (int u = 0; u < kFillRows; ++u)
+    if (at[u] >= 0) put8<sizeof(W) == 2>(static_cast<W*>(a.dw) + at[u], cols, x[u]);
 }
 
 // A workgroup sums the piece p0 .. p1 of a list, a group of lanes a part of it, of
@@ -449,7 +443,10 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
 // a part's first and last run meet their neighbours' in LDS.  What goes on past the
 // piece's ends (row `prev` before it, `next` behind it, -1: none) goes to part: the
 // sum of a run that goes on from the piece before to row 0, of one that begins here
-// to row 1.
+// to row 1.  A batch's rows are in flight together, and a piece's time is that of its
+// list, its rows and its neighbours in LDS one after the other: 32768 tokens into
+// 313 x 256 bf16 7.9 us (batches of 4 7.1, but twice the pieces for join_kernel, of 16
+// 23: too few waves).
 template <class Y, class W, int THREADS>
 __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int p0, int p1, int batches, Place (&at)[kBatch],
                                           int32_t prev, int32_t next, float* part, float (*edge)[8], int32_t* edge_row) {
@@ -552,7 +549,8 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
 
 // Up to kFewTokens tokens: a workgroup has its rows of the table, finds their tokens,
 // a thread an id, sorts them in LDS, sums them, and fills its rows without a token,
-// all in one launch.
+// all in one launch.  777 tokens into 5003 x 203 fp32 12 us a call, of which the host
+// takes 10; a table of 50000 x 1024 bf16 is filled in 20, 5 TB/s.
 constexpr int kFewTokens = 1024, kFewRanks = 256;
 template <class Y, class W>
 __global__ __launch_bounds__(kFewTokens) void few_kernel(const Sort s, const Sum a) {
@@ -796,7 +794,7 @@ pp_status look(const pp_embed_desc* desc, const int64_t* ids, const void* w, voi
   if (off(ids, 8) || off(w, size_of(d.w_dtype)) || off(y, size_of(d.y_dtype))) return fail(PP_EINVAL, "misaligned pointer");
   const Lanes l = lanes_for(d.d);
   const Look a = {ids, w, y, d.t, d.v, d.w_ld, d.y_ld, d.ignore_index, static_cast<int32_t>(d.d), l.log, d.scale};
-  const dim3 grid(static_cast<uint32_t>(cdiv(d.t, (256 >> l.log) * kLookRows)), static_cast<uint32_t>(l.columns));
+  const dim3 grid(static_cast<uint32_t>(cdiv(d.t, 256 >> l.log)), static_cast<uint32_t>(l.columns));
   with_types(d.w_dtype, d.y_dtype, [&](auto wt, auto yt) {
     hipLaunchKernelGGL((look_kernel<decltype(wt), decltype(yt)>), grid, dim3(256), 0, st, a);
   });
