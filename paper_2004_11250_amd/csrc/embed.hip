@@ -499,7 +499,8 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
   __syncthreads();
   if (cols <= 0) return;
 
-  // the runs that begin at this group's edges
+  // the runs that begin at this group's edges; groups past the piece's end have none
+  const int slots = 2 * min(groups, (p1 - p0 + batches * kBatch - 1) / (batches * kBatch));
   for (int s = 2 * g; s < 2 * g + 2; ++s) {
     const int32_t row = edge_row[s];
     if (row < 0) continue;
@@ -508,13 +509,26 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = edge[(s << a.lanes) + lane][e];
     bool ends = false;          // another run follows in this piece
-    for (int q = s + 1; q < 2 * groups && !ends; ++q) {
-      const int32_t r = edge_row[q];
-      if (r == row) {
+    constexpr int kNear = 4;    // (read together, whether they belong to the run or not)
+    for (int q = s + 1; q < slots && !ends; q += kNear) {
+      int32_t r[kNear];
+      float x[kNear][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += edge[(q << a.lanes) + lane][e];
-      } else if (r >= 0) {
-        ends = true;
+      for (int u = 0; u < kNear; ++u) {
+        const int k = min(q + u, slots - 1);
+        r[u] = edge_row[k];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u][e] = edge[(k << a.lanes) + lane][e];
+      }
+#pragma unroll
+      for (int u = 0; u < kNear; ++u) {
+        if (q + u >= slots || ends) break;
+        if (r[u] == row) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] += x[u][e];
+        } else if (r[u] >= 0) {
+          ends = true;
+        }
       }
     }
     const bool from = s == 0 && prev == row, on = !ends && next == row;
