@@ -676,7 +676,8 @@ typedef struct {
 /*
  * pp_embed_fwd
  *   ids   device int64 [t]
- *   w, y  device [v][d] and [t][d] (rows w_ld and y_ld apart)
+ *   w, y  device [v][d] and [t][d] (rows w_ld and y_ld apart); y may overlap neither
+ *         of the others
  * pp_embed_workspace -- device bytes pp_embed_bwd needs: up to 8 v + 16 t, about
  * 0.5 MB, and up to 2048 rows of d fp32 values for rows of the table that many
  * tokens share.
@@ -688,7 +689,7 @@ typedef struct {
  *              array of the call (but be add)
  *   workspace  256-byte aligned
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, dtypes, rows closer
- * than d), PP_EUNSUPPORTED (2^30 tokens or rows of the table or more, d of 2^24
+ * than d), PP_EUNSUPPORTED (2^30 tokens or rows of the table or more, d of 2^23
  * or more, rows 2^32 elements apart or more), PP_ESIZE, PP_EHIP.
  */
 pp_status pp_embed_fwd(const pp_embed_desc* desc, const int64_t* ids, const void* w, void* y, void* hip_stream);
@@ -708,7 +709,7 @@ pp_status pp_embed_bwd(const pp_embed_desc* desc, const int64_t* ids, const void
  *
  * The moments of all tensors of a list lie in one array each: tensor i's from
  * element `at` on, a multiple of PP_ADAMW_BLOCK; what follows them up to the next
- * multiple is written as 0.  With 32 bits they are fp32.  With 8 bits each
+ * multiple is written as 0, and no other tensor's may lie there.  With 32 bits they are fp32.  With 8 bits each
  * block of PP_ADAMW_BLOCK elements has a scale for each moment, and a code an
  * element:
  *   m   e4m3 (OCP, 448 at most), times the block's scale: its largest |m'| / 448

@@ -167,6 +167,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   // time (a step's lanes add to each row once: additions to one address take turns)
   const int bits = 32 - __clz(per - 1);
   auto each_entry = [&](auto&& f) {
+    __builtin_amdgcn_wave_barrier();   // (the list is the wave's own; LDS is done in order)
     for (uint32_t i = 0; i < mine; i += 64) {
       const bool on = i + lane < mine;
       const uint32_t x = own[on ? i + lane : 0], r = x & (kSortRows - 1);
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
 // first.  A workgroup has `each` places of the list so far.  count_kernel counts its
 // tokens of each digit; place_kernel adds up the counts, which gives each workgroup
 // the places of its tokens of each digit, and puts them there, in their order.  32768
-// pixels 2.7 and 5.4 us, latency: of the counts, two scans and an exchange.
+// pixels 2.7 and 5.5 us: latency, of ids, counts, a scan and an exchange in turn.
 constexpr int64_t kCounts = 128;                // workgroups at most
 struct Digit {
   const int64_t* ids;           // the first digit's list
@@ -259,31 +260,45 @@ struct Digit {
   int32_t bits;
 };
 
-// f(token, row, digit or -1) for the places of a wave of the workgroup, a lane each
-template <bool FIRST, class F>
-__device__ __forceinline__ void wave_tokens(const Digit& a, F&& f) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = a.each / kSortWaves;
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * a.each + wave * part;
-  const uint2* p = (FIRST ? reinterpret_cast<const uint2*>(a.ids) : reinterpret_cast<const uint2*>(a.in)) + t0 + lane;
-  const int64_t left = (FIRST ? a.t : *a.in_total) - t0 - lane;
-  for (int i = 0; i < part; i += 64) {
-    const uint2 x = i < left ? p[i] : uint2{0u, 1u};
-    const uint32_t row = FIRST ? x.x : x.y;
-    const bool live = FIRST ? x.y == 0 && row < a.v && row != a.ignore : i < left;
-    f(FIRST ? static_cast<int>(t0 + i + lane) : static_cast<int>(x.x), static_cast<int>(row),
-      live ? static_cast<int>(row >> a.shift & ((1u << a.bits) - 1)) : -1);
+// The places of a wave of the workgroup, a lane each: f(token, row, digit or -1).  The
+// first ones are fetched at once, and kept.
+template <bool FIRST>
+struct WaveTokens {
+  const uint2* p;
+  int64_t t, left;
+  int32_t part;
+  uint2 first;
+  __device__ __forceinline__ explicit WaveTokens(const Digit& a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    part = a.each / kSortWaves;
+    t = static_cast<int64_t>(blockIdx.x) * a.each + wave * part + lane;
+    p = (FIRST ? reinterpret_cast<const uint2*>(a.ids) : reinterpret_cast<const uint2*>(a.in)) + t;
+    left = (FIRST ? a.t : *a.in_total) - t;
+    first = fetch(0);
   }
-}
+  __device__ __forceinline__ uint2 fetch(int i) const { return i < left ? p[i] : uint2{0u, 1u}; }
+  template <class F>
+  __device__ __forceinline__ void each(const Digit& a, F&& f) const {
+    for (int i = 0; i < part; i += 64) {
+      const uint2 x = i ? fetch(i) : first;
+      const uint32_t row = FIRST ? x.x : x.y;
+      const bool live = FIRST ? x.y == 0 && row < a.v && row != a.ignore : i < left;
+      f(FIRST ? static_cast<int>(t + i) : static_cast<int>(x.x), static_cast<int>(row),
+        live ? static_cast<int>(row >> a.shift & ((1u << a.bits) - 1)) : -1);
+    }
+  }
+};
 
 template <bool FIRST>
 __global__ __launch_bounds__(kSortWaves * 64) void count_kernel(const Digit a) {
   __shared__ uint32_t count[kSortRows];
+  const WaveTokens<FIRST> tokens(a);
   count[threadIdx.x] = 0;
   __syncthreads();
   if constexpr (FIRST)
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kSortWaves * 64 + threadIdx.x; i < a.cleared; i += static_cast<int64_t>(gridDim.x) * kSortWaves * 64)
       a.clear[i] = 0;
-  wave_tokens<FIRST>(a, [&](int, int, int k) {
+  tokens.each(a, [&](int, int, int k) {
     if (k >= 0) atomicAdd(&count[k], 1u);
   });
   __syncthreads();
@@ -296,16 +311,18 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Digit a) {
   __shared__ uint32_t sums[kSortWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint64_t before = (uint64_t(1) << lane) - 1;
+  const WaveTokens<FIRST> tokens(a);
   // a thread a value: its tokens in all, and in the workgroups before this one
+  constexpr int kAtOnce = 32;
   uint32_t n = 0, earlier = 0;
   if (tid < a.values) {
     const int groups = gridDim.x;
-    for (int g = 0; g < groups; g += 8) {
-      uint32_t x[8];
+    for (int g = 0; g < groups; g += kAtOnce) {
+      uint32_t x[kAtOnce];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = a.count[static_cast<int64_t>(min(g + u, groups - 1)) * a.values + tid];
+      for (int u = 0; u < kAtOnce; ++u) x[u] = a.count[static_cast<int64_t>(min(g + u, groups - 1)) * a.values + tid];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kAtOnce; ++u) {
         n += g + u < groups ? x[u] : 0u;
         earlier += g + u < static_cast<int>(blockIdx.x) ? x[u] : 0u;
       }
@@ -330,7 +347,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Digit a) {
     }
     return same;
   };
-  wave_tokens<FIRST>(a, [&](int, int, int k) {
+  tokens.each(a, [&](int, int, int k) {
     const uint64_t same = same_digit(k);
     if (k >= 0 && (same & before) == 0) atomicAdd(&count[wave][k], static_cast<uint32_t>(__popcll(same)));
   });
@@ -351,7 +368,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Digit a) {
   }
   __syncthreads();
   volatile uint32_t* next = count[wave];
-  wave_tokens<FIRST>(a, [&](int t, int row, int k) {
+  tokens.each(a, [&](int t, int row, int k) {
     const uint64_t same = same_digit(k);
     if (k >= 0) {
       const uint32_t place = next[k];
@@ -715,7 +732,7 @@ pp_status check(const pp_embed_desc* desc) {
   if (d.t < 0 || d.v < 1 || d.d < 1) return fail(PP_EINVAL, "bad size");
   if ((d.v > 1 && d.w_ld < d.d) || (d.t > 1 && d.y_ld < d.d)) return fail(PP_EINVAL, "rows closer than their length");
   if (d.t >= int64_t(1) << 30 || d.v >= int64_t(1) << 30) return fail(PP_EUNSUPPORTED, "tokens and rows must be fewer than 2^30");
-  if (d.d >= 1 << 24) return fail(PP_EUNSUPPORTED, "rows must have fewer than 2^24 features");
+  if (d.d >= 1 << 23) return fail(PP_EUNSUPPORTED, "rows must have fewer than 2^23 features");
   for (int64_t n : {d.w_ld, d.y_ld})
     if (n >= int64_t(1) << 32) return fail(PP_EUNSUPPORTED, "rows must be fewer than 2^32 elements apart");
   return PP_OK;

@@ -29,7 +29,7 @@ def test_embed_descriptions(lib):
     for bad in (dict(w_dtype=2), dict(y_dtype=-1), dict(t=-1), dict(v=0), dict(d=0), dict(w_ld=7), dict(y_ld=7)):
         assert lib.pp_embed_workspace(ctypes.byref(desc(**bad)), ctypes.byref(nb)) == pp.PP_EINVAL, bad
         assert lib.pp_embed_fwd(ctypes.byref(desc(**bad)), A, A, A, None) == pp.PP_EINVAL, bad
-    for bad in (dict(t=1 << 30), dict(v=1 << 30), dict(d=1 << 24, w_ld=1 << 24, y_ld=1 << 24), dict(w_ld=1 << 32), dict(y_ld=1 << 32)):
+    for bad in (dict(t=1 << 30), dict(v=1 << 30), dict(d=1 << 23, w_ld=1 << 23, y_ld=1 << 23), dict(w_ld=1 << 32), dict(y_ld=1 << 32)):
         assert lib.pp_embed_workspace(ctypes.byref(desc(**bad)), ctypes.byref(nb)) == pp.PP_EUNSUPPORTED, bad
         assert lib.pp_embed_bwd(ctypes.byref(desc(**bad)), A, A, None, A, A, 1 << 50, None) == pp.PP_EUNSUPPORTED, bad
     assert lib.pp_embed_workspace(None, ctypes.byref(nb)) == pp.PP_EINVAL
