@@ -12,13 +12,14 @@ recorded graph can be replayed with others.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import struct
 
 import numpy as np
 
 from . import _check, _torch, load_library
-from .train import _changed, _empty, _on, _stream_of
+from .train import _empty, _on, _stream_of
 
 BLOCK = 128     # PP_ADAMW_BLOCK
 
@@ -70,6 +71,7 @@ class AdamWState:
         # the list as the library takes it, without addresses
         self._table = np.zeros((len(self.sizes), len(_TENSOR)), np.int64)
         self._table[:, _N], self._table[:, _AT] = self.sizes, self.places
+        self._dims = np.array([n for s in self.shapes for n in (len(s), *s)] or [0], np.int64)
 
         def zeros(n, dtype):
             return torch.zeros(n, dtype=torch.uint8, device=device).view(dtype)
@@ -124,16 +126,33 @@ def _list(t):
     return [t] if _torch().is_tensor(t) else list(t)
 
 
-def _pointers(name, tensors, dtype, device, shapes=None):
-    """Addresses of a list that fits the state's, checked in few passes: a list may
-    have hundreds of tensors, and each costs the host."""
-    tensor = _torch().Tensor
-    if shapes is not None and [t.shape for t in tensors] != shapes:
+@functools.lru_cache(maxsize=None)
+def _lists():
+    try:
+        from . import _tensors
+    except ImportError as e:
+        raise RuntimeError("the binding's module for lists of tensors is not built (python -m paper_2004_11250_amd.build)") from e
+    return _tensors
+
+
+def _address(a):
+    return a.__array_interface__["data"][0]
+
+
+def _gather(name, tensors, dtype, device, table, at, column, state=None, sizes=False):
+    """Addresses of a list's tensors, which have to be contiguous, of a dtype and
+    device (and of the state's shapes), into a column of the table (which lies at
+    ``at``); with sizes, their numbers of elements into the next."""
+    if device.type == "cuda" and _lists().gather(tensors, 0 if state is None else _address(state._dims), dtype, device.index,
+                                                 at + 8 * column, table.shape[1], sizes):
+        return
+    if state is not None and [t.shape for t in tensors] != state.shapes:
         raise ValueError(f"{name} must be of the state's shapes")
-    there = set(map(tensor.get_device, tensors)) == {device.index} if device.type == "cuda" else {t.device for t in tensors} == {device}
-    if not there or {t.dtype for t in tensors} != {dtype} or not all(map(tensor.is_contiguous, tensors)):
+    if any(t.device != device or t.dtype != dtype or not t.is_contiguous() for t in tensors) or device.type == "cuda":
         raise ValueError(f"{name} must be contiguous {dtype} on one device, {device}")
-    return list(map(tensor.data_ptr, tensors))
+    table[:, column] = [t.data_ptr() for t in tensors]
+    if sizes:
+        table[:, column + 1] = [t.numel() for t in tensors]
 
 
 def _scalar(name, t, dtype, device):
@@ -142,16 +161,8 @@ def _scalar(name, t, dtype, device):
     return t.data_ptr()
 
 
-def _own(outs, wp, op, gp):
-    """Outputs are each their own, but an element's weight may be written in place.
-    (By where the tensors begin.)"""
-    at = set(outs)
-    if len(at) != len(outs):
-        raise ValueError("two outputs are the same tensor")
-    if not at.isdisjoint(gp):
-        raise ValueError("an output is another tensor of the call")
-    if any(w != o and w in at for w, o in zip(wp, op)):
-        raise ValueError("an output is another tensor's input")
+# outputs are each their own, but a weight may be written in place (by where tensors begin)
+_OWN = (None, "two outputs are the same tensor", "an output is another tensor of the call", "an output is another tensor's input")
 
 
 def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, keep=None, copies=None,
@@ -182,25 +193,28 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
         if dt not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
     table = state._table.copy()
-    wp, gp = _pointers("weights", weights, wt, dev, shapes), _pointers("grads", grads, gt, dev, shapes)
+    at = _address(table)
+    _gather("weights", weights, wt, dev, table, at, _W, state)
+    _gather("grads", grads, gt, dev, table, at, _G, state)
     if out is None:
-        new, state_out, op, bufs_out = weights, state, wp, bufs
+        new, state_out, bufs_out = weights, state, bufs
+        table[:, _W_OUT] = table[:, _W]
     else:
         new, state_out = _list(out[0]), out[1]
         if len(new) != count or state_out.bits != state.bits or state_out.shapes != shapes:
             raise ValueError("out must be weights and a state of the same shapes and bits")
-        op, bufs_out = _pointers("out weights", new, wt, dev, shapes), state_out.buffers()
+        _gather("out weights", new, wt, dev, table, at, _W_OUT, state)
+        bufs_out = state_out.buffers()
         if bufs_out[0].device != dev:
             raise ValueError("out must be on the state's device")
-    outs = [p for p, n in zip(op, state.sizes) if n] if 0 in state.sizes else list(op)
     if copies is not None:
         copies = _list(copies)
         if len(copies) != count:
             raise ValueError(f"copies must be of the state's length {count}")
-        cp = _pointers("copies", copies, torch.bfloat16, dev, shapes)
-        table[:, _COPY] = cp
-        outs += [p for p, n in zip(cp, state.sizes) if n] if 0 in state.sizes else cp
-    _own(outs, wp, op, gp)
+        _gather("copies", copies, torch.bfloat16, dev, table, at, _COPY, state)
+    wrong = _lists().own(at, count, copies is not None)
+    if wrong:
+        raise ValueError(_OWN[wrong])
     if keep is not None:
         keep = list(keep)
         if len(keep) != count:
@@ -212,7 +226,6 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
                     or not k.is_contiguous() or k.device != dev:
                 raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
             table[i, _KEEP] = k.data_ptr()
-    table[:, _W], table[:, _G], table[:, _W_OUT] = wp, gp, op
     table.view(np.float64)[:, _DECAY] = weight_decay
     d_lr = _scalar("lr", lr, torch.float32, dev) if torch.is_tensor(lr) else 0
     d_step = _scalar("step", step, torch.int64, dev) if torch.is_tensor(step) else 0
@@ -222,8 +235,8 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     with _stream_of(stream, dev) as sp:
-        _check(load_library().pp_adamw_step(table.ctypes.data, count, desc, sp), "pp_adamw_step")
-    _changed(new + [t for t in bufs_out if t is not None] + (copies or []))
+        _check(load_library().pp_adamw_step(at, count, desc, sp), "pp_adamw_step")
+    _lists().changed([*new, *bufs_out, *(copies or ())])
     return (new[0], state_out) if single else (new, state_out)
 
 
@@ -243,14 +256,15 @@ def grad_norm(grads, max_norm=None, stream=None):
     if not most > 0:
         raise ValueError(f"max_norm must be above 0, got {max_norm}")
     table = np.empty((len(grads), 2), np.int64)      # (pp_grad: address, elements)
-    table[:, 0], table[:, 1] = _pointers("grads", grads, dt, dev), list(map(torch.Tensor.numel, grads))
+    at = _address(table)
+    _gather("grads", grads, dt, dev, table, at, 0, sizes=True)
     if dev.type != "cuda":
         raise ValueError("the tensors must be on a GPU")
     code, lib, nb = int(dt == torch.bfloat16), load_library(), ctypes.c_size_t(0)
-    _check(lib.pp_grad_norm_workspace(table.ctypes.data, len(grads), code, ctypes.byref(nb)), "pp_grad_norm_workspace")
+    _check(lib.pp_grad_norm_workspace(at, len(grads), code, ctypes.byref(nb)), "pp_grad_norm_workspace")
     with _stream_of(stream, dev) as sp:
         both = _empty(2, torch.float32, dev, stream)
         ws = _empty(max(nb.value, 256), torch.uint8, dev, stream)
-        _check(lib.pp_grad_norm(table.ctypes.data, len(grads), code, most, both.data_ptr(), ws.data_ptr(), ws.numel(), sp),
+        _check(lib.pp_grad_norm(at, len(grads), code, most, both.data_ptr(), ws.data_ptr(), ws.numel(), sp),
                "pp_grad_norm")
     return both.unbind()

@@ -22,6 +22,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libppconv.so")
 HOST_LIB = os.path.join(PKG, "libppconv_host.so")
 CEIL_LIB = os.path.join(PKG, "libppceil.so")
+TENSORS_LIB = os.path.join(PKG, "_tensors.so")
 OBJDIR = os.path.join(PKG, "_build")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -92,7 +93,23 @@ def build(verbose: bool = False) -> str:
     _run([HIPCC, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp] + objs + ["-lhiprtc", "-ldl"])
     os.replace(tmp, LIB)
     build_ceiling()
+    build_tensors()
     return LIB
+
+
+def build_tensors() -> str:
+    """The binding's Python module for lists of tensors (g++, torch's headers; the
+    library itself knows nothing of torch)."""
+    import sysconfig
+
+    import torch
+    at = os.path.dirname(torch.__file__)
+    tmp = TENSORS_LIB + ".tmp"
+    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-I{at}/include", f"-I{at}/include/torch/csrc/api/include",
+          f"-I{sysconfig.get_paths()['include']}", os.path.join(PKG, "binding", "tensors.cpp"), "-o", tmp,
+          f"-L{at}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, TENSORS_LIB)
+    return TENSORS_LIB
 
 
 def build_ceiling() -> str:

@@ -259,3 +259,46 @@ def test_embed_tensors():
                      (torch.zeros(5, 4), (5, 3)), (torch.zeros(9).as_strided((5, 4), (1, 1)), (5, 4))):
         with pytest.raises(ValueError):
             rows(t, shape)
+
+
+# the binding's native module for lists
+
+def test_outputs_of_their_own():
+    own = adamw._lists().own
+
+    def code(rows, copies=False):
+        t = np.zeros((len(rows), 8), np.int64)
+        for r, (n, w, g, o, *c) in zip(t, rows):
+            r[:4] = n, w, g, o
+            r[4] = c[0] if c else 0
+        return own(t.ctypes.data, len(rows), copies)
+
+    assert code([(4, 10, 20, 10), (4, 11, 20, 11)]) == 0 and code([]) == 0
+    assert code([(4, 10, 20, 12), (4, 10, 21, 13)]) == 0
+    assert code([(4, 10, 20, 10), (4, 11, 21, 10)]) == 1
+    assert code([(4, 10, 20, 10), (0, 11, 21, 10), (0, 0, 0, 0), (0, 0, 0, 0)]) == 0
+    assert code([(4, 10, 20, 20)]) == 2 and code([(4, 10, 20, 12), (4, 11, 12, 13)]) == 2
+    assert code([(4, 10, 20, 11), (4, 11, 21, 12)]) == 3
+    assert code([(4, 10, 20, 10, 10)], True) == 1 and code([(4, 10, 20, 10, 20)], True) == 2 and code([(4, 10, 20, 12, 10)], True) == 3
+    assert code([(4, 10, 20, 10, 10)], False) == 0
+
+
+def test_gather_takes_tensors_on_a_gpu_only():
+    lists, t = adamw._lists(), np.zeros((2, 2), np.int64)
+    assert lists.gather([torch.zeros(3)], 0, torch.float32, 0, t.ctypes.data, 2, True) is False
+    assert lists.gather([None], 0, torch.float32, 0, t.ctypes.data, 2, True) is False
+    assert lists.gather(["x"], 0, torch.float32, 0, t.ctypes.data, 2, True) is False
+    assert lists.gather([], 0, torch.float32, 0, t.ctypes.data, 2, True) is True and not t.any()
+    for bad in ((), ([], 0, torch.float32, 0, 0, 2), ((), 0, torch.float32, 0, 0, 2, 0), ([], 0, "f", 0, 0, 2, 0), ([], 0, torch.float32, "0", 0, 2, 0)):
+        with pytest.raises(TypeError):
+            lists.gather(*bad)
+    with pytest.raises(TypeError):
+        lists.own(0, "x", 0)
+    with pytest.raises(TypeError):
+        lists.changed((torch.zeros(1),))
+    with pytest.raises(TypeError):
+        lists.changed([torch.zeros(1), 3])
+    x = torch.zeros(3)
+    before = x._version
+    lists.changed([x, None, x])
+    assert x._version == before + 2

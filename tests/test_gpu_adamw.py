@@ -409,3 +409,30 @@ def test_what_autograd_sees():
     assert new is w and same is state and w._version > before[0] and state.m._version > before[1]
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+def test_lists_are_checked_on_the_gpu_too():
+    w, g = [normal(1, 4, 6), normal(2, 9)], [normal(3, 4, 6), normal(4, 9)]
+    state = pp.AdamWState(w)
+    before = [t.clone() for t in w]
+    go = lambda w=w, g=g, **kw: pp.adamw_step(w, g, state, lr=1e-3, step=1, **kw)   # noqa: E731
+    for bad in ([w[0].t().contiguous(), w[1]], [w[0].view(24), w[1]], [w[1], w[0]]):
+        with pytest.raises(ValueError, match="shapes"):
+            go(w=bad)
+        with pytest.raises(ValueError, match="shapes"):
+            go(g=bad)
+    for bad in ([normal(5, 6, 4).t(), g[1]], [g[0], g[1].bfloat16()], [g[0], g[1].cpu()], [normal(6, 1, 6).expand(4, 6), g[1]]):
+        with pytest.raises(ValueError, match="contiguous"):
+            go(g=bad)
+    with pytest.raises(ValueError, match="same tensor"):
+        pp.adamw_step([w[1], w[1]], [g[1], g[1]], pp.AdamWState([w[1], w[1]]), lr=1e-3, step=1)
+    with pytest.raises(ValueError, match="another tensor of the call"):
+        go(out=([g[0], w[1]], state))
+    with pytest.raises(ValueError, match="another tensor's input"):
+        pp.adamw_step([w[1], before[1]], [g[1], g[1]], pp.AdamWState([w[1], w[1]]), lr=1e-3, step=1,
+                      out=([before[1], normal(9, 9)], pp.AdamWState([w[1], w[1]])))
+    with pytest.raises(ValueError, match="contiguous"):
+        pp.grad_norm([g[0], normal(5, 6, 4).t()])
+    assert all(torch.equal(a, b) for a, b in zip(w, before))
+    go()
+    assert not torch.equal(w[0], before[0])
