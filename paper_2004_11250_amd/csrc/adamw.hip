@@ -69,19 +69,28 @@ __device__ __forceinline__ float row_max(float x) {
   return fmaxf(x, turn(x, std::integral_constant<int, 1>()));
 }
 
-// sqrt to 1 ulp for every v >= 0: the hardware's takes no denormal values.
-__device__ __forceinline__ float root(float v) {
-  const bool small = v < 0x1p-96f;
-  const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
-  return small ? r * 0x1p-32f : r;
+// Square roots of eight v >= 0, to 1 ulp.  The hardware's takes values below fp32's
+// normal range for 0; eight that hold one are scaled (one instruction and a half an
+// element to find out, in place of five to scale all).
+__device__ __forceinline__ void roots(const float (&v)[8], float (&r)[8]) {
+  uint32_t least = ~0u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    least = min(least, __builtin_bit_cast(uint32_t, v[e]) - 1u);   // (0: the largest)
+    r[e] = __builtin_amdgcn_sqrtf(v[e]);
+  }
+  if (least < 0x007fffffu) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = v[e] < 0x1p-96f ? __builtin_amdgcn_sqrtf(v[e] * 0x1p64f) * 0x1p-32f : r[e];
+  }
 }
 
 // Codes of second moments (square roots over the block's scale): rounded to 4
 // bits after the leading one, and these with the exponent's low 4 bits kept.
 __device__ __forceinline__ uint32_t code_of(float r) {
   const int bits = __builtin_bit_cast(int, r);
-  const int c = ((bits + 0x3ffff + ((bits >> 19) & 1)) >> 19) - kFirstCode;
-  return r > 0.f ? static_cast<uint32_t>(min(max(c, 1), 255)) : 0u;
+  const int c = (bits + ((bits >> 19) & 1) + (0x3ffff - (kFirstCode << 19))) >> 19;
+  return static_cast<uint32_t>(min(max(c, min(bits, 1)), 255));     // (r = 0: 0, above it 1 at least)
 }
 __device__ __forceinline__ float value_of(uint32_t c) { return __builtin_bit_cast(float, c ? (c + kFirstCode) << 19 : 0u); }
 
@@ -189,24 +198,46 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       if constexpr (BITS == 8) m_values(mc, ms, m), v_values(vc, vs, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool off = !(on >> e & 1);
         const float ge = scale * g[e];
         m[e] = s.b1 * m[e] + s.n1 * ge;
         v[e] = s.b2 * v[e] + s.n2 * (ge * ge);
-        const float r = root(v[e]);
-        w[e] = decay * w[e] - rate * m[e] * __builtin_amdgcn_rcpf(r * c2 + s.eps);
-        if (off) w[e] = m[e] = v[e] = 0.f;
-        if (e >= there) m[e] = v[e] = 0.f;
+      }
+      if (keep) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!(on >> e & 1)) m[e] = v[e] = 0.f;
+      }
+      if (there < 8) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= there) m[e] = v[e] = 0.f;
+      }
+      float r[8];
+      roots(v, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = decay * w[e] - rate * m[e] * __builtin_amdgcn_rcpf(r[e] * c2 + s.eps);
+      if (keep) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = on >> e & 1 ? w[e] : 0.f;
       }
       if constexpr (BITS == 8) {
-        float top = 0.f, vtop = 0.f, r[8];
+        float top = 0.f, vtop = 0.f, odd = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const bool fine = fabsf(m[e]) < INFINITY;
-          r[e] = fine ? root(fminf(v[e], std::numeric_limits<float>::max())) : 0.f;
-          top = fmaxf(top, fine ? fabsf(m[e]) : 0.f);
+          top = fmaxf(top, fabsf(m[e]));
           vtop = fmaxf(vtop, r[e]);
-          m[e] = fine ? m[e] : __builtin_nanf("");
+          odd += 0.f * m[e];              // NaN, if one is not finite
+        }
+        if (!(odd == 0.f && vtop < INFINITY)) {
+          top = vtop = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool fine = fabsf(m[e]) < INFINITY;
+            r[e] = fine ? fminf(r[e], 0x1.fffffep63f) : 0.f;       // (the root of fp32's largest value)
+            m[e] = fine ? m[e] : __builtin_nanf("");
+            top = fmaxf(top, fine ? fabsf(m[e]) : 0.f);
+            vtop = fmaxf(vtop, r[e]);
+          }
         }
         ms = fmaxf(row_max(top) * (1.f / 448.f), kTiny);
         vs = fmaxf(row_max(vtop), kTiny);

@@ -436,3 +436,34 @@ def test_lists_are_checked_on_the_gpu_too():
     assert all(torch.equal(a, b) for a, b in zip(w, before))
     go()
     assert not torch.equal(w[0], before[0])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_second_moments_below_the_normal_range(bits):
+    # beta2 = 1/2 halves v; eps = 0: the update is m' / sqrt(v') to the bounds above
+    n = 64
+    w, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    state = pp.AdamWState([w], bits=bits)
+    v = torch.ldexp(torch.ones(n, device="cuda"), -148 + torch.arange(n, device="cuda"))      # 2^-148 .. 2^-85
+    m = v.sqrt() * 0.25
+    if bits == 32:
+        state.m[:n], state.v[:n] = m, v
+        pp.adamw_step([w], [g], state, lr=1.0, step=10 ** 6, betas=(0.5, 0.5), eps=0.0, weight_decay=0.0)
+        # (the least step there is 2^-149, so that half of an odd number of them is off by 2^-150; the update is of
+        # what is held)
+        assert bool(((state.v[:n].double() - v.double() / 2).abs() <= 2.0 ** -150).all())
+        want = -(m.double() / 2) / state.v[:n].double().sqrt()
+        assert bool(((w.double() - want).abs() <= 20 * U * want.abs()).all())
+    else:
+        pad = torch.zeros(B - n, device="cuda")
+        for name, t in zip(("m", "v", "m_scale", "v_scale"), encode(torch.cat([m, pad]), torch.cat([v, pad]))):
+            getattr(state, name).copy_(t)
+        # (the scales are 2^-42.5 and 2^-44.5 / 448: codes reach down to 2^-58 of the root; below it they are the least)
+        _, was = decode(*state.buffers())
+        pp.adamw_step([w], [g], state, lr=1.0, step=10 ** 6, betas=(0.5, 0.5), eps=0.0, weight_decay=0.0)
+        _, now = decode(*state.buffers())
+        assert bool(torch.isfinite(w).all()) and bool((now[:n] > 0).all()) and bool((now[n:] == 0).all())
+        root, held = (was / 2).sqrt()[:n], now.sqrt()[:n]
+        least = 1.125 * 2.0 ** -16 * float(state.v_scale[0])
+        want = root.clamp(min=least)
+        assert bool(((held - want).abs() <= 1.001 * 2.0 ** -5 * want).all())
