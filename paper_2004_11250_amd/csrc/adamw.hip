@@ -137,18 +137,19 @@ __device__ __forceinline__ void put_codes8(void* p, int64_t at, Codes c) {
 }
 
 // Eight elements a lane, a chunk of one tensor a workgroup; a block's scales are the
-// largest of 16 lanes.  fp32 w, g and moments: VGG-16, 15 M weights, 78 us (5.3 TB/s, in
-// part from the caches), 51 M weights 257 us (5.6 TB/s); bf16 w and g with 8-bit moments:
-// 102 M weights 198 us, 5.2 TB/s; fp32 w, bf16 g and copies, 8-bit moments, 31 M weights
-// 98 us, 5.1 TB/s.
-// With 8 bits what is read and written by 8 or 16 bytes a lane in a row goes past the
-// caches (102 M weights: 219 us without); what is read by 32 bytes a lane does not, where
-// each half would fetch the line again (VGG-16 78 us, past the caches 100).  Elements of
-// a workgroup, 32 bits 2048, 4096, 8192: VGG-16 78, 81, 86; 8 bits: 102 M 223, 198, 198,
-// 31 M 98, 99, 103.
-// The update's division is a product with the hardware's reciprocal, 1 ulp (exact
-// division: 102 M weights 232 us), and moments' codes are made by integer instructions and
-// the fp8 conversions: some 60 instructions an element at 10 bytes of memory.
+// largest of 16 lanes.  us a step into other arrays / in place: fp32 w, g and moments,
+// VGG-16, 15 M weights 78 / 62 (5.3 TB/s, 6.7 with the caches' help), 51 M weights 257;
+// bf16 w and g, 8-bit moments, 102 M weights 169 / 178 (6.1 TB/s); fp32 w, bf16 g and
+// copies, 8-bit moments, 31 M weights 86 / 89 (5.8 TB/s).
+// With 8 bits what a lane reads and writes by 8 or 16 bytes in a row goes past the
+// caches (102 M weights 186 / 193 without); what it reads by 32 bytes does not, where
+// each half would fetch the line again (VGG-16 78, past the caches 100).  Elements of a
+// workgroup, 32 bits 2048, 4096, 8192: VGG-16 78, 81, 86; 8 bits: 102 M 173, 169, 191.
+// With 8 bits some 45 instructions an element stand beside 10 bytes of memory, and count:
+// one root serves the update and the code, what only some steps need (masks, a tensor's
+// end, values that are not finite, roots below the normal range) is looked for by eight
+// elements together (all with it 193 / 213), and the update's division is a product with
+// the hardware's reciprocal, 1 ulp (an exact one: 175 / 197).
 template <class W, class G, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const Step s) {
   constexpr bool ONCE = BITS == 8;
