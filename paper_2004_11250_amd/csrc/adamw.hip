@@ -121,38 +121,69 @@ __device__ __forceinline__ uint32_t kept8(const uint16_t* keep, int64_t cell, in
   return bits >> (y - 9u * k);
 }
 
-template <bool ONCE>
-__device__ __forceinline__ Codes codes8(const void* p, int64_t at) {
-  const Codes* q = reinterpret_cast<const Codes*>(static_cast<const uint8_t*>(p) + at);
-  if constexpr (ONCE) return __builtin_nontemporal_load(q);
-  return *q;
+// A lane's eight elements: eight in a row, or (SPLIT) four and, 64 further on, four.
+template <bool SPLIT, bool ONCE, class S>
+__device__ __forceinline__ void load(const S* p, int64_t n, float (&v)[8]) {
+  if constexpr (!SPLIT) {
+    load8<ONCE>(p, n, v);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const Four<S> x = get<ONCE, Four<S>>(p + 64 * h, n - 64 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * h + e] = static_cast<float>(x[e]);
+    }
+  }
 }
-template <bool ONCE>
-__device__ __forceinline__ void put_codes8(void* p, int64_t at, Codes c) {
-  Codes* q = reinterpret_cast<Codes*>(static_cast<uint8_t*>(p) + at);
-  if constexpr (ONCE)
-    __builtin_nontemporal_store(c, q);
+template <bool SPLIT, bool ONCE, class S>
+__device__ __forceinline__ void store(S* p, int64_t n, const float (&v)[8]) {
+  if constexpr (!SPLIT) {
+    store8<ONCE>(p, n, v);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      Four<S> x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = static_cast<S>(v[4 * h + e]);
+      put<ONCE>(p + 64 * h, n - 64 * h, x);
+    }
+  }
+}
+template <bool SPLIT, bool ONCE>
+__device__ __forceinline__ Codes codes(const void* p, int64_t at) {
+  const uint8_t* q = static_cast<const uint8_t*>(p) + at;
+  if constexpr (SPLIT)
+    return {fetch<ONCE>(reinterpret_cast<const uint32_t*>(q)), fetch<ONCE>(reinterpret_cast<const uint32_t*>(q + 64))};
   else
-    *q = c;
+    return fetch<ONCE>(reinterpret_cast<const Codes*>(q));
+}
+template <bool SPLIT, bool ONCE>
+__device__ __forceinline__ void put_codes(void* p, int64_t at, Codes c) {
+  uint8_t* q = static_cast<uint8_t*>(p) + at;
+  if constexpr (SPLIT)
+    keep_at<ONCE>(reinterpret_cast<uint32_t*>(q), c[0]), keep_at<ONCE>(reinterpret_cast<uint32_t*>(q + 64), c[1]);
+  else
+    keep_at<ONCE>(reinterpret_cast<Codes*>(q), c);
 }
 
 // Eight elements a lane, a chunk of one tensor a workgroup; a block's scales are the
-// largest of 16 lanes.  us a step into other arrays / in place: fp32 w, g and moments,
-// VGG-16, 15 M weights 78 / 62 (5.3 TB/s, 6.7 with the caches' help), 51 M weights 257;
-// bf16 w and g, 8-bit moments, 102 M weights 169 / 178 (6.1 TB/s); fp32 w, bf16 g and
-// copies, 8-bit moments, 31 M weights 86 / 89 (5.8 TB/s).
-// With 8 bits what a lane reads and writes by 8 or 16 bytes in a row goes past the
-// caches (102 M weights 186 / 193 without); what it reads by 32 bytes does not, where
-// each half would fetch the line again (VGG-16 78, past the caches 100).  Elements of a
-// workgroup, 32 bits 2048, 4096, 8192: VGG-16 78, 81, 86; 8 bits: 102 M 173, 169, 191.
+// largest of 16 lanes.  Three states in turn, us a step in place / into other arrays:
+// fp32 w, g and moments, VGG-16, 15 M weights 75 / 75 (5.5 TB/s), 51 M 237 / 237
+// (6.05 TB/s); bf16 w and g, 8-bit moments, 102 M 172 / 172 (6.0 TB/s); fp32 w, bf16 g
+// and copies, 8-bit moments, 31 M 104 / 99 (5.0 TB/s).
+// Where a value has four bytes a lane's eight are two fours 64 elements apart, so that
+// each access of 16 lanes is 256 bytes in a row (eight in a row are two accesses of half
+// of each line: 51 M fp32 weights 263, and past the caches 362).
+// Elements of a workgroup, 32 bits 2048, 4096: 51 M fp32 237, 247; 8 bits 2048, 4096,
+// 8192: 102 M 173, 169, 191.
 // With 8 bits some 45 instructions an element stand beside 10 bytes of memory, and count:
 // one root serves the update and the code, what only some steps need (masks, a tensor's
 // end, values that are not finite, roots below the normal range) is looked for by eight
 // elements together (all with it 193 / 213), and the update's division is a product with
 // the hardware's reciprocal, 1 ulp (an exact one: 175 / 197).
-template <class W, class G, int BITS>
+template <class W, class G, int BITS, bool ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const Step s) {
-  constexpr bool ONCE = BITS == 8;
+  constexpr bool SPLIT = sizeof(W) == 4 || sizeof(G) == 4 || BITS == 32;
   int chunk;
   const Tensor& t = list.item[find(list, blockIdx.x, &chunk)];
   const int64_t e0 = static_cast<int64_t>(chunk) * s.chunk, n = t.n, left = n - e0;
@@ -179,22 +210,22 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
   }
   const float rate = static_cast<float>(lr * c1), decay = static_cast<float>(1. - lr * static_cast<double>(t.decay));
 
-  for (int x = 8 * threadIdx.x; x < len; x += 2048) {
+  for (int x = SPLIT ? 4 * (threadIdx.x & 15) + kBlock * (threadIdx.x >> 4) : 8 * threadIdx.x; x < len; x += 2048) {
     const int64_t there = left - x;     // elements from here on
     float w[8], g[8], m[8], v[8];
     Codes mc, vc;
     float ms, vs;
-    load8<ONCE && sizeof(W) == 2>(w_in + x, there, w);
-    load8<ONCE && sizeof(G) == 2>(g_in + x, there, g);
+    load<SPLIT, ONCE>(w_in + x, there, w);
+    load<SPLIT, ONCE>(g_in + x, there, g);
     if constexpr (BITS == 32) {
-      load8<ONCE>(static_cast<const float*>(s.m) + at + x, 8, m);
-      load8<ONCE>(static_cast<const float*>(s.v) + at + x, 8, v);
+      load<SPLIT, ONCE>(static_cast<const float*>(s.m) + at + x, kBlock, m);
+      load<SPLIT, ONCE>(static_cast<const float*>(s.v) + at + x, kBlock, v);
     } else {
-      mc = codes8<ONCE>(s.m, at + x);
-      vc = codes8<ONCE>(s.v, at + x);
+      mc = codes<SPLIT, ONCE>(s.m, at + x);
+      vc = codes<SPLIT, ONCE>(s.v, at + x);
       ms = s.ms[block + x / kBlock], vs = s.vs[block + x / kBlock];
     }
-    const uint32_t on = keep ? kept8(keep, cell, tap, cells, x) : 255u;
+    const uint32_t on = !keep ? 255u : SPLIT ? (kept8(keep, cell, tap, cells, x) & 15u) | kept8(keep, cell, tap, cells, x + 64) << 4 : kept8(keep, cell, tap, cells, x);
     if (go) {
       if constexpr (BITS == 8) m_values(mc, ms, m), v_values(vc, vs, v);
 #pragma unroll
@@ -208,10 +239,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
         for (int e = 0; e < 8; ++e)
           if (!(on >> e & 1)) m[e] = v[e] = 0.f;
       }
-      if (there < 8) {
+      if (there < (SPLIT ? 68 : 8)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e >= there) m[e] = v[e] = 0.f;
+          if ((SPLIT && e >= 4 ? e + 60 : e) >= there) m[e] = v[e] = 0.f;
       }
       float r[8];
       roots(v, r);
@@ -256,15 +287,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       }
     }
     if (there > 0) {
-      store8<ONCE && sizeof(W) == 2>(w_out + x, there, w);
-      if (copy) store8<ONCE>(copy + x, there, w);
+      store<SPLIT, ONCE>(w_out + x, there, w);
+      if (copy) store<SPLIT, ONCE>(copy + x, there, w);
     }
     if constexpr (BITS == 32) {
-      store8<ONCE>(static_cast<float*>(s.m_out) + at + x, 8, m);
-      store8<ONCE>(static_cast<float*>(s.v_out) + at + x, 8, v);
+      store<SPLIT, ONCE>(static_cast<float*>(s.m_out) + at + x, kBlock, m);
+      store<SPLIT, ONCE>(static_cast<float*>(s.v_out) + at + x, kBlock, v);
     } else {
-      put_codes8<ONCE>(s.m_out, at + x, mc);
-      put_codes8<ONCE>(s.v_out, at + x, vc);
+      put_codes<SPLIT, ONCE>(s.m_out, at + x, mc);
+      put_codes<SPLIT, ONCE>(s.v_out, at + x, vc);
       if (threadIdx.x % 16 == 0) s.ms_out[block + x / kBlock] = ms, s.vs_out[block + x / kBlock] = vs;
     }
   }
@@ -277,11 +308,11 @@ __global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const uin
   for (int64_t x = 8 * (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x); x < all; x += static_cast<int64_t>(gridDim.x) * 2048) {
     float a[8];
     if (m_out) {
-      m_values(codes8<false>(m, x), ms[x / kBlock], a);
+      m_values(codes<false, false>(m, x), ms[x / kBlock], a);
       store8(m_out + x, 8, a);
     }
     if (v_out) {
-      v_values(codes8<false>(v, x), vs[x / kBlock], a);
+      v_values(codes<false, false>(v, x), vs[x / kBlock], a);
       store8(v_out + x, 8, a);
     }
   }
@@ -435,6 +466,11 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   s.m = d.m, s.v = d.v, s.ms = d.m_scale, s.vs = d.v_scale;
   s.m_out = d.m_out, s.v_out = d.v_out, s.ms_out = d.m_scale_out, s.vs_out = d.v_scale_out;
   s.chunk = chunk_of(total, d.bits == 8 ? 4096 : 2048);
+  // Steps of more than the last cache holds (256 MB) go past the caches.  us, past them /
+  // not, three states in turn in place: 15 M fp32 weights 75 / 85, 51 M 237 / 265, with
+  // 8-bit moments 131 / 140, 102 M bf16 weights with 8-bit moments 172 / 192; 3 M fp32
+  // weights (86 MB) 17.9 / 15.5, 8 M bf16 with 8-bit moments (82 MB) 19.9 / 18.1.
+  const bool past = total * static_cast<double>(2 * size_of(d.w_dtype) + size_of(d.g_dtype) + (d.bits == 8 ? 4 : 16)) > 256e6;
   auto fill = [](Tensor& x, const pp_adamw_tensor& t) {
     x = {t.w, t.g, t.w_out, static_cast<bf16*>(t.copy), t.keep, t.n, t.at, static_cast<float>(t.weight_decay)};
   };
@@ -442,7 +478,10 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
     using W = decltype(w);
     using G = decltype(g);
     return each_launch<Tensors>(tensors, count, s.chunk, fill, [&](const Tensors& list, uint32_t blocks) {
-      hipLaunchKernelGGL((adamw_kernel<W, G, decltype(bits)::value>), dim3(blocks), dim3(256), 0, st, list, s);
+      if (past)
+        hipLaunchKernelGGL((adamw_kernel<W, G, decltype(bits)::value, true>), dim3(blocks), dim3(256), 0, st, list, s);
+      else
+        hipLaunchKernelGGL((adamw_kernel<W, G, decltype(bits)::value, false>), dim3(blocks), dim3(256), 0, st, list, s);
     });
   };
   auto with_g = [&](auto w, auto bits) { return d.g_dtype == PP_BF16 ? launch(w, bf16(), bits) : launch(w, float(), bits); };

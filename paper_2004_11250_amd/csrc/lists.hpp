@@ -8,38 +8,55 @@
 
 namespace pp {
 
-// Eight consecutive values; the hardware loads and stores 16 bytes at any
-// address of the element's own alignment.
+// Consecutive values; the hardware loads and stores 16 bytes at any address of the
+// element's own alignment.
 template <class S>
 using Eight = __attribute__((ext_vector_type(8), aligned(sizeof(S)))) S;
+template <class S>
+using Four = __attribute__((ext_vector_type(4), aligned(sizeof(S)))) S;
 
-// n values from p on (n >= 8: eight), 0 in the place of the others.  ONCE: they
-// are not read again soon, and take no room in the caches.
+// ONCE: it is not used again soon, and takes no room in the caches
+template <bool ONCE, class T>
+__device__ __forceinline__ T fetch(const T* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(p);
+  return *p;
+}
+template <bool ONCE, class T>
+__device__ __forceinline__ void keep_at(T* p, T x) {
+  if constexpr (ONCE)
+    __builtin_nontemporal_store(x, p);
+  else
+    *p = x;
+}
+
+// The n values from p on, or as many as a vector has; 0 in the place of the others.
+template <bool ONCE, class V, class S>
+__device__ __forceinline__ V get(const S* p, int64_t n) {
+  constexpr int N = sizeof(V) / sizeof(S);
+  if (n >= N) return fetch<ONCE>(reinterpret_cast<const V*>(p));
+  V x;
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] = e < n ? p[e] : static_cast<S>(0.f);
+  return x;
+}
+template <bool ONCE, class V, class S>
+__device__ __forceinline__ void put(S* p, int64_t n, const V& x) {
+  constexpr int N = sizeof(V) / sizeof(S);
+  if (n >= N) {
+    keep_at<ONCE>(reinterpret_cast<V*>(p), x);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < n) p[e] = x[e];
+  }
+}
 template <bool ONCE = false, class S>
 __device__ __forceinline__ Eight<S> get8(const S* p, int64_t n) {
-  if (n >= 8) {
-    const Eight<S>* q = reinterpret_cast<const Eight<S>*>(p);
-    if constexpr (ONCE) return __builtin_nontemporal_load(q);
-    return *q;
-  }
-  Eight<S> x;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = e < n ? p[e] : static_cast<S>(0.f);
-  return x;
+  return get<ONCE, Eight<S>>(p, n);
 }
 template <bool ONCE = false, class S>
 __device__ __forceinline__ void put8(S* p, int64_t n, const Eight<S>& x) {
-  if (n >= 8) {
-    Eight<S>* q = reinterpret_cast<Eight<S>*>(p);
-    if constexpr (ONCE)
-      __builtin_nontemporal_store(x, q);
-    else
-      *q = x;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) p[e] = x[e];
-  }
+  put<ONCE>(p, n, x);
 }
 // the same by way of fp32
 template <bool ONCE = false, class S>

@@ -467,3 +467,11 @@ def test_second_moments_below_the_normal_range(bits):
         least = 1.125 * 2.0 ** -16 * float(state.v_scale[0])
         want = root.clamp(min=least)
         assert bool(((held - want).abs() <= 1.001 * 2.0 ** -5 * want).all())
+
+
+@pytest.mark.parametrize("w,g,bits", [("f32", "f32", 32), ("f32", "bf16", 32), ("bf16", "bf16", 32), ("bf16", "f32", 32), ("f32", "bf16", 8),
+                                      ("f32", "f32", 8), ("bf16", "bf16", 8), ("bf16", "f32", 8)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_steps_past_the_caches(w, g, bits, shift):
+    # more than 256 MB in all: the small tensors of the list go the same way
+    check(Run(12, SHAPES + [(26000011,)], w, g, bits, keep=(6,), shift=shift))
