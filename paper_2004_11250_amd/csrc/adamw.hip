@@ -121,39 +121,12 @@ __device__ __forceinline__ uint32_t kept8(const uint16_t* keep, int64_t cell, in
   return bits >> (y - 9u * k);
 }
 
-// A lane's eight elements: eight in a row, or (SPLIT) four and, 64 further on, four.
-template <bool SPLIT, bool ONCE, class S>
-__device__ __forceinline__ void load(const S* p, int64_t n, float (&v)[8]) {
-  if constexpr (!SPLIT) {
-    load8<ONCE>(p, n, v);
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const Four<S> x = get<ONCE, Four<S>>(p + 64 * h, n - 64 * h);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * h + e] = static_cast<float>(x[e]);
-    }
-  }
-}
-template <bool SPLIT, bool ONCE, class S>
-__device__ __forceinline__ void store(S* p, int64_t n, const float (&v)[8]) {
-  if constexpr (!SPLIT) {
-    store8<ONCE>(p, n, v);
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      Four<S> x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = static_cast<S>(v[4 * h + e]);
-      put<ONCE>(p + 64 * h, n - 64 * h, x);
-    }
-  }
-}
+constexpr int kFar = kBlock / 2;   // (the second half of a lane's elements, where they are two fours)
 template <bool SPLIT, bool ONCE>
 __device__ __forceinline__ Codes codes(const void* p, int64_t at) {
   const uint8_t* q = static_cast<const uint8_t*>(p) + at;
   if constexpr (SPLIT)
-    return {fetch<ONCE>(reinterpret_cast<const uint32_t*>(q)), fetch<ONCE>(reinterpret_cast<const uint32_t*>(q + 64))};
+    return {fetch<ONCE>(reinterpret_cast<const uint32_t*>(q)), fetch<ONCE>(reinterpret_cast<const uint32_t*>(q + kFar))};
   else
     return fetch<ONCE>(reinterpret_cast<const Codes*>(q));
 }
@@ -161,7 +134,7 @@ template <bool SPLIT, bool ONCE>
 __device__ __forceinline__ void put_codes(void* p, int64_t at, Codes c) {
   uint8_t* q = static_cast<uint8_t*>(p) + at;
   if constexpr (SPLIT)
-    keep_at<ONCE>(reinterpret_cast<uint32_t*>(q), c[0]), keep_at<ONCE>(reinterpret_cast<uint32_t*>(q + 64), c[1]);
+    keep_at<ONCE>(reinterpret_cast<uint32_t*>(q), c[0]), keep_at<ONCE>(reinterpret_cast<uint32_t*>(q + kFar), c[1]);
   else
     keep_at<ONCE>(reinterpret_cast<Codes*>(q), c);
 }
@@ -183,7 +156,7 @@ __device__ __forceinline__ void put_codes(void* p, int64_t at, Codes c) {
 // the hardware's reciprocal, 1 ulp (an exact one: 175 / 197).
 template <class W, class G, int BITS, bool ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const Step s) {
-  constexpr bool SPLIT = sizeof(W) == 4 || sizeof(G) == 4 || BITS == 32;
+  constexpr bool SPLIT = kSplit<W, G> || BITS == 32;
   int chunk;
   const Tensor& t = list.item[find(list, blockIdx.x, &chunk)];
   const int64_t e0 = static_cast<int64_t>(chunk) * s.chunk, n = t.n, left = n - e0;
@@ -215,17 +188,17 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
     float w[8], g[8], m[8], v[8];
     Codes mc, vc;
     float ms, vs;
-    load<SPLIT, ONCE>(w_in + x, there, w);
-    load<SPLIT, ONCE>(g_in + x, there, g);
+    load8<SPLIT, ONCE>(w_in + x, there, kFar, w);
+    load8<SPLIT, ONCE>(g_in + x, there, kFar, g);
     if constexpr (BITS == 32) {
-      load<SPLIT, ONCE>(static_cast<const float*>(s.m) + at + x, kBlock, m);
-      load<SPLIT, ONCE>(static_cast<const float*>(s.v) + at + x, kBlock, v);
+      load8<SPLIT, ONCE>(static_cast<const float*>(s.m) + at + x, kBlock, kFar, m);
+      load8<SPLIT, ONCE>(static_cast<const float*>(s.v) + at + x, kBlock, kFar, v);
     } else {
       mc = codes<SPLIT, ONCE>(s.m, at + x);
       vc = codes<SPLIT, ONCE>(s.v, at + x);
       ms = s.ms[block + x / kBlock], vs = s.vs[block + x / kBlock];
     }
-    const uint32_t on = !keep ? 255u : SPLIT ? (kept8(keep, cell, tap, cells, x) & 15u) | kept8(keep, cell, tap, cells, x + 64) << 4 : kept8(keep, cell, tap, cells, x);
+    const uint32_t on = !keep ? 255u : SPLIT ? (kept8(keep, cell, tap, cells, x) & 15u) | kept8(keep, cell, tap, cells, x + kFar) << 4 : kept8(keep, cell, tap, cells, x);
     if (go) {
       if constexpr (BITS == 8) m_values(mc, ms, m), v_values(vc, vs, v);
 #pragma unroll
@@ -239,10 +212,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
         for (int e = 0; e < 8; ++e)
           if (!(on >> e & 1)) m[e] = v[e] = 0.f;
       }
-      if (there < (SPLIT ? 68 : 8)) {
+      if (there < (SPLIT ? kFar + 4 : 8)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if ((SPLIT && e >= 4 ? e + 60 : e) >= there) m[e] = v[e] = 0.f;
+          if ((SPLIT && e >= 4 ? e - 4 + kFar : e) >= there) m[e] = v[e] = 0.f;
       }
       float r[8];
       roots(v, r);
@@ -287,12 +260,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       }
     }
     if (there > 0) {
-      store<SPLIT, ONCE>(w_out + x, there, w);
-      if (copy) store<SPLIT, ONCE>(copy + x, there, w);
+      store8<SPLIT, ONCE>(w_out + x, there, kFar, w);
+      if (copy) store8<SPLIT, ONCE>(copy + x, there, kFar, w);
     }
     if constexpr (BITS == 32) {
-      store<SPLIT, ONCE>(static_cast<float*>(s.m_out) + at + x, kBlock, m);
-      store<SPLIT, ONCE>(static_cast<float*>(s.v_out) + at + x, kBlock, v);
+      store8<SPLIT, ONCE>(static_cast<float*>(s.m_out) + at + x, kBlock, kFar, m);
+      store8<SPLIT, ONCE>(static_cast<float*>(s.v_out) + at + x, kBlock, kFar, v);
     } else {
       put_codes<SPLIT, ONCE>(s.m_out, at + x, mc);
       put_codes<SPLIT, ONCE>(s.v_out, at + x, vc);
@@ -305,15 +278,17 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
 template <class S>
 __global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const uint8_t* v, const float* ms, const float* vs,
                                                      int64_t all, S* m_out, S* v_out) {
-  for (int64_t x = 8 * (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x); x < all; x += static_cast<int64_t>(gridDim.x) * 2048) {
+  constexpr bool SPLIT = kSplit<S>;
+  const int lane = SPLIT ? 4 * (threadIdx.x & 15) + kBlock * (threadIdx.x >> 4) : 8 * threadIdx.x;
+  for (int64_t x = static_cast<int64_t>(blockIdx.x) * 2048 + lane; x < all; x += static_cast<int64_t>(gridDim.x) * 2048) {
     float a[8];
     if (m_out) {
-      m_values(codes<false, false>(m, x), ms[x / kBlock], a);
-      store8(m_out + x, 8, a);
+      m_values(codes<SPLIT, false>(m, x), ms[x / kBlock], a);
+      store8<SPLIT>(m_out + x, kBlock, kFar, a);
     }
     if (v_out) {
-      v_values(codes<false, false>(v, x), vs[x / kBlock], a);
-      store8(v_out + x, 8, a);
+      v_values(codes<SPLIT, false>(v, x), vs[x / kBlock], a);
+      store8<SPLIT>(v_out + x, kBlock, kFar, a);
     }
   }
 }
@@ -346,9 +321,10 @@ __global__ __launch_bounds__(256) void square_kernel(const Grads list, int32_t s
   const int len = static_cast<int>(left < size ? left : size);
   const G* p = static_cast<const G*>(t.g) + e0;
   double sum[2] = {0., 0.};
-  for (int x = 8 * threadIdx.x; x < len; x += 2048) {
+  constexpr bool SPLIT = kSplit<G>;
+  for (int x = SPLIT ? 4 * (threadIdx.x & 63) + 512 * (threadIdx.x >> 6) : 8 * threadIdx.x; x < len; x += 2048) {
     float g[8];
-    load8(p + x, len - x, g);
+    load8<SPLIT>(p + x, len - x, 256, g);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e & 1] += static_cast<double>(g[e]) * g[e];
   }

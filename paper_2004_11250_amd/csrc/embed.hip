@@ -24,7 +24,7 @@ namespace {
 
 using bf16 = __bf16;
 
-// A row is read by 2^lanes lanes of a workgroup of 256, eight features each, and
+// A row is read by 2^log lanes of a workgroup of 256, eight features each, and
 // by as many columns of the grid as that needs.
 struct Lanes {
   int32_t log, columns;
@@ -34,6 +34,14 @@ Lanes lanes_for(int64_t d) {
   while (log < 8 && (int64_t(8) << log) < d) ++log;
   return {log, static_cast<int32_t>(cdiv(d, int64_t(8) << log))};
 }
+
+// The first of a lane's features, and how far the second four are from it (SPLIT).
+template <bool SPLIT>
+__device__ __forceinline__ int first_of(int log) {
+  const int lane = threadIdx.x & ((1 << log) - 1);
+  return (static_cast<int>(blockIdx.y) << log) * 8 + lane * (SPLIT ? 4 : 8);
+}
+__device__ __forceinline__ int far_of(int log) { return 4 << log; }
 
 struct Look {
   const int64_t* ids;
@@ -47,23 +55,25 @@ struct Look {
 // A group of lanes a token.  Bound by memory: 8192 tokens of 1024 bf16 features from a
 // table of 50000 6.4 us (5.2 TB/s), 65536 39.6 (two, four and eight tokens of a group,
 // read together: 6.6, 7.0 and 7.9, the last ones' waves leave the card too early);
-// one token 1.8, the launch.
+// one token 1.8, the launch.  16384 tokens of 4096 fp32 features 86 us, 6.3 TB/s (a lane's
+// eight in a row instead of two fours: 96; their gradient into 20000 rows 122 and 163).
 template <class W, class Y>
 __global__ __launch_bounds__(256) void look_kernel(const Look a) {
-  const int c = ((blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1))) * 8, cols = a.d - c;
+  constexpr bool SPLIT = kSplit<W, Y>;
+  const int c = first_of<SPLIT>(a.lanes), cols = a.d - c, far = far_of(a.lanes);
   const int64_t t = static_cast<int64_t>(blockIdx.x) * (256 >> a.lanes) + (threadIdx.x >> a.lanes);
   if (cols <= 0 || t >= a.t) return;
   const int64_t id = a.ids[t];
   float y[8];
   if (id != a.ignore && static_cast<uint64_t>(id) < static_cast<uint64_t>(a.v)) {
-    load8(static_cast<const W*>(a.w) + id * a.w_ld + c, cols, y);
+    load8<SPLIT>(static_cast<const W*>(a.w) + id * a.w_ld + c, cols, far, y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] *= a.scale;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) y[e] = id == a.ignore ? 0.f : __builtin_nanf("");
   }
-  store8(static_cast<Y*>(a.y) + t * a.y_ld + c, cols, y);
+  store8<SPLIT>(static_cast<Y*>(a.y) + t * a.y_ld + c, cols, far, y);
 }
 
 // ---------------------------------------------------------------------------
@@ -412,29 +422,28 @@ struct Sum {
 
 constexpr int kBatch = 8;
 
-template <class W>
+template <bool SPLIT, class W>
 __device__ __forceinline__ void put_row(const Sum& a, int64_t row, int c, const float (&acc)[8]) {
   float x[8] = {};
   const int64_t at = row * a.w_ld + c;
-  if (a.add) load8(static_cast<const W*>(a.add) + at, a.d - c, x);
+  if (a.add) load8<SPLIT>(static_cast<const W*>(a.add) + at, a.d - c, far_of(a.lanes), x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] += a.scale * acc[e];
-  store8(static_cast<W*>(a.dw) + at, a.d - c, x);
+  store8<SPLIT>(static_cast<W*>(a.dw) + at, a.d - c, far_of(a.lanes), x);
 }
 
 // Rows without a token, of kFillRows a group of lanes: what they are added to, or 0.
 // They lie between the tokens' workgroups in one launch, which is bound by memory then:
 // 8192 tokens into 50000 x 1024 bf16 21 us, 5.7 TB/s (in a launch before it, together
 // with the sort: 22 + 9.5 in place of 7.5 + 21); added to another gradient, 32768 tokens,
-// 47 us, 6 TB/s, 67 without the hint that what is copied is not read again.  (The hint
-// only for values of two bytes: a lane's eight of four bytes are two accesses, and the
-// second would fetch the same lines again, 205 MB 99 us in place of 46.  Rows of a group:
-// 4; 8 and 16 take 49 and 54 us.)
+// 47 us, 6 TB/s, 67 without the hint that what is copied is not read again.  (Rows of a
+// group: 4; 8 and 16 take 49 and 54 us.)
 constexpr int kFillRows = 4;
 template <class W>
 __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
+  constexpr bool SPLIT = kSplit<W>;
   const int groups = 256 >> a.lanes, g = threadIdx.x >> a.lanes;
-  const int c = ((blockIdx.y << a.lanes) + (threadIdx.x & ((1 << a.lanes) - 1))) * 8, cols = a.d - c;
+  const int c = first_of<SPLIT>(a.lanes), cols = a.d - c, far = far_of(a.lanes);
   if (cols <= 0) return;
   const int64_t first = static_cast<int64_t>(block) * groups * kFillRows + g;
   int64_t at[kFillRows];
@@ -447,11 +456,11 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
   if (a.add) {
 #pragma unroll
     for (int u = 0; u < kFillRows; ++u)
-      if (at[u] >= 0) x[u] = get8<sizeof(W) == 2>(static_cast<const W*>(a.add) + at[u], cols);
+      if (at[u] >= 0) x[u] = get8<SPLIT, true>(static_cast<const W*>(a.add) + at[u], cols, far);
   }
 #pragma unroll
   for (int u = 0; u < kFillRows; ++u)
-    if (at[u] >= 0) put8<sizeof(W) == 2>(static_cast<W*>(a.dw) + at[u], cols, x[u]);
+    if (at[u] >= 0) put8<SPLIT, true>(static_cast<W*>(a.dw) + at[u], cols, far, x[u]);
 }
 
 // A workgroup sums the piece p0 .. p1 of a list, a group of lanes a part of it, of
@@ -467,8 +476,9 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
 template <class Y, class W, int THREADS>
 __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int p0, int p1, int batches, Place (&at)[kBatch],
                                           int32_t prev, int32_t next, float* part, float (*edge)[8], int32_t* edge_row) {
+  constexpr bool SPLIT = kSplit<Y, W>;
   const int groups = THREADS >> a.lanes, g = threadIdx.x >> a.lanes, lane = threadIdx.x & ((1 << a.lanes) - 1);
-  const int c = ((blockIdx.y << a.lanes) + lane) * 8, cols = a.d - c;
+  const int c = first_of<SPLIT>(a.lanes), cols = a.d - c, far = far_of(a.lanes);
   const Y* dy = static_cast<const Y*>(a.dy) + c;
   const int i0 = p0 + g * batches * kBatch, i1 = min(i0 + batches * kBatch, p1);
 
@@ -488,7 +498,7 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
     }
     if (cols > 0) {
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) x[u] = get8<sizeof(Y) == 2>(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols);
+      for (int u = 0; u < kBatch; ++u) x[u] = get8<SPLIT, true>(dy + (i + u < i1 ? at[u].token : at[0].token) * a.y_ld, cols, far);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -498,7 +508,7 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
           if (first)
             to_edge(2 * g), first = false;
           else if (cols > 0)
-            put_row<W>(a, cur, c, acc);
+            put_row<SPLIT, W>(a, cur, c, acc);
         }
         cur = at[u].row;
 #pragma unroll
@@ -550,9 +560,9 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
     }
     const bool from = s == 0 && prev == row, on = !ends && next == row;
     if (from || on)
-      store8(part + static_cast<int64_t>(!from) * a.part_ld + c, 8, acc);
+      store8<SPLIT>(part + static_cast<int64_t>(!from) * a.part_ld + c, a.part_ld - c, far, acc);
     else
-      put_row<W>(a, row, c, acc);
+      put_row<SPLIT, W>(a, row, c, acc);
   }
 }
 
@@ -647,7 +657,8 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(const Sort s, const Sum
 
   if (a.add == a.dw) return;
   constexpr int kRows = 4;
-  const int groups = kFewTokens >> a.lanes, c = ((blockIdx.y << a.lanes) + (tid & ((1 << a.lanes) - 1))) * 8, cols = a.d - c;
+  constexpr bool SPLIT = kSplit<W>;
+  const int groups = kFewTokens >> a.lanes, c = first_of<SPLIT>(a.lanes), cols = a.d - c, far = far_of(a.lanes);
   if (cols <= 0) return;
   for (int l = tid >> a.lanes; l < s.deal.per; l += kRows * groups) {
     Eight<W> x[kRows] = {};
@@ -661,11 +672,11 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(const Sort s, const Sum
     if (a.add) {
 #pragma unroll
       for (int u = 0; u < kRows; ++u)
-        if (to[u] >= 0) x[u] = get8<sizeof(W) == 2>(static_cast<const W*>(a.add) + to[u], cols);
+        if (to[u] >= 0) x[u] = get8<SPLIT, true>(static_cast<const W*>(a.add) + to[u], cols, far);
     }
 #pragma unroll
     for (int u = 0; u < kRows; ++u)
-      if (to[u] >= 0) put8<sizeof(W) == 2>(static_cast<W*>(a.dw) + to[u], cols, x[u]);
+      if (to[u] >= 0) put8<SPLIT, true>(static_cast<W*>(a.dw) + to[u], cols, far, x[u]);
   }
 }
 

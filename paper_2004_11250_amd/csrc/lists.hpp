@@ -50,27 +50,43 @@ __device__ __forceinline__ void put(S* p, int64_t n, const V& x) {
       if (e < n) p[e] = x[e];
   }
 }
-template <bool ONCE = false, class S>
-__device__ __forceinline__ Eight<S> get8(const S* p, int64_t n) {
-  return get<ONCE, Eight<S>>(p, n);
+
+// A lane's eight of the n values from p on: in a row, or (SPLIT) four, and four `far`
+// values further on.  Lanes that lie 8, or 4, values apart then have 16 bytes in a row
+// at each access, whole lines together.
+template <class... S>
+constexpr bool kSplit = ((sizeof(S) == 4) || ...);
+template <bool SPLIT, bool ONCE = false, class S>
+__device__ __forceinline__ Eight<S> get8(const S* p, int64_t n, int far) {
+  if constexpr (SPLIT) {
+    const Four<S> x = get<ONCE, Four<S>>(p, n), y = get<ONCE, Four<S>>(p + far, n - far);
+    return {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  } else {
+    return get<ONCE, Eight<S>>(p, n);
+  }
 }
-template <bool ONCE = false, class S>
-__device__ __forceinline__ void put8(S* p, int64_t n, const Eight<S>& x) {
-  put<ONCE>(p, n, x);
+template <bool SPLIT, bool ONCE = false, class S>
+__device__ __forceinline__ void put8(S* p, int64_t n, int far, const Eight<S>& x) {
+  if constexpr (SPLIT) {
+    put<ONCE>(p, n, Four<S>{x[0], x[1], x[2], x[3]});
+    put<ONCE>(p + far, n - far, Four<S>{x[4], x[5], x[6], x[7]});
+  } else {
+    put<ONCE>(p, n, x);
+  }
 }
 // the same by way of fp32
-template <bool ONCE = false, class S>
-__device__ __forceinline__ void load8(const S* p, int64_t n, float (&v)[8]) {
-  const Eight<S> x = get8<ONCE>(p, n);
+template <bool SPLIT, bool ONCE = false, class S>
+__device__ __forceinline__ void load8(const S* p, int64_t n, int far, float (&v)[8]) {
+  const Eight<S> x = get8<SPLIT, ONCE>(p, n, far);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(x[e]);
 }
-template <bool ONCE = false, class S>
-__device__ __forceinline__ void store8(S* p, int64_t n, const float (&v)[8]) {
+template <bool SPLIT, bool ONCE = false, class S>
+__device__ __forceinline__ void store8(S* p, int64_t n, int far, const float (&v)[8]) {
   Eight<S> x;
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = static_cast<S>(v[e]);
-  put8<ONCE>(p, n, x);
+  put8<SPLIT, ONCE>(p, n, far, x);
 }
 
 // A list's tensors in a kernel's arguments (which hold 4 KB), each with the
