@@ -679,7 +679,7 @@ typedef struct {
  *   w, y  device [v][d] and [t][d] (rows w_ld and y_ld apart); y may overlap neither
  *         of the others
  * pp_embed_workspace -- device bytes pp_embed_bwd needs: up to 8 v + 16 t, about
- * 0.5 MB, and up to 2048 rows of d fp32 values for rows of the table that many
+ * 0.6 MB, and up to 2048 rows of d fp32 values for rows of the table that many
  * tokens share.
  * pp_embed_bwd
  *   dy         device [t][d]

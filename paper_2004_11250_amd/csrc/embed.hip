@@ -136,9 +136,9 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   const uint32_t most = kSortWords - per;
   for (int i = lane; i < per; i += 64) count[wave * per + i] = 0;   // (a wave's own until all have counted)
 
-  // All of a wave's tokens: those of the workgroup's rows go on a list in LDS, and
-  // `use(list's length, the token that its entries count from)` takes it when it is
-  // full (the last list is left to the caller).
+  // All of a wave's tokens: those of the workgroup's rows go on a list in LDS, of `mine`
+  // entries that count tokens from `base` on, and `use` takes it when it is full (the
+  // last list is left to the caller).
   constexpr int kAtOnce = 8, kStep = 64 * kAtOnce;
   uint32_t below = 0, mine = 0;
   int base = t0;
@@ -248,19 +248,19 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
   place();
 }
 
-// The same by digits of the row's number, without a workgroup that has all tokens of
-// a row: one digit for tables of up to kSortRows rows, two for others, the lower
-// first.  A workgroup has `each` places of the list so far.  count_kernel counts its
+// The same by digits of the row's number, up to kOwnBits bits each, the lowest first,
+// without a workgroup that has all tokens of a row.  A workgroup has `each` places of the list so far.  count_kernel counts its
 // tokens of each digit; place_kernel adds up the counts, which gives each workgroup
 // the places of its tokens of each digit, and puts them there, in their order.  32768
 // pixels 2.7 and 5.5 us: latency, of ids, counts, a scan and an exchange in turn.
 constexpr int64_t kCounts = 128;                // workgroups at most
 struct Digit {
   const int64_t* ids;           // the first digit's list
-  const Place* in;              // the second's, and its length
+  const Place* in;              // the others', and its length
   const int32_t* in_total;
   int32_t* clear;               // [cleared] values that the first digit's count_kernel sets to 0
   int64_t cleared;
+  int32_t groups;               // workgroups that count (others only clear)
   uint32_t* count;              // [workgroups][values]
   int32_t* start;               // [values + 1]: where each value's tokens begin
   Place* order;
@@ -302,12 +302,13 @@ struct WaveTokens {
 template <bool FIRST>
 __global__ __launch_bounds__(kSortWaves * 64) void count_kernel(const Digit a) {
   __shared__ uint32_t count[kSortRows];
-  const WaveTokens<FIRST> tokens(a);
-  count[threadIdx.x] = 0;
-  __syncthreads();
   if constexpr (FIRST)
     for (int64_t i = static_cast<int64_t>(blockIdx.x) * kSortWaves * 64 + threadIdx.x; i < a.cleared; i += static_cast<int64_t>(gridDim.x) * kSortWaves * 64)
       a.clear[i] = 0;
+  if (static_cast<int>(blockIdx.x) >= a.groups) return;
+  const WaveTokens<FIRST> tokens(a);
+  count[threadIdx.x] = 0;
+  __syncthreads();
   tokens.each(a, [&](int, int, int k) {
     if (k >= 0) atomicAdd(&count[k], 1u);
   });
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(kSortWaves * 64) void place_kernel(const Digit a) {
   });
 }
 
-// Where each row's tokens begin and end in a list sorted by two digits; rows without
+// Where each row's tokens begin and end in a list sorted by several digits; rows without
 // tokens have 0 and 0 already.
 __global__ __launch_bounds__(256) void bounds_kernel(const Place* order, const int32_t* total, int32_t* begin, int32_t* end) {
   const int n = *total;
@@ -757,9 +758,9 @@ struct Plan {
   Deal deal;
   bool few;                     // one launch
   int digits = 0;               // sorted by so many digits (0: by sort_kernel)
-  int32_t values[2] = {}, bits[2] = {};
+  int32_t values[3] = {}, bits[3] = {};
   int32_t batches = 1, piece = 0, pieces = 0, part_ld = 0, each = 0, counts = 0;
-  size_t order = 0, part = 0, count = 0, start2 = 0, order2 = 0, total = 0;
+  size_t order = 0, part = 0, count = 0, starts[2] = {}, order2 = 0, total = 0;
 };
 Plan plan_of(const pp_embed_desc& d) {
   Plan p;
@@ -769,36 +770,36 @@ Plan plan_of(const pp_embed_desc& d) {
   // 777 tokens into 5003 x 203 fp32 12 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
   // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
   p.few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
-  // The sort by digits: two launches (five for two digits), but no workgroup that reads
-  // all ids or has all tokens of a row.  us a call, sort_kernel / digits: 313 rows of 256
-  // bf16 features, three in ten ids the same, 8192 tokens 17 / 18, 32768 28 / 22, 2^20
-  // 675 / 132; 50000 rows of 64 features, 32768 tokens: ids log-uniform 32 / 38, uniform
-  // 20 / 34, three in ten the same 40 / 37; 65536: 42 / 42, 25 / 36, 60 / 43; 2^20: 575 /
-  // 108, 177 / 100, 861 / 118.
-  if (!p.few && d.t > 16384 && d.v <= kSortRows)
-    p.digits = 1;
-  else if (!p.few && d.t >= 65536 && d.v <= kSortRows * kSortRows)
-    p.digits = 2;
   // Workgroups of sort_kernel and few_kernel: as many as CUs, or more where one's rows
   // would be too many; of narrow rows some at a time, 256 bytes, so that whole lines of
   // memory are written by one.
   const int64_t bytes = d.d * static_cast<int64_t>(size_of(d.w_dtype));
   p.deal.run = 0, p.deal.log = 0;
-  if (!p.digits) {
-    while (bytes << p.deal.run < 256) ++p.deal.run;
-    const int64_t runs = cdiv(d.v, int64_t(1) << p.deal.run);
-    while (int64_t(1) << p.deal.log < std::min<int64_t>(runs, kCUs) || cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run > kSortRows)
-      ++p.deal.log;
-    p.deal.per = static_cast<int32_t>(cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run);
-  } else {
-    p.deal.per = static_cast<int32_t>(d.v);
+  while (bytes << p.deal.run < 256) ++p.deal.run;
+  const int64_t runs = cdiv(d.v, int64_t(1) << p.deal.run);
+  while (int64_t(1) << p.deal.log < std::min<int64_t>(runs, kCUs) || cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run > kSortRows)
+    ++p.deal.log;
+  p.deal.per = static_cast<int32_t>(cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run);
+  // The sort by digits: two launches (five for two digits), but no workgroup that reads
+  // all ids or has all tokens of a row.  us a call, sort_kernel / digits: 313 rows of 256
+  // bf16 features, three in ten ids the same, 8192 tokens 17 / 18, 32768 28 / 22, 2^20
+  // 675 / 132; 50000 rows of 64 features, 32768 tokens: ids log-uniform 32 / 38, uniform
+  // 20 / 34, three in ten the same 40 / 37; 65536: 42 / 42, 25 / 36, 60 / 43; 2^20: 575 /
+  // 108, 177 / 100, 861 / 118.  sort_kernel's workgroups come in rounds of kCUs, each of
+  // about 4.5 us and 0.2 for 1000 tokens.
+  const int64_t rounds = cdiv(int64_t(1) << p.deal.log, kCUs);
+  int all = 0;
+  while (int64_t(1) << all < d.v) ++all;
+  if (!p.few && (d.v <= kSortRows ? d.t > 16384 : rounds * (d.t + 22500) >= 88000)) {
+    p.digits = d.v <= kSortRows ? 1 : (all + kOwnBits - 1) / kOwnBits;
+    p.deal.run = 0, p.deal.log = 0, p.deal.per = static_cast<int32_t>(d.v);
     p.each = static_cast<int32_t>(cdiv(d.t, kCounts * 1024) * 1024);
     p.counts = static_cast<int32_t>(cdiv(d.t, p.each));
-    int all = 0;
-    while (int64_t(1) << all < d.v) ++all;
-    p.bits[0] = p.digits == 1 ? all : all / 2, p.bits[1] = all - p.bits[0];
-    p.values[0] = p.digits == 1 ? static_cast<int32_t>(d.v) : 1 << p.bits[0];
-    p.values[1] = static_cast<int32_t>(cdiv(d.v, int64_t(1) << p.bits[0]));
+    for (int k = 0, done = 0; k < p.digits; ++k) {
+      p.bits[k] = (all - done) / (p.digits - k);
+      p.values[k] = k + 1 < p.digits ? 1 << p.bits[k] : static_cast<int32_t>(cdiv(d.v, int64_t(1) << done));
+      done += p.bits[k];
+    }
   }
   const int64_t groups = 256 >> p.lanes.log;
   p.batches = static_cast<int32_t>(std::max<int64_t>(1, cdiv(d.t, groups * kBatch * kPieces)));
@@ -810,12 +811,12 @@ Plan plan_of(const pp_embed_desc& d) {
     p.total += static_cast<size_t>(cdiv(n, 256) * 256);
     return at;
   };
-  take(4 * (p.digits == 2 ? 2 * d.v : p.deal.entries()));
+  take(4 * (p.digits > 1 ? 2 * d.v : p.deal.entries()));
   p.order = take(static_cast<int64_t>(sizeof(Place)) * d.t);
   p.part = take(p.pieces > 1 ? static_cast<int64_t>(p.pieces) * 2 * p.part_ld * 4 : 0);
-  p.count = take(4 * static_cast<int64_t>(p.counts) * std::max(p.values[0], p.digits == 2 ? p.values[1] : 0));
-  if (p.digits == 2) {
-    p.start2 = take(4 * (p.values[0] + 1 + p.values[1] + 1));
+  if (p.digits) p.count = take(4 * static_cast<int64_t>(p.counts) * kSortRows);
+  if (p.digits > 1) {
+    for (size_t& at : p.starts) at = take(4 * (kSortRows + 1));
     p.order2 = take(static_cast<int64_t>(sizeof(Place)) * d.t);
   }
   return p;
@@ -861,10 +862,10 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
   const bool row = d.ignore_index >= 0 && d.ignore_index < d.v;
   const Sort s = {ids, start, order, static_cast<uint32_t>(d.v), static_cast<uint32_t>(row ? d.ignore_index : d.v),
                   static_cast<int32_t>(d.t), p.deal};
-  int32_t* start2 = reinterpret_cast<int32_t*>(base + p.start2);
-  const bool two = p.digits == 2;
-  const Sum a = {start, start + (two ? d.v : 1), two ? start2 + p.values[0] + 1 + p.values[1] : start + p.deal.entries() - 1, order, dy, add, dw,
-                 reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.t), static_cast<int32_t>(d.v),
+  const bool several = p.digits > 1;
+  auto start_of = [&](int k) { return several ? reinterpret_cast<int32_t*>(base + p.starts[k & 1]) : start; };   // of digit k
+  const Sum a = {start, start + (several ? d.v : 1), p.digits ? start_of(p.digits - 1) + p.values[p.digits - 1] : start + p.deal.entries() - 1, order,
+                 dy, add, dw, reinterpret_cast<float*>(base + p.part), d.y_ld, d.w_ld, static_cast<int32_t>(d.t), static_cast<int32_t>(d.v),
                  static_cast<int32_t>(d.d), p.lanes.log, p.deal, p.pieces, p.batches, p.piece, p.part_ld, d.scale};
   // (a gradient that is added to in place: rows without a token stay as they are)
   const int64_t fills = add == dw ? 0 : cdiv(d.v, (256 >> p.lanes.log) * kFillRows);
@@ -878,19 +879,27 @@ pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, co
       return;
     }
     if (p.digits) {
-      Place* order2 = reinterpret_cast<Place*>(base + p.order2);
-      Digit f = {ids, nullptr, nullptr, two ? start : nullptr, two ? 2 * d.v : 0, reinterpret_cast<uint32_t*>(base + p.count),
-                 two ? start2 : start, two ? order2 : order, s.v, s.ignore, s.t, p.each, 0, p.values[0], p.bits[0]};
-      const dim3 grid(p.counts), block(kSortWaves * 64);
-      hipLaunchKernelGGL((count_kernel<true>), grid, block, 0, st, f);
-      hipLaunchKernelGGL((place_kernel<true>), grid, block, 0, st, f);
-      if (two) {
-        f.in = order2, f.in_total = start2 + p.values[0], f.start = start2 + p.values[0] + 1, f.order = order;
-        f.shift = p.bits[0], f.values = p.values[1], f.bits = p.bits[1];
-        hipLaunchKernelGGL((count_kernel<false>), grid, block, 0, st, f);
-        hipLaunchKernelGGL((place_kernel<false>), grid, block, 0, st, f);
-        hipLaunchKernelGGL(bounds_kernel, dim3(static_cast<uint32_t>(cdiv(d.t, 256))), dim3(256), 0, st, order, a.total, start, start + d.v);
+      const dim3 block(kSortWaves * 64);
+      Digit f = {};
+      f.ids = ids, f.count = reinterpret_cast<uint32_t*>(base + p.count), f.v = s.v, f.ignore = s.ignore, f.t = s.t;
+      f.each = p.each, f.groups = p.counts;
+      if (several && fills) f.clear = start, f.cleared = 2 * d.v;   // (rows without a token are looked for by it)
+      for (int k = 0; k < p.digits; ++k) {
+        f.start = start_of(k), f.values = p.values[k], f.bits = p.bits[k];
+        // (the last digit's list is `order`)
+        f.order = (p.digits - k) % 2 ? order : reinterpret_cast<Place*>(base + p.order2);
+        if (k == 0) {
+          const int64_t clears = std::min<int64_t>(1024, cdiv(f.cleared, 16384));
+          hipLaunchKernelGGL((count_kernel<true>), dim3(static_cast<uint32_t>(std::max<int64_t>(p.counts, clears))), block, 0, st, f);
+          hipLaunchKernelGGL((place_kernel<true>), dim3(p.counts), block, 0, st, f);
+        } else {
+          hipLaunchKernelGGL((count_kernel<false>), dim3(p.counts), block, 0, st, f);
+          hipLaunchKernelGGL((place_kernel<false>), dim3(p.counts), block, 0, st, f);
+        }
+        f.in = f.order, f.in_total = f.start + f.values, f.shift += f.bits;
       }
+      if (several)
+        hipLaunchKernelGGL(bounds_kernel, dim3(static_cast<uint32_t>(cdiv(d.t, 256))), dim3(256), 0, st, order, a.total, start, start + d.v);
     } else {
       hipLaunchKernelGGL(sort_kernel, dim3(1u << p.deal.log), dim3(kSortWaves * 64), 0, st, s);
     }

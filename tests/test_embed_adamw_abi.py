@@ -37,7 +37,7 @@ def test_embed_descriptions(lib):
     # the workspace goes with the tokens and the rows, not with their product with d
     for t, v, d in ((1 << 20, 1 << 20, 4096), (1 << 29, 7, 64), (33, 5, 1 << 20)):
         assert lib.pp_embed_workspace(ctypes.byref(desc(t=t, v=v, d=d, w_ld=d, y_ld=d)), ctypes.byref(nb)) == pp.PP_OK
-        assert nb.value <= 5 * v + 8 * t + 4096 * 4 * (d + 8) + 4 * 256 * 128 + 4 * 128 * 1024 + 1024
+        assert nb.value <= 8 * v + 16 * t + 2048 * 4 * (d + 8) + 4 * 256 * 128 + 4 * 128 * 1024 + 4 * 4096
 
 
 def test_embed_calls(lib):

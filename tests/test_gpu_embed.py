@@ -143,14 +143,17 @@ def test_token_counts(t, v, how):
     assert same(got, pp.embed_bwd(ids, dy, v, add=add, out=add))
 
 
-@pytest.mark.parametrize("v", [1023, 1024, 1025, 2047, 65536, 1 << 20, (1 << 20) + 1])
-@pytest.mark.parametrize("t", [16384, 16385, 65535, 65536, 200003])
+@pytest.mark.parametrize("v", [1023, 1024, 1025, 2047, 65536, 600000, 1 << 20, (1 << 20) + 1, 3000001])
+@pytest.mark.parametrize("t", [2000, 16384, 16385, 65535, 65536, 200003])
 def test_sorts(v, t):
-    # one digit and two, the largest of each, and what lies beside them
+    # one digit, two and three, the largest of each, and what lies beside them
     ids, dy = make_ids(t, t, v, "heavy" if v % 2 else "uniform", ignored=0.1), normal(t, t, 5)
     got = pp.embed_bwd(ids, dy, v, ignore_index=v // 2)
     check_bwd(got, ids, dy, v, ignore=v // 2)
     assert same(got, pp.embed_bwd(ids, dy, v, ignore_index=v // 2))
+    add = normal(3, v, 5)
+    got = pp.embed_bwd(ids, dy, v, ignore_index=v // 2, add=add)
+    assert same(got, pp.embed_bwd(ids, dy, v, ignore_index=v // 2, add=add, out=add))
 
 
 def test_ids_that_reach_no_row():
