@@ -139,20 +139,19 @@ def _address(a):
     return a.__array_interface__["data"][0]
 
 
-def _gather(name, tensors, dtype, device, table, at, column, state=None, sizes=False):
-    """Addresses of a list's tensors, which have to be contiguous, of a dtype and
-    device (and of the state's shapes), into a column of the table (which lies at
-    ``at``); with sizes, their numbers of elements into the next."""
-    if device.type == "cuda" and _lists().gather(tensors, 0 if state is None else _address(state._dims), dtype, device.index,
-                                                 at + 8 * column, table.shape[1], sizes):
-        return
-    if state is not None and [t.shape for t in tensors] != state.shapes:
+def _fit(name, tensors, dtype, device, shapes=None):
+    """Refuses a list whose tensors are not contiguous, of a dtype and device, and of
+    the shapes."""
+    if shapes is not None and [t.shape for t in tensors] != shapes:
         raise ValueError(f"{name} must be of the state's shapes")
-    if any(t.device != device or t.dtype != dtype or not t.is_contiguous() for t in tensors) or device.type == "cuda":
+    if any(t.device != device or t.dtype != dtype or not t.is_contiguous() for t in tensors):
         raise ValueError(f"{name} must be contiguous {dtype} on one device, {device}")
-    table[:, column] = [t.data_ptr() for t in tensors]
-    if sizes:
-        table[:, column + 1] = [t.numel() for t in tensors]
+
+
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    """Address of an entry point of the library."""
+    return ctypes.cast(getattr(load_library(), name), ctypes.c_void_p).value
 
 
 def _scalar(name, t, dtype, device):
@@ -162,6 +161,7 @@ def _scalar(name, t, dtype, device):
 
 
 # outputs are each their own, but a weight may be written in place (by where tensors begin)
+_NAMES = ("weights", "grads", "out weights", "copies")
 _OWN = (None, "two outputs are the same tensor", "an output is another tensor of the call", "an output is another tensor's input")
 
 
@@ -193,17 +193,11 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
         if dt not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
     table = state._table.copy()
-    at = _address(table)
-    _gather("weights", weights, wt, dev, table, at, _W, state)
-    _gather("grads", grads, gt, dev, table, at, _G, state)
-    if out is None:
-        new, state_out, bufs_out = weights, state, bufs
-        table[:, _W_OUT] = table[:, _W]
-    else:
+    new, state_out, bufs_out = weights, state, bufs
+    if out is not None:
         new, state_out = _list(out[0]), out[1]
         if len(new) != count or state_out.bits != state.bits or state_out.shapes != shapes:
             raise ValueError("out must be weights and a state of the same shapes and bits")
-        _gather("out weights", new, wt, dev, table, at, _W_OUT, state)
         bufs_out = state_out.buffers()
         if bufs_out[0].device != dev:
             raise ValueError("out must be on the state's device")
@@ -211,10 +205,6 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
         copies = _list(copies)
         if len(copies) != count:
             raise ValueError(f"copies must be of the state's length {count}")
-        _gather("copies", copies, torch.bfloat16, dev, table, at, _COPY, state)
-    wrong = _lists().own(at, count, copies is not None)
-    if wrong:
-        raise ValueError(_OWN[wrong])
     if keep is not None:
         keep = list(keep)
         if len(keep) != count:
@@ -232,11 +222,27 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
     d_scale = 0 if grad_scale is None else _scalar("grad_scale", grad_scale, torch.float32, dev)
     desc = _DESC.pack(int(wt == torch.bfloat16), int(gt == torch.bfloat16), state.bits, 0.0 if d_lr else lr, betas[0], betas[1], eps,
                       0 if d_step else int(step), d_lr, d_step, d_scale, *[t.data_ptr() if t is not None else 0 for t in bufs + bufs_out])
-    if dev.type != "cuda":
-        raise ValueError("the tensors must be on a GPU")
-    with _stream_of(stream, dev) as sp:
-        _check(load_library().pp_adamw_step(at, count, desc, sp), "pp_adamw_step")
-    _lists().changed([*new, *bufs_out, *(copies or ())])
+    lists = (weights, grads, None if out is None else new, copies)
+    if dev.type == "cuda":
+        native = _lists()
+        with _stream_of(stream, dev) as sp:
+            got = native.adamw(lists, (wt, gt), dev.index, _address(state._dims), _address(table), _entry("pp_adamw_step"), desc, sp, bufs_out)
+    else:
+        got = 10
+    if got:
+        for name, t, dt in zip(_NAMES, lists, (wt, gt, wt, torch.bfloat16)):
+            if got >= 10 and t is not None:
+                _fit(name, t, dt, dev, shapes)
+        if got >= 10 and dev.type != "cuda":
+            for column, t in zip((_W, _G, _W_OUT, _COPY), (weights, grads, new, copies)):
+                if t is not None:
+                    table[:, column] = [x.data_ptr() for x in t]
+            got = _lists().own(_address(table), count, copies is not None) or 10
+        if 0 < got < 10:
+            raise ValueError(_OWN[got])
+        if got >= 10:
+            raise ValueError("the tensors must be on a GPU")
+        _check(got, "pp_adamw_step")
     return (new[0], state_out) if single else (new, state_out)
 
 
@@ -255,16 +261,13 @@ def grad_norm(grads, max_norm=None, stream=None):
     most = math.inf if max_norm is None else float(max_norm)
     if not most > 0:
         raise ValueError(f"max_norm must be above 0, got {max_norm}")
-    table = np.empty((len(grads), 2), np.int64)      # (pp_grad: address, elements)
-    at = _address(table)
-    _gather("grads", grads, dt, dev, table, at, 0, sizes=True)
-    if dev.type != "cuda":
-        raise ValueError("the tensors must be on a GPU")
-    code, lib, nb = int(dt == torch.bfloat16), load_library(), ctypes.c_size_t(0)
-    _check(lib.pp_grad_norm_workspace(at, len(grads), code, ctypes.byref(nb)), "pp_grad_norm_workspace")
-    with _stream_of(stream, dev) as sp:
-        both = _empty(2, torch.float32, dev, stream)
-        ws = _empty(max(nb.value, 256), torch.uint8, dev, stream)
-        _check(lib.pp_grad_norm(at, len(grads), code, most, both.data_ptr(), ws.data_ptr(), ws.numel(), sp),
-               "pp_grad_norm")
-    return both.unbind()
+    if dev.type == "cuda":
+        native = _lists()
+        with _stream_of(stream, dev) as sp, _on(stream, dev):
+            got = native.grad_norm(grads, dt, dev.index, most, _entry("pp_grad_norm_workspace"), _entry("pp_grad_norm"), sp)
+        if type(got) is tuple:
+            return got
+        if got < 0:
+            _check(got, "pp_grad_norm")
+    _fit("grads", grads, dt, dev)
+    raise ValueError("the tensors must be on a GPU")

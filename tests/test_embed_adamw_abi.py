@@ -283,22 +283,18 @@ def test_outputs_of_their_own():
     assert code([(4, 10, 20, 10, 10)], False) == 0
 
 
-def test_gather_takes_tensors_on_a_gpu_only():
-    lists, t = adamw._lists(), np.zeros((2, 2), np.int64)
-    assert lists.gather([torch.zeros(3)], 0, torch.float32, 0, t.ctypes.data, 2, True) is False
-    assert lists.gather([None], 0, torch.float32, 0, t.ctypes.data, 2, True) is False
-    assert lists.gather(["x"], 0, torch.float32, 0, t.ctypes.data, 2, True) is False
-    assert lists.gather([], 0, torch.float32, 0, t.ctypes.data, 2, True) is True and not t.any()
-    for bad in ((), ([], 0, torch.float32, 0, 0, 2), ((), 0, torch.float32, 0, 0, 2, 0), ([], 0, "f", 0, 0, 2, 0), ([], 0, torch.float32, "0", 0, 2, 0)):
+def test_native_calls_take_tensors_on_a_gpu_only():
+    lists, f32 = adamw._lists(), torch.float32
+    t, dims = np.zeros((2, 8), np.int64), np.array([1, 3, 1, 3], np.int64)
+    x = [torch.zeros(3), torch.zeros(3)]
+    go = lambda w=x, g=x, new=None, copies=None, dt=(f32, f32): lists.adamw((w, g, new, copies), dt, 0, dims.ctypes.data, t.ctypes.data, 1, b"", 0, ())   # noqa: E731
+    assert go() == 10 and go(w=[None, None]) == 10 and go(w=["a", 3]) == 10
+    for bad in (dict(w=None), dict(g=x[:1]), dict(new=x[:1]), dict(copies=(1, 2)), dict(dt=("f", f32)), dict(dt=f32)):
         with pytest.raises(TypeError):
-            lists.gather(*bad)
+            go(**bad)
+    assert lists.grad_norm(x, f32, 0, 1.0, 1, 1, 0) == 10 and lists.grad_norm([3], f32, 0, 1.0, 1, 1, 0) == 10
+    for bad in ((), (x, f32, 0, 1.0, 1, 1), (tuple(x), f32, 0, 1.0, 1, 1, 0), (x, "f", 0, 1.0, 1, 1, 0), (x, f32, "0", 1.0, 1, 1, 0)):
+        with pytest.raises(TypeError):
+            lists.grad_norm(*bad)
     with pytest.raises(TypeError):
         lists.own(0, "x", 0)
-    with pytest.raises(TypeError):
-        lists.changed((torch.zeros(1),))
-    with pytest.raises(TypeError):
-        lists.changed([torch.zeros(1), 3])
-    x = torch.zeros(3)
-    before = x._version
-    lists.changed([x, None, x])
-    assert x._version == before + 2
