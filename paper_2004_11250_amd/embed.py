@@ -11,22 +11,18 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import struct
 
 from . import _check, _dtype_code, _torch, load_library
 from .train import _changed, _empty, _p, _stream_of
 
-
-class EmbedDesc(ctypes.Structure):
-    _fields_ = [("w_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("t", ctypes.c_int64), ("v", ctypes.c_int64),
-                ("d", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("y_ld", ctypes.c_int64), ("ignore_index", ctypes.c_int64),
-                ("scale", ctypes.c_float)]
+_DESC = struct.Struct("@2i6qf4x")     # pp_embed_desc as the library lays it out
 
 
 def bind(lib):
     vp, sz = ctypes.c_void_p, ctypes.c_size_t
-    desc = ctypes.POINTER(EmbedDesc)
-    for name, at in {"pp_embed_fwd": [desc, vp, vp, vp, vp], "pp_embed_workspace": [desc, ctypes.POINTER(sz)],
-                     "pp_embed_bwd": [desc, vp, vp, vp, vp, vp, sz, vp]}.items():
+    for name, at in {"pp_embed_fwd": [vp, vp, vp, vp, vp], "pp_embed_workspace": [vp, ctypes.POINTER(sz)],
+                     "pp_embed_bwd": [vp, vp, vp, vp, vp, vp, sz, vp]}.items():
         if hasattr(lib, name):
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = at, ctypes.c_int32
@@ -100,12 +96,12 @@ def embed_fwd(ids, w, scale=1.0, ignore_index=-100, dtype=None, out=None, stream
         y_ld = _rows(out, "out", shape, ids.device)
         if out.numel() and out.data_ptr() in (w.data_ptr(), ids.data_ptr()):
             raise ValueError("out is another tensor of the call")
-    desc = EmbedDesc(code, yc, ids.numel(), v, d, w_ld, y_ld, int(ignore_index), float(scale))
+    desc = _DESC.pack(code, yc, ids.numel(), v, d, w_ld, y_ld, ignore_index, scale)
     given = out is not None
     with _stream_of(stream, ids.device) as sp:
         if not given:
             out = _empty(shape, torch.bfloat16 if yc else torch.float32, ids.device, stream)
-        _check(load_library().pp_embed_fwd(ctypes.byref(desc), ids.data_ptr(), w.data_ptr(), out.data_ptr(), sp),
+        _check(load_library().pp_embed_fwd(desc, ids.data_ptr(), w.data_ptr(), out.data_ptr(), sp),
                "pp_embed_fwd")
     if given:
         _changed([out])
@@ -114,10 +110,9 @@ def embed_fwd(ids, w, scale=1.0, ignore_index=-100, dtype=None, out=None, stream
 
 @functools.lru_cache(maxsize=256)
 def _bytes(desc):
-    """pp_embed_workspace of a description (as bytes): a function of it alone."""
+    """pp_embed_workspace of a description: a function of it alone."""
     nb = ctypes.c_size_t(0)
-    _check(load_library().pp_embed_workspace(ctypes.byref(EmbedDesc.from_buffer_copy(desc)), ctypes.byref(nb)),
-           "pp_embed_workspace")
+    _check(load_library().pp_embed_workspace(desc, ctypes.byref(nb)), "pp_embed_workspace")
     return nb.value
 
 
@@ -151,14 +146,14 @@ def embed_bwd(ids, dy, v, scale=1.0, ignore_index=-100, dtype=None, add=None, ou
         raise ValueError("add must be contiguous where out is not given")
     if out is not None and out.data_ptr() in (ids.data_ptr(), dy.data_ptr()):
         raise ValueError("out is another tensor of the call")
-    desc = EmbedDesc(wc, yc, ids.numel(), int(v), d, w_ld or d, y_ld, int(ignore_index), float(scale))
+    desc = _DESC.pack(wc, yc, ids.numel(), int(v), d, w_ld or d, y_ld, ignore_index, scale)
     given = out is not None
     with _stream_of(stream, ids.device) as sp:
         if not given:
             out = _empty(shape, torch.bfloat16 if wc else torch.float32, ids.device, stream)
-        nb = _bytes(bytes(desc))
+        nb = _bytes(desc)
         ws = _empty(nb, torch.uint8, ids.device, stream)
-        _check(load_library().pp_embed_bwd(ctypes.byref(desc), ids.data_ptr(), dy.data_ptr(), _p(add), out.data_ptr(),
+        _check(load_library().pp_embed_bwd(desc, ids.data_ptr(), dy.data_ptr(), _p(add), out.data_ptr(),
                                            ws.data_ptr(), nb, sp), "pp_embed_bwd")
     if given:
         _changed([out])

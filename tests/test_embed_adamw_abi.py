@@ -17,10 +17,16 @@ def lib():
     return pp.load_library()
 
 
+class EmbedDesc(ctypes.Structure):
+    _fields_ = [("w_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("t", ctypes.c_int64), ("v", ctypes.c_int64),
+                ("d", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("y_ld", ctypes.c_int64), ("ignore_index", ctypes.c_int64),
+                ("scale", ctypes.c_float)]
+
+
 def desc(**kw):
     d = dict(w_dtype=0, y_dtype=0, t=100, v=7, d=8, w_ld=8, y_ld=8, ignore_index=-100, scale=1.0)
     d.update(kw)
-    return embed.EmbedDesc(**d)
+    return EmbedDesc(**d)
 
 
 def test_embed_descriptions(lib):
@@ -80,7 +86,8 @@ class AdamWDesc(ctypes.Structure):
 
 
 def test_layouts():
-    assert ctypes.sizeof(AdamWDesc) == adamw._DESC.size and TENSOR.itemsize == 8 * len(adamw._TENSOR)
+    assert ctypes.sizeof(EmbedDesc) == embed._DESC.size and ctypes.sizeof(AdamWDesc) == adamw._DESC.size
+    assert TENSOR.itemsize == 8 * len(adamw._TENSOR)
     assert TENSOR.names == adamw._TENSOR
 
 
