@@ -709,9 +709,9 @@ pp_status pp_embed_bwd(const pp_embed_desc* desc, const int64_t* ids, const void
  *
  * The moments of all tensors of a list lie in one array each: tensor i's from
  * element `at` on, a multiple of PP_ADAMW_BLOCK; what follows them up to the next
- * multiple is written as 0, and no other tensor's may lie there.  With 32 bits they are fp32.  With 8 bits each
- * block of PP_ADAMW_BLOCK elements has a scale for each moment, and a code an
- * element:
+ * multiple is written as 0, and no other tensor's may lie there.  With 32 bits
+ * they are fp32.  With 8 bits each block of PP_ADAMW_BLOCK elements has a scale
+ * for each moment, and a code an element:
  *   m   e4m3 (OCP, 448 at most), times the block's scale: its largest |m'| / 448
  *   v   c > 0: r = 2^(q / 16 - 127) (1 + (q mod 16) / 16), q = c + 1777 (whole
  *       division: 4 bits of the exponent and 4 after the leading one, c = 255

@@ -11,22 +11,22 @@ recorded graph can be replayed with others.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
-import functools
 import math
 import struct
 
 import numpy as np
 
 from . import _check, _torch, load_library
-from .train import _empty, _on, _stream_of
+from .train import _empty, _entry, _native, _on, _stream_of
 
 BLOCK = 128     # PP_ADAMW_BLOCK
 
 # pp_adamw_tensor (as eight words), pp_adamw_desc and pp_grad as the library lays them out
 _TENSOR = ("n", "w", "g", "w_out", "copy", "keep", "at", "weight_decay")
-_N, _W, _G, _W_OUT, _COPY, _KEEP, _AT, _DECAY = range(8)
-_DESC = struct.Struct("@3i4dq11Q")
+_N, _KEEP, _AT, _DECAY = (_TENSOR.index(name) for name in ("n", "keep", "at", "weight_decay"))
+_DESC = struct.Struct("@3i4dq3Q64x")     # (the moments' addresses: the native module's)
 
 
 def bind(lib):
@@ -72,6 +72,7 @@ class AdamWState:
         self._table = np.zeros((len(self.sizes), len(_TENSOR)), np.int64)
         self._table[:, _N], self._table[:, _AT] = self.sizes, self.places
         self._dims = np.array([n for s in self.shapes for n in (len(s), *s)] or [0], np.int64)
+        self._at = _address(self._dims), _address(self._table)
 
         def zeros(n, dtype):
             return torch.zeros(n, dtype=torch.uint8, device=device).view(dtype)
@@ -83,10 +84,13 @@ class AdamWState:
             self.m, self.v = zeros(at, torch.float8_e4m3fn), zeros(at, torch.uint8)
             self.m_scale, self.v_scale = (zeros(4 * (at // BLOCK), torch.float32) for _ in range(2))
 
+    def _buffers(self):
+        return self.m, self.v, self.m_scale, self.v_scale
+
     def buffers(self):
         """(m, v, m_scale, v_scale), checked: whoever holds a state may have put others in their places."""
         torch, n, blocks = _torch(), self.elements, self.elements // BLOCK
-        got = (self.m, self.v, self.m_scale, self.v_scale)
+        got = self._buffers()
         if self.bits == 32:
             want = ((torch.float32, n), (torch.float32, n))
         else:
@@ -126,15 +130,6 @@ def _list(t):
     return [t] if _torch().is_tensor(t) else list(t)
 
 
-@functools.lru_cache(maxsize=None)
-def _lists():
-    try:
-        from . import _tensors
-    except ImportError as e:
-        raise RuntimeError("the binding's module for lists of tensors is not built (python -m paper_2004_11250_amd.build)") from e
-    return _tensors
-
-
 def _address(a):
     return a.__array_interface__["data"][0]
 
@@ -146,12 +141,6 @@ def _fit(name, tensors, dtype, device, shapes=None):
         raise ValueError(f"{name} must be of the state's shapes")
     if any(t.device != device or t.dtype != dtype or not t.is_contiguous() for t in tensors):
         raise ValueError(f"{name} must be contiguous {dtype} on one device, {device}")
-
-
-@functools.lru_cache(maxsize=None)
-def _entry(name):
-    """Address of an entry point of the library."""
-    return ctypes.cast(getattr(load_library(), name), ctypes.c_void_p).value
 
 
 def _scalar(name, t, dtype, device):
@@ -187,24 +176,25 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
     shapes, count = state.shapes, len(state.shapes)
     if len(weights) != count or len(grads) != count:
         raise ValueError(f"weights and grads must be of the state's length {count}")
-    bufs = state.buffers()
-    dev, wt, gt = bufs[0].device, weights[0].dtype, grads[0].dtype
+    dev, wt, gt = state.m.device, weights[0].dtype, grads[0].dtype
     for name, dt in (("weights", wt), ("grads", gt)):
         if dt not in (torch.float32, torch.bfloat16):
             raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
-    table = state._table.copy()
-    new, state_out, bufs_out = weights, state, bufs
+    new, state_out = weights, state
     if out is not None:
         new, state_out = _list(out[0]), out[1]
         if len(new) != count or state_out.bits != state.bits or state_out.shapes != shapes:
             raise ValueError("out must be weights and a state of the same shapes and bits")
-        bufs_out = state_out.buffers()
-        if bufs_out[0].device != dev:
+        if state_out.m.device != dev:
             raise ValueError("out must be on the state's device")
     if copies is not None:
         copies = _list(copies)
         if len(copies) != count:
             raise ValueError(f"copies must be of the state's length {count}")
+    table, decay = state._table, weight_decay
+    if keep is not None or type(decay) not in (float, int):
+        table, decay = table.copy(), None
+        table.view(np.float64)[:, _DECAY] = weight_decay
     if keep is not None:
         keep = list(keep)
         if len(keep) != count:
@@ -216,32 +206,26 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
                     or not k.is_contiguous() or k.device != dev:
                 raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
             table[i, _KEEP] = k.data_ptr()
-    table.view(np.float64)[:, _DECAY] = weight_decay
     d_lr = _scalar("lr", lr, torch.float32, dev) if torch.is_tensor(lr) else 0
     d_step = _scalar("step", step, torch.int64, dev) if torch.is_tensor(step) else 0
     d_scale = 0 if grad_scale is None else _scalar("grad_scale", grad_scale, torch.float32, dev)
     desc = _DESC.pack(int(wt == torch.bfloat16), int(gt == torch.bfloat16), state.bits, 0.0 if d_lr else lr, betas[0], betas[1], eps,
-                      0 if d_step else int(step), d_lr, d_step, d_scale, *[t.data_ptr() if t is not None else 0 for t in bufs + bufs_out])
+                      0 if d_step else int(step), d_lr, d_step, d_scale)
     lists = (weights, grads, None if out is None else new, copies)
-    if dev.type == "cuda":
-        native = _lists()
-        with _stream_of(stream, dev) as sp:
-            got = native.adamw(lists, (wt, gt), dev.index, _address(state._dims), _address(table), _entry("pp_adamw_step"), desc, sp, bufs_out)
-    else:
-        got = 10
+    dims, at = state._at
+    with _stream_of(stream, dev) if dev.type == "cuda" else contextlib.nullcontext(0) as sp:
+        got = _native().adamw(lists, (wt, gt), dev.index if dev.type == "cuda" else -1, dims, at if table is state._table else _address(table),
+                              decay, state.elements, (*state._buffers(), *state_out._buffers()), desc, _entry("pp_adamw_step"), sp)
     if got:
-        for name, t, dt in zip(_NAMES, lists, (wt, gt, wt, torch.bfloat16)):
-            if got >= 10 and t is not None:
-                _fit(name, t, dt, dev, shapes)
-        if got >= 10 and dev.type != "cuda":
-            for column, t in zip((_W, _G, _W_OUT, _COPY), (weights, grads, new, copies)):
-                if t is not None:
-                    table[:, column] = [x.data_ptr() for x in t]
-            got = _lists().own(_address(table), count, copies is not None) or 10
-        if 0 < got < 10:
-            raise ValueError(_OWN[got])
         if got >= 10:
+            for s in (state, state_out):
+                s.buffers()
+            for name, t, dt in zip(_NAMES, lists, (wt, gt, wt, torch.bfloat16)):
+                if t is not None:
+                    _fit(name, t, dt, dev, shapes)
             raise ValueError("the tensors must be on a GPU")
+        if got > 0:
+            raise ValueError(_OWN[got])
         _check(got, "pp_adamw_step")
     return (new[0], state_out) if single else (new, state_out)
 
@@ -262,7 +246,7 @@ def grad_norm(grads, max_norm=None, stream=None):
     if not most > 0:
         raise ValueError(f"max_norm must be above 0, got {max_norm}")
     if dev.type == "cuda":
-        native = _lists()
+        native = _native()
         with _stream_of(stream, dev) as sp, _on(stream, dev):
             got = native.grad_norm(grads, dt, dev.index, most, _entry("pp_grad_norm_workspace"), _entry("pp_grad_norm"), sp)
         if type(got) is tuple:

@@ -98,15 +98,15 @@ def build(verbose: bool = False) -> str:
 
 
 def build_tensors() -> str:
-    """The binding's Python module for lists of tensors (g++, torch's headers; the
-    library itself knows nothing of torch)."""
+    """The binding's Python module of calls with native checks (g++, torch's headers;
+    the library itself knows nothing of torch)."""
     import sysconfig
 
     import torch
     at = os.path.dirname(torch.__file__)
     tmp = TENSORS_LIB + ".tmp"
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-I{at}/include", f"-I{at}/include/torch/csrc/api/include",
-          f"-I{sysconfig.get_paths()['include']}", os.path.join(PKG, "binding", "tensors.cpp"), "-o", tmp,
+          f"-I{sysconfig.get_paths()['include']}", f"-I{INCLUDE}", os.path.join(PKG, "binding", "tensors.cpp"), "-o", tmp,
           f"-L{at}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"])
     os.replace(tmp, TENSORS_LIB)
     return TENSORS_LIB

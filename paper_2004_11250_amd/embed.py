@@ -14,7 +14,7 @@ import functools
 import struct
 
 from . import _check, _dtype_code, _torch, load_library
-from .train import _changed, _empty, _p, _stream_of
+from .train import _changed, _empty, _entry, _native, _p, _stream_of
 
 _DESC = struct.Struct("@2i6qf4x")     # pp_embed_desc as the library lays it out
 
@@ -71,6 +71,13 @@ def _rows(t, name, shape, device):
     return ld
 
 
+def _done(got, name):
+    """What a native call gave, unless it is a status."""
+    if type(got) is int:
+        _check(got, name)
+    return got
+
+
 def embed_fwd(ids, w, scale=1.0, ignore_index=-100, dtype=None, out=None, stream=None):
     """pp_embed_fwd: ``scale * w[ids]``, features [*ids.shape, d].
 
@@ -79,6 +86,11 @@ def embed_fwd(ids, w, scale=1.0, ignore_index=-100, dtype=None, out=None, stream
     given, whose rows may lie apart.  ``ignore_index`` gives zeros, another id
     outside of 0..v-1 NaN."""
     torch = _torch()
+    if out is None and stream is None and ids.is_cuda:
+        with _stream_of(None, ids.device) as sp:
+            y = _native().embed_fwd(ids, w, dtype, scale, ignore_index, _entry("pp_embed_fwd"), sp)
+        if y is not None:
+            return _done(y, "pp_embed_fwd")
     code = _dtype_code(w)
     if w.dim() != 2 or w.shape[0] < 1 or w.shape[1] < 1:
         raise ValueError(f"w must be [v, d], got {tuple(w.shape)}")
@@ -125,6 +137,11 @@ def embed_bwd(ids, dy, v, scale=1.0, ignore_index=-100, dtype=None, add=None, ou
     head's weights too).  Fills ``out``, if given; it may be ``add``, and then only
     the rows that ids reach are touched."""
     torch = _torch()
+    if out is None and add is None and stream is None and ids.is_cuda:
+        with _stream_of(None, ids.device) as sp:
+            dw = _native().embed_bwd(ids, dy, v, dtype, scale, ignore_index, _entry("pp_embed_workspace"), _entry("pp_embed_bwd"), sp)
+        if dw is not None:
+            return _done(dw, "pp_embed_bwd")
     yc = _dtype_code(dy)
     _ids(ids)
     if dy.dim() < 1 or dy.shape[-1] < 1 or int(v) < 1:

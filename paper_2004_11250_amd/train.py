@@ -118,6 +118,22 @@ class _stream_of:
             self.guard.__exit__(*exc)
 
 
+@functools.lru_cache(maxsize=None)
+def _native():
+    """The binding's module of calls whose checks are native."""
+    try:
+        from . import _tensors
+    except ImportError as e:
+        raise RuntimeError("the binding's native module is not built (python -m paper_2004_11250_amd.build)") from e
+    return _tensors
+
+
+@functools.lru_cache(maxsize=None)
+def _entry(name):
+    """Address of an entry point of the library."""
+    return ctypes.cast(getattr(load_library(), name), ctypes.c_void_p).value
+
+
 def _empty(shape, dtype, device, stream):
     """A tensor that belongs to the call's stream."""
     torch = _torch()

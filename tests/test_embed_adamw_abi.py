@@ -271,37 +271,51 @@ def test_embed_tensors():
 # the binding's native module for lists
 
 def test_outputs_of_their_own():
-    own = adamw._lists().own
+    x = [torch.zeros(4) for _ in range(8)]
+    table = np.zeros((2, 8), np.int64)
+    desc = AdamWDesc(bits=32)
+    moments = [torch.zeros(256) for _ in range(2)]
 
-    def code(rows, copies=False):
-        t = np.zeros((len(rows), 8), np.int64)
-        for r, (n, w, g, o, *c) in zip(t, rows):
-            r[:4] = n, w, g, o
-            r[4] = c[0] if c else 0
-        return own(t.ctypes.data, len(rows), copies)
+    def code(w, g, new=None, copies=None, n=(4, 4)):
+        """Of two tensors: indices into x."""
+        table[:, 0] = n
+        pick = lambda t, dt=torch.float32: None if t is None else [x[i].view(dt) if dt != torch.float32 else x[i] for i in t]   # noqa: E731
+        return adamw._native().adamw((pick(w), pick(g), pick(new), pick(copies, torch.bfloat16)), (torch.float32, torch.float32), -1, 0,
+                                     table.ctypes.data, None, 256, (*moments, None, None) * 2, bytes(desc), 1, 0)
 
-    assert code([(4, 10, 20, 10), (4, 11, 20, 11)]) == 0 and code([]) == 0
-    assert code([(4, 10, 20, 12), (4, 10, 21, 13)]) == 0
-    assert code([(4, 10, 20, 10), (4, 11, 21, 10)]) == 1
-    assert code([(4, 10, 20, 10), (0, 11, 21, 10), (0, 0, 0, 0), (0, 0, 0, 0)]) == 0
-    assert code([(4, 10, 20, 20)]) == 2 and code([(4, 10, 20, 12), (4, 11, 12, 13)]) == 2
-    assert code([(4, 10, 20, 11), (4, 11, 21, 12)]) == 3
-    assert code([(4, 10, 20, 10, 10)], True) == 1 and code([(4, 10, 20, 10, 20)], True) == 2 and code([(4, 10, 20, 12, 10)], True) == 3
-    assert code([(4, 10, 20, 10, 10)], False) == 0
+    assert code((0, 1), (2, 2)) == 30 and code((0, 1), (2, 3), (4, 5)) == 30 and code((0, 1), (2, 3), None, (4, 5)) == 30
+    assert code((0, 0), (2, 3)) == 1 and code((0, 0), (2, 3), n=(4, 0)) == 30
+    assert code((0, 1), (2, 3), (0, 0)) == 1 and code((0, 1), (2, 3), None, (0, 4)) == 1
+    assert code((0, 1), (0, 3)) == 2 and code((0, 1), (2, 3), (4, 2)) == 2 and code((0, 1), (2, 3), None, (4, 3)) == 2
+    assert code((0, 1), (2, 3), (1, 4)) == 3 and code((0, 1), (2, 3), (4, 5), (0, 6)) == 3
 
 
 def test_native_calls_take_tensors_on_a_gpu_only():
-    lists, f32 = adamw._lists(), torch.float32
+    lists, f32 = adamw._native(), torch.float32
     t, dims = np.zeros((2, 8), np.int64), np.array([1, 3, 1, 3], np.int64)
     x = [torch.zeros(3), torch.zeros(3)]
-    go = lambda w=x, g=x, new=None, copies=None, dt=(f32, f32): lists.adamw((w, g, new, copies), dt, 0, dims.ctypes.data, t.ctypes.data, 1, b"", 0, ())   # noqa: E731
-    assert go() == 10 and go(w=[None, None]) == 10 and go(w=["a", 3]) == 10
-    for bad in (dict(w=None), dict(g=x[:1]), dict(new=x[:1]), dict(copies=(1, 2)), dict(dt=("f", f32)), dict(dt=f32)):
+    bufs, desc = [torch.zeros(256), torch.zeros(256), None, None], bytes(AdamWDesc(bits=32))
+    go = lambda w=x, g=x, new=None, copies=None, dt=(f32, f32), at=-1, b=bufs, d=desc, n=256: lists.adamw(   # noqa: E731
+        (w, g, new, copies), dt, at, dims.ctypes.data, t.ctypes.data, 0.5, n, (*b, *b), d, 1, 0)
+    assert go() == 30 and not t.any()
+    assert go(at=0) == 20 and go(n=128) == 20 and go(b=bufs[:3] + bufs[:1]) == 20 and go(d=bytes(AdamWDesc(bits=8))) == 20
+    assert go(b=[torch.zeros(256).bfloat16(), *bufs[1:]]) == 20 and go(b=[torch.zeros(512)[::2], *bufs[1:]]) == 20
+    assert go(w=[None, None]) == 10 and go(w=["a", 3]) == 10 and go(g=[x[0], x[1].double()]) == 11 and go(new=[x[0], torch.zeros(4)]) == 12
+    assert go(copies=x) == 13
+    for bad in (dict(w=None), dict(g=x[:1]), dict(new=x[:1]), dict(copies=(1, 2)), dict(dt=("f", f32)), dict(dt=f32), dict(b=bufs[:3]),
+                dict(d=desc[1:]), dict(d="x"), dict(n=0.5)):
         with pytest.raises(TypeError):
             go(**bad)
     assert lists.grad_norm(x, f32, 0, 1.0, 1, 1, 0) == 10 and lists.grad_norm([3], f32, 0, 1.0, 1, 1, 0) == 10
     for bad in ((), (x, f32, 0, 1.0, 1, 1), (tuple(x), f32, 0, 1.0, 1, 1, 0), (x, "f", 0, 1.0, 1, 1, 0), (x, f32, "0", 1.0, 1, 1, 0)):
         with pytest.raises(TypeError):
             lists.grad_norm(*bad)
-    with pytest.raises(TypeError):
-        lists.own(0, "x", 0)
+    ids, w = torch.zeros(3, dtype=torch.int64), torch.zeros(2, 4)
+    assert lists.embed_fwd(ids, w, None, 1.0, -100, 1, 0) is None and lists.embed_fwd([0], w, None, 1.0, -100, 1, 0) is None
+    assert lists.embed_bwd(ids, torch.zeros(3, 4), 2, None, 1.0, -100, 1, 1, 0) is None
+    for bad in ((), (ids, w, None, 1.0, -100, 1), (ids, w, None, 1.0, -100, "1", 0)):
+        with pytest.raises(TypeError):
+            lists.embed_fwd(*bad)
+    for bad in ((), (ids, w, 2, None, 1.0, -100, 1, 1), (ids, w, 2, None, 1.0, -100, 1, 1, "0")):
+        with pytest.raises(TypeError):
+            lists.embed_bwd(*bad)

@@ -120,6 +120,20 @@ def test_rows_apart(dtype, d, left, pitch):
     assert torch.equal(base[:, left:left + d], dw[:, left:left + d]) and torch.equal(base[:, rest], keep[:, rest])
 
 
+def test_same_results_however_called():
+    ids, table, dy = make_ids(7, 300, 40, ignored=0.1).view(3, 100), normal(8, 40, 24), normal(9, 3, 100, 24)
+    y, dw = pp.embed_fwd(ids, table, scale=0.5), pp.embed_bwd(ids, dy, 40, scale=0.5)
+    assert torch.equal(y, ref_fwd(ids, table, 0.5, torch.float32)) and not y.requires_grad
+    wide, wide_dy = torch.zeros(40, 30, device="cuda"), torch.zeros(3, 100, 30, device="cuda")
+    wide[:, 3:27], wide_dy[..., 3:27] = table, dy
+    half = torch.tensor(0.5, dtype=torch.float64).numpy()[()]
+    for kw in (dict(scale=half), dict(scale=0.5, ignore_index=make_ids(1, 1, 9, "one").new_tensor(IGNORE)), dict(scale=torch.tensor(0.5))):
+        assert torch.equal(pp.embed_fwd(ids, table, **kw), y) and torch.equal(pp.embed_bwd(ids, dy, 40, **kw), dw)
+    assert torch.equal(pp.embed_fwd(ids, wide[:, 3:27], scale=0.5), y)
+    assert torch.equal(pp.embed_bwd(ids, wide_dy[..., 3:27], 40, scale=0.5), dw)
+    assert torch.equal(pp.embed_fwd(ids, table.requires_grad_(), scale=0.5), y)
+
+
 @pytest.mark.parametrize("w,y", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("d", [1, 8, 9, 63, 203, 256, 1030, 2056])
 @pytest.mark.parametrize("how", ["uniform", "heavy"])
