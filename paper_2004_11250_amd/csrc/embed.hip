@@ -249,10 +249,11 @@ __global__ __launch_bounds__(kSortWaves * 64) void sort_kernel(const Sort a) {
 }
 
 // The same by digits of the row's number, up to kOwnBits bits each, the lowest first,
-// without a workgroup that has all tokens of a row.  A workgroup has `each` places of the list so far.  count_kernel counts its
-// tokens of each digit; place_kernel adds up the counts, which gives each workgroup
-// the places of its tokens of each digit, and puts them there, in their order.  32768
-// pixels 2.7 and 5.5 us: latency, of ids, counts, a scan and an exchange in turn.
+// without a workgroup that has all tokens of a row.  A workgroup has `each` places of
+// the list so far.  count_kernel counts its tokens of each digit; place_kernel adds up
+// the counts, which gives each workgroup the places of its tokens of each digit, and
+// puts them there, in their order.  32768 pixels 2.9 and 6.7 us: latency, of ids,
+// counts, a scan and an exchange in turn.
 constexpr int64_t kCounts = 128;                // workgroups at most
 struct Digit {
   const int64_t* ids;           // the first digit's list
@@ -591,8 +592,9 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
 
 // Up to kFewTokens tokens: a workgroup has its rows of the table, finds their tokens,
 // a thread an id, sorts them in LDS, sums them, and fills its rows without a token,
-// all in one launch.  777 tokens into 5003 x 203 fp32 12 us a call, of which the host
-// takes 10; a table of 50000 x 1024 bf16 is filled in 20, 5 TB/s.
+// all in one launch.  777 tokens into 5003 x 203 fp32 9 us: ids, the order, rows of
+// features and edges, one after the other; a table of 50000 x 1024 bf16 is filled in
+// 20, 5 TB/s.
 constexpr int kFewTokens = 1024, kFewRanks = 256;
 template <class Y, class W>
 __global__ __launch_bounds__(kFewTokens) void few_kernel(const Sort s, const Sum a) {
@@ -750,9 +752,16 @@ pp_status check(const pp_embed_desc* desc) {
   return PP_OK;
 }
 
+constexpr int64_t kPieces = 1024;            // of the sorted list, at most
+constexpr int64_t kGrid = int64_t(1) << 24;  // (a launch has fewer than 2^32 threads)
+// Whether a table's rows without a token are fewer workgroups than that.
+pp_status check_rows(const pp_embed_desc& d) {
+  if (cdiv(d.v, (256 >> lanes_for(d.d).log) * kFillRows) + kPieces >= kGrid) return fail(PP_EUNSUPPORTED, "a table of too many rows of this length");
+  return PP_OK;
+}
+
 // Tokens of a group's part: kBatch, or as many times that as keep the pieces
 // to kPieces.
-constexpr int64_t kPieces = 1024;
 struct Plan {
   Lanes lanes;
   Deal deal;
@@ -767,7 +776,7 @@ Plan plan_of(const pp_embed_desc& d) {
   p.lanes = lanes_for(d.d);
   // One launch instead of two or three, at the risk that one row has all tokens, whose
   // features one workgroup then reads (at 100 GB/s).  us a call, one launch / three:
-  // 777 tokens into 5003 x 203 fp32 12 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
+  // 777 tokens into 5003 x 203 fp32 9 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
   // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
   p.few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
   // Workgroups of sort_kernel and few_kernel: as many as CUs, or more where one's rows
@@ -836,6 +845,7 @@ pp_status look(const pp_embed_desc* desc, const int64_t* ids, const void* w, voi
   if (!ids || !w || !y) return fail(PP_EINVAL, "NULL pointer");
   if (off(ids, 8) || off(w, size_of(d.w_dtype)) || off(y, size_of(d.y_dtype))) return fail(PP_EINVAL, "misaligned pointer");
   const Lanes l = lanes_for(d.d);
+  if (cdiv(d.t, 256 >> l.log) >= kGrid) return fail(PP_EUNSUPPORTED, "too many tokens of this length");
   const Look a = {ids, w, y, d.t, d.v, d.w_ld, d.y_ld, d.ignore_index, static_cast<int32_t>(d.d), l.log, d.scale};
   const dim3 grid(static_cast<uint32_t>(cdiv(d.t, 256 >> l.log)), static_cast<uint32_t>(l.columns));
   with_types(d.w_dtype, d.y_dtype, [&](auto wt, auto yt) {
@@ -846,7 +856,8 @@ pp_status look(const pp_embed_desc* desc, const int64_t* ids, const void* w, voi
 
 pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, const void* add, void* dw, void* ws, size_t bytes,
                hipStream_t st) {
-  const pp_status r = check(desc);
+  pp_status r = check(desc);
+  if (r == PP_OK) r = check_rows(*desc);
   if (r != PP_OK) return r;
   const pp_embed_desc& d = *desc;
   if (!dw || (d.t && (!ids || !dy))) return fail(PP_EINVAL, "NULL pointer");
@@ -924,7 +935,8 @@ extern "C" pp_status pp_embed_fwd(const pp_embed_desc* desc, const int64_t* ids,
 
 extern "C" pp_status pp_embed_workspace(const pp_embed_desc* desc, size_t* bytes) {
   return guarded([&]() -> pp_status {
-    const pp_status s = check(desc);
+    pp_status s = check(desc);
+    if (s == PP_OK) s = check_rows(*desc);
     if (s != PP_OK) return s;
     if (!bytes) return fail(PP_EINVAL, "bytes is NULL");
     *bytes = plan_of(*desc).total;

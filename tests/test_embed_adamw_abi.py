@@ -38,6 +38,13 @@ def test_embed_descriptions(lib):
     for bad in (dict(t=1 << 30), dict(v=1 << 30), dict(d=1 << 23, w_ld=1 << 23, y_ld=1 << 23), dict(w_ld=1 << 32), dict(y_ld=1 << 32)):
         assert lib.pp_embed_workspace(ctypes.byref(desc(**bad)), ctypes.byref(nb)) == pp.PP_EUNSUPPORTED, bad
         assert lib.pp_embed_bwd(ctypes.byref(desc(**bad)), A, A, None, A, A, 1 << 50, None) == pp.PP_EUNSUPPORTED, bad
+    # launches of 2^32 threads or more: 256 a row of 1025 features and above
+    long = dict(d=2000, w_ld=2000, y_ld=2000)
+    assert lib.pp_embed_fwd(ctypes.byref(desc(t=1 << 24, **long)), A, A, A, None) == pp.PP_EUNSUPPORTED
+    assert lib.pp_embed_workspace(ctypes.byref(desc(t=1 << 24, **long)), ctypes.byref(nb)) == pp.PP_OK
+    assert lib.pp_embed_workspace(ctypes.byref(desc(v=(1 << 26) - 4200, **long)), ctypes.byref(nb)) == pp.PP_OK
+    assert lib.pp_embed_workspace(ctypes.byref(desc(v=1 << 26, **long)), ctypes.byref(nb)) == pp.PP_EUNSUPPORTED
+    assert lib.pp_embed_bwd(ctypes.byref(desc(v=1 << 26, **long)), A, A, None, A, A, 1 << 50, None) == pp.PP_EUNSUPPORTED
     assert lib.pp_embed_workspace(None, ctypes.byref(nb)) == pp.PP_EINVAL
     assert lib.pp_embed_workspace(ctypes.byref(desc()), None) == pp.PP_EINVAL
     # the workspace goes with the tokens and the rows, not with their product with d
