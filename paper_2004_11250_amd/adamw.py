@@ -25,7 +25,7 @@ BLOCK = 128     # PP_ADAMW_BLOCK
 
 # pp_adamw_tensor (as eight words), pp_adamw_desc and pp_grad as the library lays them out
 _TENSOR = ("n", "w", "g", "w_out", "copy", "keep", "at", "weight_decay")
-_N, _KEEP, _AT, _DECAY = (_TENSOR.index(name) for name in ("n", "keep", "at", "weight_decay"))
+_N, _AT, _DECAY = (_TENSOR.index(name) for name in ("n", "at", "weight_decay"))
 _DESC = struct.Struct("@3i4dq3Q64x")     # (the moments' addresses: the native module's)
 
 
@@ -191,27 +191,20 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
         copies = _list(copies)
         if len(copies) != count:
             raise ValueError(f"copies must be of the state's length {count}")
-    table, decay = state._table, weight_decay
-    if keep is not None or type(decay) not in (float, int):
-        table, decay = table.copy(), None
-        table.view(np.float64)[:, _DECAY] = weight_decay
     if keep is not None:
         keep = list(keep)
         if len(keep) != count:
             raise ValueError(f"keep must be of the state's length {count}")
-        for i, (k, s) in enumerate(zip(keep, shapes)):
-            if k is None:
-                continue
-            if len(s) < 2 or k.dtype != torch.int16 or tuple(k.shape) != tuple(s[:2]) or state.sizes[i] != 9 * k.numel() \
-                    or not k.is_contiguous() or k.device != dev:
-                raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
-            table[i, _KEEP] = k.data_ptr()
+    table, decay = state._table, weight_decay
+    if type(decay) not in (float, int):
+        table, decay = table.copy(), None
+        table.view(np.float64)[:, _DECAY] = weight_decay
     d_lr = _scalar("lr", lr, torch.float32, dev) if torch.is_tensor(lr) else 0
     d_step = _scalar("step", step, torch.int64, dev) if torch.is_tensor(step) else 0
     d_scale = 0 if grad_scale is None else _scalar("grad_scale", grad_scale, torch.float32, dev)
     desc = _DESC.pack(int(wt == torch.bfloat16), int(gt == torch.bfloat16), state.bits, 0.0 if d_lr else lr, betas[0], betas[1], eps,
                       0 if d_step else int(step), d_lr, d_step, d_scale)
-    lists = (weights, grads, None if out is None else new, copies)
+    lists = (weights, grads, None if out is None else new, copies, keep)
     dims, at = state._at
     with _stream_of(stream, dev) if dev.type == "cuda" else contextlib.nullcontext(0) as sp:
         got = _native().adamw(lists, (wt, gt), dev.index if dev.type == "cuda" else -1, dims, at if table is state._table else _address(table),
@@ -223,6 +216,10 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
             for name, t, dt in zip(_NAMES, lists, (wt, gt, wt, torch.bfloat16)):
                 if t is not None:
                     _fit(name, t, dt, dev, shapes)
+            for k, shape, n in zip(keep or (), shapes, state.sizes):
+                if k is not None and (len(shape) < 2 or k.dtype != torch.int16 or k.shape != shape[:2] or n != 9 * k.numel() or
+                                      not k.is_contiguous() or k.device != dev):
+                    raise ValueError("keep must be contiguous int16 [c_out][c_in] of a 3x3 layer's weights, on their device")
             raise ValueError("the tensors must be on a GPU")
         if got > 0:
             raise ValueError(_OWN[got])

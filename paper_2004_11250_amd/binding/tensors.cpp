@@ -7,8 +7,8 @@
 //
 // adamw(lists, dtypes, device, dims, table, weight_decay, elements, buffers, desc, fn,
 //       stream) -> int
-//     lists: weights, grads, new weights and copies (None: weights; none), of the
-//     table's length.  table: rows of pp_adamw_tensor (weight_decay: of all, or None:
+//     lists: weights, grads, new weights, copies and tap masks (None: weights; none;
+//     none, as may be one of the masks), of the table's length.  table: rows of pp_adamw_tensor (weight_decay: of all, or None:
 //     the rows' own); desc: a pp_adamw_desc without moments; buffers: m, v, m_scale and
 //     v_scale of the state and of the new one, of `elements`; fn: pp_adamw_step.
 //     Counts a change of what was written.  0; 1: two outputs begin at the same
@@ -19,11 +19,13 @@
 //     with pp_grad_norm_workspace and pp_grad_norm; 10: the list does not fit; a pp_status
 // embed_fwd(ids, w, dtype, scale, ignore_index, fn, stream) -> features
 //     with pp_embed_fwd, of contiguous tensors on one GPU, dtype None: w's
-// embed_bwd(ids, dy, v, dtype, scale, ignore_index, workspace_fn, fn, stream) -> gradient
-//     with pp_embed_workspace and pp_embed_bwd, likewise.  Both: None, with nothing
+// embed_bwd(ids, dy, v, dtype, scale, ignore_index, add, workspace_fn, fn, stream)
+//     -> gradient
+//     with pp_embed_workspace and pp_embed_bwd, likewise (add: or None).  Both: None, with nothing
 //     done, where an argument is another than these; a pp_status
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -77,6 +79,21 @@ bool gather(PyObject* list, at::ScalarType dtype, at::Device device, const int64
   return true;
 }
 
+// addresses of tap masks to the table: int16, of the first two sizes of a tensor that
+// has nine values for each
+bool masks(PyObject* list, at::Device device, const int64_t* dims, pp_adamw_tensor* table) {
+  for (Py_ssize_t i = 0; i < PyList_GET_SIZE(list); ++i, dims += dims[0] + 1) {
+    PyObject* o = PyList_GET_ITEM(list, i);
+    if (o == Py_None) continue;
+    const at::Tensor* t = whole(o, 2, 2);
+    if (!t || t->device() != device || t->scalar_type() != at::kShort || dims[0] < 2 || t->size(0) != dims[1] || t->size(1) != dims[2] ||
+        table[i].n != 9 * t->numel())
+      return false;
+    table[i].keep = static_cast<const uint16_t*>(t->data_ptr());
+  }
+  return true;
+}
+
 // 0, or which rule the outputs break
 int own_of(const int64_t* table, Py_ssize_t count, bool copies) {
   std::vector<int64_t> outs;
@@ -122,12 +139,12 @@ PyObject* guarded(F&& f) {
 }
 
 PyObject* adamw(PyObject*, PyObject* const* arg, Py_ssize_t n) {
-  if (n != 11 || !PyTuple_Check(arg[0]) || PyTuple_GET_SIZE(arg[0]) != 4 || !PyTuple_Check(arg[1]) || PyTuple_GET_SIZE(arg[1]) != 2 ||
+  if (n != 11 || !PyTuple_Check(arg[0]) || PyTuple_GET_SIZE(arg[0]) != 5 || !PyTuple_Check(arg[1]) || PyTuple_GET_SIZE(arg[1]) != 2 ||
       !PyTuple_Check(arg[7]) || PyTuple_GET_SIZE(arg[7]) != 8 || !PyBytes_Check(arg[8]) || PyBytes_GET_SIZE(arg[8]) != sizeof(pp_adamw_desc))
     return refuse("adamw(lists, dtypes, device, dims, table, weight_decay, elements, buffers, desc, fn, stream)");
-  PyObject* lists[4];
+  PyObject* lists[5];
   at::ScalarType dtypes[4];
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < 5; ++k) {
     lists[k] = PyTuple_GET_ITEM(arg[0], k);
     if (!(k > 1 && lists[k] == Py_None) && (!PyList_Check(lists[k]) || PyList_GET_SIZE(lists[k]) != PyList_GET_SIZE(lists[0])))
       return refuse("lists of one length");
@@ -170,6 +187,7 @@ PyObject* adamw(PyObject*, PyObject* const* arg, Py_ssize_t n) {
     int64_t* table = reinterpret_cast<int64_t*>(all.data());
     for (int k = 0; k < 4; ++k)
       if (lists[k] != Py_None && !gather(lists[k], dtypes[k], on(device), dims, table + 1 + k, kRow, false)) return PyLong_FromLong(10 + k);
+    if (lists[4] != Py_None && (!dims || !masks(lists[4], on(device), dims, all.data()))) return PyLong_FromLong(14);
     for (Py_ssize_t i = 0; i < count; ++i) {
       if (lists[2] == Py_None) table[kRow * i + 3] = table[kRow * i + 1];
       if (arg[5] != Py_None) all[i].weight_decay = decay;
@@ -211,6 +229,7 @@ PyObject* grad_norm(PyObject*, PyObject* const* arg, Py_ssize_t n) {
     status = fn(table.data(), static_cast<int32_t>(count), code, static_cast<float>(most), both.data_ptr<float>(), ws.data_ptr(),
                 static_cast<size_t>(ws.numel()), stream);
     if (status) return PyLong_FromLong(status);
+    const at::AutoDispatchBelowADInplaceOrView plain;   // (no autograd's part of two views: 1 us)
     PyObject *x = THPVariable_Wrap(both.select(0, 0)), *y = THPVariable_Wrap(both.select(0, 1));
     PyObject* got = x && y ? PyTuple_Pack(2, x, y) : nullptr;
     Py_XDECREF(x);
@@ -267,10 +286,10 @@ PyObject* embed_fwd(PyObject*, PyObject* const* arg, Py_ssize_t n) {
 }
 
 PyObject* embed_bwd(PyObject*, PyObject* const* arg, Py_ssize_t n) {
-  if (n != 9) return refuse("embed_bwd(ids, dy, v, dtype, scale, ignore_index, workspace_fn, fn, stream)");
-  auto need = reinterpret_cast<decltype(&pp_embed_workspace)>(words(arg[6]));
-  auto fn = reinterpret_cast<decltype(&pp_embed_bwd)>(words(arg[7]));
-  void* stream = words(arg[8]);
+  if (n != 10) return refuse("embed_bwd(ids, dy, v, dtype, scale, ignore_index, add, workspace_fn, fn, stream)");
+  auto need = reinterpret_cast<decltype(&pp_embed_workspace)>(words(arg[7]));
+  auto fn = reinterpret_cast<decltype(&pp_embed_bwd)>(words(arg[8]));
+  void* stream = words(arg[9]);
   if (PyErr_Occurred()) return nullptr;
   return guarded([&]() -> PyObject* {
     const at::Tensor *ids = whole(arg[0], 0, 63), *dy = whole(arg[1], 1, 64);
@@ -281,12 +300,19 @@ PyObject* embed_bwd(PyObject*, PyObject* const* arg, Py_ssize_t n) {
         !number(arg[5], &d.ignore_index))
       Py_RETURN_NONE;
     d.t = ids->numel(), d.d = d.w_ld = d.y_ld = dy->size(-1);
+    const at::Tensor* add = nullptr;
+    if (arg[6] != Py_None) {
+      add = whole(arg[6], 2, 2);
+      if (!add || add->device() != ids->device() || add->size(0) != d.v || add->size(1) != d.d ||
+          (d.w_dtype = code_of(add->scalar_type())) < 0 || code_of(arg[3], d.w_dtype) != d.w_dtype)
+        Py_RETURN_NONE;
+    }
     size_t bytes = 0;
     int32_t status = need(&d, &bytes);
     if (status) return PyLong_FromLong(status);
     const at::Tensor dw = rows_of({d.v, d.d}, d.w_dtype, *ids);
     const at::Tensor ws = at::empty({static_cast<int64_t>(bytes)}, at::TensorOptions().device(ids->device()).dtype(at::kByte));
-    status = fn(&d, ids->data_ptr<int64_t>(), dy->data_ptr(), nullptr, dw.data_ptr(), ws.data_ptr(), bytes, stream);
+    status = fn(&d, ids->data_ptr<int64_t>(), dy->data_ptr(), add ? add->data_ptr() : nullptr, dw.data_ptr(), ws.data_ptr(), bytes, stream);
     return status ? PyLong_FromLong(status) : THPVariable_Wrap(dw);
   });
 }

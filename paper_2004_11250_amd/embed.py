@@ -137,9 +137,9 @@ def embed_bwd(ids, dy, v, scale=1.0, ignore_index=-100, dtype=None, add=None, ou
     head's weights too).  Fills ``out``, if given; it may be ``add``, and then only
     the rows that ids reach are touched."""
     torch = _torch()
-    if out is None and add is None and stream is None and ids.is_cuda:
+    if out is None and stream is None and ids.is_cuda:
         with _stream_of(None, ids.device) as sp:
-            dw = _native().embed_bwd(ids, dy, v, dtype, scale, ignore_index, _entry("pp_embed_workspace"), _entry("pp_embed_bwd"), sp)
+            dw = _native().embed_bwd(ids, dy, v, dtype, scale, ignore_index, add, _entry("pp_embed_workspace"), _entry("pp_embed_bwd"), sp)
         if dw is not None:
             return _done(dw, "pp_embed_bwd")
     yc = _dtype_code(dy)

@@ -229,9 +229,13 @@ def test_adamw_tensors():
         go(keep=[torch.zeros(4, 6, dtype=torch.int16), None])
     with refused("length"):
         go(keep=[None])
+    layer = torch.zeros(2, 3, 3, 3)
+    pruned = lambda keep: pp.adamw_step(layer, layer.clone(), pp.AdamWState(layer), lr=1e-3, step=1, keep=keep)   # noqa: E731
     with refused("GPU"):
-        pp.adamw_step(torch.zeros(2, 3, 3, 3), torch.zeros(2, 3, 3, 3), pp.AdamWState(torch.zeros(2, 3, 3, 3)), lr=1e-3, step=1,
-                      keep=torch.zeros(2, 3, dtype=torch.int16))
+        pruned(torch.zeros(2, 3, dtype=torch.int16))
+    for bad in (torch.zeros(2, 3), torch.zeros(3, 2, dtype=torch.int16), torch.zeros(3, 2, dtype=torch.int16).t(), torch.zeros(6, dtype=torch.int16)):
+        with refused("keep"):
+            pruned(bad)
 
 
 def test_norm_tensors():
@@ -287,7 +291,7 @@ def test_outputs_of_their_own():
         """Of two tensors: indices into x."""
         table[:, 0] = n
         pick = lambda t, dt=torch.float32: None if t is None else [x[i].view(dt) if dt != torch.float32 else x[i] for i in t]   # noqa: E731
-        return adamw._native().adamw((pick(w), pick(g), pick(new), pick(copies, torch.bfloat16)), (torch.float32, torch.float32), -1, 0,
+        return adamw._native().adamw((pick(w), pick(g), pick(new), pick(copies, torch.bfloat16), None), (torch.float32, torch.float32), -1, 0,
                                      table.ctypes.data, None, 256, (*moments, None, None) * 2, bytes(desc), 1, 0)
 
     assert code((0, 1), (2, 2)) == 30 and code((0, 1), (2, 3), (4, 5)) == 30 and code((0, 1), (2, 3), None, (4, 5)) == 30
@@ -302,14 +306,14 @@ def test_native_calls_take_tensors_on_a_gpu_only():
     t, dims = np.zeros((2, 8), np.int64), np.array([1, 3, 1, 3], np.int64)
     x = [torch.zeros(3), torch.zeros(3)]
     bufs, desc = [torch.zeros(256), torch.zeros(256), None, None], bytes(AdamWDesc(bits=32))
-    go = lambda w=x, g=x, new=None, copies=None, dt=(f32, f32), at=-1, b=bufs, d=desc, n=256: lists.adamw(   # noqa: E731
-        (w, g, new, copies), dt, at, dims.ctypes.data, t.ctypes.data, 0.5, n, (*b, *b), d, 1, 0)
+    go = lambda w=x, g=x, new=None, copies=None, keep=None, dt=(f32, f32), at=-1, b=bufs, d=desc, n=256: lists.adamw(   # noqa: E731
+        (w, g, new, copies, keep), dt, at, dims.ctypes.data, t.ctypes.data, 0.5, n, (*b, *b), d, 1, 0)
     assert go() == 30 and not t.any()
     assert go(at=0) == 20 and go(n=128) == 20 and go(b=bufs[:3] + bufs[:1]) == 20 and go(d=bytes(AdamWDesc(bits=8))) == 20
     assert go(b=[torch.zeros(256).bfloat16(), *bufs[1:]]) == 20 and go(b=[torch.zeros(512)[::2], *bufs[1:]]) == 20
     assert go(w=[None, None]) == 10 and go(w=["a", 3]) == 10 and go(g=[x[0], x[1].double()]) == 11 and go(new=[x[0], torch.zeros(4)]) == 12
-    assert go(copies=x) == 13
-    for bad in (dict(w=None), dict(g=x[:1]), dict(new=x[:1]), dict(copies=(1, 2)), dict(dt=("f", f32)), dict(dt=f32), dict(b=bufs[:3]),
+    assert go(copies=x) == 13 and go(keep=[None, torch.zeros(1, 1, dtype=torch.int16)]) == 14 and go(keep=[None, None]) == 30
+    for bad in (dict(w=None), dict(g=x[:1]), dict(new=x[:1]), dict(copies=(1, 2)), dict(keep=[None]), dict(dt=("f", f32)), dict(dt=f32), dict(b=bufs[:3]),
                 dict(d=desc[1:]), dict(d="x"), dict(n=0.5)):
         with pytest.raises(TypeError):
             go(**bad)
@@ -319,10 +323,10 @@ def test_native_calls_take_tensors_on_a_gpu_only():
             lists.grad_norm(*bad)
     ids, w = torch.zeros(3, dtype=torch.int64), torch.zeros(2, 4)
     assert lists.embed_fwd(ids, w, None, 1.0, -100, 1, 0) is None and lists.embed_fwd([0], w, None, 1.0, -100, 1, 0) is None
-    assert lists.embed_bwd(ids, torch.zeros(3, 4), 2, None, 1.0, -100, 1, 1, 0) is None
+    assert lists.embed_bwd(ids, torch.zeros(3, 4), 2, None, 1.0, -100, None, 1, 1, 0) is None
     for bad in ((), (ids, w, None, 1.0, -100, 1), (ids, w, None, 1.0, -100, "1", 0)):
         with pytest.raises(TypeError):
             lists.embed_fwd(*bad)
-    for bad in ((), (ids, w, 2, None, 1.0, -100, 1, 1), (ids, w, 2, None, 1.0, -100, 1, 1, "0")):
+    for bad in ((), (ids, w, 2, None, 1.0, -100, None, 1, 1), (ids, w, 2, None, 1.0, -100, None, 1, 1, "0")):
         with pytest.raises(TypeError):
             lists.embed_bwd(*bad)
