@@ -297,9 +297,8 @@ struct Grad {
   const void* g;
   int64_t n;
 };
-constexpr int kGrads = 192;
-using Grads = List<Grad, kGrads>;
-static_assert(sizeof(Grads) + 16 <= 4096, "kernel arguments hold 4 KB");
+constexpr int kGrads = 192, kShort = 8;   // (a short list's launch takes 0.6 us less of the host)
+static_assert(sizeof(List<Grad, kGrads>) + 16 <= 4096, "kernel arguments hold 4 KB");
 
 template <int WAVES>
 __device__ __forceinline__ double sum_of_block(double x, double* sums) {
@@ -312,8 +311,8 @@ __device__ __forceinline__ double sum_of_block(double x, double* sums) {
 }
 
 // A chunk's sum of squares.  59 MB of fp32 11.5 us, 63 MB of bf16 13.3: 5.1 and 4.7 TB/s.
-template <class G>
-__global__ __launch_bounds__(256) void square_kernel(const Grads list, int32_t size, double* part) {
+template <class G, int N>
+__global__ __launch_bounds__(256) void square_kernel(const List<Grad, N> list, int32_t size, double* part) {
   __shared__ double sums[4];
   int chunk;
   const Grad& t = list.item[find(list, blockIdx.x, &chunk)];
@@ -514,13 +513,17 @@ pp_status norm(const pp_grad* grads, int32_t count, int32_t dtype, float most, f
   double* part = static_cast<double*>(ws);
   auto fill = [](Grad& x, const pp_grad& t) { x = {t.g, t.n}; };
   int64_t at = 0;
-  r = each_launch<Grads>(grads, count, chunk, fill, [&](const Grads& list, uint32_t blocks) {
-    if (dtype == PP_BF16)
-      hipLaunchKernelGGL((square_kernel<bf16>), dim3(blocks), dim3(256), 0, st, list, chunk, part + at);
-    else
-      hipLaunchKernelGGL((square_kernel<float>), dim3(blocks), dim3(256), 0, st, list, chunk, part + at);
-    at += blocks;
-  });
+  auto launch = [&](auto size) {
+    constexpr int N = decltype(size)::value;
+    return each_launch<List<Grad, N>>(grads, count, chunk, fill, [&](const List<Grad, N>& list, uint32_t blocks) {
+      if (dtype == PP_BF16)
+        hipLaunchKernelGGL((square_kernel<bf16, N>), dim3(blocks), dim3(256), 0, st, list, chunk, part + at);
+      else
+        hipLaunchKernelGGL((square_kernel<float, N>), dim3(blocks), dim3(256), 0, st, list, chunk, part + at);
+      at += blocks;
+    });
+  };
+  r = count <= kShort ? launch(std::integral_constant<int, kShort>()) : launch(std::integral_constant<int, kGrads>());
   if (r != PP_OK) return r;
   hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(1024), 0, st, part, parts, most, out);
   return launched();
