@@ -141,19 +141,19 @@ __device__ __forceinline__ void put_codes(void* p, int64_t at, Codes c) {
 
 // Eight elements a lane, a chunk of one tensor a workgroup; a block's scales are the
 // largest of 16 lanes.  Three states in turn, us a step in place / into other arrays:
-// fp32 w, g and moments, VGG-16, 15 M weights 75 / 75 (5.5 TB/s), 51 M 237 / 237
-// (6.05 TB/s); bf16 w and g, 8-bit moments, 102 M 172 / 172 (6.0 TB/s); fp32 w, bf16 g
-// and copies, 8-bit moments, 31 M 104 / 99 (5.0 TB/s).
+// fp32 w, g and moments, VGG-16, 15 M weights 75 / 75 (5.5 TB/s), 51 M 239 / 238
+// (6.0 TB/s); bf16 w and g, 8-bit moments, 102 M 172 / 172 (6.0 TB/s); fp32 w, bf16 g
+// and copies, 8-bit moments, 31 M 98 / 94 (5.3 TB/s).
 // Where a value has four bytes a lane's eight are two fours 64 elements apart, so that
 // each access of 16 lanes is 256 bytes in a row (eight in a row are two accesses of half
 // of each line: 51 M fp32 weights 263, and past the caches 362).
-// Elements of a workgroup, 32 bits 2048, 4096: 51 M fp32 237, 247; 8 bits 2048, 4096,
-// 8192: 102 M 173, 169, 191.
+// Elements of a workgroup, 2048 / 4096 / 8192: fp32 w, 32 bits, 51 M 237 / 247 / -, 8 bits
+// 124 / 131 / 139; bf16 w and g, 8 bits, 102 M 178 / 172 / 193.
 // With 8 bits some 45 instructions an element stand beside 10 bytes of memory, and count:
-// one root serves the update and the code, what only some steps need (masks, a tensor's
-// end, values that are not finite, roots below the normal range) is looked for by eight
-// elements together (all with it 193 / 213), and the update's division is a product with
-// the hardware's reciprocal, 1 ulp (an exact one: 175 / 197).
+// one root serves the update and the code, what only some steps need (masks: 181 without
+// the test; a tensor's end, values that are not finite, roots below the normal range) is
+// looked for by eight elements together, and the update's division is a product with the
+// hardware's reciprocal, 1 ulp (102 M, an exact one: 183 / 178).
 template <class W, class G, int BITS, bool ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const Step s) {
   constexpr bool SPLIT = kSplit<W, G> || BITS == 32;
@@ -440,11 +440,13 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   s.d_lr = d.d_lr, s.d_step = d.d_step, s.d_scale = d.d_grad_scale;
   s.m = d.m, s.v = d.v, s.ms = d.m_scale, s.vs = d.v_scale;
   s.m_out = d.m_out, s.v_out = d.v_out, s.ms_out = d.m_scale_out, s.vs_out = d.v_scale_out;
-  s.chunk = chunk_of(total, d.bits == 8 ? 4096 : 2048);
+  const bool narrow = d.bits == 8 && d.w_dtype == PP_BF16 && d.g_dtype == PP_BF16;
+  s.chunk = chunk_of(total, narrow ? 4096 : 2048);
   // Steps of more than the last cache holds (256 MB) go past the caches.  us, past them /
-  // not, three states in turn in place: 15 M fp32 weights 75 / 85, 51 M 237 / 265, with
-  // 8-bit moments 131 / 140, 102 M bf16 weights with 8-bit moments 172 / 192; 3 M fp32
-  // weights (86 MB) 17.9 / 15.5, 8 M bf16 with 8-bit moments (82 MB) 19.9 / 18.1.
+  // not, three states in turn in place: 15 M fp32 weights 75 / 85 (one again and again:
+  // 74 / 60), 51 M 239 / 267, with 8-bit moments 124 / 135, 102 M bf16 weights with 8-bit
+  // moments 172 / 193; 3 M fp32 weights (86 MB) 17.6 / 15.3, 8 M bf16 with 8-bit moments
+  // (82 MB) 19.5 / 17.5.
   const bool past = total * static_cast<double>(2 * size_of(d.w_dtype) + size_of(d.g_dtype) + (d.bits == 8 ? 4 : 16)) > 256e6;
   auto fill = [](Tensor& x, const pp_adamw_tensor& t) {
     x = {t.w, t.g, t.w_out, static_cast<bf16*>(t.copy), t.keep, t.n, t.at, static_cast<float>(t.weight_decay)};
