@@ -467,14 +467,17 @@ __device__ __forceinline__ void fill_rows(const Sum& a, int block) {
 
 // A workgroup sums the piece p0 .. p1 of a list, a group of lanes a part of it, of
 // `batches` batches of kBatch tokens; `at`: the group's first batch.  A run of one
-// row's tokens that begins and ends inside a group's part is written by the group;
-// a part's first and last run meet their neighbours' in LDS.  What goes on past the
-// piece's ends (row `prev` before it, `next` behind it, -1: none) goes to part: the
-// sum of a run that goes on from the piece before to row 0, of one that begins here
-// to row 1.  A batch's rows are in flight together, and a piece's time is that of its
-// list, its rows and its neighbours in LDS one after the other: 32768 tokens into
-// 313 x 256 bf16 7.9 us (batches of 4 7.1, but twice the pieces for join_kernel, of 16
-// 23: too few waves).
+// row's tokens that begins and ends inside a group's part is written by the group; a
+// part's first and last run meet their neighbours' in the wave, by steps that double,
+// and a wave's first and last run (where a group is a wave or more, a group's) meet
+// theirs in LDS.  (All groups' in LDS, one after the other: 17102 tokens into 112 x 32
+// bf16, three in ten ids the same, 27 us a call, now 18; with as many rows as tokens
+// it was 0.5 us less.)  What goes on past the piece's ends (row `prev` before it,
+// `next` behind it, -1: none) goes to part: the sum of a run that goes on from the
+// piece before to row 0, of one that begins here to row 1.  A batch's rows are in
+// flight together, and a piece's time is that of its list, its rows and its neighbours
+// in LDS one after the other: 32768 tokens into 313 x 256 bf16 7.9 us (batches of 4
+// 7.1, but twice the pieces for join_kernel, of 16 23: too few waves).
 template <class Y, class W, int THREADS>
 __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int p0, int p1, int batches, Place (&at)[kBatch],
                                           int32_t prev, int32_t next, float* part, float (*edge)[8], int32_t* edge_row) {
@@ -484,14 +487,21 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
   const Y* dy = static_cast<const Y*>(a.dy) + c;
   const int i0 = p0 + g * batches * kBatch, i1 = min(i0 + batches * kBatch, p1);
 
-  float acc[8];
-  int cur = -1;
-  bool first = true;
-  auto to_edge = [&](int slot) {
+  float acc[8] = {};
+  int cur = -1, head = -1;      // the row of acc, and of the group's first run where that is another
+  // Units whose runs meet in LDS: groups, or waves of several.  A unit's first run has
+  // its first slot, its last one, where that is another, its second.
+  const int unit = a.lanes < 6 ? static_cast<int>(threadIdx.x) >> 6 : g;
+  const int wide = max(a.lanes, 6);
+  auto to_edge = [&](int slot, const float (&x)[8]) {     // (slot: of the unit, or 2 k: the wave's group k's)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) edge[(slot << a.lanes) + lane][e] = acc[e];
-    if (lane == 0) edge_row[slot] = cur;
+    for (int e = 0; e < 8; ++e) edge[(unit << (wide + 1)) + (slot << a.lanes) + lane][e] = x[e];
   };
+  auto from_edge = [&](int at, int slot, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = edge[(at << (wide + 1)) + (slot << a.lanes) + lane][e];
+  };
+  const int member = a.lanes < 6 ? g & ((64 >> a.lanes) - 1) : 0;
   for (int i = i0; i < i1; i += kBatch) {
     Eight<Y> x[kBatch];
     if (i > i0) {
@@ -507,8 +517,8 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
       if (i + u >= i1) break;
       if (at[u].row != cur) {
         if (cur >= 0) {
-          if (first)
-            to_edge(2 * g), first = false;
+          if (head < 0)
+            to_edge(2 * member, acc), head = cur;
           else if (cols > 0)
             put_row<SPLIT, W>(a, cur, c, acc);
         }
@@ -520,23 +530,73 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
       for (int e = 0; e < 8; ++e) acc[e] += static_cast<float>(x[u][e]);
     }
   }
-  if (lane == 0) {
-    if (first) edge_row[2 * g] = -1;
-    edge_row[2 * g + 1] = -1;
+  const int32_t last = head >= 0 ? cur : -1;      // the row of the last run, where it is another
+  if (head < 0) head = cur;
+  if (a.lanes < 6) {
+    // in a wave: each group's first run with what follows of it (rows of a sorted list
+    // are the same only where all between them are), then the last runs with the next
+    // group's first
+    const int in_wave = 64 >> a.lanes, step = 1 << a.lanes;
+    float x[8];
+    __builtin_amdgcn_wave_barrier();
+    if (last >= 0) {
+      from_edge(unit, 2 * member, x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = acc[e];
+    }
+    const int32_t end = last >= 0 ? last : head, prior = __shfl_up(end, step), follows = __shfl_down(head, step);
+    const uint64_t some = __ballot(head >= 0);
+    const int32_t row0 = __builtin_amdgcn_readlane(head, 0), row1 = __builtin_amdgcn_readlane(end, some ? 63 - __clzll(some) : 0);
+    int32_t row = follows;
+    for (int k = 1; k < in_wave; k *= 2) {
+      if (k > 1) row = __shfl_down(head, k * step);
+      const bool on = member + k < in_wave && row == head && row >= 0;
+      if (!__ballot(on)) break;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = __shfl_down(x[e], k * step);
+        x[e] += on ? y : 0.f;
+      }
+    }
+    const bool more = member + 1 < in_wave && follows == last && last >= 0;
+    if (__ballot(more)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float y = __shfl_down(x[e], step);
+        acc[e] += more ? y : 0.f;
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (head >= 0 && (member == 0 || prior != head)) {
+      if (member == 0 || head == row1)
+        to_edge(member == 0 ? 0 : 1, x);
+      else if (cols > 0)
+        put_row<SPLIT, W>(a, head, c, x);
+    }
+    if (last >= 0) {
+      if (last == row1)
+        to_edge(1, acc);
+      else if (cols > 0)
+        put_row<SPLIT, W>(a, last, c, acc);
+    }
+    if ((threadIdx.x & 63) == 0) edge_row[2 * unit] = row0, edge_row[2 * unit + 1] = row1 == row0 ? -1 : row1;
+  } else {
+    if (cur >= 0) to_edge(last >= 0 ? 1 : 0, acc);
+    if (lane == 0) edge_row[2 * unit] = head, edge_row[2 * unit + 1] = last;
   }
-  if (cur >= 0) to_edge(2 * g + (first ? 0 : 1));
   __syncthreads();
-  if (cols <= 0) return;
+  if (cols <= 0 || member > 0) return;
 
-  // the runs that begin at this group's edges; groups past the piece's end have none
-  const int slots = 2 * min(groups, (p1 - p0 + batches * kBatch - 1) / (batches * kBatch));
-  for (int s = 2 * g; s < 2 * g + 2; ++s) {
+  // the runs that begin at this unit's edges; units past the piece's end have none
+  const int of_unit = (batches * kBatch) << (wide - a.lanes);
+  const int slots = 2 * min(THREADS >> wide, (p1 - p0 + of_unit - 1) / of_unit);
+  for (int s = 2 * unit; s < 2 * unit + 2; ++s) {
     const int32_t row = edge_row[s];
     if (row < 0) continue;
     const int32_t left = s == 0 ? -1 : edge_row[s - 1] >= 0 ? edge_row[s - 1] : s > 1 ? edge_row[s - 2] : -1;
     if (left == row) continue;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = edge[(s << a.lanes) + lane][e];
+    from_edge(unit, s & 1, acc);
     bool ends = false;          // another run follows in this piece
     constexpr int kNear = 4;    // (read together, whether they belong to the run or not)
     for (int q = s + 1; q < slots && !ends; q += kNear) {
@@ -546,8 +606,7 @@ __device__ __forceinline__ void sum_piece(const Sum& a, const Place* order, int 
       for (int u = 0; u < kNear; ++u) {
         const int k = min(q + u, slots - 1);
         r[u] = edge_row[k];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[u][e] = edge[(k << a.lanes) + lane][e];
+        from_edge(k >> 1, k & 1, x[u]);
       }
 #pragma unroll
       for (int u = 0; u < kNear; ++u) {

@@ -170,6 +170,28 @@ def test_sorts(v, t):
     assert same(got, pp.embed_bwd(ids, dy, v, ignore_index=v // 2, add=add, out=add))
 
 
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [1, 8, 16, 31, 32, 64, 128, 203, 256, 512, 1024])
+@pytest.mark.parametrize("t", [900, 6000, 40000])
+def test_runs_of_every_length(y, d, t):
+    """Of whole numbers below 2^24 in all, whose sums are exact in any order; a row with infinities keeps them to itself."""
+    g = torch.Generator().manual_seed(t + d)
+    kinds = torch.tensor([1, 2, 3, 7, 8, 9, 15, 16, 17, 31, 64, 65, 127, 130, 257, 511, 520, 1100])
+    lens = kinds[torch.randint(0, len(kinds), (600,), generator=g)]
+    lens = lens[:int((lens.cumsum(0) <= t).sum())]
+    v = len(lens) + 3                   # (with rows that no token reaches)
+    rows = torch.randperm(v, generator=g)[:len(lens)]
+    ids = rows.repeat_interleave(lens)[torch.randperm(int(lens.sum()), generator=g)].cuda()
+    dy = torch.randint(-8, 9, (len(ids), d), generator=g).cuda().to(DT[y])
+    want = torch.zeros(v, d, dtype=torch.float64, device="cuda").index_add_(0, ids, dy.double())
+    assert torch.equal(pp.embed_bwd(ids, dy, v, dtype=torch.float32).double(), want)
+    wild = int(rows[0])
+    dy[ids == wild] = float("inf")
+    got = pp.embed_bwd(ids, dy, v, dtype=torch.float32).double()
+    want[wild] = float("inf")
+    assert torch.equal(got, want)
+
+
 def test_ids_that_reach_no_row():
     ids = torch.tensor([-1, 10, 1 << 33, -100, 4, 4, 9, -(1 << 63), (1 << 63) - 1], device="cuda")
     dy = normal(2, 9, 40)
