@@ -850,11 +850,12 @@ Plan plan_of(const pp_embed_desc& d) {
   p.deal.per = static_cast<int32_t>(cdiv(runs, int64_t(1) << p.deal.log) << p.deal.run);
   // The sort by digits: two launches (five for two digits), but no workgroup that reads
   // all ids or has all tokens of a row.  us a call, sort_kernel / digits: 313 rows of 256
-  // bf16 features, three in ten ids the same, 8192 tokens 17 / 18, 32768 28 / 22, 2^20
-  // 675 / 132; 50000 rows of 64 features, 32768 tokens: ids log-uniform 32 / 38, uniform
-  // 20 / 34, three in ten the same 40 / 37; 65536: 42 / 42, 25 / 36, 60 / 43; 2^20: 575 /
-  // 108, 177 / 100, 861 / 118.  sort_kernel's workgroups come in rounds of kCUs, each of
-  // about 4.5 us and 0.2 for 1000 tokens.
+  // bf16 features, three in ten ids the same, 16384 tokens 20 / 20, 32768 27 / 21, 2^20
+  // 665 / 129; 50000 rows of 64 features, 32768 tokens: ids log-uniform 27 / 30, uniform
+  // 22 / 30, three in ten the same 35 / 31; 65536: 38 / 33, 26 / 33, 56 / 35; 2^20: 571 /
+  // 102, 179 / 96, 845 / 100; 200000 rows of 256, 16384 tokens: 33 / 44, 32 / 44, 40 / 46.
+  // sort_kernel's workgroups come in rounds of kCUs, each of about 4.5 us and 0.2 for
+  // 1000 tokens.
   const int64_t rounds = cdiv(int64_t(1) << p.deal.log, kCUs);
   int all = 0;
   while (int64_t(1) << all < d.v) ++all;
