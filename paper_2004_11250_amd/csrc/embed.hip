@@ -651,7 +651,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Sum a) {
 
 // Up to kFewTokens tokens: a workgroup has its rows of the table, finds their tokens,
 // a thread an id, sorts them in LDS, sums them, and fills its rows without a token,
-// all in one launch.  777 tokens into 5003 x 203 fp32 9 us: ids, the order, rows of
+// all in one launch.  777 tokens into 5003 x 203 fp32 8 us: ids, the order, rows of
 // features and edges, one after the other; a table of 50000 x 1024 bf16 is filled in
 // 20, 5 TB/s.
 constexpr int kFewTokens = 1024, kFewRanks = 256;
@@ -835,8 +835,9 @@ Plan plan_of(const pp_embed_desc& d) {
   p.lanes = lanes_for(d.d);
   // One launch instead of two or three, at the risk that one row has all tokens, whose
   // features one workgroup then reads (at 100 GB/s).  us a call, one launch / three:
-  // 777 tokens into 5003 x 203 fp32 9 / 16, 128 tokens into 50000 x 1024 bf16 21 / 28;
-  // all of one row: 256 tokens, 1024 features, fp32 (1 MB) 19 / 17, 1024 tokens (4 MB) 68 / 18.
+  // 777 tokens into 5003 x 203 fp32 8 / 15, 128 tokens into 50000 x 1024 bf16 21 / 26;
+  // all of one row: 777 tokens 26 / 15, 256 tokens, 1024 features, fp32 (1 MB) 25 / 15,
+  // 1024 tokens (4 MB) 85 / 18.
   p.few = d.t <= kFewTokens && d.t * d.d * static_cast<int64_t>(size_of(d.y_dtype)) <= 1 << 20;
   // Workgroups of sort_kernel and few_kernel: as many as CUs, or more where one's rows
   // would be too many; of narrow rows some at a time, 256 bytes, so that whole lines of
