@@ -718,7 +718,9 @@ pp_status pp_embed_bwd(const pp_embed_desc* desc, const int64_t* ids, const void
  *       division: 4 bits of the exponent and 4 after the leading one, c = 255
  *       being 1); c = 0: r = 0; and v = (r times the block's scale)^2, the scale
  *       being the largest sqrt(v')
- * rounded to the nearest, ties to even codes.  A v' above 0 has a code of 1 at
+ * rounded to the nearest, ties to even codes (so that a code stays where a step
+ * moves its value by less than half a code, and follows the block's scale, which
+ * is not rounded).  A v' above 0 has a code of 1 at
  * least (2^-16 1.125), so that a small second moment is held too large, never as
  * 0.  A scale is at least 2^-100.  W' is taken from m' and v' before they are
  * rounded.  An element whose m' is not finite keeps a NaN as m (the others of its

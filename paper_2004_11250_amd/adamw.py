@@ -72,7 +72,6 @@ class AdamWState:
         self._table = np.zeros((len(self.sizes), len(_TENSOR)), np.int64)
         self._table[:, _N], self._table[:, _AT] = self.sizes, self.places
         self._dims = np.array([n for s in self.shapes for n in (len(s), *s)] or [0], np.int64)
-        self._at = _address(self._dims), _address(self._table)
 
         def zeros(n, dtype):
             return torch.zeros(n, dtype=torch.uint8, device=device).view(dtype)
@@ -128,10 +127,6 @@ class AdamWState:
 
 def _list(t):
     return [t] if _torch().is_tensor(t) else list(t)
-
-
-def _address(a):
-    return a.__array_interface__["data"][0]
 
 
 def _fit(name, tensors, dtype, device, shapes=None):
@@ -205,10 +200,9 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
     desc = _DESC.pack(int(wt == torch.bfloat16), int(gt == torch.bfloat16), state.bits, 0.0 if d_lr else lr, betas[0], betas[1], eps,
                       0 if d_step else int(step), d_lr, d_step, d_scale)
     lists = (weights, grads, None if out is None else new, copies, keep)
-    dims, at = state._at
     with _stream_of(stream, dev) if dev.type == "cuda" else contextlib.nullcontext(0) as sp:
-        got = _native().adamw(lists, (wt, gt), dev.index if dev.type == "cuda" else -1, dims, at if table is state._table else _address(table),
-                              decay, state.elements, (*state._buffers(), *state_out._buffers()), desc, _entry("pp_adamw_step"), sp)
+        got = _native().adamw(lists, (wt, gt), dev.index if dev.type == "cuda" else -1, state._dims, table, decay,
+                              state.elements, (*state._buffers(), *state_out._buffers()), desc, _entry("pp_adamw_step"), sp)
     if got:
         if got >= 10:
             for s in (state, state_out):

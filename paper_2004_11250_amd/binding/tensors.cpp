@@ -1,16 +1,18 @@
 // tensors.cpp -- calls of the binding whose checks cost Python more than the kernels
 // take: lists of tensors (half a microsecond a tensor and check), and single tokens.
 //
-// Addresses of the library's functions and of memory come as numbers.  A list "fits"
-// if its tensors are contiguous, of the dtype and on the device that is asked for, and,
-// where dims is not 0, of the sizes there (of each tensor how many, and the sizes).
+// Addresses of the library's functions come as numbers, tables as buffers of int64.  A
+// list "fits" if its tensors are contiguous, of the dtype and on the device that is
+// asked for, and, where dims is given, of the sizes there (of each tensor how many, and
+// the sizes).
 //
 // adamw(lists, dtypes, device, dims, table, weight_decay, elements, buffers, desc, fn,
 //       stream) -> int
 //     lists: weights, grads, new weights, copies and tap masks (None: weights; none;
-//     none, as may be one of the masks), of the table's length.  table: rows of pp_adamw_tensor (weight_decay: of all, or None:
-//     the rows' own); desc: a pp_adamw_desc without moments; buffers: m, v, m_scale and
-//     v_scale of the state and of the new one, of `elements`; fn: pp_adamw_step.
+//     none, as may be one of the masks), of the table's length.  table: rows of
+//     pp_adamw_tensor (weight_decay: of all, or None: the rows' own); desc: a
+//     pp_adamw_desc without moments; buffers: m, v, m_scale and v_scale of the state
+//     and of the new one, of `elements`; fn: pp_adamw_step.
 //     Counts a change of what was written.  0; 1: two outputs begin at the same
 //     address, 2: an output and a gradient, 3: an output and another tensor's weight;
 //     10 + k: list k does not fit; 20: the buffers do not; 30: device is below 0 (the
@@ -21,13 +23,14 @@
 //     with pp_embed_fwd, of contiguous tensors on one GPU, dtype None: w's
 // embed_bwd(ids, dy, v, dtype, scale, ignore_index, add, workspace_fn, fn, stream)
 //     -> gradient
-//     with pp_embed_workspace and pp_embed_bwd, likewise (add: or None).  Both: None, with nothing
-//     done, where an argument is another than these; a pp_status
+//     with pp_embed_workspace and pp_embed_bwd, likewise (add: or None).  Both: None,
+//     with nothing done, where an argument is another than these; a pp_status
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Dtype.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
@@ -42,6 +45,16 @@
 namespace {
 
 int64_t* words(PyObject* o) { return reinterpret_cast<int64_t*>(PyLong_AsUnsignedLongLong(o)); }
+
+// What a buffer of int64 holds.
+struct Words {
+  Py_buffer b = {};
+  explicit Words(PyObject* o) { PyObject_GetBuffer(o, &b, PyBUF_SIMPLE); }
+  ~Words() { PyBuffer_Release(&b); }
+  Words(const Words&) = delete;
+  const int64_t* begin() const { return static_cast<const int64_t*>(b.buf); }
+  Py_ssize_t size() const { return b.len / 8; }
+};
 
 // The GPU of a number, or the CPU.
 at::Device on(long device) { return device < 0 ? at::Device(at::kCPU) : at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device)); }
@@ -77,6 +90,16 @@ bool gather(PyObject* list, at::ScalarType dtype, at::Device device, const int64
     if (sizes) table[i * stride + 1] = t.numel();
   }
   return true;
+}
+
+// Whether a buffer has the sizes of `count` tensors.
+bool sized(const Words& dims, Py_ssize_t count) {
+  Py_ssize_t at = 0;
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    if (at >= dims.size() || dims.begin()[at] < 0 || dims.begin()[at] > dims.size()) return false;
+    at += 1 + dims.begin()[at];
+  }
+  return at <= dims.size();
 }
 
 // addresses of tap masks to the table: int16, of the first two sizes of a tensor that
@@ -130,12 +153,9 @@ PyObject* refuse(const char* what) {
 // f(), whose C++ exceptions become Python's
 template <class F>
 PyObject* guarded(F&& f) {
-  try {
-    return f();
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
-    return nullptr;
-  }
+  HANDLE_TH_ERRORS
+  return f();
+  END_HANDLE_TH_ERRORS
 }
 
 PyObject* adamw(PyObject*, PyObject* const* arg, Py_ssize_t n) {
@@ -156,15 +176,17 @@ PyObject* adamw(PyObject*, PyObject* const* arg, Py_ssize_t n) {
   }
   dtypes[2] = dtypes[0], dtypes[3] = at::kBFloat16;
   const long device = PyLong_AsLong(arg[2]);
-  const int64_t* dims = words(arg[3]);
-  const auto* rows = reinterpret_cast<const pp_adamw_tensor*>(words(arg[4]));
+  const Words sizes(arg[3]), table_in(arg[4]);
   const double decay = arg[5] == Py_None ? 0. : PyFloat_AsDouble(arg[5]);
   const int64_t elements = PyLong_AsLongLong(arg[6]);
   auto fn = reinterpret_cast<decltype(&pp_adamw_step)>(words(arg[9]));
   void* stream = words(arg[10]);
   if (PyErr_Occurred()) return nullptr;
+  const Py_ssize_t count = PyList_GET_SIZE(lists[0]);
+  if (table_in.size() != kRow * count || !sized(sizes, count)) return refuse("tables of the lists' length");
   return guarded([&]() -> PyObject* {
-    const Py_ssize_t count = PyList_GET_SIZE(lists[0]);
+    const int64_t* dims = sizes.begin();
+    const auto* rows = reinterpret_cast<const pp_adamw_tensor*>(table_in.begin());
     pp_adamw_desc d;
     std::memcpy(&d, PyBytes_AS_STRING(arg[8]), sizeof(d));
     void* at[8] = {};
@@ -187,7 +209,7 @@ PyObject* adamw(PyObject*, PyObject* const* arg, Py_ssize_t n) {
     int64_t* table = reinterpret_cast<int64_t*>(all.data());
     for (int k = 0; k < 4; ++k)
       if (lists[k] != Py_None && !gather(lists[k], dtypes[k], on(device), dims, table + 1 + k, kRow, false)) return PyLong_FromLong(10 + k);
-    if (lists[4] != Py_None && (!dims || !masks(lists[4], on(device), dims, all.data()))) return PyLong_FromLong(14);
+    if (lists[4] != Py_None && !masks(lists[4], on(device), dims, all.data())) return PyLong_FromLong(14);
     for (Py_ssize_t i = 0; i < count; ++i) {
       if (lists[2] == Py_None) table[kRow * i + 3] = table[kRow * i + 1];
       if (arg[5] != Py_None) all[i].weight_decay = decay;

@@ -238,6 +238,29 @@ def test_adamw_tensors():
             pruned(bad)
 
 
+def test_a_state_is_copied_whole():
+    import copy
+    import gc
+    import io
+    w = [torch.zeros(3, 4), torch.zeros(5)]
+
+    def saved(state):
+        at = io.BytesIO()
+        torch.save(state, at)
+        return torch.load(io.BytesIO(at.getvalue()), weights_only=False)
+
+    for again in (copy.deepcopy, saved):
+        state = pp.AdamWState([t.shape for t in w], bits=8, device="cpu")
+        new = again(state)
+        state._dims[:], state._table[:] = -7, -7        # (nothing of the first is looked at any more)
+        del state
+        gc.collect()
+        with refused("GPU"):
+            pp.adamw_step(w, [t.clone() for t in w], new, lr=1e-3, step=1)
+        with refused("shapes"):
+            pp.adamw_step(w[::-1], [t.clone() for t in w], new, lr=1e-3, step=1)
+
+
 def test_norm_tensors():
     with refused("empty"):
         pp.grad_norm([])
@@ -283,16 +306,16 @@ def test_embed_tensors():
 
 def test_outputs_of_their_own():
     x = [torch.zeros(4) for _ in range(8)]
-    table = np.zeros((2, 8), np.int64)
+    table, dims = np.zeros((2, 8), np.int64), np.array([1, 4] * 2, np.int64)
     desc = AdamWDesc(bits=32)
     moments = [torch.zeros(256) for _ in range(2)]
 
     def code(w, g, new=None, copies=None, n=(4, 4)):
         """Of two tensors: indices into x."""
         table[:, 0] = n
-        pick = lambda t, dt=torch.float32: None if t is None else [x[i].view(dt) if dt != torch.float32 else x[i] for i in t]   # noqa: E731
-        return adamw._native().adamw((pick(w), pick(g), pick(new), pick(copies, torch.bfloat16), None), (torch.float32, torch.float32), -1, 0,
-                                     table.ctypes.data, None, 256, (*moments, None, None) * 2, bytes(desc), 1, 0)
+        pick = lambda t, dt=torch.float32: None if t is None else [x[i].view(dt)[:4] for i in t]   # noqa: E731
+        return adamw._native().adamw((pick(w), pick(g), pick(new), pick(copies, torch.bfloat16), None), (torch.float32, torch.float32), -1, dims,
+                                     table, None, 256, (*moments, None, None) * 2, bytes(desc), 1, 0)
 
     assert code((0, 1), (2, 2)) == 30 and code((0, 1), (2, 3), (4, 5)) == 30 and code((0, 1), (2, 3), None, (4, 5)) == 30
     assert code((0, 0), (2, 3)) == 1 and code((0, 0), (2, 3), n=(4, 0)) == 30
@@ -306,15 +329,16 @@ def test_native_calls_take_tensors_on_a_gpu_only():
     t, dims = np.zeros((2, 8), np.int64), np.array([1, 3, 1, 3], np.int64)
     x = [torch.zeros(3), torch.zeros(3)]
     bufs, desc = [torch.zeros(256), torch.zeros(256), None, None], bytes(AdamWDesc(bits=32))
-    go = lambda w=x, g=x, new=None, copies=None, keep=None, dt=(f32, f32), at=-1, b=bufs, d=desc, n=256: lists.adamw(   # noqa: E731
-        (w, g, new, copies, keep), dt, at, dims.ctypes.data, t.ctypes.data, 0.5, n, (*b, *b), d, 1, 0)
+    go = lambda w=x, g=x, new=None, copies=None, keep=None, dt=(f32, f32), at=-1, b=bufs, d=desc, n=256, rows=None, sizes=None: lists.adamw(   # noqa: E731
+        (w, g, new, copies, keep), dt, at, dims if sizes is None else sizes, t if rows is None else rows, 0.5, n, (*b, *b), d, 1, 0)
     assert go() == 30 and not t.any()
     assert go(at=0) == 20 and go(n=128) == 20 and go(b=bufs[:3] + bufs[:1]) == 20 and go(d=bytes(AdamWDesc(bits=8))) == 20
     assert go(b=[torch.zeros(256).bfloat16(), *bufs[1:]]) == 20 and go(b=[torch.zeros(512)[::2], *bufs[1:]]) == 20
     assert go(w=[None, None]) == 10 and go(w=["a", 3]) == 10 and go(g=[x[0], x[1].double()]) == 11 and go(new=[x[0], torch.zeros(4)]) == 12
     assert go(copies=x) == 13 and go(keep=[None, torch.zeros(1, 1, dtype=torch.int16)]) == 14 and go(keep=[None, None]) == 30
     for bad in (dict(w=None), dict(g=x[:1]), dict(new=x[:1]), dict(copies=(1, 2)), dict(keep=[None]), dict(dt=("f", f32)), dict(dt=f32), dict(b=bufs[:3]),
-                dict(d=desc[1:]), dict(d="x"), dict(n=0.5)):
+                dict(d=desc[1:]), dict(d="x"), dict(n=0.5), dict(rows=t[:1]), dict(rows=3), dict(sizes=dims[:3]), dict(sizes=dims[1:]),
+                dict(sizes="x")):
         with pytest.raises(TypeError):
             go(**bad)
     assert lists.grad_norm(x, f32, 0, 1.0, 1, 1, 0) == 10 and lists.grad_norm([3], f32, 0, 1.0, 1, 1, 0) == 10

@@ -134,6 +134,13 @@ def test_same_results_however_called():
     assert torch.equal(pp.embed_fwd(ids, table.requires_grad_(), scale=0.5), y)
 
 
+def test_more_than_the_card_holds():
+    ids = torch.zeros(1 << 20, dtype=torch.int64, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):
+        pp.embed_fwd(ids, torch.zeros(1, 1 << 20, device="cuda"))      # 4 TB
+    assert torch.equal(pp.embed_fwd(ids[:2], torch.ones(1, 3, device="cuda")), torch.ones(2, 3, device="cuda"))
+
+
 @pytest.mark.parametrize("w,y", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("d", [1, 8, 9, 63, 203, 256, 1030, 2056])
 @pytest.mark.parametrize("how", ["uniform", "heavy"])
