@@ -712,18 +712,24 @@ pp_status pp_embed_bwd(const pp_embed_desc* desc, const int64_t* ids, const void
  * element `at` on, a multiple of PP_ADAMW_BLOCK; what follows them up to the next
  * multiple is written as 0, and no other tensor's may lie there.  With 32 bits
  * they are fp32.  With 8 bits each block of PP_ADAMW_BLOCK elements has a scale
- * for each moment, and a code an element:
+ * for each moment, and an element a code for each:
  *   m   e4m3 (OCP, 448 at most), times the block's scale: its largest |m'| / 448
  *   v   c > 0: r = 2^(q / 16 - 127) (1 + (q mod 16) / 16), q = c + 1777 (whole
  *       division: 4 bits of the exponent and 4 after the leading one, c = 255
  *       being 1); c = 0: r = 0; and v = (r times the block's scale)^2, the scale
  *       being the largest sqrt(v')
- * rounded to the nearest, ties to even codes (so that a code stays where a step
- * moves its value by less than half a code, and follows the block's scale, which
- * is not rounded).  A v' above 0 has a code of 1 at
- * least (2^-16 1.125), so that a small second moment is held too large, never as
- * 0.  A scale is at least 2^-100.  W' is taken from m' and v' before they are
- * rounded.  An element whose m' is not finite keeps a NaN as m (the others of its
+ * each the nearest, ties to even codes of m and to even q.  A v' above 0 has a code
+ * of 1 at least (2^-16 1.125), so that a small second moment is held too large,
+ * never as 0.  A scale is not rounded, and at least 2^-100.  W' is taken from m'
+ * and v' before they are rounded.
+ * beta2 near 1 moves v by far less than a code a step.  So an element of v is two
+ * bytes, a half-precision number c + (k mod 8) / 8: its whole part is the code, and
+ * k = -3 .. 3 is what the code leaves out, in sixths of a code (of the one above,
+ * or, k < 0, below); the next step begins from c + k / 6.  What lies between two
+ * sixths is rounded up in as many of the steps as it is beyond the lower one, in an
+ * order that element and step fix: count the steps taken, 1, 2, 3, ...  Codes alone
+ * (k = 0) are a state too.
+ * An element whose m' is not finite keeps a NaN as m (the others of its
  * block are held as if it were not there); a v' above fp32's range is held as
  * its largest value.
  */
@@ -748,7 +754,7 @@ typedef struct {
   const float* d_lr;                   /* device, or NULL: read in place of lr        */
   const int64_t* d_step;               /* device, or NULL: read in place of step (below 1: as 1) */
   const float* d_grad_scale;           /* device, or NULL for 1                       */
-  const void *m, *v;                   /* device: fp32, or 8-bit codes; 16-byte aligned */
+  const void *m, *v;                   /* device: fp32; or 8 bits: bytes, and halves; 16-byte aligned */
   const float *m_scale, *v_scale;      /* device, 8 bits: a value a block             */
   void *m_out, *v_out;                 /* may be m, v                                 */
   float *m_scale_out, *v_scale_out;    /* may be m_scale, v_scale                     */
@@ -761,7 +767,7 @@ typedef struct {
  *   tensors, count  host array (read during the call)
  * Arrays that are written may overlap no other array of the call, but be their
  * own input.
- * pp_adamw_values -- the moments that codes of 8 bits stand for.
+ * pp_adamw_values -- the moments that codes of 8 bits stand for (v: without k).
  *   elements  of the arrays, a multiple of PP_ADAMW_BLOCK
  *   m, v, m_scale, v_scale   as pp_adamw_step left them
  *   m_out, v_out             device [elements] of dtype; either may be NULL

@@ -45,7 +45,9 @@ class AdamWState:
 
     m, v             flat tensors of all moments.  Tensor i's are the elements from
                      ``places[i]`` on (a multiple of 128), 0 up to the next tensor.
-                     float32 with bits=32; with bits=8 codes, float8_e4m3fn and uint8
+                     float32 with bits=32; with bits=8 float8_e4m3fn, and float16
+                     whose whole part is a code of 8 bits and whose fraction what the
+                     code leaves out, in sixths of one (pp.h has the format)
     m_scale, v_scale with bits=8: float32, for each block of 128 codes (else None)
 
     Saving these four and copying them into a new state continues a run.
@@ -80,7 +82,7 @@ class AdamWState:
             self.m, self.v = zeros(4 * at, torch.float32), zeros(4 * at, torch.float32)
             self.m_scale = self.v_scale = None
         else:
-            self.m, self.v = zeros(at, torch.float8_e4m3fn), zeros(at, torch.uint8)
+            self.m, self.v = zeros(at, torch.float8_e4m3fn), zeros(2 * at, torch.float16)
             self.m_scale, self.v_scale = (zeros(4 * (at // BLOCK), torch.float32) for _ in range(2))
 
     def _buffers(self):
@@ -93,7 +95,7 @@ class AdamWState:
         if self.bits == 32:
             want = ((torch.float32, n), (torch.float32, n))
         else:
-            want = ((torch.float8_e4m3fn, n), (torch.uint8, n), (torch.float32, blocks), (torch.float32, blocks))
+            want = ((torch.float8_e4m3fn, n), (torch.float16, n), (torch.float32, blocks), (torch.float32, blocks))
         device = self.m.device
         for t, (dtype, n) in zip(got, want):
             if t.dtype != dtype or t.numel() != n or not t.is_contiguous() or t.device != device:
@@ -106,7 +108,8 @@ class AdamWState:
 
     def values(self, dtype=None, stream=None):
         """pp_adamw_values: the moments (m, v) as flat tensors of ``dtype`` (float32
-        if None, or bfloat16).  With bits=32 and float32 they are the state's own."""
+        if None, or bfloat16): what the codes stand for with bits=8, without their
+        fractions.  With bits=32 and float32 they are the state's own."""
         torch = _torch()
         dtype = torch.float32 if dtype is None else dtype
         if dtype not in (torch.float32, torch.bfloat16):

@@ -198,7 +198,7 @@ PyObject* adamw(PyObject*, PyObject* const* arg, Py_ssize_t n) {
         continue;
       }
       const at::Tensor* t = whole(o, 0, 64);
-      const auto dtype = scale || d.bits == 32 ? at::kFloat : k % 4 ? at::kByte : at::kFloat8_e4m3fn;
+      const auto dtype = scale || d.bits == 32 ? at::kFloat : k % 4 ? at::kHalf : at::kFloat8_e4m3fn;
       if (!t || t->scalar_type() != dtype || t->device() != on(device) || t->numel() != (scale ? elements / PP_ADAMW_BLOCK : elements))
         return PyLong_FromLong(20);
       at[k] = t->data_ptr();

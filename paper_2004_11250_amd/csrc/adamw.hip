@@ -28,7 +28,8 @@ constexpr int kBlock = PP_ADAMW_BLOCK;   // elements that share their scales: 16
 constexpr float kTiny = 0x1p-100f;       // the least scale
 constexpr int kFirstCode = 1777;         // v: code c stands for the float whose bits are (c + 1777) << 19
 
-using Codes = __attribute__((ext_vector_type(2))) uint32_t;
+using half = _Float16;
+using Codes = __attribute__((ext_vector_type(2))) uint32_t;   // of eight first moments
 
 struct Tensor {
   const void* w;
@@ -55,6 +56,7 @@ struct Step {
   void *m_out, *v_out;
   float *ms_out, *vs_out;
   int32_t chunk;                 // elements a workgroup takes
+  uint32_t turn;                 // turn_of(the step), where it is the host's
 };
 static_assert(sizeof(Tensors) + sizeof(Step) <= 4096, "kernel arguments hold 4 KB");
 
@@ -85,14 +87,36 @@ __device__ __forceinline__ void roots(const float (&v)[8], float (&r)[8]) {
   }
 }
 
-// Codes of second moments (square roots over the block's scale): rounded to 4
-// bits after the leading one, and these with the exponent's low 4 bits kept.
-__device__ __forceinline__ uint32_t code_of(float r) {
-  const int bits = __builtin_bit_cast(int, r);
+// Second moments: a root over the block's scale has 4 bits of the exponent and 4 after
+// the leading one, its code c, and between codes it is held to sixths of one: c + k / 6,
+// k = -3 .. 3, is the half c + (k mod 8) / 8, which holds 11 bits.  beta2 near 1 moves a
+// root by far less than half a code a step (at 0.999 by 0.0005 (g^2 / v - 1) of itself; a
+// code is 2^-4 to 2^-5), which codes alone would round away at every step: an element
+// whose gradients grow, shrink or stop beside a steady one would be left where it was.  So
+// what is held is rounded up where the part beyond a sixth is above 1 - u, u being
+// spread evenly over 0..1 by step and element (multiples of the golden section and of
+// another such number, modulo 1): over the steps the roundings add up to nothing.
+// (u at random would do the same with errors of the root of their count.)
+constexpr uint32_t kTurnStep = 0x9e3779b9u, kTurnElement = 0xc13fa9a9u;
+__host__ __device__ inline uint32_t turn_of(int64_t step) { return static_cast<uint32_t>(step) * kTurnStep; }
+
+__device__ __forceinline__ half code_of(float r, uint32_t turn) {
+  const int whole = __builtin_bit_cast(int, r);
+  const int bits = min(max(whole, (kFirstCode + 1) << 19), (kFirstCode + 255) << 19);           // (r = 0: 0, above it 1 at least)
   const int c = (bits + ((bits >> 19) & 1) + (0x3ffff - (kFirstCode << 19))) >> 19;
-  return static_cast<uint32_t>(min(max(c, min(bits, 1)), 255));     // (r = 0: 0, above it 1 at least)
+  const int k = (6 * (bits - ((c + kFirstCode) << 19)) + static_cast<int>(turn >> 13)) >> 19;   // (at most half a code: -3 .. 3)
+  return static_cast<half>(static_cast<uint16_t>(whole ? c << 3 | (k & 7) : 0)) * static_cast<half>(0.125f);
 }
-__device__ __forceinline__ float value_of(uint32_t c) { return __builtin_bit_cast(float, c ? (c + kFirstCode) << 19 : 0u); }
+// What is held, and what its code alone stands for.
+__device__ __forceinline__ float value_of(half held) {
+  const int x = __builtin_bit_cast(int, static_cast<float>(held) + 0x1p20f), c = x & 0x7f8;    // (in eighths)
+  const int k = (x << 29) >> 29;
+  return __builtin_bit_cast(float, c ? (kFirstCode << 19) + (c << 16) + k * 87381 : 0);        // (2^19 / 6)
+}
+__device__ __forceinline__ float code_value(half held) {
+  const int c = static_cast<uint16_t>(held) & 255;
+  return __builtin_bit_cast(float, c ? (c + kFirstCode) << 19 : 0);
+}
 
 __device__ __forceinline__ void m_values(Codes c, float s, float (&m)[8]) {
 #pragma unroll
@@ -102,10 +126,11 @@ __device__ __forceinline__ void m_values(Codes c, float s, float (&m)[8]) {
     m[4 * h] = a[0] * s, m[4 * h + 1] = a[1] * s, m[4 * h + 2] = b[0] * s, m[4 * h + 3] = b[1] * s;
   }
 }
-__device__ __forceinline__ void v_values(Codes c, float s, float (&v)[8]) {
+template <class F>
+__device__ __forceinline__ void v_values(const Eight<half>& held, float s, float (&v)[8], F&& value) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const float r = value_of(((e < 4 ? c.x : c.y) >> (8 * (e & 3))) & 255u) * s;
+    const float r = value(held[e]) * s;
     v[e] = r * r;
   }
 }
@@ -175,9 +200,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
   const double lr = s.d_lr ? static_cast<double>(*s.d_lr) : s.lr;
   double c1 = s.c1;
   float c2 = s.c2;
+  uint32_t turn = s.turn;
   if (s.d_step) {
-    const int64_t step = *s.d_step;
-    const double k = static_cast<double>(step > 1 ? step : 1);
+    const int64_t step = max(*s.d_step, int64_t(1));
+    const double k = static_cast<double>(step);
+    turn = turn_of(step);
     c1 = -1. / expm1(k * s.ln1);
     c2 = static_cast<float>(1. / sqrt(-expm1(k * s.ln2)));
   }
@@ -186,7 +213,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
   for (int x = SPLIT ? 4 * (threadIdx.x & 15) + kBlock * (threadIdx.x >> 4) : 8 * threadIdx.x; x < len; x += 2048) {
     const int64_t there = left - x;     // elements from here on
     float w[8], g[8], m[8], v[8];
-    Codes mc, vc;
+    Codes mc;
+    Eight<half> held;
     float ms, vs;
     load8<SPLIT, ONCE>(w_in + x, there, kFar, w);
     load8<SPLIT, ONCE>(g_in + x, there, kFar, g);
@@ -195,12 +223,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       load8<SPLIT, ONCE>(static_cast<const float*>(s.v) + at + x, kBlock, kFar, v);
     } else {
       mc = codes<SPLIT, ONCE>(s.m, at + x);
-      vc = codes<SPLIT, ONCE>(s.v, at + x);
+      held = get8<SPLIT, ONCE>(static_cast<const half*>(s.v) + at + x, kBlock, kFar);
       ms = s.ms[block + x / kBlock], vs = s.vs[block + x / kBlock];
     }
     const uint32_t on = !keep ? 255u : SPLIT ? (kept8(keep, cell, tap, cells, x) & 15u) | kept8(keep, cell, tap, cells, x + kFar) << 4 : kept8(keep, cell, tap, cells, x);
     if (go) {
-      if constexpr (BITS == 8) m_values(mc, ms, m), v_values(vc, vs, v);
+      if constexpr (BITS == 8) m_values(mc, ms, m), v_values(held, vs, v, [](half h) { return value_of(h); });
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float ge = scale * g[e];
@@ -247,16 +275,18 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
         ms = fmaxf(row_max(top) * (1.f / 448.f), kTiny);
         vs = fmaxf(row_max(vtop), kTiny);
         const float im = 1.f / ms, iv = 1.f / vs;
-        uint32_t c[4] = {};
+        uint32_t c[2];
+        const uint32_t first = static_cast<uint32_t>(at + x) * kTurnElement + turn;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           int q = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h] * im, m[4 * h + 1] * im, 0, false);
           q = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h + 2] * im, m[4 * h + 3] * im, q, true);
           c[h] = q;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) c[2 + h] |= code_of(r[4 * h + e] * iv) << (8 * e);
+          for (int e = 0; e < 4; ++e)
+            held[4 * h + e] = code_of(r[4 * h + e] * iv, first + static_cast<uint32_t>(h * (SPLIT ? kFar : 4) + e) * kTurnElement);
         }
-        mc = {c[0], c[1]}, vc = {c[2], c[3]};
+        mc = {c[0], c[1]};
       }
     }
     if (there > 0) {
@@ -268,7 +298,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
       store8<SPLIT, ONCE>(static_cast<float*>(s.v_out) + at + x, kBlock, kFar, v);
     } else {
       put_codes<SPLIT, ONCE>(s.m_out, at + x, mc);
-      put_codes<SPLIT, ONCE>(s.v_out, at + x, vc);
+      put8<SPLIT, ONCE>(static_cast<half*>(s.v_out) + at + x, kBlock, kFar, held);
       if (threadIdx.x % 16 == 0) s.ms_out[block + x / kBlock] = ms, s.vs_out[block + x / kBlock] = vs;
     }
   }
@@ -276,7 +306,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
 
 // What codes stand for: 8 elements a lane.  102 M to bf16 103 us, 6 TB/s.
 template <class S>
-__global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const uint8_t* v, const float* ms, const float* vs,
+__global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const half* v, const float* ms, const float* vs,
                                                      int64_t all, S* m_out, S* v_out) {
   constexpr bool SPLIT = kSplit<S>;
   const int lane = SPLIT ? 4 * (threadIdx.x & 15) + kBlock * (threadIdx.x >> 4) : 8 * threadIdx.x;
@@ -287,7 +317,7 @@ __global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const uin
       store8<SPLIT>(m_out + x, kBlock, kFar, a);
     }
     if (v_out) {
-      v_values(codes<SPLIT, false>(v, x), vs[x / kBlock], a);
+      v_values(get8<SPLIT>(v + x, kBlock, kFar), vs[x / kBlock], a, [](half h) { return code_value(h); });
       store8<SPLIT>(v_out + x, kBlock, kFar, a);
     }
   }
@@ -434,6 +464,7 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   if (!d.d_step) {
     s.c1 = -1. / std::expm1(static_cast<double>(d.step) * s.ln1);
     s.c2 = static_cast<float>(1. / std::sqrt(-std::expm1(static_cast<double>(d.step) * s.ln2)));
+    s.turn = turn_of(d.step);
   }
   s.b1 = static_cast<float>(d.beta1), s.n1 = static_cast<float>(1. - d.beta1);
   s.b2 = static_cast<float>(d.beta2), s.n2 = static_cast<float>(1. - d.beta2), s.eps = static_cast<float>(d.eps);
@@ -447,7 +478,7 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   // 74 / 60), 51 M 239 / 267, with 8-bit moments 124 / 135, 102 M bf16 weights with 8-bit
   // moments 172 / 193; 3 M fp32 weights (86 MB) 17.6 / 15.3, 8 M bf16 with 8-bit moments
   // (82 MB) 19.5 / 17.5.
-  const bool past = total * static_cast<double>(2 * size_of(d.w_dtype) + size_of(d.g_dtype) + (d.bits == 8 ? 4 : 16)) > 256e6;
+  const bool past = total * static_cast<double>(2 * size_of(d.w_dtype) + size_of(d.g_dtype) + (d.bits == 8 ? 6 : 16)) > 256e6;
   auto fill = [](Tensor& x, const pp_adamw_tensor& t) {
     x = {t.w, t.g, t.w_out, static_cast<bf16*>(t.copy), t.keep, t.n, t.at, static_cast<float>(t.weight_decay)};
   };
@@ -478,7 +509,7 @@ pp_status values(const void* m, const void* v, const float* ms, const float* vs,
   const dim3 grid(static_cast<uint32_t>(std::min<int64_t>(cdiv(all, 2048), 1 << 20)));
   auto go = [&](auto o) {
     using S = decltype(o);
-    hipLaunchKernelGGL((values_kernel<S>), grid, dim3(256), 0, st, static_cast<const uint8_t*>(m), static_cast<const uint8_t*>(v), ms,
+    hipLaunchKernelGGL((values_kernel<S>), grid, dim3(256), 0, st, static_cast<const uint8_t*>(m), static_cast<const half*>(v), ms,
                        vs, all, static_cast<S*>(m_out), static_cast<S*>(v_out));
   };
   dtype == PP_BF16 ? go(bf16()) : go(float());
