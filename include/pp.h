@@ -691,7 +691,8 @@ typedef struct {
  * Errors: PP_EINVAL (NULL or misaligned pointers, sizes, dtypes, rows closer
  * than d), PP_EUNSUPPORTED (2^30 tokens or rows of the table or more, d of 2^23
  * or more, rows 2^32 elements apart or more; with d above 1024 a lookup of 2^24
- * tokens or more, a gradient of some 2^26 rows or more), PP_ESIZE, PP_EHIP.
+ * tokens or more; a gradient of some 2^26 rows or more with d above 1024, 2^27
+ * from 513 on, 2^28 from 257, 2^29 from 129, 2^30 from 65), PP_ESIZE, PP_EHIP.
  */
 pp_status pp_embed_fwd(const pp_embed_desc* desc, const int64_t* ids, const void* w, void* y, void* hip_stream);
 pp_status pp_embed_workspace(const pp_embed_desc* desc, size_t* bytes);

@@ -906,13 +906,22 @@ pp_status look(const pp_embed_desc* desc, const int64_t* ids, const void* w, voi
   if (!ids || !w || !y) return fail(PP_EINVAL, "NULL pointer");
   if (off(ids, 8) || off(w, size_of(d.w_dtype)) || off(y, size_of(d.y_dtype))) return fail(PP_EINVAL, "misaligned pointer");
   const Lanes l = lanes_for(d.d);
-  if (cdiv(d.t, 256 >> l.log) >= kGrid) return fail(PP_EUNSUPPORTED, "too many tokens of this length");
-  const Look a = {ids, w, y, d.t, d.v, d.w_ld, d.y_ld, d.ignore_index, static_cast<int32_t>(d.d), l.log, d.scale};
-  const dim3 grid(static_cast<uint32_t>(cdiv(d.t, 256 >> l.log)), static_cast<uint32_t>(l.columns));
-  with_types(d.w_dtype, d.y_dtype, [&](auto wt, auto yt) {
-    hipLaunchKernelGGL((look_kernel<decltype(wt), decltype(yt)>), grid, dim3(256), 0, st, a);
-  });
-  return launched();
+  const int64_t per = 256 >> l.log;        // tokens of a workgroup
+  if (per == 1 && d.t >= kGrid) return fail(PP_EUNSUPPORTED, "too many tokens of this length");
+  // (a launch of fewer than kGrid workgroups; nearly always one)
+  const int64_t most = (kGrid - 1) * per;
+  for (int64_t t0 = 0; t0 < d.t; t0 += most) {
+    const int64_t t = std::min(most, d.t - t0);
+    uint8_t* rows = static_cast<uint8_t*>(y) + t0 * d.y_ld * static_cast<int64_t>(size_of(d.y_dtype));
+    const Look a = {ids + t0, w, rows, t, d.v, d.w_ld, d.y_ld, d.ignore_index, static_cast<int32_t>(d.d), l.log, d.scale};
+    const dim3 grid(static_cast<uint32_t>(cdiv(t, per)), static_cast<uint32_t>(l.columns));
+    with_types(d.w_dtype, d.y_dtype, [&](auto wt, auto yt) {
+      hipLaunchKernelGGL((look_kernel<decltype(wt), decltype(yt)>), grid, dim3(256), 0, st, a);
+    });
+    const pp_status s = launched();
+    if (s != PP_OK) return s;
+  }
+  return PP_OK;
 }
 
 pp_status grad(const pp_embed_desc* desc, const int64_t* ids, const void* dy, const void* add, void* dw, void* ws, size_t bytes,

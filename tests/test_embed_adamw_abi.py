@@ -53,6 +53,17 @@ def test_embed_descriptions(lib):
         assert nb.value <= 8 * v + 16 * t + 2048 * 4 * (d + 8) + 4 * 256 * 128 + 4 * 128 * 1024 + 4 * 4096
 
 
+def test_rows_of_a_gradient_are_limited_as_pp_h_says(lib):
+    nb = ctypes.c_size_t(0)
+    status = lambda v, d: lib.pp_embed_workspace(ctypes.byref(desc(v=v, d=d, w_ld=d, y_ld=d)), ctypes.byref(nb))   # noqa: E731
+    for d, most in ((129, 29), (256, 29), (257, 28), (512, 28), (513, 27), (1024, 27), (1025, 26), (5000, 26)):
+        assert status((1 << most) - (1 << most - 13), d) == pp.PP_OK, d          # (1024 of the 2^24 workgroups are left to the tokens)
+        assert status(1 << most, d) == pp.PP_EUNSUPPORTED, d
+    for d in (1, 8, 32, 64, 128):
+        assert status((1 << 30) - 1, d) == (pp.PP_OK if d <= 64 else pp.PP_EUNSUPPORTED), d
+        assert status((1 << 30) - (1 << 17), d) == pp.PP_OK, d
+
+
 def test_embed_calls(lib):
     d = ctypes.byref(desc())
     for i in range(3):

@@ -251,6 +251,19 @@ def test_offsets_past_32_bits():
     check_bwd(pp.embed_bwd(ids[-3:], y[-3:], 2), ids[-3:], y[-3:], 2)
 
 
+def test_lookups_of_more_than_one_launch():
+    # 2^25 - 2 tokens are a launch where two lie in a workgroup
+    t, d = (1 << 25) + 5, 513
+    ids, table = torch.zeros(t, dtype=torch.int64, device="cuda"), normal(1, 3, d, dtype="bf16")
+    ids[-9:] = torch.tensor([1, 2, 0, 1, 2, 2, IGNORE, 1, 2], device="cuda")
+    ids[:3] = torch.tensor([2, IGNORE, 1], device="cuda")
+    y = pp.embed_fwd(ids, table)
+    want = ref_fwd(torch.arange(3, device="cuda"), table, 1.0, torch.bfloat16)
+    assert torch.equal(y[-9:], ref_fwd(ids[-9:], table, 1.0, torch.bfloat16)) and torch.equal(y[:3], ref_fwd(ids[:3], table, 1.0, torch.bfloat16))
+    for part in y[3:-9].split(1 << 21):
+        assert bool((part == want[0]).all())
+
+
 def test_streams_and_graphs():
     t, v, d = 3000, 400, 96
     ids, table, dy = make_ids(1, t, v, "heavy"), normal(2, v, d), normal(3, t, d)
