@@ -47,8 +47,8 @@ class Model:
         return loss, [dtable, dz.t() @ x, dbias]
 
     def update(self, grads, lr):
-        self.step += 1
         _, factor = pp.grad_norm(grads, max_norm=1.0)
+        self.step += torch.isfinite(factor)         # (where it is not, no step is taken, and none counts)
         more = dict(lr=lr, step=self.step, grad_scale=factor)
         pp.adamw_step([self.table], grads[:1], self.table_state, weight_decay=0.01, **more)
         pp.adamw_step([self.w, self.bias], grads[1:], self.state, weight_decay=[0.01, 0.0], **more)

@@ -764,7 +764,8 @@ typedef struct {
 /*
  * pp_adamw_step -- one step of a list.  Where *d_grad_scale is not finite
  * (pp_grad_norm of gradients that are not) no step is taken: what is written is
- * what was read.
+ * what was read.  Such a call is none of the steps that `step` counts: the bias
+ * corrections go by how often the moments were updated.
  *   tensors, count  host array (read during the call)
  * Arrays that are written may overlap no other array of the call, but be their
  * own input.

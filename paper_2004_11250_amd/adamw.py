@@ -162,7 +162,8 @@ def adamw_step(weights, grads, state, lr, step, betas=(0.9, 0.999), eps=1e-8, we
     a pruned 3x3 layer (keep_masks); ``copies``: bfloat16 tensors that get the new
     weights, rounded.  ``lr``, ``step`` and ``grad_scale`` (that ``grad_norm``
     returns) may be tensors of one float32, int64 and float32 on the GPU.  Where
-    grad_scale is not finite no step is taken.
+    grad_scale is not finite no step is taken, and ``step`` must not count it: a
+    count on the GPU goes on by ``torch.isfinite(grad_scale)``.
 
     Updates weights and state in place, or fills ``out`` = (weights, state), and
     returns them."""

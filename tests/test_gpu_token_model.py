@@ -102,6 +102,37 @@ def test_two_graphs():
             assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
 
 
+def test_a_step_that_is_left_out_does_not_count():
+    # first, between others, and in a recorded step: what follows is as if it had not been
+    for graph in (False, True):
+        models = [ex.Model(11), ex.Model(11)]
+        data = [ex.batch(k) for k in range(4)]
+        bad = torch.zeros((), device="cuda")
+
+        def step(m, ids, target):
+            _, grads = m.gradients(ids, target)
+            grads[2] += bad
+            m.update(grads, 1e-3)
+
+        ids, target = (t.clone() for t in data[0])
+        if graph:
+            recorded = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(recorded):
+                step(models[0], ids, target)
+        taken = 0
+        for k, wrong in enumerate((float("nan"), 0.0, float("inf"), 0.0)):
+            bad.fill_(wrong)
+            ids.copy_(data[k][0])
+            target.copy_(data[k][1])
+            recorded.replay() if graph else step(models[0], ids, target)
+            if not wrong:
+                taken += 1
+                step(models[1], *data[k])
+            assert int(models[0].step) == int(models[1].step) == taken
+            for x, y in zip(state_of(models[0]), state_of(models[1])):
+                assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), k
+
+
 def test_a_step_that_is_not_finite_is_left_out():
     m = ex.Model(9)
     ids, target = ex.batch(10)
