@@ -97,16 +97,28 @@ def build(verbose: bool = False) -> str:
     return LIB
 
 
-def build_tensors() -> str:
-    """The binding's Python module of calls with native checks (g++, torch's headers;
-    the library itself knows nothing of torch)."""
+def build_tensors():
+    """The binding's Python module of calls with native checks (torch's and Python's
+    headers; the library itself knows nothing of either).  Where those are missing it
+    is left out with a note, and None: the library is whole without it, and the calls
+    that need the module say that it is not built."""
     import sysconfig
 
-    import torch
+    headers = sysconfig.get_paths()["include"]
+    try:
+        import torch
+        missing = None if os.path.exists(os.path.join(headers, "Python.h")) else f"{headers}/Python.h"
+    except ImportError:
+        missing = "torch"
+    if missing:
+        if os.path.exists(TENSORS_LIB):
+            os.remove(TENSORS_LIB)      # (of other sources, perhaps)
+        print(f"{os.path.basename(TENSORS_LIB)} is not built: no {missing}", file=sys.stderr)
+        return None
     at = os.path.dirname(torch.__file__)
     tmp = TENSORS_LIB + ".tmp"
-    _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-I{at}/include", f"-I{at}/include/torch/csrc/api/include",
-          f"-I{sysconfig.get_paths()['include']}", f"-I{INCLUDE}", os.path.join(PKG, "binding", "tensors.cpp"), "-o", tmp,
+    _run([HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-I{at}/include", f"-I{at}/include/torch/csrc/api/include",
+          f"-I{headers}", f"-I{INCLUDE}", os.path.join(PKG, "binding", "tensors.cpp"), "-o", tmp,
           f"-L{at}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"])
     os.replace(tmp, TENSORS_LIB)
     return TENSORS_LIB
