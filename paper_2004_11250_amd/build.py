@@ -117,7 +117,7 @@ def build_tensors():
         return None
     at = os.path.dirname(torch.__file__)
     tmp = TENSORS_LIB + ".tmp"
-    _run([HIPCC, "-x", "c++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-I{at}/include", f"-I{at}/include/torch/csrc/api/include",
+    _run([HIPCC, "-x", "c++", "-no-hip-rt", "-O2", "-std=c++17", "-fPIC", "-shared", f"-I{at}/include", f"-I{at}/include/torch/csrc/api/include",
           f"-I{headers}", f"-I{INCLUDE}", os.path.join(PKG, "binding", "tensors.cpp"), "-o", tmp,
           f"-L{at}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"])
     os.replace(tmp, TENSORS_LIB)
