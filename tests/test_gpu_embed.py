@@ -177,6 +177,30 @@ def test_sorts(v, t):
     assert same(got, pp.embed_bwd(ids, dy, v, ignore_index=v // 2, add=add, out=add))
 
 
+@pytest.mark.parametrize("t,v", [(1024, 300), (16384, 1024), (16385, 1024), (65535, 5000), (65536, 5000), (100003, 313), (200003, 313),
+                                 (200003, 1025), (200003, 65537), (200003, (1 << 20) + 1), (70001, 3000001), (200003, 1)])
+@pytest.mark.parametrize("how", ["one", "heavy", "two"])
+@pytest.mark.parametrize("d", [5, 64, 200])
+def test_long_rows_exactly(t, v, how, d):
+    """Of whole numbers of at most 8, whose sums of up to 2^21 are exact in any order, in every sort: a row that all, or half of
+    all tokens share, and two such rows beside each other."""
+    if how == "two":
+        ids = make_ids(t + v, t, v, "uniform")
+        half = torch.rand(t, generator=rng(t), device="cuda")
+        ids = torch.where(half < 0.4, v // 2, torch.where(half < 0.8, min(v // 2 + 1, v - 1), ids))
+    else:
+        ids = make_ids(t + v, t, v, how)
+    ids = torch.where(torch.rand(t, generator=rng(v), device="cuda") < 0.1, torch.full_like(ids, IGNORE), ids)
+    dy = torch.randint(-8, 9, (t, d), generator=rng(d), device="cuda").float()
+    live = ids != IGNORE
+    want = torch.zeros(v, d, device="cuda").index_add_(0, ids[live], dy[live])
+    assert torch.equal(pp.embed_bwd(ids, dy, v), want)
+    assert torch.equal(pp.embed_bwd(ids, dy.bfloat16(), v, dtype=torch.float32), want)
+    base = torch.randint(-8, 9, (v, d), generator=rng(1), device="cuda").float()
+    want += base
+    assert torch.equal(pp.embed_bwd(ids, dy, v, add=base, out=base), want)
+
+
 @pytest.mark.parametrize("y", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [1, 8, 16, 31, 32, 64, 128, 203, 256, 512, 1024])
 @pytest.mark.parametrize("t", [900, 6000, 40000])
