@@ -55,7 +55,6 @@ struct Step {
   const float *ms, *vs;
   void *m_out, *v_out;
   float *ms_out, *vs_out;
-  int32_t chunk;                 // elements a workgroup takes
   uint32_t turn;                 // turn_of(the step), where it is the host's
 };
 static_assert(sizeof(Tensors) + sizeof(Step) <= 4096, "kernel arguments hold 4 KB");
@@ -146,6 +145,7 @@ __device__ __forceinline__ uint32_t kept8(const uint16_t* keep, int64_t cell, in
   return bits >> (y - 9u * k);
 }
 
+constexpr int kChunk = 2048;       // elements of a workgroup of AdamW
 constexpr int kFar = kBlock / 2;   // (the second half of a lane's elements, where they are two fours)
 template <bool SPLIT, bool ONCE>
 __device__ __forceinline__ Codes codes(const void* p, int64_t at) {
@@ -164,28 +164,28 @@ __device__ __forceinline__ void put_codes(void* p, int64_t at, Codes c) {
     keep_at<ONCE>(reinterpret_cast<Codes*>(q), c);
 }
 
-// Eight elements a lane, a chunk of one tensor a workgroup; a block's scales are the
+// Eight elements a lane, 2048 of one tensor a workgroup; a block's scales are the
 // largest of 16 lanes.  Three states in turn, us a step in place / into other arrays:
-// fp32 w, g and moments, VGG-16, 15 M weights 75 / 75 (5.5 TB/s), 51 M 239 / 238
-// (6.0 TB/s); bf16 w and g, 8-bit moments, 102 M 172 / 172 (6.0 TB/s); fp32 w, bf16 g
-// and copies, 8-bit moments, 31 M 98 / 94 (5.3 TB/s).
+// fp32 w, g and moments, VGG-16, 15 M weights 69 / 70 (6.0 TB/s), 51 M 239 / 236
+// (6.1 TB/s); bf16 w and g, 8-bit moments, 102 M 209 / 199 (6.2 TB/s); fp32 w, bf16 g
+// and copies, 8-bit moments, 31 M 104 / 104 (5.4 TB/s).
 // Where a value has four bytes a lane's eight are two fours 64 elements apart, so that
 // each access of 16 lanes is 256 bytes in a row (eight in a row are two accesses of half
 // of each line: 51 M fp32 weights 263, and past the caches 362).
-// Elements of a workgroup, 2048 / 4096 / 8192: fp32 w, 32 bits, 51 M 237 / 247 / -, 8 bits
-// 124 / 131 / 139; bf16 w and g, 8 bits, 102 M 178 / 172 / 193.
-// With 8 bits some 45 instructions an element stand beside 10 bytes of memory, and count:
-// one root serves the update and the code, what only some steps need (masks: 181 without
+// Elements of a workgroup, 2048 / 4096 / 8192: fp32 w, 32 bits, 51 M 236 / 248 / 252, 8 bits
+// 150 / 160 / 164; bf16 w and g, 8 bits, 102 M 207 / 214 / 228 (199 without a loop).
+// With 8 bits some 60 instructions an element stand beside 12 bytes of memory, and count:
+// one root serves the update and the code, what only some steps need (masks: 202 without
 // the test; a tensor's end, values that are not finite, roots below the normal range) is
 // looked for by eight elements together, and the update's division is a product with the
-// hardware's reciprocal, 1 ulp (102 M, an exact one: 183 / 178).
+// hardware's reciprocal, 1 ulp (102 M, an exact one: 209 / 199).
 template <class W, class G, int BITS, bool ONCE>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const Step s) {
   constexpr bool SPLIT = kSplit<W, G> || BITS == 32;
   int chunk;
   const Tensor& t = list.item[find(list, blockIdx.x, &chunk)];
-  const int64_t e0 = static_cast<int64_t>(chunk) * s.chunk, n = t.n, left = n - e0;
-  const int len = static_cast<int>(left < s.chunk ? (left + kBlock - 1) / kBlock * kBlock : s.chunk);
+  const int64_t e0 = static_cast<int64_t>(chunk) * kChunk, n = t.n, left = n - e0;
+  const int len = static_cast<int>(left < kChunk ? (left + kBlock - 1) / kBlock * kBlock : kChunk);
   const W* w_in = static_cast<const W*>(t.w) + e0;
   const G* g_in = static_cast<const G*>(t.g) + e0;
   W* w_out = static_cast<W*>(t.w_out) + e0;
@@ -210,101 +210,101 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors list, const St
   }
   const float rate = static_cast<float>(lr * c1), decay = static_cast<float>(1. - lr * static_cast<double>(t.decay));
 
-  for (int x = SPLIT ? 4 * (threadIdx.x & 15) + kBlock * (threadIdx.x >> 4) : 8 * threadIdx.x; x < len; x += 2048) {
-    const int64_t there = left - x;     // elements from here on
-    float w[8], g[8], m[8], v[8];
-    Codes mc;
-    Eight<half> held;
-    float ms, vs;
-    load8<SPLIT, ONCE>(w_in + x, there, kFar, w);
-    load8<SPLIT, ONCE>(g_in + x, there, kFar, g);
-    if constexpr (BITS == 32) {
-      load8<SPLIT, ONCE>(static_cast<const float*>(s.m) + at + x, kBlock, kFar, m);
-      load8<SPLIT, ONCE>(static_cast<const float*>(s.v) + at + x, kBlock, kFar, v);
-    } else {
-      mc = codes<SPLIT, ONCE>(s.m, at + x);
-      held = get8<SPLIT, ONCE>(static_cast<const half*>(s.v) + at + x, kBlock, kFar);
-      ms = s.ms[block + x / kBlock], vs = s.vs[block + x / kBlock];
+  const int x = SPLIT ? 4 * (threadIdx.x & 15) + kBlock * (threadIdx.x >> 4) : 8 * threadIdx.x;
+  if (x >= len) return;            // (whole blocks: rows of 16 lanes)
+  const int64_t there = left - x;     // elements from here on
+  float w[8], g[8], m[8], v[8];
+  Codes mc;
+  Eight<half> held;
+  float ms, vs;
+  load8<SPLIT, ONCE>(w_in + x, there, kFar, w);
+  load8<SPLIT, ONCE>(g_in + x, there, kFar, g);
+  if constexpr (BITS == 32) {
+    load8<SPLIT, ONCE>(static_cast<const float*>(s.m) + at + x, kBlock, kFar, m);
+    load8<SPLIT, ONCE>(static_cast<const float*>(s.v) + at + x, kBlock, kFar, v);
+  } else {
+    mc = codes<SPLIT, ONCE>(s.m, at + x);
+    held = get8<SPLIT, ONCE>(static_cast<const half*>(s.v) + at + x, kBlock, kFar);
+    ms = s.ms[block + x / kBlock], vs = s.vs[block + x / kBlock];
+  }
+  const uint32_t on = !keep ? 255u : SPLIT ? (kept8(keep, cell, tap, cells, x) & 15u) | kept8(keep, cell, tap, cells, x + kFar) << 4 : kept8(keep, cell, tap, cells, x);
+  if (go) {
+    if constexpr (BITS == 8) m_values(mc, ms, m), v_values(held, vs, v, [](half h) { return value_of(h); });
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float ge = scale * g[e];
+      m[e] = s.b1 * m[e] + s.n1 * ge;
+      v[e] = s.b2 * v[e] + s.n2 * (ge * ge);
     }
-    const uint32_t on = !keep ? 255u : SPLIT ? (kept8(keep, cell, tap, cells, x) & 15u) | kept8(keep, cell, tap, cells, x + kFar) << 4 : kept8(keep, cell, tap, cells, x);
-    if (go) {
-      if constexpr (BITS == 8) m_values(mc, ms, m), v_values(held, vs, v, [](half h) { return value_of(h); });
+    if (keep) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (!(on >> e & 1)) m[e] = v[e] = 0.f;
+    }
+    if (there < (SPLIT ? kFar + 4 : 8)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if ((SPLIT && e >= 4 ? e - 4 + kFar : e) >= there) m[e] = v[e] = 0.f;
+    }
+    float r[8];
+    roots(v, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = decay * w[e] - rate * m[e] * __builtin_amdgcn_rcpf(r[e] * c2 + s.eps);
+    if (keep) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = on >> e & 1 ? w[e] : 0.f;
+    }
+    if constexpr (BITS == 8) {
+      float top = 0.f, vtop = 0.f, odd = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float ge = scale * g[e];
-        m[e] = s.b1 * m[e] + s.n1 * ge;
-        v[e] = s.b2 * v[e] + s.n2 * (ge * ge);
+        top = fmaxf(top, fabsf(m[e]));
+        vtop = fmaxf(vtop, r[e]);
+        odd += 0.f * m[e];              // NaN, if one is not finite
       }
-      if (keep) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (!(on >> e & 1)) m[e] = v[e] = 0.f;
-      }
-      if (there < (SPLIT ? kFar + 4 : 8)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if ((SPLIT && e >= 4 ? e - 4 + kFar : e) >= there) m[e] = v[e] = 0.f;
-      }
-      float r[8];
-      roots(v, r);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = decay * w[e] - rate * m[e] * __builtin_amdgcn_rcpf(r[e] * c2 + s.eps);
-      if (keep) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = on >> e & 1 ? w[e] : 0.f;
-      }
-      if constexpr (BITS == 8) {
-        float top = 0.f, vtop = 0.f, odd = 0.f;
+      if (!(odd == 0.f && vtop < INFINITY)) {
+        top = vtop = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          top = fmaxf(top, fabsf(m[e]));
+          const bool fine = fabsf(m[e]) < INFINITY;
+          r[e] = fine ? fminf(r[e], 0x1.fffffep63f) : 0.f;       // (the root of fp32's largest value)
+          m[e] = fine ? m[e] : __builtin_nanf("");
+          top = fmaxf(top, fine ? fabsf(m[e]) : 0.f);
           vtop = fmaxf(vtop, r[e]);
-          odd += 0.f * m[e];              // NaN, if one is not finite
         }
-        if (!(odd == 0.f && vtop < INFINITY)) {
-          top = vtop = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool fine = fabsf(m[e]) < INFINITY;
-            r[e] = fine ? fminf(r[e], 0x1.fffffep63f) : 0.f;       // (the root of fp32's largest value)
-            m[e] = fine ? m[e] : __builtin_nanf("");
-            top = fmaxf(top, fine ? fabsf(m[e]) : 0.f);
-            vtop = fmaxf(vtop, r[e]);
-          }
-        }
-        ms = fmaxf(row_max(top) * (1.f / 448.f), kTiny);
-        vs = fmaxf(row_max(vtop), kTiny);
-        const float im = 1.f / ms, iv = 1.f / vs;
-        uint32_t c[2];
-        const uint32_t first = static_cast<uint32_t>(at + x) * kTurnElement + turn;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          int q = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h] * im, m[4 * h + 1] * im, 0, false);
-          q = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h + 2] * im, m[4 * h + 3] * im, q, true);
-          c[h] = q;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            held[4 * h + e] = code_of(r[4 * h + e] * iv, first + static_cast<uint32_t>(h * (SPLIT ? kFar : 4) + e) * kTurnElement);
-        }
-        mc = {c[0], c[1]};
       }
+      ms = fmaxf(row_max(top) * (1.f / 448.f), kTiny);
+      vs = fmaxf(row_max(vtop), kTiny);
+      const float im = 1.f / ms, iv = 1.f / vs;
+      uint32_t c[2];
+      const uint32_t first = static_cast<uint32_t>(at + x) * kTurnElement + turn;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int q = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h] * im, m[4 * h + 1] * im, 0, false);
+        q = __builtin_amdgcn_cvt_pk_fp8_f32(m[4 * h + 2] * im, m[4 * h + 3] * im, q, true);
+        c[h] = q;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          held[4 * h + e] = code_of(r[4 * h + e] * iv, first + static_cast<uint32_t>(h * (SPLIT ? kFar : 4) + e) * kTurnElement);
+      }
+      mc = {c[0], c[1]};
     }
-    if (there > 0) {
-      store8<SPLIT, ONCE>(w_out + x, there, kFar, w);
-      if (copy) store8<SPLIT, ONCE>(copy + x, there, kFar, w);
-    }
-    if constexpr (BITS == 32) {
-      store8<SPLIT, ONCE>(static_cast<float*>(s.m_out) + at + x, kBlock, kFar, m);
-      store8<SPLIT, ONCE>(static_cast<float*>(s.v_out) + at + x, kBlock, kFar, v);
-    } else {
-      put_codes<SPLIT, ONCE>(s.m_out, at + x, mc);
-      put8<SPLIT, ONCE>(static_cast<half*>(s.v_out) + at + x, kBlock, kFar, held);
-      if (threadIdx.x % 16 == 0) s.ms_out[block + x / kBlock] = ms, s.vs_out[block + x / kBlock] = vs;
-    }
+  }
+  if (there > 0) {
+    store8<SPLIT, ONCE>(w_out + x, there, kFar, w);
+    if (copy) store8<SPLIT, ONCE>(copy + x, there, kFar, w);
+  }
+  if constexpr (BITS == 32) {
+    store8<SPLIT, ONCE>(static_cast<float*>(s.m_out) + at + x, kBlock, kFar, m);
+    store8<SPLIT, ONCE>(static_cast<float*>(s.v_out) + at + x, kBlock, kFar, v);
+  } else {
+    put_codes<SPLIT, ONCE>(s.m_out, at + x, mc);
+    put8<SPLIT, ONCE>(static_cast<half*>(s.v_out) + at + x, kBlock, kFar, held);
+    if (threadIdx.x % 16 == 0) s.ms_out[block + x / kBlock] = ms, s.vs_out[block + x / kBlock] = vs;
   }
 }
 
-// What codes stand for: 8 elements a lane.  102 M to bf16 103 us, 6 TB/s.
+// What codes stand for: 8 elements a lane.  102 M to bf16 119 us, 6 TB/s.
 template <class S>
 __global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const half* v, const float* ms, const float* vs,
                                                      int64_t all, S* m_out, S* v_out) {
@@ -361,9 +361,11 @@ __global__ __launch_bounds__(256) void square_kernel(const List<Grad, N> list, i
   if (threadIdx.x == 0) part[blockIdx.x] = all;
 }
 
-// The norm of up to 2048 sums, or more where there are more than 30 M elements, and the
-// factor: 2 to 4 us, the launch.  (In a launch of its own: the first launch's last
-// workgroup could do it, but would need a counter that something has cleared.)
+// The norm of all chunks' sums (one at least of each tensor that is not empty; a chunk has
+// 2048 elements, more where there are more than 2 M in all, 16384 from 15 M on), and the
+// factor: 2 to 4 us, the launch.  (The first launch's last workgroup could do it, with a
+// counter that something has cleared; a list so short that one workgroup reads it all
+// would need no second launch, but has one here too.)
 __global__ __launch_bounds__(1024) void norm_kernel(const double* part, int64_t parts, float most, float* out) {
   __shared__ double sums[16];
   double x = 0.;
@@ -384,14 +386,16 @@ size_t size_of(int32_t dtype) { return dtype == PP_BF16 ? 2 : 4; }
 bool known(int32_t dtype) { return dtype == PP_F32 || dtype == PP_BF16; }
 constexpr int64_t kMost = int64_t(1) << 34;   // (a launch has fewer than 2^32 threads, eight elements each at least)
 
-// Elements a workgroup takes: enough workgroups for the card where there is
+// Elements that a workgroup sums: enough workgroups for the card where there is
 // little to do, long ones where there is much.
 int32_t chunk_of(int64_t total, int64_t most) {
   return static_cast<int32_t>(std::min<int64_t>(most, std::max<int64_t>(1, cdiv(total, 2048 * 4 * kCUs)) * 2048));
 }
 
-// f(count) for each launch of a list: tensors of `per` elements a workgroup each,
-// up to N of them.  add(item, i): fills in item i of the list.
+// The launches of a list: up to N tensors each that are not empty, a workgroup for every
+// `per` elements of one.  fill(item, tensor) makes an item of the list, go(list, blocks)
+// launches it.  (Lists of equal length, where one does not hold all: 72 tensors of 31 M
+// elements 103.6 us a step in place of 103.0, norms of 250 tensors of 300000 58 of 54.)
 template <class L, class T, class Fill, class Go>
 pp_status each_launch(const T* tensors, int32_t count, int64_t per, Fill&& fill, Go&& go) {
   constexpr int N = sizeof(L::first) / 4;
@@ -471,13 +475,11 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   s.d_lr = d.d_lr, s.d_step = d.d_step, s.d_scale = d.d_grad_scale;
   s.m = d.m, s.v = d.v, s.ms = d.m_scale, s.vs = d.v_scale;
   s.m_out = d.m_out, s.v_out = d.v_out, s.ms_out = d.m_scale_out, s.vs_out = d.v_scale_out;
-  const bool narrow = d.bits == 8 && d.w_dtype == PP_BF16 && d.g_dtype == PP_BF16;
-  s.chunk = chunk_of(total, narrow ? 4096 : 2048);
   // Steps of more than the last cache holds (256 MB) go past the caches.  us, past them /
-  // not, three states in turn in place: 15 M fp32 weights 75 / 85 (one again and again:
-  // 74 / 60), 51 M 239 / 267, with 8-bit moments 124 / 135, 102 M bf16 weights with 8-bit
-  // moments 172 / 193; 3 M fp32 weights (86 MB) 17.6 / 15.3, 8 M bf16 with 8-bit moments
-  // (82 MB) 19.5 / 17.5.
+  // not, three states in turn in place: 15 M fp32 weights 69 / 79 (one again and again:
+  // 74 / 60), 51 M 239 / 266, with 8-bit moments 150 / 173, 102 M bf16 weights with 8-bit
+  // moments 209 / 236; 3 M fp32 weights (86 MB) 16.4 / 14.4, 8 M bf16 with 8-bit moments
+  // (98 MB) 21.8 / 20.7.
   const bool past = total * static_cast<double>(2 * size_of(d.w_dtype) + size_of(d.g_dtype) + (d.bits == 8 ? 6 : 16)) > 256e6;
   auto fill = [](Tensor& x, const pp_adamw_tensor& t) {
     x = {t.w, t.g, t.w_out, static_cast<bf16*>(t.copy), t.keep, t.n, t.at, static_cast<float>(t.weight_decay)};
@@ -485,7 +487,7 @@ pp_status adamw(const pp_adamw_tensor* tensors, int32_t count, const pp_adamw_de
   auto launch = [&](auto w, auto g, auto bits) {
     using W = decltype(w);
     using G = decltype(g);
-    return each_launch<Tensors>(tensors, count, s.chunk, fill, [&](const Tensors& list, uint32_t blocks) {
+    return each_launch<Tensors>(tensors, count, kChunk, fill, [&](const Tensors& list, uint32_t blocks) {
       if (past)
         hipLaunchKernelGGL((adamw_kernel<W, G, decltype(bits)::value, true>), dim3(blocks), dim3(256), 0, st, list, s);
       else
